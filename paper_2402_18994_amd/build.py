@@ -26,6 +26,9 @@ UNITS = {"snn_api.hip": ["-Xarch_device", "-falign-functions=1024"],
          "layer_reverse.hip": ["-Xarch_device", "-falign-functions=4096"],
          "layer_reverse_wide.hip": ["-Xarch_device", "-falign-functions=1024"],
          "rlif_wide.hip": [],
+         "seq_conv.hip": [],
+         "seq_scan.hip": [],
+         "adamw.hip": [],
          # results of MFMAs in ordinary vector registers (the time loops read them at once)
          "rlif_pair.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "rlif_tile.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}

@@ -1,0 +1,839 @@
+// Selective scan (include/snn_ops.h): N leaky states per channel, whose decay and input gain follow the data,
+//   delta = softplus(dt + dt_bias),  h[t,n] = a[t,n] h[t-1,n] + delta x Bv[n],  a[t,n] = exp(delta A[n]),
+//   y = (sum_n Cv[n] h[t,n] + skip x) z sigmoid(z).
+//
+// Layout of the work.  A lane holds NS = 4 states of a channel; L = 1, 2, 4, 8 or 16 neighbouring lanes hold all of
+// them (N <= 4 L, states beyond N are zero), so a wavefront carries 64 / L channels, and the state never leaves the
+// registers.  Time goes in tiles of 16 steps: for a tile the 64 lanes first do what is once per (step, channel) -
+// loads, softplus, the products delta and delta x - spread evenly, and put it into LDS; then every lane steps through
+// the tile, reading its channel's (delta, delta x) and its four values of Bv and Cv as broadcasts; outputs go back
+// through LDS and leave in the first mapping.  Holding only four states a lane costs LDS reads, but gives four times
+// the wavefronts at N = 16 without computing anything twice.
+//
+// Where sequences and channels are too few to fill the chip, time is cut into chunks as well: the state after a chunk
+// is exp(A sum(delta)) times the state before it plus the chunk's own, so a first launch runs every chunk from zero
+// (scan_local_kernel), a second joins them in order (scan_join_kernel), and the third scans with the right states.
+// The reverse pass is cut the same way, from the other end.
+#include "seq_common.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace snn {
+namespace {
+
+constexpr int TILE = 16;
+constexpr int NS = 4;
+
+struct ScanP {
+  int T, B, D, N, G, softplus;
+  int chunk, nchunks;                // steps per chunk (a multiple of TILE), chunks
+  int blocks;                        // workgroups per (chunk, sequence, group)
+  Rows<void> x, dt, z, bv, cv, y;
+  const float *A, *skip, *dt_bias, *init;
+  const int32_t *lengths;
+  float *state;
+  float4 *saved;                     // [tile][B][D][L]: the state before every tile, or NULL
+  float4 *local;                     // [chunk][B][D][L]: of the chunks from zero, then (joined) the states before them
+  float *sums;                       // [chunk][B][D]: sum of delta
+  explicit ScanP(const snn_scan_args &a)
+      : T(a.T), B(a.B), D(a.D), N(a.N), G(a.groups), softplus(a.softplus), chunk(TILE), nchunks(1), blocks(1), x(a.x), dt(a.dt),
+        z(a.z), bv(a.bv), cv(a.cv), y(a.y), A(a.A), skip(a.skip), dt_bias(a.dt_bias), init(a.init), lengths(a.lengths),
+        state(a.state), saved(nullptr), local(nullptr), sums(nullptr) {}
+};
+
+struct ScanGradP {
+  Rows<void> dy, dx, ddt, dz;
+  const float *d_state;
+  float *dinit;
+  float4 *dA;                        // [chunk * B][D][L] partial sums
+  float *dsum;                       // [chunk * B][2][D]: of dskip and ddt_bias
+  float *dbc;                        // [blocks][T][B][G][2][4 L] partial sums of dBv and dCv
+  explicit ScanGradP(const snn_scan_grads &g)
+      : dy(g.dy), dx(g.dx), ddt(g.ddt), dz(g.dz), d_state(g.d_state), dinit(g.dinit), dA(nullptr), dsum(nullptr), dbc(nullptr) {}
+};
+
+// Where a wavefront's work lies.
+template <int L, int WAVES> struct Place {
+  static constexpr int CH = 64 / L, E = CH * TILE / 64;
+  int blk, g, b, s, lane, wave, ch, part, ec, et;
+  int d, ed;                         // channel of the scan and of the elementwise mapping
+  bool live, elive;
+  __device__ Place(const ScanP &p) {
+    unsigned id = blockIdx.x;
+    blk = id % p.blocks; id /= p.blocks;
+    g = id % p.G; id /= p.G;
+    b = id % p.B; s = id / p.B;
+    lane = threadIdx.x & 63; wave = threadIdx.x >> 6;
+    ch = lane / L; part = lane % L;
+    ec = lane % CH; et = lane / CH;
+    const int dg = p.D / p.G, c0 = (blk * WAVES + wave) * CH;
+    live = c0 + ch < dg; elive = c0 + ec < dg;
+    d = g * dg + (live ? c0 + ch : 0);
+    ed = g * dg + (elive ? c0 + ec : 0);
+  }
+};
+
+// Four states of [D][N] or [B][D][N] rows, zero beyond N.
+__device__ __forceinline__ void load4(float r[NS], const float *row, int part, int N, bool live) {
+#pragma unroll
+  for (int j = 0; j < NS; ++j) r[j] = live && row && part * NS + j < N ? row[part * NS + j] : 0.f;
+}
+__device__ __forceinline__ void store4(float *row, const float r[NS], int part, int N) {
+#pragma unroll
+  for (int j = 0; j < NS; ++j)
+    if (part * NS + j < N) row[part * NS + j] = r[j];
+}
+
+// Rows of Bv (and Cv) of a tile into LDS as fp32 [TILE][NP], zero beyond N and for steps that do not exist.  COUNT
+// threads share the work; `me` is this one's number.
+template <typename T, int NP, int COUNT>
+__device__ __forceinline__ void fetch_rows(T r[(TILE * NP + COUNT - 1) / COUNT], const Rows<void> &src, int b, int g, int N, int t0, int end, int me) {
+  constexpr int EACH = (TILE * NP + COUNT - 1) / COUNT;
+  const T *base = (const T *)src.p + b * src.sb + (int64_t)g * N;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int at = i * COUNT + me, t = t0 + at / NP, n = at % NP;
+    r[i] = (T)0.f;
+    if (at < TILE * NP && n < N && t < end) r[i] = base[(int64_t)t * src.st + n];
+  }
+}
+template <typename T, int NP, int COUNT>
+__device__ __forceinline__ void put_rows(float *lds, const T r[(TILE * NP + COUNT - 1) / COUNT], int me) {
+  constexpr int EACH = (TILE * NP + COUNT - 1) / COUNT;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int at = i * COUNT + me;
+    if (at < TILE * NP) lds[at] = widen(r[i]);
+  }
+}
+
+// E values of a streamed tensor in the elementwise mapping: step et + i TILE / E of the tile, channel ed.
+template <typename T, int E>
+__device__ __forceinline__ void fetch(T r[E], const Rows<void> &src, int b, int d, int t0, int et, int end, bool live) {
+  const T *base = (const T *)src.p + b * src.sb + d;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int t = t0 + et + i * (TILE / E);
+    r[i] = (T)0.f;
+    if (live && t < end) r[i] = base[(int64_t)t * src.st];
+  }
+}
+template <typename T, int E>
+__device__ __forceinline__ void put(const Rows<void> &dst, const float r[E], int b, int d, int t0, int et, int end, bool live) {
+  T *base = (T *)dst.p + b * dst.sb + d;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int t = t0 + et + i * (TILE / E);
+    if (live && t < end) base[(int64_t)t * dst.st] = narrow<T>(r[i]);
+  }
+}
+
+// ---------------------------------------------------------------- forward
+// LOCAL: the chunk from zero, for its end state and its sum of delta alone; no outputs.
+template <typename T, int L, int WAVES, bool LOCAL>
+__global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p) {
+  using P = Place<L, WAVES>;
+  constexpr int CH = P::CH, E = P::E, NP = NS * L;
+  __shared__ float2 s_d[WAVES][TILE * CH];
+  __shared__ __attribute__((aligned(16))) float s_b[WAVES][TILE * NP], s_c[WAVES][LOCAL ? 4 : TILE * NP];
+  __shared__ float s_y[WAVES][LOCAL ? 4 : TILE * CH];
+  const P me(p);
+  float2 *sd = s_d[me.wave];
+  float *sb = s_b[me.wave], *sc = s_c[me.wave], *sy = s_y[me.wave];
+  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, length_of(p.lengths, me.b, p.T));
+  const size_t seq = (size_t)me.b * p.D + me.d;
+
+  float A[NS], h[NS], sum = 0.f;
+  load4(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
+#pragma unroll
+  for (int j = 0; j < NS; ++j) { A[j] *= LOG2E; h[j] = 0.f; }
+  if constexpr (!LOCAL) {
+    if (p.nchunks > 1) {
+      if (me.live) {
+        const float4 v = p.local[((size_t)me.s * p.B * p.D + seq) * L + me.part];
+        h[0] = v.x; h[1] = v.y; h[2] = v.z; h[3] = v.w;
+      }
+    } else {
+      load4(h, p.init ? p.init + seq * p.N : nullptr, me.part, p.N, me.live);
+    }
+  }
+  const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f, skip = p.skip ? p.skip[me.ed] : 0.f;
+
+  T rx[E], rd[E], rz[E], rb[L], rc[L];                    // (TILE * NP values by 64 lanes are L each)
+  auto load = [&](int t0) {
+    fetch<T, E>(rx, p.x, me.b, me.ed, t0, me.et, end, me.elive);
+    fetch<T, E>(rd, p.dt, me.b, me.ed, t0, me.et, end, me.elive);
+    fetch_rows<T, NP, 64>(rb, p.bv, me.b, me.g, p.N, t0, end, me.lane);
+    if constexpr (!LOCAL) {
+      if (p.z.p) fetch<T, E>(rz, p.z, me.b, me.ed, t0, me.et, end, me.elive);
+      fetch_rows<T, NP, 64>(rc, p.cv, me.b, me.g, p.N, t0, end, me.lane);
+    }
+  };
+  load(c0);
+  for (int t0 = c0; t0 < (LOCAL ? end : c1); t0 += TILE) {
+    float x[E], z[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int t = me.et + i * (TILE / E);
+      const float raw = widen(rd[i]) + dt_bias;
+      x[i] = widen(rx[i]);
+      z[i] = LOCAL ? 0.f : widen(rz[i]);
+      const float delta = t0 + t < end && me.elive ? (p.softplus ? softplus(raw) : raw) : 0.f;
+      sd[t * CH + me.ec] = make_float2(delta, delta * x[i]);
+    }
+    put_rows<T, NP, 64>(sb, rb, me.lane);
+    if constexpr (!LOCAL) put_rows<T, NP, 64>(sc, rc, me.lane);
+    if (t0 + TILE < end) load(t0 + TILE);
+    wave_lds_order();
+    if constexpr (!LOCAL) {
+      if (p.saved && me.live)
+        p.saved[((size_t)(t0 / TILE) * p.B * p.D + seq) * L + me.part] = make_float4(h[0], h[1], h[2], h[3]);
+    }
+    if (t0 < end) {
+#pragma unroll
+      for (int t = 0; t < TILE; ++t) {
+        const float2 u = sd[t * CH + me.ch];
+        const float4 b4 = *(const float4 *)(sb + t * NP + me.part * NS);
+        const float bq[NS] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+        for (int j = 0; j < NS; ++j) h[j] = fmaf(__builtin_amdgcn_exp2f(u.x * A[j]), h[j], u.y * bq[j]);
+        if constexpr (LOCAL) {
+          sum += u.x;
+        } else {
+          const float4 c4 = *(const float4 *)(sc + t * NP + me.part * NS);
+          float v = c4.x * h[0];
+          v = fmaf(c4.y, h[1], v);
+          v = fmaf(c4.z, h[2], v);
+          v = fmaf(c4.w, h[3], v);
+          v = sum_neighbours<L>(v);
+          if (me.part == 0) sy[t * CH + me.ch] = v;
+        }
+      }
+    }
+    if constexpr (!LOCAL) {
+      wave_lds_order();
+      float out[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const int t = me.et + i * (TILE / E);
+        float v = sy[t * CH + me.ec] + skip * x[i];
+        if (p.z.p) v *= z[i] * sigmoid_fast(z[i]);
+        out[i] = t0 + t < end ? v : 0.f;
+      }
+      put<T, E>(p.y, out, me.b, me.ed, t0, me.et, c1, me.elive);
+    }
+    wave_lds_order();
+  }
+  if (!me.live) return;
+  if constexpr (LOCAL) {
+    p.local[((size_t)me.s * p.B * p.D + seq) * L + me.part] = make_float4(h[0], h[1], h[2], h[3]);
+    if (me.part == 0) p.sums[(size_t)me.s * p.B * p.D + seq] = sum;
+  } else if (p.state && me.s == p.nchunks - 1) {
+    store4(p.state + seq * p.N, h, me.part, p.N);
+  }
+}
+
+// Joins the chunks: local[s] (of the chunk from zero) becomes the state before chunk s, in order; with REVERSE the
+// gradient behind it, from the last one.  A thread per (sequence, channel, four states).
+template <int L, bool REVERSE> __global__ __launch_bounds__(256) void scan_join_kernel(const ScanP p, const float *first) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)p.B * p.D * L;
+  if (id >= all) return;
+  const int part = (int)(id % L);
+  const int64_t seq = id / L;
+  float A[NS], h[NS];
+  load4(A, p.A + (seq % p.D) * p.N, part, p.N, true);
+  load4(h, first ? first + seq * p.N : nullptr, part, p.N, true);
+#pragma unroll
+  for (int j = 0; j < NS; ++j) A[j] *= LOG2E;
+  const int last = REVERSE ? 0 : p.nchunks - 1;            // (the chunk that nobody follows was not run from zero)
+  for (int i = 0; i < p.nchunks; ++i) {
+    const int s = REVERSE ? p.nchunks - 1 - i : i;
+    float4 *at = p.local + (int64_t)s * all + id;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+    if (s != last) { v = *at; sum = p.sums[(int64_t)s * p.B * p.D + seq]; }
+    *at = make_float4(h[0], h[1], h[2], h[3]);
+    h[0] = fmaf(__builtin_amdgcn_exp2f(sum * A[0]), h[0], v.x);
+    h[1] = fmaf(__builtin_amdgcn_exp2f(sum * A[1]), h[1], v.y);
+    h[2] = fmaf(__builtin_amdgcn_exp2f(sum * A[2]), h[2], v.z);
+    h[3] = fmaf(__builtin_amdgcn_exp2f(sum * A[3]), h[3], v.w);
+  }
+}
+
+// ---------------------------------------------------------------- reverse
+// The chunk from a zero gradient behind it: the gradient of the state before it and the sum of delta.
+template <typename T, int L, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const ScanP p, const ScanGradP g) {
+  using P = Place<L, WAVES>;
+  constexpr int CH = P::CH, E = P::E, NP = NS * L;
+  __shared__ float2 s_d[WAVES][TILE * CH];
+  __shared__ __attribute__((aligned(16))) float s_c[WAVES][TILE * NP];
+  P me(p);
+  me.s += 1;                                               // (nothing is in front of chunk 0)
+  float2 *sd = s_d[me.wave];
+  float *sc = s_c[me.wave];
+  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, length_of(p.lengths, me.b, p.T));
+  const size_t seq = (size_t)me.b * p.D + me.d;
+  float A[NS], q[NS], sum = 0.f;
+  load4(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
+#pragma unroll
+  for (int j = 0; j < NS; ++j) { A[j] *= LOG2E; q[j] = 0.f; }
+  const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f;
+  T ry[E], rd[E], rz[E], rc[L];
+  auto load = [&](int t0) {
+    fetch<T, E>(ry, g.dy, me.b, me.ed, t0, me.et, end, me.elive);
+    fetch<T, E>(rd, p.dt, me.b, me.ed, t0, me.et, end, me.elive);
+    if (p.z.p) fetch<T, E>(rz, p.z, me.b, me.ed, t0, me.et, end, me.elive);
+    fetch_rows<T, NP, 64>(rc, p.cv, me.b, me.g, p.N, t0, end, me.lane);
+  };
+  const int tiles = end > c0 ? (end - c0 + TILE - 1) / TILE : 0;
+  if (tiles) load(c0 + (tiles - 1) * TILE);
+  for (int i0 = tiles - 1; i0 >= 0; --i0) {
+    const int t0 = c0 + i0 * TILE;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int t = me.et + i * (TILE / E);
+      const float raw = widen(rd[i]) + dt_bias;
+      float dy = widen(ry[i]);
+      if (p.z.p) { const float z = widen(rz[i]); dy *= z * sigmoid_fast(z); }
+      const bool on = t0 + t < end && me.elive;
+      sd[t * CH + me.ec] = make_float2(on ? (p.softplus ? softplus(raw) : raw) : 0.f, on ? dy : 0.f);
+    }
+    put_rows<T, NP, 64>(sc, rc, me.lane);
+    if (i0 > 0) load(t0 - TILE);
+    wave_lds_order();
+#pragma unroll
+    for (int t = TILE - 1; t >= 0; --t) {
+      const float2 u = sd[t * CH + me.ch];
+      const float4 c4 = *(const float4 *)(sc + t * NP + me.part * NS);
+      q[0] = fmaf(u.y, c4.x, q[0]) * __builtin_amdgcn_exp2f(u.x * A[0]);
+      q[1] = fmaf(u.y, c4.y, q[1]) * __builtin_amdgcn_exp2f(u.x * A[1]);
+      q[2] = fmaf(u.y, c4.z, q[2]) * __builtin_amdgcn_exp2f(u.x * A[2]);
+      q[3] = fmaf(u.y, c4.w, q[3]) * __builtin_amdgcn_exp2f(u.x * A[3]);
+      sum += u.x;
+    }
+    wave_lds_order();
+  }
+  if (!me.live) return;
+  p.local[((size_t)me.s * p.B * p.D + seq) * L + me.part] = make_float4(q[0], q[1], q[2], q[3]);
+  if (me.part == 0) p.sums[(size_t)me.s * p.B * p.D + seq] = sum;
+}
+
+// Sums v[0..7] (four of dBv, four of dCv) over the wavefront's channels, lane bits log2(L) to 5.  While eight values
+// are left, the halves of the wavefront trade: each keeps half the values, summed; then the rows of 16 likewise; what
+// is left of the bits goes by rotations.  Returns the two sums of this lane: of dBv in lanes 0-31, of dCv in 32-63,
+// of values 2 (lane bit 4) and the next.
+template <int L> __device__ __forceinline__ float2 sum_channels(const float v[2 * NS]) {
+  float a[4], c[2];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v[j]), __builtin_bit_cast(unsigned, v[j + 4]), false, false);
+    a[j] = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a[j]), __builtin_bit_cast(unsigned, a[j + 2]), false, false);
+    c[j] = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if constexpr (L <= 8) c[j] += dpp<0x128>(c[j]);
+    if constexpr (L <= 4) c[j] += dpp<0x124>(c[j]);
+    if constexpr (L <= 2) c[j] += dpp<0x122>(c[j]);
+    if constexpr (L <= 1) c[j] += dpp<0x121>(c[j]);
+  }
+  return make_float2(c[0], c[1]);
+}
+
+// The reverse pass proper.  Per tile, from the last: the states of the tile once more from the one that the forward
+// pass saved in front of it, kept with their decays in registers (128 of them), then back through the steps:
+//   g = q + dy0 C,   dC += dy0 h,  dB += g delta x  (over the channels),   u = g a h[t-1]
+//   d(delta) = sum_n u A + x sum_n g B,   dx = delta sum_n g B + dy0 skip,   dA += u delta,   q = g a.
+// The workgroup's wavefronts share the rows of Bv and Cv, and add their channel sums of dBv and dCv through LDS in a
+// fixed order; sums over workgroups are left to scan_sum_rows_kernel.
+template <typename T, int L, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void scan_reverse_kernel(const ScanP p, const ScanGradP g) {
+  using P = Place<L, WAVES>;
+  constexpr int CH = P::CH, E = P::E, NP = NS * L, THREADS = 64 * WAVES;
+  constexpr int EACH = (TILE * NP + THREADS - 1) / THREADS;
+  __shared__ float4 s_d[WAVES][TILE * CH];                  // delta, delta x, dy0 and sum C h, then sum g B, sum u A
+  __shared__ __attribute__((aligned(16))) float s_b[TILE * NP], s_c[TILE * NP];
+  __shared__ __attribute__((aligned(8))) float s_s[WAVES][2][TILE * NP];
+  const P me(p);
+  float4 *sd = s_d[me.wave];
+  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, length_of(p.lengths, me.b, p.T));
+  const size_t seq = (size_t)me.b * p.D + me.d;
+  float A[NS], A2[NS], q[NS], dA[NS] = {0.f, 0.f, 0.f, 0.f};
+  load4(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
+#pragma unroll
+  for (int j = 0; j < NS; ++j) A2[j] = A[j] * LOG2E;
+  if (p.nchunks > 1) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (me.live) v = p.local[((size_t)me.s * p.B * p.D + seq) * L + me.part];
+    q[0] = v.x; q[1] = v.y; q[2] = v.z; q[3] = v.w;
+  } else {
+    load4(q, g.d_state ? g.d_state + seq * p.N : nullptr, me.part, p.N, me.live);
+  }
+  const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f, skip = p.skip ? p.skip[me.ed] : 0.f;
+  float dskip = 0.f, ddtb = 0.f;
+
+  T rx[E], rd[E], rz[E], ry[E], rb[EACH], rc[EACH];
+  float4 rh = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto load = [&](int t0) {
+    fetch<T, E>(rx, p.x, me.b, me.ed, t0, me.et, end, me.elive);
+    fetch<T, E>(rd, p.dt, me.b, me.ed, t0, me.et, end, me.elive);
+    fetch<T, E>(ry, g.dy, me.b, me.ed, t0, me.et, end, me.elive);
+    if (p.z.p) fetch<T, E>(rz, p.z, me.b, me.ed, t0, me.et, end, me.elive);
+    fetch_rows<T, NP, THREADS>(rb, p.bv, me.b, me.g, p.N, t0, end, threadIdx.x);
+    fetch_rows<T, NP, THREADS>(rc, p.cv, me.b, me.g, p.N, t0, end, threadIdx.x);
+    if (me.live) rh = p.saved[((size_t)(t0 / TILE) * p.B * p.D + seq) * L + me.part];
+  };
+  const int tiles = end > c0 ? (end - c0 + TILE - 1) / TILE : 0;
+  const int rows = (c1 - c0 + TILE - 1) / TILE;             // tiles with rows to write, those that do not exist among them
+  {
+    float zero[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) zero[i] = 0.f;
+    for (int i0 = tiles; i0 < rows; ++i0) {
+      const int t0 = c0 + i0 * TILE;
+      put<T, E>(g.dx, zero, me.b, me.ed, t0, me.et, c1, me.elive);
+      put<T, E>(g.ddt, zero, me.b, me.ed, t0, me.et, c1, me.elive);
+      if (p.z.p) put<T, E>(g.dz, zero, me.b, me.ed, t0, me.et, c1, me.elive);
+    }
+  }
+  if (tiles) load(c0 + (tiles - 1) * TILE);
+  for (int i0 = tiles - 1; i0 >= 0; --i0) {
+    const int t0 = c0 + i0 * TILE;
+    float x[E], z[E], dy[E], delta[E], slope[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int t = me.et + i * (TILE / E);
+      const bool on = t0 + t < end && me.elive;
+      const float raw = widen(rd[i]) + dt_bias;
+      x[i] = widen(rx[i]);
+      dy[i] = widen(ry[i]);
+      z[i] = p.z.p ? widen(rz[i]) : 0.f;
+      const float e = exp_fast(-fabsf(raw)), r = rcp_fast(1.f + e);
+      delta[i] = on ? (p.softplus ? softplus(raw) : raw) : 0.f;
+      slope[i] = p.softplus ? (raw >= 0.f ? r : e * r) : 1.f;       // d(delta) / d(dt)
+      const float dy0 = p.z.p ? dy[i] * z[i] * sigmoid_fast(z[i]) : dy[i];
+      sd[t * CH + me.ec] = make_float4(delta[i], delta[i] * x[i], dy0, 0.f);
+    }
+    put_rows<T, NP, THREADS>(s_b, rb, threadIdx.x);
+    put_rows<T, NP, THREADS>(s_c, rc, threadIdx.x);
+    float h[TILE + 1][NS], a[TILE][NS];
+    h[0][0] = rh.x; h[0][1] = rh.y; h[0][2] = rh.z; h[0][3] = rh.w;
+    __syncthreads();
+    if (i0 > 0) load(t0 - TILE);
+#pragma unroll
+    for (int t = 0; t < TILE; ++t) {
+      const float2 u = *(const float2 *)(sd + t * CH + me.ch);
+      const float4 b4 = *(const float4 *)(s_b + t * NP + me.part * NS);
+      const float bq[NS] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {
+        a[t][j] = __builtin_amdgcn_exp2f(u.x * A2[j]);
+        h[t + 1][j] = fmaf(a[t][j], h[t][j], u.y * bq[j]);
+      }
+      if (p.z.p) {                                          // dz needs the output before the gate
+        const float4 c4 = *(const float4 *)(s_c + t * NP + me.part * NS);
+        float v = c4.x * h[t + 1][0];
+        v = fmaf(c4.y, h[t + 1][1], v);
+        v = fmaf(c4.z, h[t + 1][2], v);
+        v = fmaf(c4.w, h[t + 1][3], v);
+        v = sum_neighbours<L>(v);
+        if (me.part == 0) sd[t * CH + me.ch].w = v;
+      }
+    }
+    wave_lds_order();
+#pragma unroll
+    for (int t = TILE - 1; t >= 0; --t) {
+      const float4 u = sd[t * CH + me.ch];
+      const float4 b4 = *(const float4 *)(s_b + t * NP + me.part * NS);
+      const float4 c4 = *(const float4 *)(s_c + t * NP + me.part * NS);
+      const float bq[NS] = {b4.x, b4.y, b4.z, b4.w}, cq[NS] = {c4.x, c4.y, c4.z, c4.w};
+      float v[2 * NS], gb = 0.f, ua = 0.f;
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {
+        const float gh = fmaf(u.z, cq[j], q[j]);
+        v[j] = gh * u.y;
+        v[NS + j] = u.z * h[t + 1][j];
+        gb = fmaf(gh, bq[j], gb);
+        q[j] = gh * a[t][j];
+        const float w = q[j] * h[t][j];
+        ua = fmaf(w, A[j], ua);
+        dA[j] = fmaf(w, u.x, dA[j]);
+      }
+      gb = sum_neighbours<L>(gb);
+      ua = sum_neighbours<L>(ua);
+      if (me.part == 0) { sd[t * CH + me.ch].x = gb; sd[t * CH + me.ch].y = ua; }
+      const float2 s = sum_channels<L>(v);
+      if ((me.lane & 15) < L)
+        *(float2 *)(&s_s[me.wave][me.lane >> 5][t * NP + me.part * NS + ((me.lane >> 4) & 1) * 2]) = s;
+    }
+    wave_lds_order();
+    float ox[E], od[E], oz[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int t = me.et + i * (TILE / E);
+      const bool on = t0 + t < end && me.elive;
+      const float4 r = sd[t * CH + me.ec];
+      float dy0 = dy[i];
+      oz[i] = 0.f;
+      if (p.z.p) {
+        const float e = sigmoid_fast(z[i]);
+        dy0 = dy[i] * z[i] * e;
+        oz[i] = on ? dy[i] * (r.w + skip * x[i]) * e * (1.f + z[i] * (1.f - e)) : 0.f;
+      }
+      ox[i] = on ? fmaf(delta[i], r.x, dy0 * skip) : 0.f;
+      od[i] = on ? fmaf(x[i], r.x, r.y) * slope[i] : 0.f;
+      ddtb += od[i];
+      if (on) dskip = fmaf(dy0, x[i], dskip);
+    }
+    put<T, E>(g.dx, ox, me.b, me.ed, t0, me.et, c1, me.elive);
+    put<T, E>(g.ddt, od, me.b, me.ed, t0, me.et, c1, me.elive);
+    if (p.z.p) put<T, E>(g.dz, oz, me.b, me.ed, t0, me.et, c1, me.elive);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < (2 * TILE * NP + THREADS - 1) / THREADS; ++i) {
+      const int at = i * THREADS + threadIdx.x, t = at / (2 * NP), kn = at % (2 * NP);
+      if (at < 2 * TILE * NP && t0 + t < end) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) s += s_s[w][kn / NP][t * NP + kn % NP];
+        g.dbc[((((size_t)me.blk * p.T + t0 + t) * p.B + me.b) * p.G + me.g) * (2 * NP) + kn] = s;
+      }
+    }
+  }
+  // sums over the lanes that share a channel of the elementwise mapping: lane bits log2(CH) to 5
+  wave_lds_order();
+  sd[me.lane].x = dskip;
+  sd[me.lane].y = ddtb;
+  wave_lds_order();
+  if (me.lane < CH && me.elive) {
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < L; ++i) { s0 += sd[i * CH + me.lane].x; s1 += sd[i * CH + me.lane].y; }
+    float *to = g.dsum + ((size_t)me.s * p.B + me.b) * 2 * p.D + me.ed;
+    to[0] = s0;
+    to[p.D] = s1;
+  }
+  if (!me.live) return;
+  g.dA[(((size_t)me.s * p.B + me.b) * p.D + me.d) * L + me.part] = make_float4(dA[0], dA[1], dA[2], dA[3]);
+  if (g.dinit && me.s == 0) store4(g.dinit + seq * p.N, q, me.part, p.N);
+}
+
+// dBv and dCv: sums of the workgroups' partial sums, zero where the step does not exist.  A thread per value.
+template <typename T, int L>
+__global__ __launch_bounds__(256) void scan_sum_rows_kernel(const ScanP p, const float *__restrict__ dbc, Rows<void> dbv, Rows<void> dcv) {
+  constexpr int NP = NS * L;
+  const int64_t all = (int64_t)p.T * p.B * p.G * 2 * NP;
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
+    const int n = (int)(id % NP), kind = (int)(id / NP % 2);
+    const int64_t row = id / (2 * NP);
+    const int gr = (int)(row % p.G), b = (int)(row / p.G % p.B), t = (int)(row / p.G / p.B);
+    if (n >= p.N) continue;
+    float s = 0.f;
+    if (t < length_of(p.lengths, b, p.T))
+      for (int k = 0; k < p.blocks; ++k) s += dbc[k * all + id];
+    const Rows<void> &to = kind ? dcv : dbv;
+    ((T *)to.p)[t * to.st + b * to.sb + (int64_t)gr * p.N + n] = narrow<T>(s);
+  }
+}
+
+// dA, dskip, ddt_bias: sums over chunks and sequences.  64 columns by four interleaved runs a workgroup.
+template <int L>
+__global__ __launch_bounds__(256) void scan_sum_params_kernel(const ScanP p, const float *__restrict__ dA_part, const float *__restrict__ dsum,
+                                                              float *__restrict__ dA, float *__restrict__ dskip, float *__restrict__ ddt_bias) {
+  constexpr int NP = NS * L;
+  __shared__ float part[256];
+  const int col = threadIdx.x & 63, run = threadIdx.x >> 6, rows = p.nchunks * p.B;
+  const int64_t na = (int64_t)p.D * NP, c = (int64_t)blockIdx.x * 64 + col, cols = na + 2 * (int64_t)p.D;
+  float s = 0.f;
+  if (c < na)
+    for (int r = run; r < rows; r += 4) s += dA_part[r * na + c];
+  else if (c < cols)
+    for (int r = run; r < rows; r += 4) s += dsum[r * 2 * (int64_t)p.D + (c - na)];
+  part[threadIdx.x] = s;
+  __syncthreads();
+  if (run != 0 || c >= cols) return;
+  s = ((part[col] + part[64 + col]) + part[128 + col]) + part[192 + col];
+  if (c < na) {
+    const int n = (int)(c % NP);
+    if (n < p.N) dA[c / NP * p.N + n] = s;
+  } else if (c < na + p.D) {
+    if (dskip) dskip[c - na] = s;
+  } else if (ddt_bias) {
+    ddt_bias[c - na - p.D] = s;
+  }
+}
+
+// ---------------------------------------------------------------- one step
+// A lane holds four states of a (sequence, channel); the state [B][D][N] is read and written once, 16 bytes a lane where
+// N is a multiple of four and the rows are aligned (FOUR).
+template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void scan_step_kernel(const ScanP p) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= (int64_t)p.B * p.D * L) return;                 // (the L lanes of a channel leave together)
+  const int part = (int)(id % L);
+  const int64_t seq = id / L;
+  const int b = (int)(seq / p.D), d = (int)(seq % p.D), gr = d / (p.D / p.G);
+  const bool some = part * NS < p.N;
+  const T *bv = (const T *)p.bv.p + b * p.bv.sb + (int64_t)gr * p.N, *cv = (const T *)p.cv.p + b * p.cv.sb + (int64_t)gr * p.N;
+  float A[NS], h[NS], bq[NS], cq[NS];
+  float *state = p.state + seq * p.N;
+  if constexpr (FOUR) {
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 av = some ? *(const float4 *)(p.A + (int64_t)d * p.N + part * NS) : zero;
+    const float4 hv = some ? *(const float4 *)(state + part * NS) : zero;
+    A[0] = av.x; A[1] = av.y; A[2] = av.z; A[3] = av.w;
+    h[0] = hv.x; h[1] = hv.y; h[2] = hv.z; h[3] = hv.w;
+  } else {
+    load4(A, p.A + (int64_t)d * p.N, part, p.N, true);
+    load4(h, state, part, p.N, true);
+  }
+#pragma unroll
+  for (int j = 0; j < NS; ++j) {
+    const int n = part * NS + j;
+    bq[j] = n < p.N ? widen(bv[n]) : 0.f;
+    cq[j] = n < p.N ? widen(cv[n]) : 0.f;
+  }
+  const float x = widen(((const T *)p.x.p)[b * p.x.sb + d]);
+  const float raw = widen(((const T *)p.dt.p)[b * p.dt.sb + d]) + (p.dt_bias ? p.dt_bias[d] : 0.f);
+  const float delta = p.softplus ? softplus(raw) : raw, u = delta * x;
+  float v = 0.f;
+#pragma unroll
+  for (int j = 0; j < NS; ++j) {
+    h[j] = fmaf(exp_fast(delta * A[j]), h[j], u * bq[j]);
+    v = fmaf(cq[j], h[j], v);
+  }
+  v = sum_neighbours<L>(v);
+  if constexpr (FOUR) {
+    if (some) *(float4 *)(state + part * NS) = make_float4(h[0], h[1], h[2], h[3]);
+  } else {
+    store4(state, h, part, p.N);
+  }
+  if (part == 0) {
+    if (p.skip) v = fmaf(p.skip[d], x, v);
+    if (p.z.p) { const float z = widen(((const T *)p.z.p)[b * p.z.sb + d]); v *= z * sigmoid_fast(z); }
+    ((T *)p.y.p)[b * p.y.sb + d] = narrow<T>(v);
+  }
+}
+
+// ---------------------------------------------------------------- host side
+int lanes_of(int N) {                                       // L
+  int l = 1;
+  while (l * NS < N) l *= 2;
+  return l;
+}
+constexpr int waves_of(int L) { return L == 1 ? 2 : 4; }    // (64 channels a wavefront: LDS holds the tiles of two)
+
+// Workgroups per (chunk, sequence, group).
+int blocks_of(const snn_scan_args &a, int L) {
+  const int per = 64 / L * waves_of(L), dg = a.D / a.groups;
+  return (dg + per - 1) / per;
+}
+
+int scan_sizes(const snn_scan_args *a) {
+  if (!a) return ops_fail(SNN_ERR_NULL, "scan: arguments are NULL");
+  if (a->T < 0 || a->B <= 0 || a->D <= 0) return ops_fail(SNN_ERR_ARG, "scan: T >= 0, B > 0 and D > 0 are required");
+  if (a->N < 1 || a->N > SNN_SCAN_MAX_STATES) return ops_fail(SNN_ERR_ARG, "scan: N must be 1 to %d", SNN_SCAN_MAX_STATES);
+  if (a->groups < 1 || a->D % a->groups) return ops_fail(SNN_ERR_ARG, "scan: groups must divide D");
+  if ((int64_t)a->B * a->D >= (1ll << 31) / 64) return ops_fail(SNN_ERR_ARG, "scan: B * D must stay below 2^25");
+  if (a->T > (1 << 30)) return ops_fail(SNN_ERR_ARG, "scan: T must not exceed 2^30");
+  if ((int64_t)a->B * a->groups * blocks_of(*a, lanes_of(a->N)) > (1 << 23))       // (a launch has less than 2^32 threads)
+    return ops_fail(SNN_ERR_ARG, "scan: too many sequences of narrow groups: more than 2^23 workgroups");
+  if ((int64_t)a->T * a->B * a->groups >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "scan: T * B * groups must stay below 2^32");
+  return SNN_OK;
+}
+
+int scan_check(const snn_scan_args *a, bool step, bool grads) {
+  int rc = scan_sizes(a);
+  if (rc) return rc;
+  if (a->type != SNN_TYPE_FP32 && a->type != SNN_TYPE_BF16) return ops_fail(SNN_ERR_ARG, "scan: unknown type %d", a->type);
+  if (!a->A) return ops_fail(SNN_ERR_NULL, "scan: A is NULL");
+  if (a->T > 0 && (!a->x.p || !a->dt.p || !a->bv.p || !a->cv.p || (!grads && !a->y.p)))
+    return ops_fail(SNN_ERR_NULL, "scan: x, dt, bv, cv or y is NULL");
+  if (step) {
+    if (a->T != 1) return ops_fail(SNN_ERR_ARG, "scan step: T must be 1");
+    if (a->init || a->lengths) return ops_fail(SNN_ERR_ARG, "scan step: init and lengths must be NULL");
+    if (!a->state) return ops_fail(SNN_ERR_NULL, "scan step: state is NULL");
+  }
+  const size_t z = a->type == SNN_TYPE_FP32 ? 4 : 2;
+  for (const void *q : {a->x.p, a->dt.p, a->z.p, a->bv.p, a->cv.p, a->y.p})
+    if (!aligned(q, z)) return ops_fail(SNN_ERR_ARG, "scan: a pointer is not aligned to its element type");
+  for (const void *q : {(const void *)a->A, (const void *)a->skip, (const void *)a->dt_bias, (const void *)a->init, (const void *)a->lengths, (const void *)a->state})
+    if (!aligned(q, 4)) return ops_fail(SNN_ERR_ARG, "scan: a pointer is not aligned to its element type");
+  return SNN_OK;
+}
+
+// How time is cut: enough chunks that every SIMD has a wavefront, of at least 64 steps.
+void scan_cut(const snn_scan_args &a, int L, int *chunk, int *nchunks) {
+  const int64_t waves = (int64_t)a.B * a.groups * blocks_of(a, L) * waves_of(L);
+  int64_t n = 1024 / waves;
+  if (n > a.T / 64) n = a.T / 64;
+  if (n < 1) n = 1;
+  const int64_t tiles = ((int64_t)a.T + TILE - 1) / TILE;
+  const int64_t each = tiles ? (tiles + n - 1) / n : 1;
+  *chunk = (int)(each * TILE);
+  *nchunks = (int)(tiles ? (tiles + each - 1) / each : 1);
+}
+
+// The pieces of a workspace: chunk states, sums of delta, and for the reverse pass the partial sums.
+struct ScanSpace {
+  size_t local, sums, dA, dsum, dbc, all;
+};
+ScanSpace scan_space(const snn_scan_args &a, bool backward) {
+  const int L = lanes_of(a.N);
+  int chunk, n;
+  scan_cut(a, L, &chunk, &n);
+  const size_t seqs = (size_t)a.B * a.D;
+  ScanSpace s;
+  s.local = 0;
+  s.sums = s.local + (n > 1 ? rup256(n * seqs * L * 16) : 0);
+  s.dA = s.sums + (n > 1 ? rup256(n * seqs * 4) : 0);
+  s.dsum = s.dA + (backward ? rup256(n * seqs * L * 16) : 0);
+  s.dbc = s.dsum + (backward ? rup256(n * seqs * 8) : 0);
+  s.all = s.dbc + (backward ? rup256((size_t)blocks_of(a, L) * a.T * a.B * a.groups * 2 * NS * L * 4) : 0);
+  return s;
+}
+
+template <typename F> int with_lanes(int L, F f) {
+  switch (L) {
+    case 1: return f(std::integral_constant<int, 1>());
+    case 2: return f(std::integral_constant<int, 2>());
+    case 4: return f(std::integral_constant<int, 4>());
+    case 8: return f(std::integral_constant<int, 8>());
+    default: return f(std::integral_constant<int, 16>());
+  }
+}
+
+ScanP plan(const snn_scan_args &a, int L, char *ws, const ScanSpace &s) {
+  ScanP p(a);
+  scan_cut(a, L, &p.chunk, &p.nchunks);
+  p.blocks = blocks_of(a, L);
+  if (p.nchunks > 1) { p.local = (float4 *)(ws + s.local); p.sums = (float *)(ws + s.sums); }
+  return p;
+}
+
+template <typename T, int L> int forward(const snn_scan_args &a, void *saved, char *ws, hipStream_t st) {
+  constexpr int W = waves_of(L);
+  ScanP p = plan(a, L, ws, scan_space(a, false));
+  p.saved = (float4 *)saved;
+  const unsigned per = (unsigned)((size_t)p.blocks * p.G * p.B);
+  int rc = SNN_OK;
+  if (p.nchunks > 1) {
+    hipLaunchKernelGGL((scan_forward_kernel<T, L, W, true>), dim3(per * (p.nchunks - 1)), dim3(64 * W), 0, st, p);
+    if ((rc = ops_launched("scan, chunks"))) return rc;
+    hipLaunchKernelGGL((scan_join_kernel<L, false>), dim3((unsigned)(((int64_t)p.B * p.D * L + 255) / 256)), dim3(256), 0, st, p, a.init);
+    if ((rc = ops_launched("scan, join"))) return rc;
+  }
+  hipLaunchKernelGGL((scan_forward_kernel<T, L, W, false>), dim3(per * p.nchunks), dim3(64 * W), 0, st, p);
+  return ops_launched("scan");
+}
+
+template <typename T, int L> int backward(const snn_scan_args &a, const snn_scan_grads &gr, const void *saved, char *ws, hipStream_t st) {
+  constexpr int W = waves_of(L);
+  const ScanSpace s = scan_space(a, true);
+  ScanP p = plan(a, L, ws, s);
+  p.saved = (float4 *)const_cast<void *>(saved);
+  ScanGradP g(gr);
+  g.dA = (float4 *)(ws + s.dA);
+  g.dsum = (float *)(ws + s.dsum);
+  g.dbc = (float *)(ws + s.dbc);
+  const unsigned per = (unsigned)((size_t)p.blocks * p.G * p.B);
+  int rc = SNN_OK;
+  if (p.nchunks > 1) {
+    hipLaunchKernelGGL((scan_reverse_local_kernel<T, L, W>), dim3(per * (p.nchunks - 1)), dim3(64 * W), 0, st, p, g);
+    if ((rc = ops_launched("scan reverse, chunks"))) return rc;
+    hipLaunchKernelGGL((scan_join_kernel<L, true>), dim3((unsigned)(((int64_t)p.B * p.D * L + 255) / 256)), dim3(256), 0, st, p, gr.d_state);
+    if ((rc = ops_launched("scan reverse, join"))) return rc;
+  }
+  hipLaunchKernelGGL((scan_reverse_kernel<T, L, W>), dim3(per * p.nchunks), dim3(64 * W), 0, st, p, g);
+  if ((rc = ops_launched("scan reverse"))) return rc;
+  const int64_t values = (int64_t)a.T * a.B * a.groups * 2 * NS * L;
+  if (values) {
+    hipLaunchKernelGGL((scan_sum_rows_kernel<T, L>), dim3((unsigned)std::min<int64_t>((values + 255) / 256, 1 << 16)), dim3(256), 0, st, p, g.dbc, Rows<void>(gr.dbv), Rows<void>(gr.dcv));
+    if ((rc = ops_launched("scan reverse, rows"))) return rc;
+  }
+  const int64_t cols = (int64_t)a.D * (NS * L + 2);
+  hipLaunchKernelGGL((scan_sum_params_kernel<L>), dim3((unsigned)((cols + 63) / 64)), dim3(256), 0, st, p, (const float *)g.dA, g.dsum, gr.dA, gr.dskip, gr.ddt_bias);
+  return ops_launched("scan reverse, parameters");
+}
+
+template <typename T, int L> int step(const snn_scan_args &a, hipStream_t st) {
+  const ScanP p(a);
+  const dim3 grid((unsigned)(((int64_t)a.B * a.D * L + 255) / 256));
+  if (a.N % 4 == 0 && aligned(a.A, 16) && aligned(a.state, 16)) hipLaunchKernelGGL((scan_step_kernel<T, L, true>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((scan_step_kernel<T, L, false>), grid, dim3(256), 0, st, p);
+  return ops_launched("scan step");
+}
+
+int check_workspace(size_t need, const void *ws, size_t have) {
+  if (need && (!ws || !aligned(ws, 16) || have < need))
+    return ops_fail(SNN_ERR_WORKSPACE, "scan: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, ws ? have : (size_t)0);
+  return SNN_OK;
+}
+
+}  // namespace
+}  // namespace snn
+
+using namespace snn;
+
+extern "C" {
+
+int32_t snn_scan_workspace_bytes(const snn_scan_args *a, int32_t backward, size_t *bytes) {
+  if (!bytes) return ops_fail(SNN_ERR_NULL, "bytes is NULL");
+  int rc = scan_sizes(a);
+  if (rc) return rc;
+  *bytes = scan_space(*a, backward != 0).all;
+  return SNN_OK;
+}
+
+int32_t snn_scan_saved_bytes(const snn_scan_args *a, size_t *bytes) {
+  if (!bytes) return ops_fail(SNN_ERR_NULL, "bytes is NULL");
+  int rc = scan_sizes(a);
+  if (rc) return rc;
+  *bytes = ((size_t)a->T + TILE - 1) / TILE * a->B * a->D * lanes_of(a->N) * 16;
+  return SNN_OK;
+}
+
+int32_t snn_scan_forward(const snn_scan_args *a, void *saved, void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = scan_check(a, false, false);
+  if (rc) return rc;
+  if (!aligned(saved, 16)) return ops_fail(SNN_ERR_ARG, "scan: saved must be 16-byte aligned");
+  if ((rc = check_workspace(scan_space(*a, false).all, workspace, workspace_bytes))) return rc;
+  return with_lanes(lanes_of(a->N), [&](auto l) {
+    return a->type == SNN_TYPE_FP32 ? forward<float, l.value>(*a, saved, (char *)workspace, (hipStream_t)stream)
+                                    : forward<__bf16, l.value>(*a, saved, (char *)workspace, (hipStream_t)stream);
+  });
+}
+
+int32_t snn_scan_backward(const snn_scan_args *a, const snn_scan_grads *g, const void *saved, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+  int rc = scan_check(a, false, true);
+  if (rc) return rc;
+  if (!g || !g->dA || (a->T > 0 && (!saved || !g->dy.p || !g->dx.p || !g->ddt.p || !g->dbv.p || !g->dcv.p || (a->z.p && !g->dz.p))))
+    return ops_fail(SNN_ERR_NULL, "scan backward: saved, dy, dx, ddt, dz, dbv, dcv or dA is NULL");
+  const size_t z = a->type == SNN_TYPE_FP32 ? 4 : 2;
+  for (const void *q : {g->dy.p, g->dx.p, g->ddt.p, g->dz.p, g->dbv.p, g->dcv.p})
+    if (!aligned(q, z)) return ops_fail(SNN_ERR_ARG, "scan backward: a pointer is not aligned to its element type");
+  for (const void *q : {(const void *)g->d_state, (const void *)g->dA, (const void *)g->dskip, (const void *)g->ddt_bias, (const void *)g->dinit})
+    if (!aligned(q, 4)) return ops_fail(SNN_ERR_ARG, "scan backward: a pointer is not aligned to its element type");
+  if (!aligned(saved, 16)) return ops_fail(SNN_ERR_ARG, "scan backward: saved must be 16-byte aligned");
+  if ((rc = check_workspace(scan_space(*a, true).all, workspace, workspace_bytes))) return rc;
+  return with_lanes(lanes_of(a->N), [&](auto l) {
+    return a->type == SNN_TYPE_FP32 ? backward<float, l.value>(*a, *g, saved, (char *)workspace, (hipStream_t)stream)
+                                    : backward<__bf16, l.value>(*a, *g, saved, (char *)workspace, (hipStream_t)stream);
+  });
+}
+
+int32_t snn_scan_step(const snn_scan_args *a, void *stream) {
+  int rc = scan_check(a, true, false);
+  if (rc) return rc;
+  return with_lanes(lanes_of(a->N), [&](auto l) {
+    return a->type == SNN_TYPE_FP32 ? step<float, l.value>(*a, (hipStream_t)stream) : step<__bf16, l.value>(*a, (hipStream_t)stream);
+  });
+}
+
+}  // extern "C"

@@ -1461,6 +1461,19 @@ inline float host_bf16_value(uint16_t b) {
 
 }  // namespace
 
+// Errors of the entry points in seq_conv.hip, seq_scan.hip and adamw.hip, which have no context.
+namespace snn {
+int ops_fail(int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_err = buf;
+  return code;
+}
+}  // namespace snn
+
 // ====================================================================== C ABI
 extern "C" {
 

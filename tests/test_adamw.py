@@ -1,0 +1,212 @@
+"""AdamW on the GPU against its definition in 64 bits, and the 8-bit moments against their rule."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import seq_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(1,), (5,), (128,), (129,), (37, 20), (700, 33), (64, 64), (3, 1, 7), (0,), (2049,), (130, 1030)]
+LR, BETAS, EPS = 3e-3, (0.9, 0.999), 1e-8
+
+
+def make(shapes, seed, t=torch.float32):
+    gen = torch.Generator().manual_seed(seed)
+    p = [torch.randn(*s, generator=gen) for s in shapes]
+    g = [(torch.randn(*s, generator=gen) * 10.0 ** torch.randint(-4, 1, (1,), generator=gen).item()).to(t) for s in shapes]
+    return p, g
+
+
+def near(name, got, want, steps, scale=None):
+    """A step is about ten operations on a value, each rounded by 2^-24 of the terms: sixteen of them."""
+    g, w = got.double().cpu(), want
+    room = 16 * steps * 2.0 ** -24 * (w.abs() + (scale if scale is not None else 0)) + 1e-30
+    assert ((g - w).abs() <= room).all(), f"{name}: {((g - w).abs() / room).max().item():.3g} of what is allowed"
+
+
+@pytest.mark.parametrize("t", (torch.float32, torch.bfloat16), ids=("fp32", "bf16"))
+@pytest.mark.parametrize("many", (1, 9), ids=("few", "many"))
+def test_steps_in_32_bits(t, many):
+    from paper_2402_18994_amd import AdamW
+    shapes = SHAPES * many                                # (99 tensors: more than one launch holds)
+    p, g = make(shapes, 1, t)
+    dev = [x.cuda() for x in p]
+    copies = [torch.empty_like(x, dtype=torch.bfloat16) if i % 2 else None for i, x in enumerate(dev)]
+    decay = [0.1 if x.dim() > 1 else 0.0 for x in p]
+    opt = AdamW(dev, lr=LR, betas=BETAS, eps=EPS, weight_decay=decay, copies=copies)
+    ref = [(x.double(), torch.zeros_like(x).double(), torch.zeros_like(x).double()) for x in p]
+    for step in range(1, 4):
+        gs = [(x * (0.5 + step)).to(t) for x in g]
+        opt.step([x.cuda() for x in gs], grad_scale=0.25)
+        ref = [oracle.adamw(a, x.double() * 0.25, m, v, step, LR, BETAS, EPS, w) for (a, m, v), x, w in zip(ref, gs, decay)]
+    for i, (x, (wp, wm, wv)) in enumerate(zip(dev, ref)):
+        near(f"parameter {i}", x, wp, 3, LR)
+        a = opt.at[i]
+        near(f"m {i}", opt.m[a:a + x.numel()].view(x.shape), wm, 3, wm.abs().max().item() if wm.numel() else 0)
+        near(f"v {i}", opt.v[a:a + x.numel()].view(x.shape), wv, 3)
+        if copies[i] is not None:
+            assert torch.equal(copies[i], x.to(torch.bfloat16))
+    assert opt.state_dict()["step"] == 3
+
+
+def moments(opt, i, n):
+    a, blocks = opt.at[i], -(-n // 128)
+    s = slice(a // 128, a // 128 + blocks)
+    m = opt.m[a:a + 128 * blocks].double().view(-1, 128) * opt.m_scale[s, None].double()
+    r = opt.v[a:a + 128 * blocks].double().view(-1, 128) * opt.v_scale[s, None].double()
+    return m.view(-1)[:n].cpu(), r.square().view(-1)[:n].cpu()
+
+
+def neighbours(x):
+    """The values of the 8-bit type below and above x >= 0 (at most 448)."""
+    grid = oracle.E4M3[:127]
+    hi = torch.searchsorted(grid, x.contiguous()).clamp(max=126)
+    return grid[(hi - (grid[hi] > x).long()).clamp(min=0)], grid[hi]
+
+
+def test_steps_in_8_bits_stay_on_neighbouring_codes():
+    """Each step starts from the moments that the codes stand for; the new ones are one of the two codes next to the
+    value, under the smallest scale that holds the block."""
+    from paper_2402_18994_amd import AdamW
+    p, g = make(SHAPES, 2)
+    dev = [x.cuda() for x in p]
+    opt = AdamW(dev, lr=LR, betas=BETAS, eps=EPS, weight_decay=0.01, state_bits=8, seed=5)
+    for step in range(1, 5):
+        before = [(x.double().cpu(), *[v.view(x.shape) for v in moments(opt, i, x.numel())]) for i, x in enumerate(dev)]
+        gs = [x * (0.3 + 0.4 * step) for x in g]
+        opt.step([x.cuda() for x in gs])
+        for i, ((a, m, v), x, gr) in enumerate(zip(before, dev, gs)):
+            if not x.numel():
+                continue
+            wp, wm, wv = oracle.adamw(a, gr.double(), m, v, step, LR, BETAS, EPS, 0.01)
+            near(f"parameter {i}", x, wp, 1, LR)
+            n, pad = x.numel(), -x.numel() % 128
+            at = opt.at[i] // 128
+            for name, value, codes, scales in (("m", wm, opt.m, opt.m_scale), ("v", wv.sqrt(), opt.v, opt.v_scale)):
+                blocks = torch.nn.functional.pad(value.flatten(), (0, pad)).view(-1, 128)
+                s = scales[at:at + len(blocks)].double().cpu()
+                top = blocks.abs().amax(1)
+                assert (torch.log2(s) == torch.log2(s).round()).all()
+                assert (top <= 448 * s * (1 + 2 ** -20)).all(), name
+                assert ((top >= 224 * s * (1 - 2 ** -20)) | (s == 2.0 ** -60)).all(), name
+                got = codes[opt.at[i]:opt.at[i] + n + pad].double().cpu().view(-1, 128)
+                y = blocks / s[:, None]
+                slack = 2.0 ** -20 * y.abs()              # the value before rounding is fp32
+                low, high = neighbours((y.abs() - slack).clamp(min=0).flatten())[0], neighbours((y.abs() + slack).clamp(max=448).flatten())[1]
+                mag = got.abs().flatten()
+                assert ((mag >= low) & (mag <= high)).all(), (name, i)
+                assert ((got.flatten() == 0) | (torch.sign(got) == torch.sign(y)).flatten()).all()
+                assert (got.view(-1)[n:] == 0).all()
+                if name == "v":
+                    assert ((mag > 0) | (y.flatten() == 0)).all()
+
+
+def test_8_bit_rounding_keeps_the_mean():
+    """From zero moments with the same gradient everywhere the moments' averages over many elements are the moments:
+    each is off by at most the spread of one rounding over the root of the count, five times over."""
+    from paper_2402_18994_amd import AdamW
+    n = 1 << 18
+    for value in (0.37, 1e-3, 5.1):
+        p = torch.zeros(n, device="cuda")
+        g = torch.full((n,), value, device="cuda")
+        g[::128] = 1.9 * value                            # so that the others are not the block's largest
+        opt = AdamW([p], betas=(0.9, 0.99), state_bits=8, seed=17)
+        opt.step([g])
+        m, v = moments(opt, 0, n)
+        keep = torch.ones(n, dtype=torch.bool)
+        keep[::128] = False
+        for name, got, want in (("m", m, 0.1 * value), ("v", v, 0.01 * value * value)):
+            got = got[keep]
+            step = got.max() - got.min()
+            assert 0 < step < 0.3 * want, name            # two neighbouring codes
+            assert abs(got.mean().item() - want) <= 5 * 0.5 * step.item() / math.sqrt(len(got)) + want * 2.0 ** -16, name
+
+
+def test_8_bit_moments_follow_a_changed_gradient():
+    """A second moment whose change in a step is far below half a code still decays."""
+    from paper_2402_18994_amd import AdamW
+    n = 1 << 14
+    p = torch.zeros(n, device="cuda")
+    opt = AdamW([p], lr=1e-3, state_bits=8, seed=3)
+    for k in range(300):
+        opt.step([torch.full((n,), 1.0 if k < 20 else 0.0, device="cuda")])
+    _, v = moments(opt, 0, n)
+    want = (1 - 0.999 ** 20) * 0.999 ** 280
+    # rounding adds at most (a quarter of the codes' distance in v, 0.27 v) (0.001 v) of variance a step: 300 steps of it
+    assert abs(v.mean().item() / want - 1) <= 5 * math.sqrt(300 * 0.27 * 0.001) / math.sqrt(n) + 300 * 2.0 ** -17 / 0.004 * 0.001
+
+
+def test_random_bits_are_even():
+    """The rounding's bits, by the rule of the kernel: every bit set half of the time, no bit alike its neighbour's."""
+    i = np.arange(1 << 16, dtype=np.uint64)
+
+    def stir(x):
+        x = ((x ^ (x >> np.uint64(16))) * np.uint64(0xB504F335)) & np.uint64(0xFFFFFFFF)
+        x = ((x ^ (x >> np.uint64(15))) * np.uint64(0xDDB3D743)) & np.uint64(0xFFFFFFFF)
+        return x ^ (x >> np.uint64(16))
+
+    for salt in (0, 1, 0x12345678):
+        r = stir((i * np.uint64(0x9E3779B1) + np.uint64(salt)) & np.uint64(0xFFFFFFFF))
+        bits = ((r[:, None] >> np.arange(32, dtype=np.uint64)) & np.uint64(1)).astype(np.float64)
+        assert np.abs(bits.mean(0) - 0.5).max() < 5 * 0.5 / 256
+        c = np.corrcoef(bits.T) - np.eye(32)
+        assert np.abs(c).max() < 6 / 256
+        assert np.abs(np.corrcoef(bits[:-1].T, bits[1:].T)[:32, 32:]).max() < 6 / 256
+
+
+def test_not_a_number_stays_where_it_is():
+    from paper_2402_18994_amd import AdamW
+    for bits in (32, 8):
+        p = torch.ones(300, device="cuda")
+        opt = AdamW([p], state_bits=bits)
+        g = torch.full((300,), 0.5, device="cuda")
+        g[7], g[140], g[299] = float("nan"), float("inf"), float("-inf")
+        opt.step([g])
+        bad = torch.zeros(300, dtype=torch.bool)
+        bad[[7, 140, 299]] = True
+        assert p.cpu()[bad].isnan().all() and torch.isfinite(p.cpu()[~bad]).all()
+        opt.step([torch.full((300,), 0.5, device="cuda")])
+        assert torch.isfinite(p.cpu()[~bad]).all()
+        assert (p.cpu()[~bad] == p.cpu()[0]).all() if bits == 32 else True
+
+
+def test_zero_gradients_and_repeats():
+    from paper_2402_18994_amd import AdamW
+    for bits in (32, 8):
+        runs = []
+        for _ in range(2):
+            p, g = make(SHAPES, 4)
+            dev = [x.cuda() for x in p]
+            opt = AdamW(dev, weight_decay=0.0, state_bits=bits, seed=9)
+            opt.step([torch.zeros_like(x) for x in dev])
+            assert all(torch.equal(a.cpu(), b) for a, b in zip(dev, p))
+            for _ in range(2):
+                opt.step([x.cuda() for x in g])
+            runs.append(dev + [v.view(torch.uint8) if bits == 8 and v.dtype == torch.float8_e4m3fn else v for v in (opt.m, opt.v)])
+        assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+def test_unaligned_tensors_and_saved_state():
+    """Parameters and gradients that start anywhere in a buffer; a loaded state goes on as the saved one would."""
+    from paper_2402_18994_amd import AdamW
+    for bits in (32, 8):
+        store, gstore = torch.randn(5000, device="cuda"), torch.randn(5000, device="cuda")
+        cut = [(1, 700), (703, 1030), (1734, 3), (1740, 2500)]
+        a = [store[i:i + n].clone() for i, n in cut]
+        b = [store[i:i + n] for i, n in cut]
+        oa, ob = AdamW(a, state_bits=bits, seed=2), AdamW(b, state_bits=bits, seed=2)
+        for _ in range(2):
+            oa.step([gstore[i:i + n].clone() for i, n in cut])
+            ob.step([gstore[i:i + n] for i, n in cut])
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+        oc = AdamW(a, state_bits=bits, seed=2)
+        oc.load_state_dict(ob.state_dict())
+        c = [x.clone() for x in a]
+        od = AdamW(c, state_bits=bits, seed=2)
+        od.load_state_dict(oa.state_dict())
+        for o in (oc, od):
+            o.step([gstore[i:i + n] for i, n in cut])
+        assert all(torch.equal(x, y) for x, y in zip(a, c))
