@@ -78,6 +78,33 @@ template <int L> __device__ __forceinline__ float sum_neighbours(float v) {
   return v;
 }
 
+// Sum of column `col` of partial sums [rows][cols], for a workgroup of 16 columns (threadIdx.x % 16) by 16 runs: run r
+// adds rows r, r + 16, .. with eight loads in flight, and the runs' sums are added in order.  Few columns and many rows
+// leave a launch like this to the latency of its loads: 5120 columns of 256 rows took 20 us with four runs of single
+// loads.  Every thread of the workgroup calls it; run 0 has the sum (of columns below `cols`).
+__device__ __forceinline__ float sum_column(const float *__restrict__ part, int64_t cols, int64_t col, int rows, float *lds) {
+  const int run = threadIdx.x >> 4;
+  float s = 0.f;
+  if (col < cols) {
+    const float *p = part + col;
+    int r = run;
+    for (; r + 112 < rows; r += 128) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = p[(r + 16 * u) * cols];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; r < rows; r += 16) s += p[r * cols];
+  }
+  lds[threadIdx.x] = s;
+  __syncthreads();
+  if (run == 0)
+#pragma unroll
+    for (int k = 1; k < 16; ++k) s += lds[k * 16 + threadIdx.x];
+  return s;
+}
+
 // Orders the LDS accesses of one wavefront for the compiler; the hardware keeps them in order by itself.
 __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");

@@ -263,19 +263,13 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvP a, const
   }
 }
 
-// dweight[d][k] and dbias[d]: sums of `rows` partial sums [W+1][D], four interleaved runs each.
+// dweight[d][k] and dbias[d]: sums of `rows` partial sums [W+1][D].
 __global__ __launch_bounds__(256) void conv_sum_kernel(const float *__restrict__ partial, int rows, int W, int D,
                                                        float *__restrict__ dweight, float *__restrict__ dbias) {
-  __shared__ float part[256];
-  const int col = threadIdx.x & 63, run = threadIdx.x >> 6;
-  const int64_t cols = (int64_t)(W + 1) * D, c = (int64_t)blockIdx.x * 64 + col;
-  float s = 0.f;
-  if (c < cols)
-    for (int r = run; r < rows; r += 4) s += partial[r * cols + c];
-  part[threadIdx.x] = s;
-  __syncthreads();
-  if (run == 0 && c < cols) {
-    s = ((part[col] + part[64 + col]) + part[128 + col]) + part[192 + col];
+  __shared__ float lds[256];
+  const int64_t cols = (int64_t)(W + 1) * D, c = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
+  const float s = sum_column(partial, cols, c, rows, lds);
+  if (threadIdx.x < 16 && c < cols) {
     const int k = (int)(c / D), d = (int)(c % D);
     if (k < W) dweight[(size_t)d * W + k] = s;
     else if (dbias) dbias[d] = s;
@@ -378,7 +372,7 @@ template <typename T, int VEC> int launch_backward(const snn_conv_args &a, const
     int rc = ops_launched("convolution backward");
     if (rc) return rc;
     const int64_t cols = (int64_t)(a.W + 1) * a.D;
-    hipLaunchKernelGGL(conv_sum_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(256), 0, st, ws, c.gy, a.W, a.D, g.dweight, g.dbias);
+    hipLaunchKernelGGL(conv_sum_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(256), 0, st, ws, c.gy, a.W, a.D, g.dweight, g.dbias);
     return ops_launched("convolution backward, sums");
   });
 }

@@ -2,7 +2,7 @@
 //   delta = softplus(dt + dt_bias),  h[t,n] = a[t,n] h[t-1,n] + delta x Bv[n],  a[t,n] = exp(delta A[n]),
 //   y = (sum_n Cv[n] h[t,n] + skip x) z sigmoid(z).
 //
-// Layout of the work.  A lane holds NS = 4 states of a channel; L = 1, 2, 4, 8 or 16 neighbouring lanes hold all of
+// Layout of the work.  A lane holds NS = 4 states of a channel; L = 4, 8 or 16 neighbouring lanes hold all of
 // them (N <= 4 L, states beyond N are zero), so a wavefront carries 64 / L channels, and the state never leaves the
 // registers.  Time goes in tiles of 16 steps: for a tile the 64 lanes first do what is once per (step, channel) -
 // loads, softplus, the products delta and delta x - spread evenly, and put it into LDS; then every lane steps through
@@ -14,6 +14,7 @@
 // is exp(A sum(delta)) times the state before it plus the chunk's own, so a first launch runs every chunk from zero
 // (scan_local_kernel), a second joins them in order (scan_join_kernel), and the third scans with the right states.
 // The reverse pass is cut the same way, from the other end.
+#include "common.hpp"
 #include "seq_common.hpp"
 
 #include <algorithm>
@@ -24,6 +25,9 @@ namespace {
 
 constexpr int TILE = 16;
 constexpr int NS = 4;
+#ifndef FENCE
+#define FENCE 16
+#endif
 
 struct ScanP {
   int T, B, D, N, G, softplus;
@@ -74,67 +78,116 @@ template <int L, int WAVES> struct Place {
   }
 };
 
+// The loads and address computations below are the same for all lanes: a lane without a channel, a state or a step of
+// its own takes another one's, and the value is replaced by zero afterwards.  Where lanes took turns instead, under high
+// register pressure, the compiler put copies of values that all lanes need later into the region where only some run.
+
 // Four states of [D][N] or [B][D][N] rows, zero beyond N.
 __device__ __forceinline__ void load4(float r[NS], const float *row, int part, int N, bool live) {
 #pragma unroll
-  for (int j = 0; j < NS; ++j) r[j] = live && row && part * NS + j < N ? row[part * NS + j] : 0.f;
+  for (int j = 0; j < NS; ++j) r[j] = 0.f;
+  if (row)
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      const float v = row[min(part * NS + j, N - 1)];
+      r[j] = live & (part * NS + j < N) ? v : 0.f;
+    }
 }
 __device__ __forceinline__ void store4(float *row, const float r[NS], int part, int N) {
 #pragma unroll
   for (int j = 0; j < NS; ++j)
     if (part * NS + j < N) row[part * NS + j] = r[j];
 }
-
-// Rows of Bv (and Cv) of a tile into LDS as fp32 [TILE][NP], zero beyond N and for steps that do not exist.  COUNT
-// threads share the work; `me` is this one's number.
-template <typename T, int NP, int COUNT>
-__device__ __forceinline__ void fetch_rows(T r[(TILE * NP + COUNT - 1) / COUNT], const Rows<void> &src, int b, int g, int N, int t0, int end, int me) {
-  constexpr int EACH = (TILE * NP + COUNT - 1) / COUNT;
-  const T *base = (const T *)src.p + b * src.sb + (int64_t)g * N;
-#pragma unroll
-  for (int i = 0; i < EACH; ++i) {
-    const int at = i * COUNT + me, t = t0 + at / NP, n = at % NP;
-    r[i] = (T)0.f;
-    if (at < TILE * NP && n < N && t < end) r[i] = base[(int64_t)t * src.st + n];
-  }
-}
-template <typename T, int NP, int COUNT>
-__device__ __forceinline__ void put_rows(float *lds, const T r[(TILE * NP + COUNT - 1) / COUNT], int me) {
-  constexpr int EACH = (TILE * NP + COUNT - 1) / COUNT;
-#pragma unroll
-  for (int i = 0; i < EACH; ++i) {
-    const int at = i * COUNT + me;
-    if (at < TILE * NP) lds[at] = widen(r[i]);
-  }
+__device__ __forceinline__ void take4(float r[NS], const float4 *p, bool live) {
+  const float4 v = *p;
+  r[0] = live ? v.x : 0.f;
+  r[1] = live ? v.y : 0.f;
+  r[2] = live ? v.z : 0.f;
+  r[3] = live ? v.w : 0.f;
 }
 
-// E values of a streamed tensor in the elementwise mapping: step et + i TILE / E of the tile, channel ed.
-template <typename T, int E>
-__device__ __forceinline__ void fetch(T r[E], const Rows<void> &src, int b, int d, int t0, int et, int end, bool live) {
-  const T *base = (const T *)src.p + b * src.sb + d;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int t = t0 + et + i * (TILE / E);
-    r[i] = (T)0.f;
-    if (live && t < end) r[i] = base[(int64_t)t * src.st];
-  }
+// Streamed tensors go through buffer instructions: a base that the whole wavefront shares (tensor, sequence, tile), the
+// byte offset of the lane in it (channel, step within the tile: one register, computed once) and a scalar offset for
+// the steps of a round.  The host keeps lane offsets below SPAN (scan_strides); a store at NOWHERE is dropped.
+constexpr int SPAN = 0x7FFF0000, NOWHERE = 0x7FFFFF00;
+__device__ __forceinline__ float take(rsrc_t r, int voff, int soff, float) { return __uint_as_float(ld_b32(r, voff, soff)); }
+__device__ __forceinline__ __bf16 take(rsrc_t r, int voff, int soff, __bf16) {
+  return __builtin_bit_cast(__bf16, (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(r, voff, soff, 0));
 }
-template <typename T, int E>
-__device__ __forceinline__ void put(const Rows<void> &dst, const float r[E], int b, int d, int t0, int et, int end, bool live) {
-  T *base = (T *)dst.p + b * dst.sb + d;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int t = t0 + et + i * (TILE / E);
-    if (live && t < end) base[(int64_t)t * dst.st] = narrow<T>(r[i]);
+__device__ __forceinline__ void give(rsrc_t r, int voff, int soff, float v) { st_b32(r, voff, soff, __float_as_uint(v)); }
+__device__ __forceinline__ void give(rsrc_t r, int voff, int soff, __bf16 v) { st_b16(r, voff, soff, __builtin_bit_cast(unsigned short, v)); }
+
+// What a lane loads of the rows of Bv (or Cv), COUNT threads sharing a tile of TILE x NP values: value n of step
+// et + i COUNT / NP.  In LDS they stand as fp32 [TILE][NP], zero beyond N and for steps that do not exist.
+template <typename T, int NP, int COUNT> struct Vectors {
+  static constexpr int STEP = COUNT / NP, EACH = TILE / STEP;
+  static_assert(STEP * EACH == TILE, "a tile is a whole number of rounds");
+  const T *p;
+  int64_t st;
+  int et, n, at, row;                // `at`: the lane's offset; `row`: bytes between steps
+  bool on;
+  T r[EACH];
+  __device__ Vectors(const Rows<void> &src, int b, int g, int N, int me)
+      : p((const T *)src.p + b * src.sb + (int64_t)g * N), st(src.st), et(me / NP), n(me % NP), row((int)(src.st * sizeof(T))), on(me % NP < N) {
+    at = min(n, N - 1) * (int)sizeof(T) + et * row;
   }
-}
+  __device__ __forceinline__ void fetch_whole(int t0) {
+    const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) r[i] = take(q, at, i * STEP * row, (T)0.f);
+  }
+  __device__ __forceinline__ void fetch(int t0, int end) {
+    if (t0 + TILE <= end) {                                 // (a tile that is there as a whole, as nearly all are)
+      fetch_whole(t0);
+    } else {
+      const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) r[i] = take(q, at + (min(et + i * STEP, end - 1 - t0) - et) * row, 0, (T)0.f);
+    }
+  }
+  __device__ __forceinline__ void put(float *lds, int t0, int end) const {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) lds[(et + i * STEP) * NP + n] = on & (t0 + et + i * STEP < end) ? widen(r[i]) : 0.f;
+  }
+};
+
+// What a lane loads or stores of a streamed tensor in the elementwise mapping: channel ed, steps et + i TILE / E.
+template <typename T, int E> struct Stream {
+  static constexpr int STEP = TILE / E;
+  T *p;
+  int64_t st;
+  int et, at, row;
+  T r[E];
+  __device__ Stream(const Rows<void> &src, int b, int d, int et_) : p((T *)src.p + b * src.sb), st(src.st), et(et_), row((int)(src.st * sizeof(T))) {
+    at = d * (int)sizeof(T) + et * row;
+  }
+  __device__ __forceinline__ void fetch_whole(int t0) {
+    const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
+#pragma unroll
+    for (int i = 0; i < E; ++i) r[i] = take(q, at, i * STEP * row, (T)0.f);
+  }
+  __device__ __forceinline__ void fetch(int t0, int end) {
+    if (t0 + TILE <= end) {
+      fetch_whole(t0);
+    } else {
+      const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
+#pragma unroll
+      for (int i = 0; i < E; ++i) r[i] = take(q, at + (min(et + i * STEP, end - 1 - t0) - et) * row, 0, (T)0.f);
+    }
+  }
+  __device__ __forceinline__ void put(const float v[E], int t0, int end, bool live) const {
+    const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
+#pragma unroll
+    for (int i = 0; i < E; ++i) give(q, live & (t0 + et + i * STEP < end) ? at : NOWHERE, i * STEP * row, narrow<T>(v[i]));
+  }
+};
 
 // ---------------------------------------------------------------- forward
 // LOCAL: the chunk from zero, for its end state and its sum of delta alone; no outputs.
-template <typename T, int L, int WAVES, bool LOCAL>
+template <typename T, int L, int WAVES, bool GATE, bool LOCAL>
 __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p) {
   using P = Place<L, WAVES>;
-  constexpr int CH = P::CH, E = P::E, NP = NS * L;
+  constexpr int CH = P::CH, E = P::E, NP = NS * L, KEEP = TILE / L;
   __shared__ float2 s_d[WAVES][TILE * CH];
   __shared__ __attribute__((aligned(16))) float s_b[WAVES][TILE * NP], s_c[WAVES][LOCAL ? 4 : TILE * NP];
   __shared__ float s_y[WAVES][LOCAL ? 4 : TILE * CH];
@@ -150,80 +203,87 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
   for (int j = 0; j < NS; ++j) { A[j] *= LOG2E; h[j] = 0.f; }
   if constexpr (!LOCAL) {
     if (p.nchunks > 1) {
-      if (me.live) {
-        const float4 v = p.local[((size_t)me.s * p.B * p.D + seq) * L + me.part];
-        h[0] = v.x; h[1] = v.y; h[2] = v.z; h[3] = v.w;
-      }
+      take4(h, p.local + ((size_t)me.s * p.B * p.D + seq) * L + me.part, me.live);
     } else {
       load4(h, p.init ? p.init + seq * p.N : nullptr, me.part, p.N, me.live);
     }
   }
   const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f, skip = p.skip ? p.skip[me.ed] : 0.f;
 
-  T rx[E], rd[E], rz[E], rb[L], rc[L];                    // (TILE * NP values by 64 lanes are L each)
+  Stream<T, E> gx(p.x, me.b, me.ed, me.et), gd(p.dt, me.b, me.ed, me.et), gz(p.z, me.b, me.ed, me.et), gy(p.y, me.b, me.ed, me.et);
+  Vectors<T, NP, 64> gb(p.bv, me.b, me.g, p.N, me.lane), gc(p.cv, me.b, me.g, p.N, me.lane);
   auto load = [&](int t0) {
-    fetch<T, E>(rx, p.x, me.b, me.ed, t0, me.et, end, me.elive);
-    fetch<T, E>(rd, p.dt, me.b, me.ed, t0, me.et, end, me.elive);
-    fetch_rows<T, NP, 64>(rb, p.bv, me.b, me.g, p.N, t0, end, me.lane);
+    gx.fetch(t0, end);
+    gd.fetch(t0, end);
+    gb.fetch(t0, end);
     if constexpr (!LOCAL) {
-      if (p.z.p) fetch<T, E>(rz, p.z, me.b, me.ed, t0, me.et, end, me.elive);
-      fetch_rows<T, NP, 64>(rc, p.cv, me.b, me.g, p.N, t0, end, me.lane);
+      if constexpr (GATE) gz.fetch(t0, end);
+      gc.fetch(t0, end);
     }
   };
-  load(c0);
-  for (int t0 = c0; t0 < (LOCAL ? end : c1); t0 += TILE) {
+  if (c0 < end) load(c0);
+  int t0 = c0;
+  for (; t0 < end; t0 += TILE) {
     float x[E], z[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int t = me.et + i * (TILE / E);
-      const float raw = widen(rd[i]) + dt_bias;
-      x[i] = widen(rx[i]);
-      z[i] = LOCAL ? 0.f : widen(rz[i]);
-      const float delta = t0 + t < end && me.elive ? (p.softplus ? softplus(raw) : raw) : 0.f;
+      const bool on = (t0 + t < end) & me.elive;
+      const float raw = widen(gd.r[i]) + dt_bias;
+      x[i] = on ? widen(gx.r[i]) : 0.f;
+      z[i] = !LOCAL && GATE ? widen(gz.r[i]) : 0.f;
+      const float soft = softplus(raw), delta = on ? (p.softplus ? soft : raw) : 0.f;
       sd[t * CH + me.ec] = make_float2(delta, delta * x[i]);
     }
-    put_rows<T, NP, 64>(sb, rb, me.lane);
-    if constexpr (!LOCAL) put_rows<T, NP, 64>(sc, rc, me.lane);
+    gb.put(sb, t0, end);
+    if constexpr (!LOCAL) gc.put(sc, t0, end);
     if (t0 + TILE < end) load(t0 + TILE);
     wave_lds_order();
     if constexpr (!LOCAL) {
       if (p.saved && me.live)
         p.saved[((size_t)(t0 / TILE) * p.B * p.D + seq) * L + me.part] = make_float4(h[0], h[1], h[2], h[3]);
     }
-    if (t0 < end) {
+    float keep[KEEP];                                       // outputs of the steps whose number mod L is this lane's part
 #pragma unroll
-      for (int t = 0; t < TILE; ++t) {
-        const float2 u = sd[t * CH + me.ch];
-        const float4 b4 = *(const float4 *)(sb + t * NP + me.part * NS);
-        const float bq[NS] = {b4.x, b4.y, b4.z, b4.w};
+    for (int t = 0; t < TILE; ++t) {
+      const float2 u = sd[t * CH + me.ch];
+      const float4 b4 = *(const float4 *)(sb + t * NP + me.part * NS);
+      const float bq[NS] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
-        for (int j = 0; j < NS; ++j) h[j] = fmaf(__builtin_amdgcn_exp2f(u.x * A[j]), h[j], u.y * bq[j]);
-        if constexpr (LOCAL) {
-          sum += u.x;
-        } else {
-          const float4 c4 = *(const float4 *)(sc + t * NP + me.part * NS);
-          float v = c4.x * h[0];
-          v = fmaf(c4.y, h[1], v);
-          v = fmaf(c4.z, h[2], v);
-          v = fmaf(c4.w, h[3], v);
-          v = sum_neighbours<L>(v);
-          if (me.part == 0) sy[t * CH + me.ch] = v;
-        }
+      for (int j = 0; j < NS; ++j) h[j] = fmaf(__builtin_amdgcn_exp2f(u.x * A[j]), h[j], u.y * bq[j]);
+      if constexpr (LOCAL) {
+        sum += u.x;
+      } else {
+        const float4 c4 = *(const float4 *)(sc + t * NP + me.part * NS);
+        float v = c4.x * h[0];
+        v = fmaf(c4.y, h[1], v);
+        v = fmaf(c4.z, h[2], v);
+        v = fmaf(c4.w, h[3], v);
+        v = sum_neighbours<L>(v);
+        keep[t / L] = t % L == 0 || me.part == t % L ? v : keep[t / L];
       }
     }
     if constexpr (!LOCAL) {
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i) sy[(i * L + me.part) * CH + me.ch] = keep[i];
       wave_lds_order();
       float out[E];
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         const int t = me.et + i * (TILE / E);
-        float v = sy[t * CH + me.ec] + skip * x[i];
-        if (p.z.p) v *= z[i] * sigmoid_fast(z[i]);
+        float v = fmaf(skip, x[i], sy[t * CH + me.ec]);
+        if constexpr (GATE) v *= z[i] * sigmoid_fast(z[i]);
         out[i] = t0 + t < end ? v : 0.f;
       }
-      put<T, E>(p.y, out, me.b, me.ed, t0, me.et, c1, me.elive);
+      gy.put(out, t0, c1, me.elive);
     }
     wave_lds_order();
+  }
+  if constexpr (!LOCAL) {
+    float zero[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) zero[i] = 0.f;
+    for (; t0 < c1; t0 += TILE) gy.put(zero, t0, c1, me.elive);          // steps that do not exist
   }
   if (!me.live) return;
   if constexpr (LOCAL) {
@@ -263,7 +323,7 @@ template <int L, bool REVERSE> __global__ __launch_bounds__(256) void scan_join_
 
 // ---------------------------------------------------------------- reverse
 // The chunk from a zero gradient behind it: the gradient of the state before it and the sum of delta.
-template <typename T, int L, int WAVES>
+template <typename T, int L, int WAVES, bool GATE>
 __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const ScanP p, const ScanGradP g) {
   using P = Place<L, WAVES>;
   constexpr int CH = P::CH, E = P::E, NP = NS * L;
@@ -280,12 +340,13 @@ __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const Sc
 #pragma unroll
   for (int j = 0; j < NS; ++j) { A[j] *= LOG2E; q[j] = 0.f; }
   const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f;
-  T ry[E], rd[E], rz[E], rc[L];
+  Stream<T, E> gy(g.dy, me.b, me.ed, me.et), gd(p.dt, me.b, me.ed, me.et), gz(p.z, me.b, me.ed, me.et);
+  Vectors<T, NP, 64> gc(p.cv, me.b, me.g, p.N, me.lane);
   auto load = [&](int t0) {
-    fetch<T, E>(ry, g.dy, me.b, me.ed, t0, me.et, end, me.elive);
-    fetch<T, E>(rd, p.dt, me.b, me.ed, t0, me.et, end, me.elive);
-    if (p.z.p) fetch<T, E>(rz, p.z, me.b, me.ed, t0, me.et, end, me.elive);
-    fetch_rows<T, NP, 64>(rc, p.cv, me.b, me.g, p.N, t0, end, me.lane);
+    gy.fetch(t0, end);
+    gd.fetch(t0, end);
+    if constexpr (GATE) gz.fetch(t0, end);
+    gc.fetch(t0, end);
   };
   const int tiles = end > c0 ? (end - c0 + TILE - 1) / TILE : 0;
   if (tiles) load(c0 + (tiles - 1) * TILE);
@@ -294,13 +355,14 @@ __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const Sc
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int t = me.et + i * (TILE / E);
-      const float raw = widen(rd[i]) + dt_bias;
-      float dy = widen(ry[i]);
-      if (p.z.p) { const float z = widen(rz[i]); dy *= z * sigmoid_fast(z); }
-      const bool on = t0 + t < end && me.elive;
-      sd[t * CH + me.ec] = make_float2(on ? (p.softplus ? softplus(raw) : raw) : 0.f, on ? dy : 0.f);
+      const float raw = widen(gd.r[i]) + dt_bias;
+      float dy = widen(gy.r[i]);
+      if constexpr (GATE) { const float z = widen(gz.r[i]); dy *= z * sigmoid_fast(z); }
+      const bool on = (t0 + t < end) & me.elive;
+      const float soft = softplus(raw);
+      sd[t * CH + me.ec] = make_float2(on ? (p.softplus ? soft : raw) : 0.f, on ? dy : 0.f);
     }
-    put_rows<T, NP, 64>(sc, rc, me.lane);
+    gc.put(sc, t0, end);
     if (i0 > 0) load(t0 - TILE);
     wave_lds_order();
 #pragma unroll
@@ -340,8 +402,6 @@ template <int L> __device__ __forceinline__ float2 sum_channels(const float v[2 
   for (int j = 0; j < 2; ++j) {
     if constexpr (L <= 8) c[j] += dpp<0x128>(c[j]);
     if constexpr (L <= 4) c[j] += dpp<0x124>(c[j]);
-    if constexpr (L <= 2) c[j] += dpp<0x122>(c[j]);
-    if constexpr (L <= 1) c[j] += dpp<0x121>(c[j]);
   }
   return make_float2(c[0], c[1]);
 }
@@ -352,16 +412,21 @@ template <int L> __device__ __forceinline__ float2 sum_channels(const float v[2 
 //   d(delta) = sum_n u A + x sum_n g B,   dx = delta sum_n g B + dy0 skip,   dA += u delta,   q = g a.
 // The workgroup's wavefronts share the rows of Bv and Cv, and add their channel sums of dBv and dCv through LDS in a
 // fixed order; sums over workgroups are left to scan_sum_rows_kernel.
-template <typename T, int L, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void scan_reverse_kernel(const ScanP p, const ScanGradP g) {
+template <typename T, int L, int WAVES, bool GATE>
+__global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP p, const ScanGradP g) {
   using P = Place<L, WAVES>;
-  constexpr int CH = P::CH, E = P::E, NP = NS * L, THREADS = 64 * WAVES;
-  constexpr int EACH = (TILE * NP + THREADS - 1) / THREADS;
-  __shared__ float4 s_d[WAVES][TILE * CH];                  // delta, delta x, dy0 and sum C h, then sum g B, sum u A
+  constexpr int CH = P::CH, E = P::E, NP = NS * L, THREADS = 64 * WAVES, KEEP = TILE / L, TWINS = 16 / L, HALF = TILE / 2;
+  __shared__ float4 s_d[WAVES][TILE * CH];                  // delta, delta x, dy0, d(delta) / d(dt)
+  __shared__ float s_y[WAVES][TILE * CH];                   // sum C h
+  __shared__ float2 s_g[WAVES][TILE * CH];                  // sum g B, sum u A
+  __shared__ float4 s_h[WAVES][(HALF - 1) * 64];            // states of the first half of a tile
   __shared__ __attribute__((aligned(16))) float s_b[TILE * NP], s_c[TILE * NP];
   __shared__ __attribute__((aligned(8))) float s_s[WAVES][2][TILE * NP];
   const P me(p);
   float4 *sd = s_d[me.wave];
+  float *sy = s_y[me.wave];
+  float2 *sg = s_g[me.wave];
+  float4 *sh = s_h[me.wave] + me.lane;
   const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, length_of(p.lengths, me.b, p.T));
   const size_t seq = (size_t)me.b * p.D + me.d;
   float A[NS], A2[NS], q[NS], dA[NS] = {0.f, 0.f, 0.f, 0.f};
@@ -369,141 +434,177 @@ __global__ __launch_bounds__(64 * WAVES) void scan_reverse_kernel(const ScanP p,
 #pragma unroll
   for (int j = 0; j < NS; ++j) A2[j] = A[j] * LOG2E;
   if (p.nchunks > 1) {
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (me.live) v = p.local[((size_t)me.s * p.B * p.D + seq) * L + me.part];
-    q[0] = v.x; q[1] = v.y; q[2] = v.z; q[3] = v.w;
+    take4(q, p.local + ((size_t)me.s * p.B * p.D + seq) * L + me.part, me.live);
   } else {
     load4(q, g.d_state ? g.d_state + seq * p.N : nullptr, me.part, p.N, me.live);
   }
   const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f, skip = p.skip ? p.skip[me.ed] : 0.f;
   float dskip = 0.f, ddtb = 0.f;
 
-  T rx[E], rd[E], rz[E], ry[E], rb[EACH], rc[EACH];
+  Stream<T, E> gx(p.x, me.b, me.ed, me.et), gd(p.dt, me.b, me.ed, me.et), gy(g.dy, me.b, me.ed, me.et), gz(p.z, me.b, me.ed, me.et);
+  const Stream<T, E> wx(g.dx, me.b, me.ed, me.et), wd(g.ddt, me.b, me.ed, me.et), wz(g.dz, me.b, me.ed, me.et);
+  Vectors<T, NP, THREADS> gb(p.bv, me.b, me.g, p.N, threadIdx.x), gc(p.cv, me.b, me.g, p.N, threadIdx.x);
   float4 rh = make_float4(0.f, 0.f, 0.f, 0.f);
   auto load = [&](int t0) {
-    fetch<T, E>(rx, p.x, me.b, me.ed, t0, me.et, end, me.elive);
-    fetch<T, E>(rd, p.dt, me.b, me.ed, t0, me.et, end, me.elive);
-    fetch<T, E>(ry, g.dy, me.b, me.ed, t0, me.et, end, me.elive);
-    if (p.z.p) fetch<T, E>(rz, p.z, me.b, me.ed, t0, me.et, end, me.elive);
-    fetch_rows<T, NP, THREADS>(rb, p.bv, me.b, me.g, p.N, t0, end, threadIdx.x);
-    fetch_rows<T, NP, THREADS>(rc, p.cv, me.b, me.g, p.N, t0, end, threadIdx.x);
-    if (me.live) rh = p.saved[((size_t)(t0 / TILE) * p.B * p.D + seq) * L + me.part];
+    gx.fetch(t0, end);
+    gd.fetch(t0, end);
+    gy.fetch(t0, end);
+    if constexpr (GATE) gz.fetch(t0, end);
+    gb.fetch(t0, end);
+    gc.fetch(t0, end);
+    rh = p.saved[((size_t)(t0 / TILE) * p.B * p.D + seq) * L + me.part];
   };
   const int tiles = end > c0 ? (end - c0 + TILE - 1) / TILE : 0;
-  const int rows = (c1 - c0 + TILE - 1) / TILE;             // tiles with rows to write, those that do not exist among them
   {
     float zero[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) zero[i] = 0.f;
-    for (int i0 = tiles; i0 < rows; ++i0) {
-      const int t0 = c0 + i0 * TILE;
-      put<T, E>(g.dx, zero, me.b, me.ed, t0, me.et, c1, me.elive);
-      put<T, E>(g.ddt, zero, me.b, me.ed, t0, me.et, c1, me.elive);
-      if (p.z.p) put<T, E>(g.dz, zero, me.b, me.ed, t0, me.et, c1, me.elive);
+    for (int t0 = c0 + tiles * TILE; t0 < c1; t0 += TILE) {                // steps that do not exist
+      wx.put(zero, t0, c1, me.elive);
+      wd.put(zero, t0, c1, me.elive);
+      if constexpr (GATE) wz.put(zero, t0, c1, me.elive);
     }
   }
   if (tiles) load(c0 + (tiles - 1) * TILE);
   for (int i0 = tiles - 1; i0 >= 0; --i0) {
     const int t0 = c0 + i0 * TILE;
-    float x[E], z[E], dy[E], delta[E], slope[E];
+    float x[E], z[E], dy[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int t = me.et + i * (TILE / E);
-      const bool on = t0 + t < end && me.elive;
-      const float raw = widen(rd[i]) + dt_bias;
-      x[i] = widen(rx[i]);
-      dy[i] = widen(ry[i]);
-      z[i] = p.z.p ? widen(rz[i]) : 0.f;
+      const bool on = (t0 + t < end) & me.elive;
+      const float raw = widen(gd.r[i]) + dt_bias;
+      x[i] = on ? widen(gx.r[i]) : 0.f;
+      dy[i] = on ? widen(gy.r[i]) : 0.f;
+      z[i] = GATE && on ? widen(gz.r[i]) : 0.f;
       const float e = exp_fast(-fabsf(raw)), r = rcp_fast(1.f + e);
-      delta[i] = on ? (p.softplus ? softplus(raw) : raw) : 0.f;
-      slope[i] = p.softplus ? (raw >= 0.f ? r : e * r) : 1.f;       // d(delta) / d(dt)
-      const float dy0 = p.z.p ? dy[i] * z[i] * sigmoid_fast(z[i]) : dy[i];
-      sd[t * CH + me.ec] = make_float4(delta[i], delta[i] * x[i], dy0, 0.f);
+      const float soft = softplus(raw), delta = on ? (p.softplus ? soft : raw) : 0.f;
+      const float slope = p.softplus ? (raw >= 0.f ? r : e * r) : 1.f;
+      const float dy0 = GATE ? dy[i] * z[i] * sigmoid_fast(z[i]) : dy[i];
+      sd[t * CH + me.ec] = make_float4(delta, delta * x[i], dy0, slope);
     }
-    put_rows<T, NP, THREADS>(s_b, rb, threadIdx.x);
-    put_rows<T, NP, THREADS>(s_c, rc, threadIdx.x);
-    float h[TILE + 1][NS], a[TILE][NS];
-    h[0][0] = rh.x; h[0][1] = rh.y; h[0][2] = rh.z; h[0][3] = rh.w;
+    gb.put(s_b, t0, end);
+    gc.put(s_c, t0, end);
+    float h0[NS] = {me.live ? rh.x : 0.f, me.live ? rh.y : 0.f, me.live ? rh.z : 0.f, me.live ? rh.w : 0.f};
+    float h[HALF + 1][NS], a[TILE][NS];                     // h: of the steps from HALF - 1 on
     __syncthreads();
-    if (i0 > 0) load(t0 - TILE);
+    float k0[KEEP], k1[KEEP];                               // of the steps whose number mod L is this lane's part
+    {
+      float hn[NS] = {h0[0], h0[1], h0[2], h0[3]};
 #pragma unroll
-    for (int t = 0; t < TILE; ++t) {
-      const float2 u = *(const float2 *)(sd + t * CH + me.ch);
-      const float4 b4 = *(const float4 *)(s_b + t * NP + me.part * NS);
-      const float bq[NS] = {b4.x, b4.y, b4.z, b4.w};
+      for (int t = 0; t < TILE; ++t) {
+
+        if (t % FENCE == 0) __builtin_amdgcn_sched_barrier(0);
+        const float2 u = *(const float2 *)(sd + t * CH + me.ch);
+        const float4 b4 = *(const float4 *)(s_b + t * NP + me.part * NS);
+        const float bq[NS] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
-      for (int j = 0; j < NS; ++j) {
-        a[t][j] = __builtin_amdgcn_exp2f(u.x * A2[j]);
-        h[t + 1][j] = fmaf(a[t][j], h[t][j], u.y * bq[j]);
+        for (int j = 0; j < NS; ++j) {
+          a[t][j] = __builtin_amdgcn_exp2f(u.x * A2[j]);
+          hn[j] = fmaf(a[t][j], hn[j], u.y * bq[j]);
+          if (t >= HALF - 1) h[t - HALF + 1][j] = hn[j];
+        }
+        if (t < HALF - 1) sh[t * 64] = make_float4(hn[0], hn[1], hn[2], hn[3]);
+        if constexpr (GATE) {                                         // dz needs the output before the gate
+          const float4 c4 = *(const float4 *)(s_c + t * NP + me.part * NS);
+          float v = c4.x * hn[0];
+          v = fmaf(c4.y, hn[1], v);
+          v = fmaf(c4.z, hn[2], v);
+          v = fmaf(c4.w, hn[3], v);
+          v = sum_neighbours<L>(v);
+          k0[t / L] = t % L == 0 || me.part == t % L ? v : k0[t / L];
+        }
       }
-      if (p.z.p) {                                          // dz needs the output before the gate
-        const float4 c4 = *(const float4 *)(s_c + t * NP + me.part * NS);
-        float v = c4.x * h[t + 1][0];
-        v = fmaf(c4.y, h[t + 1][1], v);
-        v = fmaf(c4.z, h[t + 1][2], v);
-        v = fmaf(c4.w, h[t + 1][3], v);
-        v = sum_neighbours<L>(v);
-        if (me.part == 0) sd[t * CH + me.ch].w = v;
-      }
+      if constexpr (GATE)
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) sy[(i * L + me.part) * CH + me.ch] = k0[i];
     }
-    wave_lds_order();
+    asm volatile("" ::: "memory");                          // (the rows of Bv, Cv and sd are read again, not kept in registers)
+    float hc[NS];                                           // the state after step t
+    float2 kv[TILE / TWINS];                                // of the steps whose number mod TWINS is this lane's among its twins
 #pragma unroll
     for (int t = TILE - 1; t >= 0; --t) {
+      if (t == HALF - 1 && i0 > 0) {                        // the tile in front; here half of the registers of h and a are free again
+        const int next = t0 - TILE;
+        gx.fetch_whole(next);
+        gd.fetch_whole(next);
+        gy.fetch_whole(next);
+        if constexpr (GATE) gz.fetch_whole(next);
+        gb.fetch_whole(next);
+        gc.fetch_whole(next);
+        rh = p.saved[((size_t)(next / TILE) * p.B * p.D + seq) * L + me.part];
+      }
+      if (t % FENCE == FENCE - 1) __builtin_amdgcn_sched_barrier(0);
       const float4 u = sd[t * CH + me.ch];
       const float4 b4 = *(const float4 *)(s_b + t * NP + me.part * NS);
       const float4 c4 = *(const float4 *)(s_c + t * NP + me.part * NS);
       const float bq[NS] = {b4.x, b4.y, b4.z, b4.w}, cq[NS] = {c4.x, c4.y, c4.z, c4.w};
-      float v[2 * NS], gb = 0.f, ua = 0.f;
+      float v[2 * NS], gsum = 0.f, usum = 0.f, hp[NS];
+      if (t > 0 && t < HALF) {
+        const float4 r = sh[(t - 1) * 64];
+        hp[0] = r.x; hp[1] = r.y; hp[2] = r.z; hp[3] = r.w;
+      }
 #pragma unroll
       for (int j = 0; j < NS; ++j) {
+        if (t == TILE - 1) hc[j] = h[HALF][j];
+        if (t >= HALF) hp[j] = h[t - HALF][j];
+        if (t == 0) hp[j] = h0[j];
         const float gh = fmaf(u.z, cq[j], q[j]);
         v[j] = gh * u.y;
-        v[NS + j] = u.z * h[t + 1][j];
-        gb = fmaf(gh, bq[j], gb);
+        v[NS + j] = u.z * hc[j];
+        gsum = fmaf(gh, bq[j], gsum);
         q[j] = gh * a[t][j];
-        const float w = q[j] * h[t][j];
-        ua = fmaf(w, A[j], ua);
+        const float w = q[j] * hp[j];
+        hc[j] = hp[j];
+        usum = fmaf(w, A[j], usum);
         dA[j] = fmaf(w, u.x, dA[j]);
       }
-      gb = sum_neighbours<L>(gb);
-      ua = sum_neighbours<L>(ua);
-      if (me.part == 0) { sd[t * CH + me.ch].x = gb; sd[t * CH + me.ch].y = ua; }
+      gsum = sum_neighbours<L>(gsum);
+      usum = sum_neighbours<L>(usum);
+      const bool mine = t % L == L - 1 || me.part == t % L;
+      k0[t / L] = mine ? gsum : k0[t / L];
+      k1[t / L] = mine ? usum : k1[t / L];
       const float2 s = sum_channels<L>(v);
-      if ((me.lane & 15) < L)
-        *(float2 *)(&s_s[me.wave][me.lane >> 5][t * NP + me.part * NS + ((me.lane >> 4) & 1) * 2]) = s;
+      const bool twin = t % TWINS == TWINS - 1 || (me.lane & 15) / L == t % TWINS;
+      kv[t / TWINS].x = twin ? s.x : kv[t / TWINS].x;
+      kv[t / TWINS].y = twin ? s.y : kv[t / TWINS].y;
     }
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) sg[(i * L + me.part) * CH + me.ch] = make_float2(k0[i], k1[i]);
+#pragma unroll
+    for (int i = 0; i < TILE / TWINS; ++i)
+      *(float2 *)(&s_s[me.wave][me.lane >> 5][(i * TWINS + (me.lane & 15) / L) * NP + me.part * NS + ((me.lane >> 4) & 1) * 2]) = kv[i];
     wave_lds_order();
     float ox[E], od[E], oz[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int t = me.et + i * (TILE / E);
-      const bool on = t0 + t < end && me.elive;
-      const float4 r = sd[t * CH + me.ec];
-      float dy0 = dy[i];
-      oz[i] = 0.f;
-      if (p.z.p) {
-        const float e = sigmoid_fast(z[i]);
-        dy0 = dy[i] * z[i] * e;
-        oz[i] = on ? dy[i] * (r.w + skip * x[i]) * e * (1.f + z[i] * (1.f - e)) : 0.f;
+      const bool on = (t0 + t < end) & me.elive;
+      const float4 u = sd[t * CH + me.ec];
+      const float2 r = sg[t * CH + me.ec];
+      if constexpr (GATE) {
+        const float e = sigmoid_fast(z[i]), v = dy[i] * (sy[t * CH + me.ec] + skip * x[i]) * e * (1.f + z[i] * (1.f - e));
+        oz[i] = on ? v : 0.f;
       }
-      ox[i] = on ? fmaf(delta[i], r.x, dy0 * skip) : 0.f;
-      od[i] = on ? fmaf(x[i], r.x, r.y) * slope[i] : 0.f;
+      const float vx = fmaf(u.x, r.x, u.z * skip), vd = fmaf(x[i], r.x, r.y) * u.w;
+      ox[i] = on ? vx : 0.f;
+      od[i] = on ? vd : 0.f;
       ddtb += od[i];
-      if (on) dskip = fmaf(dy0, x[i], dskip);
+      dskip = fmaf(u.z, x[i], dskip);
     }
-    put<T, E>(g.dx, ox, me.b, me.ed, t0, me.et, c1, me.elive);
-    put<T, E>(g.ddt, od, me.b, me.ed, t0, me.et, c1, me.elive);
-    if (p.z.p) put<T, E>(g.dz, oz, me.b, me.ed, t0, me.et, c1, me.elive);
+    wx.put(ox, t0, c1, me.elive);
+    wd.put(od, t0, c1, me.elive);
+    if constexpr (GATE) wz.put(oz, t0, c1, me.elive);
     __syncthreads();
+    const int pitch = p.B * p.G * 2 * NP * 4;               // bytes between steps (scan_sizes: 16 of them stay below SPAN)
+    const rsrc_t out = make_rsrc(g.dbc + ((((size_t)me.blk * p.T + t0) * p.B + me.b) * p.G + me.g) * (2 * NP), SPAN);
 #pragma unroll
-    for (int i = 0; i < (2 * TILE * NP + THREADS - 1) / THREADS; ++i) {
+    for (int i = 0; i < 2 * TILE * NP / THREADS; ++i) {
       const int at = i * THREADS + threadIdx.x, t = at / (2 * NP), kn = at % (2 * NP);
-      if (at < 2 * TILE * NP && t0 + t < end) {
-        float s = 0.f;
+      float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) s += s_s[w][kn / NP][t * NP + kn % NP];
-        g.dbc[((((size_t)me.blk * p.T + t0 + t) * p.B + me.b) * p.G + me.g) * (2 * NP) + kn] = s;
-      }
+      for (int w = 0; w < WAVES; ++w) s += s_s[w][kn / NP][t * NP + kn % NP];
+      st_b32(out, t0 + t < end ? t * pitch + kn * 4 : NOWHERE, 0, __float_as_uint(s));
     }
   }
   // sums over the lanes that share a channel of the elementwise mapping: lane bits log2(CH) to 5
@@ -542,30 +643,25 @@ __global__ __launch_bounds__(256) void scan_sum_rows_kernel(const ScanP p, const
   }
 }
 
-// dA, dskip, ddt_bias: sums over chunks and sequences.  64 columns by four interleaved runs a workgroup.
+// dA, dskip, ddt_bias: sums over chunks and sequences.
 template <int L>
 __global__ __launch_bounds__(256) void scan_sum_params_kernel(const ScanP p, const float *__restrict__ dA_part, const float *__restrict__ dsum,
                                                               float *__restrict__ dA, float *__restrict__ dskip, float *__restrict__ ddt_bias) {
   constexpr int NP = NS * L;
-  __shared__ float part[256];
-  const int col = threadIdx.x & 63, run = threadIdx.x >> 6, rows = p.nchunks * p.B;
-  const int64_t na = (int64_t)p.D * NP, c = (int64_t)blockIdx.x * 64 + col, cols = na + 2 * (int64_t)p.D;
-  float s = 0.f;
-  if (c < na)
-    for (int r = run; r < rows; r += 4) s += dA_part[r * na + c];
-  else if (c < cols)
-    for (int r = run; r < rows; r += 4) s += dsum[r * 2 * (int64_t)p.D + (c - na)];
-  part[threadIdx.x] = s;
-  __syncthreads();
-  if (run != 0 || c >= cols) return;
-  s = ((part[col] + part[64 + col]) + part[128 + col]) + part[192 + col];
-  if (c < na) {
+  __shared__ float lds[256];
+  const int rows = p.nchunks * p.B;
+  const int64_t na = (int64_t)p.D * NP, blocks = (na + 15) / 16;
+  const bool first = blockIdx.x < blocks;                   // workgroups of dA, then those of the other two
+  const int64_t cols = first ? na : 2 * (int64_t)p.D, c = (blockIdx.x - (first ? 0 : blocks)) * 16 + (threadIdx.x & 15);
+  const float s = sum_column(first ? dA_part : dsum, cols, c, rows, lds);
+  if (threadIdx.x >= 16 || c >= cols) return;
+  if (first) {
     const int n = (int)(c % NP);
     if (n < p.N) dA[c / NP * p.N + n] = s;
-  } else if (c < na + p.D) {
-    if (dskip) dskip[c - na] = s;
+  } else if (c < p.D) {
+    if (dskip) dskip[c] = s;
   } else if (ddt_bias) {
-    ddt_bias[c - na - p.D] = s;
+    ddt_bias[c - p.D] = s;
   }
 }
 
@@ -582,12 +678,10 @@ template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void s
   const T *bv = (const T *)p.bv.p + b * p.bv.sb + (int64_t)gr * p.N, *cv = (const T *)p.cv.p + b * p.cv.sb + (int64_t)gr * p.N;
   float A[NS], h[NS], bq[NS], cq[NS];
   float *state = p.state + seq * p.N;
-  if constexpr (FOUR) {
-    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float4 av = some ? *(const float4 *)(p.A + (int64_t)d * p.N + part * NS) : zero;
-    const float4 hv = some ? *(const float4 *)(state + part * NS) : zero;
-    A[0] = av.x; A[1] = av.y; A[2] = av.z; A[3] = av.w;
-    h[0] = hv.x; h[1] = hv.y; h[2] = hv.z; h[3] = hv.w;
+  if constexpr (FOUR) {                                     // (N is 4, 8, .. : lanes beyond it read the last four)
+    const int at = min(part * NS, p.N - NS);
+    take4(A, (const float4 *)(p.A + (int64_t)d * p.N + at), some);
+    take4(h, (const float4 *)(state + at), some);
   } else {
     load4(A, p.A + (int64_t)d * p.N, part, p.N, true);
     load4(h, state, part, p.N, true);
@@ -621,16 +715,12 @@ template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void s
 }
 
 // ---------------------------------------------------------------- host side
-int lanes_of(int N) {                                       // L
-  int l = 1;
-  while (l * NS < N) l *= 2;
-  return l;
-}
-constexpr int waves_of(int L) { return L == 1 ? 2 : 4; }    // (64 channels a wavefront: LDS holds the tiles of two)
+int lanes_of(int N) { return N <= 16 ? 4 : N <= 32 ? 8 : 16; }   // L
+constexpr int WAVES = 4;                                    // of a workgroup
 
 // Workgroups per (chunk, sequence, group).
 int blocks_of(const snn_scan_args &a, int L) {
-  const int per = 64 / L * waves_of(L), dg = a.D / a.groups;
+  const int per = 64 / L * WAVES, dg = a.D / a.groups;
   return (dg + per - 1) / per;
 }
 
@@ -641,8 +731,7 @@ int scan_sizes(const snn_scan_args *a) {
   if (a->groups < 1 || a->D % a->groups) return ops_fail(SNN_ERR_ARG, "scan: groups must divide D");
   if ((int64_t)a->B * a->D >= (1ll << 31) / 64) return ops_fail(SNN_ERR_ARG, "scan: B * D must stay below 2^25");
   if (a->T > (1 << 30)) return ops_fail(SNN_ERR_ARG, "scan: T must not exceed 2^30");
-  if ((int64_t)a->B * a->groups * blocks_of(*a, lanes_of(a->N)) > (1 << 23))       // (a launch has less than 2^32 threads)
-    return ops_fail(SNN_ERR_ARG, "scan: too many sequences of narrow groups: more than 2^23 workgroups");
+  if ((int64_t)a->B * a->groups >= (1 << 18)) return ops_fail(SNN_ERR_ARG, "scan: B * groups must stay below 2^18");
   if ((int64_t)a->T * a->B * a->groups >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "scan: T * B * groups must stay below 2^32");
   return SNN_OK;
 }
@@ -667,9 +756,20 @@ int scan_check(const snn_scan_args *a, bool step, bool grads) {
   return SNN_OK;
 }
 
+// Strides of the streamed tensors: a lane's offset within a tile (15 steps and its channel) stays below SPAN.
+int scan_strides(const snn_scan_args *a, const snn_rows *rows, int count) {
+  const int64_t z = a->type == SNN_TYPE_FP32 ? 4 : 2;
+  for (int i = 0; i < count; ++i) {
+    if (!rows[i].p || a->T <= 1) continue;
+    if (rows[i].stride_t < 0 || rows[i].stride_t > (1 << 28) || (15 * rows[i].stride_t + a->D + a->groups * (int64_t)a->N) * z >= SPAN)
+      return ops_fail(SNN_ERR_ARG, "scan: a stride between steps is negative or too large: 15 steps have to stay below 2 GiB");
+  }
+  return SNN_OK;
+}
+
 // How time is cut: enough chunks that every SIMD has a wavefront, of at least 64 steps.
 void scan_cut(const snn_scan_args &a, int L, int *chunk, int *nchunks) {
-  const int64_t waves = (int64_t)a.B * a.groups * blocks_of(a, L) * waves_of(L);
+  const int64_t waves = (int64_t)a.B * a.groups * blocks_of(a, L) * WAVES;
   int64_t n = 1024 / waves;
   if (n > a.T / 64) n = a.T / 64;
   if (n < 1) n = 1;
@@ -698,14 +798,13 @@ ScanSpace scan_space(const snn_scan_args &a, bool backward) {
   return s;
 }
 
-template <typename F> int with_lanes(int L, F f) {
-  switch (L) {
-    case 1: return f(std::integral_constant<int, 1>());
-    case 2: return f(std::integral_constant<int, 2>());
-    case 4: return f(std::integral_constant<int, 4>());
-    case 8: return f(std::integral_constant<int, 8>());
-    default: return f(std::integral_constant<int, 16>());
-  }
+// f(a value of the streamed type, L)
+template <typename F> int with_kind(const snn_scan_args &a, F f) {
+  const int L = lanes_of(a.N);
+  const auto lanes = [&](auto zero) {
+    return L == 4 ? f(zero, std::integral_constant<int, 4>()) : L == 8 ? f(zero, std::integral_constant<int, 8>()) : f(zero, std::integral_constant<int, 16>());
+  };
+  return a.type == SNN_TYPE_FP32 ? lanes(0.f) : lanes((__bf16)0.f);
 }
 
 ScanP plan(const snn_scan_args &a, int L, char *ws, const ScanSpace &s) {
@@ -716,24 +815,24 @@ ScanP plan(const snn_scan_args &a, int L, char *ws, const ScanSpace &s) {
   return p;
 }
 
-template <typename T, int L> int forward(const snn_scan_args &a, void *saved, char *ws, hipStream_t st) {
-  constexpr int W = waves_of(L);
+template <typename T, int L, bool GATE> int forward(const snn_scan_args &a, void *saved, char *ws, hipStream_t st) {
+  constexpr int W = WAVES;
   ScanP p = plan(a, L, ws, scan_space(a, false));
   p.saved = (float4 *)saved;
   const unsigned per = (unsigned)((size_t)p.blocks * p.G * p.B);
   int rc = SNN_OK;
   if (p.nchunks > 1) {
-    hipLaunchKernelGGL((scan_forward_kernel<T, L, W, true>), dim3(per * (p.nchunks - 1)), dim3(64 * W), 0, st, p);
+    hipLaunchKernelGGL((scan_forward_kernel<T, L, W, false, true>), dim3(per * (p.nchunks - 1)), dim3(64 * W), 0, st, p);
     if ((rc = ops_launched("scan, chunks"))) return rc;
     hipLaunchKernelGGL((scan_join_kernel<L, false>), dim3((unsigned)(((int64_t)p.B * p.D * L + 255) / 256)), dim3(256), 0, st, p, a.init);
     if ((rc = ops_launched("scan, join"))) return rc;
   }
-  hipLaunchKernelGGL((scan_forward_kernel<T, L, W, false>), dim3(per * p.nchunks), dim3(64 * W), 0, st, p);
+  hipLaunchKernelGGL((scan_forward_kernel<T, L, W, GATE, false>), dim3(per * p.nchunks), dim3(64 * W), 0, st, p);
   return ops_launched("scan");
 }
 
-template <typename T, int L> int backward(const snn_scan_args &a, const snn_scan_grads &gr, const void *saved, char *ws, hipStream_t st) {
-  constexpr int W = waves_of(L);
+template <typename T, int L, bool GATE> int backward(const snn_scan_args &a, const snn_scan_grads &gr, const void *saved, char *ws, hipStream_t st) {
+  constexpr int W = WAVES;
   const ScanSpace s = scan_space(a, true);
   ScanP p = plan(a, L, ws, s);
   p.saved = (float4 *)const_cast<void *>(saved);
@@ -744,20 +843,20 @@ template <typename T, int L> int backward(const snn_scan_args &a, const snn_scan
   const unsigned per = (unsigned)((size_t)p.blocks * p.G * p.B);
   int rc = SNN_OK;
   if (p.nchunks > 1) {
-    hipLaunchKernelGGL((scan_reverse_local_kernel<T, L, W>), dim3(per * (p.nchunks - 1)), dim3(64 * W), 0, st, p, g);
+    hipLaunchKernelGGL((scan_reverse_local_kernel<T, L, W, GATE>), dim3(per * (p.nchunks - 1)), dim3(64 * W), 0, st, p, g);
     if ((rc = ops_launched("scan reverse, chunks"))) return rc;
     hipLaunchKernelGGL((scan_join_kernel<L, true>), dim3((unsigned)(((int64_t)p.B * p.D * L + 255) / 256)), dim3(256), 0, st, p, gr.d_state);
     if ((rc = ops_launched("scan reverse, join"))) return rc;
   }
-  hipLaunchKernelGGL((scan_reverse_kernel<T, L, W>), dim3(per * p.nchunks), dim3(64 * W), 0, st, p, g);
+  hipLaunchKernelGGL((scan_reverse_kernel<T, L, W, GATE>), dim3(per * p.nchunks), dim3(64 * W), 0, st, p, g);
   if ((rc = ops_launched("scan reverse"))) return rc;
   const int64_t values = (int64_t)a.T * a.B * a.groups * 2 * NS * L;
   if (values) {
     hipLaunchKernelGGL((scan_sum_rows_kernel<T, L>), dim3((unsigned)std::min<int64_t>((values + 255) / 256, 1 << 16)), dim3(256), 0, st, p, g.dbc, Rows<void>(gr.dbv), Rows<void>(gr.dcv));
     if ((rc = ops_launched("scan reverse, rows"))) return rc;
   }
-  const int64_t cols = (int64_t)a.D * (NS * L + 2);
-  hipLaunchKernelGGL((scan_sum_params_kernel<L>), dim3((unsigned)((cols + 63) / 64)), dim3(256), 0, st, p, (const float *)g.dA, g.dsum, gr.dA, gr.dskip, gr.ddt_bias);
+  const int64_t groups = ((int64_t)a.D * NS * L + 15) / 16 + (2 * (int64_t)a.D + 15) / 16;
+  hipLaunchKernelGGL((scan_sum_params_kernel<L>), dim3((unsigned)groups), dim3(256), 0, st, p, (const float *)g.dA, g.dsum, gr.dA, gr.dskip, gr.ddt_bias);
   return ops_launched("scan reverse, parameters");
 }
 
@@ -801,11 +900,14 @@ int32_t snn_scan_saved_bytes(const snn_scan_args *a, size_t *bytes) {
 int32_t snn_scan_forward(const snn_scan_args *a, void *saved, void *workspace, size_t workspace_bytes, void *stream) {
   int rc = scan_check(a, false, false);
   if (rc) return rc;
+  const snn_rows rows[] = {a->x, a->dt, a->z, a->bv, a->cv, a->y};
+  if ((rc = scan_strides(a, rows, 6))) return rc;
   if (!aligned(saved, 16)) return ops_fail(SNN_ERR_ARG, "scan: saved must be 16-byte aligned");
   if ((rc = check_workspace(scan_space(*a, false).all, workspace, workspace_bytes))) return rc;
-  return with_lanes(lanes_of(a->N), [&](auto l) {
-    return a->type == SNN_TYPE_FP32 ? forward<float, l.value>(*a, saved, (char *)workspace, (hipStream_t)stream)
-                                    : forward<__bf16, l.value>(*a, saved, (char *)workspace, (hipStream_t)stream);
+  return with_kind(*a, [&](auto zero, auto l) {
+    using T = decltype(zero);
+    return a->z.p ? forward<T, l.value, true>(*a, saved, (char *)workspace, (hipStream_t)stream)
+                  : forward<T, l.value, false>(*a, saved, (char *)workspace, (hipStream_t)stream);
   });
 }
 
@@ -820,20 +922,21 @@ int32_t snn_scan_backward(const snn_scan_args *a, const snn_scan_grads *g, const
     if (!aligned(q, z)) return ops_fail(SNN_ERR_ARG, "scan backward: a pointer is not aligned to its element type");
   for (const void *q : {(const void *)g->d_state, (const void *)g->dA, (const void *)g->dskip, (const void *)g->ddt_bias, (const void *)g->dinit})
     if (!aligned(q, 4)) return ops_fail(SNN_ERR_ARG, "scan backward: a pointer is not aligned to its element type");
+  const snn_rows rows[] = {a->x, a->dt, a->z, a->bv, a->cv, g->dy, g->dx, g->ddt, g->dz};
+  if ((rc = scan_strides(a, rows, 9))) return rc;
   if (!aligned(saved, 16)) return ops_fail(SNN_ERR_ARG, "scan backward: saved must be 16-byte aligned");
   if ((rc = check_workspace(scan_space(*a, true).all, workspace, workspace_bytes))) return rc;
-  return with_lanes(lanes_of(a->N), [&](auto l) {
-    return a->type == SNN_TYPE_FP32 ? backward<float, l.value>(*a, *g, saved, (char *)workspace, (hipStream_t)stream)
-                                    : backward<__bf16, l.value>(*a, *g, saved, (char *)workspace, (hipStream_t)stream);
+  return with_kind(*a, [&](auto zero, auto l) {
+    using T = decltype(zero);
+    return a->z.p ? backward<T, l.value, true>(*a, *g, saved, (char *)workspace, (hipStream_t)stream)
+                  : backward<T, l.value, false>(*a, *g, saved, (char *)workspace, (hipStream_t)stream);
   });
 }
 
 int32_t snn_scan_step(const snn_scan_args *a, void *stream) {
   int rc = scan_check(a, true, false);
   if (rc) return rc;
-  return with_lanes(lanes_of(a->N), [&](auto l) {
-    return a->type == SNN_TYPE_FP32 ? step<float, l.value>(*a, (hipStream_t)stream) : step<__bf16, l.value>(*a, (hipStream_t)stream);
-  });
+  return with_kind(*a, [&](auto zero, auto l) { return step<decltype(zero), l.value>(*a, (hipStream_t)stream); });
 }
 
 }  // extern "C"

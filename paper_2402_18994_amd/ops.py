@@ -13,7 +13,10 @@ wraps the pair in a torch.autograd.Function.)
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import NamedTuple, Optional, Sequence
+
+import numpy as np
 
 from . import binding
 from .binding import SnnError
@@ -88,38 +91,42 @@ class ScanGrads(NamedTuple):
     dinit: object
 
 
+torch = None                      # bound by _lib(), so that importing the package does not import torch
 _declared = None
 _types = None
+_stream_of = None
+
+# The argument structures are packed in one go: a call spends its host time on checks, not on fields.
+_CONV = struct.Struct("6i" + "3q" * 2 + "5q")
+_CONV_GRADS = struct.Struct("3q" * 2 + "4q")
+_SCAN = struct.Struct("7i4x" + "3q" * 6 + "6q")
+_SCAN_GRADS = struct.Struct("3qq" + "3q" * 5 + "4q")
+assert [s.size for s in (_CONV, _CONV_GRADS, _SCAN, _SCAN_GRADS)] == [C.sizeof(c) for c in (_ConvArgs, _ConvGrads, _ScanArgs, _ScanGrads)]
 
 
 def _lib():
-    """The built library with the signatures of these entry points."""
-    global _declared, _types
+    """The built library with the signatures of these entry points (structures go in by address)."""
+    global _declared, _types, _stream_of, torch
     if _declared is None:
-        import torch
+        import torch as torch_
+        torch = torch_
         lib = binding.load_library()
-        vp, sz, p = C.c_void_p, C.c_size_t, C.POINTER
-        lib.snn_conv_forward.argtypes = [p(_ConvArgs), vp]
-        lib.snn_conv_workspace_bytes.argtypes = [p(_ConvArgs), p(sz)]
-        lib.snn_conv_backward.argtypes = [p(_ConvArgs), p(_ConvGrads), vp, sz, vp]
-        lib.snn_conv_step.argtypes = [p(_ConvArgs), vp]
-        lib.snn_scan_workspace_bytes.argtypes = [p(_ScanArgs), C.c_int32, p(sz)]
-        lib.snn_scan_saved_bytes.argtypes = [p(_ScanArgs), p(sz)]
-        lib.snn_scan_forward.argtypes = [p(_ScanArgs), vp, vp, sz, vp]
-        lib.snn_scan_backward.argtypes = [p(_ScanArgs), p(_ScanGrads), vp, vp, sz, vp]
-        lib.snn_scan_step.argtypes = [p(_ScanArgs), vp]
-        lib.snn_adamw_step.argtypes = [p(_AdamArgs), p(_AdamTensor), C.c_int32, vp]
-        for name in ("conv_forward", "conv_workspace_bytes", "conv_backward", "conv_step", "scan_workspace_bytes",
-                     "scan_saved_bytes", "scan_forward", "scan_backward", "scan_step", "adamw_step"):
-            getattr(lib, "snn_" + name).restype = C.c_int32
+        vp, sz = C.c_void_p, C.c_size_t
+        for name, args in (("conv_forward", [vp, vp]), ("conv_workspace_bytes", [vp, vp]), ("conv_backward", [vp, vp, vp, sz, vp]),
+                           ("conv_step", [vp, vp]), ("scan_workspace_bytes", [vp, C.c_int32, vp]), ("scan_saved_bytes", [vp, vp]),
+                           ("scan_forward", [vp, vp, vp, sz, vp]), ("scan_backward", [vp, vp, vp, vp, sz, vp]), ("scan_step", [vp, vp]),
+                           ("adamw_step", [vp, vp, C.c_int32, vp])):
+            f = getattr(lib, "snn_" + name)
+            f.argtypes, f.restype = args, C.c_int32
         _types = {torch.float32: 0, torch.bfloat16: 1}
+        # the handle of a device's current stream, without a Stream object around it where torch offers that
+        _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         _declared = lib
     return _declared
 
 
-def _check(rc):
-    if rc:
-        raise SnnError(rc, binding.load_library().snn_last_error(None).decode())
+def _refuse(text, status=ERR_ARG):
+    raise SnnError(status, text)
 
 
 def _need(ok, text, status=ERR_ARG):
@@ -127,81 +134,101 @@ def _need(ok, text, status=ERR_ARG):
         raise SnnError(status, text)
 
 
-def _type(x):
-    _lib()
-    _need(x.dtype in _types, f"streamed tensors are float32 or bfloat16, not {x.dtype}")
-    _need(x.is_cuda, "tensors have to be on a HIP device")
-    return _types[x.dtype]
+def _start(x):
+    """snn_type and device number of a call's first tensor."""
+    if _declared is None:
+        _lib()
+    kind = _types.get(x.dtype)
+    if kind is None:
+        _refuse(f"streamed tensors are float32 or bfloat16, not {x.dtype}")
+    dev = x.get_device()
+    if dev < 0:
+        _refuse("tensors have to be on a HIP device")
+    return kind, dev
 
 
-def _rows(t, like, shape, name):
-    """snn_rows of a [T, B, D] tensor."""
-    _need(t.shape == shape, f"{name} is {tuple(t.shape)}, {tuple(shape)} is needed", ERR_SHAPE)
-    _need(t.dtype == like.dtype and t.device == like.device, f"{name} has another type or device than x")
-    st, sb, sd = t.stride()
-    _need(sd == 1 or shape[2] <= 1, f"the channels of {name} have to be dense")
-    return _Rows(t.data_ptr(), st, sb)
-
-
-def _vectors(t, like, T, B, D, N, name):
-    """snn_rows of a [T, B, G, N] tensor, or [T, B, N] for one group."""
-    g = t.shape[2] if t.dim() == 4 else 1
-    _need(tuple(t.shape) in ((T, B, g, N), (T, B, N)), f"{name} is {tuple(t.shape)}, {(T, B, g, N)} is needed", ERR_SHAPE)
-    _need(t.dtype == like.dtype and t.device == like.device, f"{name} has another type or device than x")
+def _rows(t, x, dev, shape, name):
+    """The fields of the snn_rows of a [T, B, D] or, for one step, [B, D] tensor like x."""
+    if t.shape != shape:
+        _refuse(f"{name} is {tuple(t.shape)}, {tuple(shape)} is needed", ERR_SHAPE)
+    if t.dtype is not x.dtype or t.get_device() != dev:
+        _refuse(f"{name} has another type or device than x")
     s = t.stride()
-    _need((s[-1] == 1 or N <= 1) and (t.dim() == 3 or g <= 1 or s[2] == N), f"the vectors of {name} have to be dense")
-    return _Rows(t.data_ptr(), s[0], s[1]), g
+    if s[-1] != 1 and shape[-1] > 1:
+        _refuse(f"the channels of {name} have to be dense")
+    return (t.data_ptr(), s[0], s[1]) if len(s) == 3 else (t.data_ptr(), 0, s[0])
 
 
-def _dense(t, like, shape, dtype, name):
-    """The address of a dense tensor, or None."""
+def _vectors(t, x, dev, lead, N, name):
+    """The fields of the snn_rows of a [*lead, G, N] tensor, or [*lead, N] for one group, and G."""
+    k, s, shape = len(lead), t.stride(), t.shape
+    grouped = len(shape) == k + 2
+    g = shape[k] if grouped else 1
+    if shape[:k] != lead or shape[-1] != N or len(shape) != k + 1 + grouped:
+        _refuse(f"{name} is {tuple(shape)}, {(*lead, g, N)} is needed", ERR_SHAPE)
+    if t.dtype is not x.dtype or t.get_device() != dev:
+        _refuse(f"{name} has another type or device than x")
+    if (s[-1] != 1 and N > 1) or (grouped and g > 1 and s[k] != N):
+        _refuse(f"the vectors of {name} have to be dense")
+    return (t.data_ptr(), s[0], s[1]) if k == 2 else (t.data_ptr(), 0, s[0]), g
+
+
+def _dense(t, dev, shape, dtype, name):
+    """The address of a dense tensor, 0 for none."""
     if t is None:
-        return None
-    _need(tuple(t.shape) == tuple(shape), f"{name} is {tuple(t.shape)}, {tuple(shape)} is needed", ERR_SHAPE)
-    _need(t.dtype == dtype and t.device == like.device and t.is_contiguous(), f"{name} has to be dense, {dtype}, on the device of x")
+        return 0
+    if t.shape != shape:
+        _refuse(f"{name} is {tuple(t.shape)}, {tuple(shape)} is needed", ERR_SHAPE)
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        _refuse(f"{name} has to be dense, {dtype}, on the device of x")
     return t.data_ptr()
 
 
-class _On:
-    """The current stream of a tensor's device, with that device the current one for the launch."""
+def _call(f, dev, *args):
+    """f(*args, stream): on the current stream of the device, with that device current for the launch."""
+    if torch.cuda.current_device() == dev:
+        rc = f(*args, _stream_of(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = f(*args, _stream_of(dev))
+    if rc:
+        _check(rc)
 
-    def __init__(self, x):
-        import torch
-        self.stream = C.c_void_p(torch.cuda.current_stream(x.device).cuda_stream)
-        self.guard = None if torch.cuda.current_device() == x.device.index else torch.cuda.device(x.device)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
+def _check(rc):
+    if rc:
+        raise SnnError(rc, _declared.snn_last_error(None).decode())
 
-    def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
+
+def _bytes_of(f, *args):
+    n = C.c_size_t(0)
+    _check(f(*args, C.byref(n)))
+    return n.value
 
 
 def _space(n, x):
-    import torch
     return torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
 
 
 # ---------------------------------------------------------------------------------------------- convolution
 
-def _conv_args(x, weight, bias, init, lengths, silu):
-    import torch
-    kind = _type(x)
-    _need(x.dim() == 3, "x has to be [T, B, D]", ERR_SHAPE)
-    T, B, D = x.shape
-    _need(B > 0 and D > 0, "there has to be a sequence and a channel", ERR_SHAPE)
-    _need(weight.dim() == 2 and weight.shape[0] == D and 1 <= weight.shape[1] <= MAX_TAPS, f"weight has to be [D, W], W from 1 to {MAX_TAPS}", ERR_SHAPE)
-    W = weight.shape[1]
-    f32 = torch.float32
-    a = _ConvArgs(T, B, D, W, kind, int(bool(silu)), _rows(x, x, x.shape, "x"))
-    a.weight = _dense(weight, x, (D, W), f32, "weight")
-    a.bias = _dense(bias, x, (D,), f32, "bias")
-    a.init = _dense(init, x, (W - 1, B, D), x.dtype, "init")
-    a.lengths = _dense(lengths, x, (B,), torch.int32, "lengths")
-    return a
+def _conv_args(x, weight, bias, init, lengths, silu, step=False):
+    """-> the device number, W, and the packer of the call's structure: f(y's address, the state's address)."""
+    kind, dev = _start(x)
+    shape = x.shape
+    if len(shape) != (2 if step else 3):
+        _refuse("x has to be [B, D]" if step else "x has to be [T, B, D]", ERR_SHAPE)
+    B, D = shape[-2:]
+    if B == 0 or D == 0:
+        _refuse("there has to be a sequence and a channel", ERR_SHAPE)
+    if weight.dim() != 2 or weight.shape[0] != D or not 1 <= weight.shape[1] <= MAX_TAPS:
+        _refuse(f"weight has to be [D, W], W from 1 to {MAX_TAPS}", ERR_SHAPE)
+    W, f32 = weight.shape[1], torch.float32
+    T = 1 if step else shape[0]
+    head = (T, B, D, W, kind, 1 if silu else 0, *_rows(x, x, dev, shape, "x"))
+    tail = (_dense(weight, dev, (D, W), f32, "weight"), _dense(bias, dev, (D,), f32, "bias"), _dense(init, dev, (W - 1, B, D), x.dtype, "init"),
+            _dense(lengths, dev, (B,), torch.int32, "lengths"))
+    return dev, W, lambda y, state: _CONV.pack(*head, y, B * D, D, *tail, state)
 
 
 def causal_conv(x, weight, bias=None, init=None, lengths=None, silu: bool = True) -> ConvOutput:
@@ -210,74 +237,62 @@ def causal_conv(x, weight, bias=None, init=None, lengths=None, silu: bool = True
     x [T, B, D]; weight [D, W] and bias [D] float32; init [W-1, B, D], the inputs before the first step (zeros without
     it); lengths [B] int32: steps beyond a sequence's length give zeros and are not looked at.  Returns y and the last
     W-1 inputs of every sequence, which `causal_conv_step` or the next call's `init` goes on from."""
-    import torch
-    a = _conv_args(x, weight, bias, init, lengths, silu)
+    dev, W, pack = _conv_args(x, weight, bias, init, lengths, silu)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    state = torch.empty((a.W - 1, a.B, a.D), dtype=x.dtype, device=x.device)
-    a.y, a.state = _Rows(y.data_ptr(), a.B * a.D, a.D), state.data_ptr()
-    with _On(x) as st:
-        _check(_declared.snn_conv_forward(C.byref(a), st))
+    state = torch.empty((W - 1, *x.shape[1:]), dtype=x.dtype, device=x.device)
+    _call(_declared.snn_conv_forward, dev, pack(y.data_ptr(), state.data_ptr()))
     return ConvOutput(y, state)
 
 
 def causal_conv_backward(dy, x, weight, bias=None, init=None, lengths=None, silu: bool = True, d_state=None) -> ConvGrads:
     """Gradients of causal_conv for dy = dL/dy and (optionally) d_state = dL/dstate; dbias and dinit are None where
     the forward call had no bias or init."""
-    import torch
-    a = _conv_args(x, weight, bias, init, lengths, silu)
-    g = _ConvGrads(_rows(dy, x, x.shape, "dy"))
-    g.d_state = _dense(d_state, x, (a.W - 1, a.B, a.D), x.dtype, "d_state")
+    dev, W, pack = _conv_args(x, weight, bias, init, lengths, silu)
+    a, (_, B, D) = pack(0, 0), x.shape
     dx, dweight = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty_like(weight)
     dbias = torch.empty_like(bias) if bias is not None else None
     dinit = torch.empty_like(init) if init is not None else None
-    g.dx, g.dweight = _Rows(dx.data_ptr(), a.B * a.D, a.D), dweight.data_ptr()
-    g.dbias = dbias.data_ptr() if bias is not None else None
-    g.dinit = dinit.data_ptr() if init is not None else None
-    n = C.c_size_t(0)
-    _check(_declared.snn_conv_workspace_bytes(C.byref(a), C.byref(n)))
-    ws = _space(n.value, x)
-    with _On(x) as st:
-        _check(_declared.snn_conv_backward(C.byref(a), C.byref(g), ws.data_ptr(), n.value, st))
+    g = _CONV_GRADS.pack(*_rows(dy, x, dev, x.shape, "dy"), dx.data_ptr(), B * D, D, _dense(d_state, dev, (W - 1, B, D), x.dtype, "d_state"),
+                         dweight.data_ptr(), dbias.data_ptr() if bias is not None else 0, dinit.data_ptr() if init is not None else 0)
+    n = _bytes_of(_declared.snn_conv_workspace_bytes, a)
+    ws = _space(n, x)
+    _call(_declared.snn_conv_backward, dev, a, g, ws.data_ptr(), n)
     return ConvGrads(dx, dweight, dbias, dinit)
 
 
 def causal_conv_step(x, state, weight, bias=None, silu: bool = True):
     """One step of every sequence: x [B, D] -> y [B, D]; `state` [W-1, B, D] is moved on in place."""
-    import torch
-    _need(x.dim() == 2, "x has to be [B, D]", ERR_SHAPE)
-    a = _conv_args(x[None], weight, bias, None, None, silu)
+    dev, W, pack = _conv_args(x, weight, bias, None, None, silu, step=True)
     _need(state is not None, "state is needed")
-    a.state = _dense(state, x, (a.W - 1, a.B, a.D), x.dtype, "state")
+    at = _dense(state, dev, (W - 1, *x.shape), x.dtype, "state")
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    a.y = _Rows(y.data_ptr(), 0, a.D)
-    with _On(x) as st:
-        _check(_declared.snn_conv_step(C.byref(a), st))
+    _call(_declared.snn_conv_step, dev, pack(y.data_ptr(), at))
     return y
 
 
 # --------------------------------------------------------------------------------------------- selective scan
 
-def _scan_args(x, dt, A, B, Cv, D, z, dt_bias, softplus, init, lengths):
-    import torch
-    kind = _type(x)
-    _need(x.dim() == 3, "x has to be [T, B, D]", ERR_SHAPE)
-    T, nb, nd = x.shape
-    _need(nb > 0 and nd > 0, "there has to be a sequence and a channel", ERR_SHAPE)
-    _need(A.dim() == 2 and A.shape[0] == nd and 1 <= A.shape[1] <= MAX_STATES, f"A has to be [D, N], N from 1 to {MAX_STATES}", ERR_SHAPE)
-    N, f32 = A.shape[1], torch.float32
-    bv, g = _vectors(B, x, T, nb, nd, N, "B")
-    cv, gc = _vectors(Cv, x, T, nb, nd, N, "C")
-    _need(g == gc and g >= 1 and nd % g == 0, "B and C have to have the same number of groups, which divides D", ERR_SHAPE)
-    a = _ScanArgs(T, nb, nd, N, g, kind, int(bool(softplus)), _rows(x, x, x.shape, "x"), _rows(dt, x, x.shape, "dt"))
-    if z is not None:
-        a.z = _rows(z, x, x.shape, "z")
-    a.bv, a.cv = bv, cv
-    a.A = _dense(A, x, (nd, N), f32, "A")
-    a.skip = _dense(D, x, (nd,), f32, "D")
-    a.dt_bias = _dense(dt_bias, x, (nd,), f32, "dt_bias")
-    a.init = _dense(init, x, (nb, nd, N), f32, "init")
-    a.lengths = _dense(lengths, x, (nb,), torch.int32, "lengths")
-    return a
+def _scan_args(x, dt, A, B, Cv, D, z, dt_bias, softplus, init, lengths, step=False):
+    """-> the device number, (N, groups), and the packer of the call's structure: f(y's address, the state's address)."""
+    kind, dev = _start(x)
+    shape = x.shape
+    if len(shape) != (2 if step else 3):
+        _refuse("x has to be [B, D]" if step else "x has to be [T, B, D]", ERR_SHAPE)
+    nb, nd = shape[-2:]
+    if nb == 0 or nd == 0:
+        _refuse("there has to be a sequence and a channel", ERR_SHAPE)
+    if A.dim() != 2 or A.shape[0] != nd or not 1 <= A.shape[1] <= MAX_STATES:
+        _refuse(f"A has to be [D, N], N from 1 to {MAX_STATES}", ERR_SHAPE)
+    N, f32, lead = A.shape[1], torch.float32, shape[:-1]
+    bv, g = _vectors(B, x, dev, lead, N, "B")
+    cv, gc = _vectors(Cv, x, dev, lead, N, "C")
+    if g != gc or g < 1 or nd % g:
+        _refuse("B and C have to have the same number of groups, which divides D", ERR_SHAPE)
+    head = (1 if step else shape[0], nb, nd, N, g, kind, 1 if softplus else 0, *_rows(x, x, dev, shape, "x"), *_rows(dt, x, dev, shape, "dt"),
+            *(_rows(z, x, dev, shape, "z") if z is not None else (0, 0, 0)), *bv, *cv)
+    tail = (_dense(A, dev, (nd, N), f32, "A"), _dense(D, dev, (nd,), f32, "D"), _dense(dt_bias, dev, (nd,), f32, "dt_bias"),
+            _dense(init, dev, (nb, nd, N), f32, "init"), _dense(lengths, dev, (nb,), torch.int32, "lengths"))
+    return dev, (N, g), lambda y, state: _SCAN.pack(*head, y, nb * nd, nd, *tail, state)
 
 
 def selective_scan(x, dt, A, B, C_, D=None, z=None, dt_bias=None, softplus: bool = True, init=None, lengths=None,
@@ -287,19 +302,16 @@ def selective_scan(x, dt, A, B, C_, D=None, z=None, dt_bias=None, softplus: bool
     x, dt, z [T, B, D]; B, C [T, B, G, N] (or [T, B, N]), channels d // (D // G) share a group's vectors; A [D, N], D,
     dt_bias [D] and init [B, D, N] float32; lengths [B] int32: steps beyond a sequence's length give zeros, leave its
     state alone and are not looked at.  `save` keeps the state before every 16th step for selective_scan_backward."""
-    import torch
-    a = _scan_args(x, dt, A, B, C_, D, z, dt_bias, softplus, init, lengths)
-    lib, n, k = _declared, C.c_size_t(0), C.c_size_t(0)
+    dev, (N, _), pack = _scan_args(x, dt, A, B, C_, D, z, dt_bias, softplus, init, lengths)
+    lib, saved = _declared, None
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    state = torch.empty((a.B, a.D, a.N), dtype=torch.float32, device=x.device)
-    a.y, a.state = _Rows(y.data_ptr(), a.B * a.D, a.D), state.data_ptr()
-    _check(lib.snn_scan_workspace_bytes(C.byref(a), 0, C.byref(n)))
-    ws, saved = _space(n.value, x), None
+    state = torch.empty((*x.shape[1:], N), dtype=torch.float32, device=x.device)
+    a = pack(y.data_ptr(), state.data_ptr())
+    n = _bytes_of(lib.snn_scan_workspace_bytes, a, 0)
+    ws = _space(n, x)
     if save:
-        _check(lib.snn_scan_saved_bytes(C.byref(a), C.byref(k)))
-        saved = torch.empty(k.value // 4, dtype=torch.float32, device=x.device)
-    with _On(x) as st:
-        _check(lib.snn_scan_forward(C.byref(a), saved.data_ptr() if save else None, ws.data_ptr() if ws is not None else None, n.value, st))
+        saved = torch.empty(_bytes_of(lib.snn_scan_saved_bytes, a) // 4, dtype=torch.float32, device=x.device)
+    _call(lib.snn_scan_forward, dev, a, saved.data_ptr() if save else 0, ws.data_ptr() if n else 0, n)
     return ScanOutput(y, state, saved)
 
 
@@ -307,51 +319,35 @@ def selective_scan_backward(dy, saved, x, dt, A, B, C_, D=None, z=None, dt_bias=
                             lengths=None, d_state=None) -> ScanGrads:
     """Gradients of selective_scan(..., save=True) for dy = dL/dy and (optionally) d_state = dL/dstate.  dD, dz,
     ddt_bias and dinit are None where the forward call had no such argument; dB and dC have B's and C's shape."""
-    import torch
-    a = _scan_args(x, dt, A, B, C_, D, z, dt_bias, softplus, init, lengths)
-    lib, n, k = _declared, C.c_size_t(0), C.c_size_t(0)
-    _check(lib.snn_scan_saved_bytes(C.byref(a), C.byref(k)))
+    dev, (N, groups), pack = _scan_args(x, dt, A, B, C_, D, z, dt_bias, softplus, init, lengths)
+    lib, a, (_, nb, nd) = _declared, pack(0, 0), x.shape
     _need(saved is not None, "saved is needed: call selective_scan with save=True")
-    saved_at = _dense(saved, x, (k.value // 4,), torch.float32, "saved")
-    g = _ScanGrads(_rows(dy, x, x.shape, "dy"))
-    g.d_state = _dense(d_state, x, (a.B, a.D, a.N), torch.float32, "d_state")
+    saved_at = _dense(saved, dev, (_bytes_of(lib.snn_scan_saved_bytes, a) // 4,), torch.float32, "saved")
 
-    def streamed(like):
-        return torch.empty(like.shape, dtype=x.dtype, device=x.device)
+    def like(t, dtype=None):
+        return torch.empty(t.shape, dtype=dtype or t.dtype, device=x.device) if t is not None else None
 
-    dx, ddt, dz = streamed(x), streamed(x), streamed(x) if z is not None else None
-    dB, dC, dA = streamed(B), streamed(C_), torch.empty_like(A)
-    dD = torch.empty_like(D) if D is not None else None
-    ddt_bias = torch.empty_like(dt_bias) if dt_bias is not None else None
-    dinit = torch.empty_like(init) if init is not None else None
-    step, row = a.B * a.D, a.groups * a.N
-    g.dx, g.ddt = _Rows(dx.data_ptr(), step, a.D), _Rows(ddt.data_ptr(), step, a.D)
-    if z is not None:
-        g.dz = _Rows(dz.data_ptr(), step, a.D)
-    g.dbv, g.dcv = _Rows(dB.data_ptr(), a.B * row, row), _Rows(dC.data_ptr(), a.B * row, row)
-    g.dA = dA.data_ptr()
-    for name, t in (("dskip", dD), ("ddt_bias", ddt_bias), ("dinit", dinit)):
-        if t is not None:
-            setattr(g, name, t.data_ptr())
-    _check(lib.snn_scan_workspace_bytes(C.byref(a), 1, C.byref(n)))
-    ws = _space(n.value, x)
-    with _On(x) as st:
-        _check(lib.snn_scan_backward(C.byref(a), C.byref(g), saved_at, ws.data_ptr(), n.value, st))
-    return ScanGrads(dx, ddt, dA, dB, dC, dD, dz, ddt_bias, dinit)
+    def at(t):
+        return t.data_ptr() if t is not None else 0
+
+    out = ScanGrads(like(x), like(x), like(A), like(B), like(C_), like(D), like(z), like(dt_bias), like(init))
+    full, row = (nb * nd, nd), (nb * groups * N, groups * N)
+    g = _SCAN_GRADS.pack(*_rows(dy, x, dev, x.shape, "dy"), _dense(d_state, dev, (nb, nd, N), torch.float32, "d_state"), at(out.dx), *full,
+                         at(out.ddt), *full, at(out.dz), *full, at(out.dB), *row, at(out.dC), *row, at(out.dA), at(out.dD), at(out.ddt_bias), at(out.dinit))
+    n = _bytes_of(lib.snn_scan_workspace_bytes, a, 1)
+    ws = _space(n, x)
+    _call(lib.snn_scan_backward, dev, a, g, saved_at, ws.data_ptr(), n)
+    return out
 
 
 def selective_scan_step(x, dt, state, A, B, C_, D=None, z=None, dt_bias=None, softplus: bool = True):
     """One step of every sequence: x, dt, z [B, D], B, C [B, G, N] or [B, N] -> y [B, D]; `state` [B, D, N] (float32) is
     moved on in place."""
-    import torch
-    _need(x.dim() == 2, "x has to be [B, D]", ERR_SHAPE)
-    a = _scan_args(x[None], dt[None], A, B[None], C_[None], D, z[None] if z is not None else None, dt_bias, softplus, None, None)
+    dev, (N, _), pack = _scan_args(x, dt, A, B, C_, D, z, dt_bias, softplus, None, None, step=True)
     _need(state is not None, "state is needed")
-    a.state = _dense(state, x, (a.B, a.D, a.N), torch.float32, "state")
+    at = _dense(state, dev, (*x.shape, N), torch.float32, "state")
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    a.y = _Rows(y.data_ptr(), 0, a.D)
-    with _On(x) as st:
-        _check(_declared.snn_scan_step(C.byref(a), st))
+    _call(_declared.snn_scan_step, dev, pack(y.data_ptr(), at))
     return y
 
 
@@ -367,16 +363,19 @@ class AdamW:
 
     def __init__(self, params: Sequence, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
                  state_bits: int = 32, seed: int = 0, copies: Optional[Sequence] = None):
-        import torch
         _lib()
         self.params = list(params)
         _need(len(self.params) > 0, "there has to be a parameter")
         _need(state_bits in (32, 8), "state_bits has to be 32 or 8")
-        dev = self.params[0].device
+        self.device = dev = self.params[0].device
         _need(dev.type == "cuda", "parameters have to be on a HIP device")
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(self.params)
         self.copies = list(copies) if copies is not None else [None] * len(self.params)
         _need(len(decay) == len(self.params) and len(self.copies) == len(self.params), "weight_decay and copies go with the parameters", ERR_SHAPE)
+        for p, c in zip(self.params, self.copies):
+            _need(p.dtype == torch.float32 and p.device == dev and p.is_contiguous(), "parameters have to be dense, float32, on one device")
+            _need(c is None or (c.dtype == torch.bfloat16 and c.device == dev and c.is_contiguous() and c.shape == p.shape),
+                  "copies have to be dense, bfloat16, of their parameters' shapes")
         self.lr, self.betas, self.eps, self.bits, self.seed, self.steps = float(lr), betas, float(eps), state_bits, int(seed), 0
         self.at, n = [], 0
         for p in self.params:
@@ -388,30 +387,32 @@ class AdamW:
         self.m_scale = self.v_scale = None
         if state_bits == 8:
             self.m_scale, self.v_scale = (torch.ones(n // BLOCK, device=dev) for _ in range(2))
-        self._tensors = (_AdamTensor * len(self.params))()
-        for e, p, at, wd, c in zip(self._tensors, self.params, self.at, decay, self.copies):
-            _need(p.dtype == torch.float32 and p.device == dev and p.is_contiguous(), "parameters have to be dense, float32, on one device")
-            _need(c is None or (c.dtype == torch.bfloat16 and c.device == dev and c.is_contiguous() and c.shape == p.shape),
-                  "copies have to be dense, bfloat16, of their parameters' shapes")
-            e.n, e.at, e.weight_decay = p.numel(), at, float(wd)
+        self._shapes = [p.shape for p in self.params]
+        self._copied = [i for i, c in enumerate(self.copies) if c is not None]
+        # snn_adamw_tensor, one a row; addresses are filled in by every step
+        self._table = np.zeros((len(self.params), 6), np.int64)
+        self._table[:, 3], self._table[:, 4] = [p.numel() for p in self.params], self.at
+        self._table[:, 5] = np.array(decay, np.float64).view(np.int64)
 
     def step(self, grads: Sequence, lr: Optional[float] = None, grad_scale: float = 1.0) -> None:
         """One step with these gradients (dense, all float32 or all bfloat16, multiplied by `grad_scale` first)."""
-        _need(len(grads) == len(self.params), "a gradient for every parameter is needed", ERR_SHAPE)
-        kind, dev = grads[0].dtype, self.m.device
+        if [g.shape for g in grads] != self._shapes or [p.shape for p in self.params] != self._shapes:
+            _refuse("a gradient of its shape is needed for every parameter", ERR_SHAPE)
+        kind, dev = grads[0].dtype, self.m.get_device()
         _need(kind in _types, f"gradients are float32 or bfloat16, not {kind}")
-        for e, p, g, c in zip(self._tensors, self.params, grads, self.copies):
-            _need(g.shape == p.shape, f"a gradient is {tuple(g.shape)}, its parameter {tuple(p.shape)}", ERR_SHAPE)
-            _need(g.dtype == kind and g.device == dev and g.is_contiguous(), "gradients have to be dense and alike, on the parameters' device")
-            _need(p.is_contiguous() and p.numel() == e.n, "a parameter is not what it was when the optimiser was made")
-            e.param, e.grad = p.data_ptr(), g.data_ptr()
-            e.copy = c.data_ptr() if c is not None else None
-        a = _AdamArgs(self.bits, _types[kind], self.m.data_ptr(), self.v.data_ptr(),
-                      self.m_scale.data_ptr() if self.bits == 8 else None, self.v_scale.data_ptr() if self.bits == 8 else None,
-                      self.steps + 1, self.seed & 0xFFFFFFFF, self.lr if lr is None else float(lr), self.betas[0], self.betas[1],
-                      self.eps, float(grad_scale))
-        with _On(self.m) as st:
-            _check(_declared.snn_adamw_step(C.byref(a), self._tensors, len(self.params), st))
+        if any(g.dtype is not kind or g.get_device() != dev or not g.is_contiguous() for g in grads):
+            _refuse("gradients have to be dense and alike, on the parameters' device")
+        if any(p.dtype is not torch.float32 or p.get_device() != dev or not p.is_contiguous() for p in self.params):
+            _refuse("a parameter is not what it was when the optimiser was made")
+        t = self._table
+        t[:, 0], t[:, 1] = [p.data_ptr() for p in self.params], [g.data_ptr() for g in grads]
+        for i in self._copied:
+            t[i, 2] = self.copies[i].data_ptr()
+        small = self.bits == 8
+        a = _AdamArgs(self.bits, _types[kind], self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr() if small else None,
+                      self.v_scale.data_ptr() if small else None, self.steps + 1, self.seed & 0xFFFFFFFF,
+                      self.lr if lr is None else float(lr), self.betas[0], self.betas[1], self.eps, float(grad_scale))
+        _call(_declared.snn_adamw_step, dev, C.byref(a), t.ctypes.data, len(t))
         self.steps += 1
 
     def state_dict(self) -> dict:
