@@ -25,9 +25,7 @@ namespace {
 
 constexpr int TILE = 16;
 constexpr int NS = 4;
-#ifndef FENCE
-#define FENCE 16
-#endif
+constexpr int GROUP = 2;
 
 struct ScanP {
   int T, B, D, N, G, softplus;
@@ -82,6 +80,9 @@ template <int L, int WAVES> struct Place {
 // its own takes another one's, and the value is replaced by zero afterwards.  Where lanes took turns instead, under high
 // register pressure, the compiler put copies of values that all lanes need later into the region where only some run.
 
+// The length of a sequence, in a scalar register: tiles are whole or not for all lanes alike.
+__device__ __forceinline__ int wave_length(const ScanP &p, int b) { return __builtin_amdgcn_readfirstlane(length_of(p.lengths, b, p.T)); }
+
 // Four states of [D][N] or [B][D][N] rows, zero beyond N.
 __device__ __forceinline__ void load4(float r[NS], const float *row, int part, int N, bool live) {
 #pragma unroll
@@ -108,7 +109,8 @@ __device__ __forceinline__ void take4(float r[NS], const float4 *p, bool live) {
 
 // Streamed tensors go through buffer instructions: a base that the whole wavefront shares (tensor, sequence, tile), the
 // byte offset of the lane in it (channel, step within the tile: one register, computed once) and a scalar offset for
-// the steps of a round.  The host keeps lane offsets below SPAN (scan_strides); a store at NOWHERE is dropped.
+// the steps of a round.  The host keeps the sum below SPAN (scan_strides); at NOWHERE a load gives zero and a store is
+// dropped, so steps that do not exist need no branch.
 constexpr int SPAN = 0x7FFF0000, NOWHERE = 0x7FFFFF00;
 __device__ __forceinline__ float take(rsrc_t r, int voff, int soff, float) { return __uint_as_float(ld_b32(r, voff, soff)); }
 __device__ __forceinline__ __bf16 take(rsrc_t r, int voff, int soff, __bf16) {
@@ -125,29 +127,19 @@ template <typename T, int NP, int COUNT> struct Vectors {
   const T *p;
   int64_t st;
   int et, n, at, row;                // `at`: the lane's offset; `row`: bytes between steps
-  bool on;
   T r[EACH];
   __device__ Vectors(const Rows<void> &src, int b, int g, int N, int me)
-      : p((const T *)src.p + b * src.sb + (int64_t)g * N), st(src.st), et(me / NP), n(me % NP), row((int)(src.st * sizeof(T))), on(me % NP < N) {
-    at = min(n, N - 1) * (int)sizeof(T) + et * row;
-  }
-  __device__ __forceinline__ void fetch_whole(int t0) {
-    const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) r[i] = take(q, at, i * STEP * row, (T)0.f);
+      : p((const T *)src.p + b * src.sb + (int64_t)g * N), st(src.st), et(me / NP), n(me % NP), row((int)(src.st * sizeof(T))) {
+    at = n < N ? n * (int)sizeof(T) + et * row : NOWHERE;
   }
   __device__ __forceinline__ void fetch(int t0, int end) {
-    if (t0 + TILE <= end) {                                 // (a tile that is there as a whole, as nearly all are)
-      fetch_whole(t0);
-    } else {
-      const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
+    const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) r[i] = take(q, at + (min(et + i * STEP, end - 1 - t0) - et) * row, 0, (T)0.f);
-    }
+    for (int i = 0; i < EACH; ++i) r[i] = take(q, t0 + et + i * STEP < end ? at : NOWHERE, i * STEP * row, (T)0.f);
   }
-  __device__ __forceinline__ void put(float *lds, int t0, int end) const {
+  __device__ __forceinline__ void put(float *lds) const {
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) lds[(et + i * STEP) * NP + n] = on & (t0 + et + i * STEP < end) ? widen(r[i]) : 0.f;
+    for (int i = 0; i < EACH; ++i) lds[(et + i * STEP) * NP + n] = widen(r[i]);
   }
 };
 
@@ -161,19 +153,10 @@ template <typename T, int E> struct Stream {
   __device__ Stream(const Rows<void> &src, int b, int d, int et_) : p((T *)src.p + b * src.sb), st(src.st), et(et_), row((int)(src.st * sizeof(T))) {
     at = d * (int)sizeof(T) + et * row;
   }
-  __device__ __forceinline__ void fetch_whole(int t0) {
+  __device__ __forceinline__ void fetch(int t0, int end) {
     const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
 #pragma unroll
-    for (int i = 0; i < E; ++i) r[i] = take(q, at, i * STEP * row, (T)0.f);
-  }
-  __device__ __forceinline__ void fetch(int t0, int end) {
-    if (t0 + TILE <= end) {
-      fetch_whole(t0);
-    } else {
-      const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
-#pragma unroll
-      for (int i = 0; i < E; ++i) r[i] = take(q, at + (min(et + i * STEP, end - 1 - t0) - et) * row, 0, (T)0.f);
-    }
+    for (int i = 0; i < E; ++i) r[i] = take(q, t0 + et + i * STEP < end ? at : NOWHERE, i * STEP * row, (T)0.f);
   }
   __device__ __forceinline__ void put(const float v[E], int t0, int end, bool live) const {
     const rsrc_t q = make_rsrc(p + t0 * st, SPAN);
@@ -194,7 +177,7 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
   const P me(p);
   float2 *sd = s_d[me.wave];
   float *sb = s_b[me.wave], *sc = s_c[me.wave], *sy = s_y[me.wave];
-  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, length_of(p.lengths, me.b, p.T));
+  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, wave_length(p, me.b));
   const size_t seq = (size_t)me.b * p.D + me.d;
 
   float A[NS], h[NS], sum = 0.f;
@@ -221,7 +204,7 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
       gc.fetch(t0, end);
     }
   };
-  if (c0 < end) load(c0);
+  load(c0);
   int t0 = c0;
   for (; t0 < end; t0 += TILE) {
     float x[E], z[E];
@@ -235,30 +218,45 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
       const float soft = softplus(raw), delta = on ? (p.softplus ? soft : raw) : 0.f;
       sd[t * CH + me.ec] = make_float2(delta, delta * x[i]);
     }
-    gb.put(sb, t0, end);
-    if constexpr (!LOCAL) gc.put(sc, t0, end);
-    if (t0 + TILE < end) load(t0 + TILE);
+    gb.put(sb);
+    if constexpr (!LOCAL) gc.put(sc);
+    load(t0 + TILE);                                        // (what does not exist is not read)
     wave_lds_order();
     if constexpr (!LOCAL) {
-      if (p.saved && me.live)
-        p.saved[((size_t)(t0 / TILE) * p.B * p.D + seq) * L + me.part] = make_float4(h[0], h[1], h[2], h[3]);
+      const u32x4 v = {__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3])};
+      st_b128(make_rsrc(p.saved + ((size_t)(t0 / TILE) * p.B + me.b) * p.D * L, SPAN), (p.saved != nullptr) & me.live ? (me.d * L + me.part) * 16 : NOWHERE, 0, v);
     }
     float keep[KEEP];                                       // outputs of the steps whose number mod L is this lane's part
+    // what GROUP steps read of LDS, loaded while the GROUP before them is computed
+    float2 u[2][GROUP];
+    float4 b4[2][GROUP], c4[2][GROUP];
+    const auto read = [&](int t) {
+#pragma unroll
+      for (int k = 0; k < GROUP; ++k) {
+        const int i = t / GROUP % 2;
+        u[i][k] = sd[(t + k) * CH + me.ch];
+        b4[i][k] = *(const float4 *)(sb + (t + k) * NP + me.part * NS);
+        if constexpr (!LOCAL) c4[i][k] = *(const float4 *)(sc + (t + k) * NP + me.part * NS);
+      }
+    };
+    read(0);
 #pragma unroll
     for (int t = 0; t < TILE; ++t) {
-      const float2 u = sd[t * CH + me.ch];
-      const float4 b4 = *(const float4 *)(sb + t * NP + me.part * NS);
-      const float bq[NS] = {b4.x, b4.y, b4.z, b4.w};
+      const int i = t / GROUP % 2, k = t % GROUP;
+      if (k == 0) {
+        if (t + GROUP < TILE) read(t + GROUP);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const float bq[NS] = {b4[i][k].x, b4[i][k].y, b4[i][k].z, b4[i][k].w};
 #pragma unroll
-      for (int j = 0; j < NS; ++j) h[j] = fmaf(__builtin_amdgcn_exp2f(u.x * A[j]), h[j], u.y * bq[j]);
+      for (int j = 0; j < NS; ++j) h[j] = fmaf(__builtin_amdgcn_exp2f(u[i][k].x * A[j]), h[j], u[i][k].y * bq[j]);
       if constexpr (LOCAL) {
-        sum += u.x;
+        sum += u[i][k].x;
       } else {
-        const float4 c4 = *(const float4 *)(sc + t * NP + me.part * NS);
-        float v = c4.x * h[0];
-        v = fmaf(c4.y, h[1], v);
-        v = fmaf(c4.z, h[2], v);
-        v = fmaf(c4.w, h[3], v);
+        float v = c4[i][k].x * h[0];
+        v = fmaf(c4[i][k].y, h[1], v);
+        v = fmaf(c4[i][k].z, h[2], v);
+        v = fmaf(c4[i][k].w, h[3], v);
         v = sum_neighbours<L>(v);
         keep[t / L] = t % L == 0 || me.part == t % L ? v : keep[t / L];
       }
@@ -333,7 +331,7 @@ __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const Sc
   me.s += 1;                                               // (nothing is in front of chunk 0)
   float2 *sd = s_d[me.wave];
   float *sc = s_c[me.wave];
-  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, length_of(p.lengths, me.b, p.T));
+  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, wave_length(p, me.b));
   const size_t seq = (size_t)me.b * p.D + me.d;
   float A[NS], q[NS], sum = 0.f;
   load4(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
@@ -362,7 +360,7 @@ __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const Sc
       const float soft = softplus(raw);
       sd[t * CH + me.ec] = make_float2(on ? (p.softplus ? soft : raw) : 0.f, on ? dy : 0.f);
     }
-    gc.put(sc, t0, end);
+    gc.put(sc);
     if (i0 > 0) load(t0 - TILE);
     wave_lds_order();
 #pragma unroll
@@ -427,7 +425,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
   float *sy = s_y[me.wave];
   float2 *sg = s_g[me.wave];
   float4 *sh = s_h[me.wave] + me.lane;
-  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, length_of(p.lengths, me.b, p.T));
+  const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, wave_length(p, me.b));
   const size_t seq = (size_t)me.b * p.D + me.d;
   float A[NS], A2[NS], q[NS], dA[NS] = {0.f, 0.f, 0.f, 0.f};
   load4(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
@@ -483,34 +481,42 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
       const float dy0 = GATE ? dy[i] * z[i] * sigmoid_fast(z[i]) : dy[i];
       sd[t * CH + me.ec] = make_float4(delta, delta * x[i], dy0, slope);
     }
-    gb.put(s_b, t0, end);
-    gc.put(s_c, t0, end);
+    gb.put(s_b);
+    gc.put(s_c);
     float h0[NS] = {me.live ? rh.x : 0.f, me.live ? rh.y : 0.f, me.live ? rh.z : 0.f, me.live ? rh.w : 0.f};
     float h[HALF + 1][NS], a[TILE][NS];                     // h: of the steps from HALF - 1 on
     __syncthreads();
     float k0[KEEP], k1[KEEP];                               // of the steps whose number mod L is this lane's part
     {
       float hn[NS] = {h0[0], h0[1], h0[2], h0[3]};
+      float2 u[2];                                          // what a step reads of LDS, loaded a step ahead
+      float4 b4[2], c4[2];
+      const auto read = [&](int t) {
+        u[t % 2] = *(const float2 *)(sd + t * CH + me.ch);
+        b4[t % 2] = *(const float4 *)(s_b + t * NP + me.part * NS);
+        if constexpr (GATE) c4[t % 2] = *(const float4 *)(s_c + t * NP + me.part * NS);
+      };
+      read(0);
 #pragma unroll
       for (int t = 0; t < TILE; ++t) {
-
-        if (t % FENCE == 0) __builtin_amdgcn_sched_barrier(0);
-        const float2 u = *(const float2 *)(sd + t * CH + me.ch);
-        const float4 b4 = *(const float4 *)(s_b + t * NP + me.part * NS);
-        const float bq[NS] = {b4.x, b4.y, b4.z, b4.w};
+        if (t + 1 < TILE) read(t + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const float2 un = u[t % 2];
+        const float4 bn = b4[t % 2];
+        const float bq[NS] = {bn.x, bn.y, bn.z, bn.w};
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
-          a[t][j] = __builtin_amdgcn_exp2f(u.x * A2[j]);
-          hn[j] = fmaf(a[t][j], hn[j], u.y * bq[j]);
+          a[t][j] = __builtin_amdgcn_exp2f(un.x * A2[j]);
+          hn[j] = fmaf(a[t][j], hn[j], un.y * bq[j]);
           if (t >= HALF - 1) h[t - HALF + 1][j] = hn[j];
         }
         if (t < HALF - 1) sh[t * 64] = make_float4(hn[0], hn[1], hn[2], hn[3]);
         if constexpr (GATE) {                                         // dz needs the output before the gate
-          const float4 c4 = *(const float4 *)(s_c + t * NP + me.part * NS);
-          float v = c4.x * hn[0];
-          v = fmaf(c4.y, hn[1], v);
-          v = fmaf(c4.z, hn[2], v);
-          v = fmaf(c4.w, hn[3], v);
+          const float4 cn = c4[t % 2];
+          float v = cn.x * hn[0];
+          v = fmaf(cn.y, hn[1], v);
+          v = fmaf(cn.z, hn[2], v);
+          v = fmaf(cn.w, hn[3], v);
           v = sum_neighbours<L>(v);
           k0[t / L] = t % L == 0 || me.part == t % L ? v : k0[t / L];
         }
@@ -522,28 +528,35 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
     asm volatile("" ::: "memory");                          // (the rows of Bv, Cv and sd are read again, not kept in registers)
     float hc[NS];                                           // the state after step t
     float2 kv[TILE / TWINS];                                // of the steps whose number mod TWINS is this lane's among its twins
+    float4 ur[2], br[2], cr[2], hr[2];                      // what a step reads of LDS, loaded a step ahead
+    const auto read = [&](int t) {
+      ur[t % 2] = sd[t * CH + me.ch];
+      br[t % 2] = *(const float4 *)(s_b + t * NP + me.part * NS);
+      cr[t % 2] = *(const float4 *)(s_c + t * NP + me.part * NS);
+      if (t > 0 && t < HALF) hr[t % 2] = sh[(t - 1) * 64];
+    };
+    read(TILE - 1);
 #pragma unroll
     for (int t = TILE - 1; t >= 0; --t) {
-      if (t == HALF - 1 && i0 > 0) {                        // the tile in front; here half of the registers of h and a are free again
-        const int next = t0 - TILE;
-        gx.fetch_whole(next);
-        gd.fetch_whole(next);
-        gy.fetch_whole(next);
-        if constexpr (GATE) gz.fetch_whole(next);
-        gb.fetch_whole(next);
-        gc.fetch_whole(next);
+      if (t > 0) read(t - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if (t == HALF - 1) {
+        // The tile in front, for which half of the registers of h and a are free by now.  No branch for the first tile,
+        // which has none (no step of it exists then): sums that only a later block needs would be put off to there, and
+        // what they are sums of would be kept in registers until then.
+        const int next = max(t0 - TILE, c0), stop = i0 > 0 ? end : 0;
+        gx.fetch(next, stop);
+        gd.fetch(next, stop);
+        gy.fetch(next, stop);
+        if constexpr (GATE) gz.fetch(next, stop);
+        gb.fetch(next, stop);
+        gc.fetch(next, stop);
         rh = p.saved[((size_t)(next / TILE) * p.B * p.D + seq) * L + me.part];
       }
-      if (t % FENCE == FENCE - 1) __builtin_amdgcn_sched_barrier(0);
-      const float4 u = sd[t * CH + me.ch];
-      const float4 b4 = *(const float4 *)(s_b + t * NP + me.part * NS);
-      const float4 c4 = *(const float4 *)(s_c + t * NP + me.part * NS);
+      const float4 u = ur[t % 2], b4 = br[t % 2], c4 = cr[t % 2], h4 = hr[t % 2];
       const float bq[NS] = {b4.x, b4.y, b4.z, b4.w}, cq[NS] = {c4.x, c4.y, c4.z, c4.w};
       float v[2 * NS], gsum = 0.f, usum = 0.f, hp[NS];
-      if (t > 0 && t < HALF) {
-        const float4 r = sh[(t - 1) * 64];
-        hp[0] = r.x; hp[1] = r.y; hp[2] = r.z; hp[3] = r.w;
-      }
+      if (t > 0 && t < HALF) { hp[0] = h4.x; hp[1] = h4.y; hp[2] = h4.z; hp[3] = h4.w; }
 #pragma unroll
       for (int j = 0; j < NS; ++j) {
         if (t == TILE - 1) hc[j] = h[HALF][j];
@@ -729,6 +742,7 @@ int scan_sizes(const snn_scan_args *a) {
   if (a->T < 0 || a->B <= 0 || a->D <= 0) return ops_fail(SNN_ERR_ARG, "scan: T >= 0, B > 0 and D > 0 are required");
   if (a->N < 1 || a->N > SNN_SCAN_MAX_STATES) return ops_fail(SNN_ERR_ARG, "scan: N must be 1 to %d", SNN_SCAN_MAX_STATES);
   if (a->groups < 1 || a->D % a->groups) return ops_fail(SNN_ERR_ARG, "scan: groups must divide D");
+  if (a->D > (1 << 22)) return ops_fail(SNN_ERR_ARG, "scan: D must not exceed 2^22");
   if ((int64_t)a->B * a->D >= (1ll << 31) / 64) return ops_fail(SNN_ERR_ARG, "scan: B * D must stay below 2^25");
   if (a->T > (1 << 30)) return ops_fail(SNN_ERR_ARG, "scan: T must not exceed 2^30");
   if ((int64_t)a->B * a->groups >= (1 << 18)) return ops_fail(SNN_ERR_ARG, "scan: B * groups must stay below 2^18");
