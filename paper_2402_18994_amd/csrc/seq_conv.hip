@@ -10,7 +10,22 @@
 namespace snn {
 namespace {
 
-constexpr int AHEAD = 8;            // rows in flight per thread, forward
+#ifndef CV
+#define CV 8
+#endif
+#ifndef CSEG
+#define CSEG 32
+#endif
+#ifndef CAH
+#define CAH 8
+#endif
+#ifndef BSEG
+#define BSEG 32
+#endif
+#ifndef BBL
+#define BBL 1024
+#endif
+constexpr int AHEAD = CAH;            // rows in flight per thread, forward
 constexpr int AHEAD_BWD = 4;
 
 struct ConvP {
@@ -320,11 +335,11 @@ ConvCut conv_cut(const snn_conv_args &a, int vec) {
   c.lx_log2 = 0;
   while (c.lx_log2 < 6 && (1 << c.lx_log2) < dv) ++c.lx_log2;
   c.gx = (dv + (1 << c.lx_log2) - 1) >> c.lx_log2;
-  c.seg = 32;
+  c.seg = BSEG;
   while (c.seg < (1 << 20) && a.T / c.seg > 65536) c.seg *= 2;
   c.nseg = a.T > c.seg ? (a.T + c.seg - 1) / c.seg : 1;
   const int64_t rows = 256 >> c.lx_log2, items = (int64_t)a.B * c.nseg;
-  const int64_t want = 1024 / c.gx > 1 ? 1024 / c.gx : 1;
+  const int64_t want = BBL / c.gx > 1 ? BBL / c.gx : 1;
   const int64_t all = (items + rows - 1) / rows;
   c.gy = (int)(all < want ? all : want);
   return c;
@@ -346,7 +361,7 @@ template <typename F> int with_taps(int W, F f) {
 template <typename T, int VEC> int launch_forward(const snn_conv_args &a, hipStream_t st) {
   ConvP p(a);
   const int64_t threads = (int64_t)a.B * (a.D / VEC);
-  p.seg = 32;
+  p.seg = CSEG;
   while (a.T / p.seg > 32768) p.seg *= 2;              // (a grid has at most 65535 rows)
   const int gy = a.T > p.seg ? (a.T + p.seg - 1) / p.seg : 1;
   return with_taps(a.W, [&](auto w) {
@@ -389,7 +404,7 @@ int32_t snn_conv_forward(const snn_conv_args *a, void *stream) {
   if (rc) return rc;
   const hipStream_t st = (hipStream_t)stream;
   if (a->type == SNN_TYPE_FP32) return conv_vector(*a, 4, nullptr, false) ? launch_forward<float, 4>(*a, st) : launch_forward<float, 1>(*a, st);
-  return conv_vector(*a, 8, nullptr, false) ? launch_forward<__bf16, 8>(*a, st) : launch_forward<__bf16, 1>(*a, st);
+  return conv_vector(*a, CV, nullptr, false) ? launch_forward<__bf16, CV>(*a, st) : launch_forward<__bf16, 1>(*a, st);
 }
 
 int32_t snn_conv_workspace_bytes(const snn_conv_args *a, size_t *bytes) {

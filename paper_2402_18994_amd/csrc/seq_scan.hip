@@ -24,7 +24,6 @@ namespace snn {
 namespace {
 
 constexpr int TILE = 16;
-constexpr int NS = 4;
 constexpr int GROUP = 2;
 
 struct ScanP {
@@ -35,8 +34,8 @@ struct ScanP {
   const float *A, *skip, *dt_bias, *init;
   const int32_t *lengths;
   float *state;
-  float4 *saved;                     // [tile][B][D][L]: the state before every tile, or NULL
-  float4 *local;                     // [chunk][B][D][L]: of the chunks from zero, then (joined) the states before them
+  float *saved;                      // [tile][B][D][NP]: the state before every tile, or NULL
+  float *local;                      // [chunk][B][D][NP]: of the chunks from zero, then (joined) the states before them
   float *sums;                       // [chunk][B][D]: sum of delta
   explicit ScanP(const snn_scan_args &a)
       : T(a.T), B(a.B), D(a.D), N(a.N), G(a.groups), softplus(a.softplus), chunk(TILE), nchunks(1), blocks(1), x(a.x), dt(a.dt),
@@ -48,9 +47,9 @@ struct ScanGradP {
   Rows<void> dy, dx, ddt, dz;
   const float *d_state;
   float *dinit;
-  float4 *dA;                        // [chunk * B][D][L] partial sums
+  float *dA;                         // [chunk * B][D][NP] partial sums
   float *dsum;                       // [chunk * B][2][D]: of dskip and ddt_bias
-  float *dbc;                        // [blocks][T][B][G][2][4 L] partial sums of dBv and dCv
+  float *dbc;                        // [blocks][T][B][G][2][NP] partial sums of dBv and dCv
   explicit ScanGradP(const snn_scan_grads &g)
       : dy(g.dy), dx(g.dx), ddt(g.ddt), dz(g.dz), d_state(g.d_state), dinit(g.dinit), dA(nullptr), dsum(nullptr), dbc(nullptr) {}
 };
@@ -83,8 +82,8 @@ template <int L, int WAVES> struct Place {
 // The length of a sequence, in a scalar register: tiles are whole or not for all lanes alike.
 __device__ __forceinline__ int wave_length(const ScanP &p, int b) { return __builtin_amdgcn_readfirstlane(length_of(p.lengths, b, p.T)); }
 
-// Four states of [D][N] or [B][D][N] rows, zero beyond N.
-__device__ __forceinline__ void load4(float r[NS], const float *row, int part, int N, bool live) {
+// A lane's states out of [D][N] or [B][D][N] rows, zero beyond N.
+template <int NS> __device__ __forceinline__ void load_states(float r[NS], const float *row, int part, int N, bool live) {
 #pragma unroll
   for (int j = 0; j < NS; ++j) r[j] = 0.f;
   if (row)
@@ -94,17 +93,19 @@ __device__ __forceinline__ void load4(float r[NS], const float *row, int part, i
       r[j] = live & (part * NS + j < N) ? v : 0.f;
     }
 }
-__device__ __forceinline__ void store4(float *row, const float r[NS], int part, int N) {
+template <int NS> __device__ __forceinline__ void store_states(float *row, const float r[NS], int part, int N) {
 #pragma unroll
   for (int j = 0; j < NS; ++j)
     if (part * NS + j < N) row[part * NS + j] = r[j];
 }
-__device__ __forceinline__ void take4(float r[NS], const float4 *p, bool live) {
-  const float4 v = *p;
-  r[0] = live ? v.x : 0.f;
-  r[1] = live ? v.y : 0.f;
-  r[2] = live ? v.z : 0.f;
-  r[3] = live ? v.w : 0.f;
+// The same out of rows of the library's own, which are padded and aligned.
+template <int NS> using States = Pack<float, NS>;
+template <int NS> __device__ __forceinline__ States<NS> pick(const float *p) { return *(const States<NS> *)p; }
+template <int NS> __device__ __forceinline__ void put_states(float *p, const float r[NS]) {
+  States<NS> v;
+#pragma unroll
+  for (int j = 0; j < NS; ++j) v.v[j] = r[j];
+  *(States<NS> *)p = v;
 }
 
 // Streamed tensors go through buffer instructions: a base that the whole wavefront shares (tensor, sequence, tile), the
@@ -119,17 +120,18 @@ __device__ __forceinline__ __bf16 take(rsrc_t r, int voff, int soff, __bf16) {
 __device__ __forceinline__ void give(rsrc_t r, int voff, int soff, float v) { st_b32(r, voff, soff, __float_as_uint(v)); }
 __device__ __forceinline__ void give(rsrc_t r, int voff, int soff, __bf16 v) { st_b16(r, voff, soff, __builtin_bit_cast(unsigned short, v)); }
 
-// What a lane loads of the rows of Bv (or Cv), COUNT threads sharing a tile of TILE x NP values: value n of step
-// et + i COUNT / NP.  In LDS they stand as fp32 [TILE][NP], zero beyond N and for steps that do not exist.
-template <typename T, int NP, int COUNT> struct Vectors {
-  static constexpr int STEP = COUNT / NP, EACH = TILE / STEP;
+// What a lane loads of the rows of Bv (or Cv), THREADS threads sharing a tile of TILE x NP values: value n of step
+// et + i COUNT / NP; threads beyond one for every value repeat what others do.  In LDS they stand as fp32 [TILE][NP],
+// zero beyond N and for steps that do not exist.
+template <typename T, int NP, int THREADS> struct Vectors {
+  static constexpr int COUNT = THREADS < TILE * NP ? THREADS : TILE * NP, STEP = COUNT / NP, EACH = TILE / STEP;
   static_assert(STEP * EACH == TILE, "a tile is a whole number of rounds");
   const T *p;
   int64_t st;
   int et, n, at, row;                // `at`: the lane's offset; `row`: bytes between steps
   T r[EACH];
   __device__ Vectors(const Rows<void> &src, int b, int g, int N, int me)
-      : p((const T *)src.p + b * src.sb + (int64_t)g * N), st(src.st), et(me / NP), n(me % NP), row((int)(src.st * sizeof(T))) {
+      : p((const T *)src.p + b * src.sb + (int64_t)g * N), st(src.st), et(me % COUNT / NP), n(me % NP), row((int)(src.st * sizeof(T))) {
     at = n < N ? n * (int)sizeof(T) + et * row : NOWHERE;
   }
   __device__ __forceinline__ void fetch(int t0, int end) {
@@ -167,7 +169,7 @@ template <typename T, int E> struct Stream {
 
 // ---------------------------------------------------------------- forward
 // LOCAL: the chunk from zero, for its end state and its sum of delta alone; no outputs.
-template <typename T, int L, int WAVES, bool GATE, bool LOCAL>
+template <typename T, int NS, int L, int WAVES, bool GATE, bool LOCAL>
 __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p) {
   using P = Place<L, WAVES>;
   constexpr int CH = P::CH, E = P::E, NP = NS * L, KEEP = TILE / L;
@@ -181,14 +183,16 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
   const size_t seq = (size_t)me.b * p.D + me.d;
 
   float A[NS], h[NS], sum = 0.f;
-  load4(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
+  load_states<NS>(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
 #pragma unroll
   for (int j = 0; j < NS; ++j) { A[j] *= LOG2E; h[j] = 0.f; }
   if constexpr (!LOCAL) {
     if (p.nchunks > 1) {
-      take4(h, p.local + ((size_t)me.s * p.B * p.D + seq) * L + me.part, me.live);
+      const States<NS> v = pick<NS>(p.local + ((size_t)me.s * p.B * p.D + seq) * NP + me.part * NS);
+#pragma unroll
+      for (int j = 0; j < NS; ++j) h[j] = me.live ? v.v[j] : 0.f;
     } else {
-      load4(h, p.init ? p.init + seq * p.N : nullptr, me.part, p.N, me.live);
+      load_states<NS>(h, p.init ? p.init + seq * p.N : nullptr, me.part, p.N, me.live);
     }
   }
   const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f, skip = p.skip ? p.skip[me.ed] : 0.f;
@@ -223,20 +227,22 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
     load(t0 + TILE);                                        // (what does not exist is not read)
     wave_lds_order();
     if constexpr (!LOCAL) {
-      const u32x4 v = {__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3])};
-      st_b128(make_rsrc(p.saved + ((size_t)(t0 / TILE) * p.B + me.b) * p.D * L, SPAN), (p.saved != nullptr) & me.live ? (me.d * L + me.part) * 16 : NOWHERE, 0, v);
+      const rsrc_t to = make_rsrc(p.saved + ((size_t)(t0 / TILE) * p.B + me.b) * p.D * NP, SPAN);
+      const int at = (p.saved != nullptr) & me.live ? (me.d * NP + me.part * NS) * 4 : NOWHERE;
+      if constexpr (NS == 4) st_b128(to, at, 0, (u32x4){__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3])});
+      else st_b64(to, at, 0, (u32x2){__float_as_uint(h[0]), __float_as_uint(h[1])});
     }
     float keep[KEEP];                                       // outputs of the steps whose number mod L is this lane's part
     // what GROUP steps read of LDS, loaded while the GROUP before them is computed
     float2 u[2][GROUP];
-    float4 b4[2][GROUP], c4[2][GROUP];
+    States<NS> bs[2][GROUP], cs[2][GROUP];
     const auto read = [&](int t) {
 #pragma unroll
       for (int k = 0; k < GROUP; ++k) {
         const int i = t / GROUP % 2;
         u[i][k] = sd[(t + k) * CH + me.ch];
-        b4[i][k] = *(const float4 *)(sb + (t + k) * NP + me.part * NS);
-        if constexpr (!LOCAL) c4[i][k] = *(const float4 *)(sc + (t + k) * NP + me.part * NS);
+        bs[i][k] = pick<NS>(sb + (t + k) * NP + me.part * NS);
+        if constexpr (!LOCAL) cs[i][k] = pick<NS>(sc + (t + k) * NP + me.part * NS);
       }
     };
     read(0);
@@ -247,16 +253,14 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
         if (t + GROUP < TILE) read(t + GROUP);
         __builtin_amdgcn_sched_barrier(0);
       }
-      const float bq[NS] = {b4[i][k].x, b4[i][k].y, b4[i][k].z, b4[i][k].w};
 #pragma unroll
-      for (int j = 0; j < NS; ++j) h[j] = fmaf(__builtin_amdgcn_exp2f(u[i][k].x * A[j]), h[j], u[i][k].y * bq[j]);
+      for (int j = 0; j < NS; ++j) h[j] = fmaf(__builtin_amdgcn_exp2f(u[i][k].x * A[j]), h[j], u[i][k].y * bs[i][k].v[j]);
       if constexpr (LOCAL) {
         sum += u[i][k].x;
       } else {
-        float v = c4[i][k].x * h[0];
-        v = fmaf(c4[i][k].y, h[1], v);
-        v = fmaf(c4[i][k].z, h[2], v);
-        v = fmaf(c4[i][k].w, h[3], v);
+        float v = cs[i][k].v[0] * h[0];
+#pragma unroll
+        for (int j = 1; j < NS; ++j) v = fmaf(cs[i][k].v[j], h[j], v);
         v = sum_neighbours<L>(v);
         keep[t / L] = t % L == 0 || me.part == t % L ? v : keep[t / L];
       }
@@ -285,43 +289,46 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
   }
   if (!me.live) return;
   if constexpr (LOCAL) {
-    p.local[((size_t)me.s * p.B * p.D + seq) * L + me.part] = make_float4(h[0], h[1], h[2], h[3]);
+    put_states<NS>(p.local + ((size_t)me.s * p.B * p.D + seq) * NP + me.part * NS, h);
     if (me.part == 0) p.sums[(size_t)me.s * p.B * p.D + seq] = sum;
   } else if (p.state && me.s == p.nchunks - 1) {
-    store4(p.state + seq * p.N, h, me.part, p.N);
+    store_states<NS>(p.state + seq * p.N, h, me.part, p.N);
   }
 }
 
 // Joins the chunks: local[s] (of the chunk from zero) becomes the state before chunk s, in order; with REVERSE the
-// gradient behind it, from the last one.  A thread per (sequence, channel, four states).
-template <int L, bool REVERSE> __global__ __launch_bounds__(256) void scan_join_kernel(const ScanP p, const float *first) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)p.B * p.D * L;
+// gradient behind it, from the last one.  A thread per (sequence, channel, state); the loads of eight chunks are in
+// flight at a time.
+template <int NP, bool REVERSE> __global__ __launch_bounds__(256) void scan_join_kernel(const ScanP p, const float *first) {
+  constexpr int AHEAD = 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, seqs = (int64_t)p.B * p.D, all = seqs * NP;
   if (id >= all) return;
-  const int part = (int)(id % L);
-  const int64_t seq = id / L;
-  float A[NS], h[NS];
-  load4(A, p.A + (seq % p.D) * p.N, part, p.N, true);
-  load4(h, first ? first + seq * p.N : nullptr, part, p.N, true);
+  const int n = (int)(id % NP);
+  const int64_t seq = id / NP;
+  const bool live = n < p.N;
+  const float A = live ? p.A[(seq % p.D) * p.N + n] * LOG2E : 0.f;
+  float h = first && live ? first[seq * p.N + n] : 0.f;
+  const int last = p.nchunks - 1;                          // (the chunk that nobody follows was not run from zero)
+  for (int i0 = 0; i0 <= last; i0 += AHEAD) {
+    float v[AHEAD], d[AHEAD];
 #pragma unroll
-  for (int j = 0; j < NS; ++j) A[j] *= LOG2E;
-  const int last = REVERSE ? 0 : p.nchunks - 1;            // (the chunk that nobody follows was not run from zero)
-  for (int i = 0; i < p.nchunks; ++i) {
-    const int s = REVERSE ? p.nchunks - 1 - i : i;
-    float4 *at = p.local + (int64_t)s * all + id;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    if (s != last) { v = *at; sum = p.sums[(int64_t)s * p.B * p.D + seq]; }
-    *at = make_float4(h[0], h[1], h[2], h[3]);
-    h[0] = fmaf(__builtin_amdgcn_exp2f(sum * A[0]), h[0], v.x);
-    h[1] = fmaf(__builtin_amdgcn_exp2f(sum * A[1]), h[1], v.y);
-    h[2] = fmaf(__builtin_amdgcn_exp2f(sum * A[2]), h[2], v.z);
-    h[3] = fmaf(__builtin_amdgcn_exp2f(sum * A[3]), h[3], v.w);
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + k, s = REVERSE ? last - i : i;
+      v[k] = i < last ? p.local[s * all + id] : 0.f;
+      d[k] = i < last ? p.sums[s * seqs + seq] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + k, s = REVERSE ? last - i : i;
+      if (i <= last) p.local[s * all + id] = h;
+      h = fmaf(__builtin_amdgcn_exp2f(d[k] * A), h, v[k]);
+    }
   }
 }
 
 // ---------------------------------------------------------------- reverse
 // The chunk from a zero gradient behind it: the gradient of the state before it and the sum of delta.
-template <typename T, int L, int WAVES, bool GATE>
+template <typename T, int NS, int L, int WAVES, bool GATE>
 __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const ScanP p, const ScanGradP g) {
   using P = Place<L, WAVES>;
   constexpr int CH = P::CH, E = P::E, NP = NS * L;
@@ -334,7 +341,7 @@ __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const Sc
   const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, wave_length(p, me.b));
   const size_t seq = (size_t)me.b * p.D + me.d;
   float A[NS], q[NS], sum = 0.f;
-  load4(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
+  load_states<NS>(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
 #pragma unroll
   for (int j = 0; j < NS; ++j) { A[j] *= LOG2E; q[j] = 0.f; }
   const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f;
@@ -361,47 +368,41 @@ __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const Sc
       sd[t * CH + me.ec] = make_float2(on ? (p.softplus ? soft : raw) : 0.f, on ? dy : 0.f);
     }
     gc.put(sc);
-    if (i0 > 0) load(t0 - TILE);
+    load(max(t0 - TILE, c0));
     wave_lds_order();
 #pragma unroll
     for (int t = TILE - 1; t >= 0; --t) {
       const float2 u = sd[t * CH + me.ch];
-      const float4 c4 = *(const float4 *)(sc + t * NP + me.part * NS);
-      q[0] = fmaf(u.y, c4.x, q[0]) * __builtin_amdgcn_exp2f(u.x * A[0]);
-      q[1] = fmaf(u.y, c4.y, q[1]) * __builtin_amdgcn_exp2f(u.x * A[1]);
-      q[2] = fmaf(u.y, c4.z, q[2]) * __builtin_amdgcn_exp2f(u.x * A[2]);
-      q[3] = fmaf(u.y, c4.w, q[3]) * __builtin_amdgcn_exp2f(u.x * A[3]);
+      const States<NS> c = pick<NS>(sc + t * NP + me.part * NS);
+#pragma unroll
+      for (int j = 0; j < NS; ++j) q[j] = fmaf(u.y, c.v[j], q[j]) * __builtin_amdgcn_exp2f(u.x * A[j]);
       sum += u.x;
     }
     wave_lds_order();
   }
   if (!me.live) return;
-  p.local[((size_t)me.s * p.B * p.D + seq) * L + me.part] = make_float4(q[0], q[1], q[2], q[3]);
+  put_states<NS>(p.local + ((size_t)me.s * p.B * p.D + seq) * NP + me.part * NS, q);
   if (me.part == 0) p.sums[(size_t)me.s * p.B * p.D + seq] = sum;
 }
 
-// Sums v[0..7] (four of dBv, four of dCv) over the wavefront's channels, lane bits log2(L) to 5.  While eight values
-// are left, the halves of the wavefront trade: each keeps half the values, summed; then the rows of 16 likewise; what
-// is left of the bits goes by rotations.  Returns the two sums of this lane: of dBv in lanes 0-31, of dCv in 32-63,
-// of values 2 (lane bit 4) and the next.
-template <int L> __device__ __forceinline__ float2 sum_channels(const float v[2 * NS]) {
-  float a[4], c[2];
+// Sums v (NS of dBv, NS of dCv) over the wavefront's channels, lane bits log2(L) to 5.  While there are values enough,
+// the halves of the wavefront trade: each keeps half the values, summed; then the rows of 16 likewise; what is left of
+// the bits goes by rotations.  This lane gets NS / 2 sums: of dBv in lanes 0-31, of dCv in 32-63, the first ones where
+// lane bit 4 is 0, the others where it is 1.
+template <int NS, int L> __device__ __forceinline__ void sum_channels(const float v[2 * NS], float c[NS / 2]) {
+  float a[NS];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v[j]), __builtin_bit_cast(unsigned, v[j + 4]), false, false);
+  for (int j = 0; j < NS; ++j) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v[j]), __builtin_bit_cast(unsigned, v[j + NS]), false, false);
     a[j] = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
   }
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a[j]), __builtin_bit_cast(unsigned, a[j + 2]), false, false);
+  for (int j = 0; j < NS / 2; ++j) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a[j]), __builtin_bit_cast(unsigned, a[j + NS / 2]), false, false);
     c[j] = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
-  }
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
     if constexpr (L <= 8) c[j] += dpp<0x128>(c[j]);
     if constexpr (L <= 4) c[j] += dpp<0x124>(c[j]);
   }
-  return make_float2(c[0], c[1]);
 }
 
 // The reverse pass proper.  Per tile, from the last: the states of the tile once more from the one that the forward
@@ -410,31 +411,33 @@ template <int L> __device__ __forceinline__ float2 sum_channels(const float v[2 
 //   d(delta) = sum_n u A + x sum_n g B,   dx = delta sum_n g B + dy0 skip,   dA += u delta,   q = g a.
 // The workgroup's wavefronts share the rows of Bv and Cv, and add their channel sums of dBv and dCv through LDS in a
 // fixed order; sums over workgroups are left to scan_sum_rows_kernel.
-template <typename T, int L, int WAVES, bool GATE>
+template <typename T, int NS, int L, int WAVES, bool GATE>
 __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP p, const ScanGradP g) {
   using P = Place<L, WAVES>;
   constexpr int CH = P::CH, E = P::E, NP = NS * L, THREADS = 64 * WAVES, KEEP = TILE / L, TWINS = 16 / L, HALF = TILE / 2;
   __shared__ float4 s_d[WAVES][TILE * CH];                  // delta, delta x, dy0, d(delta) / d(dt)
   __shared__ float s_y[WAVES][TILE * CH];                   // sum C h
   __shared__ float2 s_g[WAVES][TILE * CH];                  // sum g B, sum u A
-  __shared__ float4 s_h[WAVES][(HALF - 1) * 64];            // states of the first half of a tile
+  __shared__ States<NS> s_h[WAVES][(HALF - 1) * 64];        // states of the first half of a tile
   __shared__ __attribute__((aligned(16))) float s_b[TILE * NP], s_c[TILE * NP];
-  __shared__ __attribute__((aligned(8))) float s_s[WAVES][2][TILE * NP];
+  __shared__ __attribute__((aligned(16))) float s_s[WAVES][2][TILE * NP];
   const P me(p);
   float4 *sd = s_d[me.wave];
   float *sy = s_y[me.wave];
   float2 *sg = s_g[me.wave];
-  float4 *sh = s_h[me.wave] + me.lane;
+  States<NS> *sh = s_h[me.wave] + me.lane;
   const int c0 = me.s * p.chunk, c1 = min(p.T, c0 + p.chunk), end = min(c1, wave_length(p, me.b));
   const size_t seq = (size_t)me.b * p.D + me.d;
-  float A[NS], A2[NS], q[NS], dA[NS] = {0.f, 0.f, 0.f, 0.f};
-  load4(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
+  float A[NS], A2[NS], q[NS], dA[NS];
+  load_states<NS>(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
 #pragma unroll
-  for (int j = 0; j < NS; ++j) A2[j] = A[j] * LOG2E;
+  for (int j = 0; j < NS; ++j) { A2[j] = A[j] * LOG2E; dA[j] = 0.f; }
   if (p.nchunks > 1) {
-    take4(q, p.local + ((size_t)me.s * p.B * p.D + seq) * L + me.part, me.live);
+    const States<NS> v = pick<NS>(p.local + ((size_t)me.s * p.B * p.D + seq) * NP + me.part * NS);
+#pragma unroll
+    for (int j = 0; j < NS; ++j) q[j] = me.live ? v.v[j] : 0.f;
   } else {
-    load4(q, g.d_state ? g.d_state + seq * p.N : nullptr, me.part, p.N, me.live);
+    load_states<NS>(q, g.d_state ? g.d_state + seq * p.N : nullptr, me.part, p.N, me.live);
   }
   const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f, skip = p.skip ? p.skip[me.ed] : 0.f;
   float dskip = 0.f, ddtb = 0.f;
@@ -442,7 +445,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
   Stream<T, E> gx(p.x, me.b, me.ed, me.et), gd(p.dt, me.b, me.ed, me.et), gy(g.dy, me.b, me.ed, me.et), gz(p.z, me.b, me.ed, me.et);
   const Stream<T, E> wx(g.dx, me.b, me.ed, me.et), wd(g.ddt, me.b, me.ed, me.et), wz(g.dz, me.b, me.ed, me.et);
   Vectors<T, NP, THREADS> gb(p.bv, me.b, me.g, p.N, threadIdx.x), gc(p.cv, me.b, me.g, p.N, threadIdx.x);
-  float4 rh = make_float4(0.f, 0.f, 0.f, 0.f);
+  States<NS> rh;
   auto load = [&](int t0) {
     gx.fetch(t0, end);
     gd.fetch(t0, end);
@@ -450,7 +453,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
     if constexpr (GATE) gz.fetch(t0, end);
     gb.fetch(t0, end);
     gc.fetch(t0, end);
-    rh = p.saved[((size_t)(t0 / TILE) * p.B * p.D + seq) * L + me.part];
+    rh = pick<NS>(p.saved + ((size_t)(t0 / TILE) * p.B * p.D + seq) * NP + me.part * NS);
   };
   const int tiles = end > c0 ? (end - c0 + TILE - 1) / TILE : 0;
   {
@@ -483,18 +486,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
     }
     gb.put(s_b);
     gc.put(s_c);
-    float h0[NS] = {me.live ? rh.x : 0.f, me.live ? rh.y : 0.f, me.live ? rh.z : 0.f, me.live ? rh.w : 0.f};
+    float h0[NS], hn[NS];
+#pragma unroll
+    for (int j = 0; j < NS; ++j) hn[j] = h0[j] = me.live ? rh.v[j] : 0.f;
     float h[HALF + 1][NS], a[TILE][NS];                     // h: of the steps from HALF - 1 on
     __syncthreads();
     float k0[KEEP], k1[KEEP];                               // of the steps whose number mod L is this lane's part
     {
-      float hn[NS] = {h0[0], h0[1], h0[2], h0[3]};
       float2 u[2];                                          // what a step reads of LDS, loaded a step ahead
-      float4 b4[2], c4[2];
+      States<NS> bs[2], cs[2];
       const auto read = [&](int t) {
         u[t % 2] = *(const float2 *)(sd + t * CH + me.ch);
-        b4[t % 2] = *(const float4 *)(s_b + t * NP + me.part * NS);
-        if constexpr (GATE) c4[t % 2] = *(const float4 *)(s_c + t * NP + me.part * NS);
+        bs[t % 2] = pick<NS>(s_b + t * NP + me.part * NS);
+        if constexpr (GATE) cs[t % 2] = pick<NS>(s_c + t * NP + me.part * NS);
       };
       read(0);
 #pragma unroll
@@ -502,21 +506,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
         if (t + 1 < TILE) read(t + 1);
         __builtin_amdgcn_sched_barrier(0);
         const float2 un = u[t % 2];
-        const float4 bn = b4[t % 2];
-        const float bq[NS] = {bn.x, bn.y, bn.z, bn.w};
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
           a[t][j] = __builtin_amdgcn_exp2f(un.x * A2[j]);
-          hn[j] = fmaf(a[t][j], hn[j], un.y * bq[j]);
+          hn[j] = fmaf(a[t][j], hn[j], un.y * bs[t % 2].v[j]);
           if (t >= HALF - 1) h[t - HALF + 1][j] = hn[j];
         }
-        if (t < HALF - 1) sh[t * 64] = make_float4(hn[0], hn[1], hn[2], hn[3]);
-        if constexpr (GATE) {                                         // dz needs the output before the gate
-          const float4 cn = c4[t % 2];
-          float v = cn.x * hn[0];
-          v = fmaf(cn.y, hn[1], v);
-          v = fmaf(cn.z, hn[2], v);
-          v = fmaf(cn.w, hn[3], v);
+        if (t < HALF - 1) put_states<NS>((float *)(sh + t * 64), hn);
+        if constexpr (GATE) {                               // dz needs the output before the gate
+          float v = cs[t % 2].v[0] * hn[0];
+#pragma unroll
+          for (int j = 1; j < NS; ++j) v = fmaf(cs[t % 2].v[j], hn[j], v);
           v = sum_neighbours<L>(v);
           k0[t / L] = t % L == 0 || me.part == t % L ? v : k0[t / L];
         }
@@ -527,12 +527,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
     }
     asm volatile("" ::: "memory");                          // (the rows of Bv, Cv and sd are read again, not kept in registers)
     float hc[NS];                                           // the state after step t
-    float2 kv[TILE / TWINS];                                // of the steps whose number mod TWINS is this lane's among its twins
-    float4 ur[2], br[2], cr[2], hr[2];                      // what a step reads of LDS, loaded a step ahead
+    float kv[TILE / TWINS][NS / 2];                         // of the steps whose number mod TWINS is this lane's among its twins
+    float4 ur[2];                                           // what a step reads of LDS, loaded a step ahead
+    States<NS> br[2], cr[2], hr[2];
     const auto read = [&](int t) {
       ur[t % 2] = sd[t * CH + me.ch];
-      br[t % 2] = *(const float4 *)(s_b + t * NP + me.part * NS);
-      cr[t % 2] = *(const float4 *)(s_c + t * NP + me.part * NS);
+      br[t % 2] = pick<NS>(s_b + t * NP + me.part * NS);
+      cr[t % 2] = pick<NS>(s_c + t * NP + me.part * NS);
       if (t > 0 && t < HALF) hr[t % 2] = sh[(t - 1) * 64];
     };
     read(TILE - 1);
@@ -551,21 +552,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
         if constexpr (GATE) gz.fetch(next, stop);
         gb.fetch(next, stop);
         gc.fetch(next, stop);
-        rh = p.saved[((size_t)(next / TILE) * p.B * p.D + seq) * L + me.part];
+        rh = pick<NS>(p.saved + ((size_t)(next / TILE) * p.B * p.D + seq) * NP + me.part * NS);
       }
-      const float4 u = ur[t % 2], b4 = br[t % 2], c4 = cr[t % 2], h4 = hr[t % 2];
-      const float bq[NS] = {b4.x, b4.y, b4.z, b4.w}, cq[NS] = {c4.x, c4.y, c4.z, c4.w};
+      const float4 u = ur[t % 2];
       float v[2 * NS], gsum = 0.f, usum = 0.f, hp[NS];
-      if (t > 0 && t < HALF) { hp[0] = h4.x; hp[1] = h4.y; hp[2] = h4.z; hp[3] = h4.w; }
 #pragma unroll
       for (int j = 0; j < NS; ++j) {
         if (t == TILE - 1) hc[j] = h[HALF][j];
         if (t >= HALF) hp[j] = h[t - HALF][j];
-        if (t == 0) hp[j] = h0[j];
-        const float gh = fmaf(u.z, cq[j], q[j]);
+        else if (t > 0) hp[j] = hr[t % 2].v[j];
+        else hp[j] = h0[j];
+        const float gh = fmaf(u.z, cr[t % 2].v[j], q[j]);
         v[j] = gh * u.y;
         v[NS + j] = u.z * hc[j];
-        gsum = fmaf(gh, bq[j], gsum);
+        gsum = fmaf(gh, br[t % 2].v[j], gsum);
         q[j] = gh * a[t][j];
         const float w = q[j] * hp[j];
         hc[j] = hp[j];
@@ -577,16 +577,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
       const bool mine = t % L == L - 1 || me.part == t % L;
       k0[t / L] = mine ? gsum : k0[t / L];
       k1[t / L] = mine ? usum : k1[t / L];
-      const float2 s = sum_channels<L>(v);
+      float s[NS / 2];
+      sum_channels<NS, L>(v, s);
       const bool twin = t % TWINS == TWINS - 1 || (me.lane & 15) / L == t % TWINS;
-      kv[t / TWINS].x = twin ? s.x : kv[t / TWINS].x;
-      kv[t / TWINS].y = twin ? s.y : kv[t / TWINS].y;
+#pragma unroll
+      for (int j = 0; j < NS / 2; ++j) kv[t / TWINS][j] = twin ? s[j] : kv[t / TWINS][j];
     }
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) sg[(i * L + me.part) * CH + me.ch] = make_float2(k0[i], k1[i]);
 #pragma unroll
     for (int i = 0; i < TILE / TWINS; ++i)
-      *(float2 *)(&s_s[me.wave][me.lane >> 5][(i * TWINS + (me.lane & 15) / L) * NP + me.part * NS + ((me.lane >> 4) & 1) * 2]) = kv[i];
+      put_states<NS / 2>(&s_s[me.wave][me.lane >> 5][(i * TWINS + (me.lane & 15) / L) * NP + me.part * NS + ((me.lane >> 4) & 1) * (NS / 2)], kv[i]);
     wave_lds_order();
     float ox[E], od[E], oz[E];
 #pragma unroll
@@ -612,12 +613,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
     const int pitch = p.B * p.G * 2 * NP * 4;               // bytes between steps (scan_sizes: 16 of them stay below SPAN)
     const rsrc_t out = make_rsrc(g.dbc + ((((size_t)me.blk * p.T + t0) * p.B + me.b) * p.G + me.g) * (2 * NP), SPAN);
 #pragma unroll
-    for (int i = 0; i < 2 * TILE * NP / THREADS; ++i) {
+    for (int i = 0; i < (2 * TILE * NP + THREADS - 1) / THREADS; ++i) {
       const int at = i * THREADS + threadIdx.x, t = at / (2 * NP), kn = at % (2 * NP);
       float s = 0.f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) s += s_s[w][kn / NP][t * NP + kn % NP];
-      st_b32(out, t0 + t < end ? t * pitch + kn * 4 : NOWHERE, 0, __float_as_uint(s));
+      for (int w = 0; w < WAVES; ++w) s += s_s[w][kn / NP][t % TILE * NP + kn % NP];
+      st_b32(out, (t0 + t < end) & (at < 2 * TILE * NP) ? t * pitch + kn * 4 : NOWHERE, 0, __float_as_uint(s));
     }
   }
   // sums over the lanes that share a channel of the elementwise mapping: lane bits log2(CH) to 5
@@ -634,14 +635,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
     to[p.D] = s1;
   }
   if (!me.live) return;
-  g.dA[(((size_t)me.s * p.B + me.b) * p.D + me.d) * L + me.part] = make_float4(dA[0], dA[1], dA[2], dA[3]);
-  if (g.dinit && me.s == 0) store4(g.dinit + seq * p.N, q, me.part, p.N);
+  put_states<NS>(g.dA + (((size_t)me.s * p.B + me.b) * p.D + me.d) * NP + me.part * NS, dA);
+  if (g.dinit && me.s == 0) store_states<NS>(g.dinit + seq * p.N, q, me.part, p.N);
 }
 
 // dBv and dCv: sums of the workgroups' partial sums, zero where the step does not exist.  A thread per value.
-template <typename T, int L>
+template <typename T, int NP>
 __global__ __launch_bounds__(256) void scan_sum_rows_kernel(const ScanP p, const float *__restrict__ dbc, Rows<void> dbv, Rows<void> dcv) {
-  constexpr int NP = NS * L;
   const int64_t all = (int64_t)p.T * p.B * p.G * 2 * NP;
   for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
     const int n = (int)(id % NP), kind = (int)(id / NP % 2);
@@ -657,10 +657,9 @@ __global__ __launch_bounds__(256) void scan_sum_rows_kernel(const ScanP p, const
 }
 
 // dA, dskip, ddt_bias: sums over chunks and sequences.
-template <int L>
+template <int NP>
 __global__ __launch_bounds__(256) void scan_sum_params_kernel(const ScanP p, const float *__restrict__ dA_part, const float *__restrict__ dsum,
                                                               float *__restrict__ dA, float *__restrict__ dskip, float *__restrict__ ddt_bias) {
-  constexpr int NP = NS * L;
   __shared__ float lds[256];
   const int rows = p.nchunks * p.B;
   const int64_t na = (int64_t)p.D * NP, blocks = (na + 15) / 16;
@@ -682,6 +681,7 @@ __global__ __launch_bounds__(256) void scan_sum_params_kernel(const ScanP p, con
 // A lane holds four states of a (sequence, channel); the state [B][D][N] is read and written once, 16 bytes a lane where
 // N is a multiple of four and the rows are aligned (FOUR).
 template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void scan_step_kernel(const ScanP p) {
+  constexpr int NS = 4;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= (int64_t)p.B * p.D * L) return;                 // (the L lanes of a channel leave together)
   const int part = (int)(id % L);
@@ -693,11 +693,12 @@ template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void s
   float *state = p.state + seq * p.N;
   if constexpr (FOUR) {                                     // (N is 4, 8, .. : lanes beyond it read the last four)
     const int at = min(part * NS, p.N - NS);
-    take4(A, (const float4 *)(p.A + (int64_t)d * p.N + at), some);
-    take4(h, (const float4 *)(state + at), some);
+    const States<NS> av = pick<NS>(p.A + (int64_t)d * p.N + at), hv = pick<NS>(state + at);
+#pragma unroll
+    for (int j = 0; j < NS; ++j) { A[j] = some ? av.v[j] : 0.f; h[j] = some ? hv.v[j] : 0.f; }
   } else {
-    load4(A, p.A + (int64_t)d * p.N, part, p.N, true);
-    load4(h, state, part, p.N, true);
+    load_states<NS>(A, p.A + (int64_t)d * p.N, part, p.N, true);
+    load_states<NS>(h, state, part, p.N, true);
   }
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
@@ -716,9 +717,9 @@ template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void s
   }
   v = sum_neighbours<L>(v);
   if constexpr (FOUR) {
-    if (some) *(float4 *)(state + part * NS) = make_float4(h[0], h[1], h[2], h[3]);
+    if (some) put_states<NS>(state + part * NS, h);
   } else {
-    store4(state, h, part, p.N);
+    store_states<NS>(state, h, part, p.N);
   }
   if (part == 0) {
     if (p.skip) v = fmaf(p.skip[d], x, v);
@@ -728,13 +729,37 @@ template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void s
 }
 
 // ---------------------------------------------------------------- host side
-int lanes_of(int N) { return N <= 16 ? 4 : N <= 32 ? 8 : 16; }   // L
-constexpr int WAVES = 4;                                    // of a workgroup
+// How a call's states lie in lanes: NS of a channel in each of L lanes, NP = NS L of them with those that are zero, and
+// wavefronts of a workgroup (64 channels to a workgroup where that is eight wavefronts or less).
+struct Shape {
+  int NS, L, waves;
+  int channels() const { return 64 / L * waves; }
+};
+template <int NS_, int L_, int W_> struct FixedShape {
+  static constexpr int NS = NS_, L = L_, W = W_, NP = NS_ * L_;
+};
+int padded(int N) { return N <= 8 ? 8 : N <= 16 ? 16 : N <= 32 ? 32 : 64; }
+// Wavefronts of a call with four states a lane, time uncut.
+int64_t waves_of_four(const snn_scan_args &a) {
+  const int64_t dg = a.D / a.groups, per = 256 / padded(a.N);
+  return (int64_t)a.B * a.groups * ((dg + per - 1) / per);
+}
+// Four states a lane.  Two, with twice the wavefronts and more to do around each state, where a forward pass has one to
+// two wavefronts of four for each of the 1024 SIMDs: 1024 steps of 8 x 2048 channels of 16 states (1024 wavefronts)
+// take 104 us with two against 116 with four, 119 with four and time in four chunks; at 4096 wavefronts 79 with
+// four, 93 with two.  (Up to eight states: always two in each of four lanes.)
+Shape shape_of(const snn_scan_args &a, bool backward) {
+  const int np = padded(a.N);
+  if (np == 8) return {2, 4, 4};
+  const int64_t waves = waves_of_four(a);
+  if (!backward && np < 64 && waves >= 1024 && waves < 2048) return {2, np / 2, 8};
+  return {4, np / 4, 4};
+}
 
 // Workgroups per (chunk, sequence, group).
-int blocks_of(const snn_scan_args &a, int L) {
-  const int per = 64 / L * WAVES, dg = a.D / a.groups;
-  return (dg + per - 1) / per;
+int blocks_of(const snn_scan_args &a, const Shape &k) {
+  const int dg = a.D / a.groups;
+  return (dg + k.channels() - 1) / k.channels();
 }
 
 int scan_sizes(const snn_scan_args *a) {
@@ -781,10 +806,14 @@ int scan_strides(const snn_scan_args *a, const snn_rows *rows, int count) {
   return SNN_OK;
 }
 
-// How time is cut: enough chunks that every SIMD has a wavefront, of at least 64 steps.
-void scan_cut(const snn_scan_args &a, int L, int *chunk, int *nchunks) {
-  const int64_t waves = (int64_t)a.B * a.groups * blocks_of(a, L) * WAVES;
-  int64_t n = 1024 / waves;
+// How time is cut: into chunks of at least 64 steps for 4096 wavefronts, four to a SIMD, where there are few; not at
+// all where there are 1024 (forward, which does a chunk twice but for the outputs) or 1536 (reverse, which does half of
+// the work twice).  16 states, one cut for 4096 wavefronts against none, us: forward, 512 wavefronts (1024 steps of
+// 4 x 2048 channels) 70 and 100; 1024 wavefronts 119 and 116; forward and reverse, 512 wavefronts 240 and 324, 1024
+// wavefronts 417 and 445, 1536 wavefronts 331 and 332.  Cut for 2048 wavefronts, the case of 512 takes 75 and 253.
+void scan_cut(const snn_scan_args &a, const Shape &k, bool backward, int *chunk, int *nchunks) {
+  const int64_t waves = (int64_t)a.B * a.groups * blocks_of(a, k) * k.waves, enough = backward ? 1536 : 1024;
+  int64_t n = waves < enough ? 4096 / waves : 1;
   if (n > a.T / 64) n = a.T / 64;
   if (n < 1) n = 1;
   const int64_t tiles = ((int64_t)a.T + TILE - 1) / TILE;
@@ -798,79 +827,79 @@ struct ScanSpace {
   size_t local, sums, dA, dsum, dbc, all;
 };
 ScanSpace scan_space(const snn_scan_args &a, bool backward) {
-  const int L = lanes_of(a.N);
+  const Shape k = shape_of(a, backward);
   int chunk, n;
-  scan_cut(a, L, &chunk, &n);
-  const size_t seqs = (size_t)a.B * a.D;
+  scan_cut(a, k, backward, &chunk, &n);
+  const size_t seqs = (size_t)a.B * a.D, np = padded(a.N);
   ScanSpace s;
   s.local = 0;
-  s.sums = s.local + (n > 1 ? rup256(n * seqs * L * 16) : 0);
+  s.sums = s.local + (n > 1 ? rup256(n * seqs * np * 4) : 0);
   s.dA = s.sums + (n > 1 ? rup256(n * seqs * 4) : 0);
-  s.dsum = s.dA + (backward ? rup256(n * seqs * L * 16) : 0);
+  s.dsum = s.dA + (backward ? rup256(n * seqs * np * 4) : 0);
   s.dbc = s.dsum + (backward ? rup256(n * seqs * 8) : 0);
-  s.all = s.dbc + (backward ? rup256((size_t)blocks_of(a, L) * a.T * a.B * a.groups * 2 * NS * L * 4) : 0);
+  s.all = s.dbc + (backward ? rup256((size_t)blocks_of(a, k) * a.T * a.B * a.groups * 2 * np * 4) : 0);
   return s;
 }
 
-// f(a value of the streamed type, L)
-template <typename F> int with_kind(const snn_scan_args &a, F f) {
-  const int L = lanes_of(a.N);
-  const auto lanes = [&](auto zero) {
-    return L == 4 ? f(zero, std::integral_constant<int, 4>()) : L == 8 ? f(zero, std::integral_constant<int, 8>()) : f(zero, std::integral_constant<int, 16>());
+// f(a value of the streamed type, a FixedShape)
+template <bool BACKWARD, typename F> int with_kind(const snn_scan_args &a, const Shape &k, F f) {
+  const auto shapes = [&](auto zero) {
+    if (k.NS == 4) return k.L == 4 ? f(zero, FixedShape<4, 4, 4>()) : k.L == 8 ? f(zero, FixedShape<4, 8, 4>()) : f(zero, FixedShape<4, 16, 4>());
+    if constexpr (!BACKWARD)
+      if (k.L > 4) return k.L == 8 ? f(zero, FixedShape<2, 8, 8>()) : f(zero, FixedShape<2, 16, 8>());
+    return f(zero, FixedShape<2, 4, 4>());
   };
-  return a.type == SNN_TYPE_FP32 ? lanes(0.f) : lanes((__bf16)0.f);
+  return a.type == SNN_TYPE_FP32 ? shapes(0.f) : shapes((__bf16)0.f);
 }
 
-ScanP plan(const snn_scan_args &a, int L, char *ws, const ScanSpace &s) {
+ScanP plan(const snn_scan_args &a, const Shape &k, bool backward, const void *saved, char *ws, const ScanSpace &s) {
   ScanP p(a);
-  scan_cut(a, L, &p.chunk, &p.nchunks);
-  p.blocks = blocks_of(a, L);
-  if (p.nchunks > 1) { p.local = (float4 *)(ws + s.local); p.sums = (float *)(ws + s.sums); }
+  scan_cut(a, k, backward, &p.chunk, &p.nchunks);
+  p.blocks = blocks_of(a, k);
+  p.saved = (float *)const_cast<void *>(saved);
+  if (p.nchunks > 1) { p.local = (float *)(ws + s.local); p.sums = (float *)(ws + s.sums); }
   return p;
 }
 
-template <typename T, int L, bool GATE> int forward(const snn_scan_args &a, void *saved, char *ws, hipStream_t st) {
-  constexpr int W = WAVES;
-  ScanP p = plan(a, L, ws, scan_space(a, false));
-  p.saved = (float4 *)saved;
+template <typename T, typename K, bool GATE> int forward(const snn_scan_args &a, const Shape &k, void *saved, char *ws, hipStream_t st) {
+  const ScanP p = plan(a, k, false, saved, ws, scan_space(a, false));
   const unsigned per = (unsigned)((size_t)p.blocks * p.G * p.B);
   int rc = SNN_OK;
   if (p.nchunks > 1) {
-    hipLaunchKernelGGL((scan_forward_kernel<T, L, W, false, true>), dim3(per * (p.nchunks - 1)), dim3(64 * W), 0, st, p);
+    hipLaunchKernelGGL((scan_forward_kernel<T, K::NS, K::L, K::W, false, true>), dim3(per * (p.nchunks - 1)), dim3(64 * K::W), 0, st, p);
     if ((rc = ops_launched("scan, chunks"))) return rc;
-    hipLaunchKernelGGL((scan_join_kernel<L, false>), dim3((unsigned)(((int64_t)p.B * p.D * L + 255) / 256)), dim3(256), 0, st, p, a.init);
+    hipLaunchKernelGGL((scan_join_kernel<K::NP, false>), dim3((unsigned)(((int64_t)p.B * p.D * K::NP + 255) / 256)), dim3(256), 0, st, p, a.init);
     if ((rc = ops_launched("scan, join"))) return rc;
   }
-  hipLaunchKernelGGL((scan_forward_kernel<T, L, W, GATE, false>), dim3(per * p.nchunks), dim3(64 * W), 0, st, p);
+  hipLaunchKernelGGL((scan_forward_kernel<T, K::NS, K::L, K::W, GATE, false>), dim3(per * p.nchunks), dim3(64 * K::W), 0, st, p);
   return ops_launched("scan");
 }
 
-template <typename T, int L, bool GATE> int backward(const snn_scan_args &a, const snn_scan_grads &gr, const void *saved, char *ws, hipStream_t st) {
-  constexpr int W = WAVES;
+template <typename T, typename K, bool GATE>
+int backward(const snn_scan_args &a, const Shape &k, const snn_scan_grads &gr, const void *saved, char *ws, hipStream_t st) {
   const ScanSpace s = scan_space(a, true);
-  ScanP p = plan(a, L, ws, s);
-  p.saved = (float4 *)const_cast<void *>(saved);
+  const ScanP p = plan(a, k, true, saved, ws, s);
   ScanGradP g(gr);
-  g.dA = (float4 *)(ws + s.dA);
+  g.dA = (float *)(ws + s.dA);
   g.dsum = (float *)(ws + s.dsum);
   g.dbc = (float *)(ws + s.dbc);
   const unsigned per = (unsigned)((size_t)p.blocks * p.G * p.B);
   int rc = SNN_OK;
   if (p.nchunks > 1) {
-    hipLaunchKernelGGL((scan_reverse_local_kernel<T, L, W, GATE>), dim3(per * (p.nchunks - 1)), dim3(64 * W), 0, st, p, g);
+    hipLaunchKernelGGL((scan_reverse_local_kernel<T, K::NS, K::L, K::W, GATE>), dim3(per * (p.nchunks - 1)), dim3(64 * K::W), 0, st, p, g);
     if ((rc = ops_launched("scan reverse, chunks"))) return rc;
-    hipLaunchKernelGGL((scan_join_kernel<L, true>), dim3((unsigned)(((int64_t)p.B * p.D * L + 255) / 256)), dim3(256), 0, st, p, gr.d_state);
+    hipLaunchKernelGGL((scan_join_kernel<K::NP, true>), dim3((unsigned)(((int64_t)p.B * p.D * K::NP + 255) / 256)), dim3(256), 0, st, p, gr.d_state);
     if ((rc = ops_launched("scan reverse, join"))) return rc;
   }
-  hipLaunchKernelGGL((scan_reverse_kernel<T, L, W, GATE>), dim3(per * p.nchunks), dim3(64 * W), 0, st, p, g);
+  hipLaunchKernelGGL((scan_reverse_kernel<T, K::NS, K::L, K::W, GATE>), dim3(per * p.nchunks), dim3(64 * K::W), 0, st, p, g);
   if ((rc = ops_launched("scan reverse"))) return rc;
-  const int64_t values = (int64_t)a.T * a.B * a.groups * 2 * NS * L;
+  const int64_t values = (int64_t)a.T * a.B * a.groups * 2 * K::NP;
   if (values) {
-    hipLaunchKernelGGL((scan_sum_rows_kernel<T, L>), dim3((unsigned)std::min<int64_t>((values + 255) / 256, 1 << 16)), dim3(256), 0, st, p, g.dbc, Rows<void>(gr.dbv), Rows<void>(gr.dcv));
+    hipLaunchKernelGGL((scan_sum_rows_kernel<T, K::NP>), dim3((unsigned)std::min<int64_t>((values + 255) / 256, 1 << 16)), dim3(256), 0, st, p, g.dbc, Rows<void>(gr.dbv), Rows<void>(gr.dcv));
     if ((rc = ops_launched("scan reverse, rows"))) return rc;
   }
-  const int64_t groups = ((int64_t)a.D * NS * L + 15) / 16 + (2 * (int64_t)a.D + 15) / 16;
-  hipLaunchKernelGGL((scan_sum_params_kernel<L>), dim3((unsigned)groups), dim3(256), 0, st, p, (const float *)g.dA, g.dsum, gr.dA, gr.dskip, gr.ddt_bias);
+  const int64_t groups = ((int64_t)a.D * K::NP + 15) / 16 + (2 * (int64_t)a.D + 15) / 16;
+  hipLaunchKernelGGL((scan_sum_params_kernel<K::NP>), dim3((unsigned)groups), dim3(256), 0, st, p, g.dA, g.dsum, gr.dA, gr.dskip, gr.ddt_bias);
   return ops_launched("scan reverse, parameters");
 }
 
@@ -880,6 +909,9 @@ template <typename T, int L> int step(const snn_scan_args &a, hipStream_t st) {
   if (a.N % 4 == 0 && aligned(a.A, 16) && aligned(a.state, 16)) hipLaunchKernelGGL((scan_step_kernel<T, L, true>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((scan_step_kernel<T, L, false>), grid, dim3(256), 0, st, p);
   return ops_launched("scan step");
+}
+template <typename T> int step_of(const snn_scan_args &a, hipStream_t st) {
+  return a.N <= 4 ? step<T, 1>(a, st) : a.N <= 8 ? step<T, 2>(a, st) : a.N <= 16 ? step<T, 4>(a, st) : a.N <= 32 ? step<T, 8>(a, st) : step<T, 16>(a, st);
 }
 
 int check_workspace(size_t need, const void *ws, size_t have) {
@@ -907,7 +939,7 @@ int32_t snn_scan_saved_bytes(const snn_scan_args *a, size_t *bytes) {
   if (!bytes) return ops_fail(SNN_ERR_NULL, "bytes is NULL");
   int rc = scan_sizes(a);
   if (rc) return rc;
-  *bytes = ((size_t)a->T + TILE - 1) / TILE * a->B * a->D * lanes_of(a->N) * 16;
+  *bytes = ((size_t)a->T + TILE - 1) / TILE * a->B * a->D * padded(a->N) * 4;
   return SNN_OK;
 }
 
@@ -918,10 +950,12 @@ int32_t snn_scan_forward(const snn_scan_args *a, void *saved, void *workspace, s
   if ((rc = scan_strides(a, rows, 6))) return rc;
   if (!aligned(saved, 16)) return ops_fail(SNN_ERR_ARG, "scan: saved must be 16-byte aligned");
   if ((rc = check_workspace(scan_space(*a, false).all, workspace, workspace_bytes))) return rc;
-  return with_kind(*a, [&](auto zero, auto l) {
+  const Shape k = shape_of(*a, false);
+  return with_kind<false>(*a, k, [&](auto zero, auto fixed) {
     using T = decltype(zero);
-    return a->z.p ? forward<T, l.value, true>(*a, saved, (char *)workspace, (hipStream_t)stream)
-                  : forward<T, l.value, false>(*a, saved, (char *)workspace, (hipStream_t)stream);
+    using K = decltype(fixed);
+    return a->z.p ? forward<T, K, true>(*a, k, saved, (char *)workspace, (hipStream_t)stream)
+                  : forward<T, K, false>(*a, k, saved, (char *)workspace, (hipStream_t)stream);
   });
 }
 
@@ -940,17 +974,19 @@ int32_t snn_scan_backward(const snn_scan_args *a, const snn_scan_grads *g, const
   if ((rc = scan_strides(a, rows, 9))) return rc;
   if (!aligned(saved, 16)) return ops_fail(SNN_ERR_ARG, "scan backward: saved must be 16-byte aligned");
   if ((rc = check_workspace(scan_space(*a, true).all, workspace, workspace_bytes))) return rc;
-  return with_kind(*a, [&](auto zero, auto l) {
+  const Shape k = shape_of(*a, true);
+  return with_kind<true>(*a, k, [&](auto zero, auto fixed) {
     using T = decltype(zero);
-    return a->z.p ? backward<T, l.value, true>(*a, *g, saved, (char *)workspace, (hipStream_t)stream)
-                  : backward<T, l.value, false>(*a, *g, saved, (char *)workspace, (hipStream_t)stream);
+    using K = decltype(fixed);
+    return a->z.p ? backward<T, K, true>(*a, k, *g, saved, (char *)workspace, (hipStream_t)stream)
+                  : backward<T, K, false>(*a, k, *g, saved, (char *)workspace, (hipStream_t)stream);
   });
 }
 
 int32_t snn_scan_step(const snn_scan_args *a, void *stream) {
   int rc = scan_check(a, true, false);
   if (rc) return rc;
-  return with_kind(*a, [&](auto zero, auto l) { return step<decltype(zero), l.value>(*a, (hipStream_t)stream); });
+  return a->type == SNN_TYPE_FP32 ? step_of<float>(*a, (hipStream_t)stream) : step_of<__bf16>(*a, (hipStream_t)stream);
 }
 
 }  // extern "C"
