@@ -7,6 +7,11 @@
 // times, with all loads of the chunk issued before the first result.
 // Every operation is rounded by itself (no contraction), so that the codes of 8-bit moments do not depend on how the
 // compiler joins operations.
+// With 8-bit moments the arithmetic counts as well (the random bits, two roundings, the scales: 38 us for 7.6 million
+// parameters when root and quotient were the correctly rounded ones, about ten operations more each).  There the roots
+// of single elements and the quotient come from the hardware's approximations, one unit of the last place off: the
+// parameter feels 2^-23 of its update, and a code does not feel it, since a root taken for just below a code or just
+// above goes to that code with a chance next to 1 from either side.  The root that the scale goes by is exact.
 #include "seq_common.hpp"
 
 #include <math.h>
@@ -187,8 +192,13 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamP p) {
       const float gj = g[k][j] * p.grad_scale;
       m[k][j] = m[k][j] * p.b1 + gj * p.c1;
       v[k][j] = v[k][j] * p.b2 + (gj * gj) * p.c2;
-      root[j] = sqrtf(v[k][j]);
-      w[k][j] = w[k][j] * keep - (m[k][j] * p.k1) / (root[j] * p.k2 + p.eps);
+      if constexpr (BITS == 8) {
+        root[j] = __builtin_amdgcn_sqrtf(v[k][j]);
+        w[k][j] = w[k][j] * keep - (m[k][j] * p.k1) * rcp_fast(root[j] * p.k2 + p.eps);
+      } else {
+        root[j] = sqrtf(v[k][j]);
+        w[k][j] = w[k][j] * keep - (m[k][j] * p.k1) / (root[j] * p.k2 + p.eps);
+      }
     }
     if constexpr (BITS == 8) {
       // 32 lanes hold a block: its largest finite magnitudes give the scales
@@ -198,15 +208,16 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamP p) {
         const bool in = i + j < n;
         if (!in) { m[k][j] = 0.f; v[k][j] = 0.f; root[j] = 0.f; }
         tm = fmaxf(tm, finite(m[k][j]) ? fabsf(m[k][j]) : 0.f);
-        tv = fmaxf(tv, finite(v[k][j]) ? root[j] : 0.f);
+        tv = fmaxf(tv, finite(v[k][j]) ? v[k][j] : 0.f);
       }
-      const int em = scale_exponent(max_neighbours<32>(tm)), ev = scale_exponent(max_neighbours<32>(tv));
+      const int em = scale_exponent(max_neighbours<32>(tm)), ev = scale_exponent(sqrtf(max_neighbours<32>(tv)));
       const float im = power2(-em), iv = power2(-ev);
       uint32_t qm = 0, qv = 0;
+      const int64_t where = at + i;                        // (a multiple of four)
+      const uint32_t first = (uint32_t)where * 0x9E3779B1u + (uint32_t)(where >> 32) * 0xC2B2AE3Du + p.salt;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int64_t where = at + i + j;
-        const uint32_t rand = stir((uint32_t)where * 0x9E3779B1u + (uint32_t)(where >> 32) * 0xC2B2AE3Du + p.salt);
+        const uint32_t rand = stir(first + j * 0x9E3779B1u);
         qm |= code_m(m[k][j], im, rand) << (8 * j);
         qv |= code_v(v[k][j], root[j], iv, rand) << (8 * j);
       }

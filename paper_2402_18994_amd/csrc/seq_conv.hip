@@ -1,42 +1,31 @@
 // Short causal convolution along time, one filter of W taps per channel (include/snn_ops.h):
 //   v[t,d] = bias[d] + sum_(k<W) w[d,k] x[t-(W-1)+k, d],  y = v or v sigmoid(v).
-// Tensors are time-major with the channels fastest, so a thread owns VEC neighbouring channels of one sequence and
-// walks a segment of its steps with the last W - 1 inputs in registers: every row piece is read and written once, as
-// 16 bytes where the layout allows, and a wavefront's access is one contiguous kilobyte.
+// Bound by memory: every row piece is read once and written once.  Tensors are time-major with the channels fastest; a
+// wavefront owns 64 lanes x VEC neighbouring channels of one sequence and walks a segment of its steps with the last
+// W - 1 inputs in registers, AHEAD rows in flight.  Sequence, segment and length are the same for the whole wavefront,
+// so all tests are on scalars, and a row that does not exist is a buffer access that the hardware drops.
+#include "common.hpp"
 #include "seq_common.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace snn {
 namespace {
 
-#ifndef CV
-#define CV 8
-#endif
-#ifndef CSEG
-#define CSEG 32
-#endif
-#ifndef CAH
-#define CAH 8
-#endif
-#ifndef BSEG
-#define BSEG 32
-#endif
-#ifndef BBL
-#define BBL 1024
-#endif
-constexpr int AHEAD = CAH;            // rows in flight per thread, forward
-constexpr int AHEAD_BWD = 4;
+constexpr int AHEAD = 4;            // rows in flight per wavefront, forward (8: 2 to 7 % slower) ..
+constexpr int AHEAD_BWD = 2;        // .. and of x and of dy each, reverse (4: 1 % either way)
+constexpr int SPAN = 0x7FFF0000, NOWHERE = 0x7FFFFF00;     // see seq_scan.hip: lane offsets stay below the first
 
 struct ConvP {
-  int T, B, D, silu, seg, nseg;
+  int T, B, D, silu, seg, nseg, groups;                    // groups: of 64 * VEC channels
   Rows<void> x, y;
   const float *weight, *bias;
   const void *init;
   const int32_t *lengths;
   void *state;
   explicit ConvP(const snn_conv_args &a)
-      : T(a.T), B(a.B), D(a.D), silu(a.silu), seg(1), nseg(1), x(a.x), y(a.y), weight(a.weight), bias(a.bias), init(a.init),
+      : T(a.T), B(a.B), D(a.D), silu(a.silu), seg(1), nseg(1), groups(1), x(a.x), y(a.y), weight(a.weight), bias(a.bias), init(a.init),
         lengths(a.lengths), state(a.state) {}
 };
 
@@ -50,78 +39,88 @@ __device__ __forceinline__ void load_filter(const ConvP &a, int d, float w[W][VE
   }
 }
 
-// Row `t` of the input of sequence b, t from -(W-1) on; zeros before the first step without `init`, and for t >= end.
+// VEC channels of a row; `on` (a scalar): whether the row exists, zeros if not.  `at`: the lane's byte offset.
+template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> load_row(const T *row, int at, bool on) {
+  using Packed = Pack<T, VEC>;
+  const rsrc_t r = make_rsrc(row, SPAN);
+  const int off = on ? at : NOWHERE;
+  if constexpr (sizeof(T) * VEC == 16) return __builtin_bit_cast(Packed, ld_b128(r, off, 0));
+  else if constexpr (sizeof(T) * VEC == 8) return __builtin_bit_cast(Packed, ld_b64(r, off, 0));
+  else if constexpr (sizeof(T) * VEC == 4) return __builtin_bit_cast(Packed, ld_b32(r, off, 0));
+  else return __builtin_bit_cast(Packed, (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
+}
+template <typename T, int VEC> __device__ __forceinline__ void store_row(T *row, int at, Pack<T, VEC> v) {
+  const rsrc_t r = make_rsrc(row, SPAN);
+  if constexpr (sizeof(T) * VEC == 16) st_b128(r, at, 0, __builtin_bit_cast(u32x4, v));
+  else if constexpr (sizeof(T) * VEC == 8) st_b64(r, at, 0, __builtin_bit_cast(u32x2, v));
+  else if constexpr (sizeof(T) * VEC == 4) st_b32(r, at, 0, __builtin_bit_cast(uint32_t, v));
+  else st_b16(r, at, 0, __builtin_bit_cast(unsigned short, v));
+}
+// Row `t` of the input of sequence b, from -(W-1) on; zeros before the first step without `init`, and for t >= end.
 template <typename T, int VEC, int W>
-__device__ __forceinline__ Pack<T, VEC> input_row(const ConvP &a, const T *x, int b, int d, int t, int end) {
-  Pack<T, VEC> r;
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) r.v[v] = (T)0.f;
-  if (t >= 0) {
-    if (t < end) r = *(const Pack<T, VEC> *)(x + (int64_t)t * a.x.st);
-  } else if (a.init) {
-    r = *(const Pack<T, VEC> *)((const T *)a.init + ((size_t)(t + W - 1) * a.B + b) * a.D + d);
-  }
-  return r;
+__device__ __forceinline__ Pack<T, VEC> input_row(const ConvP &a, int b, int at, int t, int end) {
+  const T *p = t >= 0 ? (const T *)a.x.p + b * a.x.sb + t * a.x.st : (const T *)a.init + ((int64_t)(t + W - 1) * a.B + b) * a.D;
+  return load_row<T, VEC>(p, at, t >= 0 ? t < end : a.init != nullptr);
 }
 
-// Forward: blockIdx.y is the segment.
+// Forward.  A wavefront takes one (segment, sequence, channel group), in the order of the memory: wavefronts that run at
+// the same time share rows of it.
 template <typename T, int VEC, int W>
 __global__ __launch_bounds__(256) void conv_forward_kernel(const ConvP a) {
-  const int dv = a.D / VEC;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= (int64_t)a.B * dv) return;
-  const int b = (int)(id / dv), d = (int)(id % dv) * VEC;
-  const int len = length_of(a.lengths, b, a.T);
-  const T *x = (const T *)a.x.p + b * a.x.sb + d;
-  T *y = (T *)a.y.p + b * a.y.sb + d;
-  const int64_t t0 = (int64_t)blockIdx.y * a.seg;
-  const int t1 = (int)min((int64_t)a.T, t0 + a.seg), end = min(t1, len);
+  const int lane = threadIdx.x & 63;
+  int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = (int)(id % a.groups);
+  id /= a.groups;
+  const int b = (int)(id % a.B), s = (int)(id / a.B);
+  if (s >= a.nseg) return;
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a.lengths, b, a.T));
+  const int d = (group * 64 + lane) * VEC;
+  const bool live = d < a.D;
+  const int at = live ? d * (int)sizeof(T) : NOWHERE;
+  const int t0 = s * a.seg, t1 = min(a.T, t0 + a.seg), end = min(t1, len);
+  T *y = (T *)a.y.p + b * a.y.sb;
 
   float w[W][VEC], bias[VEC], xs[W - 1 + AHEAD][VEC];
-  load_filter<T, VEC, W>(a, d, w, bias);
+  load_filter<T, VEC, W>(a, live ? d : 0, w, bias);
 #pragma unroll
   for (int k = 0; k < W - 1; ++k) {
-    const Pack<T, VEC> r = input_row<T, VEC, W>(a, x, b, d, (int)t0 - (W - 1) + k, end);
+    const Pack<T, VEC> r = input_row<T, VEC, W>(a, b, at, t0 - (W - 1) + k, len);
 #pragma unroll
     for (int v = 0; v < VEC; ++v) xs[k][v] = widen(r.v[v]);
   }
+  const T *x = (const T *)a.x.p + b * a.x.sb;
   Pack<T, VEC> next[AHEAD];
 #pragma unroll
-  for (int u = 0; u < AHEAD; ++u) next[u] = input_row<T, VEC, W>(a, x, b, d, (int)t0 + u, end);
-  for (int t = (int)t0; t < t1; t += AHEAD) {
+  for (int u = 0; u < AHEAD; ++u) next[u] = load_row<T, VEC>(x + (t0 + u) * a.x.st, at, t0 + u < end);
+  for (int t = t0; t < t1; t += AHEAD) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) xs[W - 1 + u][v] = widen(next[u].v[v]);
-    if (t + AHEAD < t1) {
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) next[u] = input_row<T, VEC, W>(a, x, b, d, t + AHEAD + u, end);
-    }
+    for (int u = 0; u < AHEAD; ++u) next[u] = load_row<T, VEC>(x + (t + AHEAD + u) * a.x.st, at, t + AHEAD + u < end);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      if (t + u < t1) {
-        Pack<T, VEC> r;
+      Pack<T, VEC> r;
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          float s = bias[v];
+      for (int v = 0; v < VEC; ++v) {
+        float q = bias[v];
 #pragma unroll
-          for (int k = 0; k < W; ++k) s = fmaf(w[k][v], xs[u + k][v], s);
-          if (a.silu) s *= sigmoid_fast(s);
-          r.v[v] = narrow<T>(t + u < len ? s : 0.f);
-        }
-        *(Pack<T, VEC> *)(y + (int64_t)(t + u) * a.y.st) = r;
+        for (int k = 0; k < W; ++k) q = fmaf(w[k][v], xs[u + k][v], q);
+        const float g = q * sigmoid_fast(q);
+        r.v[v] = narrow<T>(t + u < len ? (a.silu ? g : q) : 0.f);
       }
+      store_row<T, VEC>(y + (t + u) * a.y.st, t + u < t1 ? at : NOWHERE, r);
     }
 #pragma unroll
     for (int k = 0; k < W - 1; ++k)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) xs[k][v] = xs[k + AHEAD][v];
   }
-  if (a.state && blockIdx.y == 0) {
+  if (a.state && s == 0) {
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
-      *(Pack<T, VEC> *)((T *)a.state + ((size_t)j * a.B + b) * a.D + d) =
-          input_row<T, VEC, W>(a, x, b, d, len - (W - 1) + j, len);
+      store_row<T, VEC>((T *)a.state + ((int64_t)j * a.B + b) * a.D, at, input_row<T, VEC, W>(a, b, at, len - (W - 1) + j, len));
   }
 }
 
@@ -153,29 +152,27 @@ __global__ __launch_bounds__(256) void conv_step_kernel(const ConvP a) {
   for (int k = 0; k < W - 1; ++k) *(Pack<T, VEC> *)(state + k * row) = r[k + 1];
 }
 
-// Backward.  With q[t] = dy[t] (dv/dy at step t; zero outside [0, len)):
+// Backward.  With q[t] = dL/dv at step t, which is dy[t] times the slope of f (zero outside [0, len)):
 //   dx[s] = sum_k w[k] q[s + (W-1) - k],  dw[k] = sum_(t,b) q[t] x[t-(W-1)+k],  dbias = sum_(t,b) q[t].
-// A thread walks its segment of a sequence and W - 1 steps more (dx of the last steps needs their q; v is computed
-// again from x), emitting the gradient of input row t - (W-1) at step t.  A workgroup's threads stand in R rows of LX
-// channel groups; every row takes (sequence, segment) items in turn, with dw and dbias in registers, and at the end
-// the rows' sums go through LDS into one partial sum per workgroup, added up by sum_rows_kernel in a fixed order.
+// A wavefront walks its segment of a sequence and W - 1 steps more (dx of the last steps needs their q; v is computed
+// again from x), emitting the gradient of input row t - (W-1) at step t.  The four wavefronts of a workgroup are on the
+// same channels; each takes (sequence, segment) items in turn, with dw and dbias in registers, and at the end their
+// sums go through LDS into one partial sum per workgroup, added up by conv_sum_kernel in a fixed order.
 struct ConvGradP {
   Rows<void> dy, dx;
   const void *d_state;
   void *dinit;
   float *partial;                    // [gridDim.y][W+1][D]
-  int lx_log2;
-  ConvGradP(const snn_conv_grads &g) : dy(g.dy), dx(g.dx), d_state(g.d_state), dinit(g.dinit), partial(nullptr), lx_log2(0) {}
+  ConvGradP(const snn_conv_grads &g, float *ws) : dy(g.dy), dx(g.dx), d_state(g.d_state), dinit(g.dinit), partial(ws) {}
 };
 
 template <typename T, int VEC, int W>
 __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvP a, const ConvGradP g) {
-  __shared__ float part[256 * VEC];
-  const int lx = 1 << g.lx_log2, rows = 256 >> g.lx_log2;
-  const int lane = threadIdx.x & (lx - 1), row = threadIdx.x >> g.lx_log2;
-  const int dv = a.D / VEC, chunk = blockIdx.x * lx + lane;
-  const bool live = chunk < dv;
-  const int d = chunk * VEC;
+  __shared__ float part[4][64 * VEC];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int d = (blockIdx.x * 64 + lane) * VEC;
+  const bool live = d < a.D;
+  const int at = live ? d * (int)sizeof(T) : NOWHERE;
   float w[W][VEC], bias[VEC], dw[W][VEC], db[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
@@ -183,97 +180,83 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvP a, const
 #pragma unroll
     for (int k = 0; k < W; ++k) dw[k][v] = 0.f;
   }
-  if (live) {
-    load_filter<T, VEC, W>(a, d, w, bias);
-    const int64_t items = (int64_t)a.B * a.nseg;
-    for (int64_t item = (int64_t)blockIdx.y * rows + row; item < items; item += (int64_t)gridDim.y * rows) {
-      const int b = (int)(item / a.nseg), s0 = (int)(item % a.nseg);
-      const int len = length_of(a.lengths, b, a.T);
-      const T *x = (const T *)a.x.p + b * a.x.sb + d;
-      const T *dy = (const T *)g.dy.p + b * g.dy.sb + d;
-      T *dx = (T *)g.dx.p + b * g.dx.sb + d;
-      const int t0 = s0 * a.seg, t1 = min(a.T, t0 + a.seg), stop = t1 + W - 1;
-      float xs[W - 1 + AHEAD_BWD][VEC], q[W - 1 + AHEAD_BWD][VEC];
+  load_filter<T, VEC, W>(a, live ? d : 0, w, bias);
+  const int64_t items = (int64_t)a.B * a.nseg;
+  for (int64_t item = (int64_t)blockIdx.y * 4 + wave; item < items; item += (int64_t)gridDim.y * 4) {
+    const int b = (int)(item % a.B), s0 = (int)(item / a.B);
+    const int len = __builtin_amdgcn_readfirstlane(length_of(a.lengths, b, a.T));
+    const T *x = (const T *)a.x.p + b * a.x.sb;
+    const T *dy = (const T *)g.dy.p + b * g.dy.sb;
+    T *dx = (T *)g.dx.p + b * g.dx.sb;
+    const int t0 = s0 * a.seg, t1 = min(a.T, t0 + a.seg), stop = t1 + W - 1, end = min(stop, len);
+    float xs[W - 1 + AHEAD_BWD][VEC], q[W - 1 + AHEAD_BWD][VEC];
 #pragma unroll
-      for (int k = 0; k < W - 1; ++k) {
-        const Pack<T, VEC> r = input_row<T, VEC, W>(a, x, b, d, t0 - (W - 1) + k, len);
+    for (int k = 0; k < W - 1; ++k) {
+      const Pack<T, VEC> r = input_row<T, VEC, W>(a, b, at, t0 - (W - 1) + k, len);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) { xs[k][v] = widen(r.v[v]); q[k][v] = 0.f; }
+      for (int v = 0; v < VEC; ++v) { xs[k][v] = widen(r.v[v]); q[k][v] = 0.f; }
+    }
+    Pack<T, VEC> nx[AHEAD_BWD], ny[AHEAD_BWD];
+    const auto fetch = [&](int t) {
+#pragma unroll
+      for (int u = 0; u < AHEAD_BWD; ++u) {
+        nx[u] = load_row<T, VEC>(x + (t + u) * a.x.st, at, t + u < end);
+        ny[u] = load_row<T, VEC>(dy + (t + u) * g.dy.st, at, t + u < end);
       }
-      Pack<T, VEC> nx[AHEAD_BWD], ny[AHEAD_BWD];
-      auto fetch = [&](int t) {
+    };
+    fetch(t0);
+    for (int t = t0; t < stop; t += AHEAD_BWD) {
 #pragma unroll
-        for (int u = 0; u < AHEAD_BWD; ++u) {
+      for (int u = 0; u < AHEAD_BWD; ++u)
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) { nx[u].v[v] = (T)0.f; ny[u].v[v] = (T)0.f; }
-          if (t + u < min(stop, len)) {
-            nx[u] = *(const Pack<T, VEC> *)(x + (int64_t)(t + u) * a.x.st);
-            ny[u] = *(const Pack<T, VEC> *)(dy + (int64_t)(t + u) * g.dy.st);
+        for (int v = 0; v < VEC; ++v) { xs[W - 1 + u][v] = widen(nx[u].v[v]); q[W - 1 + u][v] = widen(ny[u].v[v]); }
+      fetch(t + AHEAD_BWD);
+#pragma unroll
+      for (int u = 0; u < AHEAD_BWD; ++u) {
+        const int now = t + u, j = now - len;               // j: row of d_state that belongs to input row now - (W-1)
+        const bool kept = g.d_state && j >= 0 && j < W - 1;
+        const Pack<T, VEC> ds = load_row<T, VEC>((const T *)g.d_state + ((int64_t)j * a.B + b) * a.D, at, kept);
+        Pack<T, VEC> out;
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          float &qv = q[W - 1 + u][v];
+          if (a.silu) {
+            float r = bias[v];
+#pragma unroll
+            for (int k = 0; k < W; ++k) r = fmaf(w[k][v], xs[u + k][v], r);
+            const float e = sigmoid_fast(r);
+            qv *= e * (1.f + r * (1.f - e));
           }
-        }
-      };
-      fetch(t0);
-      for (int t = t0; t < stop; t += AHEAD_BWD) {
+          qv = now < len ? qv : 0.f;
+          const float own = now < t1 ? qv : 0.f;
+          db[v] += own;
+          float sum = widen(ds.v[v]);
 #pragma unroll
-        for (int u = 0; u < AHEAD_BWD; ++u)
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) { xs[W - 1 + u][v] = widen(nx[u].v[v]); q[W - 1 + u][v] = widen(ny[u].v[v]); }
-        if (t + AHEAD_BWD < stop) fetch(t + AHEAD_BWD);
-#pragma unroll
-        for (int u = 0; u < AHEAD_BWD; ++u) {
-          const int now = t + u;
-          if (now < stop) {
-            Pack<T, VEC> out;
-            const int j = now - len;                        // row of d_state that belongs to input row now - (W-1)
-            const bool kept = g.d_state && j >= 0 && j < W - 1;
-            Pack<T, VEC> ds;
-            if (kept) ds = *(const Pack<T, VEC> *)((const T *)g.d_state + ((size_t)j * a.B + b) * a.D + d);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-              float &qv = q[W - 1 + u][v];
-              if (a.silu) {
-                float s = bias[v];
-#pragma unroll
-                for (int k = 0; k < W; ++k) s = fmaf(w[k][v], xs[u + k][v], s);
-                const float e = sigmoid_fast(s);
-                qv *= e * (1.f + s * (1.f - e));
-              }
-              if (now >= len) qv = 0.f;
-              const float own = now < t1 ? qv : 0.f;
-              db[v] += own;
-              float sum = 0.f;
-#pragma unroll
-              for (int k = 0; k < W; ++k) {
-                dw[k][v] = fmaf(own, xs[u + k][v], dw[k][v]);
-                sum = fmaf(w[k][v], q[W - 1 + u - k][v], sum);
-              }
-              if (kept) sum += widen(ds.v[v]);
-              out.v[v] = narrow<T>(sum);
-            }
-            const int s = now - (W - 1);
-            if (s >= t0) *(Pack<T, VEC> *)(dx + (int64_t)s * g.dx.st) = out;
-            else if (s < 0 && g.dinit) *(Pack<T, VEC> *)((T *)g.dinit + ((size_t)now * a.B + b) * a.D + d) = out;
+          for (int k = 0; k < W; ++k) {
+            dw[k][v] = fmaf(own, xs[u + k][v], dw[k][v]);
+            sum = fmaf(w[k][v], q[W - 1 + u - k][v], sum);
           }
+          out.v[v] = narrow<T>(sum);
         }
-#pragma unroll
-        for (int k = 0; k < W - 1; ++k)
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) { xs[k][v] = xs[k + AHEAD_BWD][v]; q[k][v] = q[k + AHEAD_BWD][v]; }
+        const int r = now - (W - 1);
+        if (r >= 0) store_row<T, VEC>(dx + r * g.dx.st, (r >= t0) & (now < stop) ? at : NOWHERE, out);
+        else store_row<T, VEC>((T *)g.dinit + ((int64_t)now * a.B + b) * a.D, g.dinit != nullptr ? at : NOWHERE, out);
       }
+#pragma unroll
+      for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) { xs[k][v] = xs[k + AHEAD_BWD][v]; q[k][v] = q[k + AHEAD_BWD][v]; }
     }
   }
 #pragma unroll
   for (int k = 0; k <= W; ++k) {
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) part[threadIdx.x * VEC + v] = k < W ? dw[k < W ? k : 0][v] : db[v];
+    for (int v = 0; v < VEC; ++v) part[wave][lane * VEC + v] = k < W ? dw[k < W ? k : 0][v] : db[v];
     __syncthreads();
-    if (row == 0 && live)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        float s = 0.f;
-        for (int r = 0; r < rows; ++r) s += part[(r * lx + lane) * VEC + v];
-        g.partial[((size_t)blockIdx.y * (W + 1) + k) * a.D + d + v] = s;
-      }
+    for (int c = threadIdx.x; c < 64 * VEC; c += 256) {
+      const int col = blockIdx.x * 64 * VEC + c;
+      if (col < a.D) g.partial[((size_t)blockIdx.y * (W + 1) + k) * a.D + col] = ((part[0][c] + part[1][c]) + part[2][c]) + part[3][c];
+    }
     __syncthreads();
   }
 }
@@ -295,7 +278,7 @@ __global__ __launch_bounds__(256) void conv_sum_kernel(const float *__restrict__
 int conv_check(const snn_conv_args *a, bool step, bool grads) {
   if (!a) return ops_fail(SNN_ERR_NULL, "convolution: arguments are NULL");
   if (a->T < 0 || a->B <= 0 || a->D <= 0) return ops_fail(SNN_ERR_ARG, "convolution: T >= 0, B > 0 and D > 0 are required");
-  if ((int64_t)a->B * a->D >= (1ll << 31)) return ops_fail(SNN_ERR_ARG, "convolution: B * D must stay below 2^31");
+  if ((int64_t)a->B * a->D >= (1ll << 31) || a->D > (1 << 28)) return ops_fail(SNN_ERR_ARG, "convolution: B * D must stay below 2^31, D must not exceed 2^28");
   if (a->T > (1 << 30)) return ops_fail(SNN_ERR_ARG, "convolution: T must not exceed 2^30");
   if (a->W < 1 || a->W > SNN_CONV_MAX_TAPS) return ops_fail(SNN_ERR_ARG, "convolution: W must be 1 to %d", SNN_CONV_MAX_TAPS);
   if (a->type != SNN_TYPE_FP32 && a->type != SNN_TYPE_BF16) return ops_fail(SNN_ERR_ARG, "convolution: unknown type %d", a->type);
@@ -324,24 +307,24 @@ bool conv_vector(const snn_conv_args &a, int vec, const snn_conv_grads *g, bool 
          (g ? rows_allow(g->dy, T, a.B, vec, bytes) && rows_allow(g->dx, T, a.B, vec, bytes) && aligned(g->d_state, bytes) && aligned(g->dinit, bytes)
             : rows_allow(a.y, T, a.B, vec, bytes) && aligned(a.state, bytes));
 }
+// Four channels a lane where a row has more than one wavefront of single ones (a wavefront that is half empty with four
+// is full with one).
+int conv_width(const snn_conv_args &a, const snn_conv_grads *g) { return a.D > 64 && conv_vector(a, 4, g, false) ? 4 : 1; }
 
-// How a backward call is cut: channel groups per workgroup, steps per segment, workgroups over the items.
+// How a call is cut: channel groups, steps per segment, and for the reverse pass workgroups over the items.  Segments of
+// 32 steps, of 16 where that leaves fewer than 4096 wavefronts (W - 1 rows of each are read twice).  us of a call, 16 and
+// 32 steps: forward, 2048 wavefronts (1024 steps of 8 x 2048 channels, bf16) 15.8 and 16.7, 16384 wavefronts 113 and
+// 108; forward and reverse, 2048 wavefronts 51.2 and 53.2, 4096 wavefronts 87.8 and 79.9; 64 steps are slower by more.
 struct ConvCut {
-  int lx_log2, seg, nseg, gx, gy;
+  int groups, seg, nseg, gy;
 };
 ConvCut conv_cut(const snn_conv_args &a, int vec) {
   ConvCut c;
-  const int dv = a.D / vec;
-  c.lx_log2 = 0;
-  while (c.lx_log2 < 6 && (1 << c.lx_log2) < dv) ++c.lx_log2;
-  c.gx = (dv + (1 << c.lx_log2) - 1) >> c.lx_log2;
-  c.seg = BSEG;
-  while (c.seg < (1 << 20) && a.T / c.seg > 65536) c.seg *= 2;
+  c.groups = (a.D + 64 * vec - 1) / (64 * vec);
+  c.seg = (int64_t)c.groups * a.B * (a.T / 32) < 4096 ? 16 : 32;
   c.nseg = a.T > c.seg ? (a.T + c.seg - 1) / c.seg : 1;
-  const int64_t rows = 256 >> c.lx_log2, items = (int64_t)a.B * c.nseg;
-  const int64_t want = BBL / c.gx > 1 ? BBL / c.gx : 1;
-  const int64_t all = (items + rows - 1) / rows;
-  c.gy = (int)(all < want ? all : want);
+  const int64_t all = ((int64_t)a.B * c.nseg + 3) / 4, want = std::max(1, 1024 / c.groups);
+  c.gy = (int)std::min(all, want);
   return c;
 }
 
@@ -360,12 +343,12 @@ template <typename F> int with_taps(int W, F f) {
 
 template <typename T, int VEC> int launch_forward(const snn_conv_args &a, hipStream_t st) {
   ConvP p(a);
-  const int64_t threads = (int64_t)a.B * (a.D / VEC);
-  p.seg = CSEG;
-  while (a.T / p.seg > 32768) p.seg *= 2;              // (a grid has at most 65535 rows)
-  const int gy = a.T > p.seg ? (a.T + p.seg - 1) / p.seg : 1;
+  const ConvCut c = conv_cut(a, VEC);
+  p.seg = c.seg; p.nseg = c.nseg; p.groups = c.groups;
+  const int64_t waves = (int64_t)a.B * c.nseg * c.groups;
+  if (waves >= (1ll << 26)) return ops_fail(SNN_ERR_ARG, "convolution: too large for one launch");
   return with_taps(a.W, [&](auto w) {
-    hipLaunchKernelGGL((conv_forward_kernel<T, VEC, w.value>), dim3((unsigned)((threads + 255) / 256), gy), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((conv_forward_kernel<T, VEC, w.value>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, p);
     return ops_launched("convolution");
   });
 }
@@ -379,11 +362,11 @@ template <typename T, int VEC> int launch_step(const snn_conv_args &a, hipStream
 }
 template <typename T, int VEC> int launch_backward(const snn_conv_args &a, const snn_conv_grads &g, float *ws, hipStream_t st) {
   ConvP p(a);
-  ConvGradP q(g);
+  const ConvGradP q(g, ws);
   const ConvCut c = conv_cut(a, VEC);
-  p.seg = c.seg; p.nseg = c.nseg; q.partial = ws; q.lx_log2 = c.lx_log2;
+  p.seg = c.seg; p.nseg = c.nseg; p.groups = c.groups;
   return with_taps(a.W, [&](auto w) {
-    hipLaunchKernelGGL((conv_backward_kernel<T, VEC, w.value>), dim3(c.gx, c.gy), dim3(256), 0, st, p, q);
+    hipLaunchKernelGGL((conv_backward_kernel<T, VEC, w.value>), dim3(c.groups, c.gy), dim3(256), 0, st, p, q);
     int rc = ops_launched("convolution backward");
     if (rc) return rc;
     const int64_t cols = (int64_t)(a.W + 1) * a.D;
@@ -403,16 +386,17 @@ int32_t snn_conv_forward(const snn_conv_args *a, void *stream) {
   int rc = conv_check(a, false, false);
   if (rc) return rc;
   const hipStream_t st = (hipStream_t)stream;
-  if (a->type == SNN_TYPE_FP32) return conv_vector(*a, 4, nullptr, false) ? launch_forward<float, 4>(*a, st) : launch_forward<float, 1>(*a, st);
-  return conv_vector(*a, CV, nullptr, false) ? launch_forward<__bf16, CV>(*a, st) : launch_forward<__bf16, 1>(*a, st);
+  const bool four = conv_width(*a, nullptr) == 4;
+  if (a->type == SNN_TYPE_FP32) return four ? launch_forward<float, 4>(*a, st) : launch_forward<float, 1>(*a, st);
+  return four ? launch_forward<__bf16, 4>(*a, st) : launch_forward<__bf16, 1>(*a, st);
 }
 
 int32_t snn_conv_workspace_bytes(const snn_conv_args *a, size_t *bytes) {
   if (!bytes) return ops_fail(SNN_ERR_NULL, "bytes is NULL");
   if (!a) return ops_fail(SNN_ERR_NULL, "convolution: arguments are NULL");
-  if (a->T < 0 || a->B <= 0 || a->D <= 0 || (int64_t)a->B * a->D >= (1ll << 31) || a->T > (1 << 30) || a->W < 1 || a->W > SNN_CONV_MAX_TAPS)
+  if (a->T < 0 || a->B <= 0 || a->D <= 0 || (int64_t)a->B * a->D >= (1ll << 31) || a->D > (1 << 28) || a->T > (1 << 30) || a->W < 1 || a->W > SNN_CONV_MAX_TAPS)
     return ops_fail(SNN_ERR_ARG, "convolution: sizes out of range");
-  const int gy1 = conv_cut(*a, 1).gy, gy4 = a->D % 4 == 0 ? conv_cut(*a, 4).gy : 0;   // (which one runs depends on the pointers too)
+  const int gy1 = conv_cut(*a, 1).gy, gy4 = conv_cut(*a, 4).gy;   // (which one runs depends on the pointers too)
   *bytes = rup256((size_t)(gy1 > gy4 ? gy1 : gy4) * (a->W + 1) * a->D * 4);
   return SNN_OK;
 }
@@ -430,7 +414,7 @@ int32_t snn_conv_backward(const snn_conv_args *a, const snn_conv_grads *g, void 
     return ops_fail(SNN_ERR_ARG, "convolution backward: a pointer is not aligned to its element type");
   const hipStream_t st = (hipStream_t)stream;
   float *ws = (float *)workspace;
-  const bool vec = conv_vector(*a, 4, g, false);
+  const bool vec = conv_width(*a, g) == 4;
   if (a->type == SNN_TYPE_FP32) return vec ? launch_backward<float, 4>(*a, *g, ws, st) : launch_backward<float, 1>(*a, *g, ws, st);
   return vec ? launch_backward<__bf16, 4>(*a, *g, ws, st) : launch_backward<__bf16, 1>(*a, *g, ws, st);
 }

@@ -13,6 +13,7 @@ wraps the pair in a torch.autograd.Function.)
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import struct
 from typing import NamedTuple, Optional, Sequence
 
@@ -23,8 +24,8 @@ from .binding import SnnError
 
 BLOCK = 128                       # SNN_ADAMW_BLOCK
 MAX_TAPS, MAX_STATES = 8, 64
-TILE = 16                         # steps between saved states
 ERR_ARG, ERR_SHAPE = 2, 3
+_DTYPE = operator.attrgetter("dtype")
 
 
 class _Rows(C.Structure):
@@ -101,7 +102,9 @@ _CONV = struct.Struct("6i" + "3q" * 2 + "5q")
 _CONV_GRADS = struct.Struct("3q" * 2 + "4q")
 _SCAN = struct.Struct("7i4x" + "3q" * 6 + "6q")
 _SCAN_GRADS = struct.Struct("3qq" + "3q" * 5 + "4q")
-assert [s.size for s in (_CONV, _CONV_GRADS, _SCAN, _SCAN_GRADS)] == [C.sizeof(c) for c in (_ConvArgs, _ConvGrads, _ScanArgs, _ScanGrads)]
+_ADAM = struct.Struct("2i4qqI4x5d")
+assert [s.size for s in (_CONV, _CONV_GRADS, _SCAN, _SCAN_GRADS, _ADAM)] == \
+    [C.sizeof(c) for c in (_ConvArgs, _ConvGrads, _ScanArgs, _ScanGrads, _AdamArgs)]
 
 
 def _lib():
@@ -238,7 +241,7 @@ def causal_conv(x, weight, bias=None, init=None, lengths=None, silu: bool = True
     it); lengths [B] int32: steps beyond a sequence's length give zeros and are not looked at.  Returns y and the last
     W-1 inputs of every sequence, which `causal_conv_step` or the next call's `init` goes on from."""
     dev, W, pack = _conv_args(x, weight, bias, init, lengths, silu)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
     state = torch.empty((W - 1, *x.shape[1:]), dtype=x.dtype, device=x.device)
     _call(_declared.snn_conv_forward, dev, pack(y.data_ptr(), state.data_ptr()))
     return ConvOutput(y, state)
@@ -249,7 +252,7 @@ def causal_conv_backward(dy, x, weight, bias=None, init=None, lengths=None, silu
     the forward call had no bias or init."""
     dev, W, pack = _conv_args(x, weight, bias, init, lengths, silu)
     a, (_, B, D) = pack(0, 0), x.shape
-    dx, dweight = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty_like(weight)
+    dx, dweight = torch.empty_like(x, memory_format=torch.contiguous_format), torch.empty_like(weight)
     dbias = torch.empty_like(bias) if bias is not None else None
     dinit = torch.empty_like(init) if init is not None else None
     g = _CONV_GRADS.pack(*_rows(dy, x, dev, x.shape, "dy"), dx.data_ptr(), B * D, D, _dense(d_state, dev, (W - 1, B, D), x.dtype, "d_state"),
@@ -265,7 +268,7 @@ def causal_conv_step(x, state, weight, bias=None, silu: bool = True):
     dev, W, pack = _conv_args(x, weight, bias, None, None, silu, step=True)
     _need(state is not None, "state is needed")
     at = _dense(state, dev, (W - 1, *x.shape), x.dtype, "state")
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
     _call(_declared.snn_conv_step, dev, pack(y.data_ptr(), at))
     return y
 
@@ -304,7 +307,7 @@ def selective_scan(x, dt, A, B, C_, D=None, z=None, dt_bias=None, softplus: bool
     state alone and are not looked at.  `save` keeps the state before every 16th step for selective_scan_backward."""
     dev, (N, _), pack = _scan_args(x, dt, A, B, C_, D, z, dt_bias, softplus, init, lengths)
     lib, saved = _declared, None
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
     state = torch.empty((*x.shape[1:], N), dtype=torch.float32, device=x.device)
     a = pack(y.data_ptr(), state.data_ptr())
     n = _bytes_of(lib.snn_scan_workspace_bytes, a, 0)
@@ -324,8 +327,8 @@ def selective_scan_backward(dy, saved, x, dt, A, B, C_, D=None, z=None, dt_bias=
     _need(saved is not None, "saved is needed: call selective_scan with save=True")
     saved_at = _dense(saved, dev, (_bytes_of(lib.snn_scan_saved_bytes, a) // 4,), torch.float32, "saved")
 
-    def like(t, dtype=None):
-        return torch.empty(t.shape, dtype=dtype or t.dtype, device=x.device) if t is not None else None
+    def like(t):
+        return torch.empty_like(t, memory_format=torch.contiguous_format) if t is not None else None
 
     def at(t):
         return t.data_ptr() if t is not None else 0
@@ -346,7 +349,7 @@ def selective_scan_step(x, dt, state, A, B, C_, D=None, z=None, dt_bias=None, so
     dev, (N, _), pack = _scan_args(x, dt, A, B, C_, D, z, dt_bias, softplus, None, None, step=True)
     _need(state is not None, "state is needed")
     at = _dense(state, dev, (*x.shape, N), torch.float32, "state")
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
     _call(_declared.snn_scan_step, dev, pack(y.data_ptr(), at))
     return y
 
@@ -376,7 +379,7 @@ class AdamW:
             _need(p.dtype == torch.float32 and p.device == dev and p.is_contiguous(), "parameters have to be dense, float32, on one device")
             _need(c is None or (c.dtype == torch.bfloat16 and c.device == dev and c.is_contiguous() and c.shape == p.shape),
                   "copies have to be dense, bfloat16, of their parameters' shapes")
-        self.lr, self.betas, self.eps, self.bits, self.seed, self.steps = float(lr), betas, float(eps), state_bits, int(seed), 0
+        self.lr, self.betas, self.eps, self.bits, self.seed, self.steps = float(lr), (float(betas[0]), float(betas[1])), float(eps), state_bits, int(seed), 0
         self.at, n = [], 0
         for p in self.params:
             self.at.append(n)
@@ -387,7 +390,7 @@ class AdamW:
         self.m_scale = self.v_scale = None
         if state_bits == 8:
             self.m_scale, self.v_scale = (torch.ones(n // BLOCK, device=dev) for _ in range(2))
-        self._shapes = [p.shape for p in self.params]
+        self._sizes, self._strides = [p.numel() for p in self.params], [p.stride() for p in self.params]
         self._copied = [i for i, c in enumerate(self.copies) if c is not None]
         # snn_adamw_tensor, one a row; addresses are filled in by every step
         self._table = np.zeros((len(self.params), 6), np.int64)
@@ -396,23 +399,23 @@ class AdamW:
 
     def step(self, grads: Sequence, lr: Optional[float] = None, grad_scale: float = 1.0) -> None:
         """One step with these gradients (dense, all float32 or all bfloat16, multiplied by `grad_scale` first)."""
-        if [g.shape for g in grads] != self._shapes or [p.shape for p in self.params] != self._shapes:
-            _refuse("a gradient of its shape is needed for every parameter", ERR_SHAPE)
-        kind, dev = grads[0].dtype, self.m.get_device()
-        _need(kind in _types, f"gradients are float32 or bfloat16, not {kind}")
-        if any(g.dtype is not kind or g.get_device() != dev or not g.is_contiguous() for g in grads):
-            _refuse("gradients have to be dense and alike, on the parameters' device")
-        if any(p.dtype is not torch.float32 or p.get_device() != dev or not p.is_contiguous() for p in self.params):
+        # (checks run over all tensors at C speed: with many small tensors they are what a step costs)
+        tensor, params, dev = torch.Tensor, self.params, self.m.get_device()
+        if list(map(tensor.numel, grads)) != self._sizes or list(map(tensor.stride, grads)) != self._strides:   # (so they are dense too)
+            _refuse("a dense gradient of its shape is needed for every parameter", ERR_SHAPE)
+        kind = set(map(_DTYPE, grads))
+        if len(kind) != 1 or not kind <= _types.keys() or set(map(tensor.get_device, grads)) != {dev}:
+            _refuse("gradients have to be all float32 or all bfloat16, on the parameters' device")
+        if list(map(tensor.numel, params)) != self._sizes or set(map(_DTYPE, params)) != {torch.float32} or set(map(tensor.get_device, params)) != {dev} or not all(map(tensor.is_contiguous, params)):
             _refuse("a parameter is not what it was when the optimiser was made")
         t = self._table
-        t[:, 0], t[:, 1] = [p.data_ptr() for p in self.params], [g.data_ptr() for g in grads]
+        t[:, 0], t[:, 1] = list(map(tensor.data_ptr, params)), list(map(tensor.data_ptr, grads))
         for i in self._copied:
             t[i, 2] = self.copies[i].data_ptr()
-        small = self.bits == 8
-        a = _AdamArgs(self.bits, _types[kind], self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr() if small else None,
-                      self.v_scale.data_ptr() if small else None, self.steps + 1, self.seed & 0xFFFFFFFF,
-                      self.lr if lr is None else float(lr), self.betas[0], self.betas[1], self.eps, float(grad_scale))
-        _call(_declared.snn_adamw_step, dev, C.byref(a), t.ctypes.data, len(t))
+        scales = (self.m_scale.data_ptr(), self.v_scale.data_ptr()) if self.bits == 8 else (0, 0)
+        a = _ADAM.pack(self.bits, _types[kind.pop()], self.m.data_ptr(), self.v.data_ptr(), *scales, self.steps + 1, self.seed & 0xFFFFFFFF,
+                       self.lr if lr is None else float(lr), *self.betas, self.eps, float(grad_scale))
+        _call(_declared.snn_adamw_step, dev, a, t.ctypes.data, len(t))
         self.steps += 1
 
     def state_dict(self) -> dict:

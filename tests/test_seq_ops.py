@@ -81,6 +81,8 @@ CONV = [  # T, B, D, W, type, init, lengths, silu, bias
     (130, 2, 1032, 4, "bf16", False, "some", True, True),
     (200, 1, 12, 7, "fp32", True, "none", True, True),
     (0, 2, 8, 4, "fp32", True, "none", True, True),
+    (18, 4500, 5, 4, "fp32", True, "some", True, True),          # more items than workgroups
+    (300, 40, 260, 4, "bf16", False, "some", True, True),
 ]
 
 
@@ -385,3 +387,60 @@ def test_operators_run_on_the_current_stream_and_in_graphs():
         opt.step([got[2]])
         for a, e in zip(got, work()):
             assert torch.equal(a, e), k
+
+
+def test_outputs_are_dense_whatever_the_inputs_are():
+    """An input in batch-major memory, or one that repeats a row, does not decide how outputs lie."""
+    from paper_2402_18994_amd import causal_conv, selective_scan, selective_scan_backward
+    x = torch.randn(3, 20, 24, device="cuda").transpose(0, 1)
+    same = torch.randn(1, 1, 24, device="cuda").expand(20, 3, 24)
+    A, B = -torch.rand(24, 5, device="cuda"), torch.randn(3, 20, 5, device="cuda").transpose(0, 1)
+    w = torch.randn(24, 4, device="cuda")
+    for t in (x, same):
+        y, _ = causal_conv(t, w)
+        assert y.is_contiguous() and torch.equal(y, causal_conv(t.contiguous(), w).y)
+        out = selective_scan(t, x, A, B, B, save=True)
+        flat = selective_scan(t.contiguous(), x.contiguous(), A, B.contiguous(), B.contiguous(), save=True)
+        assert out.y.is_contiguous() and torch.equal(out.y, flat.y) and torch.equal(out.state, flat.state)
+        g = selective_scan_backward(t, out.saved, t, x, A, B, B)
+        f = selective_scan_backward(t.contiguous(), flat.saved, t.contiguous(), x.contiguous(), A, B.contiguous(), B.contiguous())
+        for a, b in zip(g, f):
+            assert a is None or (a.is_contiguous() and torch.equal(a, b))
+
+
+def test_tensors_used_on_another_stream():
+    """Calls on a side stream write and free their memory in that stream's order."""
+    from paper_2402_18994_amd import selective_scan
+    _, t, s, _ = scan_case(513, 1, 6, 64, 2, "fp32", True, True, "none", True)
+    d, _ = scan_gpu(s, t, None)
+    want = call(selective_scan, d)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = [call(selective_scan, d) for _ in range(8)]
+    side.synchronize()
+    for g in got:
+        assert torch.equal(g.y, want.y) and torch.equal(g.state, want.state)
+
+
+def test_refusals_name_what_is_wrong():
+    from paper_2402_18994_amd import AdamW, SnnError, causal_conv, causal_conv_step, selective_scan, selective_scan_backward, selective_scan_step
+    x, w = torch.zeros(4, 2, 8, device="cuda"), torch.zeros(8, 4, device="cuda")
+    A, B = torch.zeros(8, 16, device="cuda"), torch.zeros(4, 2, 16, device="cuda")
+    good = selective_scan(x, x, A, B, B, save=True)
+    bad = [lambda: causal_conv(x[0], w), lambda: causal_conv(x, w[:4]), lambda: causal_conv(x, w.double()), lambda: causal_conv(x, torch.zeros(8, 9, device="cuda")),
+           lambda: causal_conv(x, w, init=torch.zeros(2, 2, 8, device="cuda")), lambda: causal_conv(x, w, lengths=torch.zeros(2, device="cuda")),
+           lambda: causal_conv(x.transpose(1, 2), w[:2]), lambda: causal_conv(x, w.cpu()), lambda: causal_conv(x.half(), w),
+           lambda: causal_conv_step(x[0], None, w), lambda: causal_conv_step(x[0], torch.zeros(3, 8, 2, device="cuda").transpose(1, 2), w),
+           lambda: selective_scan(x, x[:3], A, B, B), lambda: selective_scan(x, x, A, B, B[..., :8]), lambda: selective_scan(x, x.bfloat16(), A, B, B),
+           lambda: selective_scan(x, x, A, B[:, :, None].expand(4, 2, 3, 16), B[:, :, None].expand(4, 2, 3, 16)), lambda: selective_scan(x, x, A[:, :0], B[..., :0], B[..., :0]),
+           lambda: selective_scan(x, x, A, B[..., ::2].repeat(1, 1, 2)[..., ::2], B), lambda: selective_scan(x, x, A.t().contiguous().t(), B, B),
+           lambda: selective_scan_backward(x, None, x, x, A, B, B), lambda: selective_scan_backward(x, good.saved[:-1], x, x, A, B, B),
+           lambda: selective_scan_step(x[0], x[0], None, A, B[0], B[0]), lambda: selective_scan_step(x[0], x[0], torch.zeros(2, 8, 8, device="cuda"), A, B[0], B[0]),
+           lambda: AdamW([w.bfloat16()]), lambda: AdamW([w], state_bits=16), lambda: AdamW([w], weight_decay=[0.1, 0.1]),
+           lambda: AdamW([w]).step([x]), lambda: AdamW([w]).step([w.t().contiguous().t()]), lambda: AdamW([w]).step([]), lambda: AdamW([w]).step([w.half()]),
+           lambda: AdamW([w]).load_state_dict({"step": 0, "m": w, "v": w})]
+    for i, f in enumerate(bad):
+        with pytest.raises(SnnError) as e:
+            f()
+        assert e.value.status in (2, 3) and len(str(e.value)) > 20, i
