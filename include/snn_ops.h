@@ -153,6 +153,15 @@ typedef struct {
 /* `tensors`: host array; read before the call returns.  A tensor with n = 0 is passed over. */
 int32_t snn_adamw_step(const snn_adamw_args *a, const snn_adamw_tensor *tensors, int32_t count, void *hip_stream);
 
+/* The same for a network of snn.h, in the place of snn_sgd_step: every W and R, and the decays where they are trained
+ * (these without weight decay, and kept in [0, 1] as snn_sgd_step keeps them), then the refresh of the operand copies.
+ * `a` as above, with grad_type SNN_TYPE_FP32 and moment buffers of snn_adamw_network_elements elements (a multiple of
+ * SNN_ADAMW_BLOCK; layer by layer W, R, decays), zeroed before the first step.  Needs a preceding snn_backward (else
+ * SNN_ERR_STATE).  Currents and spike gradients that the pass's launches kept to themselves cannot be read after it
+ * (snn_get_tensor gives SNN_ERR_STATE): they would have to be formed again on weights that are gone. */
+int32_t snn_adamw_network_elements(const snn_ctx *ctx, int64_t *elements);
+int32_t snn_adamw_network_step(snn_ctx *ctx, const snn_adamw_args *a, double weight_decay);
+
 #ifdef __cplusplus
 }
 #endif

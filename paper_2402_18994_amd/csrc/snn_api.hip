@@ -2,6 +2,7 @@
 // the forward and reverse passes, and the launches.  Host code only enqueues kernels; every
 // step of the path runs on the GPU.
 #include "../../include/snn.h"
+#include "../../include/snn_ops.h"
 
 #include <hip/hip_runtime.h>
 
@@ -71,6 +72,7 @@ struct Layer {
   bool i_ready = true;     // I is in memory (false: the last forward pass ran the layer in one launch and never stored it)
   bool ds_ready = true;    // dS is in memory (false: the layer's reverse scan formed it itself in the last backward pass)
   bool moved = false;      // the weights are one snn_sgd_step past those of the last pass
+  bool gone = false;       // the weights of the last pass cannot be had again (snn_adamw_network_step)
   int splits_w = 1, splits_r = 1;                     // contraction splits of dW and dR
   long long per_w = 0, per_r = 0;                     // rows per split
   float *part_w = nullptr, *part_r = nullptr;         // per-split partial results
@@ -1262,6 +1264,7 @@ int update_layers(snn_ctx *c, int l0, int l1, bool with_grad, float lr, bool sto
 int form_again(snn_ctx *c, int l, int (*product)(snn_ctx *, int)) {
   const bool moved = c->layers[l].moved;
   int rc, back = SNN_OK;
+  if (c->layers[l].gone) return fail(c, SNN_ERR_STATE, "the pass's launches kept this tensor to themselves, and snn_adamw_network_step has replaced the weights it was formed with");
   if (moved && (rc = update_layers(c, l, l + 1, true, -c->last_lr, false))) return rc;
   rc = product(c, l);
   if (moved) back = update_layers(c, l, l + 1, false, 0.f);
@@ -1611,7 +1614,7 @@ static int32_t forward_layers(snn_ctx *c, const int32_t *labels_dev, float *loss
 
 static int32_t forward_launches(snn_ctx *c, const int32_t *labels_dev) {
   int rc;
-  for (Layer &y : c->layers) y.moved = false;
+  for (Layer &y : c->layers) y.moved = y.gone = false;
   const int whole = layer_fuse_mode(c);                 // layers that run as one launch, product and scan
   const bool whole_top = whole >= 2 && layer_forward_fusable(c, c->L - 2);
   const int with_readout = whole_top ? layer_forward_takes_readout(c) : 0;
@@ -1758,6 +1761,54 @@ int32_t snn_sgd_step(snn_ctx *c, float lr) {
   return SNN_OK;
 }
 
+int32_t snn_adamw_network_elements(const snn_ctx *c, int64_t *elements) {
+  if (!c || !elements) return fail(nullptr, SNN_ERR_NULL, "context or elements is NULL");
+  const auto blocks = [](int64_t n) { return (n + SNN_ADAMW_BLOCK - 1) / SNN_ADAMW_BLOCK * SNN_ADAMW_BLOCK; };
+  int64_t n = 0;
+  for (const Layer &y : c->layers)
+    n += blocks((int64_t)y.K * y.N) + (y.recurrent ? blocks((int64_t)y.N * y.N) : 0) + (c->learn_beta ? blocks(y.N) : 0);
+  *elements = n;
+  return SNN_OK;
+}
+
+int32_t snn_adamw_network_step(snn_ctx *c, const snn_adamw_args *a, double weight_decay) {
+  if (!c) return fail(nullptr, SNN_ERR_NULL, "context is NULL");
+  if (!a) return fail(c, SNN_ERR_NULL, "arguments are NULL");
+  if (a->grad_type != SNN_TYPE_FP32) return fail(c, SNN_ERR_ARG, "the gradients of a network are fp32");
+  if (c->state < 2) return fail(c, SNN_ERR_STATE, "snn_adamw_network_step needs a preceding snn_backward");
+  int rc = flush_reduce(c);
+  if (rc) return rc;
+  snn_adamw_tensor t[3 * SNN_MAX_LAYERS];
+  int n = 0;
+  int64_t at = 0;
+  const auto add = [&](float *p, const float *g, int64_t size, double decay) {
+    t[n++] = {p, g, nullptr, size, at, decay};
+    at += (size + SNN_ADAMW_BLOCK - 1) / SNN_ADAMW_BLOCK * SNN_ADAMW_BLOCK;
+  };
+  for (Layer &y : c->layers) {
+    add(y.Wm, y.dW, (int64_t)y.K * y.N, weight_decay);
+    if (y.recurrent) add(y.Rm, y.dR, (int64_t)y.N * y.N, weight_decay);
+    if (c->learn_beta) add(y.beta_v, y.dbeta, y.N, 0.0);
+  }
+  Bracket br(c, SNN_K_SGD, 0);
+  if ((rc = snn_adamw_step(a, t, n, c->stream))) return fail(c, rc, "%s", g_err.c_str());
+  if (c->learn_beta) {
+    BetaJobs bj;
+    memset(&bj, 0, sizeof bj);
+    for (Layer &y : c->layers) {
+      const int j = bj.njobs++;
+      bj.beta[j] = y.beta_v; bj.dbeta[j] = y.dbeta;
+      bj.first[j + 1] = bj.first[j] + y.N;
+    }
+    hipLaunchKernelGGL(beta_update_kernel, dim3((bj.first[bj.njobs] + 255) / 256), dim3(256), 0, c->stream, bj, 0.f);   // the clipping alone
+    HIPCHK(c, hipGetLastError());
+  }
+  if ((rc = update_layers(c, 0, c->L, false, 0.f))) return rc;
+  for (Layer &y : c->layers) { y.moved = false; y.gone = true; }
+  c->state = 0;
+  return SNN_OK;
+}
+
 int32_t snn_get_tensor(snn_ctx *c, int32_t tensor, int32_t layer, void *dst, size_t bytes) {
   if (!c) return fail(nullptr, SNN_ERR_NULL, "context is NULL");
   if (!dst) return fail(c, SNN_ERR_NULL, "dst_host is NULL");
@@ -1807,7 +1858,7 @@ int32_t snn_set_tensor(snn_ctx *c, int32_t tensor, int32_t layer, const void *sr
   if (tensor == SNN_T_CURRENT) c->layers[layer - 1].i_ready = true;     // what the caller imposed is what a reader gets
   if (tensor == SNN_T_D_SPIKES) c->layers[layer - 1].ds_ready = true;
   if (tensor == SNN_T_BETA) c->state = 0;                               // a forward pass on other decays is stale
-  if (tensor == SNN_T_WEIGHT) c->layers[layer - 1].moved = false;
+  if (tensor == SNN_T_WEIGHT) c->layers[layer - 1].moved = c->layers[layer - 1].gone = false;
   if (tensor == SNN_T_WEIGHT || tensor == SNN_T_RWEIGHT) {
     if ((rc = update_layers(c, layer - 1, layer, false, 0.f))) return rc;
     HIPCHK(c, hipStreamSynchronize(c->stream));

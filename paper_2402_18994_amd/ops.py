@@ -118,7 +118,8 @@ def _lib():
         for name, args in (("conv_forward", [vp, vp]), ("conv_workspace_bytes", [vp, vp]), ("conv_backward", [vp, vp, vp, sz, vp]),
                            ("conv_step", [vp, vp]), ("scan_workspace_bytes", [vp, C.c_int32, vp]), ("scan_saved_bytes", [vp, vp]),
                            ("scan_forward", [vp, vp, vp, sz, vp]), ("scan_backward", [vp, vp, vp, vp, sz, vp]), ("scan_step", [vp, vp]),
-                           ("adamw_step", [vp, vp, C.c_int32, vp])):
+                           ("adamw_step", [vp, vp, C.c_int32, vp]), ("adamw_network_elements", [vp, vp]),
+                           ("adamw_network_step", [vp, vp, C.c_double])):
             f = getattr(lib, "snn_" + name)
             f.argtypes, f.restype = args, C.c_int32
         _types = {torch.float32: 0, torch.bfloat16: 1}
@@ -432,3 +433,30 @@ class AdamW:
         for k in names:
             getattr(self, k).copy_(d[k])
         self.steps = int(d["step"])
+
+
+class NetworkAdamW:
+    """AdamW for an SNN (binding.py), in the place of its sgd_step: `step` after every `backward` (snn_adamw_network_step).
+    Arguments as for AdamW; trained decays take part without weight decay."""
+
+    def __init__(self, snn, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, state_bits: int = 32, seed: int = 0):
+        lib = _lib()
+        _need(state_bits in (32, 8), "state_bits has to be 32 or 8")
+        self.snn, self.lr, self.betas, self.eps, self.weight_decay = snn, float(lr), (float(betas[0]), float(betas[1])), float(eps), float(weight_decay)
+        self.bits, self.seed, self.steps = state_bits, int(seed), 0
+        n = C.c_int64(0)
+        _check(lib.snn_adamw_network_elements(snn.ctx, C.byref(n)))
+        # (made in the network's stream, which the steps run on)
+        with torch.cuda.stream(snn.stream):
+            kind = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+            self.m, self.v = (torch.zeros(n.value, dtype=torch.uint8 if state_bits == 8 else kind, device=snn.device).view(kind) for _ in range(2))
+            self.m_scale, self.v_scale = (torch.ones(n.value // BLOCK, device=snn.device) for _ in range(2)) if state_bits == 8 else (None, None)
+
+    def step(self, lr: Optional[float] = None) -> None:
+        scales = (self.m_scale.data_ptr(), self.v_scale.data_ptr()) if self.bits == 8 else (0, 0)
+        a = _ADAM.pack(self.bits, 0, self.m.data_ptr(), self.v.data_ptr(), *scales, self.steps + 1, self.seed & 0xFFFFFFFF,
+                       self.lr if lr is None else float(lr), *self.betas, self.eps, 1.0)
+        rc = _declared.snn_adamw_network_step(self.snn.ctx, a, self.weight_decay)
+        if rc:
+            raise SnnError(rc, _declared.snn_last_error(self.snn.ctx).decode())
+        self.steps += 1

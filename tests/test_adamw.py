@@ -210,3 +210,74 @@ def test_unaligned_tensors_and_saved_state():
         for o in (oc, od):
             o.step([gstore[i:i + n] for i, n in cut])
         assert all(torch.equal(x, y) for x, y in zip(a, c))
+
+
+# ---------------------------------------------------------------------------------------- networks of spiking layers
+
+@pytest.mark.parametrize("kind", ("plain", "recurrent", "decays", "wide"))
+def test_network_steps(kind):
+    """A network's parameters after a step are AdamW's of its own gradients; the next pass runs on them."""
+    from paper_2402_18994_amd import SNN, NetworkAdamW, SnnError
+    rng = np.random.default_rng(5)
+    T, B, sizes, rec = 24, 6, (40, 36, 30, 5), (False, kind == "recurrent")
+    if kind == "wide":
+        sizes, rec = (100, 256, 256, 20), (False, False)
+    W = [(3 * rng.standard_normal((a, b)) / math.sqrt(a)).astype(np.float32) for a, b in zip(sizes, sizes[1:])]
+    R = [None if not r else (0.3 * rng.standard_normal((n, n)) / math.sqrt(n)).astype(np.float32) for n, r in zip(sizes[1:], rec)]
+    snn = SNN(T, B, sizes, rec, (0.9, 0.85, 0.95), 1.0, "superspike", 25.0, "bf16", W, R, learn_beta=kind == "decays")
+    opt = NetworkAdamW(snn, lr=0.01, weight_decay=0.05)
+    x, labels = (rng.random((T, B, sizes[0])) < 0.2).astype(np.uint8), rng.integers(0, sizes[-1], B).astype(np.int32)
+    names = [("weight", "grad_w", l) for l in (1, 2, 3)] + ([("rweight", "grad_r", 2)] if rec[1] else [])
+    names += [("beta", "grad_beta", l) for l in (1, 2, 3)] if kind == "decays" else []
+    read = lambda which: {(n[0], n[2]): torch.from_numpy(snn.get_tensor(n[which], n[2])).double() for n in names}
+    state = {k: (p, torch.zeros_like(p), torch.zeros_like(p)) for k, p in read(0).items()}
+    with pytest.raises(SnnError):
+        opt.step()                                        # no gradients yet
+    for step in range(1, 4):
+        loss = snn.forward(x, labels)
+        snn.backward()
+        grads = read(1) if step != 2 else None            # the second step adds up the partial sums itself
+        opt.step()
+        grads = grads or read(1)
+        assert any((g != 0).any() for g in grads.values())
+        for k, (p, m, v) in state.items():
+            w, m, v = oracle.adamw(p, grads[k], m, v, step, 0.01, BETAS, EPS, 0.0 if k[0] == "beta" else 0.05)
+            state[k] = (w.clamp(0, 1) if k[0] == "beta" else w, m, v)
+            got = torch.from_numpy(snn.get_tensor(*k))
+            near(str(k), got, state[k][0], step, 0.01)
+            state[k] = (got.double(), m, v)
+        if kind == "wide" and step == 1:                  # kept to themselves by the pass's launches, and the weights are gone
+            with pytest.raises(SnnError) as e:
+                snn.get_tensor("current", 1)
+            assert e.value.status == 5
+    # the products see the new weights: a network made of them computes the same
+    fresh = SNN(T, B, sizes, rec, (0.9, 0.85, 0.95), 1.0, "superspike", 25.0, "bf16", [snn.get_tensor("weight", l) for l in (1, 2, 3)],
+                [snn.get_tensor("rweight", l) if r else None for l, r in zip((1, 2), rec)], learn_beta=kind == "decays")
+    if kind == "decays":
+        for l in (1, 2, 3):
+            fresh.set_tensor("beta", l, snn.get_tensor("beta", l))
+    assert snn.forward(x, labels) == fresh.forward(x, labels)
+    snn.get_tensor("current", 1)                          # a new pass, whose weights are there
+    snn.destroy()
+    fresh.destroy()
+
+
+def test_network_learns_with_8_bit_moments():
+    from paper_2402_18994_amd import SNN, NetworkAdamW
+    rng = np.random.default_rng(1)
+    T, B, sizes = 32, 32, (64, 64, 64, 4)
+    W = [(2 * rng.standard_normal((a, b)) / math.sqrt(a)).astype(np.float32) for a, b in zip(sizes, sizes[1:])]
+    labels = rng.integers(0, 4, B).astype(np.int32)
+    rates = rng.random((4, sizes[0])) * 0.4
+    x = (rng.random((T, B, sizes[0])) < rates[labels]).astype(np.uint8)
+    first = None
+    for bits in (32, 8):
+        snn = SNN(T, B, sizes, (False, False), (0.9, 0.9, 0.9), 1.0, "superspike", 25.0, "bf16", W)
+        opt = NetworkAdamW(snn, lr=0.01, state_bits=bits, seed=3)
+        for _ in range(40):
+            last = snn.forward(x, labels)
+            first = last if first is None else first
+            snn.backward()
+            opt.step()
+        assert last < 0.5 * first, (bits, first, last)
+        snn.destroy()

@@ -146,6 +146,7 @@ def test_adamw_refusals(lib):
                       (dict(param=P + 2), ARG), (dict(copy=P + 1), ARG), (dict(n=1 << 36), ARG), (dict(weight_decay=float("inf")), ARG)):
         assert call(tensor=t) == status, t
     assert call(count=0) == 0 and call(tensor=dict(n=0)) == 0       # nothing to do
+    assert lib.snn_adamw_network_elements(None, None) == NULL and lib.snn_adamw_network_step(None, None, 0.0) == NULL
 
 
 def test_python_entry_points_refuse_before_a_launch(lib):
