@@ -3,12 +3,14 @@
 //   p <- p (1 - lr wd) - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
 // Bound by memory: 28 bytes a parameter with everything in fp32, 16.1 with 8-bit moments.  The tensors' addresses
 // travel as kernel arguments, up to TENSORS in a launch, so a step needs no table on the device and no copy; a
-// workgroup finds its tensor by bisection over the chunk numbers.  A thread takes four neighbouring elements, ITER
-// times, with all loads of the chunk issued before the first result.
+// workgroup finds its tensor by bisection over the chunk numbers.  A thread takes four neighbouring elements: with more
+// of them a thread, fewer threads hide the loads (four elements, eight, sixteen: 79 million parameters in 32 bits 403,
+// 412 and 421 us, 5.5 TB/s the first; in 8 bits with bfloat16 gradients 230, 241 and 260 us, 4.8 TB/s; 7.6 million in 8
+// bits 28, 30 and 34 us).
 // Every operation is rounded by itself (no contraction), so that the codes of 8-bit moments do not depend on how the
 // compiler joins operations.
 // With 8-bit moments the arithmetic counts as well (the random bits, two roundings, the scales: 38 us for 7.6 million
-// parameters when root and quotient were the correctly rounded ones, about ten operations more each).  There the roots
+// parameters, sixteen a thread, when root and quotient were the correctly rounded ones, ten operations more each; 34 so).  There the roots
 // of single elements and the quotient come from the hardware's approximations, one unit of the last place off: the
 // parameter feels 2^-23 of its update, and a code does not feel it, since a root taken for just below a code or just
 // above goes to that code with a chance next to 1 from either side.  The root that the scale goes by is exact.
@@ -20,6 +22,7 @@ namespace snn {
 namespace {
 
 constexpr int TENSORS = 76;
+constexpr int CHUNK = 1024;          // elements of a workgroup
 
 struct AdamP {
   float *param[TENSORS];
@@ -127,7 +130,7 @@ template <typename T> __device__ __forceinline__ void give4(T *p, const float r[
   }
 }
 
-template <typename G, int BITS, int ITER>
+template <typename G, int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(const AdamP p) {
 #pragma clang fp contract(off)
   int lo = 0, hi = p.count;                                // first[lo] <= block < first[hi]
@@ -141,110 +144,84 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamP p) {
   __bf16 *copy = p.copy[lo];
   const float keep = p.keep[lo];
   const bool vp = ((uintptr_t)param & 15) == 0, vg = ((uintptr_t)grad & (4 * sizeof(G) - 1)) == 0, vc = ((uintptr_t)copy & 7) == 0;
-  const int64_t base = (int64_t)(blockIdx.x - p.first[lo]) * (1024 * ITER) + threadIdx.x * 4;
+  const int64_t i = (int64_t)(blockIdx.x - p.first[lo]) * CHUNK + threadIdx.x * 4;
 
-  float w[ITER][4], g[ITER][4], m[ITER][4], v[ITER][4];
-  uint32_t cm[ITER], cv[ITER];
-  float sm[ITER], sv[ITER];
-#pragma unroll
-  for (int k = 0; k < ITER; ++k) {
-    const int64_t i = base + k * 1024;
+  float w[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f}, m[4], v[4], root[4];
+  if constexpr (BITS == 32) {
+    if (i >= n) return;
+    take4(w, (const float *)param, i, n, vp);
+    take4(g, grad, i, n, vg);
+    take4(m, (const float *)p.m + at, i, n, true);         // (at: a multiple of SNN_ADAMW_BLOCK)
+    take4(v, (const float *)p.v + at, i, n, true);
+  } else {
+    // a lane beyond the tensor has no element of the block and only takes part in its maxima
+    uint32_t cm = 0, cv = 0;
+    float sm = 1.f, sv = 1.f;
     if (i < n) {
-      take4(w[k], (const float *)param, i, n, vp);
-      take4(g[k], grad, i, n, vg);
-      if constexpr (BITS == 32) {
-        take4(m[k], (const float *)p.m + at, i, n, true);  // (at: a multiple of SNN_ADAMW_BLOCK)
-        take4(v[k], (const float *)p.v + at, i, n, true);
-      } else {
-        cm[k] = *(const uint32_t *)((const uint8_t *)p.m + at + i);
-        cv[k] = *(const uint32_t *)((const uint8_t *)p.v + at + i);
-        sm[k] = p.m_scale[(at + i) / SNN_ADAMW_BLOCK];
-        sv[k] = p.v_scale[(at + i) / SNN_ADAMW_BLOCK];
-      }
+      take4(w, (const float *)param, i, n, vp);
+      take4(g, grad, i, n, vg);
+      cm = *(const uint32_t *)((const uint8_t *)p.m + at + i);
+      cv = *(const uint32_t *)((const uint8_t *)p.v + at + i);
+      sm = p.m_scale[(at + i) / SNN_ADAMW_BLOCK];
+      sv = p.v_scale[(at + i) / SNN_ADAMW_BLOCK];
     }
-  }
-#pragma unroll
-  for (int k = 0; k < ITER; ++k) {
-    const int64_t i = base + k * 1024;
-    if constexpr (BITS == 8) {
-      if (i >= n) {                                        // (no element of the block: the lane only takes part in the maxima)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[k][j] = g[k][j] = 0.f;
-        cm[k] = cv[k] = 0;
-        sm[k] = sv[k] = 1.f;
-      }
-      m[k][0] = __builtin_amdgcn_cvt_f32_fp8((int)cm[k], 0); m[k][1] = __builtin_amdgcn_cvt_f32_fp8((int)cm[k], 1);
-      m[k][2] = __builtin_amdgcn_cvt_f32_fp8((int)cm[k], 2); m[k][3] = __builtin_amdgcn_cvt_f32_fp8((int)cm[k], 3);
-      v[k][0] = __builtin_amdgcn_cvt_f32_fp8((int)cv[k], 0); v[k][1] = __builtin_amdgcn_cvt_f32_fp8((int)cv[k], 1);
-      v[k][2] = __builtin_amdgcn_cvt_f32_fp8((int)cv[k], 2); v[k][3] = __builtin_amdgcn_cvt_f32_fp8((int)cv[k], 3);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        m[k][j] *= sm[k];
-        const float r = v[k][j] * sv[k];
-        v[k][j] = r * r;
-      }
-    } else {
-      if (i >= n) continue;
-    }
-    float root[4];
+    m[0] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 0); m[1] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 1);
+    m[2] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 2); m[3] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 3);
+    v[0] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 0); v[1] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 1);
+    v[2] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 2); v[3] = __builtin_amdgcn_cvt_f32_fp8((int)cv, 3);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float gj = g[k][j] * p.grad_scale;
-      m[k][j] = m[k][j] * p.b1 + gj * p.c1;
-      v[k][j] = v[k][j] * p.b2 + (gj * gj) * p.c2;
-      if constexpr (BITS == 8) {
-        root[j] = __builtin_amdgcn_sqrtf(v[k][j]);
-        w[k][j] = w[k][j] * keep - (m[k][j] * p.k1) * rcp_fast(root[j] * p.k2 + p.eps);
-      } else {
-        root[j] = sqrtf(v[k][j]);
-        w[k][j] = w[k][j] * keep - (m[k][j] * p.k1) / (root[j] * p.k2 + p.eps);
-      }
-    }
-    if constexpr (BITS == 8) {
-      // 32 lanes hold a block: its largest finite magnitudes give the scales
-      float tm = 0.f, tv = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool in = i + j < n;
-        if (!in) { m[k][j] = 0.f; v[k][j] = 0.f; root[j] = 0.f; }
-        tm = fmaxf(tm, finite(m[k][j]) ? fabsf(m[k][j]) : 0.f);
-        tv = fmaxf(tv, finite(v[k][j]) ? v[k][j] : 0.f);
-      }
-      const int em = scale_exponent(max_neighbours<32>(tm)), ev = scale_exponent(sqrtf(max_neighbours<32>(tv)));
-      const float im = power2(-em), iv = power2(-ev);
-      uint32_t qm = 0, qv = 0;
-      const int64_t where = at + i;                        // (a multiple of four)
-      const uint32_t first = (uint32_t)where * 0x9E3779B1u + (uint32_t)(where >> 32) * 0xC2B2AE3Du + p.salt;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t rand = stir(first + j * 0x9E3779B1u);
-        qm |= code_m(m[k][j], im, rand) << (8 * j);
-        qv |= code_v(v[k][j], root[j], iv, rand) << (8 * j);
-      }
-      if (i < n) {
-        *(uint32_t *)((uint8_t *)p.m + at + i) = qm;
-        *(uint32_t *)((uint8_t *)p.v + at + i) = qv;
-        if ((threadIdx.x & 31) == 0) {
-          p.m_scale[(at + i) / SNN_ADAMW_BLOCK] = power2(em);
-          p.v_scale[(at + i) / SNN_ADAMW_BLOCK] = power2(ev);
-        }
-        give4(param, w[k], i, n, vp);
-        if (copy) give4(copy, w[k], i, n, vc);
-      }
-    } else {
-      give4((float *)p.m + at, m[k], i, n, true);
-      give4((float *)p.v + at, v[k], i, n, true);
-      give4(param, w[k], i, n, vp);
-      if (copy) give4(copy, w[k], i, n, vc);
+      m[j] *= sm;
+      const float r = v[j] * sv;
+      v[j] = r * r;
     }
   }
-}
-
-template <typename G, int BITS> int adamw_launch(const AdamP &p, int iter, hipStream_t st) {
-  const dim3 grid(p.first[p.count]);
-  if (iter == 4) hipLaunchKernelGGL((adamw_kernel<G, BITS, 4>), grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((adamw_kernel<G, BITS, 1>), grid, dim3(256), 0, st, p);
-  return ops_launched("AdamW");
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float gj = g[j] * p.grad_scale;
+    m[j] = m[j] * p.b1 + gj * p.c1;
+    v[j] = v[j] * p.b2 + (gj * gj) * p.c2;
+    if constexpr (BITS == 8) {
+      root[j] = __builtin_amdgcn_sqrtf(v[j]);
+      w[j] = w[j] * keep - (m[j] * p.k1) * rcp_fast(root[j] * p.k2 + p.eps);
+    } else {
+      root[j] = sqrtf(v[j]);
+      w[j] = w[j] * keep - (m[j] * p.k1) / (root[j] * p.k2 + p.eps);
+    }
+  }
+  if constexpr (BITS == 8) {
+    // 32 lanes hold a block: its largest finite magnitudes give the scales
+    float tm = 0.f, tv = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i + j >= n) { m[j] = 0.f; v[j] = 0.f; root[j] = 0.f; }
+      tm = fmaxf(tm, finite(m[j]) ? fabsf(m[j]) : 0.f);
+      tv = fmaxf(tv, finite(v[j]) ? v[j] : 0.f);
+    }
+    const int em = scale_exponent(max_neighbours<32>(tm)), ev = scale_exponent(sqrtf(max_neighbours<32>(tv)));
+    const float im = power2(-em), iv = power2(-ev);
+    uint32_t qm = 0, qv = 0;
+    const int64_t where = at + i;                          // (a multiple of four)
+    const uint32_t first = (uint32_t)where * 0x9E3779B1u + (uint32_t)(where >> 32) * 0xC2B2AE3Du + p.salt;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t rand = stir(first + j * 0x9E3779B1u);
+      qm |= code_m(m[j], im, rand) << (8 * j);
+      qv |= code_v(v[j], root[j], iv, rand) << (8 * j);
+    }
+    if (i >= n) return;
+    *(uint32_t *)((uint8_t *)p.m + where) = qm;
+    *(uint32_t *)((uint8_t *)p.v + where) = qv;
+    if ((threadIdx.x & 31) == 0) {
+      p.m_scale[where / SNN_ADAMW_BLOCK] = power2(em);
+      p.v_scale[where / SNN_ADAMW_BLOCK] = power2(ev);
+    }
+  } else {
+    give4((float *)p.m + at, m, i, n, true);
+    give4((float *)p.v + at, v, i, n, true);
+  }
+  give4(param, w, i, n, vp);
+  if (copy) give4(copy, w, i, n, vc);
 }
 
 }  // namespace
@@ -262,15 +239,13 @@ extern "C" int32_t snn_adamw_step(const snn_adamw_args *a, const snn_adamw_tenso
   if (!(a->eps >= 0) || !isfinite(a->eps) || !isfinite(a->lr) || !isfinite(a->grad_scale)) return ops_fail(SNN_ERR_ARG, "AdamW: lr, eps and grad_scale must be finite, eps not negative");
   if (!a->m || !a->v || (a->bits == 8 && (!a->m_scale || !a->v_scale))) return ops_fail(SNN_ERR_NULL, "AdamW: a moment buffer is NULL");
   if (!aligned(a->m, 16) || !aligned(a->v, 16) || !aligned(a->m_scale, 4) || !aligned(a->v_scale, 4)) return ops_fail(SNN_ERR_ARG, "AdamW: m and v must be 16-byte aligned");
-  int64_t all = 0;
   for (int i = 0; i < count; ++i) {
     const snn_adamw_tensor &t = tensors[i];
-    if (t.n < 0 || t.n > (1ll << 35) || t.at < 0 || t.at % SNN_ADAMW_BLOCK) return ops_fail(SNN_ERR_ARG, "AdamW: tensor %d: n must be 0 to 2^35, at a multiple of %d", i, SNN_ADAMW_BLOCK);
+    if (t.n < 0 || t.n > (1ll << 33) || t.at < 0 || t.at % SNN_ADAMW_BLOCK) return ops_fail(SNN_ERR_ARG, "AdamW: tensor %d: n must be 0 to 2^33, at a multiple of %d", i, SNN_ADAMW_BLOCK);
     if (!t.n) continue;
     if (!t.param || !t.grad) return ops_fail(SNN_ERR_NULL, "AdamW: tensor %d: param or grad is NULL", i);
     if (!aligned(t.param, 4) || !aligned(t.grad, a->grad_type == SNN_TYPE_FP32 ? 4 : 2) || !aligned(t.copy, 2)) return ops_fail(SNN_ERR_ARG, "AdamW: tensor %d: a pointer is not aligned to its element type", i);
     if (!isfinite(t.weight_decay)) return ops_fail(SNN_ERR_ARG, "AdamW: tensor %d: weight_decay must be finite", i);
-    all += t.n;
   }
   AdamP p;
   p.m = a->m; p.v = a->v; p.m_scale = a->m_scale; p.v_scale = a->v_scale;
@@ -280,18 +255,21 @@ extern "C" int32_t snn_adamw_step(const snn_adamw_args *a, const snn_adamw_tenso
   p.k2 = (float)(1 / sqrt(1 - pow(a->beta2, (double)a->step)));
   p.eps = (float)a->eps; p.grad_scale = (float)a->grad_scale;
   p.salt = stir(a->seed * 0x9E3779B1u + (uint32_t)a->step * 0x85EBCA77u);
-  // one element group a thread while that leaves a small model more workgroups, four where the chip is full anyway
-  const int iter = all >= (1 << 21) ? 4 : 1;
-  const int64_t chunk = 1024 * iter;
   p.count = 0;
   p.first[0] = 0;
   for (int i = 0; i <= count; ++i) {
     const bool end = i == count;
-    const int64_t chunks = end ? 0 : (tensors[i].n + chunk - 1) / chunk;
+    const int64_t chunks = end ? 0 : (tensors[i].n + CHUNK - 1) / CHUNK;
     if (!end && !chunks) continue;
     if (p.count && (end || p.count == TENSORS || p.first[p.count] + chunks > (1 << 23))) {
-      const int rc = a->grad_type == SNN_TYPE_FP32 ? (a->bits == 32 ? adamw_launch<float, 32>(p, iter, (hipStream_t)stream) : adamw_launch<float, 8>(p, iter, (hipStream_t)stream))
-                                                   : (a->bits == 32 ? adamw_launch<__bf16, 32>(p, iter, (hipStream_t)stream) : adamw_launch<__bf16, 8>(p, iter, (hipStream_t)stream));
+      const dim3 grid(p.first[p.count]), block(256);
+      const hipStream_t st = (hipStream_t)stream;
+      const bool wide = a->grad_type == SNN_TYPE_FP32;
+      if (a->bits == 32 && wide) hipLaunchKernelGGL((adamw_kernel<float, 32>), grid, block, 0, st, p);
+      else if (a->bits == 32) hipLaunchKernelGGL((adamw_kernel<__bf16, 32>), grid, block, 0, st, p);
+      else if (wide) hipLaunchKernelGGL((adamw_kernel<float, 8>), grid, block, 0, st, p);
+      else hipLaunchKernelGGL((adamw_kernel<__bf16, 8>), grid, block, 0, st, p);
+      const int rc = ops_launched("AdamW");
       if (rc) return rc;
       p.count = 0;
     }

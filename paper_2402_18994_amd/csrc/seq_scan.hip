@@ -649,8 +649,17 @@ __global__ __launch_bounds__(256) void scan_sum_rows_kernel(const ScanP p, const
     const int gr = (int)(row % p.G), b = (int)(row / p.G % p.B), t = (int)(row / p.G / p.B);
     if (n >= p.N) continue;
     float s = 0.f;
-    if (t < length_of(p.lengths, b, p.T))
-      for (int k = 0; k < p.blocks; ++k) s += dbc[k * all + id];
+    if (t < length_of(p.lengths, b, p.T)) {
+      int k = 0;
+      for (; k + 8 <= p.blocks; k += 8) {                   // (eight loads in flight)
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = dbc[(k + u) * all + id];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += v[u];
+      }
+      for (; k < p.blocks; ++k) s += dbc[k * all + id];
+    }
     const Rows<void> &to = kind ? dcv : dbv;
     ((T *)to.p)[t * to.st + b * to.sb + (int64_t)gr * p.N + n] = narrow<T>(s);
   }
