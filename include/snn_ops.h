@@ -24,6 +24,10 @@
  *     are not used (they may hold anything), outputs and gradients there are zero, states are those after the last
  *     step that exists.  Values outside [0, T] count as the nearer end.
  *   - T = 0 is a call without steps: states pass through, gradients of parameters are zero.
+ *   - Sizes that are refused (SNN_ERR_ARG): convolution, B * D from 2^31 or D above 2^28 on, or more than 2^26 wavefronts
+ *     (64 channels, or 256 where rows are aligned to four, by 32 steps of a sequence); scan, D above 2^22, B * D from 2^25,
+ *     B * groups from 2^18, T * B * groups from 2^32, strides between steps that are negative or put 16 steps of a tensor
+ *     2 GiB apart; AdamW, tensors of more than 2^33 elements.
  *   - Sums have a fixed order: the same call gives the same bits.
  */
 #ifndef SNN_OPS_H_

@@ -444,3 +444,63 @@ def test_refusals_name_what_is_wrong():
         with pytest.raises(SnnError) as e:
             f()
         assert e.value.status in (2, 3) and len(str(e.value)) > 20, i
+
+
+def test_lengths_outside_the_call_count_as_its_ends():
+    from paper_2402_18994_amd import causal_conv, selective_scan
+    x, w = torch.randn(21, 4, 24, device="cuda"), torch.randn(24, 4, device="cuda")
+    A, B = -torch.rand(24, 16, device="cuda"), torch.randn(21, 4, 16, device="cuda")
+    wild = torch.tensor([-5, 21 + 1000, -2 ** 31, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    tame = torch.tensor([0, 21, 0, 21], dtype=torch.int32, device="cuda")
+    for f in (lambda n: causal_conv(x, w, lengths=n), lambda n: selective_scan(x, x, A, B, B, lengths=n)):
+        a, b = f(wild), f(tame)
+        assert torch.equal(a.y, b.y) and torch.equal(a.state, b.state) and (a.y[:, 0] == 0).all() and (a.y[:, 1] != 0).any()
+
+
+def test_offsets_beyond_32_bits():
+    """Sequences 2.6 GB apart, then steps 100 MB apart: the same bits as from dense memory."""
+    from paper_2402_18994_amd import causal_conv, causal_conv_backward, selective_scan, selective_scan_backward
+    store = torch.empty(2_900_000_000, dtype=torch.bfloat16, device="cuda")
+    for shape, strides in (((40, 3, 72), (72, 1_300_000_000, 1)), ((55, 2, 72), (50_000_000, 100, 1))):
+        flat = torch.randn(*shape, device="cuda").to(torch.bfloat16)
+        far = store.as_strided(shape, strides, 64)
+        far.copy_(flat)
+        w = torch.randn(72, 4, device="cuda")
+        assert torch.equal(causal_conv(far, w).y, causal_conv(flat, w).y)
+        for a, b in zip(causal_conv_backward(far, far, w)[:2], causal_conv_backward(flat, flat, w)[:2]):
+            assert torch.equal(a, b)
+        A, B = -torch.rand(72, 16, device="cuda"), flat[..., :16].contiguous()
+        one, two = (selective_scan(v, v, A, b, b, z=v, save=True) for v, b in ((far, far[..., :16]), (flat, B)))
+        assert torch.equal(one.y, two.y) and torch.equal(one.state, two.state)
+        one, two = (selective_scan_backward(v, o.saved, v, v, A, b, b, z=v) for v, b, o in ((far, far[..., :16], one), (flat, B, two)))
+        for a, b in zip(one, two):
+            assert a is None or torch.equal(a, b)
+
+
+def test_strides_that_a_tile_cannot_hold_are_refused():
+    from paper_2402_18994_amd import SnnError, selective_scan
+    x = torch.zeros(1, device="cuda").expand(4, 1, 8)
+    A, B = -torch.rand(8, 4, device="cuda"), torch.zeros(4, 1, 4, device="cuda")
+    selective_scan(x[..., :1].expand(4, 1, 1), x[..., :1].expand(4, 1, 1), A[:1].contiguous(), B, B)       # strides of zero are fine
+    wide = torch.empty(3 * (1 << 26) + 8, device="cuda").as_strided((4, 1, 8), (1 << 26, 8, 1))
+    with pytest.raises(SnnError) as e:
+        selective_scan(wide, wide, A, B, B)
+    assert e.value.status == 2
+
+
+def test_infinities_stay_in_their_channel():
+    from paper_2402_18994_amd import causal_conv, selective_scan
+    _, t, s, _ = scan_case(40, 2, 70, 11, 1, "fp32", True, True, "none", True)
+    d, _ = scan_gpu(s, t, None)
+    w, b = torch.randn(70, 4, device="cuda"), torch.randn(70, device="cuda")
+    clean, conv = call(selective_scan, d), causal_conv(d["x"], w, b)
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        x = d["x"].clone()
+        x[5, 1, 33] = bad
+        hit, hit_conv = call(selective_scan, d | {"x": x}), causal_conv(x, w, b)
+        same = torch.ones_like(x, dtype=torch.bool)
+        same[5:, 1, 33] = False
+        assert torch.equal(hit.y[same], clean.y[same]) and not torch.isfinite(hit.y[5, 1, 33])
+        same = torch.ones_like(x, dtype=torch.bool)
+        same[5:9, 1, 33] = False
+        assert torch.equal(hit_conv.y[same], conv.y[same])
