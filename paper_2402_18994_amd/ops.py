@@ -25,7 +25,7 @@ from .binding import SnnError
 BLOCK = 128                       # SNN_ADAMW_BLOCK
 MAX_TAPS, MAX_STATES = 8, 64
 ERR_ARG, ERR_SHAPE = 2, 3
-_DTYPE = operator.attrgetter("dtype")
+_DTYPE, _SHAPE = operator.attrgetter("dtype"), operator.attrgetter("shape")
 
 
 class _Rows(C.Structure):
@@ -391,7 +391,7 @@ class AdamW:
         self.m_scale = self.v_scale = None
         if state_bits == 8:
             self.m_scale, self.v_scale = (torch.ones(n // BLOCK, device=dev) for _ in range(2))
-        self._sizes, self._strides = [p.numel() for p in self.params], [p.stride() for p in self.params]
+        self._shapes, self._sizes = [p.shape for p in self.params], [p.numel() for p in self.params]
         self._copied = [i for i, c in enumerate(self.copies) if c is not None]
         # snn_adamw_tensor, one a row; addresses are filled in by every step
         self._table = np.zeros((len(self.params), 6), np.int64)
@@ -402,7 +402,7 @@ class AdamW:
         """One step with these gradients (dense, all float32 or all bfloat16, multiplied by `grad_scale` first)."""
         # (checks run over all tensors at C speed: with many small tensors they are what a step costs)
         tensor, params, dev = torch.Tensor, self.params, self.m.get_device()
-        if list(map(tensor.numel, grads)) != self._sizes or list(map(tensor.stride, grads)) != self._strides:   # (so they are dense too)
+        if list(map(_SHAPE, grads)) != self._shapes or not all(map(tensor.is_contiguous, grads)):
             _refuse("a dense gradient of its shape is needed for every parameter", ERR_SHAPE)
         kind = set(map(_DTYPE, grads))
         if len(kind) != 1 or not kind <= _types.keys() or set(map(tensor.get_device, grads)) != {dev}:

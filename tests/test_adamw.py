@@ -281,3 +281,17 @@ def test_network_learns_with_8_bit_moments():
             opt.step()
         assert last < 0.5 * first, (bits, first, last)
         snn.destroy()
+
+
+def test_gradients_are_told_by_their_shapes():
+    """Strides of axes of length one do not matter; a transposed gradient, or one that repeats memory, is refused."""
+    from paper_2402_18994_amd import AdamW, SnnError
+    p, q = torch.randn(6, 1, device="cuda"), torch.randn(2, 3, device="cuda")
+    g, h = torch.randn(6, 1, device="cuda"), torch.randn(2, 3, device="cuda")
+    a, b = [p.clone(), q.clone()], [p.clone(), q.clone()]
+    AdamW(a).step([g, h])
+    AdamW(b).step([g.as_strided((6, 1), (1, 6)), h])
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    for wrong in (h.t().contiguous(), h.t(), torch.randn(1, 3, device="cuda").expand(2, 3), h.reshape(6, 1)):
+        with pytest.raises(SnnError):
+            AdamW(b).step([g, wrong])
