@@ -25,6 +25,8 @@ template <typename T> struct Rows {
   T *p;
   int64_t st, sb;
   Rows(const snn_rows &r) : p((T *)const_cast<void *>(r.p)), st(r.stride_t), sb(r.stride_b) {}
+  // Of a call of `steps` steps: the stride between steps, which may be anything where there is one, is then 0.
+  Rows(const snn_rows &r, int steps) : p((T *)const_cast<void *>(r.p)), st(steps > 1 ? r.stride_t : 0), sb(r.stride_b) {}
 };
 
 // ---------------------------------------------------------------- element types

@@ -38,8 +38,8 @@ struct ScanP {
   float *local;                      // [chunk][B][D][NP]: of the chunks from zero, then (joined) the states before them
   float *sums;                       // [chunk][B][D]: sum of delta
   explicit ScanP(const snn_scan_args &a)
-      : T(a.T), B(a.B), D(a.D), N(a.N), G(a.groups), softplus(a.softplus), chunk(TILE), nchunks(1), blocks(1), x(a.x), dt(a.dt),
-        z(a.z), bv(a.bv), cv(a.cv), y(a.y), A(a.A), skip(a.skip), dt_bias(a.dt_bias), init(a.init), lengths(a.lengths),
+      : T(a.T), B(a.B), D(a.D), N(a.N), G(a.groups), softplus(a.softplus), chunk(TILE), nchunks(1), blocks(1), x(a.x, a.T), dt(a.dt, a.T),
+        z(a.z, a.T), bv(a.bv, a.T), cv(a.cv, a.T), y(a.y, a.T), A(a.A), skip(a.skip), dt_bias(a.dt_bias), init(a.init), lengths(a.lengths),
         state(a.state), saved(nullptr), local(nullptr), sums(nullptr) {}
 };
 
@@ -50,8 +50,8 @@ struct ScanGradP {
   float *dA;                         // [chunk * B][D][NP] partial sums
   float *dsum;                       // [chunk * B][2][D]: of dskip and ddt_bias
   float *dbc;                        // [blocks][T][B][G][2][NP] partial sums of dBv and dCv
-  explicit ScanGradP(const snn_scan_grads &g)
-      : dy(g.dy), dx(g.dx), ddt(g.ddt), dz(g.dz), d_state(g.d_state), dinit(g.dinit), dA(nullptr), dsum(nullptr), dbc(nullptr) {}
+  ScanGradP(const snn_scan_grads &g, int T)
+      : dy(g.dy, T), dx(g.dx, T), ddt(g.ddt, T), dz(g.dz, T), d_state(g.d_state), dinit(g.dinit), dA(nullptr), dsum(nullptr), dbc(nullptr) {}
 };
 
 // Where a wavefront's work lies.
@@ -97,6 +97,12 @@ template <int NS> __device__ __forceinline__ void store_states(float *row, const
 #pragma unroll
   for (int j = 0; j < NS; ++j)
     if (part * NS + j < N) row[part * NS + j] = r[j];
+}
+// The decay of a state, in base 2.  That of a state which forgets at once, A = -inf, becomes the lowest finite number, so
+// that it stays what it is over steps that do not exist: their delta is 0.
+__device__ __forceinline__ float decay_rate(float A) {
+  const float r = A * LOG2E;
+  return r < -3.4028234663852886e38f ? -3.4028234663852886e38f : r;
 }
 // The same out of rows of the library's own, which are padded and aligned.
 template <int NS> using States = Pack<float, NS>;
@@ -185,7 +191,7 @@ __global__ __launch_bounds__(64 * WAVES) void scan_forward_kernel(const ScanP p)
   float A[NS], h[NS], sum = 0.f;
   load_states<NS>(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
 #pragma unroll
-  for (int j = 0; j < NS; ++j) { A[j] *= LOG2E; h[j] = 0.f; }
+  for (int j = 0; j < NS; ++j) { A[j] = decay_rate(A[j]); h[j] = 0.f; }
   if constexpr (!LOCAL) {
     if (p.nchunks > 1) {
       const States<NS> v = pick<NS>(p.local + ((size_t)me.s * p.B * p.D + seq) * NP + me.part * NS);
@@ -306,7 +312,7 @@ template <int NP, bool REVERSE> __global__ __launch_bounds__(256) void scan_join
   const int n = (int)(id % NP);
   const int64_t seq = id / NP;
   const bool live = n < p.N;
-  const float A = live ? p.A[(seq % p.D) * p.N + n] * LOG2E : 0.f;
+  const float A = live ? decay_rate(p.A[(seq % p.D) * p.N + n]) : 0.f;
   float h = first && live ? first[seq * p.N + n] : 0.f;
   const int last = p.nchunks - 1;                          // (the chunk that nobody follows was not run from zero)
   for (int i0 = 0; i0 <= last; i0 += AHEAD) {
@@ -343,7 +349,7 @@ __global__ __launch_bounds__(64 * WAVES) void scan_reverse_local_kernel(const Sc
   float A[NS], q[NS], sum = 0.f;
   load_states<NS>(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
 #pragma unroll
-  for (int j = 0; j < NS; ++j) { A[j] *= LOG2E; q[j] = 0.f; }
+  for (int j = 0; j < NS; ++j) { A[j] = decay_rate(A[j]); q[j] = 0.f; }
   const float dt_bias = p.dt_bias ? p.dt_bias[me.ed] : 0.f;
   Stream<T, E> gy(g.dy, me.b, me.ed, me.et), gd(p.dt, me.b, me.ed, me.et), gz(p.z, me.b, me.ed, me.et);
   Vectors<T, NP, 64> gc(p.cv, me.b, me.g, p.N, me.lane);
@@ -431,7 +437,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
   float A[NS], A2[NS], q[NS], dA[NS];
   load_states<NS>(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
 #pragma unroll
-  for (int j = 0; j < NS; ++j) { A2[j] = A[j] * LOG2E; dA[j] = 0.f; }
+  for (int j = 0; j < NS; ++j) { A2[j] = decay_rate(A[j]); dA[j] = 0.f; }
   if (p.nchunks > 1) {
     const States<NS> v = pick<NS>(p.local + ((size_t)me.s * p.B * p.D + seq) * NP + me.part * NS);
 #pragma unroll
@@ -721,7 +727,7 @@ template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void s
   float v = 0.f;
 #pragma unroll
   for (int j = 0; j < NS; ++j) {
-    h[j] = fmaf(exp_fast(delta * A[j]), h[j], u * bq[j]);
+    h[j] = fmaf(__builtin_amdgcn_exp2f(delta * decay_rate(A[j])), h[j], u * bq[j]);
     v = fmaf(cq[j], h[j], v);
   }
   v = sum_neighbours<L>(v);
@@ -888,7 +894,7 @@ template <typename T, typename K, bool GATE>
 int backward(const snn_scan_args &a, const Shape &k, const snn_scan_grads &gr, const void *saved, char *ws, hipStream_t st) {
   const ScanSpace s = scan_space(a, true);
   const ScanP p = plan(a, k, true, saved, ws, s);
-  ScanGradP g(gr);
+  ScanGradP g(gr, a.T);
   g.dA = (float *)(ws + s.dA);
   g.dsum = (float *)(ws + s.dsum);
   g.dbc = (float *)(ws + s.dbc);
@@ -904,7 +910,7 @@ int backward(const snn_scan_args &a, const Shape &k, const snn_scan_grads &gr, c
   if ((rc = ops_launched("scan reverse"))) return rc;
   const int64_t values = (int64_t)a.T * a.B * a.groups * 2 * K::NP;
   if (values) {
-    hipLaunchKernelGGL((scan_sum_rows_kernel<T, K::NP>), dim3((unsigned)std::min<int64_t>((values + 255) / 256, 1 << 16)), dim3(256), 0, st, p, g.dbc, Rows<void>(gr.dbv), Rows<void>(gr.dcv));
+    hipLaunchKernelGGL((scan_sum_rows_kernel<T, K::NP>), dim3((unsigned)std::min<int64_t>((values + 255) / 256, 1 << 16)), dim3(256), 0, st, p, g.dbc, Rows<void>(gr.dbv, a.T), Rows<void>(gr.dcv, a.T));
     if ((rc = ops_launched("scan reverse, rows"))) return rc;
   }
   const int64_t groups = ((int64_t)a.D * K::NP + 15) / 16 + (2 * (int64_t)a.D + 15) / 16;

@@ -504,3 +504,39 @@ def test_infinities_stay_in_their_channel():
         same = torch.ones_like(x, dtype=torch.bool)
         same[5:9, 1, 33] = False
         assert torch.equal(hit_conv.y[same], conv.y[same])
+
+
+def test_a_single_step_whose_stride_means_nothing():
+    """The stride between steps of a tensor with one step may be anything."""
+    from paper_2402_18994_amd import causal_conv, selective_scan, selective_scan_backward
+    for t in TYPES.values():
+        for far in (2 ** 29, 2 ** 30 + 2 ** 28, 2 ** 40 + 2 ** 29):
+            _, _, s, _ = scan_case(1, 2, 70, 12, 1, "fp32" if t is torch.float32 else "bf16", True, True, "none", True)
+            d, _ = scan_gpu(s, t, None)
+            odd = {k: (v.as_strided(v.shape, (far, *v.stride()[1:])) if k in ("x", "dt", "z", "Bv", "Cv") else v) for k, v in d.items()}
+            assert odd["x"].stride(0) == far
+            want, got = call(selective_scan, d, save=True), call(selective_scan, odd, save=True)
+            assert all(torch.equal(a, b) for a, b in zip(want, got))
+            for a, b in zip(call(selective_scan_backward, d, d["z"], want.saved), call(selective_scan_backward, odd, odd["z"], got.saved)):
+                assert torch.equal(a, b)
+            w = torch.randn(70, 4, device="cuda")
+            assert torch.equal(causal_conv(odd["x"], w).y, causal_conv(d["x"], w).y)
+
+
+@pytest.mark.parametrize("T", [40, 300])                   # (300: cut in chunks of time)
+def test_states_that_forget_at_once(T):
+    """A = -inf: such a state is its last step's input, also after steps that do not exist."""
+    from paper_2402_18994_amd import selective_scan, selective_scan_step
+    _, t, s, n = scan_case(T, 3, 20, 6, 1, "fp32", True, True, "some", True)
+    n[1] = T - 37                                          # (ends inside a tile, and a chunk or more before the end)
+    s["A"][:, 2] = float("-inf")
+    d, gn = scan_gpu(s, t, n)
+    wy, ws = oracle.scan(**s, lengths=n)
+    out = call(selective_scan, d, lengths=gn)
+    close("y", out.y, wy, T, 2.0 ** -24)
+    close("state", out.state, ws, T, 2.0 ** -24)
+    state = d["init"].clone()
+    selective_scan_step(d["x"][0], d["dt"][0], state, d["A"], d["Bv"][0], d["Cv"][0], d["D"], d["z"][0], d["dt_bias"])
+    _, end = oracle.scan(**(s | {k: s[k][:1] for k in ("x", "dt", "z", "Bv", "Cv")}))
+    exists = [b for b in range(3) if int(n[b])]
+    close("stepped", state[exists], end[exists], 1, 2.0 ** -24)
