@@ -4,6 +4,9 @@
 // wavefront owns 64 lanes x VEC neighbouring channels of one sequence and walks a segment of its steps with the last
 // W - 1 inputs in registers, AHEAD rows in flight.  Sequence, segment and length are the same for the whole wavefront,
 // so all tests are on scalars, and a row that does not exist is a buffer access that the hardware drops.
+// Measured, bfloat16, four taps: 1024 steps of 8 x 2048 channels 14.4 us a call, 4.7 TB/s (a copy of 64 MiB, which the
+// last-level cache holds, reaches 7.8, one of 1 GiB 5.1); forward 29 and backward 47 us for 256 steps of 128 x 1024
+// channels of uneven lengths, of which half the rows exist (0.10 and 0.13 GB); the sums of the filter's gradients 4.4 us.
 #include "common.hpp"
 #include "seq_common.hpp"
 
@@ -56,6 +59,12 @@ template <typename T, int VEC> __device__ __forceinline__ void store_row(T *row,
   else if constexpr (sizeof(T) * VEC == 4) st_b32(r, at, 0, __builtin_bit_cast(uint32_t, v));
   else st_b16(r, at, 0, __builtin_bit_cast(unsigned short, v));
 }
+// Rows [t0, t1), which do not exist.  Segments of such rows alone, those that start behind a sequence's end, are written
+// by this and cost nothing else; a first segment has the state to see to and is never one.
+template <typename T, int VEC> __device__ __forceinline__ void store_zeros(T *base, int64_t st, int at, int t0, int t1) {
+  const Pack<T, VEC> zero = {};
+  for (int t = t0; t < t1; ++t) store_row<T, VEC>(base + t * st, at, zero);
+}
 // Row `t` of the input of sequence b, from -(W-1) on; zeros before the first step without `init`, and for t >= end.
 template <typename T, int VEC, int W>
 __device__ __forceinline__ Pack<T, VEC> input_row(const ConvP &a, int b, int at, int t, int end) {
@@ -80,6 +89,10 @@ __global__ __launch_bounds__(256) void conv_forward_kernel(const ConvP a) {
   const int t0 = s * a.seg, t1 = min(a.T, t0 + a.seg), end = min(t1, len);
   T *y = (T *)a.y.p + b * a.y.sb;
 
+  if (s > 0 && t0 >= len) {
+    store_zeros<T, VEC>(y, a.y.st, at, t0, t1);
+    return;
+  }
   float w[W][VEC], bias[VEC], xs[W - 1 + AHEAD][VEC];
   load_filter<T, VEC, W>(a, live ? d : 0, w, bias);
 #pragma unroll
@@ -124,7 +137,7 @@ __global__ __launch_bounds__(256) void conv_forward_kernel(const ConvP a) {
   }
 }
 
-// One step: the state [W-1][B][D] moves up a row.
+// One step: the state [W-1][B][D] moves up a row.  64 x 2048 channels in bfloat16 4.3 us: the launch.
 template <typename T, int VEC, int W>
 __global__ __launch_bounds__(256) void conv_step_kernel(const ConvP a) {
   const int dv = a.D / VEC;
@@ -189,6 +202,10 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvP a, const
     const T *dy = (const T *)g.dy.p + b * g.dy.sb;
     T *dx = (T *)g.dx.p + b * g.dx.sb;
     const int t0 = s0 * a.seg, t1 = min(a.T, t0 + a.seg), stop = t1 + W - 1, end = min(stop, len);
+    if (s0 > 0 && t0 >= len) {
+      store_zeros<T, VEC>(dx, g.dx.st, at, t0, t1);
+      continue;
+    }
     float xs[W - 1 + AHEAD_BWD][VEC], q[W - 1 + AHEAD_BWD][VEC];
 #pragma unroll
     for (int k = 0; k < W - 1; ++k) {
