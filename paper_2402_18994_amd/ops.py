@@ -151,11 +151,19 @@ def _start(x):
     return kind, dev
 
 
-def _rows(t, x, dev, shape, name):
-    """The fields of the snn_rows of a [T, B, D] or, for one step, [B, D] tensor like x."""
+def _first(x, shape):
+    """The fields of the snn_rows of a call's first tensor, which the others are compared with."""
+    s = x.stride()
+    if s[-1] != 1 and shape[-1] > 1:
+        _refuse("the channels of x have to be dense")
+    return (x.data_ptr(), s[0], s[1]) if len(s) == 3 else (x.data_ptr(), 0, s[0])
+
+
+def _rows(t, dtype, dev, shape, name):
+    """The same of another [T, B, D] or, for one step, [B, D] tensor, which has to be like the first."""
     if t.shape != shape:
         _refuse(f"{name} is {tuple(t.shape)}, {tuple(shape)} is needed", ERR_SHAPE)
-    if t.dtype is not x.dtype or t.get_device() != dev:
+    if t.dtype is not dtype or t.get_device() != dev:
         _refuse(f"{name} has another type or device than x")
     s = t.stride()
     if s[-1] != 1 and shape[-1] > 1:
@@ -163,14 +171,14 @@ def _rows(t, x, dev, shape, name):
     return (t.data_ptr(), s[0], s[1]) if len(s) == 3 else (t.data_ptr(), 0, s[0])
 
 
-def _vectors(t, x, dev, lead, N, name):
+def _vectors(t, dtype, dev, lead, N, name):
     """The fields of the snn_rows of a [*lead, G, N] tensor, or [*lead, N] for one group, and G."""
     k, s, shape = len(lead), t.stride(), t.shape
     grouped = len(shape) == k + 2
     g = shape[k] if grouped else 1
-    if shape[:k] != lead or shape[-1] != N or len(shape) != k + 1 + grouped:
+    if shape != ((*lead, g, N) if grouped else (*lead, N)):
         _refuse(f"{name} is {tuple(shape)}, {(*lead, g, N)} is needed", ERR_SHAPE)
-    if t.dtype is not x.dtype or t.get_device() != dev:
+    if t.dtype is not dtype or t.get_device() != dev:
         _refuse(f"{name} has another type or device than x")
     if (s[-1] != 1 and N > 1) or (grouped and g > 1 and s[k] != N):
         _refuse(f"the vectors of {name} have to be dense")
@@ -222,14 +230,14 @@ def _conv_args(x, weight, bias, init, lengths, silu, step=False):
     shape = x.shape
     if len(shape) != (2 if step else 3):
         _refuse("x has to be [B, D]" if step else "x has to be [T, B, D]", ERR_SHAPE)
-    B, D = shape[-2:]
+    *_, B, D = shape
     if B == 0 or D == 0:
         _refuse("there has to be a sequence and a channel", ERR_SHAPE)
     if weight.dim() != 2 or weight.shape[0] != D or not 1 <= weight.shape[1] <= MAX_TAPS:
         _refuse(f"weight has to be [D, W], W from 1 to {MAX_TAPS}", ERR_SHAPE)
     W, f32 = weight.shape[1], torch.float32
     T = 1 if step else shape[0]
-    head = (T, B, D, W, kind, 1 if silu else 0, *_rows(x, x, dev, shape, "x"))
+    head = (T, B, D, W, kind, 1 if silu else 0, *_first(x, shape))
     tail = (_dense(weight, dev, (D, W), f32, "weight"), _dense(bias, dev, (D,), f32, "bias"), _dense(init, dev, (W - 1, B, D), x.dtype, "init"),
             _dense(lengths, dev, (B,), torch.int32, "lengths"))
     return dev, W, lambda y, state: _CONV.pack(*head, y, B * D, D, *tail, state)
@@ -256,7 +264,7 @@ def causal_conv_backward(dy, x, weight, bias=None, init=None, lengths=None, silu
     dx, dweight = torch.empty_like(x, memory_format=torch.contiguous_format), torch.empty_like(weight)
     dbias = torch.empty_like(bias) if bias is not None else None
     dinit = torch.empty_like(init) if init is not None else None
-    g = _CONV_GRADS.pack(*_rows(dy, x, dev, x.shape, "dy"), dx.data_ptr(), B * D, D, _dense(d_state, dev, (W - 1, B, D), x.dtype, "d_state"),
+    g = _CONV_GRADS.pack(*_rows(dy, x.dtype, dev, x.shape, "dy"), dx.data_ptr(), B * D, D, _dense(d_state, dev, (W - 1, B, D), x.dtype, "d_state"),
                          dweight.data_ptr(), dbias.data_ptr() if bias is not None else 0, dinit.data_ptr() if init is not None else 0)
     n = _bytes_of(_declared.snn_conv_workspace_bytes, a)
     ws = _space(n, x)
@@ -282,18 +290,18 @@ def _scan_args(x, dt, A, B, Cv, D, z, dt_bias, softplus, init, lengths, step=Fal
     shape = x.shape
     if len(shape) != (2 if step else 3):
         _refuse("x has to be [B, D]" if step else "x has to be [T, B, D]", ERR_SHAPE)
-    nb, nd = shape[-2:]
+    *_, nb, nd = shape
     if nb == 0 or nd == 0:
         _refuse("there has to be a sequence and a channel", ERR_SHAPE)
     if A.dim() != 2 or A.shape[0] != nd or not 1 <= A.shape[1] <= MAX_STATES:
         _refuse(f"A has to be [D, N], N from 1 to {MAX_STATES}", ERR_SHAPE)
-    N, f32, lead = A.shape[1], torch.float32, shape[:-1]
-    bv, g = _vectors(B, x, dev, lead, N, "B")
-    cv, gc = _vectors(Cv, x, dev, lead, N, "C")
+    N, f32, dtype, lead = A.shape[1], torch.float32, x.dtype, (nb,) if step else (shape[0], nb)
+    bv, g = _vectors(B, dtype, dev, lead, N, "B")
+    cv, gc = _vectors(Cv, dtype, dev, lead, N, "C")
     if g != gc or g < 1 or nd % g:
         _refuse("B and C have to have the same number of groups, which divides D", ERR_SHAPE)
-    head = (1 if step else shape[0], nb, nd, N, g, kind, 1 if softplus else 0, *_rows(x, x, dev, shape, "x"), *_rows(dt, x, dev, shape, "dt"),
-            *(_rows(z, x, dev, shape, "z") if z is not None else (0, 0, 0)), *bv, *cv)
+    head = (1 if step else shape[0], nb, nd, N, g, kind, 1 if softplus else 0, *_first(x, shape), *_rows(dt, dtype, dev, shape, "dt"),
+            *(_rows(z, dtype, dev, shape, "z") if z is not None else (0, 0, 0)), *bv, *cv)
     tail = (_dense(A, dev, (nd, N), f32, "A"), _dense(D, dev, (nd,), f32, "D"), _dense(dt_bias, dev, (nd,), f32, "dt_bias"),
             _dense(init, dev, (nb, nd, N), f32, "init"), _dense(lengths, dev, (nb,), torch.int32, "lengths"))
     return dev, (N, g), lambda y, state: _SCAN.pack(*head, y, nb * nd, nd, *tail, state)
@@ -336,7 +344,7 @@ def selective_scan_backward(dy, saved, x, dt, A, B, C_, D=None, z=None, dt_bias=
 
     out = ScanGrads(like(x), like(x), like(A), like(B), like(C_), like(D), like(z), like(dt_bias), like(init))
     full, row = (nb * nd, nd), (nb * groups * N, groups * N)
-    g = _SCAN_GRADS.pack(*_rows(dy, x, dev, x.shape, "dy"), _dense(d_state, dev, (nb, nd, N), torch.float32, "d_state"), at(out.dx), *full,
+    g = _SCAN_GRADS.pack(*_rows(dy, x.dtype, dev, x.shape, "dy"), _dense(d_state, dev, (nb, nd, N), torch.float32, "d_state"), at(out.dx), *full,
                          at(out.ddt), *full, at(out.dz), *full, at(out.dB), *row, at(out.dC), *row, at(out.dA), at(out.dD), at(out.ddt_bias), at(out.dinit))
     n = _bytes_of(lib.snn_scan_workspace_bytes, a, 1)
     ws = _space(n, x)
