@@ -399,26 +399,37 @@ class AdamW:
         self.m_scale = self.v_scale = None
         if state_bits == 8:
             self.m_scale, self.v_scale = (torch.ones(n // BLOCK, device=dev) for _ in range(2))
-        self._shapes, self._sizes = [p.shape for p in self.params], [p.numel() for p in self.params]
+        self._shapes = [p.shape for p in self.params]
         self._copied = [i for i, c in enumerate(self.copies) if c is not None]
-        # snn_adamw_tensor, one a row; addresses are filled in by every step
+        # snn_adamw_tensor, one a row; the gradients' addresses are filled in by every step
         self._table = np.zeros((len(self.params), 6), np.int64)
         self._table[:, 3], self._table[:, 4] = [p.numel() for p in self.params], self.at
         self._table[:, 5] = np.array(decay, np.float64).view(np.int64)
+        self._bind()
+
+    def _bind(self):
+        """Takes the parameters' memory as it is now.  The optimiser holds on to that memory (`_held`), so as long as a
+        parameter's address is the one noted here, what lies there is the memory that was looked at here."""
+        for p, shape in zip(self.params, self._shapes):
+            if p.shape != shape or p.dtype != torch.float32 or p.device != self.device or not p.is_contiguous():
+                _refuse("a parameter is not what it was when the optimiser was made")
+        self._held = [p.detach() for p in self.params]
+        self._addresses = [p.data_ptr() for p in self._held]
+        self._table[:, 0] = self._addresses
 
     def step(self, grads: Sequence, lr: Optional[float] = None, grad_scale: float = 1.0) -> None:
         """One step with these gradients (dense, all float32 or all bfloat16, multiplied by `grad_scale` first)."""
         # (checks run over all tensors at C speed: with many small tensors they are what a step costs)
-        tensor, params, dev = torch.Tensor, self.params, self.m.get_device()
+        tensor, params, dev = torch.Tensor, self.params, self.device.index
         if list(map(_SHAPE, grads)) != self._shapes or not all(map(tensor.is_contiguous, grads)):
             _refuse("a dense gradient of its shape is needed for every parameter", ERR_SHAPE)
         kind = set(map(_DTYPE, grads))
         if len(kind) != 1 or not kind <= _types.keys() or set(map(tensor.get_device, grads)) != {dev}:
             _refuse("gradients have to be all float32 or all bfloat16, on the parameters' device")
-        if list(map(tensor.numel, params)) != self._sizes or set(map(_DTYPE, params)) != {torch.float32} or set(map(tensor.get_device, params)) != {dev} or not all(map(tensor.is_contiguous, params)):
-            _refuse("a parameter is not what it was when the optimiser was made")
+        if list(map(tensor.data_ptr, params)) != self._addresses:
+            self._bind()
         t = self._table
-        t[:, 0], t[:, 1] = list(map(tensor.data_ptr, params)), list(map(tensor.data_ptr, grads))
+        t[:, 1] = list(map(tensor.data_ptr, grads))
         for i in self._copied:
             t[i, 2] = self.copies[i].data_ptr()
         scales = (self.m_scale.data_ptr(), self.v_scale.data_ptr()) if self.bits == 8 else (0, 0)

@@ -295,3 +295,25 @@ def test_gradients_are_told_by_their_shapes():
     for wrong in (h.t().contiguous(), h.t(), torch.randn(1, 3, device="cuda").expand(2, 3), h.reshape(6, 1)):
         with pytest.raises(SnnError):
             AdamW(b).step([g, wrong])
+
+
+def test_parameters_that_move():
+    """A parameter whose memory is replaced is followed; one that becomes another tensor is refused."""
+    from paper_2402_18994_amd import AdamW, SnnError
+    p = [torch.nn.Parameter(torch.randn(6, 5, device="cuda")), torch.nn.Parameter(torch.randn(40, device="cuda"))]
+    q = [x.detach().clone() for x in p]
+    g = [torch.randn_like(x) for x in q]
+    a, b = AdamW(p), AdamW(q)
+    for k in range(4):
+        if k == 2:
+            old = p[0].data
+            p[0].data = old.clone()
+            old.fill_(7)
+        a.step(g)
+        b.step(g)
+        assert all(torch.equal(x, y) for x, y in zip(p, q)), k
+    assert (old == 7).all()
+    for wrong in (torch.randn(5, 6, device="cuda"), torch.randn(5, 6, device="cuda").t(), torch.randn(6, 5, device="cuda").to(torch.bfloat16)):
+        p[0].data = wrong
+        with pytest.raises(SnnError):
+            a.step(g)
