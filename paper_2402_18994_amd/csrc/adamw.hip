@@ -5,15 +5,17 @@
 // travel as kernel arguments, up to TENSORS in a launch, so a step needs no table on the device and no copy; a
 // workgroup finds its tensor by bisection over the chunk numbers.  A thread takes four neighbouring elements: with more
 // of them a thread, fewer threads hide the loads (four elements, eight, sixteen: 79 million parameters in 32 bits 403,
-// 412 and 421 us, 5.5 TB/s the first; in 8 bits with bfloat16 gradients 230, 241 and 260 us, 4.8 TB/s; 7.6 million in 8
-// bits 28, 30 and 34 us).
+// 412 and 421 us, 5.5 TB/s the first; in 8 bits with bfloat16 gradients 230, 241 and 260 us; 7.6 million in 8 bits 28, 30
+// and 34 us, all in 8 bits with the arithmetic as it was before what follows).
 // Every operation is rounded by itself (no contraction), so that the codes of 8-bit moments do not depend on how the
 // compiler joins operations.
-// With 8-bit moments the arithmetic counts as well (the random bits, two roundings, the scales: 38 us for 7.6 million
-// parameters, sixteen a thread, when root and quotient were the correctly rounded ones, ten operations more each; 34 so).  There the roots
-// of single elements and the quotient come from the hardware's approximations, one unit of the last place off: the
+// With 8-bit moments the arithmetic counts as well: random bits, two roundings, the scales.  7.6 million parameters took
+// 28 us with codes taken apart into exponent and steps in floating point, a branch for what is not finite and 64-bit
+// places of every element; 25.8 us, 4.1 TB/s, with what stands below (a copy of 1 GiB reaches 5.1 on this card).  The roots of
+// single elements and the quotient come from the hardware's approximations, one unit of the last place off (correctly
+// rounded ones cost ten operations more each): the
 // parameter feels 2^-23 of its update, and a code does not feel it, since a root taken for just below a code or just
-// above goes to that code with a chance next to 1 from either side.  The root that the scale goes by is exact.
+// above goes to that code with a chance next to 1 from either side.  The scales go by exact comparisons.
 #include "seq_common.hpp"
 
 #include <math.h>
@@ -47,86 +49,74 @@ __host__ __device__ __forceinline__ uint32_t stir(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-template <int L> __device__ __forceinline__ float max_neighbours(float v) {
-  v = fmaxf(v, dpp<0xB1>(v));
-  v = fmaxf(v, dpp<0x4E>(v));
-  v = fmaxf(v, dpp<0x141>(v));
-  v = fmaxf(v, dpp<0x140>(v));
-  if constexpr (L == 32) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
-    v = fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
-  }
-  return v;
+// Largest value over 32 neighbouring lanes, in all of them.  (Magnitudes are compared by their bits: integers need none of
+// the care that a floating maximum takes over NaN.)
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_bits(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+__device__ __forceinline__ uint32_t max_of_32(uint32_t v) {
+  v = max(v, dpp_bits<0xB1>(v));
+  v = max(v, dpp_bits<0x4E>(v));
+  v = max(v, dpp_bits<0x141>(v));
+  v = max(v, dpp_bits<0x140>(v));
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max((uint32_t)r[0], (uint32_t)r[1]);
 }
 
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// Exponent of the least power of two s with top <= 448 s = 1.75 * 2^8 s, from -60 up: the mantissa's bits above 1.75
-// carry into the exponent.
-__device__ __forceinline__ int scale_exponent(float top) { return max(-60, (int)((__float_as_uint(top) + 0x1FFFFFu) >> 23) - 127 - 8); }
+// Exponents of the least powers of two s with top <= 448 s = 1.75 * 2^8 s, and with sqrt(top) <= 448 s, from -60 up.  For
+// the first the mantissa's bits above 1.75 carry into the exponent; for the second those above 1.75^2 = 2 * 1.53125 in the
+// pair of binades that starts at an even power (the root's rounding does not reach over the next number above that).
+__device__ __forceinline__ int scale_exponent(uint32_t top) { return max(-60, (int)((top + 0x1FFFFFu) >> 23) - 127 - 8); }
+__device__ __forceinline__ int scale_exponent_of_root(uint32_t top) { return max(-60, ((int)(top - (127u << 23) + 0x3BFFFFu) >> 24) - 8); }
 
-// The 8-bit code below or above the magnitude r >= 0 (in units of the scale): `low` steps of 2^(e-3) in the binade
-// of exponent e, from -6 up; below that the steps stay, as subnormal numbers.
-struct Grid {
-  int e;
-  float low;
-};
-__device__ __forceinline__ Grid grid_of(float r, float *frac) {
-#pragma clang fp contract(off)
-  Grid g;
-  g.e = max(-6, (int)(__float_as_uint(r) >> 23) - 127);
-  const float a = r * power2(3 - g.e);
-  g.low = floorf(a);
-  *frac = a - g.low;
-  return g;
-}
-__device__ __forceinline__ uint32_t code_of(const Grid &g, bool up) { return (uint32_t)((g.e + 6) * 8 + (int)g.low + (up ? 1 : 0)); }
+// Codes of magnitudes in units of the scale, up to 448: binades of eight codes from 2^-6 (code 8) on, below that the
+// eight codes of the subnormal numbers, 2^-9 apart.  What lies between two codes goes up where (k + 1/2) / 65536, k being
+// 16 random bits, is below a chance.  Nothing here branches: a choice of two costs less than taking turns.
 
+// The first moment, by the share of the way to the next code.  20 bits of an fp32 mantissa lie below a code's, so the
+// carry out of them is the rounding: 16 (65535 - k) + 7 on top of them carries exactly where the share exceeds the
+// chance.  A subnormal magnitude gets 2^-6 added, which puts it on the codes of the first binade, eight codes up.
 __device__ __forceinline__ uint32_t code_m(float m, float inverse, uint32_t rand) {
 #pragma clang fp contract(off)
-  if (!finite(m)) return 0x7Fu;
-  const float y = m * inverse;
-  float frac;
-  const Grid g = grid_of(fabsf(y), &frac);
-  const float chance = ((float)(rand & 0xFFFFu) + 0.5f) * (1.f / 65536.f);
-  return code_of(g, chance < frac) | (y < 0.f ? 0x80u : 0u);
+  const float y = fabsf(m) * inverse;
+  const bool low = y < 0x1p-6f;
+  const uint32_t t = __float_as_uint(low ? y + 0x1p-6f : y) + ((rand << 4 & 0xFFFF0u) ^ 0xFFFF7u);
+  return ((t >> 20) - (low ? 968u : 960u)) | (__float_as_uint(m) >> 24 & 0x80u);
 }
-// The root of v is coded; up with the chance that keeps the mean of v itself, (w - lo^2) / (hi^2 - lo^2).
-__device__ __forceinline__ uint32_t code_v(float v, float root, float inverse, uint32_t rand) {
+// The second moment: its root is coded, a = low + f in steps of the root's binade; up with the chance that keeps the mean
+// of v itself, (a^2 - low^2) / (2 low + 1).  Scaling by powers of two is exact; a^2 comes from v, not from the root.
+__device__ __forceinline__ uint32_t code_v(float v, float root, int exponent, uint32_t rand) {
 #pragma clang fp contract(off)
-  if (!finite(v)) return 0x7Fu;
-  const float w = (v * inverse) * inverse;
-  float frac;
-  const Grid g = grid_of(root * inverse, &frac);
-  const float step = power2(g.e - 3), lo = g.low * step, hi = (g.low + 1.f) * step;
+  const int e = max(-6, (int)(__float_as_uint(root) >> 23) - 127 - exponent);
+  const float steps = power2(3 - e - exponent), low = floorf(root * steps), square = (v * steps) * steps;
   const float chance = ((float)(rand >> 16) + 0.5f) * (1.f / 65536.f);
-  const float lo2 = lo * lo, hi2 = hi * hi;
-  const bool up = chance * (hi2 - lo2) < w - lo2 || (w > 0.f && g.e == -6 && g.low == 0.f);
-  return code_of(g, up);
+  const bool up = chance * fmaf(2.f, low, 1.f) < fmaf(-low, low, square);
+  const uint32_t code = (uint32_t)((e + 6) * 8 + (int)low + (up ? 1 : 0));
+  return max(code, v > 0.f ? 1u : 0u);
 }
 
-// Four elements from i on, of n; zeros beyond.
-template <typename T> __device__ __forceinline__ void take4(float r[4], const T *p, int64_t i, int64_t n, bool vec) {
-  if (vec && i + 4 <= n) {
-    const Pack<T, 4> q = *(const Pack<T, 4> *)(p + i);
+// Four elements from k on, of `left`; zeros beyond.
+template <typename T> __device__ __forceinline__ void take4(float r[4], const T *p, int k, int left, bool vec) {
+  if (vec && k + 4 <= left) {
+    const Pack<T, 4> q = *(const Pack<T, 4> *)(p + k);
 #pragma unroll
     for (int j = 0; j < 4; ++j) r[j] = widen(q.v[j]);
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r[j] = i + j < n ? widen(p[i + j]) : 0.f;
+    for (int j = 0; j < 4; ++j) r[j] = k + j < left ? widen(p[k + j]) : 0.f;
   }
 }
-template <typename T> __device__ __forceinline__ void give4(T *p, const float r[4], int64_t i, int64_t n, bool vec) {
-  if (vec && i + 4 <= n) {
+template <typename T> __device__ __forceinline__ void give4(T *p, const float r[4], int k, int left, bool vec) {
+  if (vec && k + 4 <= left) {
     Pack<T, 4> q;
 #pragma unroll
     for (int j = 0; j < 4; ++j) q.v[j] = narrow<T>(r[j]);
-    *(Pack<T, 4> *)(p + i) = q;
+    *(Pack<T, 4> *)(p + k) = q;
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (i + j < n) p[i + j] = narrow<T>(r[j]);
+      if (k + j < left) p[k + j] = narrow<T>(r[j]);
   }
 }
 
@@ -138,32 +128,38 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamP p) {
     const int mid = (lo + hi) >> 1;
     if ((int)blockIdx.x >= p.first[mid]) lo = mid; else hi = mid;
   }
-  const int64_t n = p.n[lo], at = p.at[lo];
-  float *param = p.param[lo];
-  const G *grad = (const G *)p.grad[lo];
+  // the workgroup's chunk of the tensor and of the moments, and this thread's place in it
+  const int64_t base = (int64_t)((int)blockIdx.x - p.first[lo]) * CHUNK, at = p.at[lo] + base;
+  const int left = (int)min(p.n[lo] - base, (int64_t)CHUNK), k = threadIdx.x * 4;
+  float *param = p.param[lo] + base;
+  const G *grad = (const G *)p.grad[lo] + base;
   __bf16 *copy = p.copy[lo];
   const float keep = p.keep[lo];
   const bool vp = ((uintptr_t)param & 15) == 0, vg = ((uintptr_t)grad & (4 * sizeof(G) - 1)) == 0, vc = ((uintptr_t)copy & 7) == 0;
-  const int64_t i = (int64_t)(blockIdx.x - p.first[lo]) * CHUNK + threadIdx.x * 4;
 
   float w[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f}, m[4], v[4], root[4];
   if constexpr (BITS == 32) {
-    if (i >= n) return;
-    take4(w, (const float *)param, i, n, vp);
-    take4(g, grad, i, n, vg);
-    take4(m, (const float *)p.m + at, i, n, true);         // (at: a multiple of SNN_ADAMW_BLOCK)
-    take4(v, (const float *)p.v + at, i, n, true);
+    if (k >= left) return;
+    take4(w, (const float *)param, k, left, vp);
+    take4(g, grad, k, left, vg);
+    take4(m, (const float *)p.m + at, k, left, true);      // (at: a multiple of SNN_ADAMW_BLOCK)
+    take4(v, (const float *)p.v + at, k, left, true);
   } else {
     // a lane beyond the tensor has no element of the block and only takes part in its maxima
     uint32_t cm = 0, cv = 0;
     float sm = 1.f, sv = 1.f;
-    if (i < n) {
-      take4(w, (const float *)param, i, n, vp);
-      take4(g, grad, i, n, vg);
-      cm = *(const uint32_t *)((const uint8_t *)p.m + at + i);
-      cv = *(const uint32_t *)((const uint8_t *)p.v + at + i);
-      sm = p.m_scale[(at + i) / SNN_ADAMW_BLOCK];
-      sv = p.v_scale[(at + i) / SNN_ADAMW_BLOCK];
+    if (k < left) {
+      take4(w, (const float *)param, k, left, vp);
+      take4(g, grad, k, left, vg);
+      cm = *(const uint32_t *)((const uint8_t *)p.m + at + k);
+      cv = *(const uint32_t *)((const uint8_t *)p.v + at + k);
+      sm = (p.m_scale + at / SNN_ADAMW_BLOCK)[k / SNN_ADAMW_BLOCK];
+      sv = (p.v_scale + at / SNN_ADAMW_BLOCK)[k / SNN_ADAMW_BLOCK];
+      if (k + 4 > left) {                                  // what is behind the last element counts as zero
+        const uint32_t own = (1u << 8 * (left - k)) - 1;
+        cm &= own;
+        cv &= own;
+      }
     }
     m[0] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 0); m[1] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 1);
     m[2] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 2); m[3] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 3);
@@ -191,37 +187,42 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamP p) {
   }
   if constexpr (BITS == 8) {
     // 32 lanes hold a block: its largest finite magnitudes give the scales
-    float tm = 0.f, tv = 0.f;
+    uint32_t tm = 0, tv = 0, nan_m = 0, nan_v = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (i + j >= n) { m[j] = 0.f; v[j] = 0.f; root[j] = 0.f; }
-      tm = fmaxf(tm, finite(m[j]) ? fabsf(m[j]) : 0.f);
-      tv = fmaxf(tv, finite(v[j]) ? v[j] : 0.f);
+      const bool fm = finite(m[j]), fv = finite(v[j]);
+      nan_m |= fm ? 0u : 0x7Fu << 8 * j;                   // (what is not finite is coded as zero, and then made NaN)
+      nan_v |= fv ? 0u : 0x7Fu << 8 * j;
+      m[j] = fm ? m[j] : 0.f;
+      v[j] = fv ? v[j] : 0.f;
+      root[j] = fv ? root[j] : 0.f;
+      tm = max(tm, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+      tv = max(tv, __float_as_uint(v[j]));
     }
-    const int em = scale_exponent(max_neighbours<32>(tm)), ev = scale_exponent(sqrtf(max_neighbours<32>(tv)));
-    const float im = power2(-em), iv = power2(-ev);
-    uint32_t qm = 0, qv = 0;
-    const int64_t where = at + i;                          // (a multiple of four)
-    const uint32_t first = (uint32_t)where * 0x9E3779B1u + (uint32_t)(where >> 32) * 0xC2B2AE3Du + p.salt;
+    const int em = scale_exponent(max_of_32(tm)), ev = scale_exponent_of_root(max_of_32(tv));
+    const float im = power2(-em);
+    uint32_t qm = nan_m, qv = nan_v;
+    const uint32_t low = (uint32_t)at + (uint32_t)k, high = (uint32_t)(at >> 32) + (low < (uint32_t)at ? 1u : 0u);
+    const uint32_t first = low * 0x9E3779B1u + high * 0xC2B2AE3Du + p.salt;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t rand = stir(first + j * 0x9E3779B1u);
       qm |= code_m(m[j], im, rand) << (8 * j);
-      qv |= code_v(v[j], root[j], iv, rand) << (8 * j);
+      qv |= code_v(v[j], root[j], ev, rand) << (8 * j);
     }
-    if (i >= n) return;
-    *(uint32_t *)((uint8_t *)p.m + where) = qm;
-    *(uint32_t *)((uint8_t *)p.v + where) = qv;
+    if (k >= left) return;
+    *(uint32_t *)((uint8_t *)p.m + at + k) = qm;
+    *(uint32_t *)((uint8_t *)p.v + at + k) = qv;
     if ((threadIdx.x & 31) == 0) {
-      p.m_scale[where / SNN_ADAMW_BLOCK] = power2(em);
-      p.v_scale[where / SNN_ADAMW_BLOCK] = power2(ev);
+      (p.m_scale + at / SNN_ADAMW_BLOCK)[k / SNN_ADAMW_BLOCK] = power2(em);
+      (p.v_scale + at / SNN_ADAMW_BLOCK)[k / SNN_ADAMW_BLOCK] = power2(ev);
     }
   } else {
-    give4((float *)p.m + at, m, i, n, true);
-    give4((float *)p.v + at, v, i, n, true);
+    give4((float *)p.m + at, m, k, left, true);
+    give4((float *)p.v + at, v, k, left, true);
   }
-  give4(param, w, i, n, vp);
-  if (copy) give4(copy, w, i, n, vc);
+  give4(param, w, k, left, vp);
+  if (copy) give4(copy + base, w, k, left, vc);
 }
 
 }  // namespace
