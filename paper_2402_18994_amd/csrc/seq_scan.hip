@@ -833,16 +833,18 @@ int scan_strides(const snn_scan_args *a, const snn_rows *rows, int count) {
   return SNN_OK;
 }
 
-// How time is cut: into chunks of at least 64 steps for 4096 wavefronts, four to a SIMD, where there are few; not at
-// all where there are 1024 (forward, which does a chunk twice but for the outputs) or 1536 (reverse, which does half of
-// the work twice).  16 states, one cut for 4096 wavefronts against none, us: forward, 512 wavefronts (1024 steps of
+// How time is cut: into chunks of at least 48 steps for 4096 wavefronts, four to a SIMD, where there are few; not at
+// all below 128 steps, or where there are 1024 wavefronts (forward, which does a chunk twice but for the outputs) or 1536
+// (reverse, which does half of the work twice).  16 states, one cut for 4096 wavefronts against none, us: forward, 512 wavefronts (1024 steps of
 // 4 x 2048 channels) 70 and 100; 1024 wavefronts 119 and 116; forward and reverse, 512 wavefronts 240 and 324, 1024
-// wavefronts 417 and 445, 1536 wavefronts 331 and 332.  Cut for 2048 wavefronts, the case of 512 takes 75 and 253.
+// wavefronts 417 and 445, 1536 wavefronts 331 and 332.  Cut for 2048 wavefronts, the case of 512 takes 75 and 253.  Chunks of at
+// least 32, 48 and 64 steps, forward and reverse: 500 steps of 2 x 512 channels 69, 65 and 73; 200 steps of 4 x 1024 67,
+// 66 and 74; 100 steps of 8 x 512 67, 64 and 61, the last of which is not cut.
 void scan_cut(const snn_scan_args &a, const Shape &k, bool backward, int *chunk, int *nchunks) {
   const int64_t waves = (int64_t)a.B * a.groups * blocks_of(a, k) * k.waves, enough = backward ? 1536 : 1024;
   int64_t n = waves < enough ? 4096 / waves : 1;
-  if (n > a.T / 64) n = a.T / 64;
-  if (n < 1) n = 1;
+  if (n > a.T / 48) n = a.T / 48;
+  if (n < 1 || a.T < 128) n = 1;
   const int64_t tiles = ((int64_t)a.T + TILE - 1) / TILE;
   const int64_t each = tiles ? (tiles + n - 1) / n : 1;
   *chunk = (int)(each * TILE);
