@@ -154,7 +154,8 @@ typedef struct {
   double grad_scale;         /* gradients are multiplied by it first */
 } snn_adamw_args;
 
-/* `tensors`: host array; read before the call returns.  A tensor with n = 0 is passed over. */
+/* `tensors`: host array; read before the call returns.  A tensor with n = 0 is passed over.  A call captured into a graph
+ * is replayed with the step number and the rates that it was captured with. */
 int32_t snn_adamw_step(const snn_adamw_args *a, const snn_adamw_tensor *tensors, int32_t count, void *hip_stream);
 
 /* The same for a network of snn.h, in the place of snn_sgd_step: every W and R, and the decays where they are trained

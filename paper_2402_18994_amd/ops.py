@@ -418,7 +418,8 @@ class AdamW:
         self._table[:, 0] = self._addresses
 
     def step(self, grads: Sequence, lr: Optional[float] = None, grad_scale: float = 1.0) -> None:
-        """One step with these gradients (dense, all float32 or all bfloat16, multiplied by `grad_scale` first)."""
+        """One step with these gradients (dense, all float32 or all bfloat16, multiplied by `grad_scale` first).  Captured
+        into a graph it is replayed with the step number and learning rate of the capture."""
         # (checks run over all tensors at C speed: with many small tensors they are what a step costs)
         tensor, params, dev = torch.Tensor, self.params, self.device.index
         if list(map(_SHAPE, grads)) != self._shapes or not all(map(tensor.is_contiguous, grads)):
