@@ -540,3 +540,82 @@ def test_states_that_forget_at_once(T):
     _, end = oracle.scan(**(s | {k: s[k][:1] for k in ("x", "dt", "z", "Bv", "Cv")}))
     exists = [b for b in range(3) if int(n[b])]
     close("stepped", state[exists], end[exists], 1, 2.0 ** -24)
+
+
+def room(T, growth):
+    """The number of steps for `close` at which its tolerance also covers a state that grows by e^growth: the exponent is a sum
+    of up to 64 step sizes (each addition half a step off its partial sum, 32 half steps of the whole at most) times a rate,
+    with the roundings of rate, product and softplus: 40 half steps, each of which counts `growth` times."""
+    return (math.sqrt(T + 16) + 40 * growth / TERM) ** 2 - 16
+
+
+@pytest.mark.parametrize("T,start", [(100, 20), (128, 0), (128, 64), (400, 128), (400, 336)])   # (from 128 on cut in chunks of 64)
+@pytest.mark.parametrize("kind", ["rates above zero", "rates above zero, softplus", "steps below zero"])
+def test_states_that_grow(T, start, kind):
+    """Small states and gradients that grow by more than fp32 can hold as a factor, each of them in range."""
+    from paper_2402_18994_amd import selective_scan, selective_scan_backward
+    gen = torch.Generator().manual_seed(T + start)
+    D, N = 24, 16
+    small = lambda *shape: rounded(1e-30 * rand(gen, *shape))
+    step = torch.full((T, 1, D), 1e-3, dtype=torch.float64)
+    step[start:start + 64] = 95 / 64
+    step = step * (1 + 0.02 * torch.rand(T, 1, D, generator=gen, dtype=torch.float64))
+    A = 0.97 + 0.03 * torch.rand(D, N, generator=gen, dtype=torch.float64)
+    softplus = kind.endswith("softplus")
+    if kind == "steps below zero":
+        step, A = -step, -A
+    s = {"x": small(T, 1, D), "dt": rounded(torch.log(torch.expm1(step)) if softplus else step), "A": rounded(A), "Bv": rounded(rand(gen, T, 1, 1, N)),
+         "Cv": rounded(rand(gen, T, 1, 1, N)), "D": rounded(rand(gen, D)), "z": None, "dt_bias": None, "init": small(1, D, N)}
+    dy, ds = small(T, 1, D), small(1, D, N)
+    d, _ = scan_gpu(s, torch.float32, None)
+    out = call(selective_scan, d, softplus=softplus, save=True)
+    wy, ws = oracle.scan(**s, softplus=softplus)
+    f32, steps = 2.0 ** -24, room(T, 97)
+    close("y", out.y, wy, steps, f32)
+    close("state", out.state, ws, steps, f32)
+    g = call(selective_scan_backward, d, on_gpu(dy), out.saved, softplus=softplus, d_state=on_gpu(ds))
+    want = oracle.gradients(lambda **k: oracle.scan(**({x: None for x in s} | k), softplus=softplus), s, (dy, ds))
+    for name, key in (("dx", "x"), ("ddt", "dt"), ("dA", "A"), ("dB", "Bv"), ("dC", "Cv"), ("dD", "D"), ("dinit", "init")):
+        close(name, getattr(g, name), want[key], room(T + D, 97), f32)
+
+
+@pytest.mark.parametrize("T", [100, 160, 400])
+def test_nothing_grows_to_nothing(T):
+    """States and gradients of zero stay zero, whatever the factors of the steps amount to."""
+    from paper_2402_18994_amd import selective_scan, selective_scan_backward
+    gen = torch.Generator().manual_seed(T)
+    D, N = 10, 6
+    s = {"x": rounded(rand(gen, T, 1, D)), "dt": torch.full((T, 1, D), 4.0, dtype=torch.float64), "A": torch.full((D, N), 0.5, dtype=torch.float64),
+         "Bv": rounded(rand(gen, T, 1, 1, N)), "Cv": rounded(rand(gen, T, 1, 1, N)), "D": None, "z": None, "dt_bias": None, "init": None}
+    s["x"][:T - 16] = 0
+    dy = rounded(rand(gen, T, 1, D))
+    dy[16:] = 0
+    d, _ = scan_gpu(s, torch.float32, None)
+    out = call(selective_scan, d, softplus=False, save=True)
+    wy, ws = oracle.scan(**s, softplus=False)
+    f32, steps = 2.0 ** -24, room(T, 32)
+    close("y", out.y, wy, steps, f32)
+    close("state", out.state, ws, steps, f32)
+    g = call(selective_scan_backward, d, on_gpu(dy), out.saved, softplus=False)
+    want = oracle.gradients(lambda **k: oracle.scan(**({x: None for x in s} | k), softplus=False), s, (dy, None))
+    for name, key in (("dx", "x"), ("ddt", "dt"), ("dA", "A"), ("dB", "Bv"), ("dC", "Cv")):
+        close(name, getattr(g, name), want[key], steps, f32)
+
+
+@pytest.mark.parametrize("T", [100, 400])
+def test_states_that_grow_beside_states_that_forget(T):
+    """In one channel a state that grows by e^128 and more over a chunk, one that forgets at once, and one that stays."""
+    from paper_2402_18994_amd import selective_scan
+    gen = torch.Generator().manual_seed(T)
+    D, N = 10, 3
+    s = {"x": rounded(rand(gen, T, 1, D)), "dt": torch.full((T, 1, D), 4.0, dtype=torch.float64), "A": torch.tensor([[0.5, -1e30, -1e-3]] * D, dtype=torch.float64),
+         "Bv": rounded(rand(gen, T, 1, 1, N)), "Cv": rounded(rand(gen, T, 1, 1, N)), "D": None, "z": None, "dt_bias": None, "init": rounded(rand(gen, 1, D, N))}
+    s["Bv"][:T - 16, ..., 0] = 0                           # (the state that grows starts from zero, late)
+    s["init"][..., 0] = 0
+    s["A"] = rounded(s["A"])
+    wy, ws = oracle.scan(**s, softplus=False)
+    d, _ = scan_gpu(s | {"A": torch.where(s["A"] < -1, float("-inf"), s["A"])}, torch.float32, None)
+    out = call(selective_scan, d, softplus=False)
+    for n in range(N):                                     # every state on its own scale
+        close(f"state {n}", out.state[..., n], ws[..., n], room(T, 32), 2.0 ** -24)
+    close("y", out.y, wy, room(T, 32), 2.0 ** -24)
