@@ -619,3 +619,33 @@ def test_states_that_grow_beside_states_that_forget(T):
     for n in range(N):                                     # every state on its own scale
         close(f"state {n}", out.state[..., n], ws[..., n], room(T, 32), 2.0 ** -24)
     close("y", out.y, wy, room(T, 32), 2.0 ** -24)
+
+
+def test_an_absent_skip_is_not_multiplied():
+    """Without D an infinity is not multiplied by zero: what the definition makes infinite is infinite, in a whole call as in
+    single steps, and so are the gradients that the skip would enter."""
+    from paper_2402_18994_amd import selective_scan, selective_scan_backward, selective_scan_step
+    T, D, N = 20, 40, 8                                    # (as many states as lanes hold)
+    inf = float("inf")
+    for t in TYPES.values():
+        gen = torch.Generator().manual_seed(8)
+        pos = lambda *shape: (0.5 + torch.rand(*shape, generator=gen)).to(t).cuda()
+        x, dt, z, dy, B, Cv = pos(T, 1, D), pos(T, 1, D), pos(T, 1, D), pos(T, 1, D), pos(T, 1, N), pos(T, 1, N)
+        A = -0.1 * (0.5 + torch.rand(D, N, generator=gen)).cuda()
+        for bad in (inf, -inf):
+            hit = x.clone()
+            hit[5, 0, 33] = bad
+            for gate in (None, z):
+                out = selective_scan(hit, dt, A, B, Cv, z=gate, save=True)
+                assert (out.y[5:, 0, 33] == bad).all() and torch.isfinite(out.y[:5]).all() and torch.isfinite(out.y[..., :33]).all()
+                state = torch.zeros(1, D, N, device="cuda")
+                for k in range(T):
+                    one = selective_scan_step(hit[k], dt[k], state, A, B[k], Cv[k], z=gate[k] if gate is not None else None)
+                    assert k < 5 or one[0, 33] == bad
+            g = selective_scan_backward(dy, out.saved, hit, dt, A, B, Cv, z=z)
+            assert (g.dz[5:, 0, 33] == bad).all() and torch.isfinite(g.dz[:5]).all() and torch.isfinite(g.dx).all()
+            far = dy.clone()
+            far[7, 0, 21] = bad
+            clean = selective_scan(x, dt, A, B, Cv, save=True)
+            g = selective_scan_backward(far, clean.saved, x, dt, A, B, Cv)
+            assert (g.dx[:8, 0, 21] == bad).all() and torch.isfinite(g.dx[8:]).all() and torch.isfinite(g.dx[..., :21]).all()
