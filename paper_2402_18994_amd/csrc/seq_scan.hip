@@ -114,7 +114,10 @@ __device__ __forceinline__ float decay_rate(float A) {
   const float r = A * LOG2E;
   return r < -3.4028234663852886e38f ? -3.4028234663852886e38f : r;
 }
-// The same out of rows of the library's own, which are padded and aligned.
+// The rate itself where the reverse pass multiplies by it: what a state that forgets at once hands back through its decay is zero, and
+// zero times the lowest finite number still is.
+__device__ __forceinline__ float finite_rate(float A) { return A < -3.4028234663852886e38f ? -3.4028234663852886e38f : A; }
+// A lane's states out of rows of the library's own, which are padded and aligned.
 template <int NS> using States = Pack<float, NS>;
 template <int NS> __device__ __forceinline__ States<NS> pick(const float *p) { return *(const States<NS> *)p; }
 template <int NS> __device__ __forceinline__ void put_states(float *p, const float r[NS]) {
@@ -464,7 +467,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
   float A[NS], A2[NS], q[NS], dA[NS];
   load_states<NS>(A, p.A + (size_t)me.d * p.N, me.part, p.N, me.live);
 #pragma unroll
-  for (int j = 0; j < NS; ++j) { A2[j] = decay_rate(A[j]); dA[j] = 0.f; }
+  for (int j = 0; j < NS; ++j) { A2[j] = decay_rate(A[j]); A[j] = finite_rate(A[j]); dA[j] = 0.f; }
   if (p.nchunks > 1) {
     const States<NS> v = pick<NS>(p.local + ((size_t)me.s * p.B * p.D + seq) * NP + me.part * NS);
 #pragma unroll

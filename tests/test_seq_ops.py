@@ -649,3 +649,26 @@ def test_an_absent_skip_is_not_multiplied():
             clean = selective_scan(x, dt, A, B, Cv, save=True)
             g = selective_scan_backward(far, clean.saved, x, dt, A, B, Cv)
             assert (g.dx[:8, 0, 21] == bad).all() and torch.isfinite(g.dx[8:]).all() and torch.isfinite(g.dx[..., :21]).all()
+
+
+@pytest.mark.parametrize("T", [40, 300])                   # (300: cut in chunks of time)
+@pytest.mark.parametrize("gate", [False, True])
+def test_gradients_of_states_that_forget_at_once(T, gate):
+    """A = -inf: the gradients are the limits for ever faster decays.  The definition's own are taken at A = -1e30, where
+    exp(delta A) is zero in 64 bits too, and every product with it."""
+    from paper_2402_18994_amd import selective_scan, selective_scan_backward
+    gen, t, s, n = scan_case(T, 3, 20, 6, 1, "fp32", gate, True, "some", True)
+    n[1] = T - 37
+    s["A"][:, 2] = float("-inf")
+    d, gn = scan_gpu(s, t, n)
+    s["A"][:, 2] = -1e30
+    out = call(selective_scan, d, lengths=gn, save=True)
+    dy, ds = rounded(rand(gen, T, 3, 20)), rounded(rand(gen, 3, 20, 6))
+    g = call(selective_scan_backward, d, on_gpu(dy), out.saved, lengths=gn, d_state=on_gpu(ds))
+    want = oracle.gradients(lambda **k: oracle.scan(**({x: None for x in s} | k), lengths=n), s, (dy, ds))
+    f32 = 2.0 ** -24
+    for name, key, total in (("dx", "x", T), ("ddt", "dt", T), ("dB", "Bv", T + 20), ("dC", "Cv", T + 20), ("dA", "A", T * 3), ("dD", "D", T * 3),
+                             ("dz", "z", T), ("ddt_bias", "dt_bias", T * 3), ("dinit", "init", T)):
+        if s[key] is not None:
+            close(name, getattr(g, name), want[key], total, f32)
+    assert (g.dA[:, 2] == 0).all()
