@@ -594,6 +594,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
       }
       const float4 u = ur[t % 2];
       float v[2 * NS], gsum = 0.f, usum = 0.f, hp[NS];
+      const bool exists = t0 + t < end;                     // (else delta is 0, but the state may be infinite: dA would be NaN)
 #pragma unroll
       for (int j = 0; j < NS; ++j) {
         if (t == TILE - 1) hc[j] = h[HALF][j];
@@ -608,7 +609,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_reverse_kernel(const ScanP
         const float w = q[j] * hp[j];
         hc[j] = hp[j];
         usum = fmaf(w, A[j], usum);
-        dA[j] = fmaf(w, u.x, dA[j]);
+        dA[j] = fmaf(exists ? w : 0.f, u.x, dA[j]);
       }
       gsum = sum_neighbours<L>(gsum);
       usum = sum_neighbours<L>(usum);

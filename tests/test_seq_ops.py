@@ -672,3 +672,22 @@ def test_gradients_of_states_that_forget_at_once(T, gate):
         if s[key] is not None:
             close(name, getattr(g, name), want[key], total, f32)
     assert (g.dA[:, 2] == 0).all()
+
+
+@pytest.mark.parametrize("T,end", [(40, 37), (300, 290)])  # (300: cut in chunks of time)
+def test_an_infinite_last_state_does_not_reach_the_decays(T, end):
+    """x = inf at a sequence's last step makes its last state infinite, which no step that exists starts from: dA is that of
+    the steps that exist, though the tile goes on behind them."""
+    from paper_2402_18994_amd import selective_scan, selective_scan_backward
+    gen, t, s, _ = scan_case(T, 1, 20, 8, 1, "fp32", False, True, "none", False)
+    s["x"][end - 1, 0, 7] = float("inf")
+    n = torch.tensor([end], dtype=torch.int32)
+    d, gn = scan_gpu(s, t, n)
+    out = call(selective_scan, d, lengths=gn, save=True)
+    dy, ds = rounded(rand(gen, T, 1, 20)), rounded(rand(gen, 1, 20, 8))
+    g = call(selective_scan_backward, d, on_gpu(dy), out.saved, lengths=gn, d_state=on_gpu(ds))
+    cut = {k: (v[:end] if k in ("x", "dt", "Bv", "Cv") else v) for k, v in s.items()}
+    want = oracle.gradients(lambda **k: oracle.scan(**({x: None for x in cut} | k)), cut, (dy[:end], ds))
+    close("dA", g.dA, want["A"], T, 2.0 ** -24)
+    close("dinit", g.dinit, want["init"], T, 2.0 ** -24)
+    close("dx", g.dx[:end], want["x"], T, 2.0 ** -24)
