@@ -245,15 +245,18 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvP a, const
             qv *= e * (1.f + r * (1.f - e));
           }
           qv = now < len ? qv : 0.f;
-          const float own = now < t1 ? qv : 0.f;
-          db[v] += own;
           float sum = widen(ds.v[v]);
 #pragma unroll
-          for (int k = 0; k < W; ++k) {
-            dw[k][v] = fmaf(own, xs[u + k][v], dw[k][v]);
-            sum = fmaf(w[k][v], q[W - 1 + u - k][v], sum);
-          }
+          for (int k = 0; k < W; ++k) sum = fmaf(w[k][v], q[W - 1 + u - k][v], sum);
           out.v[v] = narrow<T>(sum);
+        }
+        if (now < min(t1, len)) {                           // (beyond, q may be zero and the inputs infinite: 0 inf is no zero)
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) {
+            db[v] += q[W - 1 + u][v];
+#pragma unroll
+            for (int k = 0; k < W; ++k) dw[k][v] = fmaf(q[W - 1 + u][v], xs[u + k][v], dw[k][v]);
+          }
         }
         const int r = now - (W - 1);
         if (r >= 0) store_row<T, VEC>(dx + r * g.dx.st, (r >= t0) & (now < stop) ? at : NOWHERE, out);

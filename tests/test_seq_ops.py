@@ -691,3 +691,28 @@ def test_an_infinite_last_state_does_not_reach_the_decays(T, end):
     close("dA", g.dA, want["A"], T, 2.0 ** -24)
     close("dinit", g.dinit, want["init"], T, 2.0 ** -24)
     close("dx", g.dx[:end], want["x"], T, 2.0 ** -24)
+
+
+@pytest.mark.parametrize("D", [24, 260])                   # (one channel a lane, and four)
+def test_infinite_inputs_reach_the_taps_that_meet_them(D):
+    """dweight[k] sums dy[t] x[t - (W-1) + k] over the steps that exist: an infinity at a sequence's last step is met by the last
+    tap alone, one before a sequence of no steps by none, and one at the end of a segment makes infinities, not NaN."""
+    from paper_2402_18994_amd import causal_conv_backward
+    T, W = 70, 4
+    gen = torch.Generator().manual_seed(D)
+    x, w, init = rounded(rand(gen, T, 3, D)), rounded(rand(gen, D, W)), rounded(rand(gen, W - 1, 3, D))
+    dy = rounded(0.5 + torch.rand(T, 3, D, generator=gen, dtype=torch.float64))
+    inf = float("inf")
+    n = torch.tensor([50, 0, T], dtype=torch.int32)
+    x[49, 0, 3], init[:, 1, 5], x[31, 2, 9], x[T - 1, 2, 11] = inf, inf, inf, -inf
+    g = causal_conv_backward(on_gpu(dy), on_gpu(x), on_gpu(w), init=on_gpu(init), lengths=on_gpu(n, torch.int32), silu=False)
+    want = torch.zeros(D, W, dtype=torch.float64)
+    for b in range(3):
+        rows = torch.cat((init[:, b], x[:, b]))
+        for k in range(W):
+            want[:, k] += (dy[:int(n[b]), b] * rows[k:k + int(n[b])]).sum(0)
+    got = g.dweight.double().cpu()
+    assert torch.isinf(want[3]).tolist() == [False, False, False, True] and torch.isinf(want[9]).all() and torch.isfinite(want[5]).all()
+    wild = ~torch.isfinite(want)
+    assert torch.equal(got[wild], want[wild])
+    close("dweight", torch.where(wild, 0.0, got), torch.where(wild, 0.0, want), T * 3, 2.0 ** -24)
