@@ -408,14 +408,13 @@ class AdamW:
         self._bind()
 
     def _bind(self):
-        """Takes the parameters' memory as it is now.  The optimiser holds on to that memory (`_held`), so as long as a
-        parameter's address is the one noted here, what lies there is the memory that was looked at here."""
+        """Takes the parameters' memory as it is now.  The optimiser holds on to that memory and to how it is seen (`_held`:
+        storage, offset, sizes, strides); a parameter that is still set to that, and of that type, need not be looked at again."""
         for p, shape in zip(self.params, self._shapes):
             if p.shape != shape or p.dtype != torch.float32 or p.device != self.device or not p.is_contiguous():
                 _refuse("a parameter is not what it was when the optimiser was made")
         self._held = [p.detach() for p in self.params]
-        self._addresses = [p.data_ptr() for p in self._held]
-        self._table[:, 0] = self._addresses
+        self._table[:, 0] = [p.data_ptr() for p in self._held]
 
     def step(self, grads: Sequence, lr: Optional[float] = None, grad_scale: float = 1.0) -> None:
         """One step with these gradients (dense, all float32 or all bfloat16, multiplied by `grad_scale` first).  Captured
@@ -427,7 +426,7 @@ class AdamW:
         kind = set(map(_DTYPE, grads))
         if len(kind) != 1 or not kind <= _types.keys() or set(map(tensor.get_device, grads)) != {dev}:
             _refuse("gradients have to be all float32 or all bfloat16, on the parameters' device")
-        if list(map(tensor.data_ptr, params)) != self._addresses:
+        if not all(map(tensor.is_set_to, params, self._held)) or set(map(_DTYPE, params)) != {torch.float32}:
             self._bind()
         t = self._table
         t[:, 1] = list(map(tensor.data_ptr, grads))

@@ -317,3 +317,25 @@ def test_parameters_that_move():
         p[0].data = wrong
         with pytest.raises(SnnError):
             a.step(g)
+
+
+def test_a_parameter_that_becomes_its_own_transpose_is_refused():
+    """The same memory, the same shape, another order: an update there would go to the wrong places."""
+    from paper_2402_18994_amd import AdamW, SnnError
+    p = [torch.nn.Parameter(torch.randn(6, 6, device="cuda")), torch.randn(40, device="cuda")]
+    g = [torch.randn_like(x) for x in p]
+    opt = AdamW(p)
+    opt.step(g)
+    old = p[0].data
+    before = old.clone()
+    p[0].data = old.t()
+    assert p[0].data_ptr() == old.data_ptr() and p[0].shape == old.shape
+    with pytest.raises(SnnError):
+        opt.step(g)
+    assert torch.equal(old, before) and opt.steps == 1
+    p[0].data = old
+    opt.step(g)
+    assert opt.steps == 2
+    p[1].data = p[1].data.view(torch.int32)                # other numbers in the same memory
+    with pytest.raises(SnnError):
+        opt.step(g)
