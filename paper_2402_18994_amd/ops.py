@@ -382,12 +382,10 @@ class AdamW:
         self.device = dev = self.params[0].device
         _need(dev.type == "cuda", "parameters have to be on a HIP device")
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(self.params)
-        self.copies = list(copies) if copies is not None else [None] * len(self.params)
-        _need(len(decay) == len(self.params) and len(self.copies) == len(self.params), "weight_decay and copies go with the parameters", ERR_SHAPE)
-        for p, c in zip(self.params, self.copies):
+        self.copies = copies if copies is not None else [None] * len(self.params)
+        _need(len(decay) == len(self.params), "weight_decay goes with the parameters", ERR_SHAPE)
+        for p in self.params:
             _need(p.dtype == torch.float32 and p.device == dev and p.is_contiguous(), "parameters have to be dense, float32, on one device")
-            _need(c is None or (c.dtype == torch.bfloat16 and c.device == dev and c.is_contiguous() and c.shape == p.shape),
-                  "copies have to be dense, bfloat16, of their parameters' shapes")
         self.lr, self.betas, self.eps, self.bits, self.seed, self.steps = float(lr), (float(betas[0]), float(betas[1])), float(eps), state_bits, int(seed), 0
         self.at, n = [], 0
         for p in self.params:
@@ -400,12 +398,12 @@ class AdamW:
         if state_bits == 8:
             self.m_scale, self.v_scale = (torch.ones(n // BLOCK, device=dev) for _ in range(2))
         self._shapes = [p.shape for p in self.params]
-        self._copied = [i for i, c in enumerate(self.copies) if c is not None]
         # snn_adamw_tensor, one a row; the gradients' addresses are filled in by every step
         self._table = np.zeros((len(self.params), 6), np.int64)
         self._table[:, 3], self._table[:, 4] = [p.numel() for p in self.params], self.at
         self._table[:, 5] = np.array(decay, np.float64).view(np.int64)
         self._bind()
+        self._bind_copies()
 
     def _bind(self):
         """Takes the parameters' memory as it is now.  The optimiser holds on to that memory and to how it is seen (`_held`:
@@ -415,6 +413,18 @@ class AdamW:
                 _refuse("a parameter is not what it was when the optimiser was made")
         self._held = [p.detach() for p in self.params]
         self._table[:, 0] = [p.data_ptr() for p in self._held]
+
+    def _bind_copies(self):
+        """The same for the copies, whose list is a tuple from here on: one that is put in its place is seen."""
+        copies = tuple(self.copies)
+        _need(len(copies) == len(self.params), "copies go with the parameters", ERR_SHAPE)
+        for c, shape in zip(copies, self._shapes):
+            if c is not None and (c.shape != shape or c.dtype != torch.bfloat16 or c.device != self.device or not c.is_contiguous()):
+                _refuse("copies have to be dense, bfloat16, of their parameters' shapes, on their device", ERR_SHAPE)
+        self.copies = self._seen = copies
+        self._copied = [c for c in copies if c is not None]
+        self._held_copies = [c.detach() for c in self._copied]
+        self._table[:, 2] = [0 if c is None else c.data_ptr() for c in copies]
 
     def step(self, grads: Sequence, lr: Optional[float] = None, grad_scale: float = 1.0) -> None:
         """One step with these gradients (dense, all float32 or all bfloat16, multiplied by `grad_scale` first).  Captured
@@ -428,10 +438,11 @@ class AdamW:
             _refuse("gradients have to be all float32 or all bfloat16, on the parameters' device")
         if not all(map(tensor.is_set_to, params, self._held)) or set(map(_DTYPE, params)) != {torch.float32}:
             self._bind()
+        copies = self._copied
+        if self.copies is not self._seen or not all(map(tensor.is_set_to, copies, self._held_copies)) or not set(map(_DTYPE, copies)) <= {torch.bfloat16}:
+            self._bind_copies()
         t = self._table
         t[:, 1] = list(map(tensor.data_ptr, grads))
-        for i in self._copied:
-            t[i, 2] = self.copies[i].data_ptr()
         scales = (self.m_scale.data_ptr(), self.v_scale.data_ptr()) if self.bits == 8 else (0, 0)
         a = _ADAM.pack(self.bits, _types[kind.pop()], self.m.data_ptr(), self.v.data_ptr(), *scales, self.steps + 1, self.seed & 0xFFFFFFFF,
                        self.lr if lr is None else float(lr), *self.betas, self.eps, float(grad_scale))
