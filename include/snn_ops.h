@@ -127,7 +127,8 @@ int32_t snn_scan_step(const snn_scan_args *a, void *hip_stream);
 #define SNN_ADAMW_BLOCK 128        /* elements of an 8-bit moment that share a scale */
 
 /* One tensor.  Its moments are elements [at, at + n) of the call's moment buffers; `at` is a multiple of
- * SNN_ADAMW_BLOCK and the blocks of two tensors do not overlap. */
+ * SNN_ADAMW_BLOCK.  The blocks of two tensors do not overlap, nor does the memory of the parameters and copies: a call where
+ * they do (a tensor given twice, say) is refused with SNN_ERR_ARG. */
 typedef struct {
   float *param;              /* device, fp32, updated */
   const void *grad;          /* device, of the call's grad_type */

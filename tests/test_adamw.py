@@ -383,3 +383,19 @@ def test_copies_that_move():
     opt.step(g)
     assert torch.equal(opt.copies[1], p[1].to(torch.bfloat16)) and torch.equal(c[2], p[2].to(torch.bfloat16))
     assert torch.equal(small, before[0].to(torch.bfloat16))
+
+
+def test_tensors_that_share_memory_are_refused():
+    from paper_2402_18994_amd import AdamW, SnnError
+    store, g = torch.randn(500, device="cuda"), torch.randn(500, device="cuda")
+    copy = torch.zeros(500, device="cuda", dtype=torch.bfloat16)
+    before = store.clone()
+    for cut, copies in (([(0, 300), (0, 300)], None), ([(0, 300), (299, 500)], None), ([(200, 500), (0, 201)], None),
+                        ([(0, 200), (200, 400)], [copy[:200], copy[100:300]])):
+        opt = AdamW([store[i:j] for i, j in cut], copies=copies)
+        with pytest.raises(SnnError) as e:
+            opt.step([g[i:j] for i, j in cut])
+        assert e.value.status == 2 and "share" in str(e.value) and opt.steps == 0
+    assert torch.equal(store, before) and not copy.any()
+    AdamW([store[200:300], store[:200], store[300:]], copies=[copy[200:300], copy[:200], copy[300:]]).step([g[200:300], g[:200], g[300:]])
+    assert torch.equal(copy, store.to(torch.bfloat16)) and not torch.equal(store, before)      # neighbours that touch are fine

@@ -163,3 +163,43 @@ def test_python_entry_points_refuse_before_a_launch(lib):
         ops.AdamW([w])
     with pytest.raises(binding.SnnError):
         ops.AdamW([])
+
+
+def test_adamw_refuses_tensors_that_share_memory(lib):
+    """All tensors are updated at once: the same one twice, or two that overlap, would be a race."""
+    def call(*tensors):
+        a = ops._AdamArgs(8, 0, P, P, P, P, 1, 0, 1e-3, 0.9, 0.999, 1e-8, 1.0)
+        t = (ops._AdamTensor * len(tensors))(*(ops._AdamTensor(**(dict(grad=P, copy=None, weight_decay=0.0) | x)) for x in tensors))
+        return lib.snn_adamw_step(C.byref(a), t, len(tensors), None), lib.snn_last_error(None)
+
+    far = [dict(param=P + 4096 * i, n=200, at=256 * i) for i in range(600)]      # (more than are looked at without memory of their own)
+    for order in (lambda v: v, lambda v: v[::-1], lambda v: v[1::2] + v[::2]):
+        for extra in (dict(param=P, n=200), dict(param=P + 4096 * 7 + 796, n=1), dict(param=P - 4, n=2), dict(param=P - 4096, n=4096), dict(param=1 << 30, copy=P + 398, n=1),
+                      dict(param=1 << 30, copy=1 << 30, n=4)):
+            for some in (far[:9], far):
+                status, text = call(*order(some + [dict(at=1 << 20) | extra]))
+                assert status == ARG and b"share memory" in text, extra
+        for at in (0, 128, 256 * 8, 256 * 8 + 128):
+            status, text = call(*order(far[:9] + [dict(param=1 << 30, n=129, at=at)]))
+            assert status == ARG and b"share a block" in text, at
+    status, text = call(dict(param=P, copy=1 << 30, n=64, at=0), dict(param=P + 4096, copy=(1 << 30) + 126, n=64, at=128))
+    assert status == ARG and b"share memory" in text
+    assert call(dict(param=P, n=0, at=0), dict(param=P, n=0, at=0))[0] == 0      # nothing in them
+
+
+def test_pieces_that_touch_do_not_overlap(tmp_path):
+    """The host's comparison by itself, on pieces that may not be launched here: neighbours that touch, any order."""
+    text = open(os.path.join(ROOT, "paper_2402_18994_amd", "csrc", "adamw.hip")).read()
+    body = text[text.index("struct Piece {"):text.index("// Workgroups of one launch update all tensors at once")]
+    src = tmp_path / "pieces.cpp"
+    src.write_text("#include <algorithm>\n#include <cstdint>\n#include <cstddef>\n" + body + """
+int main() {
+  Piece touch[] = {{512, 768}, {0, 256}, {256, 512}, {768, 769}};
+  Piece one[] = {{5, 9}};
+  Piece share[] = {{512, 768}, {0, 257}, {256, 512}};
+  Piece inside[] = {{0, 1000}, {10, 20}};
+  return overlap(touch, 4) || overlap(one, 1) || overlap(one, 0) || !overlap(share, 3) || !overlap(inside, 2);
+}
+""")
+    assert os.system(f"g++ -std=c++17 -Wall -Werror -o {tmp_path}/pieces {src}") == 0
+    assert os.system(f"{tmp_path}/pieces") == 0
