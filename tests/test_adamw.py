@@ -399,3 +399,66 @@ def test_tensors_that_share_memory_are_refused():
     assert torch.equal(store, before) and not copy.any()
     AdamW([store[200:300], store[:200], store[300:]], copies=[copy[200:300], copy[:200], copy[300:]]).step([g[200:300], g[:200], g[300:]])
     assert torch.equal(copy, store.to(torch.bfloat16)) and not torch.equal(store, before)      # neighbours that touch are fine
+
+
+def stirred(places, seed, step):
+    """The 32 random bits of every place: a counter times the prime next to 2^32 / 1.618.., salted, and stirred."""
+    u64, mask = np.uint64, np.uint64(0xFFFFFFFF)
+
+    def stir(x):
+        x = ((x ^ (x >> u64(16))) * u64(0xB504F335)) & mask
+        x = ((x ^ (x >> u64(15))) * u64(0xDDB3D743)) & mask
+        return x ^ (x >> u64(16))
+
+    salt = stir(u64((seed * 0x9E3779B1 + step * 0x85EBCA77) & 0xFFFFFFFF))
+    return stir((places.astype(u64) * u64(0x9E3779B1) + salt) & mask).astype(np.int64)
+
+
+def test_8_bit_codes_are_those_of_the_rule():
+    """One step from zero moments: every code is the one that the rule picks of the two next to the value, with the random bits
+    of the seed, the step and the element's place.  Left out is what lies within the rounding of its own chance: 2^-20 of a
+    code's distance for the first moment (its subnormal codes: one rounding at 2^-6), 2^-15 for the second (a square near 256 in
+    fp32 over at most 31 steps, twice)."""
+    from paper_2402_18994_amd import AdamW
+    gen = torch.Generator().manual_seed(8)
+    shapes = [(700, 33), (5,), (129,), (3000,), (64, 64)]
+    g = [torch.randn(*s, generator=gen) * 10.0 ** (4 * torch.rand(*s, generator=gen) - 4) for s in shapes]
+    f32, grid = np.float32, oracle.E4M3[:127].numpy()
+    b1, b2 = 0.9, 0.99
+    seen = []
+    for seed, before in ((5, 0), (6, 0), (5, 1), (2 ** 32 - 3, 70000)):
+        opt = AdamW([torch.zeros(*s, device="cuda") for s in shapes], betas=(b1, b2), state_bits=8, seed=seed)
+        opt.steps = before
+        opt.step([x.cuda() for x in g])
+        codes = [opt.m.view(torch.uint8).cpu(), opt.v.view(torch.uint8).cpu()]
+        if before < 2:
+            seen.append(codes)
+        left_out = total = 0
+        for i, x in enumerate(g):
+            n, at = x.numel(), opt.at[i]
+            rand = stirred(np.arange(at, at + n), seed, before + 1)
+            flat = x.numpy().reshape(-1)
+            scales = [s[at // 128:at // 128 + -(-n // 128)].cpu().numpy().repeat(128)[:n].astype(np.float64) for s in (opt.m_scale, opt.v_scale)]
+            m, v = flat * f32(1 - b1), (flat * flat) * f32(1 - b2)         # fp32, each product rounded by itself, as the kernel's
+            for name, value, scale, low16, got, room in (("m", np.abs(m.astype(np.float64)), scales[0], True, codes[0], 2.0 ** -20),
+                                                         ("v", np.sqrt(v.astype(np.float64)), scales[1], False, codes[1], 2.0 ** -15)):
+                y = value / scale
+                low = np.minimum(np.searchsorted(grid, y, side="right") - 1, 125)
+                lo, hi = grid[low], grid[low + 1]
+                share = (y - lo) / (hi - lo) if name == "m" else (y * y - lo * lo) / (hi * hi - lo * lo)
+                chance = ((rand & 0xFFFF if low16 else rand >> 16) + 0.5) / 65536
+                want = low + (chance < share)
+                if name == "v":
+                    want = np.maximum(want, (value > 0).astype(np.int64))
+                have = got[at:at + n].numpy().astype(np.int64)
+                if name == "m":
+                    assert ((have & 0x80) != 0)[(have & 0x7F) > 0].tolist() == (flat < 0)[(have & 0x7F) > 0].tolist()
+                sure = np.abs(chance - share) > room
+                near_code = np.minimum(np.abs(y - lo), np.abs(y - hi)) <= 2.0 ** -20 * y      # (which two codes: either reading)
+                sure &= ~near_code
+                assert ((have & 0x7F) == want)[sure].all(), (name, i, seed, int((((have & 0x7F) != want) & sure).sum()))
+                assert (np.abs((have & 0x7F) - want) <= 1).all()
+                left_out, total = left_out + int((~sure).sum()), total + n
+        assert left_out < 0.001 * total
+    for k in (1, 2):                                       # another seed, another step
+        assert all((a != b).float().mean() > 0.05 for a, b in zip(seen[0], seen[k]))
