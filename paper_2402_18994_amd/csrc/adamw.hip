@@ -18,6 +18,7 @@
 // above goes to that code with a chance next to 1 from either side.  The scales go by exact comparisons.
 #include "seq_common.hpp"
 
+#include <float.h>
 #include <math.h>
 #include <stdlib.h>
 
@@ -72,6 +73,14 @@ __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_
 // pair of binades that starts at an even power (the root's rounding does not reach over the next number above that).
 __device__ __forceinline__ int scale_exponent(uint32_t top) { return max(-60, (int)((top + 0x1FFFFFu) >> 23) - 127 - 8); }
 __device__ __forceinline__ int scale_exponent_of_root(uint32_t top) { return max(-60, ((int)(top - (127u << 23) + 0x3BFFFFu) >> 24) - 8); }
+
+// The hardware's root, which takes what lies below the least normal number for zero: such a second moment (gradients of 1e-18,
+// say) has its codes and its root like any other.
+__device__ __forceinline__ float root_fast(float v) {
+  const bool tiny = v < 0x1p-100f;
+  const float r = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p100f : v);
+  return tiny ? r * 0x1p-50f : r;
+}
 
 // Codes of magnitudes in units of the scale, up to 448: binades of eight codes from 2^-6 (code 8) on, below that the
 // eight codes of the subnormal numbers, 2^-9 apart.  What lies between two codes goes up where (k + 1/2) / 65536, k being
@@ -181,7 +190,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamP p) {
     m[j] = m[j] * p.b1 + gj * p.c1;
     v[j] = v[j] * p.b2 + (gj * gj) * p.c2;
     if constexpr (BITS == 8) {
-      root[j] = __builtin_amdgcn_sqrtf(v[j]);
+      root[j] = root_fast(v[j]);
       w[j] = w[j] * keep - (m[j] * p.k1) * rcp_fast(root[j] * p.k2 + p.eps);
     } else {
       root[j] = sqrtf(v[j]);
@@ -300,7 +309,8 @@ extern "C" int32_t snn_adamw_step(const snn_adamw_args *a, const snn_adamw_tenso
   p.b2 = (float)a->beta2; p.c2 = (float)(1 - a->beta2);
   p.k1 = (float)(a->lr / (1 - pow(a->beta1, (double)a->step)));
   p.k2 = (float)(1 / sqrt(1 - pow(a->beta2, (double)a->step)));
-  p.eps = (float)a->eps; p.grad_scale = (float)a->grad_scale;
+  p.eps = a->eps > 0 ? fmaxf((float)a->eps, FLT_MIN) : 0.f;   // (a positive one stays positive, and has a reciprocal)
+  p.grad_scale = (float)a->grad_scale;
   p.salt = stir(a->seed * 0x9E3779B1u + (uint32_t)a->step * 0x85EBCA77u);
   p.count = 0;
   p.first[0] = 0;

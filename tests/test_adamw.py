@@ -462,3 +462,27 @@ def test_8_bit_codes_are_those_of_the_rule():
         assert left_out < 0.001 * total
     for k in (1, 2):                                       # another seed, another step
         assert all((a != b).float().mean() > 0.05 for a, b in zip(seen[0], seen[k]))
+
+
+def test_gradients_near_the_end_of_fp32():
+    """Second moments below the least normal number, and an epsilon that does not hide them: each product is rounded by 2^-150 at
+    most, so the second moment is off by 2^-149, and the step by half of that relative to it, beside what `near` allows."""
+    from paper_2402_18994_amd import AdamW
+    values = torch.tensor([1e-3, 1e-12, 1e-17, 4e-18, 2e-18, 1e-18, 5e-19, 2e-19, 1e-19, 0.0])
+    g = values.repeat_interleave(128)                      # (a block of moments each)
+    for bits in (32, 8):
+        for eps in (1e-20, 1e-30):
+            p = torch.zeros(len(g), device="cuda")
+            opt = AdamW([p], lr=0.5, betas=BETAS, eps=eps, weight_decay=0.0, state_bits=bits, seed=4)
+            opt.step([g.cuda()])
+            want, _, v = oracle.adamw(torch.zeros(len(g)).double(), g.double(), 0.0, 0.0, 1, 0.5, BETAS, eps, 0.0)
+            room = (16 * 2.0 ** -24 + 2.0 ** -150 / v.clamp(min=1e-300)) * want.abs()
+            assert ((p.double().cpu() - want).abs() <= room).all(), (bits, eps, p[::128], want[::128])
+            if bits == 8:
+                _, kept = moments(opt, 0, len(g))
+                off = (kept.sqrt() - v.sqrt()).abs()       # neighbouring codes: an eighth of the root, or 2^-9 of the least scale
+                assert (off <= v.sqrt() / 8 * (1 + 1e-3) + 2.0 ** -69 + v.sqrt() * 2.0 ** -150 / v.clamp(min=1e-300)).all(), (kept[::128], v[::128])
+        for eps in (1e-39, 1e-44, 1e-60):                  # positive, if only just: a gradient of zero changes nothing
+            p = torch.ones(300, device="cuda")
+            AdamW([p], eps=eps, weight_decay=0.0, state_bits=bits).step([torch.zeros(300, device="cuda")])
+            assert (p == 1).all()
