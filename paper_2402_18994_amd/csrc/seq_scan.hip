@@ -795,22 +795,24 @@ int64_t waves_of_four(const snn_scan_args &a) {
   const int64_t dg = a.D / a.groups, per = 256 / padded(a.N);
   return (int64_t)a.B * a.groups * ((dg + per - 1) / per);
 }
-// Four states a lane.  Two, with twice the wavefronts and more to do around each state, where a forward pass has one to
-// two wavefronts of four for each of the 1024 SIMDs: 1024 steps of 8 x 2048 channels of 16 states (1024 wavefronts)
-// take 104 us with two against 116 with four, 119 with four and time in four chunks; at 4096 wavefronts 79 with
-// four, 93 with two.  (Up to eight states: always two in each of four lanes.)
-Shape shape_of(const snn_scan_args &a, bool backward) {
-  const int np = padded(a.N);
-  if (np == 8) return {2, 4, 4};
-  const int64_t waves = waves_of_four(a);
-  if (!backward && np < 64 && waves >= 1024 && waves < 2048) return {2, np / 2, 8};
-  return {4, np / 4, 4};
-}
-
 // Workgroups per (chunk, sequence, group).
 int blocks_of(const snn_scan_args &a, const Shape &k) {
   const int dg = a.D / a.groups;
   return (dg + k.channels() - 1) / k.channels();
+}
+
+// Four states a lane.  Two, with twice the wavefronts and more to do around each state, where a forward pass of nine to
+// sixteen states has more than 768 wavefronts of four and its workgroups of eight wavefronts of two are at most one for each
+// of the 256 CUs: one more, and a CU that has two takes twice as long.  1024 steps of B x 2048 channels of 16 states, us with
+// two and with four (cut in chunks of time below 1024 wavefronts): 768 wavefronts of four 98 and 94, 896 100 and 115, 1024 101
+// and 117, 1152 184 and 160, 1536 197 and 163; at 4096 wavefronts 93 and 79.  32 states, 1024 wavefronts: 112 and 109.
+// (Up to eight states: always two in each of four lanes.)
+Shape shape_of(const snn_scan_args &a, bool backward) {
+  const int np = padded(a.N);
+  if (np == 8) return {2, 4, 4};
+  const Shape two = {2, np / 2, 8};
+  if (!backward && np == 16 && waves_of_four(a) > 768 && (int64_t)a.B * a.groups * blocks_of(a, two) <= 256) return two;
+  return {4, np / 4, 4};
 }
 
 int scan_sizes(const snn_scan_args *a) {
@@ -899,7 +901,7 @@ template <bool BACKWARD, typename F> int with_kind(const snn_scan_args &a, const
   const auto shapes = [&](auto zero) {
     if (k.NS == 4) return k.L == 4 ? f(zero, FixedShape<4, 4, 4>()) : k.L == 8 ? f(zero, FixedShape<4, 8, 4>()) : f(zero, FixedShape<4, 16, 4>());
     if constexpr (!BACKWARD)
-      if (k.L > 4) return k.L == 8 ? f(zero, FixedShape<2, 8, 8>()) : f(zero, FixedShape<2, 16, 8>());
+      if (k.L == 8) return f(zero, FixedShape<2, 8, 8>());
     return f(zero, FixedShape<2, 4, 4>());
   };
   return a.type == SNN_TYPE_FP32 ? shapes(0.f) : shapes((__bf16)0.f);

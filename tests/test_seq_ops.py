@@ -716,3 +716,13 @@ def test_infinite_inputs_reach_the_taps_that_meet_them(D):
     wild = ~torch.isfinite(want)
     assert torch.equal(got[wild], want[wild])
     close("dweight", torch.where(wild, 0.0, got), torch.where(wild, 0.0, want), T * 3, 2.0 ** -24)
+
+
+@pytest.mark.parametrize("case", [
+    (70, 8, 1830, 16, 1, "bf16", True, True, "some", True),      # two states a lane, the last workgroup of a sequence not full
+    (66, 9, 1700, 13, 1, "fp32", False, False, "some", True),
+    (150, 4, 3860, 9, 4, "bf16", True, False, "some", True),
+    (19, 8, 2050, 16, 1, "fp32", True, True, "some", True),      # one workgroup more than CUs: four
+    (40, 8, 1030, 16, 2, "fp32", False, True, "none", False)], ids=lambda c: "-".join(map(str, c)))
+def test_scans_on_both_sides_of_the_rule_for_states_a_lane(case):
+    test_scan_and_its_gradients(case, True)
