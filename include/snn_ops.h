@@ -29,6 +29,10 @@
  *     B * groups from 2^18, T * B * groups from 2^32, strides between steps that are negative or put 16 steps of a tensor
  *     2 GiB apart; AdamW, tensors of more than 2^33 elements.
  *   - Sums have a fixed order: the same call gives the same bits.
+ *   - The scan's A may be any number.  -inf is a state that forgets at once; its gradients are the limits (zero for A).  States
+ *     may grow (A > 0, or negative steps without softplus) as far as fp32 goes, however time is cut.  Infinities and NaN in
+ *     steps that exist stay in their sequence and channel and in the sums over them; where the definition makes an
+ *     infinity, that or NaN comes out (the states that fill N up to what lanes hold multiply an infinite input by zero).
  */
 #ifndef SNN_OPS_H_
 #define SNN_OPS_H_

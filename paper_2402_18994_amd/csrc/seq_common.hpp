@@ -41,8 +41,9 @@ template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Pack {
 };
 
 // ---------------------------------------------------------------- elementary functions
-// The hardware's base-2 exponential and logarithm are good to about one unit of the last place; results below the
-// least normal number are zero.
+// The hardware's base-2 exponential is good to about one unit of the last place; results below the least normal number are
+// zero.  exp_fast rounds x log2(e) once before it, which moves the result by about |x| 2^-24 of itself: a few units of the
+// last place for the step sizes that softplus makes of x = -5, up to eight at x = -10.
 constexpr float LOG2E = 1.4426950408889634f;
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 __device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }

@@ -1,12 +1,15 @@
 // Short causal convolution along time, one filter of W taps per channel (include/snn_ops.h):
 //   v[t,d] = bias[d] + sum_(k<W) w[d,k] x[t-(W-1)+k, d],  y = v or v sigmoid(v).
-// Bound by memory: every row piece is read once and written once.  Tensors are time-major with the channels fastest; a
+// Every row piece is read once and written once.  Tensors are time-major with the channels fastest; a
 // wavefront owns 64 lanes x VEC neighbouring channels of one sequence and walks a segment of its steps with the last
 // W - 1 inputs in registers, AHEAD rows in flight.  Sequence, segment and length are the same for the whole wavefront,
 // so all tests are on scalars, and a row that does not exist is a buffer access that the hardware drops.
-// Measured, bfloat16, four taps: 1024 steps of 8 x 2048 channels 14.4 us a call, 4.7 TB/s (a copy of 64 MiB, which the
-// last-level cache holds, reaches 7.8, one of 1 GiB 5.1); forward 29 and backward 47 us for 256 steps of 128 x 1024
-// channels of uneven lengths, of which half the rows exist (0.10 and 0.13 GB); the sums of the filter's gradients 4.4 us.
+// Measured, bfloat16, four taps: 1024 steps of 8 x 2048 channels 14.4 us a call, 67 MB at 4.7 TB/s (a copy of that size, which
+// the last-level cache holds, reaches 7.8); fp32 26.4 us; forward 27 and backward 44 us for 256 steps of 128 x 1024 channels of
+// uneven lengths, of which half the rows exist (0.10 and 0.13 GB); the sums of the filter's gradients 4.4 us.
+// What bounds it is waiting: loads and stores of a wavefront come back in one order.  Forward, the filter is first waited for
+// inside the loop, so that every round of it also waits for the stores of the round before; reverse, the row of d_state is asked
+// for last and used at once, in every row, so that all that is outstanding is waited for twice in a round of two.
 #include "common.hpp"
 #include "seq_common.hpp"
 
@@ -17,7 +20,7 @@ namespace snn {
 namespace {
 
 constexpr int AHEAD = 4;            // rows in flight per wavefront, forward (8: 2 to 7 % slower) ..
-constexpr int AHEAD_BWD = 2;        // .. and of x and of dy each, reverse (4: 1 % either way)
+constexpr int AHEAD_BWD = 2;        // .. and of x and of dy each, reverse (4: 1 % either way, as every row waits for all of them)
 constexpr int SPAN = 0x7FFF0000, NOWHERE = 0x7FFFFF00;     // see seq_scan.hip: lane offsets stay below the first
 
 struct ConvP {

@@ -15,15 +15,16 @@
 // times the wavefronts at N = 16 without computing anything twice.
 //
 // Where sequences and channels are too few to fill the chip, time is cut into chunks as well: the state after a chunk
-// is exp(A sum(delta)) times the state before it plus the chunk's own, so a first launch runs every chunk from zero
+// is exp(A sum(delta)) times the state before it plus the chunk's own (that factor may be out of range where no step is: grown_sum),
+// so a first launch runs every chunk from zero
 // (scan_forward_kernel, LOCAL), a second joins them in order (scan_join_kernel), and the third scans with the right
 // states.  The reverse pass is cut the same way, from the other end.
 //
 // Measured (us): forward, 1024 steps of 8 x 2048 channels of 16 states, bfloat16, gated: 102 (2048 wavefronts of two
 // states a lane, vector units issuing 82 % of the time), 8192 steps of 1024 channels: 30 + 8 + 43 for the three launches.
-// Forward and backward at the first size: 399, of it 113 forward with its states saved, 50 reverse from zero (98 %
-// issuing), 5 the join, 254 the reverse pass (88 %, 0.24 GB of traffic), 7 and 5 the sums.  101 ragged steps of
-// 51 x 130 channels of 11 states, fp32, forward and backward: 57.
+// Forward and backward at the first size: 407, of it 113 forward with its states saved, 50 reverse from zero (98 %
+// issuing), 5 the join, 264 the reverse pass (88 %, 0.24 GB of traffic), 7 and 4 the sums.  101 ragged steps of
+// 51 x 130 channels of 11 states, fp32, forward and backward: 60.
 #include "common.hpp"
 #include "seq_common.hpp"
 
@@ -728,9 +729,9 @@ __global__ __launch_bounds__(256) void scan_sum_params_kernel(const ScanP p, con
 
 // ---------------------------------------------------------------- one step
 // A lane holds four states of a (sequence, channel); the state [B][D][N] is read and written once, 16 bytes a lane where
-// N is a multiple of four and the rows are aligned (FOUR).  Bound by memory where there is much of it - 64 x 2048
-// channels of 16 states 7.6 us, 17 MB at 2.3 TB/s: launch and two dependent accesses, one wavefront after another, are
-// most of that - and by the launch where there is little (128 channels 2.7 us).
+// N is a multiple of four and the rows are aligned (FOUR).  64 x 2048 channels of 16 states take 7.8 us, 17 MB at 2.2 TB/s:
+// waiting, one access after another - the eight values of B and C are loaded each for itself where they exist, skip and z behind
+// the store of the state, some ten rounds in all.  Where there is little it is the launch (128 channels 2.7 us).
 template <typename T, int L, bool FOUR> __global__ __launch_bounds__(256) void scan_step_kernel(const ScanP p) {
   constexpr int NS = 4;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;

@@ -311,8 +311,8 @@ def selective_scan(x, dt, A, B, C_, D=None, z=None, dt_bias=None, softplus: bool
                    save: bool = False) -> ScanOutput:
     """delta = softplus(dt + dt_bias); h_t = exp(delta A) h_(t-1) + delta x B; y = (C h + D x) silu(z) (snn_scan_forward).
 
-    x, dt, z [T, B, D]; B, C [T, B, G, N] (or [T, B, N]), channels d // (D // G) share a group's vectors; A [D, N], D,
-    dt_bias [D] and init [B, D, N] float32; lengths [B] int32: steps beyond a sequence's length give zeros, leave its
+    x, dt, z [T, B, D]; B, C [T, B, G, N] (or [T, B, N]), channels d // (D // G) share a group's vectors; A [D, N] (any sign; -inf
+    forgets at once), D, dt_bias [D] and init [B, D, N] float32; lengths [B] int32: steps beyond a sequence's length give zeros, leave its
     state alone and are not looked at.  `save` keeps the state before every 16th step for selective_scan_backward."""
     dev, (N, _), pack = _scan_args(x, dt, A, B, C_, D, z, dt_bias, softplus, init, lengths)
     lib, saved = _declared, None
@@ -370,8 +370,10 @@ class AdamW:
 
     `state_bits` 32 or 8; 8-bit moments take 2.06 bytes a parameter instead of 8 (see snn_ops.h for their format; `seed`
     is that of their rounding).  `weight_decay`: one value, or one per parameter.  `copies`: bfloat16 tensors (or None)
-    that receive the updated parameters rounded, in the same pass.  The moments of all parameters lie in one buffer
-    each, parameter i from element `at[i]` on; state_dict and load_state_dict carry them."""
+    that receive the updated parameters rounded, in the same pass.  Parameters and copies whose memory is replaced are followed;
+    ones that no longer fit, or that share memory, are refused by the step.  The moments of all parameters lie in one
+    buffer each, parameter i from element `at[i]` on; state_dict and load_state_dict carry them and the number of steps.  Rates
+    and seed are the constructor's: a run that is resumed repeats one that went on if they are the same."""
 
     def __init__(self, params: Sequence, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
                  state_bits: int = 32, seed: int = 0, copies: Optional[Sequence] = None):
