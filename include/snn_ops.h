@@ -1,13 +1,15 @@
 /*
  * snn_ops.h - C ABI of the sequence operators and the AdamW step of the MI355X (gfx950) library.
  *
- * Beside the spiking layers of snn.h (leaky integrators whose leak is a constant of the neuron) stand here a
- * leaky integrator whose leak and input gain follow the data, the short convolution along time that feeds it,
- * and the optimiser step that trains both:
+ * Beside the spiking layers of snn.h (leaky integrators whose leak is a constant of the neuron) stand here
+ * leaky integrators whose leak and input gain follow the data, the short convolution along time that feeds them,
+ * and the optimiser step that trains all of it:
  *
  *   convolution      v[t,d] = bias[d] + sum_(k<W) weight[d,k] x[t-(W-1)+k, d];  y = v, or v sigmoid(v) (SiLU)
  *   selective scan   delta = softplus(dt + dt_bias);  h[t,d,n] = exp(delta A[d,n]) h[t-1,d,n] + delta x[t,d] Bv[t,n]
  *                    y[t,d] = (sum_n Cv[t,n] h[t,d,n] + skip[d] x[t,d]) z sigmoid(z)
+ *   recurrence       a[t,d] = exp(-c softplus(decay[d]) sigmoid(r[t,d]));  y = h
+ *                    h[t,d] = a h[t-1,d] + sqrt(1 - a^2) sigmoid(i[t,d]) x[t,d]
  *   AdamW            m, v: running means of the gradient and its square;
  *                    p <- p (1 - lr wd) - lr m' / (sqrt(v') + eps), m', v' corrected for their start at zero
  *
@@ -126,6 +128,40 @@ int32_t snn_scan_backward(const snn_scan_args *a, const snn_scan_grads *g, const
                           size_t workspace_bytes, void *hip_stream);
 /* One step of every sequence, `state` moved on in place.  T must be 1; init and lengths must be NULL. */
 int32_t snn_scan_step(const snn_scan_args *a, void *hip_stream);
+
+/* ------------------------------------------------------------------ gated linear recurrence */
+/* One state a channel.  The state's variance stays that of the gated input: what the leak takes, sqrt(1 - a^2) gives.
+ * D above 2^22, B times the number of 64-channel blocks from 2^22 on, and strides between steps that are negative or put eight steps
+ * 1 GiB apart are refused (SNN_ERR_ARG).  decay = -inf keeps a state for good, and so does a step
+ * with r = -inf (a gate below the least normal number is shut, whatever decay is); where a = 1 the gradient of r is its limit, zero. */
+typedef struct {
+  int32_t T, B, D;
+  int32_t type;
+  float sharpness;           /* c, positive and finite */
+  snn_rows x, i, r;          /* [T][B][D] */
+  snn_rows y;                /* written */
+  const float *decay;        /* [D] */
+  const float *init;         /* [B][D], or NULL: zeros */
+  const int32_t *lengths;
+  float *state;              /* [B][D], written (snn_recurrence_step: read and written), or NULL */
+} snn_recurrence_args;
+
+typedef struct {
+  snn_rows dy;
+  const float *d_state;      /* [B][D], gradient of `state`, or NULL */
+  snn_rows dx, di, dr;       /* written */
+  float *ddecay;             /* [D], written */
+  float *dinit;              /* [B][D], written, or NULL */
+} snn_recurrence_grads;
+
+/* As for the scan: workspaces and `saved` (the state before every 8th step) are 16-byte aligned device memory. */
+int32_t snn_recurrence_workspace_bytes(const snn_recurrence_args *a, int32_t backward, size_t *bytes);
+int32_t snn_recurrence_saved_bytes(const snn_recurrence_args *a, size_t *bytes);
+int32_t snn_recurrence_forward(const snn_recurrence_args *a, void *saved, void *workspace, size_t workspace_bytes, void *hip_stream);
+int32_t snn_recurrence_backward(const snn_recurrence_args *a, const snn_recurrence_grads *g, const void *saved, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+/* One step of every sequence, `state` moved on in place.  T must be 1; init and lengths must be NULL. */
+int32_t snn_recurrence_step(const snn_recurrence_args *a, void *hip_stream);
 
 /* ------------------------------------------------------------------ AdamW */
 #define SNN_ADAMW_BLOCK 128        /* elements of an 8-bit moment that share a scale */

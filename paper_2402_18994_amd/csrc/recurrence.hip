@@ -1,0 +1,576 @@
+// Gated linear recurrence, one state a channel (include/snn_ops.h):
+//   rho = sigmoid(r), l = -c softplus(decay) rho, a = exp(l), s = sqrt(1 - a^2), h_t = a h_(t-1) + s sigmoid(i) x, y = h.
+// Reverse, g_t = dy_t + a_(t+1) g_(t+1):
+//   dx = g s iota;  di = g s x iota (1 - iota);  dl = g (a h_(t-1) - a^2 / s iota x);  dr = dl l (1 - rho);
+//   ddecay = sum dl l sigmoid(decay) / softplus(decay).
+//
+// h_t = a_t h_(t-1) + b_t is a chain of affine maps, and a run of steps is one as well: (product of a, state from zero).  A lane
+// holds a run of STEPS steps of VEC channels in registers, forms its map, leaves it in LDS, joins the maps of the runs ahead of it
+// in the tile onto the tile's start, and replays its steps: every stream is read once and written once, whatever the chain's
+// length.  A workgroup walks the tiles of one sequence and CH channels; where there are too few of those to fill the chip, time is
+// cut into segments whose maps a first launch forms (the streams are then read twice).
+#include "rows.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace snn {
+namespace {
+
+constexpr int STEPS = 8;                     // a run; the state before every run is what `saved` holds
+constexpr int CH = 64;                       // channels of a workgroup
+constexpr float LN2 = 0.6931471805599453f;
+
+struct RecP {
+  int T, B, D, groups, tiles, nseg;          // tiles: of a segment
+  float sharpness;
+  Rows<void> x, i, r, y;
+  const float *decay, *init;
+  const int32_t *lengths;
+  float *state, *saved;
+  float2 *carry;                             // [nseg][B][D]: a segment's map
+  explicit RecP(const snn_recurrence_args &a)
+      : T(a.T), B(a.B), D(a.D), groups((a.D + CH - 1) / CH), tiles(0), nseg(1), sharpness(a.sharpness), x(a.x, a.T), i(a.i, a.T), r(a.r, a.T),
+        y(a.y, a.T), decay(a.decay), init(a.init), lengths(a.lengths), state(a.state), saved(nullptr), carry(nullptr) {}
+};
+struct RecGradP {
+  Rows<void> dy, dx, di, dr;
+  const float *d_state;
+  float *part, *dinit;                       // part [nseg * B][D]
+  RecGradP(const snn_recurrence_grads &g, int T) : dy(g.dy, T), dx(g.dx, T), di(g.di, T), dr(g.dr, T), d_state(g.d_state), part(nullptr), dinit(g.dinit) {}
+};
+
+// sigmoid(v) and 1 - sigmoid(v), each to its own last places.  A gate below the least normal number is shut: (0, 1).  A NaN passes.
+__device__ __forceinline__ float gate_of(float v, float &rest) {
+  const float e = exp_fast(-v), g = rcp_fast(1.f + e);
+  rest = e > 0x1p126f ? 1.f : e * g;
+  return g;
+}
+// log2 of what a wholly open gate leaves; finite, so that a shut one (times zero) holds the state whatever `decay` is.
+__device__ __forceinline__ float rate_of(float sharpness, float decay) {
+  const float v = -sharpness * LOG2E * softplus(decay);
+  return v < -0x1p127f ? -0x1p127f : v;
+}
+
+// 1 - a^2 for a = 2^L: where a^2 is near one, the series of 1 - exp(-z), whose first term left out is z^9 / 9! (2^-26 of the
+// sum at z = 1/2); 1 - a a beyond, where the rounding of a a is 1.5 units of the last place of the result.
+__device__ __forceinline__ float one_less_square(float L, float a) {
+  const float z = L * (-2.f * LN2);
+  float p = fmaf(z, -1.f / 40320.f, 1.f / 5040.f);
+  p = fmaf(p, z, -1.f / 720.f);
+  p = fmaf(p, z, 1.f / 120.f);
+  p = fmaf(p, z, -1.f / 24.f);
+  p = fmaf(p, z, 1.f / 6.f);
+  p = fmaf(p, z, -0.5f);
+  p = fmaf(p, z, 1.f);
+  return z < 0.5f ? z * p : fmaf(-a, a, 1.f);
+}
+// (root of m, its reciprocal); a root of zero has the reciprocal 2^63, so products with what goes to zero as fast stay zero.
+__device__ __forceinline__ float root_of(float m, float &inverse) {
+  inverse = __builtin_amdgcn_rsqf(fmaxf(m, 0x1p-126f));
+  return m * inverse;
+}
+
+template <typename T, int VEC> struct Place {             // where a lane's run lies
+  int run, d, at;                                         // run in the tile; first channel; byte offset from the wavefront's row
+  bool live;
+};
+
+// A tile's raw rows of one stream: row s of the run, zeros behind `n` (the run's steps that exist).
+template <typename T, int VEC>
+__device__ __forceinline__ void load_run(Pack<T, VEC> (&v)[STEPS], const T *row, int64_t st, int at, int n) {
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) v[s] = row_load<T, VEC>(row + s * st, s < n ? at : ROW_NOWHERE);
+}
+
+// WAVES wavefronts, of which each holds 64 / LANES runs of LANES lanes by VEC channels.
+template <typename T, int VEC, int WAVES> struct Shape {
+  static constexpr int LANES = CH / VEC, HALVES = 64 / LANES, RUNS = WAVES * HALVES, TILE = RUNS * STEPS;
+  // byte offset of a lane in a stream: its channel, and its half's steps
+  template <typename R> static __device__ __forceinline__ int offset(const R &r, int lane, int d, bool live) {
+    return live ? (int)((lane / LANES) * STEPS * r.st * (int64_t)sizeof(T)) + d * (int)sizeof(T) : ROW_NOWHERE;
+  }
+};
+struct alignas(8) Link {
+  float a, h;
+};
+
+// The map of each run of a tile stands in `link`; joins them onto `h` in order (reverse: from the last run on) and returns
+// what a lane's own run starts from; `h` and `p` become state and product behind the tile.
+template <int VEC, int RUNS, bool REVERSE>
+__device__ __forceinline__ void join(const Link (*link)[CH], int c, int run, float (&h)[VEC], float (&p)[VEC], float (&start)[VEC]) {
+#pragma unroll 8
+  for (int k = 0; k < RUNS; ++k) {
+    const int q = REVERSE ? RUNS - 1 - k : k;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const Link m = link[q][c + v];
+      start[v] = q == run ? h[v] : start[v];
+      h[v] = fmaf(m.a, h[v], m.h);
+      p[v] *= m.a;
+    }
+  }
+}
+
+// OUT: outputs.  Otherwise the map of the segment alone.
+template <typename T, int VEC, int WAVES, bool OUT>
+__global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const RecP a) {
+  using S = Shape<T, VEC, WAVES>;
+  __shared__ Link link[2][S::RUNS][CH];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int64_t id = blockIdx.x;
+  const int group = (int)(id % a.groups);
+  id /= a.groups;
+  const int b = (int)(id % a.B), seg = (int)(id / a.B);
+  const int c = (lane % S::LANES) * VEC, d = group * CH + c, run = wave * S::HALVES + lane / S::LANES;
+  const bool live = d < a.D;
+  const int dd = live ? d : 0;
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a.lengths, b, a.T));
+  const int at_x = S::offset(a.x, lane, d, live), at_i = S::offset(a.i, lane, d, live), at_r = S::offset(a.r, lane, d, live);
+  const int at_y = OUT ? S::offset(a.y, lane, d, live) : 0;
+  const T *x = (const T *)a.x.p + b * a.x.sb, *i = (const T *)a.i.p + b * a.i.sb, *r = (const T *)a.r.p + b * a.r.sb;
+  T *y = (T *)a.y.p + b * a.y.sb;
+  const int64_t cell = (int64_t)b * a.D + dd;
+  const int t_end = min(a.T, (seg + 1) * a.tiles * S::TILE);
+
+  float rate[VEC], h[VEC], p[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    rate[v] = rate_of(a.sharpness, a.decay[dd + v]);
+    h[v] = OUT && a.init ? a.init[cell + v] : 0.f;
+    p[v] = 1.f;
+  }
+  if (OUT)
+    for (int k = 0; k < seg; ++k)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float2 m = a.carry[(int64_t)k * a.B * a.D + cell + v];
+        h[v] = fmaf(m.x, h[v], m.y);
+      }
+
+  const int wave_t = wave * S::HALVES * STEPS, half_t = lane / S::LANES * STEPS;
+  Pack<T, VEC> rx[STEPS], ri[STEPS], rr[STEPS];
+  int t0 = seg * a.tiles * S::TILE;
+  auto fetch = [&](int t) {
+    const int tw = t + wave_t, n = len - (tw + half_t);
+    load_run<T, VEC>(rx, x + tw * a.x.st, a.x.st, at_x, n);
+    load_run<T, VEC>(ri, i + tw * a.i.st, a.i.st, at_i, n);
+    load_run<T, VEC>(rr, r + tw * a.r.st, a.r.st, at_r, n);
+  };
+  fetch(t0);
+  for (int buf = 0; t0 < t_end; t0 += S::TILE, buf ^= 1) {
+    const int tw = t0 + wave_t, t_run = tw + half_t, n = len - t_run;
+    if (t0 >= len) {                                       // (for the whole workgroup)
+      if (!OUT) break;
+      const Pack<T, VEC> zero = {};
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) row_store<T, VEC>(y + (tw + s) * a.y.st, t_run + s < a.T ? at_y : ROW_NOWHERE, zero);
+      continue;
+    }
+    float fa[STEPS][VEC], fb[STEPS][VEC], A[VEC], H[VEC], start[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      A[v] = 1.f;
+      H[v] = start[v] = 0.f;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        float rest, inverse;
+        const float rho = gate_of(widen(rr[s].v[v]), rest), iota = gate_of(widen(ri[s].v[v]), rest);
+        const float L = s < n ? rate[v] * rho : 0.f;       // (a step that does not exist: a = 1, b = 0)
+        const float e = __builtin_amdgcn_exp2f(L);
+        fa[s][v] = e;
+        fb[s][v] = s < n ? root_of(one_less_square(L, e), inverse) * iota * widen(rx[s].v[v]) : 0.f;
+        H[v] = fmaf(e, H[v], fb[s][v]);
+        A[v] *= e;
+      }
+      link[buf][run][c + v] = {A[v], H[v]};
+    }
+    if (t0 + S::TILE < t_end) fetch(t0 + S::TILE);
+    lds_barrier();                                         // (two buffers: one barrier a tile)
+    join<VEC, S::RUNS, false>(link[buf], c, run, h, p, start);
+    if (OUT) {
+      if (a.saved && live && t_run < a.T)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) a.saved[(int64_t)(t_run / STEPS) * a.B * a.D + cell + v] = start[v];
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        Pack<T, VEC> out;
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          start[v] = fmaf(fa[s][v], start[v], fb[s][v]);
+          out.v[v] = narrow<T>(s < n ? start[v] : 0.f);
+        }
+        row_store<T, VEC>(y + (tw + s) * a.y.st, t_run + s < a.T ? at_y : ROW_NOWHERE, out);
+      }
+    }
+  }
+  if (live && run == 0)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      if (!OUT) a.carry[(int64_t)seg * a.B * a.D + cell + v] = {p[v], h[v]};
+      else if (a.state && seg == a.nseg - 1) a.state[cell + v] = h[v];
+    }
+}
+
+// Reverse.  What travels from step to step is q = a g; a run's map is (product of a, q from zero).
+template <typename T, int VEC, int WAVES, bool OUT>
+__global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const RecP a, const RecGradP g) {
+  using S = Shape<T, VEC, WAVES>;
+  __shared__ Link link[2][S::RUNS][CH];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int64_t id = blockIdx.x;
+  const int group = (int)(id % a.groups);
+  id /= a.groups;
+  const int b = (int)(id % a.B), seg = (int)(id / a.B) + (OUT ? 0 : 1);     // (no segment comes before the first)
+  const int c = (lane % S::LANES) * VEC, d = group * CH + c, run = wave * S::HALVES + lane / S::LANES;
+  const bool live = d < a.D;
+  const int dd = live ? d : 0;
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a.lengths, b, a.T));
+  const int at_x = S::offset(a.x, lane, d, live), at_i = S::offset(a.i, lane, d, live), at_r = S::offset(a.r, lane, d, live);
+  const int at_dy = S::offset(g.dy, lane, d, live);
+  const int at_dx = OUT ? S::offset(g.dx, lane, d, live) : 0, at_di = OUT ? S::offset(g.di, lane, d, live) : 0, at_dr = OUT ? S::offset(g.dr, lane, d, live) : 0;
+  const T *x = (const T *)a.x.p + b * a.x.sb, *i = (const T *)a.i.p + b * a.i.sb, *r = (const T *)a.r.p + b * a.r.sb, *dy = (const T *)g.dy.p + b * g.dy.sb;
+  T *dx = (T *)g.dx.p + b * g.dx.sb, *di = (T *)g.di.p + b * g.di.sb, *dr = (T *)g.dr.p + b * g.dr.sb;
+  const int64_t cell = (int64_t)b * a.D + dd;
+  const int t_begin = seg * a.tiles * S::TILE, t_end = min(a.T, t_begin + a.tiles * S::TILE);
+
+  float rate[VEC], q[VEC], p[VEC], sum[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    rate[v] = rate_of(a.sharpness, a.decay[dd + v]);
+    q[v] = OUT && g.d_state ? g.d_state[cell + v] : 0.f;
+    p[v] = 1.f;
+    sum[v] = 0.f;
+  }
+  if (OUT)
+    for (int k = a.nseg - 1; k > seg; --k)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float2 m = a.carry[(int64_t)k * a.B * a.D + cell + v];
+        q[v] = fmaf(m.x, q[v], m.y);
+      }
+
+  const int wave_t = wave * S::HALVES * STEPS, half_t = lane / S::LANES * STEPS;
+  Pack<T, VEC> rx[STEPS], ri[STEPS], rr[STEPS], rg[STEPS];
+  float first[VEC];
+  auto fetch = [&](int t) {
+    const int tw = t + wave_t, n = len - (tw + half_t);
+    load_run<T, VEC>(rr, r + tw * a.r.st, a.r.st, at_r, n);
+    load_run<T, VEC>(rg, dy + tw * g.dy.st, g.dy.st, at_dy, n);
+    if (OUT) {
+      load_run<T, VEC>(rx, x + tw * a.x.st, a.x.st, at_x, n);
+      load_run<T, VEC>(ri, i + tw * a.i.st, a.i.st, at_i, n);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) first[v] = a.saved[(int64_t)(n > 0 ? (tw + half_t) / STEPS : 0) * a.B * a.D + cell + v];
+    }
+  };
+  int t0 = t_begin + (t_end - 1 - t_begin) / S::TILE * S::TILE;
+  for (; t0 >= t_begin && t0 >= len; t0 -= S::TILE) {      // tiles behind the sequence's end
+    if (!OUT) continue;
+    const int tw = t0 + wave_t, t_run = tw + half_t;
+    const Pack<T, VEC> zero = {};
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const bool there = t_run + s < a.T;
+      row_store<T, VEC>(dx + (tw + s) * g.dx.st, there ? at_dx : ROW_NOWHERE, zero);
+      row_store<T, VEC>(di + (tw + s) * g.di.st, there ? at_di : ROW_NOWHERE, zero);
+      row_store<T, VEC>(dr + (tw + s) * g.dr.st, there ? at_dr : ROW_NOWHERE, zero);
+    }
+  }
+  if (t0 >= t_begin) fetch(t0);
+  for (int buf = 0; t0 >= t_begin; t0 -= S::TILE, buf ^= 1) {
+    const int tw = t0 + wave_t, t_run = tw + half_t, n = len - t_run;
+    float fl[STEPS][VEC], start[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      float A = 1.f, Q = 0.f;
+      start[v] = 0.f;
+#pragma unroll
+      for (int s = STEPS - 1; s >= 0; --s) {
+        float rest;
+        const float rho = gate_of(widen(rr[s].v[v]), rest);
+        const float L = s < n ? rate[v] * rho : 0.f, e = __builtin_amdgcn_exp2f(L);
+        fl[s][v] = L;
+        Q = e * (widen(rg[s].v[v]) + Q);
+        A *= e;
+      }
+      link[buf][run][c + v] = {A, Q};
+    }
+    lds_barrier();
+    join<VEC, S::RUNS, true>(link[buf], c, run, q, p, start);
+    if (OUT) {
+      float past[STEPS][VEC];                              // the state before each step
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        float h = n > 0 ? first[v] : 0.f;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          float rest, inverse;
+          const float L = fl[s][v], e = __builtin_amdgcn_exp2f(L);
+          past[s][v] = h;
+          h = fmaf(e, h, s < n ? root_of(one_less_square(L, e), inverse) * gate_of(widen(ri[s].v[v]), rest) * widen(rx[s].v[v]) : 0.f);
+        }
+      }
+#pragma unroll
+      for (int s = STEPS - 1; s >= 0; --s) {
+        Pack<T, VEC> ox, oi, orr;
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          float closed, rest, inverse;
+          const float L = fl[s][v], e = __builtin_amdgcn_exp2f(L), xv = widen(rx[s].v[v]);
+          gate_of(widen(rr[s].v[v]), closed);
+          const float iota = gate_of(widen(ri[s].v[v]), rest), gain = root_of(one_less_square(L, e), inverse);
+          const float gt = widen(rg[s].v[v]) + start[v], gi = gt * gain * iota;
+          const float le = e == 0.f ? 0.f : L * LN2 * e;   // (l a, whose limit is zero, also where l leaves fp32)
+          const float pull = s < n ? gt * (le * past[s][v] - e * (le * inverse) * iota * xv) : 0.f;
+          ox.v[v] = narrow<T>(s < n ? gi : 0.f);
+          oi.v[v] = narrow<T>(s < n ? gi * rest * xv : 0.f);
+          orr.v[v] = narrow<T>(s < n ? pull * closed : 0.f);
+          sum[v] += pull;
+          start[v] = e * gt;
+        }
+        const bool there = t_run + s < a.T;
+        row_store<T, VEC>(dx + (tw + s) * g.dx.st, there ? at_dx : ROW_NOWHERE, ox);
+        row_store<T, VEC>(di + (tw + s) * g.di.st, there ? at_di : ROW_NOWHERE, oi);
+        row_store<T, VEC>(dr + (tw + s) * g.dr.st, there ? at_dr : ROW_NOWHERE, orr);
+      }
+    }
+    if (t0 - S::TILE >= t_begin) fetch(t0 - S::TILE);
+  }
+  if (!OUT) {
+    if (live && run == 0)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) a.carry[(int64_t)seg * a.B * a.D + cell + v] = {p[v], q[v]};
+    return;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) link[0][run][c + v].a = sum[v];
+  __syncthreads();
+  if (live && run == 0)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      float s = 0.f;
+      for (int k = 0; k < S::RUNS; ++k) s += link[0][k][c + v].a;
+      g.part[((int64_t)seg * a.B + b) * a.D + d + v] = s;
+      if (g.dinit && seg == 0) g.dinit[cell + v] = q[v];
+    }
+}
+
+// ddecay: the partial sums' sum times sigmoid(decay) / softplus(decay), which goes to 1 as decay goes to -inf.
+__global__ __launch_bounds__(256) void recurrence_sum_kernel(const float *__restrict__ part, int rows, int D, const float *__restrict__ decay, float *__restrict__ out) {
+  __shared__ float lds[256];
+  const int64_t col = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
+  const float s = sum_column(part, D, col, rows, lds);
+  if (threadIdx.x < 16 && col < D) {
+    const float v = decay[col], rate = softplus(v);
+    out[col] = s * (rate > 0.f ? sigmoid_fast(v) * rcp_fast(rate) : v != v ? v : 1.f);
+  }
+}
+
+template <typename T, int VEC> __global__ __launch_bounds__(256) void recurrence_step_kernel(const RecP a) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int cols = a.D / VEC;
+  if (id >= (int64_t)a.B * cols) return;
+  const int b = (int)(id / cols), d = (int)(id % cols) * VEC;
+  using P = Pack<T, VEC>;
+  using F = Pack<float, VEC>;
+  const P x = *(const P *)((const T *)a.x.p + b * a.x.sb + d), i = *(const P *)((const T *)a.i.p + b * a.i.sb + d),
+          r = *(const P *)((const T *)a.r.p + b * a.r.sb + d);
+  F h = *(const F *)(a.state + (int64_t)b * a.D + d);
+  const F w = *(const F *)(a.decay + d);
+  P y;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    float rest, inverse;
+    const float L = rate_of(a.sharpness, w.v[v]) * gate_of(widen(r.v[v]), rest), e = __builtin_amdgcn_exp2f(L);
+    h.v[v] = fmaf(e, h.v[v], root_of(one_less_square(L, e), inverse) * gate_of(widen(i.v[v]), rest) * widen(x.v[v]));
+    y.v[v] = narrow<T>(h.v[v]);
+  }
+  *(F *)(a.state + (int64_t)b * a.D + d) = h;
+  *(P *)((T *)a.y.p + b * a.y.sb + d) = y;
+}
+
+// ---------------------------------------------------------------- host
+int recurrence_check(const snn_recurrence_args *a, bool step, bool grads) {
+  if (!a) return ops_fail(SNN_ERR_NULL, "recurrence: arguments are NULL");
+  if (a->T < 0 || a->B <= 0 || a->D <= 0) return ops_fail(SNN_ERR_ARG, "recurrence: T >= 0, B > 0 and D > 0 are required");
+  if (a->D > (1 << 22) || (int64_t)a->B * ((a->D + CH - 1) / CH) >= (1 << 22) || a->T > (1 << 30))
+    return ops_fail(SNN_ERR_ARG, "recurrence: D must not exceed 2^22, B * (D / %d, rounded up) must stay below 2^22, T must not exceed 2^30", CH);
+  if (a->type != SNN_TYPE_FP32 && a->type != SNN_TYPE_BF16) return ops_fail(SNN_ERR_ARG, "recurrence: unknown type %d", a->type);
+  if (!(a->sharpness > 0.f) || a->sharpness > 3e38f) return ops_fail(SNN_ERR_ARG, "recurrence: sharpness has to be positive and finite");
+  if (!a->decay) return ops_fail(SNN_ERR_NULL, "recurrence: decay is NULL");
+  if (a->T > 0 && (!a->x.p || !a->i.p || !a->r.p || (!grads && !a->y.p))) return ops_fail(SNN_ERR_NULL, "recurrence: x, i, r or y is NULL");
+  if (step) {
+    if (a->T != 1) return ops_fail(SNN_ERR_ARG, "recurrence step: T must be 1");
+    if (a->init || a->lengths) return ops_fail(SNN_ERR_ARG, "recurrence step: init and lengths must be NULL");
+    if (!a->state) return ops_fail(SNN_ERR_NULL, "recurrence step: state is NULL");
+  }
+  const size_t z = a->type == SNN_TYPE_FP32 ? 4 : 2;
+  if (!aligned(a->x.p, z) || !aligned(a->i.p, z) || !aligned(a->r.p, z) || !aligned(a->y.p, z) || !aligned(a->decay, 4) || !aligned(a->init, 4) ||
+      !aligned(a->lengths, 4) || !aligned(a->state, 4))
+    return ops_fail(SNN_ERR_ARG, "recurrence: a pointer is not aligned to its element type");
+  return SNN_OK;
+}
+bool strides_fit(const snn_rows &r, int T, size_t z) { return T <= 1 || !r.p || (r.stride_t >= 0 && r.stride_t < (int64_t)((1 << 30) / (STEPS * z))); }
+
+size_t type_bytes(int32_t type) { return type == SNN_TYPE_FP32 ? 4 : 2; }
+
+// How time is cut: `waves` wavefronts a workgroup and segments of `tiles` tiles.
+struct RecCut {
+  int waves, tiles, nseg;
+};
+RecCut recurrence_cut(const snn_recurrence_args &a, int vec, bool backward) {
+  RecCut c;
+  const int64_t groups = (int64_t)(a.D + CH - 1) / CH * a.B;
+  c.waves = groups >= 256 && a.T > 128 ? (backward ? 8 : 16) : 4;
+  const int tile = c.waves * vec * STEPS;                  // (Shape::TILE)
+  const int all = std::max(1, (int)(((int64_t)a.T + tile - 1) / tile));
+  const int64_t want = groups >= 256 ? 1 : std::min<int64_t>(64, (1024 + groups - 1) / groups);
+  c.tiles = (int)((all + want - 1) / want);
+  c.nseg = (all + c.tiles - 1) / c.tiles;
+  return c;
+}
+// The workspace does not depend on the pointers, which decide between one channel a lane and two.
+int most_segments(const snn_recurrence_args &a, bool backward) { return std::max(recurrence_cut(a, 1, backward).nseg, recurrence_cut(a, 2, backward).nseg); }
+
+bool two_channels(const snn_recurrence_args &a, const snn_recurrence_grads *g) {
+  const size_t z = type_bytes(a.type);
+  auto take = [&](const snn_rows &r) { return rows_take(r, a.T, a.B, 2, z); };
+  return a.D % 2 == 0 && take(a.x) && take(a.i) && take(a.r) && (g ? take(g->dy) && take(g->dx) && take(g->di) && take(g->dr) : take(a.y));
+}
+
+template <typename T, int VEC, int WAVES> int launch_forward(RecP p, hipStream_t st) {
+  const int64_t each = (int64_t)p.groups * p.B;
+  if (p.nseg > 1) {
+    hipLaunchKernelGGL((recurrence_forward_kernel<T, VEC, WAVES, false>), dim3((unsigned)(each * (p.nseg - 1))), dim3(WAVES * 64), 0, st, p);
+    const int rc = ops_launched("recurrence, segments");
+    if (rc) return rc;
+  }
+  hipLaunchKernelGGL((recurrence_forward_kernel<T, VEC, WAVES, true>), dim3((unsigned)(each * p.nseg)), dim3(WAVES * 64), 0, st, p);
+  return ops_launched("recurrence");
+}
+template <typename T, int VEC, int WAVES> int launch_backward(RecP p, RecGradP g, float *ddecay, hipStream_t st) {
+  const int64_t each = (int64_t)p.groups * p.B;
+  if (p.T > 0 && p.nseg > 1) {
+    hipLaunchKernelGGL((recurrence_backward_kernel<T, VEC, WAVES, false>), dim3((unsigned)(each * (p.nseg - 1))), dim3(WAVES * 64), 0, st, p, g);
+    const int rc = ops_launched("recurrence backward, segments");
+    if (rc) return rc;
+  }
+  hipLaunchKernelGGL((recurrence_backward_kernel<T, VEC, WAVES, true>), dim3((unsigned)(each * p.nseg)), dim3(WAVES * 64), 0, st, p, g);
+  const int rc = ops_launched("recurrence backward");
+  if (rc) return rc;
+  hipLaunchKernelGGL(recurrence_sum_kernel, dim3((p.D + 15) / 16), dim3(256), 0, st, g.part, p.nseg * p.B, p.D, p.decay, ddecay);
+  return ops_launched("recurrence backward, sums");
+}
+
+template <int WIDE, typename F> int with_shape(const snn_recurrence_args &a, bool two, int waves, F f) {
+  auto go = [&](auto t, auto v) {
+    return waves == WIDE ? f(t, v, std::integral_constant<int, WIDE>()) : f(t, v, std::integral_constant<int, 4>());
+  };
+  auto width = [&](auto t) { return two ? go(t, std::integral_constant<int, 2>()) : go(t, std::integral_constant<int, 1>()); };
+  return a.type == SNN_TYPE_FP32 ? width(float()) : width(__bf16());
+}
+
+int recurrence_sizes(const snn_recurrence_args *a, size_t *bytes) {
+  if (!bytes) return ops_fail(SNN_ERR_NULL, "bytes is NULL");
+  if (!a) return ops_fail(SNN_ERR_NULL, "recurrence: arguments are NULL");
+  if (a->T < 0 || a->B <= 0 || a->D <= 0 || a->D > (1 << 22) || (int64_t)a->B * ((a->D + CH - 1) / CH) >= (1 << 22) || a->T > (1 << 30))
+    return ops_fail(SNN_ERR_ARG, "recurrence: sizes out of range");
+  return SNN_OK;
+}
+
+}  // namespace
+}  // namespace snn
+
+using namespace snn;
+
+extern "C" {
+
+int32_t snn_recurrence_workspace_bytes(const snn_recurrence_args *a, int32_t backward, size_t *bytes) {
+  const int rc = recurrence_sizes(a, bytes);
+  if (rc) return rc;
+  const int n = most_segments(*a, backward != 0);
+  const size_t row = (size_t)a->B * a->D * 4;
+  *bytes = (n > 1 ? rup256(2 * n * row) : 0) + (backward ? rup256(n * row) : 0);
+  return SNN_OK;
+}
+
+int32_t snn_recurrence_saved_bytes(const snn_recurrence_args *a, size_t *bytes) {
+  const int rc = recurrence_sizes(a, bytes);
+  if (rc) return rc;
+  *bytes = (size_t)std::max(1, (a->T + STEPS - 1) / STEPS) * a->B * a->D * 4;
+  return SNN_OK;
+}
+
+int32_t snn_recurrence_forward(const snn_recurrence_args *a, void *saved, void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = recurrence_check(a, false, false);
+  if (rc) return rc;
+  const size_t z = type_bytes(a->type);
+  if (!strides_fit(a->x, a->T, z) || !strides_fit(a->i, a->T, z) || !strides_fit(a->r, a->T, z) || !strides_fit(a->y, a->T, z))
+    return ops_fail(SNN_ERR_ARG, "recurrence: strides between steps must not be negative or put eight steps 1 GiB apart");
+  if (!aligned(saved, 16)) return ops_fail(SNN_ERR_ARG, "recurrence: saved has to be 16-byte aligned");
+  size_t need = 0;
+  if ((rc = snn_recurrence_workspace_bytes(a, 0, &need))) return rc;
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+    return ops_fail(SNN_ERR_WORKSPACE, "recurrence: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
+  const bool two = two_channels(*a, nullptr);
+  const RecCut c = recurrence_cut(*a, two ? 2 : 1, false);
+  RecP p(*a);
+  p.tiles = c.tiles;
+  p.nseg = c.nseg;
+  p.saved = (float *)saved;
+  p.carry = (float2 *)workspace;
+  return with_shape<16>(*a, two, c.waves, [&](auto t, auto v, auto w) { return launch_forward<decltype(t), v.value, w.value>(p, (hipStream_t)stream); });
+}
+
+int32_t snn_recurrence_backward(const snn_recurrence_args *a, const snn_recurrence_grads *g, const void *saved, void *workspace, size_t workspace_bytes,
+                                void *stream) {
+  int rc = recurrence_check(a, false, true);
+  if (rc) return rc;
+  if (!g || !g->ddecay || (a->T > 0 && (!g->dy.p || !g->dx.p || !g->di.p || !g->dr.p)))
+    return ops_fail(SNN_ERR_NULL, "recurrence backward: dy, dx, di, dr or ddecay is NULL");
+  if (!saved) return ops_fail(SNN_ERR_NULL, "recurrence backward: saved is NULL");
+  const size_t z = type_bytes(a->type);
+  if (!aligned(saved, 16) || !aligned(g->dy.p, z) || !aligned(g->dx.p, z) || !aligned(g->di.p, z) || !aligned(g->dr.p, z) || !aligned(g->d_state, 4) ||
+      !aligned(g->ddecay, 4) || !aligned(g->dinit, 4))
+    return ops_fail(SNN_ERR_ARG, "recurrence backward: a pointer is not aligned to its element type");
+  for (const snn_rows *r : {&a->x, &a->i, &a->r, &g->dy, &g->dx, &g->di, &g->dr})
+    if (!strides_fit(*r, a->T, z)) return ops_fail(SNN_ERR_ARG, "recurrence backward: strides between steps must not be negative or put eight steps 1 GiB apart");
+  size_t need = 0;
+  if ((rc = snn_recurrence_workspace_bytes(a, 1, &need))) return rc;
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < need)
+    return ops_fail(SNN_ERR_WORKSPACE, "recurrence backward: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
+  const bool two = two_channels(*a, g);
+  const RecCut c = recurrence_cut(*a, two ? 2 : 1, true);
+  RecP p(*a);
+  p.tiles = c.tiles;
+  p.nseg = c.nseg;
+  p.saved = (float *)const_cast<void *>(saved);
+  p.carry = (float2 *)workspace;
+  RecGradP q(*g, a->T);
+  const int n = most_segments(*a, true);
+  q.part = (float *)((char *)workspace + (n > 1 ? rup256((size_t)2 * n * a->B * a->D * 4) : 0));
+  return with_shape<8>(*a, two, c.waves,
+                    [&](auto t, auto v, auto w) { return launch_backward<decltype(t), v.value, w.value>(p, q, g->ddecay, (hipStream_t)stream); });
+}
+
+int32_t snn_recurrence_step(const snn_recurrence_args *a, void *stream) {
+  const int rc = recurrence_check(a, true, false);
+  if (rc) return rc;
+  const RecP p(*a);
+  const size_t z = type_bytes(a->type);
+  auto take = [&](const snn_rows &r) { return rows_take(r, 1, a->B, 4, z); };
+  const bool four = a->D % 4 == 0 && take(a->x) && take(a->i) && take(a->r) && take(a->y) && aligned(a->state, 16) && aligned(a->decay, 16);
+  const int64_t threads = (int64_t)a->B * (four ? a->D / 4 : a->D);
+  const dim3 grid((unsigned)((threads + 255) / 256));
+  const hipStream_t st = (hipStream_t)stream;
+  if (a->type == SNN_TYPE_FP32) {
+    if (four) hipLaunchKernelGGL((recurrence_step_kernel<float, 4>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((recurrence_step_kernel<float, 1>), grid, dim3(256), 0, st, p);
+  } else if (four) hipLaunchKernelGGL((recurrence_step_kernel<__bf16, 4>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((recurrence_step_kernel<__bf16, 1>), grid, dim3(256), 0, st, p);
+  return ops_launched("recurrence step");
+}
+
+}  // extern "C"

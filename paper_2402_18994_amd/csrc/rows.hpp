@@ -1,0 +1,32 @@
+// Rows of a time-major tensor as the kernels of the gated block take them: VEC neighbouring channels a lane, the row's address
+// scalar, a lane without a place of its own at an offset where the hardware drops the access.  gfx950 only.
+#pragma once
+#include "common.hpp"
+#include "seq_common.hpp"
+
+namespace snn {
+
+constexpr int ROW_SPAN = 0x7FFF0000, ROW_NOWHERE = 0x7FFFFF00;     // lane offsets that exist stay below the first
+
+template <typename T, int VEC> __device__ __forceinline__ Pack<T, VEC> row_load(const T *row, int at) {
+  using Packed = Pack<T, VEC>;
+  const rsrc_t r = make_rsrc(row, ROW_SPAN);
+  if constexpr (sizeof(T) * VEC == 16) return __builtin_bit_cast(Packed, ld_b128(r, at, 0));
+  else if constexpr (sizeof(T) * VEC == 8) return __builtin_bit_cast(Packed, ld_b64(r, at, 0));
+  else if constexpr (sizeof(T) * VEC == 4) return __builtin_bit_cast(Packed, ld_b32(r, at, 0));
+  else return __builtin_bit_cast(Packed, (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0));
+}
+template <typename T, int VEC> __device__ __forceinline__ void row_store(T *row, int at, Pack<T, VEC> v) {
+  const rsrc_t r = make_rsrc(row, ROW_SPAN);
+  if constexpr (sizeof(T) * VEC == 16) st_b128(r, at, 0, __builtin_bit_cast(u32x4, v));
+  else if constexpr (sizeof(T) * VEC == 8) st_b64(r, at, 0, __builtin_bit_cast(u32x2, v));
+  else if constexpr (sizeof(T) * VEC == 4) st_b32(r, at, 0, __builtin_bit_cast(uint32_t, v));
+  else st_b16(r, at, 0, __builtin_bit_cast(unsigned short, v));
+}
+
+// Whether the rows of a tensor of T steps of B sequences can be taken `vec` elements of `size` bytes at a time.
+inline bool rows_take(const snn_rows &r, int T, int B, int vec, size_t size) {
+  return !r.p || (aligned(r.p, vec * size) && (T <= 1 || r.stride_t % vec == 0) && (B <= 1 || r.stride_b % vec == 0));
+}
+
+}  // namespace snn

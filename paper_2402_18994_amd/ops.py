@@ -1,4 +1,5 @@
-"""Python entry points of include/snn_ops.h: the causal convolution along time, the selective scan, and AdamW.
+"""Python entry points of include/snn_ops.h: the causal convolution along time, the selective scan, the gated linear
+recurrence, and AdamW.
 
 Marshalling only, as in binding.py: PyTorch gives device memory (outputs, workspaces) and the stream, which is the
 current one of the tensors' device.  Nothing here waits for the GPU, and there is no other path: without the built
@@ -6,8 +7,8 @@ library or a device the calls raise.  Tensors are time-major, [T, B, D] with the
 steps and between sequences are taken as they are.  Streamed tensors are float32 or bfloat16, all of one call alike;
 parameters and scan states are float32.  What does not fit raises SnnError before anything is launched.
 
-Gradients are explicit calls, as snn_backward is: `causal_conv_backward` and `selective_scan_backward` take what the
-forward call took and return a tuple of gradients with names.  (No autograd node is recorded; a caller who wants one
+Gradients are explicit calls, as snn_backward is: `causal_conv_backward`, `selective_scan_backward` and their like take what
+the forward call took and return a tuple of gradients with names.  (No autograd node is recorded; a caller who wants one
 wraps the pair in a torch.autograd.Function.)
 """
 from __future__ import annotations
@@ -52,6 +53,15 @@ class _ScanGrads(C.Structure):
                [(n, C.c_void_p) for n in ("dA", "dskip", "ddt_bias", "dinit")]
 
 
+class _RecArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "B", "D", "type")] + [("sharpness", C.c_float)] + [(n, _Rows) for n in ("x", "i", "r", "y")] + \
+               [(n, C.c_void_p) for n in ("decay", "init", "lengths", "state")]
+
+
+class _RecGrads(C.Structure):
+    _fields_ = [("dy", _Rows), ("d_state", C.c_void_p)] + [(n, _Rows) for n in ("dx", "di", "dr")] + [(n, C.c_void_p) for n in ("ddecay", "dinit")]
+
+
 class _AdamTensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("at", C.c_int64),
                 ("weight_decay", C.c_double)]
@@ -92,6 +102,20 @@ class ScanGrads(NamedTuple):
     dinit: object
 
 
+class RecurrenceOutput(NamedTuple):
+    y: object
+    state: object                 # [B, D] after the last step of every sequence
+    saved: object                 # for gated_recurrence_backward (save=True), else None
+
+
+class RecurrenceGrads(NamedTuple):
+    dx: object
+    di: object
+    dr: object
+    ddecay: object
+    dinit: object
+
+
 torch = None                      # bound by _lib(), so that importing the package does not import torch
 _declared = None
 _types = None
@@ -102,9 +126,11 @@ _CONV = struct.Struct("6i" + "3q" * 2 + "5q")
 _CONV_GRADS = struct.Struct("3q" * 2 + "4q")
 _SCAN = struct.Struct("7i4x" + "3q" * 6 + "6q")
 _SCAN_GRADS = struct.Struct("3qq" + "3q" * 5 + "4q")
+_REC = struct.Struct("4if4x" + "3q" * 4 + "4q")
+_REC_GRADS = struct.Struct("3qq" + "3q" * 3 + "2q")
 _ADAM = struct.Struct("2i4qqI4x5d")
-assert [s.size for s in (_CONV, _CONV_GRADS, _SCAN, _SCAN_GRADS, _ADAM)] == \
-    [C.sizeof(c) for c in (_ConvArgs, _ConvGrads, _ScanArgs, _ScanGrads, _AdamArgs)]
+assert [s.size for s in (_CONV, _CONV_GRADS, _SCAN, _SCAN_GRADS, _REC, _REC_GRADS, _ADAM)] == \
+    [C.sizeof(c) for c in (_ConvArgs, _ConvGrads, _ScanArgs, _ScanGrads, _RecArgs, _RecGrads, _AdamArgs)]
 
 
 def _lib():
@@ -118,6 +144,8 @@ def _lib():
         for name, args in (("conv_forward", [vp, vp]), ("conv_workspace_bytes", [vp, vp]), ("conv_backward", [vp, vp, vp, sz, vp]),
                            ("conv_step", [vp, vp]), ("scan_workspace_bytes", [vp, C.c_int32, vp]), ("scan_saved_bytes", [vp, vp]),
                            ("scan_forward", [vp, vp, vp, sz, vp]), ("scan_backward", [vp, vp, vp, vp, sz, vp]), ("scan_step", [vp, vp]),
+                           ("recurrence_workspace_bytes", [vp, C.c_int32, vp]), ("recurrence_saved_bytes", [vp, vp]),
+                           ("recurrence_forward", [vp, vp, vp, sz, vp]), ("recurrence_backward", [vp, vp, vp, vp, sz, vp]), ("recurrence_step", [vp, vp]),
                            ("adamw_step", [vp, vp, C.c_int32, vp]), ("adamw_network_elements", [vp, vp]),
                            ("adamw_network_step", [vp, vp, C.c_double])):
             f = getattr(lib, "snn_" + name)
@@ -360,6 +388,88 @@ def selective_scan_step(x, dt, state, A, B, C_, D=None, z=None, dt_bias=None, so
     at = _dense(state, dev, (*x.shape, N), torch.float32, "state")
     y = torch.empty_like(x, memory_format=torch.contiguous_format)
     _call(_declared.snn_scan_step, dev, pack(y.data_ptr(), at))
+    return y
+
+
+# ------------------------------------------------------------------------------------ gated linear recurrence
+
+def _sizes(x, step):
+    """The shape of a call's first tensor, [T, B, D] or, for a step, [B, D]."""
+    shape = x.shape
+    if len(shape) != (2 if step else 3):
+        _refuse("x has to be [B, D]" if step else "x has to be [T, B, D]", ERR_SHAPE)
+    if shape[-2] == 0 or shape[-1] == 0:
+        _refuse("there has to be a sequence and a channel", ERR_SHAPE)
+    return shape
+
+
+def _like(t):
+    return torch.empty_like(t, memory_format=torch.contiguous_format) if t is not None else None
+
+
+def _at(t):
+    return t.data_ptr() if t is not None else 0
+
+
+def _saved(f, a, x):
+    """A buffer for what a forward call leaves to its backward one, float32."""
+    return torch.empty(_bytes_of(f, a) // 4, dtype=torch.float32, device=x.device)
+
+
+def _saved_at(f, a, saved, dev, name):
+    _need(saved is not None, f"saved is needed: call {name} with save=True")
+    return _dense(saved, dev, (_bytes_of(f, a) // 4,), torch.float32, "saved")
+
+
+def _rec_args(x, i, r, decay, sharpness, init, lengths, step=False):
+    """-> the device number and the packer of the call's structure: f(y's address, the state's address)."""
+    kind, dev = _start(x)
+    shape, dtype, f32 = _sizes(x, step), x.dtype, torch.float32
+    *_, B, D = shape
+    head = (1 if step else shape[0], B, D, kind, sharpness, *_first(x, shape), *_rows(i, dtype, dev, shape, "i"), *_rows(r, dtype, dev, shape, "r"))
+    _need(decay is not None, "decay is needed")
+    tail = (_dense(decay, dev, (D,), f32, "decay"), _dense(init, dev, (B, D), f32, "init"), _dense(lengths, dev, (B,), torch.int32, "lengths"))
+    return dev, lambda y, state: _REC.pack(*head, y, B * D, D, *tail, state)
+
+
+def gated_recurrence(x, i, r, decay, sharpness: float = 8.0, init=None, lengths=None, save: bool = False) -> RecurrenceOutput:
+    """a = exp(-sharpness softplus(decay) sigmoid(r)); y_t = h_t = a h_(t-1) + sqrt(1 - a^2) sigmoid(i) x (snn_recurrence_forward).
+
+    x, i, r [T, B, D]; decay [D] and init [B, D] float32; lengths [B] int32: steps beyond a sequence's length give zeros, leave its
+    state alone and are not looked at.  `save` keeps the state before every 8th step for gated_recurrence_backward."""
+    dev, pack = _rec_args(x, i, r, decay, sharpness, init, lengths)
+    lib, y = _declared, _like(x)
+    state = torch.empty(x.shape[1:], dtype=torch.float32, device=x.device)
+    a = pack(y.data_ptr(), state.data_ptr())
+    n = _bytes_of(lib.snn_recurrence_workspace_bytes, a, 0)
+    ws = _space(n, x)
+    saved = _saved(lib.snn_recurrence_saved_bytes, a, x) if save else None
+    _call(lib.snn_recurrence_forward, dev, a, _at(saved), _at(ws), n)
+    return RecurrenceOutput(y, state, saved)
+
+
+def gated_recurrence_backward(dy, saved, x, i, r, decay, sharpness: float = 8.0, init=None, lengths=None, d_state=None) -> RecurrenceGrads:
+    """Gradients of gated_recurrence(..., save=True) for dy = dL/dy and (optionally) d_state = dL/dstate; dinit is None where
+    the forward call had no init."""
+    dev, pack = _rec_args(x, i, r, decay, sharpness, init, lengths)
+    lib, a, (_, B, D) = _declared, pack(0, 0), x.shape
+    at = _saved_at(lib.snn_recurrence_saved_bytes, a, saved, dev, "gated_recurrence")
+    out = RecurrenceGrads(_like(x), _like(x), _like(x), _like(decay), _like(init))
+    g = _REC_GRADS.pack(*_rows(dy, x.dtype, dev, x.shape, "dy"), _dense(d_state, dev, (B, D), torch.float32, "d_state"), out.dx.data_ptr(), B * D, D,
+                        out.di.data_ptr(), B * D, D, out.dr.data_ptr(), B * D, D, out.ddecay.data_ptr(), _at(out.dinit))
+    n = _bytes_of(lib.snn_recurrence_workspace_bytes, a, 1)
+    ws = _space(n, x)
+    _call(lib.snn_recurrence_backward, dev, a, g, at, ws.data_ptr(), n)
+    return out
+
+
+def gated_recurrence_step(x, i, r, state, decay, sharpness: float = 8.0):
+    """One step of every sequence: x, i, r [B, D] -> y [B, D]; `state` [B, D] (float32) is moved on in place."""
+    dev, pack = _rec_args(x, i, r, decay, sharpness, None, None, step=True)
+    _need(state is not None, "state is needed")
+    at = _dense(state, dev, x.shape, torch.float32, "state")
+    y = _like(x)
+    _call(_declared.snn_recurrence_step, dev, pack(y.data_ptr(), at))
     return y
 
 
