@@ -3,13 +3,14 @@
  *
  * Beside the spiking layers of snn.h (leaky integrators whose leak is a constant of the neuron) stand here
  * leaky integrators whose leak and input gain follow the data, the short convolution along time that feeds them,
- * and the optimiser step that trains all of it:
+ * the normalisation that stands around them, and the optimiser step that trains all of it:
  *
  *   convolution      v[t,d] = bias[d] + sum_(k<W) weight[d,k] x[t-(W-1)+k, d];  y = v, or v sigmoid(v) (SiLU)
  *   selective scan   delta = softplus(dt + dt_bias);  h[t,d,n] = exp(delta A[d,n]) h[t-1,d,n] + delta x[t,d] Bv[t,n]
  *                    y[t,d] = (sum_n Cv[t,n] h[t,d,n] + skip[d] x[t,d]) z sigmoid(z)
  *   recurrence       a[t,d] = exp(-c softplus(decay[d]) sigmoid(r[t,d]));  y = h
  *                    h[t,d] = a h[t-1,d] + sqrt(1 - a^2) sigmoid(i[t,d]) x[t,d]
+ *   group norm       v = (x - mean) / sqrt(variance + eps) weight[d] + bias[d];  y = v or v sigmoid(v)
  *   AdamW            m, v: running means of the gradient and its square;
  *                    p <- p (1 - lr wd) - lr m' / (sqrt(v') + eps), m', v' corrected for their start at zero
  *
@@ -162,6 +163,36 @@ int32_t snn_recurrence_backward(const snn_recurrence_args *a, const snn_recurren
                                 size_t workspace_bytes, void *hip_stream);
 /* One step of every sequence, `state` moved on in place.  T must be 1; init and lengths must be NULL. */
 int32_t snn_recurrence_step(const snn_recurrence_args *a, void *hip_stream);
+
+/* ------------------------------------------------------------------ group norm */
+/* Channels d with the same d / (D / groups) form a group.  Statistics run over the group's channels and, unless per_step is
+ * set, over the steps of the sequence that exist.  One step at a time (a stream) is a call with per_step, T = 1.  The variance is that
+ * of the values themselves (divided by their number).  Refused (SNN_ERR_ARG): groups of more than 16384 channels, D above 2^22, T * B from
+ * 2^31, T * B * groups from 2^31. */
+typedef struct {
+  int32_t T, B, D;
+  int32_t groups;            /* divides D */
+  int32_t type;
+  int32_t silu;              /* 1: y = v sigmoid(v); 0: y = v */
+  int32_t per_step;
+  float eps;                 /* not negative, finite */
+  snn_rows x, y;             /* y is written */
+  const float *weight;       /* [D], or NULL: ones */
+  const float *bias;         /* [D], or NULL: zeros */
+  const int32_t *lengths;
+} snn_norm_args;
+
+typedef struct {
+  snn_rows dy, dx;           /* dx is written */
+  float *dweight, *dbias;    /* [D], written, or NULL */
+} snn_norm_grads;
+
+/* `saved` (may be NULL in a forward call): mean and 1 / sqrt(variance + eps) of every group, 16-byte aligned. */
+int32_t snn_norm_workspace_bytes(const snn_norm_args *a, int32_t backward, size_t *bytes);
+int32_t snn_norm_saved_bytes(const snn_norm_args *a, size_t *bytes);
+int32_t snn_norm_forward(const snn_norm_args *a, void *saved, void *workspace, size_t workspace_bytes, void *hip_stream);
+int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const void *saved, void *workspace,
+                          size_t workspace_bytes, void *hip_stream);
 
 /* ------------------------------------------------------------------ AdamW */
 #define SNN_ADAMW_BLOCK 128        /* elements of an 8-bit moment that share a scale */

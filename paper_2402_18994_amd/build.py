@@ -30,6 +30,7 @@ UNITS = {"snn_api.hip": ["-Xarch_device", "-falign-functions=1024"],
          "seq_scan.hip": [],
          "adamw.hip": [],
          "recurrence.hip": [],
+         "group_norm.hip": [],
          # results of MFMAs in ordinary vector registers (the time loops read them at once)
          "rlif_pair.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "rlif_tile.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}

@@ -1,5 +1,5 @@
 """Python entry points of include/snn_ops.h: the causal convolution along time, the selective scan, the gated linear
-recurrence, and AdamW.
+recurrence, group norm, gated units, and AdamW.
 
 Marshalling only, as in binding.py: PyTorch gives device memory (outputs, workspaces) and the stream, which is the
 current one of the tensors' device.  Nothing here waits for the GPU, and there is no other path: without the built
@@ -62,6 +62,24 @@ class _RecGrads(C.Structure):
     _fields_ = [("dy", _Rows), ("d_state", C.c_void_p)] + [(n, _Rows) for n in ("dx", "di", "dr")] + [(n, C.c_void_p) for n in ("ddecay", "dinit")]
 
 
+class _NormArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "B", "D", "groups", "type", "silu", "per_step")] + [("eps", C.c_float)] + \
+               [(n, _Rows) for n in ("x", "y")] + [(n, C.c_void_p) for n in ("weight", "bias", "lengths")]
+
+
+class _NormGrads(C.Structure):
+    _fields_ = [("dy", _Rows), ("dx", _Rows), ("dweight", C.c_void_p), ("dbias", C.c_void_p)]
+
+
+class _UnitsArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "B", "D", "F", "type", "act")] + [(n, _Rows) for n in ("x", "y")] + \
+               [(n, C.c_void_p) for n in ("gate", "up", "lengths")]
+
+
+class _UnitsGrads(C.Structure):
+    _fields_ = [("dy", _Rows), ("dx", _Rows), ("dgate", C.c_void_p), ("dup", C.c_void_p)]
+
+
 class _AdamTensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("at", C.c_int64),
                 ("weight_decay", C.c_double)]
@@ -116,6 +134,28 @@ class RecurrenceGrads(NamedTuple):
     dinit: object
 
 
+class NormOutput(NamedTuple):
+    y: object
+    saved: object                 # for group_norm_backward (save=True), else None
+
+
+class NormGrads(NamedTuple):
+    dx: object
+    dweight: object
+    dbias: object
+
+
+class UnitsOutput(NamedTuple):
+    y: object
+    saved: object                 # for gated_units_backward (save=True), else None
+
+
+class UnitsGrads(NamedTuple):
+    dx: object
+    dgate: object
+    dup: object
+
+
 torch = None                      # bound by _lib(), so that importing the package does not import torch
 _declared = None
 _types = None
@@ -128,9 +168,13 @@ _SCAN = struct.Struct("7i4x" + "3q" * 6 + "6q")
 _SCAN_GRADS = struct.Struct("3qq" + "3q" * 5 + "4q")
 _REC = struct.Struct("4if4x" + "3q" * 4 + "4q")
 _REC_GRADS = struct.Struct("3qq" + "3q" * 3 + "2q")
+_NORM = struct.Struct("7if" + "3q" * 2 + "3q")
+_NORM_GRADS = struct.Struct("3q" * 2 + "2q")
+_UNITS = struct.Struct("6i" + "3q" * 2 + "3q")
+_UNITS_GRADS = struct.Struct("3q" * 2 + "2q")
 _ADAM = struct.Struct("2i4qqI4x5d")
-assert [s.size for s in (_CONV, _CONV_GRADS, _SCAN, _SCAN_GRADS, _REC, _REC_GRADS, _ADAM)] == \
-    [C.sizeof(c) for c in (_ConvArgs, _ConvGrads, _ScanArgs, _ScanGrads, _RecArgs, _RecGrads, _AdamArgs)]
+assert [s.size for s in (_CONV, _CONV_GRADS, _SCAN, _SCAN_GRADS, _REC, _REC_GRADS, _NORM, _NORM_GRADS, _UNITS, _UNITS_GRADS, _ADAM)] == \
+    [C.sizeof(c) for c in (_ConvArgs, _ConvGrads, _ScanArgs, _ScanGrads, _RecArgs, _RecGrads, _NormArgs, _NormGrads, _UnitsArgs, _UnitsGrads, _AdamArgs)]
 
 
 def _lib():
@@ -146,6 +190,8 @@ def _lib():
                            ("scan_forward", [vp, vp, vp, sz, vp]), ("scan_backward", [vp, vp, vp, vp, sz, vp]), ("scan_step", [vp, vp]),
                            ("recurrence_workspace_bytes", [vp, C.c_int32, vp]), ("recurrence_saved_bytes", [vp, vp]),
                            ("recurrence_forward", [vp, vp, vp, sz, vp]), ("recurrence_backward", [vp, vp, vp, vp, sz, vp]), ("recurrence_step", [vp, vp]),
+                           ("norm_workspace_bytes", [vp, C.c_int32, vp]), ("norm_saved_bytes", [vp, vp]),
+                           ("norm_forward", [vp, vp, vp, sz, vp]), ("norm_backward", [vp, vp, vp, vp, sz, vp]),
                            ("adamw_step", [vp, vp, C.c_int32, vp]), ("adamw_network_elements", [vp, vp]),
                            ("adamw_network_step", [vp, vp, C.c_double])):
             f = getattr(lib, "snn_" + name)
@@ -470,6 +516,61 @@ def gated_recurrence_step(x, i, r, state, decay, sharpness: float = 8.0):
     at = _dense(state, dev, x.shape, torch.float32, "state")
     y = _like(x)
     _call(_declared.snn_recurrence_step, dev, pack(y.data_ptr(), at))
+    return y
+
+
+# ------------------------------------------------------------------------------------------------- group norm
+
+def _norm_args(x, groups, weight, bias, silu, eps, per_step, lengths, step=False):
+    """-> the device number and the packer of the call's structure: f(y's address)."""
+    kind, dev = _start(x)
+    shape, f32 = _sizes(x, step), torch.float32
+    *_, B, D = shape
+    if groups < 1 or D % groups:
+        _refuse("groups has to divide D")
+    head = (1 if step else shape[0], B, D, groups, kind, 1 if silu else 0, 1 if per_step else 0, eps, *_first(x, shape))
+    tail = (_dense(weight, dev, (D,), f32, "weight"), _dense(bias, dev, (D,), f32, "bias"), _dense(lengths, dev, (B,), torch.int32, "lengths"))
+    return dev, lambda y: _NORM.pack(*head, y, B * D, D, *tail)
+
+
+def group_norm(x, groups: int, weight=None, bias=None, silu: bool = True, eps: float = 1e-5, per_step: bool = False, lengths=None,
+               save: bool = False) -> NormOutput:
+    """y = f((x - mean) / sqrt(variance + eps) weight + bias), f = SiLU or nothing (snn_norm_forward).
+
+    x [T, B, D]; weight and bias [D] float32, or None; channels d // (D // groups) form a group.  Statistics run over a group's channels
+    and the steps of the sequence that exist, or with per_step over the group's channels of each step alone, as
+    `group_norm_step` takes them.  lengths [B] int32: steps beyond a sequence's length give zeros and are not looked at."""
+    dev, pack = _norm_args(x, groups, weight, bias, silu, eps, per_step, lengths)
+    lib, y = _declared, _like(x)
+    a = pack(y.data_ptr())
+    n = _bytes_of(lib.snn_norm_workspace_bytes, a, 0)
+    ws = _space(n, x)
+    saved = _saved(lib.snn_norm_saved_bytes, a, x) if save else None
+    _call(lib.snn_norm_forward, dev, a, _at(saved), _at(ws), n)
+    return NormOutput(y, saved)
+
+
+def group_norm_backward(dy, saved, x, groups: int, weight=None, bias=None, silu: bool = True, eps: float = 1e-5, per_step: bool = False,
+                        lengths=None) -> NormGrads:
+    """Gradients of group_norm(..., save=True) for dy = dL/dy; dweight and dbias are None where the forward call had no such
+    argument."""
+    dev, pack = _norm_args(x, groups, weight, bias, silu, eps, per_step, lengths)
+    lib, a, D = _declared, pack(0), x.shape[-1]
+    at = _saved_at(lib.snn_norm_saved_bytes, a, saved, dev, "group_norm")
+    out = NormGrads(_like(x), _like(weight), _like(bias))
+    g = _NORM_GRADS.pack(*_rows(dy, x.dtype, dev, x.shape, "dy"), out.dx.data_ptr(), x.shape[1] * D, D, _at(out.dweight), _at(out.dbias))
+    n = _bytes_of(lib.snn_norm_workspace_bytes, a, 1)
+    ws = _space(n, x)
+    _call(lib.snn_norm_backward, dev, a, g, at, ws.data_ptr(), n)
+    return out
+
+
+def group_norm_step(x, groups: int, weight=None, bias=None, silu: bool = True, eps: float = 1e-5):
+    """One step of every sequence, as group_norm with per_step takes it: x [B, D] -> y [B, D]."""
+    dev, pack = _norm_args(x, groups, weight, bias, silu, eps, True, None, step=True)
+    y = _like(x)
+    a = pack(y.data_ptr())
+    _call(_declared.snn_norm_forward, dev, a, 0, 0, 0)
     return y
 
 

@@ -181,3 +181,137 @@ def test_recurrence_infinities_stay_where_they_are():
         assert torch.equal(p[:, ~hit], q[:, ~hit])
     assert torch.equal(a.y[:17], b.y[:17]) and not torch.isfinite(b.y[17:, 1, 3]).any() and torch.isnan(b.y[60:, 0, 69]).all()
     assert torch.equal(ga.ddecay[6:69], gb.ddecay[6:69]) and torch.isnan(gb.ddecay[69])
+
+
+# ------------------------------------------------------------------------------------------------ group norm
+
+NORM = [  # T, B, D, groups, type, silu, per_step, lengths, weight, bias
+    (1, 1, 1, 1, "fp32", False, False, "none", True, True),
+    (1, 3, 8, 2, "bf16", True, True, "none", True, True),
+    (2, 2, 6, 3, "fp32", True, False, "some", True, False),
+    (7, 5, 65, 5, "bf16", True, False, "some", False, True),
+    (9, 4, 130, 5, "fp32", False, True, "some", True, True),
+    (33, 3, 64, 1, "bf16", False, False, "some", True, True),
+    (40, 3, 96, 4, "fp32", True, False, "zero", True, True),
+    (64, 2, 1040, 2, "bf16", True, True, "some", True, True),            # more threads a row than a wavefront
+    (50, 2, 1001, 1, "fp32", True, True, "none", True, True),
+    (30, 2, 3001, 1, "bf16", True, True, "some", True, True),            # rows of more than one block of columns
+    (30, 2, 3001, 1, "fp32", False, False, "some", True, True),
+    (5, 1, 16384, 1, "bf16", True, False, "none", True, True),
+    (3, 1, 16383, 1, "fp32", True, False, "none", True, True),
+    (600, 2, 64, 2, "fp32", True, False, "some", True, True),            # several chunks a sequence
+    (2000, 1, 72, 1, "bf16", True, False, "none", True, True),
+    (300, 66, 128, 2, "bf16", True, False, "some", True, True),          # one chunk of a wide workgroup
+    (700, 40, 32, 8, "bf16", True, True, "some", True, True),            # a workgroup takes several chunks
+    (0, 2, 8, 2, "fp32", True, False, "none", True, True),
+]
+
+
+def norm_case(T, B, D, groups, type, silu, per_step, lengths, weight, bias):
+    gen = torch.Generator().manual_seed(T * 139 + D)
+    t = TYPES[type]
+    x = rounded(rand(gen, T, B, D) * torch.exp(0.5 * rand(gen, D)) + rand(gen, D), t)
+    w, b = (rounded(1 + 0.2 * rand(gen, D)) if weight else None), (rounded(0.2 * rand(gen, D)) if bias else None)
+    return gen, t, x, w, b, lengths_of(lengths, T, B, gen)
+
+
+@pytest.mark.parametrize("case", NORM, ids=lambda c: "-".join(map(str, c)))
+def test_group_norm_and_its_gradients(case):
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    T, B, D, groups, _, silu, per_step, _, _, _ = case
+    gen, t, x, w, b, n = norm_case(*case)
+    print(f"\n[case] group norm {case}", flush=True)
+    gx, gw, gb, gn = on_gpu(dead(x, n), t), on_gpu(w), on_gpu(b), on_gpu(n, torch.int32)
+    kw = dict(silu=silu, per_step=per_step)
+    y, saved = group_norm(gx, groups, gw, gb, lengths=gn, save=True, **kw)
+    many = D // groups * (1 if per_step else max(T, 1))
+    h = half_step(t)
+    (wy,) = oracle.norm(x, groups, w, b, lengths=n, **kw)
+    close("y", y, wy, many, h)
+    bare = group_norm(gx, groups, gw, gb, lengths=gn, **kw)
+    assert bare.saved is None and torch.equal(bare.y, y)
+    dy = rounded(rand(gen, T, B, D), t)
+    args = (on_gpu(dead(dy, n), t), saved, gx, groups, gw, gb)
+    g = group_norm_backward(*args, lengths=gn, **kw)
+    want = gradients(lambda **k: oracle.norm(k["x"], groups, k.get("w"), k.get("b"), lengths=n, **kw), {"x": x, "w": w, "b": b}, (dy,))
+    if many > 1:
+        close("dx", g.dx, want["x"], many, h)
+    else:                                                # (one value: its deviation is zero, and so is its gradient)
+        assert (g.dx == 0).all()
+    assert (g.dweight is None) == (w is None) and (g.dbias is None) == (b is None)
+    if w is not None:
+        close("dweight", g.dweight, want["w"], T * B, 2.0 ** -24)
+    if b is not None:
+        close("dbias", g.dbias, want["b"], T * B, 2.0 ** -24)
+    assert same(g, group_norm_backward(*args, lengths=gn, **kw))
+
+
+@pytest.mark.parametrize("B,D,groups,type", [(1, 8, 1, "fp32"), (64, 2048, 16, "bf16"), (5, 130, 5, "bf16"), (3, 66, 66, "fp32"), (2, 3001, 1, "fp32")])
+def test_group_norm_steps_are_the_steps(B, D, groups, type):
+    from paper_2402_18994_amd import group_norm, group_norm_step
+    _, t, x, w, b, _ = norm_case(4, B, D, groups, type, True, True, "none", True, True)
+    gx, gw, gb = on_gpu(x, t), on_gpu(w), on_gpu(b)
+    whole = group_norm(gx, groups, gw, gb, per_step=True).y
+    (want,) = oracle.norm(x, groups, w, b, per_step=True)
+    for k in range(4):
+        y = group_norm_step(gx[k], groups, gw, gb)
+        close("step", y, want[k], D // groups, half_step(t))
+        close("step of the whole", y, whole[k].double().cpu(), D // groups, 2 * half_step(t))
+
+
+@pytest.mark.parametrize("per_step", (False, True))
+@pytest.mark.parametrize("type", ("fp32", "bf16"))
+@pytest.mark.parametrize("how", ("batch first", "parts of rows", "odd start"))
+def test_group_norm_strides(type, how, per_step):
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    T, B, D, groups = 70, 3, 64, 4
+    gen, t, x, w, b, n = norm_case(T, B, D, groups, type, True, per_step, "some", True, True)
+
+    def place(v):
+        if how == "batch first":
+            return v.transpose(0, 1).contiguous().transpose(0, 1)
+        wide = torch.full((T, B, 2 * D + 3), float("nan"), dtype=v.dtype, device=v.device)
+        at = 2 if how == "parts of rows" else 1
+        wide[..., at:at + D] = v
+        return wide[..., at:at + D]
+
+    gx, gdy, gw, gb = on_gpu(x, t), on_gpu(rounded(rand(gen, T, B, D), t), t), on_gpu(w), on_gpu(b)
+    kw = dict(per_step=per_step, lengths=on_gpu(n, torch.int32))
+    a = group_norm(gx, groups, gw, gb, save=True, **kw)
+    c = group_norm(place(gx), groups, gw, gb, save=True, **kw)
+    close("y", c.y, a.y.double().cpu(), T, 2 * half_step(t))
+    ga = group_norm_backward(gdy, a.saved, gx, groups, gw, gb, **kw)
+    gc = group_norm_backward(place(gdy), c.saved, place(gx), groups, gw, gb, **kw)
+    for k in ("dx", "dweight", "dbias"):
+        close(k, getattr(gc, k), getattr(ga, k).double().cpu(), T, 2 * half_step(t))
+    one = group_norm_backward(gdy[:1].expand(T, B, D), a.saved, gx, groups, gw, gb, **kw)
+    assert same(one, group_norm_backward(gdy[:1].expand(T, B, D).contiguous(), a.saved, gx, groups, gw, gb, **kw))
+
+
+def test_group_norm_far_from_zero():
+    """Values whose mean is 4096 times their spread: the squares are taken around the mean.  x is exact; the mean is off by a
+    rounding or two of 2^-24, 2^-11 of the spread, and that is what the outputs may be off by."""
+    from paper_2402_18994_amd import group_norm
+    gen = torch.Generator().manual_seed(3)
+    for T, per_step in ((900, False), (40, True)):
+        x = rounded(4096 + rand(gen, T, 2, 64))
+        (want,) = oracle.norm(x, 2, silu=False, per_step=per_step)
+        y = group_norm(on_gpu(x), 2, silu=False, per_step=per_step).y.double().cpu()
+        assert (y - want).abs().max().item() < 3 * 2.0 ** -11
+
+
+def test_group_norm_infinities_stay_in_their_group():
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    T, B, D, groups = 40, 3, 24, 3
+    gen, t, x, w, b, _ = norm_case(T, B, D, groups, "fp32", True, False, "none", True, True)
+    dy = on_gpu(rounded(rand(gen, T, B, D)))
+    for per_step in (False, True):
+        clean, bad = on_gpu(x), on_gpu(x)
+        bad[7, 1, 9] = float("nan")
+        hit = torch.zeros(T, B, D, dtype=torch.bool)
+        hit[7 if per_step else slice(None), 1, 8:16] = True
+        a, c = (group_norm(v, groups, on_gpu(w), on_gpu(b), per_step=per_step, save=True) for v in (clean, bad))
+        ga, gc = (group_norm_backward(dy, o.saved, v, groups, on_gpu(w), on_gpu(b), per_step=per_step) for o, v in ((a, clean), (c, bad)))
+        for p, q in ((a.y, c.y), (ga.dx, gc.dx)):
+            assert torch.equal(p[~hit], q[~hit]) and torch.isnan(q[hit]).all()
+        assert torch.equal(ga.dweight[16:], gc.dweight[16:]) and torch.isnan(gc.dweight[8:16]).all()
