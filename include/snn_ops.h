@@ -3,7 +3,7 @@
  *
  * Beside the spiking layers of snn.h (leaky integrators whose leak is a constant of the neuron) stand here
  * leaky integrators whose leak and input gain follow the data, the short convolution along time that feeds them,
- * the normalisation that stands around them, and the optimiser step that trains all of it:
+ * the normalisation and the gated units that stand around them, and the optimiser step that trains all of it:
  *
  *   convolution      v[t,d] = bias[d] + sum_(k<W) weight[d,k] x[t-(W-1)+k, d];  y = v, or v sigmoid(v) (SiLU)
  *   selective scan   delta = softplus(dt + dt_bias);  h[t,d,n] = exp(delta A[d,n]) h[t-1,d,n] + delta x[t,d] Bv[t,n]
@@ -11,6 +11,7 @@
  *   recurrence       a[t,d] = exp(-c softplus(decay[d]) sigmoid(r[t,d]));  y = h
  *                    h[t,d] = a h[t-1,d] + sqrt(1 - a^2) sigmoid(i[t,d]) x[t,d]
  *   group norm       v = (x - mean) / sqrt(variance + eps) weight[d] + bias[d];  y = v or v sigmoid(v)
+ *   gated units      y[t,f] = act(sum_d gate[f,d] x[t,d]) (sum_d up[f,d] x[t,d]),  act = SiLU or GELU
  *   AdamW            m, v: running means of the gradient and its square;
  *                    p <- p (1 - lr wd) - lr m' / (sqrt(v') + eps), m', v' corrected for their start at zero
  *
@@ -193,6 +194,36 @@ int32_t snn_norm_saved_bytes(const snn_norm_args *a, size_t *bytes);
 int32_t snn_norm_forward(const snn_norm_args *a, void *saved, void *workspace, size_t workspace_bytes, void *hip_stream);
 int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const void *saved, void *workspace,
                           size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------ gated units */
+typedef enum { SNN_ACT_SILU = 0, SNN_ACT_GELU = 1 } snn_act;    /* GELU: v (1 + erf(v / sqrt(2))) / 2 */
+
+/* The matrices have a row for each unit (what a unit reads lies together) and are of the streamed type, as are their gradients; sums
+ * are fp32, and fp32 operands enter the products as three bfloat16 pieces (all 24 bits, to multiples of 2^-133).  Rows of steps that do not
+ * exist take no part, whatever they hold.  One step of every sequence is a call with T = 1.  Refused (SNN_ERR_ARG): D or F above 2^18, T * B above 2^28. */
+typedef struct {
+  int32_t T, B, D, F;
+  int32_t type;
+  int32_t act;               /* snn_act */
+  snn_rows x;                /* [T][B][D] */
+  snn_rows y;                /* [T][B][F], written */
+  const void *gate, *up;     /* [F][D] */
+  const int32_t *lengths;
+} snn_units_args;
+
+typedef struct {
+  snn_rows dy;               /* [T][B][F] */
+  snn_rows dx;               /* [T][B][D], written */
+  void *dgate, *dup;         /* [F][D], written */
+} snn_units_grads;
+
+/* `saved` (may be NULL in a forward call): what both products came to, fp32; 16-byte aligned, as the workspaces are.  The workspace is
+ * that of a call with these very arguments: strides and alignments decide what has to be laid out anew. */
+int32_t snn_units_workspace_bytes(const snn_units_args *a, int32_t backward, size_t *bytes);
+int32_t snn_units_saved_bytes(const snn_units_args *a, size_t *bytes);
+int32_t snn_units_forward(const snn_units_args *a, void *saved, void *workspace, size_t workspace_bytes, void *hip_stream);
+int32_t snn_units_backward(const snn_units_args *a, const snn_units_grads *g, const void *saved, void *workspace,
+                           size_t workspace_bytes, void *hip_stream);
 
 /* ------------------------------------------------------------------ AdamW */
 #define SNN_ADAMW_BLOCK 128        /* elements of an 8-bit moment that share a scale */

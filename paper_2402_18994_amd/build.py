@@ -31,6 +31,7 @@ UNITS = {"snn_api.hip": ["-Xarch_device", "-falign-functions=1024"],
          "adamw.hip": [],
          "recurrence.hip": [],
          "group_norm.hip": [],
+         "gated_units.hip": [],
          # results of MFMAs in ordinary vector registers (the time loops read them at once)
          "rlif_pair.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "rlif_tile.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}

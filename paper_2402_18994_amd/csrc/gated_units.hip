@@ -1,0 +1,652 @@
+// Gated units (include/snn_ops.h): y = act(G) U, G = x gate^T, U = x up^T.  Reverse: dG = dy U act'(G), dU = dy act(G);
+//   dx = dG gate + dU up;  dgate = dG^T x, dup = dU^T x.
+//
+// Every product here is C[m][n] = sum_k A(m,k) B(n,k) with k fastest on both sides, by one kernel on the matrix units: tiles of both
+// sides travel from memory straight into LDS, 64 k a stage, and the wavefronts multiply 32 x 32 blocks out of it.  The forward
+// product takes gate and up rows in turns of 32, so that a wavefront holds both of a unit's sums and forms act(G) U itself.
+// Operands that do not lie that way (reverse: both sides of the weights' gradients, the weights of dx; any whose rows are not
+// multiples of 64 elements; fp32) are laid out first, as panels [k / 64][row][64]: a stage of a tile is one piece of memory.
+//
+// fp32 enters as three bfloat16 pieces, x = hi + mid + lo exactly (8 bits each).  Six of the nine products of pieces are summed, the
+// small ones first; those left out are 2^-25 of the product.  That costs 6 of the 16 times that bfloat16 is faster.
+#include "gemm_stream.hpp"
+#include "rows.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace snn {
+namespace {
+
+constexpr int KS = 64;                       // k of a stage: a row of it is 128 bytes
+
+// One side of a product: stage `kp` of plane `plane`, row r at p + r row + kp stage + plane plane (bytes).
+struct Side {
+  const char *p, *p2;                        // p2: up, where rows of two matrices take turns
+  int64_t row, stage, plane;
+  int rows;
+};
+// Rows in memory: what (t, b) a row m = t B + b is, and whether it exists.
+struct Steps {
+  int T, B;
+  const int32_t *lengths;
+  __device__ __forceinline__ bool live(int m, int &t, int &b) const {
+    t = (int)((unsigned)m / (unsigned)B);
+    b = m - t * B;
+    return !lengths || t < lengths[b];
+  }
+};
+struct GemmP {
+  Side a, b;
+  int panels, segs;                          // stages of a plane; products of planes
+  int mt, nt, splits;                        // tiles, parts of the contraction
+  // what becomes of it
+  Steps steps;
+  Rows<void> out = Rows<void>(snn_rows{});   // y or dx
+  void *w0, *w1;                             // dgate, dup
+  float *part;                               // [splits][rows of a][pitch]: sums of a part, or G and U ([2][rows][pitch])
+  int pitch, act;
+  int M, N;                                  // rows of a; columns (units)
+};
+enum { UNITS, DX, DW, PART };
+
+// Which pieces meet in product `seg` of six, the smallest first: mid mid, hi lo, lo hi, hi mid, mid hi, hi hi (hi = 0).
+__device__ __forceinline__ int segment_a(int seg, int segs) { return segs == 1 ? 0 : (0x102010 >> (20 - 4 * seg)) & 0xF; }
+__device__ __forceinline__ int segment_b(int seg, int segs) { return segs == 1 ? 0 : (0x120100 >> (20 - 4 * seg)) & 0xF; }
+
+__device__ __forceinline__ float erf_of(float v) { return erff(v); }
+// act(g) and its slope.
+__device__ __forceinline__ float act_of(int act, float g) { return act == SNN_ACT_SILU ? g * sigmoid_fast(g) : 0.5f * g * (1.f + erf_of(g * 0.70710678118654752f)); }
+__device__ __forceinline__ float act_slope(int act, float g) {
+  if (act == SNN_ACT_SILU) {
+    const float s = sigmoid_fast(g);
+    return s * fmaf(g, 1.f - s, 1.f);
+  }
+  return 0.5f * (1.f + erf_of(g * 0.70710678118654752f)) + g * 0.3989422804014327f * exp_fast(-0.5f * g * g);
+}
+
+// Four neighbouring values of a row from column n on.
+template <typename T> __device__ __forceinline__ void give4(T *row, int n, int N, bool wide, const float (&v)[4]) {
+  if (wide && n + 4 <= N) {
+    Pack<T, 4> q;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q.v[k] = narrow<T>(v[k]);
+    *(Pack<T, 4> *)(row + n) = q;
+  } else
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (n + k < N) row[n + k] = narrow<T>(v[k]);
+}
+
+// WM x WN wavefronts, each TM x TN blocks of 32 x 32 (m x n).  T: the type of what comes out.
+template <typename T, int WHAT, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
+  constexpr int NW = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, AI = BM / 8 / NW, BI = BN / 8 / NW;
+  constexpr int STAGE = (BM + BN) * 128;
+  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (WHAT != UNITS || TN % 2 == 0), "whole loads; gate and up in one wavefront");
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  // Tiles: neighbours in time share an XCD's L2, so every XCD (workgroups go around them in turn) takes a run of tiles, and runs
+  // walk eight rows of tiles before the next column.
+  int id = blockIdx.x;
+  const int all = a.mt * a.nt, split = id / all;
+  id -= split * all;
+  {
+    const int each = all / 8, more = all % 8, x = id % 8;
+    id = (x < more ? x * (each + 1) : more * (each + 1) + (x - more) * each) + id / 8;
+  }
+  const int band = id / (8 * a.nt), in = id - band * 8 * a.nt, high = min(8, a.mt - band * 8);
+  const int tm = band * 8 + in % high, tn = in / high;
+  const int m0 = tm * BM, n0 = tn * (WHAT == UNITS ? BN / 2 : BN);
+
+  // what a lane loads: 16 bytes, chunk lane % 8 of row lane / 8 of eight; the chunk is the one that belongs at this place of the LDS
+  int av[AI], bv[BI];
+#pragma unroll
+  for (int q = 0; q < AI; ++q) {
+    const int r = 8 * (wave + NW * q) + lane / 8, c = (lane & 7) ^ ((r >> 1) & 7);
+    av[q] = m0 + r < a.a.rows ? (int)(r * a.a.row) + c * 16 : ROW_NOWHERE;
+  }
+#pragma unroll
+  for (int q = 0; q < BI; ++q) {
+    const int r = 8 * (wave + NW * q) + lane / 8, c = (lane & 7) ^ ((r >> 1) & 7);
+    const int rr = WHAT == UNITS ? (r >> 6) * 32 + (r & 31) : r;
+    bv[q] = n0 + rr < a.b.rows ? (int)(rr * a.b.row) + c * 16 : ROW_NOWHERE;
+  }
+  const int stages = a.panels * a.segs, first = (int)((int64_t)stages * split / a.splits), last = (int)((int64_t)stages * (split + 1) / a.splits);
+  const char *const pa = a.a.p + (int64_t)m0 * a.a.row, *const pb = a.b.p + (int64_t)n0 * a.b.row,
+             *const pu = WHAT == UNITS ? a.b.p2 + (int64_t)n0 * a.b.row : nullptr;
+  const unsigned lds0 = (unsigned)(uintptr_t)(lds_ptr_t)lds;
+  int seg = first / a.panels, kp = first - seg * a.panels;
+  auto issue = [&](int buf) {
+    const int64_t at_a = segment_a(seg, a.segs) * a.a.plane + kp * a.a.stage, at_b = segment_b(seg, a.segs) * a.b.plane + kp * a.b.stage;
+    const u32x4 ra = raw_rsrc(pa + at_a, ROW_SPAN), rb = raw_rsrc(pb + at_b, ROW_SPAN), ru = WHAT == UNITS ? raw_rsrc(pu + at_b, ROW_SPAN) : rb;
+    const unsigned dst = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + wave * 1024);
+#pragma unroll
+    for (int q = 0; q < AI; ++q) load_to_lds_b128(ra, dst + q * NW * 1024, av[q], 0);
+#pragma unroll
+    for (int q = 0; q < BI; ++q) {
+      const bool up = WHAT == UNITS && ((8 * (wave + NW * q)) & 32);
+      load_to_lds_b128(up ? ru : rb, dst + BM * 128 + q * NW * 1024, bv[q], 0);
+    }
+    if (++kp == a.panels) {
+      kp = 0;
+      ++seg;
+    }
+  };
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+  const int h = lane >> 5, ra = wm * TM * 32 + (lane & 31), rb = wn * TN * 32 + (lane & 31);
+  int fa[KS / 16], fb[KS / 16];
+#pragma unroll
+  for (int s = 0; s < KS / 16; ++s) {
+    fa[s] = ra * 128 + (((2 * s + h) ^ ((ra >> 1) & 7)) << 4);
+    fb[s] = BM * 128 + rb * 128 + (((2 * s + h) ^ ((rb >> 1) & 7)) << 4);
+  }
+  if (first < last) issue(0);
+  for (int kt = first, buf = 0; kt < last; ++kt, buf ^= 1) {
+    // this wavefront's loads of the stage have landed, and behind the barrier everyone's; everyone has left the stage before
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+    if (kt + 1 < last) issue(buf ^ 1);
+    const char *st = lds + buf * STAGE;
+#pragma unroll
+    for (int s = 0; s < KS / 16; ++s) {
+      bf16x8 xa[TM], xb[TN];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) xa[i] = *(const bf16x8 *)(st + fa[s] + i * 32 * 128);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) xb[j] = *(const bf16x8 *)(st + fb[s] + j * 32 * 128);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j], xa[i], acc[i][j], 0, 0, 0);
+    }
+  }
+
+  // A lane holds, of block (i, j), row m = lane % 32 and columns 8 g + 4 h + 0..3 in element 4 g + 0..3.
+  const bool wide_out = WHAT == UNITS || WHAT == DX ? ((uintptr_t)a.out.p | (uintptr_t)(a.out.st * (int64_t)sizeof(T)) | (uintptr_t)(a.out.sb * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0
+                        : ((uintptr_t)a.w0 | (uintptr_t)a.w1 | (uintptr_t)((int64_t)a.N * sizeof(T))) % (4 * sizeof(T)) == 0;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = m0 + (wm * TM + i) * 32 + (lane & 31);
+    if (m >= a.M) continue;
+    if (WHAT == UNITS) {
+      int t, b;
+      const bool live = a.steps.live(m, t, b);
+      T *row = (T *)a.out.p + t * a.out.st + b * a.out.sb;
+#pragma unroll
+      for (int j = 0; j < TN / 2; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int n = n0 + (wn * TN / 2 + j) * 32 + 8 * g + 4 * h;
+          if (n >= a.N) continue;
+          float y[4];
+          Pack<float, 4> kg, ku;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float vg = acc[i][2 * j][4 * g + k], vu = acc[i][2 * j + 1][4 * g + k];
+            kg.v[k] = vg;
+            ku.v[k] = vu;
+            y[k] = live ? act_of(a.act, vg) * vu : 0.f;
+          }
+          give4<T>(row, n, a.N, wide_out, y);
+          if (a.part) {
+            *(Pack<float, 4> *)(a.part + (int64_t)m * a.pitch + n) = kg;
+            *(Pack<float, 4> *)(a.part + ((int64_t)a.M + m) * a.pitch + n) = ku;
+          }
+        }
+    } else {
+      int t = 0, b = 0;
+      const bool live = WHAT != DX || a.steps.live(m, t, b);
+      T *row = WHAT == DX ? (T *)a.out.p + t * a.out.st + b * a.out.sb
+               : WHAT == DW ? (m < a.M / 2 ? (T *)a.w0 + (int64_t)m * a.N : (T *)a.w1 + (int64_t)(m - a.M / 2) * a.N) : nullptr;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int n = n0 + (wn * TN + j) * 32 + 8 * g + 4 * h;
+          if (n >= a.N) continue;
+          float v[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = live ? acc[i][j][4 * g + k] : 0.f;
+          if (WHAT == PART) *(Pack<float, 4> *)(a.part + ((int64_t)split * a.M + m) * a.pitch + n) = {{v[0], v[1], v[2], v[3]}};
+          else give4<T>(row, n, a.N, wide_out, v);
+        }
+    }
+  }
+}
+
+// The parts' sum, rounded, to where a product without parts writes it.  A thread has four columns of a row.
+template <typename T, int WHAT> __global__ __launch_bounds__(256) void gemm_sum_kernel(const GemmP a) {
+  const int quads = a.pitch / 4;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t m = id / quads;
+  const int n = (int)(id - m * quads) * 4;
+  if (m >= a.M || n >= a.N) return;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; ++s) {
+    const Pack<float, 4> p = *(const Pack<float, 4> *)(a.part + ((int64_t)s * a.M + m) * a.pitch + n);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += p.v[k];
+  }
+  int t = 0, b = 0;
+  if (WHAT == DX && !a.steps.live((int)m, t, b)) v[0] = v[1] = v[2] = v[3] = 0.f;
+  T *row = WHAT == DX ? (T *)a.out.p + t * a.out.st + b * a.out.sb : m < a.M / 2 ? (T *)a.w0 + m * a.N : (T *)a.w1 + (m - a.M / 2) * a.N;
+  give4<T>(row, n, a.N, ((uintptr_t)row & (4 * sizeof(T) - 1)) == 0, v);
+}
+
+// ---------------------------------------------------------------- layouts
+// Piece `plane` of a value that enters the products.
+template <typename T> struct Pieces;
+template <> struct Pieces<__bf16> {
+  static constexpr int N = 1;
+  static __device__ __forceinline__ void split(__bf16 x, __bf16 (&p)[1]) { p[0] = x; }
+};
+template <> struct Pieces<float> {
+  static constexpr int N = 3;
+  // hi + mid + lo = x; where x would round to infinity its upper half is cut off instead; infinities and NaN are hi alone
+  static __device__ __forceinline__ void split(float x, __bf16 (&p)[3]) {
+    float hi = (float)(__bf16)x;
+    if (fabsf(x) < __builtin_huge_valf() && fabsf(hi) == __builtin_huge_valf()) hi = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+    const float r = fabsf(x) < __builtin_huge_valf() ? x - hi : 0.f, mid = (float)(__bf16)r;
+    p[0] = (__bf16)hi;
+    p[1] = (__bf16)mid;
+    p[2] = (__bf16)(r - mid);
+  }
+};
+typedef Pack<__bf16, 8> Chunk;
+
+struct LayP {
+  const void *src;                           // rows of `cols` elements
+  int64_t st, sb;                            // row m = t B + b at t st + b sb
+  Steps steps;
+  int rows, cols;
+  char *dst;                                 // panels
+  int64_t stage, plane;                      // bytes
+  int at;                                    // first panel (of rows: along the columns) or first row (transposed: along them)
+  int wide;                                  // eight elements at a time
+};
+
+// Rows as they are: panel c / 64, row m, 64 columns.  A thread makes one chunk of every piece.
+template <typename T> __global__ __launch_bounds__(256) void lay_rows_kernel(const LayP a) {
+  const int m = blockIdx.x * 32 + threadIdx.x / 8, c = blockIdx.y * KS + (threadIdx.x & 7) * 8;
+  if (m >= a.rows) return;
+  int t, b;
+  const bool live = a.steps.live(m, t, b);
+  const T *row = (const T *)a.src + t * a.st + b * a.sb;
+  Pack<T, 8> v = {};
+  if (live && a.wide && c + 8 <= a.cols) v = *(const Pack<T, 8> *)(row + c);
+  else if (live)
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c + k < a.cols) v.v[k] = row[c + k];
+  constexpr int P = Pieces<T>::N;
+  Chunk out[P];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    __bf16 p[P];
+    Pieces<T>::split(v.v[k], p);
+#pragma unroll
+    for (int q = 0; q < P; ++q) out[q].v[k] = p[q];
+  }
+#pragma unroll
+  for (int q = 0; q < P; ++q) *(Chunk *)(a.dst + q * a.plane + (a.at + blockIdx.y) * a.stage + (int64_t)m * 128 + (threadIdx.x & 7) * 16) = out[q];
+}
+
+// Columns as rows: panel m / 64, row `at` + c, 64 of the source's rows.
+template <typename T> __device__ __forceinline__ void put_transposed(const T (&tile)[KS][KS + 1], char *dst, int64_t plane, int64_t first_row, int cols_left) {
+  constexpr int P = Pieces<T>::N;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int c = (threadIdx.x + 256 * u) / 8, k0 = (threadIdx.x & 7) * 8;
+    Chunk out[P];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      __bf16 p[P];
+      Pieces<T>::split(tile[k0 + k][c], p);
+#pragma unroll
+      for (int q = 0; q < P; ++q) out[q].v[k] = p[q];
+    }
+    if (c < cols_left)
+#pragma unroll
+      for (int q = 0; q < P; ++q) *(Chunk *)(dst + q * plane + (first_row + c) * 128 + (threadIdx.x & 7) * 16) = out[q];
+  }
+}
+template <typename T> __global__ __launch_bounds__(256) void lay_transposed_kernel(const LayP a) {
+  __shared__ T tile[KS][KS + 1];
+  const int m0 = blockIdx.x * KS, c0 = blockIdx.y * KS, c = threadIdx.x & 63;
+#pragma unroll
+  for (int u = 0; u < 16; ++u) {
+    const int r = u * 4 + threadIdx.x / 64, m = m0 + r;
+    T v = narrow<T>(0.f);
+    if (m < a.rows && c0 + c < a.cols) {
+      int t, b;
+      if (a.steps.live(m, t, b)) v = ((const T *)a.src)[t * a.st + b * a.sb + c0 + c];
+    }
+    tile[r][c] = v;
+  }
+  __syncthreads();
+  put_transposed<T>(tile, a.dst + blockIdx.x * a.stage, a.plane, (int64_t)a.at + c0, a.cols - c0);
+}
+
+// dG and dU from dy and the sums of the forward pass, both ways round: [f / 64][m][64] (dU behind dG along f) and [m / 64][f][64].
+struct SlopeP {
+  Steps steps;
+  Rows<void> dy;
+  const float *g, *u;
+  int pitch, act, M, F, panels;              // panels: of F
+  char *rows, *cols;
+  int64_t rows_stage, rows_plane, cols_stage, cols_plane;
+};
+template <typename T> __global__ __launch_bounds__(256) void slope_kernel(const SlopeP a) {
+  __shared__ T tile[2][KS][KS + 1];
+  const int m0 = blockIdx.x * KS, f0 = blockIdx.y * KS, c = threadIdx.x & 63;
+#pragma unroll 4
+  for (int v = 0; v < 16; ++v) {
+    const int r = v * 4 + threadIdx.x / 64, m = m0 + r;
+    float dg = 0.f, du = 0.f;
+    if (m < a.M && f0 + c < a.F) {
+      int t, b;
+      if (a.steps.live(m, t, b)) {
+        const float d = widen(((const T *)a.dy.p)[t * a.dy.st + b * a.dy.sb + f0 + c]);
+        const float g = a.g[(int64_t)m * a.pitch + f0 + c], u = a.u[(int64_t)m * a.pitch + f0 + c];
+        dg = d * u * act_slope(a.act, g);
+        du = d * act_of(a.act, g);
+      }
+    }
+    tile[0][r][c] = narrow<T>(dg);
+    tile[1][r][c] = narrow<T>(du);
+  }
+  __syncthreads();
+  constexpr int P = Pieces<T>::N;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const int r = (threadIdx.x + 256 * v) / 8, k0 = (threadIdx.x & 7) * 8;
+      Chunk out[P];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        __bf16 p[P];
+        Pieces<T>::split(tile[w][r][k0 + k], p);
+#pragma unroll
+        for (int q = 0; q < P; ++q) out[q].v[k] = p[q];
+      }
+      if (m0 + r < a.M)
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+          *(Chunk *)(a.rows + q * a.rows_plane + (w * a.panels + blockIdx.y) * a.rows_stage + (int64_t)(m0 + r) * 128 + (threadIdx.x & 7) * 16) = out[q];
+    }
+    put_transposed<T>(tile[w], a.cols + blockIdx.x * a.cols_stage, a.cols_plane, (int64_t)w * a.F + f0, a.F - f0);
+  }
+}
+
+// ---------------------------------------------------------------- host
+int units_sizes(const snn_units_args *a) {
+  if (!a) return ops_fail(SNN_ERR_NULL, "gated units: arguments are NULL");
+  if (a->T < 0 || a->B <= 0 || a->D <= 0 || a->F <= 0) return ops_fail(SNN_ERR_ARG, "gated units: T >= 0, B > 0, D > 0 and F > 0 are required");
+  if (a->D > (1 << 18) || a->F > (1 << 18) || (int64_t)a->T * a->B > (1ll << 28))
+    return ops_fail(SNN_ERR_ARG, "gated units: D and F must not exceed 2^18, T * B 2^28");
+  if (a->type != SNN_TYPE_FP32 && a->type != SNN_TYPE_BF16) return ops_fail(SNN_ERR_ARG, "gated units: unknown type %d", a->type);
+  if (a->act != SNN_ACT_SILU && a->act != SNN_ACT_GELU) return ops_fail(SNN_ERR_ARG, "gated units: unknown activation %d", a->act);
+  return SNN_OK;
+}
+int units_check(const snn_units_args *a, bool grads) {
+  const int rc = units_sizes(a);
+  if (rc) return rc;
+  if (!a->gate || !a->up) return ops_fail(SNN_ERR_NULL, "gated units: gate or up is NULL");
+  if (a->T > 0 && (!a->x.p || (!grads && !a->y.p))) return ops_fail(SNN_ERR_NULL, "gated units: x or y is NULL");
+  const size_t z = a->type == SNN_TYPE_FP32 ? 4 : 2;
+  if (!aligned(a->x.p, z) || !aligned(a->y.p, z) || !aligned(a->gate, z) || !aligned(a->up, z) || !aligned(a->lengths, 4))
+    return ops_fail(SNN_ERR_ARG, "gated units: a pointer is not aligned to its element type");
+  return SNN_OK;
+}
+
+int panels_of(int64_t n) { return (int)((n + KS - 1) / KS); }
+int64_t panel_bytes(int64_t rows, int64_t k, int planes) { return rows * panels_of(k) * 128 * planes; }
+int pitch_of(int n) { return (n + 3) & ~3; }
+
+// x as it lies: one stride between rows, 16-byte pieces, whole stages, and tiles whose offsets fit 31 bits.
+bool x_direct(const snn_units_args &a, int64_t &row) {
+  const bool one = a.T <= 1 || a.B <= 1 || a.x.stride_t == a.x.stride_b * a.B;
+  row = (a.B > 1 ? a.x.stride_b : a.T > 1 ? a.x.stride_t : a.D) * 2;
+  return a.type == SNN_TYPE_BF16 && a.D % KS == 0 && one && aligned(a.x.p, 16) && row % 16 == 0 && row >= 0 && row < (1 << 22);
+}
+bool weights_direct(const snn_units_args &a) { return a.type == SNN_TYPE_BF16 && a.D % KS == 0 && aligned(a.gate, 16) && aligned(a.up, 16); }
+
+struct Tile {
+  int bm, bn;                                // of the product; wide: 256 x 256
+  bool wide;
+};
+Tile tile_of(int64_t m, int64_t n) {
+  const int64_t wide = ((m + 255) / 256) * ((n + 255) / 256);
+  return wide >= 192 ? Tile{256, 256, true} : Tile{128, 128, false};
+}
+// Parts of the contraction: as many as fill the chip, of eight stages at least.
+int splits_of(int64_t tiles, int64_t stages) { return (int)std::max<int64_t>(1, std::min<int64_t>({stages / 8, 16, 512 / std::max<int64_t>(1, tiles)})); }
+
+struct Product {
+  Tile tile;
+  int mt, nt, splits;
+};
+Product product_of(int64_t m, int64_t n, int64_t stages) {
+  Product p;
+  p.tile = tile_of(m, n);
+  p.mt = (int)((m + p.tile.bm - 1) / p.tile.bm);
+  p.nt = (int)((n + p.tile.bn - 1) / p.tile.bn);
+  p.splits = splits_of((int64_t)p.mt * p.nt, stages);
+  return p;
+}
+size_t part_bytes(const Product &p, int64_t m, int n) { return p.splits > 1 ? rup256((size_t)p.splits * m * pitch_of(n) * 4) : 0; }
+
+struct UnitsPlan {                           // of the reverse pass
+  int64_t M;
+  int planes, segs;
+  Product dx, dw;
+  size_t rows, cols, xt, wt, part;           // bytes of each piece of the workspace
+};
+UnitsPlan units_plan(const snn_units_args &a) {
+  UnitsPlan u;
+  u.M = (int64_t)a.T * a.B;
+  u.planes = a.type == SNN_TYPE_FP32 ? 3 : 1;
+  u.segs = u.planes == 3 ? 6 : 1;
+  const int64_t F2 = 2 * (int64_t)panels_of(a.F) * KS;
+  u.dx = product_of(u.M, a.D, (int64_t)2 * panels_of(a.F) * u.segs);
+  u.dw = product_of(2 * (int64_t)a.F, a.D, (int64_t)panels_of(u.M) * u.segs);
+  u.rows = rup256(panel_bytes(u.M, F2, u.planes));
+  u.cols = rup256(panel_bytes(2 * (int64_t)a.F, u.M, u.planes));
+  u.xt = rup256(panel_bytes(a.D, u.M, u.planes));
+  u.wt = rup256(panel_bytes(a.D, F2, u.planes));
+  u.part = std::max(part_bytes(u.dx, u.M, a.D), part_bytes(u.dw, 2 * (int64_t)a.F, a.D));
+  return u;
+}
+
+template <typename T, int WHAT> int launch_gemm(const GemmP &p, const Product &how, hipStream_t st) {
+  const int64_t n = (int64_t)p.mt * p.nt * p.splits;
+  if (n * 512 >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "gated units: too large for one launch");
+  if (how.tile.wide) {
+    auto k = gemm_kernel<T, WHAT, 2, 4, 4, 2>;
+    const int bytes = 2 * (256 + 256) * 128;
+    const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
+    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(512), bytes, st, p);
+  } else {
+    auto k = gemm_kernel<T, WHAT, 2, 2, 2, 2>;
+    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(256), 2 * (128 + 128) * 128, st, p);
+  }
+  return ops_launched("gated units, product");
+}
+template <typename T, int WHAT> int launch_product(GemmP p, const Product &how, hipStream_t st) {
+  if (p.splits == 1) return launch_gemm<T, WHAT>(p, how, st);
+  const int rc = launch_gemm<T, PART>(p, how, st);
+  if (rc) return rc;
+  const int64_t threads = (int64_t)p.M * (p.pitch / 4);
+  hipLaunchKernelGGL((gemm_sum_kernel<T, WHAT>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, p);
+  return ops_launched("gated units, sums");
+}
+
+template <typename T> int lay_rows(const void *src, int64_t st, int64_t sb, const Steps &steps, int rows, int cols, char *dst, bool wide, hipStream_t stream) {
+  LayP p{src, st, sb, steps, rows, cols, dst, (int64_t)rows * 128, (int64_t)rows * 128 * panels_of(cols), 0, wide};
+  hipLaunchKernelGGL(lay_rows_kernel<T>, dim3((rows + 31) / 32, panels_of(cols)), dim3(256), 0, stream, p);
+  return ops_launched("gated units, layout");
+}
+template <typename T>
+int lay_transposed(const void *src, int64_t st, int64_t sb, const Steps &steps, int rows, int cols, char *dst, int64_t stage, int64_t plane, int at, hipStream_t stream) {
+  LayP p{src, st, sb, steps, rows, cols, dst, stage, plane, at, 0};
+  hipLaunchKernelGGL(lay_transposed_kernel<T>, dim3(panels_of(rows), panels_of(cols)), dim3(256), 0, stream, p);
+  return ops_launched("gated units, layout");
+}
+
+template <typename T> int units_forward(const snn_units_args &a, void *saved, char *ws, hipStream_t st) {
+  const int M = a.T * a.B, planes = Pieces<T>::N;
+  const Steps steps{a.T, a.B, a.lengths}, all{1, 1 << 30, nullptr};
+  GemmP p{};
+  p.panels = panels_of(a.D);
+  p.segs = planes == 3 ? 6 : 1;
+  int64_t row;
+  int rc;
+  if (x_direct(a, row)) p.a = Side{(const char *)a.x.p, nullptr, row, 128, 0, M};
+  else {
+    const bool wide = rows_take(a.x, a.T, a.B, 8, sizeof(T));
+    if ((rc = lay_rows<T>(a.x.p, a.T > 1 ? a.x.stride_t : 0, a.x.stride_b, steps, M, a.D, ws, wide, st))) return rc;
+    p.a = Side{ws, nullptr, 128, (int64_t)M * 128, (int64_t)M * 128 * p.panels, M};
+    ws += rup256(panel_bytes(M, a.D, planes));
+  }
+  if (weights_direct(a)) p.b = Side{(const char *)a.gate, (const char *)a.up, (int64_t)a.D * 2, 128, 0, a.F};
+  else {
+    const size_t each = rup256(panel_bytes(a.F, a.D, planes));
+    const bool wide = a.D % 8 == 0 && aligned(a.gate, 8 * sizeof(T)) && aligned(a.up, 8 * sizeof(T));
+    if ((rc = lay_rows<T>(a.gate, 0, a.D, all, a.F, a.D, ws, wide, st)) || (rc = lay_rows<T>(a.up, 0, a.D, all, a.F, a.D, ws + each, wide, st))) return rc;
+    p.b = Side{ws, ws + each, 128, (int64_t)a.F * 128, (int64_t)a.F * 128 * p.panels, a.F};
+  }
+  const Tile tile = tile_of(M, 2 * (int64_t)a.F);
+  p.mt = (M + tile.bm - 1) / tile.bm;
+  p.nt = (a.F + tile.bn / 2 - 1) / (tile.bn / 2);
+  p.splits = 1;
+  p.steps = steps;
+  p.out = Rows<void>(a.y, a.T);
+  p.part = (float *)saved;
+  p.pitch = pitch_of(a.F);
+  p.act = a.act;
+  p.M = M;
+  p.N = a.F;
+  return launch_gemm<T, UNITS>(p, Product{tile, p.mt, p.nt, 1}, st);
+}
+
+template <typename T> __global__ __launch_bounds__(256) void clear_kernel(T *p, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = narrow<T>(0.f);
+}
+
+template <typename T> int units_backward(const snn_units_args &a, const snn_units_grads &g, const float *saved, char *ws, hipStream_t st) {
+  const UnitsPlan u = units_plan(a);
+  const int M = (int)u.M, pf = panels_of(a.F), pm = panels_of(M);
+  int rc;
+  if (M == 0) {
+    const int64_t n = (int64_t)a.F * a.D;
+    for (void *w : {g.dgate, g.dup}) {
+      hipLaunchKernelGGL(clear_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (T *)w, n);
+      if ((rc = ops_launched("gated units backward, no steps"))) return rc;
+    }
+    return SNN_OK;
+  }
+  const Steps steps{a.T, a.B, a.lengths}, all{1, 1 << 30, nullptr};
+  char *const rows = ws, *const cols = rows + u.rows, *const xt = cols + u.cols, *const wt = xt + u.xt, *const part = wt + u.wt;
+  const int64_t st_r = (int64_t)M * 128, st_c = (int64_t)2 * a.F * 128, st_x = (int64_t)a.D * 128, pl_w = st_x * 2 * pf;
+  SlopeP s{steps, Rows<void>(g.dy, a.T), saved, saved + (int64_t)M * pitch_of(a.F), pitch_of(a.F), a.act, M, a.F, pf, rows, cols, st_r, st_r * 2 * pf, st_c, st_c * pm};
+  hipLaunchKernelGGL(slope_kernel<T>, dim3(pm, pf), dim3(256), 0, st, s);
+  if ((rc = ops_launched("gated units backward, slopes"))) return rc;
+  if ((rc = lay_transposed<T>(a.x.p, a.T > 1 ? a.x.stride_t : 0, a.x.stride_b, steps, M, a.D, xt, st_x, st_x * pm, 0, st))) return rc;
+  if ((rc = lay_transposed<T>(a.gate, 0, a.D, all, a.F, a.D, wt, st_x, pl_w, 0, st))) return rc;
+  if ((rc = lay_transposed<T>(a.up, 0, a.D, all, a.F, a.D, wt + st_x * pf, st_x, pl_w, 0, st))) return rc;
+  GemmP p{};
+  p.segs = u.segs;
+  p.steps = steps;
+  p.part = (float *)part;
+  p.N = a.D;
+  p.pitch = pitch_of(a.D);
+  p.out = Rows<void>(g.dx, a.T);
+  p.w0 = g.dgate;
+  p.w1 = g.dup;
+  p.a = Side{rows, nullptr, 128, st_r, st_r * 2 * pf, M};
+  p.b = Side{wt, nullptr, 128, st_x, pl_w, a.D};
+  p.panels = 2 * pf;
+  p.M = M;
+  p.mt = u.dx.mt; p.nt = u.dx.nt; p.splits = u.dx.splits;
+  if ((rc = launch_product<T, DX>(p, u.dx, st))) return rc;
+  p.a = Side{cols, nullptr, 128, st_c, st_c * pm, 2 * a.F};
+  p.b = Side{xt, nullptr, 128, st_x, st_x * pm, a.D};
+  p.panels = pm;
+  p.M = 2 * a.F;
+  p.mt = u.dw.mt; p.nt = u.dw.nt; p.splits = u.dw.splits;
+  return launch_product<T, DW>(p, u.dw, st);
+}
+
+}  // namespace
+}  // namespace snn
+
+using namespace snn;
+
+extern "C" {
+
+int32_t snn_units_workspace_bytes(const snn_units_args *a, int32_t backward, size_t *bytes) {
+  if (!bytes) return ops_fail(SNN_ERR_NULL, "bytes is NULL");
+  const int rc = units_sizes(a);
+  if (rc) return rc;
+  const int planes = a->type == SNN_TYPE_FP32 ? 3 : 1;
+  if (backward) {
+    const UnitsPlan u = units_plan(*a);
+    *bytes = u.rows + u.cols + u.xt + u.wt + u.part;
+    return SNN_OK;
+  }
+  int64_t row;
+  *bytes = (x_direct(*a, row) ? 0 : rup256(panel_bytes((int64_t)a->T * a->B, a->D, planes))) + (weights_direct(*a) ? 0 : 2 * rup256(panel_bytes(a->F, a->D, planes)));
+  return SNN_OK;
+}
+
+int32_t snn_units_saved_bytes(const snn_units_args *a, size_t *bytes) {
+  if (!bytes) return ops_fail(SNN_ERR_NULL, "bytes is NULL");
+  const int rc = units_sizes(a);
+  if (rc) return rc;
+  *bytes = (size_t)std::max<int64_t>(1, (int64_t)a->T * a->B) * pitch_of(a->F) * 8;
+  return SNN_OK;
+}
+
+int32_t snn_units_forward(const snn_units_args *a, void *saved, void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = units_check(a, false);
+  if (rc) return rc;
+  if (!aligned(saved, 16)) return ops_fail(SNN_ERR_ARG, "gated units: saved has to be 16-byte aligned");
+  size_t need = 0;
+  if ((rc = snn_units_workspace_bytes(a, 0, &need))) return rc;
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+    return ops_fail(SNN_ERR_WORKSPACE, "gated units: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
+  if (a->T == 0) return SNN_OK;
+  return a->type == SNN_TYPE_FP32 ? units_forward<float>(*a, saved, (char *)workspace, (hipStream_t)stream)
+                                  : units_forward<__bf16>(*a, saved, (char *)workspace, (hipStream_t)stream);
+}
+
+int32_t snn_units_backward(const snn_units_args *a, const snn_units_grads *g, const void *saved, void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = units_check(a, true);
+  if (rc) return rc;
+  if (!g || !g->dgate || !g->dup || (a->T > 0 && (!g->dy.p || !g->dx.p))) return ops_fail(SNN_ERR_NULL, "gated units backward: dy, dx, dgate or dup is NULL");
+  if (!saved) return ops_fail(SNN_ERR_NULL, "gated units backward: saved is NULL");
+  const size_t z = a->type == SNN_TYPE_FP32 ? 4 : 2;
+  if (!aligned(saved, 16) || !aligned(g->dy.p, z) || !aligned(g->dx.p, z) || !aligned(g->dgate, z) || !aligned(g->dup, z))
+    return ops_fail(SNN_ERR_ARG, "gated units backward: a pointer is not aligned to its element type");
+  size_t need = 0;
+  if ((rc = snn_units_workspace_bytes(a, 1, &need))) return rc;
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+    return ops_fail(SNN_ERR_WORKSPACE, "gated units backward: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
+  return a->type == SNN_TYPE_FP32 ? units_backward<float>(*a, *g, (const float *)saved, (char *)workspace, (hipStream_t)stream)
+                                  : units_backward<__bf16>(*a, *g, (const float *)saved, (char *)workspace, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -25,6 +25,7 @@ from .binding import SnnError
 
 BLOCK = 128                       # SNN_ADAMW_BLOCK
 MAX_TAPS, MAX_STATES = 8, 64
+ACTS = {"silu": 0, "gelu": 1}     # snn_act
 ERR_ARG, ERR_SHAPE = 2, 3
 _DTYPE, _SHAPE = operator.attrgetter("dtype"), operator.attrgetter("shape")
 
@@ -192,6 +193,8 @@ def _lib():
                            ("recurrence_forward", [vp, vp, vp, sz, vp]), ("recurrence_backward", [vp, vp, vp, vp, sz, vp]), ("recurrence_step", [vp, vp]),
                            ("norm_workspace_bytes", [vp, C.c_int32, vp]), ("norm_saved_bytes", [vp, vp]),
                            ("norm_forward", [vp, vp, vp, sz, vp]), ("norm_backward", [vp, vp, vp, vp, sz, vp]),
+                           ("units_workspace_bytes", [vp, C.c_int32, vp]), ("units_saved_bytes", [vp, vp]),
+                           ("units_forward", [vp, vp, vp, sz, vp]), ("units_backward", [vp, vp, vp, vp, sz, vp]),
                            ("adamw_step", [vp, vp, C.c_int32, vp]), ("adamw_network_elements", [vp, vp]),
                            ("adamw_network_step", [vp, vp, C.c_double])):
             f = getattr(lib, "snn_" + name)
@@ -572,6 +575,61 @@ def group_norm_step(x, groups: int, weight=None, bias=None, silu: bool = True, e
     a = pack(y.data_ptr())
     _call(_declared.snn_norm_forward, dev, a, 0, 0, 0)
     return y
+
+
+# ------------------------------------------------------------------------------------------------ gated units
+
+def _units_args(x, gate, up, act, lengths, step=False):
+    """-> the device number, F, and the packer of the call's structure: f(y's address)."""
+    kind, dev = _start(x)
+    shape = _sizes(x, step)
+    *_, B, D = shape
+    if gate.dim() != 2 or gate.shape[1] != D or gate.shape[0] == 0:
+        _refuse("gate has to be [F, D]", ERR_SHAPE)
+    if act not in ACTS:
+        _refuse(f"act is one of {', '.join(ACTS)}, not {act!r}")
+    F = gate.shape[0]
+    head = (1 if step else shape[0], B, D, F, kind, ACTS[act], *_first(x, shape))
+    _need(up is not None, "up is needed")
+    tail = (_dense(gate, dev, (F, D), x.dtype, "gate"), _dense(up, dev, (F, D), x.dtype, "up"), _dense(lengths, dev, (B,), torch.int32, "lengths"))
+    return dev, F, lambda y: _UNITS.pack(*head, y, B * F, F, *tail)
+
+
+def _units_forward(x, gate, up, act, lengths, save, step):
+    dev, F, pack = _units_args(x, gate, up, act, lengths, step)
+    lib, y = _declared, torch.empty((*x.shape[:-1], F), dtype=x.dtype, device=x.device)
+    a = pack(y.data_ptr())
+    n = _bytes_of(lib.snn_units_workspace_bytes, a, 0)
+    ws = _space(n, x)
+    saved = _saved(lib.snn_units_saved_bytes, a, x) if save else None
+    _call(lib.snn_units_forward, dev, a, _at(saved), _at(ws), n)
+    return y, saved
+
+
+def gated_units(x, gate, up, act: str = "silu", lengths=None, save: bool = False) -> UnitsOutput:
+    """y = f(x gate^T) (x up^T), f = SiLU or GELU (the exact one): both products and what joins them in one kernel (snn_units_forward).
+
+    x [T, B, D]; gate, up [F, D] of x's type; y [T, B, F].  lengths [B] int32: steps beyond a sequence's length give zeros and are
+    not looked at.  `save` keeps both products (8 bytes a value) for gated_units_backward."""
+    return UnitsOutput(*_units_forward(x, gate, up, act, lengths, save, False))
+
+
+def gated_units_backward(dy, saved, x, gate, up, act: str = "silu", lengths=None) -> UnitsGrads:
+    """Gradients of gated_units(..., save=True) for dy = dL/dy, all of x's type."""
+    dev, F, pack = _units_args(x, gate, up, act, lengths)
+    lib, a, (T, B, D) = _declared, pack(0), x.shape
+    at = _saved_at(lib.snn_units_saved_bytes, a, saved, dev, "gated_units")
+    out = UnitsGrads(_like(x), _like(gate), _like(up))
+    g = _UNITS_GRADS.pack(*_rows(dy, x.dtype, dev, (T, B, F), "dy"), out.dx.data_ptr(), B * D, D, out.dgate.data_ptr(), out.dup.data_ptr())
+    n = _bytes_of(lib.snn_units_workspace_bytes, a, 1)
+    ws = _space(n, x)
+    _call(lib.snn_units_backward, dev, a, g, at, _at(ws), n)
+    return out
+
+
+def gated_units_step(x, gate, up, act: str = "silu"):
+    """One step of every sequence: x [B, D] -> y [B, F]."""
+    return _units_forward(x, gate, up, act, None, False, True)[0]
 
 
 # ------------------------------------------------------------------------------------------------------ AdamW
