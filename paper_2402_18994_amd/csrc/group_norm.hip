@@ -3,10 +3,12 @@
 //   dx = rstd (p - mean(p) - xh mean(p xh)), dw = sum q xh, db = sum q.
 // Means run over the channels of a group and, unless per_step, the steps of the sequence that exist.
 //
-// What bounds it is memory, so x (and dy) are read once where they can be: a workgroup holds a chunk, rows by the channels of one
-// group, in registers, forms the mean, then the squares around it, and writes the outputs.  Where a sequence's group is more
-// than one chunk, or there are too few groups to fill the chip, one launch leaves every chunk's (mean, sum of squares around it) and
-// a second one joins them and reads the rows again.  Sums over rows (dw, db) leave a row per chunk that a last launch adds up.
+// What bounds it is memory.  Where each step stands alone, and where a sequence's group fits the registers of one small workgroup, x (and
+// dy) are read once: mean, squares around it, outputs.  Otherwise a sequence's rows are cut into chunks: one launch leaves every
+// chunk's (mean, sum of squares around it), a second one joins them and reads the rows again, which the last-level cache still has up to
+// some 200 MB.  (One workgroup of 1024 threads that holds 64 values a thread needs no second reading, but fills and empties a compute
+// unit in turn: 1024 steps of 8 x 2048 channels, 32 groups, bf16: forward 24.7 us against 24.0, reverse 226, out of registers, against 43.)
+// Sums over rows (dw, db) leave a row per chunk that a last launch adds up.
 #include "rows.hpp"
 
 #include <algorithm>
@@ -15,31 +17,56 @@
 namespace snn {
 namespace {
 
-enum { WHOLE = 0, SUMS = 1, APPLY = 2, STEP = 3 };           // what a launch does: all; a chunk's sums; the rest; rows by themselves
+enum { WHOLE = 0, STEP = 1 };                                // statistics over a unit's rows, or of each row
 
 struct NormP {
   int T, B, D, G, C, silu;
   float eps;
   int64_t rows;                             // of a unit: T of a sequence, or T B where each row stands alone
-  int units, nchunk, loops;                 // loops: chunks that a workgroup takes in turn
+  int units, blocks, loops;                 // workgroups of a unit and group; how many lots of rows each takes in turn
   int tpr_log2, K, R;                       // threads a row; column blocks of a row; rows of a thread
   Rows<void> x, y;
   const float *weight, *bias;
   const int32_t *lengths;
   float2 *saved;                            // [units or rows][G]: mean, rstd
-  float2 *part;                             // [units][G][nchunk]: a chunk's sums
+  float2 *part;                             // [units][G][blocks]: a chunk's sums
   // reverse
   Rows<void> dy, dx;
-  float *dpart;                             // [units * nchunk / loops][2][D]
+  float *dpart;                             // [units * blocks][2][D]
 };
 
-__device__ __forceinline__ float wave_sum(float v, int width) {      // over aligned sets of `width` lanes, in all of them
-  for (int o = 1; o < width; o <<= 1) v += __shfl_xor(v, o);
+// v of this lane and of the one 16 (32) lanes away, added: the halves of two copies change places.
+__device__ __forceinline__ float add_16_apart(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add_32_apart(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Sum over aligned sets of 2^w lanes, in all of them.
+__device__ __forceinline__ float wave_sum(float v, int w) {
+  if (w >= 1) v += dpp<0xB1>(v);
+  if (w >= 2) v += dpp<0x4E>(v);
+  if (w >= 3) v += dpp<0x141>(v);
+  if (w >= 4) v += dpp<0x140>(v);
+  if (w >= 5) v = add_16_apart(v);
+  if (w >= 6) v = add_32_apart(v);
+  return v;
+}
+// Sum over the lanes whose numbers agree in their low w bits (row rotations, then the swaps).
+__device__ __forceinline__ float wave_fold(float v, int w) {
+  if (w <= 3) v += dpp<0x128>(v);
+  if (w <= 2) v += dpp<0x124>(v);
+  if (w <= 1) v += dpp<0x122>(v);
+  if (w <= 0) v += dpp<0x121>(v);
+  if (w <= 4) v = add_16_apart(v);
+  if (w <= 5) v = add_32_apart(v);
   return v;
 }
 // Over a workgroup, in all threads.  `lds` takes NT / 64 floats and is free again after the next barrier.
 template <int NT> __device__ __forceinline__ float block_sum(float v, float *lds) {
-  v = wave_sum(v, 64);
+  v = wave_sum(v, 6);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
   float s = 0.f;
@@ -48,8 +75,10 @@ template <int NT> __device__ __forceinline__ float block_sum(float v, float *lds
   return s;
 }
 
-template <typename T, int VEC> struct Slots {
-  static constexpr int N = sizeof(T) * VEC == 16 ? 8 : 16;           // vectors of a thread
+// Vectors that a thread holds at a time.  Rows that stand alone are taken two at a time (K1: a row is one vector a thread): more of them
+// cost registers and with them wavefronts.
+template <typename T, int VEC, int MODE, bool K1> struct Slots {
+  static constexpr int N = MODE == STEP && K1 ? 2 : sizeof(T) * VEC == 16 ? 8 : 16;
 };
 
 __device__ __forceinline__ float silu_slope(float v) {
@@ -101,6 +130,22 @@ __device__ __forceinline__ Pack<T, VEC> fetch(const W &w, const R &r, int s, boo
   return live ? v : zero;
 }
 
+// The second use of packed values widens them again: left alone, the compiler keeps all the values that it formed of them for the
+// first one, and has no registers for that.
+template <typename P, int N> __device__ __forceinline__ void keep_packed(P (&v)[N]) {
+#pragma unroll
+  for (int s = 0; s < N; ++s) {
+    if constexpr (sizeof(P) >= 4) {
+      struct Words {
+        uint32_t w[sizeof(P) / 4];
+      } u = __builtin_bit_cast(Words, v[s]);
+#pragma unroll
+      for (int k = 0; k < (int)(sizeof(P) / 4); ++k) asm volatile("" : "+v"(u.w[k]));
+      v[s] = __builtin_bit_cast(P, u);
+    }
+  }
+}
+
 template <int VEC> __device__ __forceinline__ void params(const NormP &a, int d, float (&w)[VEC], float (&b)[VEC]) {
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
@@ -111,24 +156,17 @@ template <int VEC> __device__ __forceinline__ void params(const NormP &a, int d,
 
 template <typename T, int VEC, bool K1>
 __device__ __forceinline__ Where<T, VEC, K1> where(const NormP &a, bool step, int nt) {
-  const int64_t id = blockIdx.x;
+  const unsigned rest = blockIdx.x / (unsigned)a.G, turn = rest / (unsigned)a.units;
   Where<T, VEC, K1> w{a, 0, 0, 0, 0, 0, 0, 0, step};
-  w.g = (int)(id % a.G);
-  const int64_t rest = id / a.G;
-  w.unit = (int)(rest % a.units);
+  w.g = (int)(blockIdx.x - rest * a.G);
+  w.unit = (int)(rest - turn * a.units);
   w.rsub = (int)threadIdx.x >> a.tpr_log2;
   w.col = (int)threadIdx.x & ((1 << a.tpr_log2) - 1);
   w.rp = nt >> a.tpr_log2;
-  w.r0 = (rest / a.units) * (int64_t)w.rp * a.R * a.loops;
+  w.r0 = turn * (int64_t)w.rp * a.R * a.loops;
   w.len = step ? 0 : __builtin_amdgcn_readfirstlane(length_of(a.lengths, w.unit, a.T));
   return w;
 }
-// The number of values of a unit's chunk.
-__device__ __forceinline__ float chunk_count(const NormP &a, int64_t rows, int chunk, int len) {
-  const int64_t n = (int64_t)len - chunk * rows;
-  return (float)((n < 0 ? 0 : n < rows ? n : rows) * a.C);
-}
-
 // For each of a thread's rows (K1), or for its one row: the sum over the row.  `lds` takes SLOTS * NT / 64 floats.
 template <int NT, int SLOTS, bool K1>
 __device__ __forceinline__ void row_sums(const NormP &a, float (&v)[SLOTS], float *lds) {
@@ -140,7 +178,7 @@ __device__ __forceinline__ void row_sums(const NormP &a, float (&v)[SLOTS], floa
     for (int s = 1; s < SLOTS; ++s) v[s] = v[0];
     return;
   }
-  const int width = min(64, 1 << a.tpr_log2);
+  const int width = min(6, a.tpr_log2);
 #pragma unroll
   for (int s = 0; s < SLOTS; ++s) v[s] = wave_sum(v[s], width);
   if (a.tpr_log2 <= 6) return;
@@ -156,29 +194,49 @@ __device__ __forceinline__ void row_sums(const NormP &a, float (&v)[SLOTS], floa
   }
 }
 
+__device__ __forceinline__ float output_of(float x, float mean, float rstd, float w, float b, int silu) {
+  const float v = fmaf((x - mean) * rstd, w, b);
+  return silu ? v * sigmoid_fast(v) : v;
+}
+
+// Sums over each row, or over all rows (in every slot).
+template <int NT, int SLOTS, int MODE, bool K1> __device__ __forceinline__ void sums_of(const NormP &a, float (&v)[SLOTS], float *lds) {
+  if (MODE == STEP) {
+    row_sums<NT, SLOTS, K1>(a, v, lds);
+    return;
+  }
+#pragma unroll
+  for (int s = 1; s < SLOTS; ++s) v[0] += v[s];
+  v[0] = block_sum<NT>(v[0], lds);
+#pragma unroll
+  for (int s = 1; s < SLOTS; ++s) v[s] = v[0];
+}
+
 template <typename T, int VEC, int NT, int MODE, bool K1>
 __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
-  constexpr int SLOTS = Slots<T, VEC>::N;
+  constexpr int SLOTS = Slots<T, VEC, MODE, K1>::N;
   __shared__ float lds[2][SLOTS * (NT / 64)];
   auto w = where<T, VEC, K1>(a, MODE == STEP, NT);
-  const int chunk = (int)(blockIdx.x / ((unsigned)a.G * (unsigned)a.units));
-  Pack<T, VEC> x[SLOTS];
-  bool live[SLOTS];
+  float wt[VEC], bs[VEC];
+  if (K1) params<VEC>(a, w.channel(0) < a.C ? w.g * a.C + w.channel(0) : 0, wt, bs);
+  for (int loop = 0; loop < a.loops; ++loop, w.r0 += (int64_t)w.rp * a.R) {
+    Pack<T, VEC> x[SLOTS];
+    bool live[SLOTS];
 #pragma unroll
-  for (int s = 0; s < SLOTS; ++s) {
-    live[s] = w.live(s);
-    x[s] = fetch<T, VEC>(w, a.x, s, live[s]);
-  }
-  float mean[SLOTS], rstd[SLOTS];                            // (MODE == STEP: of each row; the same in all otherwise)
-  if (MODE == STEP) {
-    const float n = 1.f / (float)a.C;
+    for (int s = 0; s < SLOTS; ++s) {
+      live[s] = w.live(s);
+      x[s] = fetch<T, VEC>(w, a.x, s, live[s]);
+    }
+    float mean[SLOTS], rstd[SLOTS];                          // (WHOLE: the same in all)
+    const float n = MODE == STEP ? 1.f / (float)a.C : 1.f / fmaxf((float)((int64_t)w.len * a.C), 1.f);
+    if (MODE == STEP && loop) __syncthreads();               // (the sums of the loop before have been read)
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       mean[s] = 0.f;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) mean[s] += widen(x[s].v[v]);
     }
-    row_sums<NT, SLOTS, K1>(a, mean, lds[0]);
+    sums_of<NT, SLOTS, MODE, K1>(a, mean, lds[0]);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       mean[s] *= n;
@@ -189,71 +247,22 @@ __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
         rstd[s] = fmaf(e, e, rstd[s]);
       }
     }
-    row_sums<NT, SLOTS, K1>(a, rstd, lds[1]);
+    sums_of<NT, SLOTS, MODE, K1>(a, rstd, lds[1]);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       rstd[s] = __builtin_amdgcn_rsqf(fmaf(rstd[s], n, a.eps));
-      if (a.saved && w.col == 0 && (K1 || s == 0) && w.there(s)) a.saved[w.row(s) * a.G + w.g] = {mean[s], rstd[s]};
+      if (MODE == STEP && a.saved && w.col == 0 && (K1 || s == 0) && w.there(s)) a.saved[w.row(s) * a.G + w.g] = {mean[s], rstd[s]};
     }
-  } else {
-    const int64_t rows = (int64_t)w.rp * a.R;
-    const int64_t first = ((int64_t)w.unit * a.G + w.g) * a.nchunk;
-    float m, q = 0.f;
-    if (MODE != APPLY) {
-      const float n = MODE == WHOLE ? (float)((int64_t)w.len * a.C) : chunk_count(a, rows, chunk, w.len);
-      m = 0.f;
-#pragma unroll
-      for (int s = 0; s < SLOTS; ++s)
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) m += widen(x[s].v[v]);
-      m = block_sum<NT>(m, lds[0]) / fmaxf(n, 1.f);
-#pragma unroll
-      for (int s = 0; s < SLOTS; ++s)
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const float e = live[s] ? widen(x[s].v[v]) - m : 0.f;
-          q = fmaf(e, e, q);
-        }
-      q = block_sum<NT>(q, lds[1]);
-      if (MODE == SUMS) {
-        if (threadIdx.x == 0) a.part[first + chunk] = {m, q};
-        return;
-      }
-      q /= fmaxf(n, 1.f);
-    } else {
-      // mean of the chunks' means, each by its number; squares around it: a chunk's own, and its mean's distance
-      const float n = fmaxf((float)((int64_t)w.len * a.C), 1.f);
-      m = 0.f;
-      for (int c = threadIdx.x; c < a.nchunk; c += NT) m += a.part[first + c].x * (chunk_count(a, rows, c, w.len) / n);
-      m = block_sum<NT>(m, lds[0]);
-      for (int c = threadIdx.x; c < a.nchunk; c += NT) {
-        const float2 p = a.part[first + c];
-        const float k = chunk_count(a, rows, c, w.len);
-        q += k > 0.f ? p.y + k * (p.x - m) * (p.x - m) : 0.f;
-      }
-      q = block_sum<NT>(q, lds[1]) / n;
-    }
-    const float r = __builtin_amdgcn_rsqf(q + a.eps);
-    if (a.saved && chunk == 0 && threadIdx.x == 0) a.saved[(int64_t)w.unit * a.G + w.g] = {m, r};
+    if (MODE == WHOLE && a.saved && threadIdx.x == 0) a.saved[(int64_t)w.unit * a.G + w.g] = {mean[0], rstd[0]};
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
-      mean[s] = m;
-      rstd[s] = r;
-    }
-  }
-  float wt[VEC], bs[VEC];
-  if (K1) params<VEC>(a, w.channel(0) < a.C ? w.g * a.C + w.channel(0) : 0, wt, bs);
+      if (!w.there(s)) continue;
+      if (!K1) params<VEC>(a, w.g * a.C + w.channel(s), wt, bs);
+      Pack<T, VEC> y;
 #pragma unroll
-  for (int s = 0; s < SLOTS; ++s) {
-    if (!w.there(s)) continue;
-    if (!K1) params<VEC>(a, w.g * a.C + w.channel(s), wt, bs);
-    Pack<T, VEC> y;
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      const float u = fmaf((widen(x[s].v[v]) - mean[s]) * rstd[s], wt[v], bs[v]);
-      y.v[v] = narrow<T>(!live[s] ? 0.f : a.silu ? u * sigmoid_fast(u) : u);
+      for (int v = 0; v < VEC; ++v) y.v[v] = narrow<T>(live[s] ? output_of(widen(x[s].v[v]), mean[s], rstd[s], wt[v], bs[v], a.silu) : 0.f);
+      *(Pack<T, VEC> *)w.at(a.y, s) = y;
     }
-    *(Pack<T, VEC> *)w.at(a.y, s) = y;
   }
 }
 
@@ -261,8 +270,7 @@ __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
 template <int VEC, int NT> __device__ __forceinline__ void column_sums(const NormP &a, float (&acc)[VEC], float *lds) {
   const int tpr = 1 << a.tpr_log2, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-  for (int v = 0; v < VEC; ++v)
-    for (int o = tpr; o < 64; o <<= 1) acc[v] += __shfl_xor(acc[v], o);
+  for (int v = 0; v < VEC; ++v) acc[v] = wave_fold(acc[v], a.tpr_log2);
   const int sets = a.tpr_log2 <= 6 ? NT / 64 : NT >> a.tpr_log2, width = tpr;
   const int set = a.tpr_log2 <= 6 ? wave : (int)threadIdx.x >> a.tpr_log2, at = a.tpr_log2 <= 6 ? lane : (int)threadIdx.x & (tpr - 1);
   __syncthreads();
@@ -281,20 +289,21 @@ template <int VEC, int NT> __device__ __forceinline__ void column_sums(const Nor
 
 template <typename T, int VEC, int NT, int MODE, bool K1>
 __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
-  constexpr int SLOTS = Slots<T, VEC>::N;
+  constexpr int SLOTS = Slots<T, VEC, MODE, K1>::N;
   __shared__ float lds[2][SLOTS * (NT / 64)];
-  __shared__ float cols[MODE == APPLY ? 1 : NT * VEC];
+  __shared__ float cols[K1 ? NT * VEC : 1];
   auto w = where<T, VEC, K1>(a, MODE == STEP, NT);
   const int chunk = (int)(blockIdx.x / ((unsigned)a.G * (unsigned)a.units));
   float wt[VEC], bs[VEC], dw[VEC], db[VEC];
   if (K1) params<VEC>(a, w.channel(0) < a.C ? w.g * a.C + w.channel(0) : 0, wt, bs);
 #pragma unroll
   for (int v = 0; v < VEC; ++v) dw[v] = db[v] = 0.f;
-  float *const out = a.dpart + ((int64_t)w.unit * (a.nchunk / a.loops) + chunk) * 2 * a.D + (int64_t)w.g * a.C;
+  float *const out = a.dpart + ((int64_t)w.unit * a.blocks + chunk) * 2 * a.D + (int64_t)w.g * a.C;
+  const float n = MODE == STEP ? 1.f / (float)a.C : 1.f / fmaxf((float)((int64_t)w.len * a.C), 1.f);
   for (int loop = 0; loop < a.loops; ++loop, w.r0 += (int64_t)w.rp * a.R) {
     Pack<T, VEC> x[SLOTS], dy[SLOTS];
     bool live[SLOTS];
-    float mean[SLOTS], rstd[SLOTS];
+    float mean[SLOTS], rstd[SLOTS], s1[SLOTS], s2[SLOTS];
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       live[s] = w.live(s);
@@ -304,7 +313,7 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
       mean[s] = m.x;
       rstd[s] = m.y;
     }
-    float s1[SLOTS], s2[SLOTS];
+    if (MODE == STEP && loop) __syncthreads();               // (the sums of the loop before have been read)
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       s1[s] = s2[s] = 0.f;
@@ -319,8 +328,8 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
         dw[v] = fmaf(q, xh, dw[v]);
         db[v] += q;
       }
-      if (!K1 && MODE != APPLY && s % a.R == a.R - 1) {      // (a thread has these columns to itself)
-        if (w.channel(s) < a.C && s < a.K * a.R)
+      if (!K1) {                                             // (a thread has these columns to itself)
+        if (w.channel(s) < a.C && s < a.K)
 #pragma unroll
           for (int v = 0; v < VEC; ++v) {
             float *const o = out + w.channel(s) + v;
@@ -331,43 +340,10 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
         for (int v = 0; v < VEC; ++v) dw[v] = db[v] = 0.f;
       }
     }
-    if (MODE == STEP) {
-      __syncthreads();                                       // (the sums of the loop before have been read)
-      row_sums<NT, SLOTS, K1>(a, s1, lds[0]);
-      row_sums<NT, SLOTS, K1>(a, s2, lds[1]);
-      const float n = 1.f / (float)a.C;
-#pragma unroll
-      for (int s = 0; s < SLOTS; ++s) {
-        s1[s] *= n;
-        s2[s] *= n;
-      }
-    } else {
-      const float n = fmaxf((float)((int64_t)w.len * a.C), 1.f);
-      const int64_t first = ((int64_t)w.unit * a.G + w.g) * a.nchunk;
-      float p1 = 0.f, p2 = 0.f;
-      if (MODE != APPLY) {
-#pragma unroll
-        for (int s = 0; s < SLOTS; ++s) {
-          p1 += s1[s];
-          p2 += s2[s];
-        }
-      } else
-        for (int c = threadIdx.x; c < a.nchunk; c += NT) {
-          p1 += a.part[first + c].x;
-          p2 += a.part[first + c].y;
-        }
-      p1 = block_sum<NT>(p1, lds[0]);
-      p2 = block_sum<NT>(p2, lds[1]);
-      if (MODE == SUMS) {
-        if (threadIdx.x == 0) a.part[first + chunk] = {p1, p2};
-        break;
-      }
-#pragma unroll
-      for (int s = 0; s < SLOTS; ++s) {
-        s1[s] = p1 / n;
-        s2[s] = p2 / n;
-      }
-    }
+    keep_packed(x);
+    keep_packed(dy);
+    sums_of<NT, SLOTS, MODE, K1>(a, s1, lds[0]);
+    sums_of<NT, SLOTS, MODE, K1>(a, s2, lds[1]);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       if (!w.there(s)) continue;
@@ -378,12 +354,12 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
         const float xh = (widen(x[s].v[v]) - mean[s]) * rstd[s];
         float p;
         gradient_of(widen(dy[s].v[v]), xh, wt[v], bs[v], a.silu, p);
-        d.v[v] = narrow<T>(live[s] ? rstd[s] * (p - s1[s] - xh * s2[s]) : 0.f);
+        d.v[v] = narrow<T>(live[s] ? rstd[s] * (p - s1[s] * n - xh * (s2[s] * n)) : 0.f);
       }
       *(Pack<T, VEC> *)w.at(a.dx, s) = d;
     }
   }
-  if (MODE == APPLY || !K1) return;
+  if (!K1) return;
   column_sums<VEC, NT>(a, dw, cols);
   column_sums<VEC, NT>(a, db, cols);
   if ((int)threadIdx.x < (1 << a.tpr_log2) && w.col * VEC < a.C)
@@ -392,6 +368,250 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
       out[w.col * VEC + v] = dw[v];
       out[a.D + w.col * VEC + v] = db[v];
     }
+}
+
+// ---------------------------------------------------------------- chunks of a sequence
+constexpr int AHEAD = 4, AHEAD_BWD = 2;      // rows in flight a thread (reverse: of x and dy each)
+
+// A thread's column block k and its rows r0 + rsub + r rp, r < there, of which the first `live` exist in their sequence.
+template <typename T, int VEC> struct Run {
+  int unit, g, chunk, col, len, live, there, rp;
+  int64_t first;
+  __device__ __forceinline__ Run(const NormP &a, int nt) {
+    const unsigned rest = blockIdx.x / (unsigned)a.G;
+    g = (int)(blockIdx.x - rest * a.G);
+    chunk = (int)(rest / (unsigned)a.units);
+    unit = (int)(rest - (unsigned)chunk * a.units);
+    col = ((int)threadIdx.x & ((1 << a.tpr_log2) - 1)) * VEC;
+    rp = nt >> a.tpr_log2;
+    len = __builtin_amdgcn_readfirstlane(length_of(a.lengths, unit, a.T));
+    first = (int64_t)chunk * rp * a.R + ((int)threadIdx.x >> a.tpr_log2);
+    there = rows_before(a, a.T);
+    live = rows_before(a, len);
+  }
+  __device__ __forceinline__ int rows_before(const NormP &a, int end) const {
+    const int64_t n = ((int64_t)end - first + rp - 1) >> (31 - __builtin_clz(rp));
+    return n < 0 ? 0 : n < a.R ? (int)n : a.R;
+  }
+  template <typename R> __device__ __forceinline__ T *at(const NormP &a, const R &r, int channel) const {
+    return (T *)r.p + unit * r.sb + first * r.st + (int64_t)g * a.C + channel;
+  }
+};
+// Rows r .. r + AHEAD of those that exist; in the place of others the first row of the tensor, whose values are not used.
+template <typename T, int VEC, int N>
+__device__ __forceinline__ void fetch_rows(Pack<T, VEC> (&v)[N], const T *base, const void *any, int64_t step, int r, int n) {
+#pragma unroll
+  for (int u = 0; u < N; ++u) v[u] = *(const Pack<T, VEC> *)(r + u < n ? base + (r + u) * step : (const T *)any);
+}
+
+template <typename P, int N> __device__ __forceinline__ void take(P (&v)[N], const P (&from)[N]) {
+#pragma unroll
+  for (int u = 0; u < N; ++u) v[u] = from[u];
+}
+
+struct Moments {
+  float n, mean, m2;
+};
+// Both sets of values as one.
+__device__ __forceinline__ Moments joined(const Moments &p, const Moments &q) {
+  const float n = p.n + q.n, share = q.n > 0.f ? q.n / n : 0.f, d = q.n > 0.f ? q.mean - p.mean : 0.f;
+  return {n, fmaf(d, share, p.mean), p.m2 + q.m2 + d * d * p.n * share};
+}
+template <int NT> __device__ __forceinline__ Moments block_moments(Moments m, Moments *lds) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) m = joined(m, Moments{__shfl_xor(m.n, o), __shfl_xor(m.mean, o), __shfl_xor(m.m2, o)});
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = lds[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) m = joined(m, lds[w]);
+  return m;
+}
+
+// Forward: a chunk's mean and sum of squares around it.  A thread goes from vector to vector, each with its own mean.
+template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_moments_kernel(const NormP a) {
+  __shared__ Moments lds[NT / 64];
+  const Run<T, VEC> w(a, NT);
+  Moments m = {0.f, 0.f, 0.f};
+  for (int k = 0; k < a.K; ++k) {
+    const int c = (k << a.tpr_log2) * VEC + w.col, n = c < a.C ? w.live : 0;
+    const T *x = w.at(a, a.x, c);
+    for (int r = 0; r < n; r += AHEAD) {
+      Pack<T, VEC> v[AHEAD];
+      fetch_rows<T, VEC>(v, x, a.x.p, w.rp * a.x.st, r, n);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        float s = 0.f, q = 0.f;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s += widen(v[u].v[i]);
+        s *= 1.f / VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float e = widen(v[u].v[i]) - s;
+          q = fmaf(e, e, q);
+        }
+        const float count = m.n + VEC, share = VEC * rcp_fast(count), d = s - m.mean;
+        const bool on = r + u < n;
+        m.m2 = on ? m.m2 + q + d * d * m.n * share : m.m2;
+        m.mean = on ? fmaf(d, share, m.mean) : m.mean;
+        m.n = on ? count : m.n;
+      }
+    }
+  }
+  m = block_moments<NT>(m, lds);
+  if (threadIdx.x == 0) a.part[((int64_t)w.unit * a.G + w.g) * a.blocks + w.chunk] = {m.mean, m.m2};
+}
+
+// The number of values in a chunk of a unit.
+__device__ __forceinline__ float chunk_count(const NormP &a, int64_t rows, int chunk, int len) {
+  const int64_t n = (int64_t)len - chunk * rows;
+  return (float)((n < 0 ? 0 : n < rows ? n : rows) * a.C);
+}
+
+template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_output_kernel(const NormP a) {
+  __shared__ Moments lds[NT / 64];
+  const Run<T, VEC> w(a, NT);
+  const int64_t unit = (int64_t)w.unit * a.G + w.g;
+  const int c0 = min(w.col, a.C - VEC);
+  Pack<T, VEC> next[AHEAD];                                  // (on their way while the chunks are joined)
+  fetch_rows<T, VEC>(next, w.at(a, a.x, c0), a.x.p, w.rp * a.x.st, 0, w.live);
+  Moments m = {0.f, 0.f, 0.f};
+  for (int c = threadIdx.x; c < a.blocks; c += NT) {
+    const float2 p = a.part[unit * a.blocks + c];
+    m = joined(m, Moments{chunk_count(a, (int64_t)w.rp * a.R, c, w.len), p.x, p.y});
+  }
+  m = block_moments<NT>(m, lds);
+  const float mean = m.mean, rstd = __builtin_amdgcn_rsqf(m.m2 / fmaxf(m.n, 1.f) + a.eps);
+  if (a.saved && w.chunk == 0 && threadIdx.x == 0) a.saved[unit] = {mean, rstd};
+  for (int k = 0; k < a.K; ++k) {
+    const int c = (k << a.tpr_log2) * VEC + w.col;
+    if (c >= a.C) break;
+    float wt[VEC], bs[VEC];
+    params<VEC>(a, w.g * a.C + c, wt, bs);
+    const T *x = w.at(a, a.x, c);
+    T *y = w.at(a, a.y, c);
+    if (k) fetch_rows<T, VEC>(next, x, a.x.p, w.rp * a.x.st, 0, w.live);
+    for (int r = 0; r < w.there; r += AHEAD) {
+      Pack<T, VEC> v[AHEAD];
+      take(v, next);
+      if (r + AHEAD < w.live) fetch_rows<T, VEC>(next, x, a.x.p, w.rp * a.x.st, r + AHEAD, w.live);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        Pack<T, VEC> out;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) out.v[i] = narrow<T>(r + u < w.live ? output_of(widen(v[u].v[i]), mean, rstd, wt[i], bs[i], a.silu) : 0.f);
+        if (r + u < w.there) *(Pack<T, VEC> *)(y + (r + u) * (w.rp * a.y.st)) = out;
+      }
+    }
+  }
+}
+
+// Reverse: a chunk's sums of p and p xh, and of q xh and q over its rows.  xh = x rstd - mean rstd in one rounding: the rounding of
+// mean rstd moves xh by no more than the rounding of the mean does.
+template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_slopes_kernel(const NormP a) {
+  __shared__ float lds[2][NT / 64], cols[NT * VEC];
+  const Run<T, VEC> w(a, NT);
+  const int64_t unit = (int64_t)w.unit * a.G + w.g;
+  const float2 st = a.saved[unit];
+  const float shift = -st.x * st.y;
+  float *const out = a.dpart + ((int64_t)w.unit * a.blocks + w.chunk) * 2 * a.D + (int64_t)w.g * a.C;
+  float s1 = 0.f, s2 = 0.f;
+  for (int k = 0; k < a.K; ++k) {
+    const int c = (k << a.tpr_log2) * VEC + w.col, n = c < a.C ? w.live : 0;
+    float wt[VEC], bs[VEC], dw[VEC], db[VEC];
+    params<VEC>(a, c < a.C ? w.g * a.C + c : 0, wt, bs);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) dw[i] = db[i] = 0.f;
+    const T *x = w.at(a, a.x, c), *dy = w.at(a, a.dy, c);
+    for (int r = 0; r < n; r += AHEAD_BWD) {
+      Pack<T, VEC> v[AHEAD_BWD], d[AHEAD_BWD];
+      fetch_rows<T, VEC>(v, x, a.x.p, w.rp * a.x.st, r, n);
+      fetch_rows<T, VEC>(d, dy, a.dy.p, w.rp * a.dy.st, r, n);
+#pragma unroll
+      for (int u = 0; u < AHEAD_BWD; ++u)
+        if (r + u < n)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const float xh = fmaf(widen(v[u].v[i]), st.y, shift);
+            float p;
+            const float q = gradient_of(widen(d[u].v[i]), xh, wt[i], bs[i], a.silu, p);
+            dw[i] = fmaf(q, xh, dw[i]);
+            db[i] += q;
+          }
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {                          // (p = q w: its sums are those of q, channel by channel)
+      s1 = fmaf(db[i], wt[i], s1);
+      s2 = fmaf(dw[i], wt[i], s2);
+    }
+    if (a.K == 1) {
+      column_sums<VEC, NT>(a, dw, cols);
+      column_sums<VEC, NT>(a, db, cols);
+    }
+    if ((int)threadIdx.x < (1 << a.tpr_log2) && c < a.C)    // (of several column blocks a thread has its columns to itself)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        out[c + i] = dw[i];
+        out[a.D + c + i] = db[i];
+      }
+  }
+  s1 = block_sum<NT>(s1, lds[0]);
+  s2 = block_sum<NT>(s2, lds[1]);
+  if (threadIdx.x == 0) a.part[unit * a.blocks + w.chunk] = {s1, s2};
+}
+
+template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_gradient_kernel(const NormP a) {
+  __shared__ float lds[2][NT / 64];
+  const Run<T, VEC> w(a, NT);
+  const int64_t unit = (int64_t)w.unit * a.G + w.g;
+  const float2 st = a.saved[unit];
+  const float shift = -st.x * st.y;
+  const int c0 = min(w.col, a.C - VEC);
+  Pack<T, VEC> next[AHEAD_BWD], dnext[AHEAD_BWD];                    // (on their way while the chunks' sums are added)
+  fetch_rows<T, VEC>(next, w.at(a, a.x, c0), a.x.p, w.rp * a.x.st, 0, w.live);
+  fetch_rows<T, VEC>(dnext, w.at(a, a.dy, c0), a.dy.p, w.rp * a.dy.st, 0, w.live);
+  float s1 = 0.f, s2 = 0.f;
+  for (int c = threadIdx.x; c < a.blocks; c += NT) {
+    const float2 p = a.part[unit * a.blocks + c];
+    s1 += p.x;
+    s2 += p.y;
+  }
+  const float n = 1.f / fmaxf((float)((int64_t)w.len * a.C), 1.f);
+  s1 = block_sum<NT>(s1, lds[0]) * n;
+  s2 = block_sum<NT>(s2, lds[1]) * n;
+  for (int k = 0; k < a.K; ++k) {
+    const int c = (k << a.tpr_log2) * VEC + w.col;
+    if (c >= a.C) break;
+    float wt[VEC], bs[VEC];
+    params<VEC>(a, w.g * a.C + c, wt, bs);
+    const T *x = w.at(a, a.x, c), *dy = w.at(a, a.dy, c);
+    T *dx = w.at(a, a.dx, c);
+    if (k) {
+      fetch_rows<T, VEC>(next, x, a.x.p, w.rp * a.x.st, 0, w.live);
+      fetch_rows<T, VEC>(dnext, dy, a.dy.p, w.rp * a.dy.st, 0, w.live);
+    }
+    for (int r = 0; r < w.there; r += AHEAD_BWD) {
+      Pack<T, VEC> v[AHEAD_BWD], d[AHEAD_BWD];
+      take(v, next);
+      take(d, dnext);
+      if (r + AHEAD_BWD < w.live) {
+        fetch_rows<T, VEC>(next, x, a.x.p, w.rp * a.x.st, r + AHEAD_BWD, w.live);
+        fetch_rows<T, VEC>(dnext, dy, a.dy.p, w.rp * a.dy.st, r + AHEAD_BWD, w.live);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD_BWD; ++u) {
+        Pack<T, VEC> out;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float xh = fmaf(widen(v[u].v[i]), st.y, shift);
+          float p;
+          gradient_of(widen(d[u].v[i]), xh, wt[i], bs[i], a.silu, p);
+          out.v[i] = narrow<T>(r + u < w.live ? st.y * (p - s1 - xh * s2) : 0.f);
+        }
+        if (r + u < w.there) *(Pack<T, VEC> *)(dx + (r + u) * (w.rp * a.dx.st)) = out;
+      }
+    }
+  }
 }
 
 __global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__ part, int rows, int D, float *dweight, float *dbias) {
@@ -430,13 +650,12 @@ int norm_check(const snn_norm_args *a, bool grads) {
 
 // How a call is cut, for `vec` channels a vector.
 struct NormCut {
-  int nt, tpr_log2, K, R, loops, blocks;       // blocks: chunks a unit, by loops
-  int64_t nchunk;
+  int nt, tpr_log2, K, R, loops, blocks;       // threads; threads a row (log2); column blocks; rows a thread; lots; workgroups a unit and group
+  bool chunks;
 };
-int slots_of(int vec, size_t z) { return vec * z == 16 ? 8 : 16; }
-NormCut norm_cut(const snn_norm_args &a, int vec, bool backward) {
+NormCut norm_cut(const snn_norm_args &a, int vec) {
   const size_t z = a.type == SNN_TYPE_FP32 ? 4 : 2;
-  const int C = a.D / a.groups, slots = slots_of(vec, z);
+  const int C = a.D / a.groups, slots = vec * z == 16 ? 8 : 16;
   const int64_t rows = a.per_step ? (int64_t)a.T * a.B : a.T, units = a.per_step ? 1 : a.B;
   NormCut c;
   auto fit = [&](int nt) {
@@ -444,28 +663,28 @@ NormCut norm_cut(const snn_norm_args &a, int vec, bool backward) {
     c.tpr_log2 = 0;
     while ((vec << c.tpr_log2) < C && (1 << c.tpr_log2) < nt) ++c.tpr_log2;
     c.K = (C + (vec << c.tpr_log2) - 1) / (vec << c.tpr_log2);
-    c.R = c.K == 1 ? slots : a.per_step ? 1 : std::max(1, slots / c.K);
-    const int64_t each = (int64_t)(nt >> c.tpr_log2) * c.R;
-    c.nchunk = std::max<int64_t>(1, (rows + each - 1) / each);
   };
+  auto blocks_of = [&](int64_t each) { return std::max<int64_t>(1, (rows + each - 1) / each); };
   fit(256);
-  if (c.K > slots || (!a.per_step && c.nchunk > 1 && units * a.groups >= 128)) fit(1024);
-  if (!a.per_step && c.nchunk > 1 && c.nt == 1024 && c.K <= slots) {
-    const NormCut wide = c;
-    fit(256);
-    if (c.K > slots) c = wide;
-  }
-  if (a.per_step && c.K == 1)                    // (few rows: fewer a thread, more workgroups)
-    while (c.R > 1 && c.nchunk * a.groups < 512) {
-      c.R /= 2;
-      const int64_t each = (int64_t)(c.nt >> c.tpr_log2) * c.R;
-      c.nchunk = std::max<int64_t>(1, (rows + each - 1) / each);
-    }
   c.loops = 1;
-  if (a.per_step && backward)                    // (fewer rows of partial sums, as long as the chip is filled)
-    while (c.loops < 32 && c.nchunk / (c.loops * 2) * a.groups >= 1024) c.loops *= 2;
-  c.blocks = (int)((c.nchunk + c.loops - 1) / c.loops);
-  c.nchunk = (int64_t)c.blocks * c.loops;
+  c.chunks = false;
+  if (a.per_step) {
+    if (c.K > slots) fit(1024);                // (16384 channels one by one)
+    const int64_t rp = c.nt >> c.tpr_log2;
+    c.R = c.K == 1 && blocks_of(rp * 2) * a.groups >= 512 ? 2 : 1;
+    int64_t n = blocks_of(rp * c.R);
+    while (c.loops < 64 && blocks_of(rp * c.R * c.loops * 2) * a.groups >= 2048) c.loops *= 2;
+    c.blocks = (int)((n + c.loops - 1) / c.loops);
+    return c;
+  }
+  const int64_t rp = c.nt >> c.tpr_log2;
+  c.R = slots;
+  c.blocks = 1;
+  if (c.K == 1 && blocks_of(rp * slots) == 1) return c;
+  c.chunks = true;
+  c.R = 64;                                    // rows a thread: as many as leave workgroups enough
+  while (c.R > AHEAD && blocks_of(rp * c.R) * units * a.groups < 1024) c.R /= 2;
+  c.blocks = (int)blocks_of(rp * c.R);
   return c;
 }
 int norm_vector(const snn_norm_args &a, const snn_norm_grads *g) {
@@ -477,39 +696,64 @@ int norm_vector(const snn_norm_args &a, const snn_norm_grads *g) {
   return 1;
 }
 // The workspace does not depend on the pointers, which decide how many channels a vector has.
+size_t part_bytes(const snn_norm_args &a, const NormCut &c) { return c.chunks ? rup256((size_t)a.B * a.groups * c.blocks * 8) : 0; }
 size_t norm_bytes(const snn_norm_args &a, bool backward) {
   size_t most = 0;
   for (int vec : {a.type == SNN_TYPE_FP32 ? 4 : 8, 2, 1}) {
-    const NormCut c = norm_cut(a, vec, backward);
-    const size_t units = a.per_step ? 1 : a.B;
-    const size_t part = !a.per_step && c.nchunk > 1 ? rup256(units * a.groups * c.nchunk * 8) : 0;
-    most = std::max(most, part + (backward ? rup256(units * c.blocks * 2 * (size_t)a.D * 4) : 0));
+    const NormCut c = norm_cut(a, vec);
+    most = std::max(most, part_bytes(a, c) + (backward ? rup256((size_t)(a.per_step ? 1 : a.B) * c.blocks * 2 * (size_t)a.D * 4) : 0));
   }
   return most;
 }
 
-template <typename F> int with_vector(const snn_norm_args &a, int vec, const NormCut &c, F f) {
-  auto deep = [&](auto t, auto v) {
-    auto k = [&](auto nt) { return c.K == 1 ? f(t, v, nt, std::true_type()) : f(t, v, nt, std::false_type()); };
-    return c.nt == 256 ? k(std::integral_constant<int, 256>()) : k(std::integral_constant<int, 1024>());
-  };
+template <typename F> int with_vector(const snn_norm_args &a, int vec, F f) {
   using std::integral_constant;
   if (a.type == SNN_TYPE_FP32)
-    return vec == 4 ? deep(float(), integral_constant<int, 4>()) : vec == 2 ? deep(float(), integral_constant<int, 2>()) : deep(float(), integral_constant<int, 1>());
-  return vec == 8 ? deep(__bf16(), integral_constant<int, 8>()) : vec == 2 ? deep(__bf16(), integral_constant<int, 2>()) : deep(__bf16(), integral_constant<int, 1>());
+    return vec == 4 ? f(float(), integral_constant<int, 4>()) : vec == 2 ? f(float(), integral_constant<int, 2>()) : f(float(), integral_constant<int, 1>());
+  return vec == 8 ? f(__bf16(), integral_constant<int, 8>()) : vec == 2 ? f(__bf16(), integral_constant<int, 2>()) : f(__bf16(), integral_constant<int, 1>());
 }
 
 NormP norm_args(const snn_norm_args &a, const NormCut &c, void *saved, void *workspace) {
-  NormP p{a.T, a.B, a.D, a.groups, a.D / a.groups, a.silu, a.eps, a.per_step ? (int64_t)a.T * a.B : a.T, a.per_step ? 1 : a.B, (int)c.nchunk, c.loops,
-          c.tpr_log2, c.K, c.R, Rows<void>(a.x, a.T), Rows<void>(a.y, a.T), a.weight, a.bias, a.lengths, (float2 *)saved, (float2 *)workspace,
-          Rows<void>(snn_rows{}), Rows<void>(snn_rows{}), nullptr};
-  return p;
+  return NormP{a.T, a.B, a.D, a.groups, a.D / a.groups, a.silu, a.eps, a.per_step ? (int64_t)a.T * a.B : a.T, a.per_step ? 1 : a.B, c.blocks, c.loops,
+               c.tpr_log2, c.K, c.R, Rows<void>(a.x, a.T), Rows<void>(a.y, a.T), a.weight, a.bias, a.lengths, (float2 *)saved, (float2 *)workspace,
+               Rows<void>(snn_rows{}), Rows<void>(snn_rows{}), nullptr};
 }
 int norm_grid(const snn_norm_args &a, const NormCut &c, dim3 &grid) {
   const int64_t n = (int64_t)a.groups * (a.per_step ? 1 : a.B) * c.blocks;
   if (n * c.nt >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "group norm: too large for one launch");
   grid = dim3((unsigned)n);
   return SNN_OK;
+}
+
+template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
+  if (!per_step) {
+    if (!c.chunks) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, WHOLE, true>), grid, dim3(256), 0, st, p);
+    else {
+      hipLaunchKernelGGL((norm_moments_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
+      const int e = ops_launched("group norm, moments");
+      if (e) return e;
+      hipLaunchKernelGGL((norm_output_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
+    }
+  } else if (c.K == 1) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, STEP, true>), grid, dim3(256), 0, st, p);
+  else if (c.nt == 256) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, STEP, false>), grid, dim3(256), 0, st, p);
+  else if constexpr (256 * V * Slots<T, V, STEP, false>::N < MOST_CHANNELS)
+    hipLaunchKernelGGL((norm_forward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
+  return ops_launched("group norm");
+}
+template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
+  if (!per_step) {
+    if (!c.chunks) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, WHOLE, true>), grid, dim3(256), 0, st, p);
+    else {
+      hipLaunchKernelGGL((norm_slopes_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
+      const int e = ops_launched("group norm backward, sums");
+      if (e) return e;
+      hipLaunchKernelGGL((norm_gradient_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
+    }
+  } else if (c.K == 1) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, STEP, true>), grid, dim3(256), 0, st, p);
+  else if (c.nt == 256) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, STEP, false>), grid, dim3(256), 0, st, p);
+  else if constexpr (256 * V * Slots<T, V, STEP, false>::N < MOST_CHANNELS)
+    hipLaunchKernelGGL((norm_backward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
+  return ops_launched("group norm backward");
 }
 
 }  // namespace
@@ -544,25 +788,11 @@ int32_t snn_norm_forward(const snn_norm_args *a, void *saved, void *workspace, s
     return ops_fail(SNN_ERR_WORKSPACE, "group norm: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
   if (a->T == 0) return SNN_OK;
   const int vec = norm_vector(*a, nullptr);
-  const NormCut c = norm_cut(*a, vec, false);
+  const NormCut c = norm_cut(*a, vec);
   dim3 grid;
   if ((rc = norm_grid(*a, c, grid))) return rc;
   const NormP p = norm_args(*a, c, saved, workspace);
-  const hipStream_t st = (hipStream_t)stream;
-  return with_vector(*a, vec, c, [&](auto t, auto v, auto nt, auto k1) {
-    using T = decltype(t);
-    constexpr int V = v.value, N = nt.value;
-    constexpr bool K1 = decltype(k1)::value;
-    if (a->per_step) hipLaunchKernelGGL((norm_forward_kernel<T, V, N, STEP, K1>), grid, dim3(N), 0, st, p);
-    else if (c.nchunk == 1) hipLaunchKernelGGL((norm_forward_kernel<T, V, N, WHOLE, K1>), grid, dim3(N), 0, st, p);
-    else {
-      hipLaunchKernelGGL((norm_forward_kernel<T, V, N, SUMS, K1>), grid, dim3(N), 0, st, p);
-      const int e = ops_launched("group norm, sums");
-      if (e) return e;
-      hipLaunchKernelGGL((norm_forward_kernel<T, V, N, APPLY, K1>), grid, dim3(N), 0, st, p);
-    }
-    return ops_launched("group norm");
-  });
+  return with_vector(*a, vec, [&](auto t, auto v) { return launch_norm<decltype(t), v.value>(c, a->per_step, p, grid, (hipStream_t)stream); });
 }
 
 int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const void *saved, void *workspace, size_t workspace_bytes, void *stream) {
@@ -577,34 +807,17 @@ int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < need)
     return ops_fail(SNN_ERR_WORKSPACE, "group norm backward: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
   const int vec = norm_vector(*a, g);
-  const NormCut c = norm_cut(*a, vec, true);
+  const NormCut c = norm_cut(*a, vec);
   dim3 grid;
   if ((rc = norm_grid(*a, c, grid))) return rc;
   NormP p = norm_args(*a, c, const_cast<void *>(saved), workspace);
-  const int units = p.units;
   p.dy = Rows<void>(g->dy, a->T);
   p.dx = Rows<void>(g->dx, a->T);
-  p.dpart = (float *)((char *)workspace + (!a->per_step && c.nchunk > 1 ? rup256((size_t)units * a->groups * c.nchunk * 8) : 0));
+  p.dpart = (float *)((char *)workspace + part_bytes(*a, c));
   const hipStream_t st = (hipStream_t)stream;
-  if (a->T > 0) {
-    rc = with_vector(*a, vec, c, [&](auto t, auto v, auto nt, auto k1) {
-      using T = decltype(t);
-      constexpr int V = v.value, N = nt.value;
-      constexpr bool K1 = decltype(k1)::value;
-      if (a->per_step) hipLaunchKernelGGL((norm_backward_kernel<T, V, N, STEP, K1>), grid, dim3(N), 0, st, p);
-      else if (c.nchunk == 1) hipLaunchKernelGGL((norm_backward_kernel<T, V, N, WHOLE, K1>), grid, dim3(N), 0, st, p);
-      else {
-        hipLaunchKernelGGL((norm_backward_kernel<T, V, N, SUMS, K1>), grid, dim3(N), 0, st, p);
-        const int e = ops_launched("group norm backward, sums");
-        if (e) return e;
-        hipLaunchKernelGGL((norm_backward_kernel<T, V, N, APPLY, K1>), grid, dim3(N), 0, st, p);
-      }
-      return ops_launched("group norm backward");
-    });
-    if (rc) return rc;
-  }
+  if (a->T > 0 && (rc = with_vector(*a, vec, [&](auto t, auto v) { return launch_norm_backward<decltype(t), v.value>(c, a->per_step, p, grid, st); }))) return rc;
   if (!g->dweight && !g->dbias) return SNN_OK;
-  hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((2 * (int64_t)a->D + 15) / 16)), dim3(256), 0, st, p.dpart, a->T > 0 ? units * c.blocks : 0, a->D, g->dweight,
+  hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((2 * (int64_t)a->D + 15) / 16)), dim3(256), 0, st, p.dpart, a->T > 0 ? p.units * c.blocks : 0, a->D, g->dweight,
                      g->dbias);
   return ops_launched("group norm backward, gradients of the parameters");
 }

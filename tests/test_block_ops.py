@@ -199,6 +199,11 @@ NORM = [  # T, B, D, groups, type, silu, per_step, lengths, weight, bias
     (30, 2, 3001, 1, "fp32", False, False, "some", True, True),
     (5, 1, 16384, 1, "bf16", True, False, "none", True, True),
     (3, 1, 16383, 1, "fp32", True, False, "none", True, True),
+    (5, 2, 16383, 1, "bf16", True, True, "some", True, True),            # as many channels as there may be, each alignment
+    (5, 2, 16382, 1, "fp32", True, True, "some", True, True),
+    (5, 2, 16384, 1, "fp32", True, True, "some", True, True),
+    (5, 2, 16384, 1, "bf16", True, True, "some", True, True),
+    (5, 2, 16382, 1, "bf16", False, False, "some", True, True),
     (600, 2, 64, 2, "fp32", True, False, "some", True, True),            # several chunks a sequence
     (2000, 1, 72, 1, "bf16", True, False, "none", True, True),
     (300, 66, 128, 2, "bf16", True, False, "some", True, True),          # one chunk of a wide workgroup
