@@ -18,6 +18,7 @@
 namespace snn {
 namespace {
 
+constexpr int WIDE_WM = 2, WIDE_WN = 4, WIDE_SK = 64, WIDE_NS = 2;      // wavefronts of a wide tile
 constexpr int KS = 64;                       // k of a stage: a row of it is 128 bytes
 
 // One side of a product: stage `kp` of plane `plane`, row r at p + r row + kp stage + plane plane (bytes).
@@ -44,7 +45,7 @@ struct GemmP {
   Steps steps;
   Rows<void> out = Rows<void>(snn_rows{});   // y or dx
   void *w0, *w1;                             // dgate, dup
-  float *part;                               // [splits][rows of a][pitch]: sums of a part, or G and U ([2][rows][pitch])
+  float *part;                               // [splits][rows of a][pitch]: sums of a part; UNITS: G and U, or NULL
   int pitch, act;
   int M, N;                                  // rows of a; columns (units)
 };
@@ -65,6 +66,12 @@ __device__ __forceinline__ float act_slope(int act, float g) {
   return 0.5f * (1.f + erf_of(g * 0.70710678118654752f)) + g * 0.3989422804014327f * exp_fast(-0.5f * g * g);
 }
 
+// G and U of 32 rows by 32 units as the accumulators hold them, which is how they are kept for the reverse pass: [G, U][g][lane][4],
+// row lane % 32, unit 8 g + 4 (lane / 32) + 0..3.  (Every store of a wavefront is one KiB; row by row it would be 32 pieces of 32
+// bytes, and the forward pass with them took 180 us longer where memory needs 50: 8192 rows, 4096 units.)
+constexpr int KEPT = 32 * 32 * 2;
+__host__ __device__ inline int64_t kept_block(int mb, int fb, int F) { return ((int64_t)mb * ((F + 31) / 32) + fb) * KEPT; }
+
 // Four neighbouring values of a row from column n on.
 template <typename T> __device__ __forceinline__ void give4(T *row, int n, int N, bool wide, const float (&v)[4]) {
   if (wide && n + 4 <= N) {
@@ -79,11 +86,15 @@ template <typename T> __device__ __forceinline__ void give4(T *row, int n, int N
 }
 
 // WM x WN wavefronts, each TM x TN blocks of 32 x 32 (m x n).  T: the type of what comes out.
-template <typename T, int WHAT, int WM, int WN, int TM, int TN>
+template <typename T, int WHAT, int WM, int WN, int TM, int TN, int SK, int NS>
 __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
-  constexpr int NW = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, AI = BM / 8 / NW, BI = BN / 8 / NW;
-  constexpr int STAGE = (BM + BN) * 128;
-  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (WHAT != UNITS || TN % 2 == 0), "whole loads; gate and up in one wavefront");
+  // SK: k of a stage; a row of it is RB bytes, RC chunks of 16, and a load of a wavefront brings RPL rows.  NS: stages in LDS
+  constexpr int RB = 2 * SK, RC = RB / 16, RPL = 64 / RC, QS = SK / 16, PER = KS / SK;
+  constexpr int NW = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, AI = BM / RPL / NW, BI = BN / RPL / NW;
+  constexpr int STAGE = (BM + BN) * RB;
+  // chunk c of row r lies at place c ^ turn(r): 16 rows that are read together touch every bank once
+  auto turn = [](int r) { return SK == 64 ? (r >> 1) & 7 : (r >> 2) & 3; };
+  static_assert(BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0 && (WHAT != UNITS || TN % 2 == 0), "whole loads; gate and up in one wavefront");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
@@ -100,38 +111,48 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
   const int tm = band * 8 + in % high, tn = in / high;
   const int m0 = tm * BM, n0 = tn * (WHAT == UNITS ? BN / 2 : BN);
 
-  // what a lane loads: 16 bytes, chunk lane % 8 of row lane / 8 of eight; the chunk is the one that belongs at this place of the LDS
+  // what a lane loads: 16 bytes of row lane / RC of a load's rows, the chunk that belongs at this place of the LDS
   int av[AI], bv[BI];
 #pragma unroll
   for (int q = 0; q < AI; ++q) {
-    const int r = 8 * (wave + NW * q) + lane / 8, c = (lane & 7) ^ ((r >> 1) & 7);
+    const int r = RPL * (wave + NW * q) + lane / RC, c = (lane % RC) ^ turn(r);
     av[q] = m0 + r < a.a.rows ? (int)(r * a.a.row) + c * 16 : ROW_NOWHERE;
   }
 #pragma unroll
   for (int q = 0; q < BI; ++q) {
-    const int r = 8 * (wave + NW * q) + lane / 8, c = (lane & 7) ^ ((r >> 1) & 7);
+    const int r = RPL * (wave + NW * q) + lane / RC, c = (lane % RC) ^ turn(r);
     const int rr = WHAT == UNITS ? (r >> 6) * 32 + (r & 31) : r;
     bv[q] = n0 + rr < a.b.rows ? (int)(rr * a.b.row) + c * 16 : ROW_NOWHERE;
   }
-  const int stages = a.panels * a.segs, first = (int)((int64_t)stages * split / a.splits), last = (int)((int64_t)stages * (split + 1) / a.splits);
+  const int panels = a.panels * PER, stages = panels * a.segs, first = (int)((int64_t)stages * split / a.splits), last = (int)((int64_t)stages * (split + 1) / a.splits);
   const char *const pa = a.a.p + (int64_t)m0 * a.a.row, *const pb = a.b.p + (int64_t)n0 * a.b.row,
              *const pu = WHAT == UNITS ? a.b.p2 + (int64_t)n0 * a.b.row : nullptr;
   const unsigned lds0 = (unsigned)(uintptr_t)(lds_ptr_t)lds;
-  int seg = first / a.panels, kp = first - seg * a.panels;
-  auto issue = [&](int buf) {
-    const int64_t at_a = segment_a(seg, a.segs) * a.a.plane + kp * a.a.stage, at_b = segment_b(seg, a.segs) * a.b.plane + kp * a.b.stage;
-    const u32x4 ra = raw_rsrc(pa + at_a, ROW_SPAN), rb = raw_rsrc(pb + at_b, ROW_SPAN), ru = WHAT == UNITS ? raw_rsrc(pu + at_b, ROW_SPAN) : rb;
-    const unsigned dst = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + wave * 1024);
-#pragma unroll
-    for (int q = 0; q < AI; ++q) load_to_lds_b128(ra, dst + q * NW * 1024, av[q], 0);
-#pragma unroll
-    for (int q = 0; q < BI; ++q) {
-      const bool up = WHAT == UNITS && ((8 * (wave + NW * q)) & 32);
-      load_to_lds_b128(up ? ru : rb, dst + BM * 128 + q * NW * 1024, bv[q], 0);
-    }
-    if (++kp == a.panels) {
+  int seg = first / panels, kp = first - seg * panels, asked_to = first;
+  struct Asked {                             // scalar operands of a stage's loads
+    u32x4 a, b, up;
+    unsigned dst;
+  } asked;
+  auto prepare = [&](int buf) {              // (behind the last stage: buffers of no size, so that the number of loads stays the same)
+    const int64_t at = kp / PER, in_row = (kp % PER) * RB;
+    const int64_t at_a = segment_a(seg, a.segs) * a.a.plane + at * a.a.stage + in_row, at_b = segment_b(seg, a.segs) * a.b.plane + at * a.b.stage + in_row;
+    const unsigned size = asked_to < last ? ROW_SPAN : 0;
+    asked.a = raw_rsrc(pa + at_a, size);
+    asked.b = raw_rsrc(pb + at_b, size);
+    asked.up = WHAT == UNITS ? raw_rsrc(pu + at_b, size) : asked.b;
+    asked.dst = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + wave * 1024);
+    ++asked_to;
+    if (++kp == panels) {
       kp = 0;
       ++seg;
+    }
+  };
+  auto load = [&](int q) {                   // load q of AI + BI
+    if (q < AI) load_to_lds_b128(asked.a, asked.dst + q * NW * 1024, av[q < AI ? q : 0], 0);
+    else {
+      const int p = q - AI;
+      const bool up = WHAT == UNITS && ((RPL * (wave + NW * p)) & 32);
+      load_to_lds_b128(up ? asked.up : asked.b, asked.dst + BM * RB + p * NW * 1024, bv[p], 0);
     }
   };
 
@@ -144,36 +165,76 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
   const int h = lane >> 5, ra = wm * TM * 32 + (lane & 31), rb = wn * TN * 32 + (lane & 31);
-  int fa[KS / 16], fb[KS / 16];
+  int fa[QS], fb[QS];
 #pragma unroll
-  for (int s = 0; s < KS / 16; ++s) {
-    fa[s] = ra * 128 + (((2 * s + h) ^ ((ra >> 1) & 7)) << 4);
-    fb[s] = BM * 128 + rb * 128 + (((2 * s + h) ^ ((rb >> 1) & 7)) << 4);
+  for (int s = 0; s < QS; ++s) {
+    fa[s] = ra * RB + (((2 * s + h) ^ turn(ra)) << 4);
+    fb[s] = BM * RB + rb * RB + (((2 * s + h) ^ turn(rb)) << 4);
   }
-  if (first < last) issue(0);
-  for (int kt = first, buf = 0; kt < last; ++kt, buf ^= 1) {
+  // Stage by stage, a step (16 k) at a time.  The last step is multiplied behind the next stage's barrier, out of registers, so that
+  // the matrix units have work while that stage's first fragments arrive; every other step's fragments are read under the
+  // step before, and the loads of a later stage go out from the first step on.  An MFMA keeps the matrix unit for 32 cycles, in which
+  // a wavefront can issue about one of these: the order is fixed by hand, one behind each MFMA.
+  constexpr int Q = TM * TN, LOADS = AI + BI, EVERY = QS * Q / 2 / LOADS < 1 ? 1 : QS * Q / 2 / LOADS;
+  static_assert(LOADS <= QS * Q && TM + TN <= Q, "a place for every load and read");
+  bf16x8 xa[2][TM], xb[2][TN];
+  auto read = [&](const char *st, int s, int f) {            // fragment f of step s
+    if (f < TN) xb[s & 1][f < TN ? f : 0] = *(const bf16x8 *)(st + fb[s] + f * 32 * RB);
+    else xa[s & 1][f - TN < TM ? f - TN : 0] = *(const bf16x8 *)(st + fa[s] + (f - TN) * 32 * RB);
+  };
+  const bf16x8 none = {};
+#pragma unroll
+  for (int i = 0; i < TM; ++i) xa[1][i] = none;
+#pragma unroll
+  for (int j = 0; j < TN; ++j) xb[1][j] = none;
+#pragma unroll
+  for (int n = 0; n < NS - 1; ++n) {
+    prepare(n);
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) load(q);
+  }
+  for (int kt = first, buf = 0; kt < last; ++kt) {
     // this wavefront's loads of the stage have landed, and behind the barrier everyone's; everyone has left the stage before
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * LOADS) : "memory");
     lds_barrier();
-    if (kt + 1 < last) issue(buf ^ 1);
     const char *st = lds + buf * STAGE;
-#pragma unroll
-    for (int s = 0; s < KS / 16; ++s) {
-      bf16x8 xa[TM], xb[TN];
-#pragma unroll
-      for (int i = 0; i < TM; ++i) xa[i] = *(const bf16x8 *)(st + fa[s] + i * 32 * 128);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) xb[j] = *(const bf16x8 *)(st + fb[s] + j * 32 * 128);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j], xa[i], acc[i][j], 0, 0, 0);
-    }
+    prepare(buf ? buf - 1 : NS - 1);
+    buf = buf + 1 < NS ? buf + 1 : 0;
+    static_for<QS * Q>([&](auto X) {
+      constexpr int x = decltype(X)::value, g = x / Q, y = x % Q, s = (g + QS - 1) % QS, i = y / TN, j = y % TN;
+      __builtin_amdgcn_sched_barrier(0);
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[s & 1][j], xa[s & 1][i], acc[i][j], 0, 0, 0);
+      if constexpr (2 * y < TM + TN) read(st, g, 2 * y);
+      if constexpr (2 * y + 1 < TM + TN) read(st, g, 2 * y + 1);
+      if constexpr (x % EVERY == EVERY - 1 && x / EVERY < LOADS) load(x / EVERY);
+    });
   }
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (no load outlives the workgroup's LDS)
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[1][j], xa[1][i], acc[i][j], 0, 0, 0);
 
   // A lane holds, of block (i, j), row m = lane % 32 and columns 8 g + 4 h + 0..3 in element 4 g + 0..3.
   const bool wide_out = WHAT == UNITS || WHAT == DX ? ((uintptr_t)a.out.p | (uintptr_t)(a.out.st * (int64_t)sizeof(T)) | (uintptr_t)(a.out.sb * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0
                         : ((uintptr_t)a.w0 | (uintptr_t)a.w1 | (uintptr_t)((int64_t)a.N * sizeof(T))) % (4 * sizeof(T)) == 0;
+  if (WHAT == UNITS && a.part)
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN / 2; ++j) {
+        const int mb = m0 / 32 + wm * TM + i, fb = n0 / 32 + wn * TN / 2 + j;
+        if (mb * 32 >= a.M || fb * 32 >= a.N) continue;
+        float *const at = a.part + kept_block(mb, fb, a.N) + lane * 4;
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const f32x16 &v = acc[i][2 * j + w];
+            *(Pack<float, 4> *)(at + (w * 4 + g) * 256) = {{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]}};
+          }
+      }
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int m = m0 + (wm * TM + i) * 32 + (lane & 31);
@@ -189,19 +250,9 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
           const int n = n0 + (wn * TN / 2 + j) * 32 + 8 * g + 4 * h;
           if (n >= a.N) continue;
           float y[4];
-          Pack<float, 4> kg, ku;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float vg = acc[i][2 * j][4 * g + k], vu = acc[i][2 * j + 1][4 * g + k];
-            kg.v[k] = vg;
-            ku.v[k] = vu;
-            y[k] = live ? act_of(a.act, vg) * vu : 0.f;
-          }
+          for (int k = 0; k < 4; ++k) y[k] = live ? act_of(a.act, acc[i][2 * j][4 * g + k]) * acc[i][2 * j + 1][4 * g + k] : 0.f;
           give4<T>(row, n, a.N, wide_out, y);
-          if (a.part) {
-            *(Pack<float, 4> *)(a.part + (int64_t)m * a.pitch + n) = kg;
-            *(Pack<float, 4> *)(a.part + ((int64_t)a.M + m) * a.pitch + n) = ku;
-          }
         }
     } else {
       int t = 0, b = 0;
@@ -341,49 +392,73 @@ template <typename T> __global__ __launch_bounds__(256) void lay_transposed_kern
 struct SlopeP {
   Steps steps;
   Rows<void> dy;
-  const float *g, *u;
-  int pitch, act, M, F, panels;              // panels: of F
+  const float *kept;
+  int act, M, F, panels, wide;               // panels: of F; wide: dy eight at a time
   char *rows, *cols;
   int64_t rows_stage, rows_plane, cols_stage, cols_plane;
 };
 template <typename T> __global__ __launch_bounds__(256) void slope_kernel(const SlopeP a) {
-  __shared__ T tile[2][KS][KS + 1];
-  const int m0 = blockIdx.x * KS, f0 = blockIdx.y * KS, c = threadIdx.x & 63;
-#pragma unroll 4
-  for (int v = 0; v < 16; ++v) {
-    const int r = v * 4 + threadIdx.x / 64, m = m0 + r;
-    float dg = 0.f, du = 0.f;
-    if (m < a.M && f0 + c < a.F) {
-      int t, b;
-      if (a.steps.live(m, t, b)) {
-        const float d = widen(((const T *)a.dy.p)[t * a.dy.st + b * a.dy.sb + f0 + c]);
-        const float g = a.g[(int64_t)m * a.pitch + f0 + c], u = a.u[(int64_t)m * a.pitch + f0 + c];
-        dg = d * u * act_slope(a.act, g);
-        du = d * act_of(a.act, g);
-      }
-    }
-    tile[0][r][c] = narrow<T>(dg);
-    tile[1][r][c] = narrow<T>(du);
+  __shared__ T tile[2][KS][KS + 1];          // dy stands in the first one at the start
+  const int m0 = blockIdx.x * KS, f0 = blockIdx.y * KS, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int mb = m0 / 32 + (wave & 1), fb = f0 / 32 + (wave >> 1), h = lane >> 5, r = (wave & 1) * 32 + (lane & 31), c = (wave >> 1) * 32 + 4 * h;
+  const bool there = mb * 32 < a.M && fb * 32 < a.F;
+  Pack<float, 4> g[4], u[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float *at = a.kept + (there ? kept_block(mb, fb, a.F) : 0) + q * 256 + lane * 4;
+    g[q] = *(const Pack<float, 4> *)at;
+    u[q] = *(const Pack<float, 4> *)(at + 1024);
   }
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    const int row = (threadIdx.x + 256 * v) / 8, k0 = (threadIdx.x & 7) * 8, m = m0 + row;
+    int t = 0, b = 0;
+    const bool live = m < a.M && a.steps.live(m, t, b);
+    const T *dy = (const T *)a.dy.p + t * a.dy.st + b * a.dy.sb + f0 + k0;
+    Pack<T, 8> d = {};
+    if (live && a.wide && f0 + k0 + 8 <= a.F) d = *(const Pack<T, 8> *)dy;
+    else if (live)
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (f0 + k0 + k < a.F) d.v[k] = dy[k];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tile[0][row][k0 + k] = d.v[k];
+  }
+  __syncthreads();
+  bool live = false;
+  if (m0 + r < a.M) {
+    int t, b;
+    live = a.steps.live(m0 + r, t, b);
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {            // (every place is its own lane's)
+      const bool on = live && f0 + c + 8 * q + k < a.F;
+      T &at = tile[0][r][c + 8 * q + k];
+      const float d = widen(at), gv = g[q].v[k];
+      at = narrow<T>(on ? d * u[q].v[k] * act_slope(a.act, gv) : 0.f);
+      tile[1][r][c + 8 * q + k] = narrow<T>(on ? d * act_of(a.act, gv) : 0.f);
+    }
   __syncthreads();
   constexpr int P = Pieces<T>::N;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
-      const int r = (threadIdx.x + 256 * v) / 8, k0 = (threadIdx.x & 7) * 8;
+      const int row = (threadIdx.x + 256 * v) / 8, k0 = (threadIdx.x & 7) * 8;
       Chunk out[P];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         __bf16 p[P];
-        Pieces<T>::split(tile[w][r][k0 + k], p);
+        Pieces<T>::split(tile[w][row][k0 + k], p);
 #pragma unroll
         for (int q = 0; q < P; ++q) out[q].v[k] = p[q];
       }
-      if (m0 + r < a.M)
+      if (m0 + row < a.M)
 #pragma unroll
         for (int q = 0; q < P; ++q)
-          *(Chunk *)(a.rows + q * a.rows_plane + (w * a.panels + blockIdx.y) * a.rows_stage + (int64_t)(m0 + r) * 128 + (threadIdx.x & 7) * 16) = out[q];
+          *(Chunk *)(a.rows + q * a.rows_plane + (w * a.panels + blockIdx.y) * a.rows_stage + (int64_t)(m0 + row) * 128 + (threadIdx.x & 7) * 16) = out[q];
     }
     put_transposed<T>(tile[w], a.cols + blockIdx.x * a.cols_stage, a.cols_plane, (int64_t)w * a.F + f0, a.F - f0);
   }
@@ -430,8 +505,11 @@ Tile tile_of(int64_t m, int64_t n) {
   const int64_t wide = ((m + 255) / 256) * ((n + 255) / 256);
   return wide >= 192 ? Tile{256, 256, true} : Tile{128, 128, false};
 }
-// Parts of the contraction: as many as fill the chip, of eight stages at least.
-int splits_of(int64_t tiles, int64_t stages) { return (int)std::max<int64_t>(1, std::min<int64_t>({stages / 8, 16, 512 / std::max<int64_t>(1, tiles)})); }
+// Parts of the contraction: as many as fill the chip (a wide tile has a compute unit to itself, small ones go two to one), of eight
+// stages at least.
+int splits_of(const Tile &t, int64_t tiles, int64_t stages) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({stages / 8, 16, (t.wide ? 256 : 512) / std::max<int64_t>(1, tiles)}));
+}
 
 struct Product {
   Tile tile;
@@ -442,7 +520,7 @@ Product product_of(int64_t m, int64_t n, int64_t stages) {
   p.tile = tile_of(m, n);
   p.mt = (int)((m + p.tile.bm - 1) / p.tile.bm);
   p.nt = (int)((n + p.tile.bn - 1) / p.tile.bn);
-  p.splits = splits_of((int64_t)p.mt * p.nt, stages);
+  p.splits = splits_of(p.tile, (int64_t)p.mt * p.nt, stages);
   return p;
 }
 size_t part_bytes(const Product &p, int64_t m, int n) { return p.splits > 1 ? rup256((size_t)p.splits * m * pitch_of(n) * 4) : 0; }
@@ -473,13 +551,13 @@ template <typename T, int WHAT> int launch_gemm(const GemmP &p, const Product &h
   const int64_t n = (int64_t)p.mt * p.nt * p.splits;
   if (n * 512 >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "gated units: too large for one launch");
   if (how.tile.wide) {
-    auto k = gemm_kernel<T, WHAT, 2, 4, 4, 2>;
-    const int bytes = 2 * (256 + 256) * 128;
+    auto k = gemm_kernel<T, WHAT, WIDE_WM, WIDE_WN, 8 / WIDE_WM, 8 / WIDE_WN, WIDE_SK, WIDE_NS>;
+    const int bytes = WIDE_NS * (256 + 256) * WIDE_SK * 2;
     const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
-    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(512), bytes, st, p);
+    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(64 * WIDE_WM * WIDE_WN), bytes, st, p);
   } else {
-    auto k = gemm_kernel<T, WHAT, 2, 2, 2, 2>;
+    auto k = gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 2>;
     hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(256), 2 * (128 + 128) * 128, st, p);
   }
   return ops_launched("gated units, product");
@@ -534,7 +612,6 @@ template <typename T> int units_forward(const snn_units_args &a, void *saved, ch
   p.steps = steps;
   p.out = Rows<void>(a.y, a.T);
   p.part = (float *)saved;
-  p.pitch = pitch_of(a.F);
   p.act = a.act;
   p.M = M;
   p.N = a.F;
@@ -561,7 +638,7 @@ template <typename T> int units_backward(const snn_units_args &a, const snn_unit
   const Steps steps{a.T, a.B, a.lengths}, all{1, 1 << 30, nullptr};
   char *const rows = ws, *const cols = rows + u.rows, *const xt = cols + u.cols, *const wt = xt + u.xt, *const part = wt + u.wt;
   const int64_t st_r = (int64_t)M * 128, st_c = (int64_t)2 * a.F * 128, st_x = (int64_t)a.D * 128, pl_w = st_x * 2 * pf;
-  SlopeP s{steps, Rows<void>(g.dy, a.T), saved, saved + (int64_t)M * pitch_of(a.F), pitch_of(a.F), a.act, M, a.F, pf, rows, cols, st_r, st_r * 2 * pf, st_c, st_c * pm};
+  SlopeP s{steps, Rows<void>(g.dy, a.T), saved, a.act, M, a.F, pf, rows_take(g.dy, a.T, a.B, 8, sizeof(T)), rows, cols, st_r, st_r * 2 * pf, st_c, st_c * pm};
   hipLaunchKernelGGL(slope_kernel<T>, dim3(pm, pf), dim3(256), 0, st, s);
   if ((rc = ops_launched("gated units backward, slopes"))) return rc;
   if ((rc = lay_transposed<T>(a.x.p, a.T > 1 ? a.x.stride_t : 0, a.x.stride_b, steps, M, a.D, xt, st_x, st_x * pm, 0, st))) return rc;
@@ -616,7 +693,7 @@ int32_t snn_units_saved_bytes(const snn_units_args *a, size_t *bytes) {
   if (!bytes) return ops_fail(SNN_ERR_NULL, "bytes is NULL");
   const int rc = units_sizes(a);
   if (rc) return rc;
-  *bytes = (size_t)std::max<int64_t>(1, (int64_t)a->T * a->B) * pitch_of(a->F) * 8;
+  *bytes = (size_t)std::max<int64_t>(1, ((int64_t)a->T * a->B + 31) / 32) * ((a->F + 31) / 32) * KEPT * 4;
   return SNN_OK;
 }
 

@@ -137,7 +137,7 @@ def test_refusals_of_a_recurrence_step(lib):
 def test_sizes_of_what_is_saved(lib):
     n = C.c_size_t(0)
     for op, kw, size in (("recurrence", dict(T=17), 3 * 2 * 8 * 4), ("norm", {}, 2 * 2 * 8), ("norm", dict(per_step=1), 4 * 2 * 2 * 8),
-                         ("units", dict(F=13), 8 * 16 * 8)):
+                         ("units", dict(F=33), 32 * 64 * 8)):
         assert getattr(lib, f"snn_{op}_saved_bytes")(C.byref(args(op, **kw)), C.byref(n)) == 0 and n.value == size, op
 
 
