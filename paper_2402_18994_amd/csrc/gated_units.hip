@@ -294,6 +294,177 @@ template <typename T, int WHAT> __global__ __launch_bounds__(256) void gemm_sum_
   give4<T>(row, n, a.N, ((uintptr_t)row & (4 * sizeof(T) - 1)) == 0, v);
 }
 
+// ---------------------------------------------------------------- few rows
+// Up to 64 rows (a token of every stream): the matrices pass through once and bound it.  A workgroup has 16 units, gate and up, and
+// each of its wavefronts every WAVES-th piece of 128 bytes of the rows; their sums meet in LDS.  A wavefront brings its pieces into
+// LDS by itself, NB - 1 of them ahead (no barrier), and takes the operands of the matrix instructions from there: loaded straight
+// into operand registers, where neighbouring lanes have different rows, every 16 lanes touch 16 cache lines, and a compute unit
+// gets 16 bytes a cycle (64 rows, 2048 -> 4096, bf16: 14.4 us against FEWNOW).  fp32 stays fp32 here: the fp32 matrix instructions
+// keep up, and the matrices need no pass before.
+constexpr int FEW = 64, FEW_UNITS = 16;
+
+struct FewP {
+  const void *gate, *up;
+  Rows<void> x, y;
+  Steps steps;
+  float *kept;                               // as the tiles keep it, or NULL
+  int M, D, F, act;
+};
+typedef __attribute__((ext_vector_type(4))) float f4;
+
+// The sums of the wavefronts, [wavefront][gate, up][16 rows][unit][row], to outputs.
+template <typename T, int MB, int WAVES> __device__ __forceinline__ void few_finish(const FewP &a, const f4 (&acc)[2][MB], float *lds, int f0, int m0) {
+  constexpr int SET = 2 * MB * 16 * 17;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lds[wave * SET + ((w * MB + i) * 16 + 4 * (lane >> 4) + e) * 17 + (lane & 15)] = acc[w][i][e];
+  __syncthreads();
+  for (int o = threadIdx.x; o < MB * 256; o += WAVES * 64) {
+    const int n = o & 15, in = o >> 4, m = m0 + in;
+    if (m >= a.M || f0 + n >= a.F) continue;
+    float vg = 0.f, vu = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      vg += lds[w * SET + ((in >> 4) * 16 + n) * 17 + (in & 15)];
+      vu += lds[w * SET + ((MB + (in >> 4)) * 16 + n) * 17 + (in & 15)];
+    }
+    if (a.kept) {
+      const int u = (f0 + n) & 31;
+      float *const at = a.kept + kept_block(m >> 5, (f0 + n) >> 5, a.F) + (u >> 3) * 256 + ((m & 31) + (u & 4) * 8) * 4 + (u & 3);
+      at[0] = vg;
+      at[1024] = vu;
+    }
+    int t, b;
+    const bool live = a.steps.live(m, t, b);
+    ((T *)a.y.p)[t * a.y.st + b * a.y.sb + f0 + n] = narrow<T>(live ? act_of(a.act, vg) * vu : 0.f);
+  }
+}
+// 16 units by 16 rows: 16 bytes of a row a lane, the four sets of 16 lanes one after another along k.
+template <typename T> __device__ __forceinline__ void few_multiply(f4 &acc, const u32x4 &w, const u32x4 &x) {
+  if constexpr (sizeof(T) == 2) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
+  else
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[e]), __uint_as_float(x[e]), acc, 0, 0, 0);
+}
+
+// Rows in 16-byte pieces, those of x within 2^30 bytes of the first.
+template <typename T, int MB, int WAVES, int NB> __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(const FewP a) {
+  constexpr int E = 16 / (int)sizeof(T), PIECE = 8 * E, ROWS = 32 + 16 * MB, LOADS = ROWS / 8, SIZE = ROWS * 128;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), f0 = blockIdx.x * FEW_UNITS,
+            m0 = blockIdx.y * MB * 16;
+  // rows of a piece: 16 of gate, 16 of up, those of x; chunk c of row r at place c ^ (r / 2 % 8), as in the tiles
+  int at[LOADS];
+#pragma unroll
+  for (int q = 0; q < LOADS; ++q) {
+    const int r = 8 * q + lane / 8, c = (lane & 7) ^ ((r >> 1) & 7);
+    int64_t row = 0;
+    bool there;
+    if (q < 4) {
+      there = f0 + (r & 15) < a.F;
+      row = (int64_t)(r & 15) * a.D;
+    } else {
+      int t, b;
+      there = m0 + r - 32 < a.M;
+      a.steps.live(there ? m0 + r - 32 : 0, t, b);
+      row = t * a.x.st + b * a.x.sb;
+    }
+    at[q] = there ? (int)(row * (int64_t)sizeof(T)) + c * 16 : ROW_NOWHERE;
+  }
+  const int chunk = ((lane & 7) ^ (lane / 16 & 7)) * E, chunk_odd = ((lane & 7) ^ ((lane / 16 + 4) & 7)) * E;   // (rows 8 q + lane / 8, q even and odd)
+  const T *const gate = (const T *)a.gate + (int64_t)f0 * a.D, *const up = (const T *)a.up + (int64_t)f0 * a.D;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_ptr_t)lds + wave * NB * SIZE);
+  auto ask = [&](int n, int k) {             // the piece from k on into buffer n; behind D nothing (zeros)
+    const unsigned size = k < a.D ? ROW_SPAN : 0;
+    const u32x4 rg = raw_rsrc(gate + k, size), ru = raw_rsrc(up + k, size), rx = raw_rsrc((const T *)a.x.p + k, size);
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) {
+      const bool in = k + ((q & 1) ? chunk_odd : chunk) < a.D;
+      load_to_lds_b128(q < 2 ? rg : q < 4 ? ru : rx, lds0 + n * SIZE + q * 1024, in ? at[q] : ROW_NOWHERE, 0);
+    }
+  };
+  f4 acc[2][MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) acc[0][i] = acc[1][i] = f4{0.f, 0.f, 0.f, 0.f};
+  const char *const mine = lds + wave * NB * SIZE;
+  const int r = lane & 15;
+  int from[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) from[s] = r * 128 + (((4 * s + (lane >> 4)) ^ ((r >> 1) & 7)) << 4);
+#pragma unroll
+  for (int n = 0; n < NB - 1; ++n) ask(n, (wave + n * WAVES) * PIECE);
+  int buf = 0;
+  for (int k = wave * PIECE; k < a.D; k += WAVES * PIECE) {
+    ask(buf ? buf - 1 : NB - 1, k + (NB - 1) * WAVES * PIECE);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 1) * LOADS) : "memory");     // the oldest piece is there
+    const char *p = mine + buf * SIZE;
+    buf = buf + 1 < NB ? buf + 1 : 0;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const u32x4 g = *(const u32x4 *)(p + from[s]), u = *(const u32x4 *)(p + 2048 + from[s]);
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const u32x4 x = *(const u32x4 *)(p + 4096 + i * 2048 + from[s]);
+        few_multiply<T>(acc[0][i], g, x);
+        few_multiply<T>(acc[1][i], u, x);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the buffer has been read before it is asked for again)
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  few_finish<T, MB, WAVES>(a, acc, (float *)lds, f0, m0);
+}
+
+// The same for rows that lie otherwise: element by element into the operand registers.
+template <typename T, int MB> __global__ __launch_bounds__(256) void few_rows_any_kernel(const FewP a) {
+  constexpr int WAVES = 4, E = 16 / (int)sizeof(T);
+  __shared__ float lds[WAVES * 2 * MB * 16 * 17];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), f0 = blockIdx.x * FEW_UNITS,
+            m0 = blockIdx.y * MB * 16;
+  const int f = f0 + (lane & 15);
+  const bool unit = f < a.F;
+  const T *gate = (const T *)a.gate + (int64_t)(unit ? f : 0) * a.D, *up = (const T *)a.up + (int64_t)(unit ? f : 0) * a.D;
+  const T *x[MB];
+  bool row[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const int m = m0 + i * 16 + (lane & 15);
+    int t, b;
+    row[i] = m < a.M;
+    a.steps.live(row[i] ? m : 0, t, b);
+    x[i] = (const T *)a.x.p + t * a.x.st + b * a.x.sb;
+  }
+  f4 acc[2][MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) acc[0][i] = acc[1][i] = f4{0.f, 0.f, 0.f, 0.f};
+  auto load = [&](const T *p, bool on, int k) {
+    Pack<T, E> v;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const bool there = on && k + e < a.D;
+      const T q = p[there ? k + e : 0];
+      v.v[e] = there ? q : narrow<T>(0.f);
+    }
+    return __builtin_bit_cast(u32x4, v);
+  };
+  for (int k = wave * 4 * E; k < a.D; k += WAVES * 4 * E) {
+    const int at = k + (lane >> 4) * E;
+    const u32x4 g = load(gate, unit, at), u = load(up, unit, at);
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const u32x4 v = load(x[i], row[i], at);
+      few_multiply<T>(acc[0][i], g, v);
+      few_multiply<T>(acc[1][i], u, v);
+    }
+  }
+  few_finish<T, MB, WAVES>(a, acc, lds, f0, m0);
+}
+
 // ---------------------------------------------------------------- layouts
 // Piece `plane` of a value that enters the products.
 template <typename T> struct Pieces;
@@ -583,6 +754,30 @@ int lay_transposed(const void *src, int64_t st, int64_t sb, const Steps &steps, 
   return ops_launched("gated units, layout");
 }
 
+// Up to as many rows as the tiles, which lay fp32 matrices out first, are slower at.  FEWRULE
+bool few_rows(const snn_units_args &a) { return (int64_t)a.T * a.B <= (a.type == SNN_TYPE_FP32 ? 4 * FEW : 2 * FEW); }
+template <typename T, int MB, int WAVES, int NB> int launch_few(const FewP &p, bool wide, hipStream_t st) {
+  const dim3 grid((p.F + FEW_UNITS - 1) / FEW_UNITS, (p.M + 16 * MB - 1) / (16 * MB));
+  if (!wide) hipLaunchKernelGGL((few_rows_any_kernel<T, MB>), grid, dim3(256), 0, st, p);
+  else {
+    auto k = few_rows_kernel<T, MB, WAVES, NB>;
+    const int bytes = WAVES * NB * (32 + 16 * MB) * 128;
+    const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
+    hipLaunchKernelGGL(k, grid, dim3(WAVES * 64), bytes, st, p);
+  }
+  return ops_launched("gated units, few rows");
+}
+template <typename T> int units_few(const snn_units_args &a, void *saved, hipStream_t st) {
+  constexpr int E = 16 / sizeof(T);
+  const FewP p{a.gate, a.up, Rows<void>(a.x, a.T), Rows<void>(a.y, a.T), Steps{a.T, a.B, a.lengths}, (float *)saved, a.T * a.B, a.D, a.F, a.act};
+  auto apart = [](int n, int64_t stride) { return n <= 1 ? 0 : stride < 0 || stride > (1 << 30) ? (int64_t)1 << 40 : (n - 1) * stride; };
+  const bool wide = a.D % E == 0 && aligned(a.gate, 16) && aligned(a.up, 16) && rows_take(a.x, a.T, a.B, E, sizeof(T)) &&
+                    (apart(a.T, a.x.stride_t) + apart(a.B, a.x.stride_b)) * (int64_t)sizeof(T) < (1 << 30);
+  // (wavefronts by buffers: what 160 KiB of LDS hold)
+  return p.M <= 16 ? launch_few<T, 1, 8, 3>(p, wide, st) : p.M <= 32 ? launch_few<T, 2, 8, 2>(p, wide, st) : launch_few<T, 4, 4, 3>(p, wide, st);
+}
+
 template <typename T> int units_forward(const snn_units_args &a, void *saved, char *ws, hipStream_t st) {
   const int M = a.T * a.B, planes = Pieces<T>::N;
   const Steps steps{a.T, a.B, a.lengths}, all{1, 1 << 30, nullptr};
@@ -685,7 +880,7 @@ int32_t snn_units_workspace_bytes(const snn_units_args *a, int32_t backward, siz
     return SNN_OK;
   }
   int64_t row;
-  *bytes = (x_direct(*a, row) ? 0 : rup256(panel_bytes((int64_t)a->T * a->B, a->D, planes))) + (weights_direct(*a) ? 0 : 2 * rup256(panel_bytes(a->F, a->D, planes)));
+  *bytes = few_rows(*a) ? 0 : (x_direct(*a, row) ? 0 : rup256(panel_bytes((int64_t)a->T * a->B, a->D, planes))) + (weights_direct(*a) ? 0 : 2 * rup256(panel_bytes(a->F, a->D, planes)));
   return SNN_OK;
 }
 
@@ -706,6 +901,7 @@ int32_t snn_units_forward(const snn_units_args *a, void *saved, void *workspace,
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
     return ops_fail(SNN_ERR_WORKSPACE, "gated units: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
   if (a->T == 0) return SNN_OK;
+  if (few_rows(*a)) return a->type == SNN_TYPE_FP32 ? units_few<float>(*a, saved, (hipStream_t)stream) : units_few<__bf16>(*a, saved, (hipStream_t)stream);
   return a->type == SNN_TYPE_FP32 ? units_forward<float>(*a, saved, (char *)workspace, (hipStream_t)stream)
                                   : units_forward<__bf16>(*a, saved, (char *)workspace, (hipStream_t)stream);
 }
