@@ -493,23 +493,31 @@ struct LayP {
   int rows, cols;
   char *dst;                                 // panels
   int64_t stage, plane;                      // bytes
-  int at;                                    // first panel (of rows: along the columns) or first row (transposed: along them)
   int wide;                                  // eight elements at a time
 };
+struct LayJobs {                             // x, gate, up: one launch
+  LayP job[3];
+};
 
-// Rows as they are: panel c / 64, row m, 64 columns.  A thread makes one chunk of every piece.
-template <typename T> __global__ __launch_bounds__(256) void lay_rows_kernel(const LayP a) {
-  const int m = blockIdx.x * 32 + threadIdx.x / 8, c = blockIdx.y * KS + (threadIdx.x & 7) * 8;
-  if (m >= a.rows) return;
-  int t, b;
-  const bool live = a.steps.live(m, t, b);
-  const T *row = (const T *)a.src + t * a.st + b * a.sb;
+// Eight elements of a row from column c on, zeros in the place of those that do not exist.
+template <typename T> __device__ __forceinline__ Pack<T, 8> eight_of(const T *row, int c, int cols, bool live, bool wide) {
   Pack<T, 8> v = {};
-  if (live && a.wide && c + 8 <= a.cols) v = *(const Pack<T, 8> *)(row + c);
+  if (live && wide && c + 8 <= cols) v = *(const Pack<T, 8> *)(row + c);
   else if (live)
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (c + k < a.cols) v.v[k] = row[c + k];
+      if (c + k < cols) v.v[k] = row[c + k];
+  return v;
+}
+
+// Rows as they are: panel c / 64, row m, 64 columns.  A thread makes one chunk of every piece.
+template <typename T> __global__ __launch_bounds__(256) void lay_rows_kernel(const LayJobs jobs) {
+  const LayP &a = jobs.job[blockIdx.z];
+  const int m = blockIdx.x * 32 + threadIdx.x / 8, c = blockIdx.y * KS + (threadIdx.x & 7) * 8;
+  if (m >= a.rows || (int)blockIdx.y * KS >= a.cols) return;
+  int t, b;
+  const bool live = a.steps.live(m, t, b);
+  const Pack<T, 8> v = eight_of((const T *)a.src + t * a.st + b * a.sb, c, a.cols, live, a.wide);
   constexpr int P = Pieces<T>::N;
   Chunk out[P];
 #pragma unroll
@@ -520,10 +528,10 @@ template <typename T> __global__ __launch_bounds__(256) void lay_rows_kernel(con
     for (int q = 0; q < P; ++q) out[q].v[k] = p[q];
   }
 #pragma unroll
-  for (int q = 0; q < P; ++q) *(Chunk *)(a.dst + q * a.plane + (a.at + blockIdx.y) * a.stage + (int64_t)m * 128 + (threadIdx.x & 7) * 16) = out[q];
+  for (int q = 0; q < P; ++q) *(Chunk *)(a.dst + q * a.plane + blockIdx.y * a.stage + (int64_t)m * 128 + (threadIdx.x & 7) * 16) = out[q];
 }
 
-// Columns as rows: panel m / 64, row `at` + c, 64 of the source's rows.
+// Columns as rows: panel m / 64, row c, 64 of the source's rows.
 template <typename T> __device__ __forceinline__ void put_transposed(const T (&tile)[KS][KS + 1], char *dst, int64_t plane, int64_t first_row, int cols_left) {
   constexpr int P = Pieces<T>::N;
 #pragma unroll
@@ -542,21 +550,22 @@ template <typename T> __device__ __forceinline__ void put_transposed(const T (&t
       for (int q = 0; q < P; ++q) *(Chunk *)(dst + q * plane + (first_row + c) * 128 + (threadIdx.x & 7) * 16) = out[q];
   }
 }
-template <typename T> __global__ __launch_bounds__(256) void lay_transposed_kernel(const LayP a) {
+template <typename T> __global__ __launch_bounds__(256) void lay_transposed_kernel(const LayJobs jobs) {
   __shared__ T tile[KS][KS + 1];
-  const int m0 = blockIdx.x * KS, c0 = blockIdx.y * KS, c = threadIdx.x & 63;
+  const LayP &a = jobs.job[blockIdx.z];
+  const int m0 = blockIdx.x * KS, c0 = blockIdx.y * KS;
+  if (m0 >= a.rows || c0 >= a.cols) return;
 #pragma unroll
-  for (int u = 0; u < 16; ++u) {
-    const int r = u * 4 + threadIdx.x / 64, m = m0 + r;
-    T v = narrow<T>(0.f);
-    if (m < a.rows && c0 + c < a.cols) {
-      int t, b;
-      if (a.steps.live(m, t, b)) v = ((const T *)a.src)[t * a.st + b * a.sb + c0 + c];
-    }
-    tile[r][c] = v;
+  for (int u = 0; u < 2; ++u) {
+    const int r = (threadIdx.x + 256 * u) / 8, c = (threadIdx.x & 7) * 8, m = m0 + r;
+    int t = 0, b = 0;
+    const bool live = m < a.rows && a.steps.live(m, t, b);
+    const Pack<T, 8> v = eight_of((const T *)a.src + t * a.st + b * a.sb, c0 + c, a.cols, live, a.wide);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tile[r][c + k] = v.v[k];
   }
   __syncthreads();
-  put_transposed<T>(tile, a.dst + blockIdx.x * a.stage, a.plane, (int64_t)a.at + c0, a.cols - c0);
+  put_transposed<T>(tile, a.dst + blockIdx.x * a.stage, a.plane, c0, a.cols - c0);
 }
 
 // dG and dU from dy and the sums of the forward pass, both ways round: [f / 64][m][64] (dU behind dG along f) and [m / 64][f][64].
@@ -585,13 +594,7 @@ template <typename T> __global__ __launch_bounds__(256) void slope_kernel(const 
     const int row = (threadIdx.x + 256 * v) / 8, k0 = (threadIdx.x & 7) * 8, m = m0 + row;
     int t = 0, b = 0;
     const bool live = m < a.M && a.steps.live(m, t, b);
-    const T *dy = (const T *)a.dy.p + t * a.dy.st + b * a.dy.sb + f0 + k0;
-    Pack<T, 8> d = {};
-    if (live && a.wide && f0 + k0 + 8 <= a.F) d = *(const Pack<T, 8> *)dy;
-    else if (live)
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (f0 + k0 + k < a.F) d.v[k] = dy[k];
+    const Pack<T, 8> d = eight_of((const T *)a.dy.p + t * a.dy.st + b * a.dy.sb, f0 + k0, a.F, live, a.wide);
 #pragma unroll
     for (int k = 0; k < 8; ++k) tile[0][row][k0 + k] = d.v[k];
   }
@@ -728,8 +731,12 @@ template <typename T, int WHAT> int launch_gemm(const GemmP &p, const Product &h
     if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
     hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(64 * WIDE_WM * WIDE_WN), bytes, st, p);
   } else {
-    auto k = gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 2>;
-    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(256), 2 * (128 + 128) * 128, st, p);
+    // (up to one a compute unit: four stages in LDS, three of them on their way; more: two, and two workgroups a compute unit)
+    auto k = n <= 256 ? gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 4> : gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 2>;
+    const int bytes = (n <= 256 ? 4 : 2) * (128 + 128) * 128;
+    const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
+    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(256), bytes, st, p);
   }
   return ops_launched("gated units, product");
 }
@@ -742,16 +749,20 @@ template <typename T, int WHAT> int launch_product(GemmP p, const Product &how, 
   return ops_launched("gated units, sums");
 }
 
-template <typename T> int lay_rows(const void *src, int64_t st, int64_t sb, const Steps &steps, int rows, int cols, char *dst, bool wide, hipStream_t stream) {
-  LayP p{src, st, sb, steps, rows, cols, dst, (int64_t)rows * 128, (int64_t)rows * 128 * panels_of(cols), 0, wide};
-  hipLaunchKernelGGL(lay_rows_kernel<T>, dim3((rows + 31) / 32, panels_of(cols)), dim3(256), 0, stream, p);
+// A launch for `n` jobs.
+template <typename T, bool TRANSPOSED> int lay(const LayJobs &jobs, int n, hipStream_t st) {
+  int rows = 0, cols = 0;
+  for (int i = 0; i < n; ++i) rows = std::max(rows, jobs.job[i].rows), cols = std::max(cols, jobs.job[i].cols);
+  if (TRANSPOSED) hipLaunchKernelGGL(lay_transposed_kernel<T>, dim3(panels_of(rows), panels_of(cols), n), dim3(256), 0, st, jobs);
+  else hipLaunchKernelGGL(lay_rows_kernel<T>, dim3((rows + 31) / 32, panels_of(cols), n), dim3(256), 0, st, jobs);
   return ops_launched("gated units, layout");
 }
-template <typename T>
-int lay_transposed(const void *src, int64_t st, int64_t sb, const Steps &steps, int rows, int cols, char *dst, int64_t stage, int64_t plane, int at, hipStream_t stream) {
-  LayP p{src, st, sb, steps, rows, cols, dst, stage, plane, at, 0};
-  hipLaunchKernelGGL(lay_transposed_kernel<T>, dim3(panels_of(rows), panels_of(cols)), dim3(256), 0, stream, p);
-  return ops_launched("gated units, layout");
+// x or a matrix as a job.
+template <typename T> LayP lay_x(const snn_units_args &a, char *dst, int64_t stage, int64_t plane) {
+  return LayP{a.x.p, a.T > 1 ? a.x.stride_t : 0, a.x.stride_b, Steps{a.T, a.B, a.lengths}, a.T * a.B, a.D, dst, stage, plane, rows_take(a.x, a.T, a.B, 8, sizeof(T))};
+}
+template <typename T> LayP lay_matrix(const snn_units_args &a, const void *w, char *dst, int64_t stage, int64_t plane) {
+  return LayP{w, 0, a.D, Steps{1, 1 << 30, nullptr}, a.F, a.D, dst, stage, plane, a.D % 8 == 0 && aligned(w, 8 * sizeof(T))};
 }
 
 // Up to as many rows as the tiles, which lay fp32 matrices out first, are slower at.  FEWRULE
@@ -780,26 +791,27 @@ template <typename T> int units_few(const snn_units_args &a, void *saved, hipStr
 
 template <typename T> int units_forward(const snn_units_args &a, void *saved, char *ws, hipStream_t st) {
   const int M = a.T * a.B, planes = Pieces<T>::N;
-  const Steps steps{a.T, a.B, a.lengths}, all{1, 1 << 30, nullptr};
+  const Steps steps{a.T, a.B, a.lengths};
   GemmP p{};
   p.panels = panels_of(a.D);
   p.segs = planes == 3 ? 6 : 1;
   int64_t row;
-  int rc;
+  int jobs = 0, rc;
+  LayJobs lays;
   if (x_direct(a, row)) p.a = Side{(const char *)a.x.p, nullptr, row, 128, 0, M};
   else {
-    const bool wide = rows_take(a.x, a.T, a.B, 8, sizeof(T));
-    if ((rc = lay_rows<T>(a.x.p, a.T > 1 ? a.x.stride_t : 0, a.x.stride_b, steps, M, a.D, ws, wide, st))) return rc;
     p.a = Side{ws, nullptr, 128, (int64_t)M * 128, (int64_t)M * 128 * p.panels, M};
+    lays.job[jobs++] = lay_x<T>(a, ws, p.a.stage, p.a.plane);
     ws += rup256(panel_bytes(M, a.D, planes));
   }
   if (weights_direct(a)) p.b = Side{(const char *)a.gate, (const char *)a.up, (int64_t)a.D * 2, 128, 0, a.F};
   else {
-    const size_t each = rup256(panel_bytes(a.F, a.D, planes));
-    const bool wide = a.D % 8 == 0 && aligned(a.gate, 8 * sizeof(T)) && aligned(a.up, 8 * sizeof(T));
-    if ((rc = lay_rows<T>(a.gate, 0, a.D, all, a.F, a.D, ws, wide, st)) || (rc = lay_rows<T>(a.up, 0, a.D, all, a.F, a.D, ws + each, wide, st))) return rc;
-    p.b = Side{ws, ws + each, 128, (int64_t)a.F * 128, (int64_t)a.F * 128 * p.panels, a.F};
+    char *const up = ws + rup256(panel_bytes(a.F, a.D, planes));
+    p.b = Side{ws, up, 128, (int64_t)a.F * 128, (int64_t)a.F * 128 * p.panels, a.F};
+    lays.job[jobs++] = lay_matrix<T>(a, a.gate, ws, p.b.stage, p.b.plane);
+    lays.job[jobs++] = lay_matrix<T>(a, a.up, up, p.b.stage, p.b.plane);
   }
+  if (jobs && (rc = lay<T, false>(lays, jobs, st))) return rc;
   const Tile tile = tile_of(M, 2 * (int64_t)a.F);
   p.mt = (M + tile.bm - 1) / tile.bm;
   p.nt = (a.F + tile.bn / 2 - 1) / (tile.bn / 2);
@@ -830,15 +842,14 @@ template <typename T> int units_backward(const snn_units_args &a, const snn_unit
     }
     return SNN_OK;
   }
-  const Steps steps{a.T, a.B, a.lengths}, all{1, 1 << 30, nullptr};
+  const Steps steps{a.T, a.B, a.lengths};
   char *const rows = ws, *const cols = rows + u.rows, *const xt = cols + u.cols, *const wt = xt + u.xt, *const part = wt + u.wt;
   const int64_t st_r = (int64_t)M * 128, st_c = (int64_t)2 * a.F * 128, st_x = (int64_t)a.D * 128, pl_w = st_x * 2 * pf;
   SlopeP s{steps, Rows<void>(g.dy, a.T), saved, a.act, M, a.F, pf, rows_take(g.dy, a.T, a.B, 8, sizeof(T)), rows, cols, st_r, st_r * 2 * pf, st_c, st_c * pm};
   hipLaunchKernelGGL(slope_kernel<T>, dim3(pm, pf), dim3(256), 0, st, s);
   if ((rc = ops_launched("gated units backward, slopes"))) return rc;
-  if ((rc = lay_transposed<T>(a.x.p, a.T > 1 ? a.x.stride_t : 0, a.x.stride_b, steps, M, a.D, xt, st_x, st_x * pm, 0, st))) return rc;
-  if ((rc = lay_transposed<T>(a.gate, 0, a.D, all, a.F, a.D, wt, st_x, pl_w, 0, st))) return rc;
-  if ((rc = lay_transposed<T>(a.up, 0, a.D, all, a.F, a.D, wt + st_x * pf, st_x, pl_w, 0, st))) return rc;
+  const LayJobs lays{{lay_x<T>(a, xt, st_x, st_x * pm), lay_matrix<T>(a, a.gate, wt, st_x, pl_w), lay_matrix<T>(a, a.up, wt + st_x * pf, st_x, pl_w)}};
+  if ((rc = lay<T, true>(lays, 3, st))) return rc;
   GemmP p{};
   p.segs = u.segs;
   p.steps = steps;
