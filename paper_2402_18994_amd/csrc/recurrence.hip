@@ -52,16 +52,15 @@ __device__ __forceinline__ float rate_of(float sharpness, float decay) {
   return v < -0x1p127f ? -0x1p127f : v;
 }
 
-// 1 - a^2 for a = 2^L: where a^2 is near one, the series of 1 - exp(-z), whose first term left out is z^9 / 9! (2^-26 of the
-// sum at z = 1/2); 1 - a a beyond, where the rounding of a a is 1.5 units of the last place of the result.
+// 1 - a^2 for a = 2^L: where a^2 is near one, z p(z) with p the polynomial of degree 5 that is closest to (1 - exp(-z)) / z over [0, 1/2]
+// (off by 1.4e-9 of it; fitted by reweighted least squares); beyond, 1 - a a, where the rounding of a a is 1.5 units of the result's
+// last place.
 __device__ __forceinline__ float one_less_square(float L, float a) {
   const float z = L * (-2.f * LN2);
-  float p = fmaf(z, -1.f / 40320.f, 1.f / 5040.f);
-  p = fmaf(p, z, -1.f / 720.f);
-  p = fmaf(p, z, 1.f / 120.f);
-  p = fmaf(p, z, -1.f / 24.f);
-  p = fmaf(p, z, 1.f / 6.f);
-  p = fmaf(p, z, -0.5f);
+  float p = fmaf(z, -0x1.26079ep-10f, 0x1.0c48c4p-7f);
+  p = fmaf(p, z, -0x1.550686p-5f);
+  p = fmaf(p, z, 0x1.555304p-3f);
+  p = fmaf(p, z, -0x1.fffff4p-2f);
   p = fmaf(p, z, 1.f);
   return z < 0.5f ? z * p : fmaf(-a, a, 1.f);
 }
@@ -71,16 +70,15 @@ __device__ __forceinline__ float root_of(float m, float &inverse) {
   return m * inverse;
 }
 
-template <typename T, int VEC> struct Place {             // where a lane's run lies
-  int run, d, at;                                         // run in the tile; first channel; byte offset from the wavefront's row
-  bool live;
-};
-
-// A tile's raw rows of one stream: row s of the run, zeros behind `n` (the run's steps that exist).
+// A run's raw rows of one stream; zeros behind `n`, the run's steps that exist (`all`: they do in every lane).
 template <typename T, int VEC>
-__device__ __forceinline__ void load_run(Pack<T, VEC> (&v)[STEPS], const T *row, int64_t st, int at, int n) {
+__device__ __forceinline__ void load_run(Pack<T, VEC> (&v)[STEPS], const T *row, int64_t st, int at, int n, bool all) {
+  if (all)
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) v[s] = row_load<T, VEC>(row + s * st, s < n ? at : ROW_NOWHERE);
+    for (int s = 0; s < STEPS; ++s) v[s] = row_load<T, VEC>(row + s * st, at);
+  else
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) v[s] = row_load<T, VEC>(row + s * st, s < n ? at : ROW_NOWHERE);
 }
 
 // WAVES wavefronts, of which each holds 64 / LANES runs of LANES lanes by VEC channels.
@@ -95,35 +93,54 @@ struct alignas(8) Link {
   float a, h;
 };
 
-// The map of each run of a tile stands in `link`; joins them onto `h` in order (reverse: from the last run on) and returns
-// what a lane's own run starts from; `h` and `p` become state and product behind the tile.
-template <int VEC, int RUNS, bool REVERSE>
-__device__ __forceinline__ void join(const Link (*link)[CH], int c, int run, float (&h)[VEC], float (&p)[VEC], float (&start)[VEC]) {
-#pragma unroll 8
-  for (int k = 0; k < RUNS; ++k) {
-    const int q = REVERSE ? RUNS - 1 - k : k;
+// The runs of a wavefront's two halves as one map, in both halves; `first` is that of the half that comes first.
+template <int HALVES, bool REVERSE> __device__ __forceinline__ Link whole_wave(Link m, Link &first) {
+  first = m;
+  if constexpr (HALVES == 2) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(m.a), __float_as_uint(m.a), false, false);
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(m.h), __float_as_uint(m.h), false, false);
+    const Link low = {__uint_as_float(a[0]), __uint_as_float(h[0])}, high = {__uint_as_float(a[1]), __uint_as_float(h[1])};
+    first = REVERSE ? high : low;
+    const Link then = REVERSE ? low : high;
+    return {first.a * then.a, fmaf(then.a, first.h, then.h)};
+  }
+  return m;
+}
+// The maps of a tile's wavefronts stand in `link`; joins them onto `h` in order (reverse: from the last one on) and returns what a
+// lane's own run starts from; `h` and `p` become state and product behind the tile.
+template <int VEC, int WAVES, int HALVES, bool REVERSE, bool PRODUCT>
+__device__ __forceinline__ void join(const Link (*link)[CH], int c, int wave, bool second, const Link (&first)[VEC], float (&h)[VEC], float (&p)[VEC],
+                                     float (&start)[VEC]) {
+  const int own = REVERSE ? WAVES - 1 - wave : wave;
+  auto add = [&](int k) {
+    const int q = REVERSE ? WAVES - 1 - k : k;
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       const Link m = link[q][c + v];
-      start[v] = q == run ? h[v] : start[v];
       h[v] = fmaf(m.a, h[v], m.h);
-      p[v] *= m.a;
+      if (PRODUCT) p[v] *= m.a;
     }
-  }
+  };
+#pragma unroll 4
+  for (int k = 0; k < own; ++k) add(k);
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) start[v] = HALVES == 2 && second ? fmaf(first[v].a, h[v], first[v].h) : h[v];
+#pragma unroll 4
+  for (int k = own; k < WAVES; ++k) add(k);
 }
 
 // OUT: outputs.  Otherwise the map of the segment alone.
 template <typename T, int VEC, int WAVES, bool OUT>
 __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const RecP a) {
   using S = Shape<T, VEC, WAVES>;
-  __shared__ Link link[2][S::RUNS][CH];
+  __shared__ Link link[2][WAVES][CH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int64_t id = blockIdx.x;
-  const int group = (int)(id % a.groups);
-  id /= a.groups;
-  const int b = (int)(id % a.B), seg = (int)(id / a.B);
-  const int c = (lane % S::LANES) * VEC, d = group * CH + c, run = wave * S::HALVES + lane / S::LANES;
-  const bool live = d < a.D;
+  unsigned id = blockIdx.x;
+  const int group = (int)(id % (unsigned)a.groups);
+  id /= (unsigned)a.groups;
+  const int b = (int)(id % (unsigned)a.B), seg = (int)(id / (unsigned)a.B);
+  const int c = (lane % S::LANES) * VEC, d = group * CH + c;
+  const bool live = d < a.D, second = lane >= S::LANES;
   const int dd = live ? d : 0;
   const int len = __builtin_amdgcn_readfirstlane(length_of(a.lengths, b, a.T));
   const int at_x = S::offset(a.x, lane, d, live), at_i = S::offset(a.i, lane, d, live), at_r = S::offset(a.r, lane, d, live);
@@ -133,6 +150,17 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
   const int64_t cell = (int64_t)b * a.D + dd;
   const int t_end = min(a.T, (seg + 1) * a.tiles * S::TILE);
 
+  const int wave_t = wave * S::HALVES * STEPS, half_t = lane / S::LANES * STEPS;
+  Pack<T, VEC> rx[STEPS], ri[STEPS], rr[STEPS];
+  int t0 = seg * a.tiles * S::TILE;
+  auto fetch = [&](int t) {
+    const int tw = t + wave_t, n = len - (tw + half_t);
+    const bool all = tw + S::HALVES * STEPS <= len;
+    load_run<T, VEC>(rr, r + tw * a.r.st, a.r.st, at_r, n, all);
+    load_run<T, VEC>(ri, i + tw * a.i.st, a.i.st, at_i, n, all);
+    load_run<T, VEC>(rx, x + tw * a.x.st, a.x.st, at_x, n, all);
+  };
+  fetch(t0);
   float rate[VEC], h[VEC], p[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
@@ -141,6 +169,7 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
     p[v] = 1.f;
   }
   if (OUT)
+#pragma unroll 4
     for (int k = 0; k < seg; ++k)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
@@ -148,16 +177,6 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
         h[v] = fmaf(m.x, h[v], m.y);
       }
 
-  const int wave_t = wave * S::HALVES * STEPS, half_t = lane / S::LANES * STEPS;
-  Pack<T, VEC> rx[STEPS], ri[STEPS], rr[STEPS];
-  int t0 = seg * a.tiles * S::TILE;
-  auto fetch = [&](int t) {
-    const int tw = t + wave_t, n = len - (tw + half_t);
-    load_run<T, VEC>(rx, x + tw * a.x.st, a.x.st, at_x, n);
-    load_run<T, VEC>(ri, i + tw * a.i.st, a.i.st, at_i, n);
-    load_run<T, VEC>(rr, r + tw * a.r.st, a.r.st, at_r, n);
-  };
-  fetch(t0);
   for (int buf = 0; t0 < t_end; t0 += S::TILE, buf ^= 1) {
     const int tw = t0 + wave_t, t_run = tw + half_t, n = len - t_run;
     if (t0 >= len) {                                       // (for the whole workgroup)
@@ -167,27 +186,35 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
       for (int s = 0; s < STEPS; ++s) row_store<T, VEC>(y + (tw + s) * a.y.st, t_run + s < a.T ? at_y : ROW_NOWHERE, zero);
       continue;
     }
-    float fa[STEPS][VEC], fb[STEPS][VEC], A[VEC], H[VEC], start[VEC];
+    float fa[STEPS][VEC], fb[STEPS][VEC], start[VEC];
+    Link first[VEC];
+    // ALL: every step of the wavefront exists; otherwise those that do not have a = 1 and b = 0
+    auto maps = [&](auto all) {
+      constexpr bool ALL = decltype(all)::value;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      A[v] = 1.f;
-      H[v] = start[v] = 0.f;
+      for (int v = 0; v < VEC; ++v) {
+        Link m = {1.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        float rest, inverse;
-        const float rho = gate_of(widen(rr[s].v[v]), rest), iota = gate_of(widen(ri[s].v[v]), rest);
-        const float L = s < n ? rate[v] * rho : 0.f;       // (a step that does not exist: a = 1, b = 0)
-        const float e = __builtin_amdgcn_exp2f(L);
-        fa[s][v] = e;
-        fb[s][v] = s < n ? root_of(one_less_square(L, e), inverse) * iota * widen(rx[s].v[v]) : 0.f;
-        H[v] = fmaf(e, H[v], fb[s][v]);
-        A[v] *= e;
+        for (int s = 0; s < STEPS; ++s) {
+          const bool on = ALL || s < n;
+          float rest;
+          const float rho = gate_of(widen(rr[s].v[v]), rest), iota = gate_of(widen(ri[s].v[v]), rest);
+          const float L = on ? rate[v] * rho : 0.f, e = __builtin_amdgcn_exp2f(L);
+          fa[s][v] = e;
+          fb[s][v] = on ? __builtin_amdgcn_sqrtf(one_less_square(L, e)) * iota * widen(rx[s].v[v]) : 0.f;
+          m.h = fmaf(e, m.h, fb[s][v]);
+          m.a *= e;
+        }
+        m = whole_wave<S::HALVES, false>(m, first[v]);
+        if (!second) link[buf][wave][c + v] = m;
       }
-      link[buf][run][c + v] = {A[v], H[v]};
-    }
+    };
+    const bool all = tw + S::HALVES * STEPS <= len;
+    if (all) maps(std::true_type());
+    else maps(std::false_type());
     if (t0 + S::TILE < t_end) fetch(t0 + S::TILE);
     lds_barrier();                                         // (two buffers: one barrier a tile)
-    join<VEC, S::RUNS, false>(link[buf], c, run, h, p, start);
+    join<VEC, WAVES, S::HALVES, false, !OUT>(link[buf], c, wave, second, first, h, p, start);
     if (OUT) {
       if (a.saved && live && t_run < a.T)
 #pragma unroll
@@ -198,13 +225,17 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
           start[v] = fmaf(fa[s][v], start[v], fb[s][v]);
-          out.v[v] = narrow<T>(s < n ? start[v] : 0.f);
+          out.v[v] = narrow<T>(start[v]);
         }
-        row_store<T, VEC>(y + (tw + s) * a.y.st, t_run + s < a.T ? at_y : ROW_NOWHERE, out);
+        if (!all) {
+          const Pack<T, VEC> zero = {};
+          if (s >= n) out = zero;
+        }
+        row_store<T, VEC>(y + (tw + s) * a.y.st, all || t_run + s < a.T ? at_y : ROW_NOWHERE, out);
       }
     }
   }
-  if (live && run == 0)
+  if (live && wave == 0 && !second)
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       if (!OUT) a.carry[(int64_t)seg * a.B * a.D + cell + v] = {p[v], h[v]};
@@ -216,14 +247,14 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
 template <typename T, int VEC, int WAVES, bool OUT>
 __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const RecP a, const RecGradP g) {
   using S = Shape<T, VEC, WAVES>;
-  __shared__ Link link[2][S::RUNS][CH];
+  __shared__ Link link[2][WAVES][CH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int64_t id = blockIdx.x;
-  const int group = (int)(id % a.groups);
-  id /= a.groups;
-  const int b = (int)(id % a.B), seg = (int)(id / a.B) + (OUT ? 0 : 1);     // (no segment comes before the first)
-  const int c = (lane % S::LANES) * VEC, d = group * CH + c, run = wave * S::HALVES + lane / S::LANES;
-  const bool live = d < a.D;
+  unsigned id = blockIdx.x;
+  const int group = (int)(id % (unsigned)a.groups);
+  id /= (unsigned)a.groups;
+  const int b = (int)(id % (unsigned)a.B), seg = (int)(id / (unsigned)a.B) + (OUT ? 0 : 1);     // (no segment comes before the first)
+  const int c = (lane % S::LANES) * VEC, d = group * CH + c;
+  const bool live = d < a.D, second = lane < 64 - S::LANES;                                     // (the upper half's steps come first)
   const int dd = live ? d : 0;
   const int len = __builtin_amdgcn_readfirstlane(length_of(a.lengths, b, a.T));
   const int at_x = S::offset(a.x, lane, d, live), at_i = S::offset(a.i, lane, d, live), at_r = S::offset(a.r, lane, d, live);
@@ -243,6 +274,7 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const R
     sum[v] = 0.f;
   }
   if (OUT)
+#pragma unroll 4
     for (int k = a.nseg - 1; k > seg; --k)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
@@ -252,17 +284,18 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const R
 
   const int wave_t = wave * S::HALVES * STEPS, half_t = lane / S::LANES * STEPS;
   Pack<T, VEC> rx[STEPS], ri[STEPS], rr[STEPS], rg[STEPS];
-  float first[VEC];
+  float before[VEC];
   auto fetch = [&](int t) {
     const int tw = t + wave_t, n = len - (tw + half_t);
-    load_run<T, VEC>(rr, r + tw * a.r.st, a.r.st, at_r, n);
-    load_run<T, VEC>(rg, dy + tw * g.dy.st, g.dy.st, at_dy, n);
+    const bool all = tw + S::HALVES * STEPS <= len;
+    load_run<T, VEC>(rr, r + tw * a.r.st, a.r.st, at_r, n, all);
     if (OUT) {
-      load_run<T, VEC>(rx, x + tw * a.x.st, a.x.st, at_x, n);
-      load_run<T, VEC>(ri, i + tw * a.i.st, a.i.st, at_i, n);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) first[v] = a.saved[(int64_t)(n > 0 ? (tw + half_t) / STEPS : 0) * a.B * a.D + cell + v];
+      for (int v = 0; v < VEC; ++v) before[v] = a.saved[(int64_t)(n > 0 ? (tw + half_t) / STEPS : 0) * a.B * a.D + cell + v];
+      load_run<T, VEC>(ri, i + tw * a.i.st, a.i.st, at_i, n, all);
+      load_run<T, VEC>(rx, x + tw * a.x.st, a.x.st, at_x, n, all);
     }
+    load_run<T, VEC>(rg, dy + tw * g.dy.st, g.dy.st, at_dy, n, all);
   };
   int t0 = t_begin + (t_end - 1 - t_begin) / S::TILE * S::TILE;
   for (; t0 >= t_begin && t0 >= len; t0 -= S::TILE) {      // tiles behind the sequence's end
@@ -280,78 +313,96 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const R
   if (t0 >= t_begin) fetch(t0);
   for (int buf = 0; t0 >= t_begin; t0 -= S::TILE, buf ^= 1) {
     const int tw = t0 + wave_t, t_run = tw + half_t, n = len - t_run;
-    float fl[STEPS][VEC], start[VEC];
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      float A = 1.f, Q = 0.f;
-      start[v] = 0.f;
-#pragma unroll
-      for (int s = STEPS - 1; s >= 0; --s) {
-        float rest;
-        const float rho = gate_of(widen(rr[s].v[v]), rest);
-        const float L = s < n ? rate[v] * rho : 0.f, e = __builtin_amdgcn_exp2f(L);
-        fl[s][v] = L;
-        Q = e * (widen(rg[s].v[v]) + Q);
-        A *= e;
-      }
-      link[buf][run][c + v] = {A, Q};
-    }
-    lds_barrier();
-    join<VEC, S::RUNS, true>(link[buf], c, run, q, p, start);
-    if (OUT) {
-      float past[STEPS][VEC];                              // the state before each step
+    const bool all = tw + S::HALVES * STEPS <= len;
+    // What each step multiplies g by: dx = g to_x, di = dx to_i, dr = g to_l closed (and g to_l is what sums up to ddecay).
+    float fa[STEPS][VEC], to_x[STEPS][VEC], to_i[STEPS][VEC], to_l[STEPS][VEC], closed[STEPS][VEC], start[VEC];
+    Link first[VEC];
+    auto maps = [&](auto exist) {
+      constexpr bool ALL = decltype(exist)::value;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        float h = n > 0 ? first[v] : 0.f;
+        Link m = {1.f, 0.f};
+        float h = OUT ? (ALL || n > 0 ? before[v] : 0.f) : 0.f;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
+          const bool on = ALL || s < n;
+          const float rho = gate_of(widen(rr[s].v[v]), closed[s][v]);
+          const float L = on ? rate[v] * rho : 0.f, e = __builtin_amdgcn_exp2f(L);
+          fa[s][v] = e;
+          if (!OUT) continue;
           float rest, inverse;
-          const float L = fl[s][v], e = __builtin_amdgcn_exp2f(L);
-          past[s][v] = h;
-          h = fmaf(e, h, s < n ? root_of(one_less_square(L, e), inverse) * gate_of(widen(ri[s].v[v]), rest) * widen(rx[s].v[v]) : 0.f);
+          const float iota = gate_of(widen(ri[s].v[v]), rest), gain = root_of(one_less_square(L, e), inverse), xv = widen(rx[s].v[v]);
+          const float gi = gain * iota, le = L * LN2 * e;  // (l a; its limit is zero, also where l is as large as it gets)
+          to_x[s][v] = gi;
+          to_i[s][v] = rest * xv;
+          to_l[s][v] = le * h - e * (le * inverse) * (iota * xv);
+          h = fmaf(e, h, on ? gi * xv : 0.f);
         }
+#pragma unroll
+        for (int s = STEPS - 1; s >= 0; --s) {
+          m.h = fa[s][v] * (widen(rg[s].v[v]) + m.h);
+          m.a *= fa[s][v];
+        }
+        m = whole_wave<S::HALVES, true>(m, first[v]);
+        if (!second) link[buf][wave][c + v] = m;
       }
+    };
+    if (all) maps(std::true_type());
+    else maps(std::false_type());
+    Pack<T, VEC> gy[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) gy[s] = rg[s];
+    if (t0 - S::TILE >= t_begin) fetch(t0 - S::TILE);
+    lds_barrier();
+    join<VEC, WAVES, S::HALVES, true, !OUT>(link[buf], c, wave, second, first, q, p, start);
+    if (!OUT) continue;
+    auto give = [&](auto exist) {
+      constexpr bool ALL = decltype(exist)::value;
 #pragma unroll
       for (int s = STEPS - 1; s >= 0; --s) {
-        Pack<T, VEC> ox, oi, orr;
+        const bool on = ALL || s < n;
+        Pack<T, VEC> ox, oi, ol;
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-          float closed, rest, inverse;
-          const float L = fl[s][v], e = __builtin_amdgcn_exp2f(L), xv = widen(rx[s].v[v]);
-          gate_of(widen(rr[s].v[v]), closed);
-          const float iota = gate_of(widen(ri[s].v[v]), rest), gain = root_of(one_less_square(L, e), inverse);
-          const float gt = widen(rg[s].v[v]) + start[v], gi = gt * gain * iota;
-          const float le = e == 0.f ? 0.f : L * LN2 * e;   // (l a, whose limit is zero, also where l leaves fp32)
-          const float pull = s < n ? gt * (le * past[s][v] - e * (le * inverse) * iota * xv) : 0.f;
-          ox.v[v] = narrow<T>(s < n ? gi : 0.f);
-          oi.v[v] = narrow<T>(s < n ? gi * rest * xv : 0.f);
-          orr.v[v] = narrow<T>(s < n ? pull * closed : 0.f);
+          const float gt = widen(gy[s].v[v]) + start[v];
+          const float vx = on ? gt * to_x[s][v] : 0.f, pull = on ? gt * to_l[s][v] : 0.f;
+          ox.v[v] = narrow<T>(vx);
+          oi.v[v] = narrow<T>(on ? vx * to_i[s][v] : 0.f);
+          ol.v[v] = narrow<T>(on ? pull * closed[s][v] : 0.f);
           sum[v] += pull;
-          start[v] = e * gt;
+          start[v] = fa[s][v] * gt;
         }
-        const bool there = t_run + s < a.T;
+        const bool there = ALL || t_run + s < a.T;
         row_store<T, VEC>(dx + (tw + s) * g.dx.st, there ? at_dx : ROW_NOWHERE, ox);
         row_store<T, VEC>(di + (tw + s) * g.di.st, there ? at_di : ROW_NOWHERE, oi);
-        row_store<T, VEC>(dr + (tw + s) * g.dr.st, there ? at_dr : ROW_NOWHERE, orr);
+        row_store<T, VEC>(dr + (tw + s) * g.dr.st, there ? at_dr : ROW_NOWHERE, ol);
       }
-    }
-    if (t0 - S::TILE >= t_begin) fetch(t0 - S::TILE);
+    };
+    if (all) give(std::true_type());
+    else give(std::false_type());
   }
   if (!OUT) {
-    if (live && run == 0)
+    if (live && wave == 0 && !second)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) a.carry[(int64_t)seg * a.B * a.D + cell + v] = {p[v], q[v]};
     return;
   }
   __syncthreads();
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) link[0][run][c + v].a = sum[v];
+  for (int v = 0; v < VEC; ++v) {
+    float s = sum[v];
+    if (S::HALVES == 2) {
+      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+      s = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    }
+    if (!second) link[0][wave][c + v].a = s;
+  }
   __syncthreads();
-  if (live && run == 0)
+  if (live && wave == 0 && !second)
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       float s = 0.f;
-      for (int k = 0; k < S::RUNS; ++k) s += link[0][k][c + v].a;
+      for (int k = 0; k < WAVES; ++k) s += link[0][k][c + v].a;
       g.part[((int64_t)seg * a.B + b) * a.D + d + v] = s;
       if (g.dinit && seg == 0) g.dinit[cell + v] = q[v];
     }
