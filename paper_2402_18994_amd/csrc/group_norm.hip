@@ -35,15 +35,6 @@ struct NormP {
   float *dpart;                             // [units * blocks][2][D]
 };
 
-// v of this lane and of the one 16 (32) lanes away, added: the halves of two copies change places.
-__device__ __forceinline__ float add_16_apart(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float add_32_apart(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 // Sum over aligned sets of 2^w lanes, in all of them.
 __device__ __forceinline__ float wave_sum(float v, int w) {
   if (w >= 1) v += dpp<0xB1>(v);

@@ -52,17 +52,18 @@ __device__ __forceinline__ float rate_of(float sharpness, float decay) {
   return v < -0x1p127f ? -0x1p127f : v;
 }
 
-// 1 - a^2 for a = 2^L: where a^2 is near one, z p(z) with p the polynomial of degree 5 that is closest to (1 - exp(-z)) / z over [0, 1/2]
-// (off by 1.4e-9 of it; fitted by reweighted least squares); beyond, 1 - a a, where the rounding of a a is 1.5 units of the result's
-// last place.
-__device__ __forceinline__ float one_less_square(float L, float a) {
-  const float z = L * (-2.f * LN2);
-  float p = fmaf(z, -0x1.26079ep-10f, 0x1.0c48c4p-7f);
-  p = fmaf(p, z, -0x1.550686p-5f);
-  p = fmaf(p, z, 0x1.555304p-3f);
-  p = fmaf(p, z, -0x1.fffff4p-2f);
-  p = fmaf(p, z, 1.f);
-  return z < 0.5f ? z * p : fmaf(-a, a, 1.f);
+// 1 - a^2 for a = 2^L.  Where a^2 is near one (z = -2 ln 2 L <= 1/2), z p(z) with p the polynomial of degree 5 that is closest to
+// (1 - exp(-z)) / z over [0, 1/2] (off by 1.4e-9 of it; fitted by reweighted least squares), written in L; beyond, 1 - a a, where the
+// rounding of a a is 1.5 units of the result's last place.  NEAR: all channels of the wavefront leave so much at every step, since a
+// wholly open gate does.
+constexpr float NEAR_RATE = -0.36f;
+template <bool NEAR> __device__ __forceinline__ float one_less_square(float L, float a) {
+  float p = fmaf(L, -0x1.04e03ep-7f, -0x1.5768dcp-5f);
+  p = fmaf(p, L, -0x1.3ae1f2p-3f);
+  p = fmaf(p, L, -0x1.c6ad78p-2f);
+  p = fmaf(p, L, -0x1.ebfbd4p-1f);
+  p = fmaf(p, L, -0x1.62e430p+0f) * L;
+  return NEAR || L > NEAR_RATE ? p : fmaf(-a, a, 1.f);
 }
 // (root of m, its reciprocal); a root of zero has the reciprocal 2^63, so products with what goes to zero as fast stay zero.
 __device__ __forceinline__ float root_of(float m, float &inverse) {
@@ -162,12 +163,15 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
   };
   fetch(t0);
   float rate[VEC], h[VEC], p[VEC];
+  bool far = false;
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
     rate[v] = rate_of(a.sharpness, a.decay[dd + v]);
+    far = far || !(rate[v] >= NEAR_RATE);
     h[v] = OUT && a.init ? a.init[cell + v] : 0.f;
     p[v] = 1.f;
   }
+  const bool near = __ballot(far) == 0;
   if (OUT)
 #pragma unroll 4
     for (int k = 0; k < seg; ++k)
@@ -188,20 +192,20 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
     }
     float fa[STEPS][VEC], fb[STEPS][VEC], start[VEC];
     Link first[VEC];
-    // ALL: every step of the wavefront exists; otherwise those that do not have a = 1 and b = 0
-    auto maps = [&](auto all) {
-      constexpr bool ALL = decltype(all)::value;
+    // FAST: every step of the wavefront exists, and NEAR; otherwise those that do not exist have a = 1 and b = 0
+    auto maps = [&](auto fast) {
+      constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         Link m = {1.f, 0.f};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-          const bool on = ALL || s < n;
+          const bool on = FAST || s < n;
           float rest;
           const float rho = gate_of(widen(rr[s].v[v]), rest), iota = gate_of(widen(ri[s].v[v]), rest);
           const float L = on ? rate[v] * rho : 0.f, e = __builtin_amdgcn_exp2f(L);
           fa[s][v] = e;
-          fb[s][v] = on ? __builtin_amdgcn_sqrtf(one_less_square(L, e)) * iota * widen(rx[s].v[v]) : 0.f;
+          fb[s][v] = on ? __builtin_amdgcn_sqrtf(one_less_square<FAST>(L, e)) * iota * widen(rx[s].v[v]) : 0.f;
           m.h = fmaf(e, m.h, fb[s][v]);
           m.a *= e;
         }
@@ -210,7 +214,7 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_forward_kernel(const Re
       }
     };
     const bool all = tw + S::HALVES * STEPS <= len;
-    if (all) maps(std::true_type());
+    if (all && near) maps(std::true_type());
     else maps(std::false_type());
     if (t0 + S::TILE < t_end) fetch(t0 + S::TILE);
     lds_barrier();                                         // (two buffers: one barrier a tile)
@@ -266,13 +270,16 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const R
   const int t_begin = seg * a.tiles * S::TILE, t_end = min(a.T, t_begin + a.tiles * S::TILE);
 
   float rate[VEC], q[VEC], p[VEC], sum[VEC];
+  bool far = false;
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
     rate[v] = rate_of(a.sharpness, a.decay[dd + v]);
+    far = far || !(rate[v] >= NEAR_RATE);
     q[v] = OUT && g.d_state ? g.d_state[cell + v] : 0.f;
     p[v] = 1.f;
     sum[v] = 0.f;
   }
+  const bool near = __ballot(far) == 0;
   if (OUT)
 #pragma unroll 4
     for (int k = a.nseg - 1; k > seg; --k)
@@ -283,19 +290,19 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const R
       }
 
   const int wave_t = wave * S::HALVES * STEPS, half_t = lane / S::LANES * STEPS;
-  Pack<T, VEC> rx[STEPS], ri[STEPS], rr[STEPS], rg[STEPS];
-  float before[VEC];
+  Pack<T, VEC> nx[STEPS], ni[STEPS], nr[STEPS], ng[STEPS];
+  float nbefore[VEC];
   auto fetch = [&](int t) {
     const int tw = t + wave_t, n = len - (tw + half_t);
     const bool all = tw + S::HALVES * STEPS <= len;
-    load_run<T, VEC>(rr, r + tw * a.r.st, a.r.st, at_r, n, all);
+    load_run<T, VEC>(nr, r + tw * a.r.st, a.r.st, at_r, n, all);
     if (OUT) {
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) before[v] = a.saved[(int64_t)(n > 0 ? (tw + half_t) / STEPS : 0) * a.B * a.D + cell + v];
-      load_run<T, VEC>(ri, i + tw * a.i.st, a.i.st, at_i, n, all);
-      load_run<T, VEC>(rx, x + tw * a.x.st, a.x.st, at_x, n, all);
+      for (int v = 0; v < VEC; ++v) nbefore[v] = a.saved[(int64_t)(n > 0 ? (tw + half_t) / STEPS : 0) * a.B * a.D + cell + v];
+      load_run<T, VEC>(ni, i + tw * a.i.st, a.i.st, at_i, n, all);
+      load_run<T, VEC>(nx, x + tw * a.x.st, a.x.st, at_x, n, all);
     }
-    load_run<T, VEC>(rg, dy + tw * g.dy.st, g.dy.st, at_dy, n, all);
+    load_run<T, VEC>(ng, dy + tw * g.dy.st, g.dy.st, at_dy, n, all);
   };
   int t0 = t_begin + (t_end - 1 - t_begin) / S::TILE * S::TILE;
   for (; t0 >= t_begin && t0 >= len; t0 -= S::TILE) {      // tiles behind the sequence's end
@@ -314,24 +321,38 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const R
   for (int buf = 0; t0 >= t_begin; t0 -= S::TILE, buf ^= 1) {
     const int tw = t0 + wave_t, t_run = tw + half_t, n = len - t_run;
     const bool all = tw + S::HALVES * STEPS <= len;
+    Pack<T, VEC> rx[STEPS], ri[STEPS], rr[STEPS], rg[STEPS];
+    float before[VEC];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      rr[s] = nr[s];
+      rg[s] = ng[s];
+      if (OUT) {
+        rx[s] = nx[s];
+        ri[s] = ni[s];
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) before[v] = OUT ? nbefore[v] : 0.f;
+    if (t0 - S::TILE >= t_begin) fetch(t0 - S::TILE);
     // What each step multiplies g by: dx = g to_x, di = dx to_i, dr = g to_l closed (and g to_l is what sums up to ddecay).
     float fa[STEPS][VEC], to_x[STEPS][VEC], to_i[STEPS][VEC], to_l[STEPS][VEC], closed[STEPS][VEC], start[VEC];
     Link first[VEC];
-    auto maps = [&](auto exist) {
-      constexpr bool ALL = decltype(exist)::value;
+    auto maps = [&](auto fast) {
+      constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         Link m = {1.f, 0.f};
-        float h = OUT ? (ALL || n > 0 ? before[v] : 0.f) : 0.f;
+        float h = OUT ? (FAST || n > 0 ? before[v] : 0.f) : 0.f;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-          const bool on = ALL || s < n;
+          const bool on = FAST || s < n;
           const float rho = gate_of(widen(rr[s].v[v]), closed[s][v]);
           const float L = on ? rate[v] * rho : 0.f, e = __builtin_amdgcn_exp2f(L);
           fa[s][v] = e;
           if (!OUT) continue;
           float rest, inverse;
-          const float iota = gate_of(widen(ri[s].v[v]), rest), gain = root_of(one_less_square(L, e), inverse), xv = widen(rx[s].v[v]);
+          const float iota = gate_of(widen(ri[s].v[v]), rest), gain = root_of(one_less_square<FAST>(L, e), inverse), xv = widen(rx[s].v[v]);
           const float gi = gain * iota, le = L * LN2 * e;  // (l a; its limit is zero, also where l is as large as it gets)
           to_x[s][v] = gi;
           to_i[s][v] = rest * xv;
@@ -347,12 +368,8 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const R
         if (!second) link[buf][wave][c + v] = m;
       }
     };
-    if (all) maps(std::true_type());
+    if (all && near) maps(std::true_type());
     else maps(std::false_type());
-    Pack<T, VEC> gy[STEPS];
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) gy[s] = rg[s];
-    if (t0 - S::TILE >= t_begin) fetch(t0 - S::TILE);
     lds_barrier();
     join<VEC, WAVES, S::HALVES, true, !OUT>(link[buf], c, wave, second, first, q, p, start);
     if (!OUT) continue;
@@ -364,7 +381,7 @@ __global__ __launch_bounds__(WAVES * 64) void recurrence_backward_kernel(const R
         Pack<T, VEC> ox, oi, ol;
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-          const float gt = widen(gy[s].v[v]) + start[v];
+          const float gt = widen(rg[s].v[v]) + start[v];
           const float vx = on ? gt * to_x[s][v] : 0.f, pull = on ? gt * to_l[s][v] : 0.f;
           ox.v[v] = narrow<T>(vx);
           oi.v[v] = narrow<T>(on ? vx * to_i[s][v] : 0.f);
@@ -435,7 +452,7 @@ template <typename T, int VEC> __global__ __launch_bounds__(256) void recurrence
   for (int v = 0; v < VEC; ++v) {
     float rest, inverse;
     const float L = rate_of(a.sharpness, w.v[v]) * gate_of(widen(r.v[v]), rest), e = __builtin_amdgcn_exp2f(L);
-    h.v[v] = fmaf(e, h.v[v], root_of(one_less_square(L, e), inverse) * gate_of(widen(i.v[v]), rest) * widen(x.v[v]));
+    h.v[v] = fmaf(e, h.v[v], root_of(one_less_square<false>(L, e), inverse) * gate_of(widen(i.v[v]), rest) * widen(x.v[v]));
     y.v[v] = narrow<T>(h.v[v]);
   }
   *(F *)(a.state + (int64_t)b * a.D + d) = h;
@@ -474,7 +491,7 @@ struct RecCut {
 RecCut recurrence_cut(const snn_recurrence_args &a, int vec, bool backward) {
   RecCut c;
   const int64_t groups = (int64_t)(a.D + CH - 1) / CH * a.B;
-  c.waves = groups >= 256 && a.T > 128 ? (backward ? 8 : 16) : 4;
+  c.waves = groups < 256 || a.T <= 64 ? 4 : backward ? 8 : 16;
   const int tile = c.waves * vec * STEPS;                  // (Shape::TILE)
   const int all = std::max(1, (int)(((int64_t)a.T + tile - 1) / tile));
   const int64_t want = groups >= 256 ? 1 : std::min<int64_t>(64, (1024 + groups - 1) / groups);

@@ -24,6 +24,16 @@ template <typename T, int VEC> __device__ __forceinline__ void row_store(T *row,
   else st_b16(r, at, 0, __builtin_bit_cast(unsigned short, v));
 }
 
+// v of this lane and of the one 16 (32) lanes away, added: the halves of two copies change places.
+__device__ __forceinline__ float add_16_apart(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add_32_apart(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Whether the rows of a tensor of T steps of B sequences can be taken `vec` elements of `size` bytes at a time.
 inline bool rows_take(const snn_rows &r, int T, int B, int vec, size_t size) {
   return !r.p || (aligned(r.p, vec * size) && (T <= 1 || r.stride_t % vec == 0) && (B <= 1 || r.stride_b % vec == 0));
