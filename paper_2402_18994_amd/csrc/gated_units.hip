@@ -45,8 +45,9 @@ struct GemmP {
   Steps steps;
   Rows<void> out = Rows<void>(snn_rows{});   // y or dx
   void *w0, *w1;                             // dgate, dup
-  float *part;                               // [splits][rows of a][pitch]: sums of a part; UNITS: G and U, or NULL
+  float *part;                               // [splits][rows of a][pitch]: sums of a part; UNITS: G and U (of a part), or NULL
   int pitch, act;
+  int64_t part_size;                         // UNITS: of a part's G and U
   int M, N;                                  // rows of a; columns (units)
 };
 enum { UNITS, DX, DW, PART };
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
       for (int j = 0; j < TN / 2; ++j) {
         const int mb = m0 / 32 + wm * TM + i, fb = n0 / 32 + wn * TN / 2 + j;
         if (mb * 32 >= a.M || fb * 32 >= a.N) continue;
-        float *const at = a.part + kept_block(mb, fb, a.N) + lane * 4;
+        float *const at = a.part + split * a.part_size + kept_block(mb, fb, a.N) + lane * 4;
 #pragma unroll
         for (int g = 0; g < 4; ++g)
 #pragma unroll
@@ -235,6 +236,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
             *(Pack<float, 4> *)(at + (w * 4 + g) * 256) = {{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]}};
           }
       }
+  if (WHAT == UNITS && a.splits > 1) return;                 // (units_sum_kernel goes on)
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int m = m0 + (wm * TM + i) * 32 + (lane & 31);
@@ -292,6 +294,38 @@ template <typename T, int WHAT> __global__ __launch_bounds__(256) void gemm_sum_
   if (WHAT == DX && !a.steps.live((int)m, t, b)) v[0] = v[1] = v[2] = v[3] = 0.f;
   T *row = WHAT == DX ? (T *)a.out.p + t * a.out.st + b * a.out.sb : m < a.M / 2 ? (T *)a.w0 + m * a.N : (T *)a.w1 + (m - a.M / 2) * a.N;
   give4<T>(row, n, a.N, ((uintptr_t)row & (4 * sizeof(T) - 1)) == 0, v);
+}
+
+// G and U out of parts, and what becomes of them.  A wavefront has 32 rows by 32 units as they are kept.
+template <typename T> __global__ __launch_bounds__(256) void units_sum_kernel(const GemmP a, float *kept) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fbs = (a.N + 31) / 32;
+  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+  const int mb = (int)(id / fbs), fb = (int)(id - (int64_t)mb * fbs), m = mb * 32 + (lane & 31), n = fb * 32 + 4 * (lane >> 5);
+  if (mb * 32 >= a.M) return;
+  const int64_t at = kept_block(mb, fb, a.N) + lane * 4;
+  int t = 0, b = 0;
+  const bool live = m < a.M && a.steps.live(m, t, b);
+  T *row = (T *)a.out.p + t * a.out.st + b * a.out.sb;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    Pack<float, 4> vg = *(const Pack<float, 4> *)(a.part + at + g * 256), vu = *(const Pack<float, 4> *)(a.part + at + (4 + g) * 256);
+    for (int s = 1; s < a.splits; ++s) {
+      const Pack<float, 4> pg = *(const Pack<float, 4> *)(a.part + s * a.part_size + at + g * 256), pu = *(const Pack<float, 4> *)(a.part + s * a.part_size + at + (4 + g) * 256);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        vg.v[k] += pg.v[k];
+        vu.v[k] += pu.v[k];
+      }
+    }
+    if (kept) {
+      *(Pack<float, 4> *)(kept + at + g * 256) = vg;
+      *(Pack<float, 4> *)(kept + at + (4 + g) * 256) = vu;
+    }
+    float y[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = live ? act_of(a.act, vg.v[k]) * vu.v[k] : 0.f;
+    if (m < a.M && n + 8 * g < a.N) give4<T>(row, n + 8 * g, a.N, ((uintptr_t)row & (4 * sizeof(T) - 1)) == 0, y);
+  }
 }
 
 // ---------------------------------------------------------------- few rows
@@ -682,7 +716,7 @@ Tile tile_of(int64_t m, int64_t n) {
 // Parts of the contraction: as many as fill the chip (a wide tile has a compute unit to itself, small ones go two to one), of eight
 // stages at least.
 int splits_of(const Tile &t, int64_t tiles, int64_t stages) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>({stages / 8, 16, (t.wide ? 256 : 512) / std::max<int64_t>(1, tiles)}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({stages / 8, 32, (t.wide ? 256 : 512) / std::max<int64_t>(1, tiles)}));
 }
 
 struct Product {
@@ -698,6 +732,19 @@ Product product_of(int64_t m, int64_t n, int64_t stages) {
   return p;
 }
 size_t part_bytes(const Product &p, int64_t m, int n) { return p.splits > 1 ? rup256((size_t)p.splits * m * pitch_of(n) * 4) : 0; }
+
+int64_t kept_size(const snn_units_args &a) { return ((int64_t)a.T * a.B + 31) / 32 * ((a.F + 31) / 32) * KEPT; }
+// The forward product.  Its parts' sums cost 16 bytes a unit and part, and a launch: where tiles fill less than half of the chip.
+// UNITSPLIT
+Product units_product(const snn_units_args &a) {
+  const int64_t M = (int64_t)a.T * a.B, stages = (int64_t)panels_of(a.D) * (a.type == SNN_TYPE_FP32 ? 6 : 1);
+  Product p;
+  p.tile = tile_of(M, 2 * (int64_t)a.F);
+  p.mt = (int)((M + p.tile.bm - 1) / p.tile.bm);
+  p.nt = (a.F + p.tile.bn / 2 - 1) / (p.tile.bn / 2);
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({stages / 8, 16, 256 / std::max<int64_t>(1, (int64_t)p.mt * p.nt)}));
+  return p;
+}
 
 struct UnitsPlan {                           // of the reverse pass
   int64_t M;
@@ -812,17 +859,23 @@ template <typename T> int units_forward(const snn_units_args &a, void *saved, ch
     lays.job[jobs++] = lay_matrix<T>(a, a.up, up, p.b.stage, p.b.plane);
   }
   if (jobs && (rc = lay<T, false>(lays, jobs, st))) return rc;
-  const Tile tile = tile_of(M, 2 * (int64_t)a.F);
-  p.mt = (M + tile.bm - 1) / tile.bm;
-  p.nt = (a.F + tile.bn / 2 - 1) / (tile.bn / 2);
-  p.splits = 1;
+  const Product how = units_product(a);
+  p.mt = how.mt;
+  p.nt = how.nt;
+  p.splits = how.splits;
   p.steps = steps;
   p.out = Rows<void>(a.y, a.T);
   p.part = (float *)saved;
+  p.part_size = kept_size(a);
   p.act = a.act;
   p.M = M;
   p.N = a.F;
-  return launch_gemm<T, UNITS>(p, Product{tile, p.mt, p.nt, 1}, st);
+  if (p.splits == 1) return launch_gemm<T, UNITS>(p, how, st);
+  p.part = (float *)(weights_direct(a) ? ws : ws + 2 * rup256(panel_bytes(a.F, a.D, planes)));
+  if ((rc = launch_gemm<T, UNITS>(p, how, st))) return rc;
+  const int64_t blocks = (int64_t)((M + 31) / 32) * ((a.F + 31) / 32);
+  hipLaunchKernelGGL(units_sum_kernel<T>, dim3((unsigned)((blocks + 3) / 4)), dim3(256), 0, st, p, (float *)saved);
+  return ops_launched("gated units, sums");
 }
 
 template <typename T> __global__ __launch_bounds__(256) void clear_kernel(T *p, int64_t n) {
@@ -891,7 +944,8 @@ int32_t snn_units_workspace_bytes(const snn_units_args *a, int32_t backward, siz
     return SNN_OK;
   }
   int64_t row;
-  *bytes = few_rows(*a) ? 0 : (x_direct(*a, row) ? 0 : rup256(panel_bytes((int64_t)a->T * a->B, a->D, planes))) + (weights_direct(*a) ? 0 : 2 * rup256(panel_bytes(a->F, a->D, planes)));
+  *bytes = few_rows(*a) ? 0 : (x_direct(*a, row) ? 0 : rup256(panel_bytes((int64_t)a->T * a->B, a->D, planes))) + (weights_direct(*a) ? 0 : 2 * rup256(panel_bytes(a->F, a->D, planes))) +
+                                (units_product(*a).splits > 1 ? rup256(units_product(*a).splits * kept_size(*a) * 4) : 0);
   return SNN_OK;
 }
 

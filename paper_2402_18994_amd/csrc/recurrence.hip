@@ -484,17 +484,21 @@ bool strides_fit(const snn_rows &r, int T, size_t z) { return T <= 1 || !r.p || 
 
 size_t type_bytes(int32_t type) { return type == SNN_TYPE_FP32 ? 4 : 2; }
 
-// How time is cut: `waves` wavefronts a workgroup and segments of `tiles` tiles.
+// How time is cut: `waves` wavefronts a workgroup and segments of `tiles` tiles.  Segments cost a second reading, and are taken where
+// there are fewer (sequence, 64 channels) than workgroups that keep the chip busy: us of a forward (reverse) call in one piece and cut,
+// bf16 but for the second: 128 of 1024 steps 28.5 and 31.3 (55 and 45), 153 of 333 steps, fp32, 18.3 and 23.5 (30 and 35), 180 of
+// 200 steps 9.4 and 14.0 (21 and 25).  As many as make 1024 workgroups, reverse 512 (16 of 8192 steps: 36 and 39, reverse 51 and 45).
 struct RecCut {
   int waves, tiles, nseg;
 };
 RecCut recurrence_cut(const snn_recurrence_args &a, int vec, bool backward) {
   RecCut c;
   const int64_t groups = (int64_t)(a.D + CH - 1) / CH * a.B;
-  c.waves = groups < 256 || a.T <= 64 ? 4 : backward ? 8 : 16;
+  const bool enough = groups >= (backward ? 144 : 128);
+  c.waves = !enough || a.T <= 64 ? 4 : backward ? 8 : 16;
   const int tile = c.waves * vec * STEPS;                  // (Shape::TILE)
   const int all = std::max(1, (int)(((int64_t)a.T + tile - 1) / tile));
-  const int64_t want = groups >= 256 ? 1 : std::min<int64_t>(64, (1024 + groups - 1) / groups);
+  const int64_t want = enough ? 1 : std::min<int64_t>(64, ((backward ? 512 : 1024) + groups - 1) / groups);
   c.tiles = (int)((all + want - 1) / want);
   c.nseg = (all + c.tiles - 1) / c.tiles;
   return c;
