@@ -18,7 +18,7 @@
 namespace snn {
 namespace {
 
-constexpr int WIDE_WM = 2, WIDE_WN = 4, WIDE_SK = 64, WIDE_NS = 2;      // wavefronts of a wide tile
+constexpr int WIDE_WM = 2, WIDE_WN = 4;      // wavefronts of a wide tile
 constexpr int KS = 64;                       // k of a stage: a row of it is 128 bytes
 
 // One side of a product: stage `kp` of plane `plane`, row r at p + r row + kp stage + plane plane (bytes).
@@ -46,11 +46,16 @@ struct GemmP {
   Rows<void> out = Rows<void>(snn_rows{});   // y or dx
   void *w0, *w1;                             // dgate, dup
   float *part;                               // [splits][rows of a][pitch]: sums of a part; UNITS: G and U (of a part), or NULL
-  int pitch, act;
+  int what, pitch, act;
   int64_t part_size;                         // UNITS: of a part's G and U
   int M, N;                                  // rows of a; columns (units)
 };
-enum { UNITS, DX, DW, PART };
+enum { UNITS, GRADS };                       // what a product is; of GRADS each job is one of
+enum { DX, DW };
+struct Jobs {                                // products of one launch: the workgroups before `first` are the first one's
+  GemmP job[2];
+  int first;
+};
 
 // Which pieces meet in product `seg` of six, the smallest first: mid mid, hi lo, lo hi, hi mid, mid hi, hi hi (hi = 0).
 __device__ __forceinline__ int segment_a(int seg, int segs) { return segs == 1 ? 0 : (0x102010 >> (20 - 4 * seg)) & 0xF; }
@@ -88,7 +93,7 @@ template <typename T> __device__ __forceinline__ void give4(T *row, int n, int N
 
 // WM x WN wavefronts, each TM x TN blocks of 32 x 32 (m x n).  T: the type of what comes out.
 template <typename T, int WHAT, int WM, int WN, int TM, int TN, int SK, int NS>
-__global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
+__global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const Jobs jobs) {
   // SK: k of a stage; a row of it is RB bytes, RC chunks of 16, and a load of a wavefront brings RPL rows.  NS: stages in LDS
   constexpr int RB = 2 * SK, RC = RB / 16, RPL = 64 / RC, QS = SK / 16, PER = KS / SK;
   constexpr int NW = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, AI = BM / RPL / NW, BI = BN / RPL / NW;
@@ -97,11 +102,13 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
   auto turn = [](int r) { return SK == 64 ? (r >> 1) & 7 : (r >> 2) & 3; };
   static_assert(BM % (RPL * NW) == 0 && BN % (RPL * NW) == 0 && (WHAT != UNITS || TN % 2 == 0), "whole loads; gate and up in one wavefront");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const bool later = WHAT == GRADS && (int)blockIdx.x >= jobs.first;
+  const GemmP &a = jobs.job[later];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
   // Tiles: neighbours in time share an XCD's L2, so every XCD (workgroups go around them in turn) takes a run of tiles, and runs
   // walk eight rows of tiles before the next column.
-  int id = blockIdx.x;
+  int id = (int)blockIdx.x - (later ? jobs.first : 0);
   const int all = a.mt * a.nt, split = id / all;
   id -= split * all;
   {
@@ -218,8 +225,9 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
     for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[1][j], xa[1][i], acc[i][j], 0, 0, 0);
 
   // A lane holds, of block (i, j), row m = lane % 32 and columns 8 g + 4 h + 0..3 in element 4 g + 0..3.
-  const bool wide_out = WHAT == UNITS || WHAT == DX ? ((uintptr_t)a.out.p | (uintptr_t)(a.out.st * (int64_t)sizeof(T)) | (uintptr_t)(a.out.sb * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0
-                        : ((uintptr_t)a.w0 | (uintptr_t)a.w1 | (uintptr_t)((int64_t)a.N * sizeof(T))) % (4 * sizeof(T)) == 0;
+  const bool rows_out = WHAT == UNITS || a.what == DX, in_parts = WHAT == GRADS && a.splits > 1;
+  const bool wide_out = rows_out ? ((uintptr_t)a.out.p | (uintptr_t)(a.out.st * (int64_t)sizeof(T)) | (uintptr_t)(a.out.sb * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0
+                                 : ((uintptr_t)a.w0 | (uintptr_t)a.w1 | (uintptr_t)((int64_t)a.N * sizeof(T))) % (4 * sizeof(T)) == 0;
   if (WHAT == UNITS && a.part)
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -258,9 +266,8 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
         }
     } else {
       int t = 0, b = 0;
-      const bool live = WHAT != DX || a.steps.live(m, t, b);
-      T *row = WHAT == DX ? (T *)a.out.p + t * a.out.st + b * a.out.sb
-               : WHAT == DW ? (m < a.M / 2 ? (T *)a.w0 + (int64_t)m * a.N : (T *)a.w1 + (int64_t)(m - a.M / 2) * a.N) : nullptr;
+      const bool live = in_parts || !rows_out || a.steps.live(m, t, b);
+      T *row = in_parts ? nullptr : rows_out ? (T *)a.out.p + t * a.out.st + b * a.out.sb : m < a.M / 2 ? (T *)a.w0 + (int64_t)m * a.N : (T *)a.w1 + (int64_t)(m - a.M / 2) * a.N;
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -270,17 +277,20 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const GemmP a) {
           float v[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[k] = live ? acc[i][j][4 * g + k] : 0.f;
-          if (WHAT == PART) *(Pack<float, 4> *)(a.part + ((int64_t)split * a.M + m) * a.pitch + n) = {{v[0], v[1], v[2], v[3]}};
+          if (in_parts) *(Pack<float, 4> *)(a.part + ((int64_t)split * a.M + m) * a.pitch + n) = {{v[0], v[1], v[2], v[3]}};
           else give4<T>(row, n, a.N, wide_out, v);
         }
     }
   }
 }
 
-// The parts' sum, rounded, to where a product without parts writes it.  A thread has four columns of a row.
-template <typename T, int WHAT> __global__ __launch_bounds__(256) void gemm_sum_kernel(const GemmP a) {
+// The parts' sums, rounded, to where a product without parts writes them.  A thread has four columns of a row; `first`: workgroups of
+// the first job.
+template <typename T> __global__ __launch_bounds__(256) void gemm_sum_kernel(const Jobs jobs) {
+  const bool later = (int)blockIdx.x >= jobs.first;
+  const GemmP &a = jobs.job[later];
   const int quads = a.pitch / 4;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t id = ((int64_t)blockIdx.x - (later ? jobs.first : 0)) * 256 + threadIdx.x;
   const int64_t m = id / quads;
   const int n = (int)(id - m * quads) * 4;
   if (m >= a.M || n >= a.N) return;
@@ -291,8 +301,8 @@ template <typename T, int WHAT> __global__ __launch_bounds__(256) void gemm_sum_
     for (int k = 0; k < 4; ++k) v[k] += p.v[k];
   }
   int t = 0, b = 0;
-  if (WHAT == DX && !a.steps.live((int)m, t, b)) v[0] = v[1] = v[2] = v[3] = 0.f;
-  T *row = WHAT == DX ? (T *)a.out.p + t * a.out.st + b * a.out.sb : m < a.M / 2 ? (T *)a.w0 + m * a.N : (T *)a.w1 + (m - a.M / 2) * a.N;
+  if (a.what == DX && !a.steps.live((int)m, t, b)) v[0] = v[1] = v[2] = v[3] = 0.f;
+  T *row = a.what == DX ? (T *)a.out.p + t * a.out.st + b * a.out.sb : m < a.M / 2 ? (T *)a.w0 + m * a.N : (T *)a.w1 + (m - a.M / 2) * a.N;
   give4<T>(row, n, a.N, ((uintptr_t)row & (4 * sizeof(T) - 1)) == 0, v);
 }
 
@@ -584,11 +594,8 @@ template <typename T> __device__ __forceinline__ void put_transposed(const T (&t
       for (int q = 0; q < P; ++q) *(Chunk *)(dst + q * plane + (first_row + c) * 128 + (threadIdx.x & 7) * 16) = out[q];
   }
 }
-template <typename T> __global__ __launch_bounds__(256) void lay_transposed_kernel(const LayJobs jobs) {
-  __shared__ T tile[KS][KS + 1];
-  const LayP &a = jobs.job[blockIdx.z];
-  const int m0 = blockIdx.x * KS, c0 = blockIdx.y * KS;
-  if (m0 >= a.rows || c0 >= a.cols) return;
+template <typename T> __device__ __forceinline__ void lay_transposed(const LayP &a, T (&tile)[KS][KS + 1], int bx, int by) {
+  const int m0 = bx * KS, c0 = by * KS;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int r = (threadIdx.x + 256 * u) / 8, c = (threadIdx.x & 7) * 8, m = m0 + r;
@@ -599,7 +606,7 @@ template <typename T> __global__ __launch_bounds__(256) void lay_transposed_kern
     for (int k = 0; k < 8; ++k) tile[r][c + k] = v.v[k];
   }
   __syncthreads();
-  put_transposed<T>(tile, a.dst + blockIdx.x * a.stage, a.plane, c0, a.cols - c0);
+  put_transposed<T>(tile, a.dst + bx * a.stage, a.plane, c0, a.cols - c0);
 }
 
 // dG and dU from dy and the sums of the forward pass, both ways round: [f / 64][m][64] (dU behind dG along f) and [m / 64][f][64].
@@ -611,9 +618,8 @@ struct SlopeP {
   char *rows, *cols;
   int64_t rows_stage, rows_plane, cols_stage, cols_plane;
 };
-template <typename T> __global__ __launch_bounds__(256) void slope_kernel(const SlopeP a) {
-  __shared__ T tile[2][KS][KS + 1];          // dy stands in the first one at the start
-  const int m0 = blockIdx.x * KS, f0 = blockIdx.y * KS, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+template <typename T> __device__ __forceinline__ void slopes(const SlopeP &a, T (&tile)[2][KS][KS + 1], int bx, int by) {
+  const int m0 = bx * KS, f0 = by * KS, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int mb = m0 / 32 + (wave & 1), fb = f0 / 32 + (wave >> 1), h = lane >> 5, r = (wave & 1) * 32 + (lane & 31), c = (wave >> 1) * 32 + 4 * h;
   const bool there = mb * 32 < a.M && fb * 32 < a.F;
   Pack<float, 4> g[4], u[4];
@@ -666,10 +672,28 @@ template <typename T> __global__ __launch_bounds__(256) void slope_kernel(const 
       if (m0 + row < a.M)
 #pragma unroll
         for (int q = 0; q < P; ++q)
-          *(Chunk *)(a.rows + q * a.rows_plane + (w * a.panels + blockIdx.y) * a.rows_stage + (int64_t)(m0 + row) * 128 + (threadIdx.x & 7) * 16) = out[q];
+          *(Chunk *)(a.rows + q * a.rows_plane + (w * a.panels + by) * a.rows_stage + (int64_t)(m0 + row) * 128 + (threadIdx.x & 7) * 16) = out[q];
     }
-    put_transposed<T>(tile[w], a.cols + blockIdx.x * a.cols_stage, a.cols_plane, (int64_t)w * a.F + f0, a.F - f0);
+    put_transposed<T>(tile[w], a.cols + bx * a.cols_stage, a.cols_plane, (int64_t)w * a.F + f0, a.F - f0);
   }
+}
+
+// What the reverse products read, in one launch: the slopes' tiles, then those of x, gate and up (first[i]: the first workgroup of job i;
+// tiles along the rows first).
+struct ReadyP {
+  SlopeP slope;
+  LayJobs lays;
+  int first[3], along[4];                    // along: tiles along the rows, of the slopes and of each job
+};
+template <typename T> __global__ __launch_bounds__(256) void ready_kernel(const ReadyP a) {
+  __shared__ T tile[2][KS][KS + 1];          // (slopes: dy stands in the first one at the start)
+  const int id = blockIdx.x;
+  if (id < a.first[0]) {
+    slopes<T>(a.slope, tile, id % a.along[0], id / a.along[0]);
+    return;
+  }
+  const int job = id < a.first[1] ? 0 : id < a.first[2] ? 1 : 2, at = id - a.first[job];
+  lay_transposed<T>(a.lays.job[job], tile[0], at % a.along[job + 1], at / a.along[job + 1]);
 }
 
 // ---------------------------------------------------------------- host
@@ -713,36 +737,24 @@ Tile tile_of(int64_t m, int64_t n) {
   const int64_t wide = ((m + 255) / 256) * ((n + 255) / 256);
   return wide >= 192 ? Tile{256, 256, true} : Tile{128, 128, false};
 }
-// Parts of the contraction: as many as fill the chip (a wide tile has a compute unit to itself, small ones go two to one), of eight
-// stages at least.
-int splits_of(const Tile &t, int64_t tiles, int64_t stages) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>({stages / 8, 32, (t.wide ? 256 : 512) / std::max<int64_t>(1, tiles)}));
-}
-
 struct Product {
   Tile tile;
   int mt, nt, splits;
 };
-Product product_of(int64_t m, int64_t n, int64_t stages) {
-  Product p;
-  p.tile = tile_of(m, n);
-  p.mt = (int)((m + p.tile.bm - 1) / p.tile.bm);
-  p.nt = (int)((n + p.tile.bn - 1) / p.tile.bn);
-  p.splits = splits_of(p.tile, (int64_t)p.mt * p.nt, stages);
-  return p;
-}
 size_t part_bytes(const Product &p, int64_t m, int n) { return p.splits > 1 ? rup256((size_t)p.splits * m * pitch_of(n) * 4) : 0; }
 
 int64_t kept_size(const snn_units_args &a) { return ((int64_t)a.T * a.B + 31) / 32 * ((a.F + 31) / 32) * KEPT; }
-// The forward product.  Its parts' sums cost 16 bytes a unit and part, and a launch: where tiles fill less than half of the chip.
-// UNITSPLIT
+// The forward product.  Its parts' sums cost 16 bytes a unit and part, and a launch: where tiles fill a third of
+// the chip at most, and have 32 stages (us without and with: 300 rows, 2048 -> 1024, bf16 20.4 and 15.9, fp32 95 and 44; 1000 rows,
+// 1000 -> 300, bf16, 16 stages 18.1 and 19.7; 2000 rows, 2048 -> 512, 128 tiles 21.6 and 22.5).
 Product units_product(const snn_units_args &a) {
   const int64_t M = (int64_t)a.T * a.B, stages = (int64_t)panels_of(a.D) * (a.type == SNN_TYPE_FP32 ? 6 : 1);
   Product p;
   p.tile = tile_of(M, 2 * (int64_t)a.F);
   p.mt = (int)((M + p.tile.bm - 1) / p.tile.bm);
   p.nt = (a.F + p.tile.bn / 2 - 1) / (p.tile.bn / 2);
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({stages / 8, 16, 256 / std::max<int64_t>(1, (int64_t)p.mt * p.nt)}));
+  const int64_t tiles = std::max<int64_t>(1, (int64_t)p.mt * p.nt);
+  p.splits = stages >= 32 && tiles <= 85 ? (int)std::min<int64_t>({stages / 8, 16, 256 / tiles}) : 1;
   return p;
 }
 
@@ -750,58 +762,59 @@ struct UnitsPlan {                           // of the reverse pass
   int64_t M;
   int planes, segs;
   Product dx, dw;
-  size_t rows, cols, xt, wt, part;           // bytes of each piece of the workspace
+  size_t rows, cols, xt, wt, part_dx, part_dw;   // bytes of each piece of the workspace
 };
+// Both products are one launch.  Small tiles, and parts of the contraction, where there are too few tiles for the chip: so many parts
+// that the workgroups (one a compute unit of wide tiles, two of small ones) have about the same number of stages, eight at least.
 UnitsPlan units_plan(const snn_units_args &a) {
   UnitsPlan u;
   u.M = (int64_t)a.T * a.B;
   u.planes = a.type == SNN_TYPE_FP32 ? 3 : 1;
   u.segs = u.planes == 3 ? 6 : 1;
   const int64_t F2 = 2 * (int64_t)panels_of(a.F) * KS;
-  u.dx = product_of(u.M, a.D, (int64_t)2 * panels_of(a.F) * u.segs);
-  u.dw = product_of(2 * (int64_t)a.F, a.D, (int64_t)panels_of(u.M) * u.segs);
+  auto tiles = [](int64_t m, int64_t n, int b) { return (m + b - 1) / b * ((n + b - 1) / b); };
+  const bool wide = tiles(u.M, a.D, 256) + tiles(2 * (int64_t)a.F, a.D, 256) >= 192;
+  const int64_t stages_dx = (int64_t)2 * panels_of(a.F) * u.segs, stages_dw = (int64_t)panels_of(u.M) * u.segs;
+  const int b = wide ? 256 : 128;
+  const int64_t all = tiles(u.M, a.D, b) * stages_dx + tiles(2 * (int64_t)a.F, a.D, b) * stages_dw, each = std::max<int64_t>(8, all / (wide ? 256 : 512));
+  auto product = [&](int64_t m, int64_t stages) {
+    Product p;
+    p.tile = Tile{b, b, wide};
+    p.mt = (int)((m + b - 1) / b);
+    p.nt = (a.D + b - 1) / b;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, stages / each));
+    return p;
+  };
+  u.dx = product(u.M, stages_dx);
+  u.dw = product(2 * (int64_t)a.F, stages_dw);
   u.rows = rup256(panel_bytes(u.M, F2, u.planes));
   u.cols = rup256(panel_bytes(2 * (int64_t)a.F, u.M, u.planes));
   u.xt = rup256(panel_bytes(a.D, u.M, u.planes));
   u.wt = rup256(panel_bytes(a.D, F2, u.planes));
-  u.part = std::max(part_bytes(u.dx, u.M, a.D), part_bytes(u.dw, 2 * (int64_t)a.F, a.D));
+  u.part_dx = part_bytes(u.dx, u.M, a.D);
+  u.part_dw = part_bytes(u.dw, 2 * (int64_t)a.F, a.D);
   return u;
 }
 
-template <typename T, int WHAT> int launch_gemm(const GemmP &p, const Product &how, hipStream_t st) {
-  const int64_t n = (int64_t)p.mt * p.nt * p.splits;
+// Workgroups of a product.
+int64_t blocks_of(const GemmP &p) { return (int64_t)p.mt * p.nt * p.splits; }
+template <typename T, int WHAT> int launch_gemm(const Jobs &jobs, int64_t n, bool wide, hipStream_t st) {
   if (n * 512 >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "gated units: too large for one launch");
-  if (how.tile.wide) {
-    auto k = gemm_kernel<T, WHAT, WIDE_WM, WIDE_WN, 8 / WIDE_WM, 8 / WIDE_WN, WIDE_SK, WIDE_NS>;
-    const int bytes = WIDE_NS * (256 + 256) * WIDE_SK * 2;
-    const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
-    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(64 * WIDE_WM * WIDE_WN), bytes, st, p);
-  } else {
-    // (up to one a compute unit: four stages in LDS, three of them on their way; more: two, and two workgroups a compute unit)
-    auto k = n <= 256 ? gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 4> : gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 2>;
-    const int bytes = (n <= 256 ? 4 : 2) * (128 + 128) * 128;
-    const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
-    hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(256), bytes, st, p);
-  }
+  // (small tiles, up to one a compute unit: four stages in LDS, three of them on their way; more: two, and two workgroups a compute unit)
+  auto k = wide ? gemm_kernel<T, WHAT, WIDE_WM, WIDE_WN, 8 / WIDE_WM, 8 / WIDE_WN, 64, 2>
+           : n <= 256 ? gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 4> : gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 2>;
+  const int bytes = wide ? 2 * (256 + 256) * 128 : (n <= 256 ? 4 : 2) * (128 + 128) * 128;
+  const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
+  hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(wide ? 64 * WIDE_WM * WIDE_WN : 256), bytes, st, jobs);
   return ops_launched("gated units, product");
-}
-template <typename T, int WHAT> int launch_product(GemmP p, const Product &how, hipStream_t st) {
-  if (p.splits == 1) return launch_gemm<T, WHAT>(p, how, st);
-  const int rc = launch_gemm<T, PART>(p, how, st);
-  if (rc) return rc;
-  const int64_t threads = (int64_t)p.M * (p.pitch / 4);
-  hipLaunchKernelGGL((gemm_sum_kernel<T, WHAT>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, p);
-  return ops_launched("gated units, sums");
 }
 
 // A launch for `n` jobs.
-template <typename T, bool TRANSPOSED> int lay(const LayJobs &jobs, int n, hipStream_t st) {
+template <typename T> int lay(const LayJobs &jobs, int n, hipStream_t st) {
   int rows = 0, cols = 0;
   for (int i = 0; i < n; ++i) rows = std::max(rows, jobs.job[i].rows), cols = std::max(cols, jobs.job[i].cols);
-  if (TRANSPOSED) hipLaunchKernelGGL(lay_transposed_kernel<T>, dim3(panels_of(rows), panels_of(cols), n), dim3(256), 0, st, jobs);
-  else hipLaunchKernelGGL(lay_rows_kernel<T>, dim3((rows + 31) / 32, panels_of(cols), n), dim3(256), 0, st, jobs);
+  hipLaunchKernelGGL(lay_rows_kernel<T>, dim3((rows + 31) / 32, panels_of(cols), n), dim3(256), 0, st, jobs);
   return ops_launched("gated units, layout");
 }
 // x or a matrix as a job.
@@ -858,7 +871,7 @@ template <typename T> int units_forward(const snn_units_args &a, void *saved, ch
     lays.job[jobs++] = lay_matrix<T>(a, a.gate, ws, p.b.stage, p.b.plane);
     lays.job[jobs++] = lay_matrix<T>(a, a.up, up, p.b.stage, p.b.plane);
   }
-  if (jobs && (rc = lay<T, false>(lays, jobs, st))) return rc;
+  if (jobs && (rc = lay<T>(lays, jobs, st))) return rc;
   const Product how = units_product(a);
   p.mt = how.mt;
   p.nt = how.nt;
@@ -870,9 +883,9 @@ template <typename T> int units_forward(const snn_units_args &a, void *saved, ch
   p.act = a.act;
   p.M = M;
   p.N = a.F;
-  if (p.splits == 1) return launch_gemm<T, UNITS>(p, how, st);
+  if (p.splits == 1) return launch_gemm<T, UNITS>(Jobs{{p, p}, 0}, blocks_of(p), how.tile.wide, st);
   p.part = (float *)(weights_direct(a) ? ws : ws + 2 * rup256(panel_bytes(a.F, a.D, planes)));
-  if ((rc = launch_gemm<T, UNITS>(p, how, st))) return rc;
+  if ((rc = launch_gemm<T, UNITS>(Jobs{{p, p}, 0}, blocks_of(p), how.tile.wide, st))) return rc;
   const int64_t blocks = (int64_t)((M + 31) / 32) * ((a.F + 31) / 32);
   hipLaunchKernelGGL(units_sum_kernel<T>, dim3((unsigned)((blocks + 3) / 4)), dim3(256), 0, st, p, (float *)saved);
   return ops_launched("gated units, sums");
@@ -898,32 +911,51 @@ template <typename T> int units_backward(const snn_units_args &a, const snn_unit
   const Steps steps{a.T, a.B, a.lengths};
   char *const rows = ws, *const cols = rows + u.rows, *const xt = cols + u.cols, *const wt = xt + u.xt, *const part = wt + u.wt;
   const int64_t st_r = (int64_t)M * 128, st_c = (int64_t)2 * a.F * 128, st_x = (int64_t)a.D * 128, pl_w = st_x * 2 * pf;
-  SlopeP s{steps, Rows<void>(g.dy, a.T), saved, a.act, M, a.F, pf, rows_take(g.dy, a.T, a.B, 8, sizeof(T)), rows, cols, st_r, st_r * 2 * pf, st_c, st_c * pm};
-  hipLaunchKernelGGL(slope_kernel<T>, dim3(pm, pf), dim3(256), 0, st, s);
+  ReadyP r{{steps, Rows<void>(g.dy, a.T), saved, a.act, M, a.F, pf, rows_take(g.dy, a.T, a.B, 8, sizeof(T)), rows, cols, st_r, st_r * 2 * pf, st_c, st_c * pm},
+           {{lay_x<T>(a, xt, st_x, st_x * pm), lay_matrix<T>(a, a.gate, wt, st_x, pl_w), lay_matrix<T>(a, a.up, wt + st_x * pf, st_x, pl_w)}},
+           {},
+           {pm, pm, pf, pf}};
+  const int64_t pd = panels_of(a.D), n0 = (int64_t)pm * pf, n1 = n0 + pm * pd, n2 = n1 + pf * pd, n3 = n2 + pf * pd;
+  if (n3 * 256 >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "gated units backward: too large for one launch");
+  r.first[0] = (int)n0; r.first[1] = (int)n1; r.first[2] = (int)n2;
+  hipLaunchKernelGGL(ready_kernel<T>, dim3((unsigned)n3), dim3(256), 0, st, r);
   if ((rc = ops_launched("gated units backward, slopes"))) return rc;
-  const LayJobs lays{{lay_x<T>(a, xt, st_x, st_x * pm), lay_matrix<T>(a, a.gate, wt, st_x, pl_w), lay_matrix<T>(a, a.up, wt + st_x * pf, st_x, pl_w)}};
-  if ((rc = lay<T, true>(lays, 3, st))) return rc;
-  GemmP p{};
-  p.segs = u.segs;
-  p.steps = steps;
-  p.part = (float *)part;
-  p.N = a.D;
-  p.pitch = pitch_of(a.D);
-  p.out = Rows<void>(g.dx, a.T);
-  p.w0 = g.dgate;
-  p.w1 = g.dup;
-  p.a = Side{rows, nullptr, 128, st_r, st_r * 2 * pf, M};
-  p.b = Side{wt, nullptr, 128, st_x, pl_w, a.D};
-  p.panels = 2 * pf;
-  p.M = M;
-  p.mt = u.dx.mt; p.nt = u.dx.nt; p.splits = u.dx.splits;
-  if ((rc = launch_product<T, DX>(p, u.dx, st))) return rc;
-  p.a = Side{cols, nullptr, 128, st_c, st_c * pm, 2 * a.F};
-  p.b = Side{xt, nullptr, 128, st_x, st_x * pm, a.D};
-  p.panels = pm;
-  p.M = 2 * a.F;
-  p.mt = u.dw.mt; p.nt = u.dw.nt; p.splits = u.dw.splits;
-  return launch_product<T, DW>(p, u.dw, st);
+
+  Jobs jobs{};
+  GemmP &x = jobs.job[0], &w = jobs.job[1];
+  x.what = DX;
+  x.a = Side{rows, nullptr, 128, st_r, st_r * 2 * pf, M};
+  x.b = Side{wt, nullptr, 128, st_x, pl_w, a.D};
+  x.panels = 2 * pf;
+  x.M = M;
+  x.part = (float *)part;
+  w.what = DW;
+  w.a = Side{cols, nullptr, 128, st_c, st_c * pm, 2 * a.F};
+  w.b = Side{xt, nullptr, 128, st_x, st_x * pm, a.D};
+  w.panels = pm;
+  w.M = 2 * a.F;
+  w.part = (float *)(part + u.part_dx);
+  for (GemmP *p : {&x, &w}) {
+    const Product &how = p == &x ? u.dx : u.dw;
+    p->mt = how.mt; p->nt = how.nt; p->splits = how.splits;
+    p->segs = u.segs;
+    p->steps = steps;
+    p->N = a.D;
+    p->pitch = pitch_of(a.D);
+    p->out = Rows<void>(g.dx, a.T);
+    p->w0 = g.dgate;
+    p->w1 = g.dup;
+  }
+  jobs.first = (int)blocks_of(x);
+  if ((rc = launch_gemm<T, GRADS>(jobs, blocks_of(x) + blocks_of(w), u.dx.tile.wide, st))) return rc;
+  // (a product without parts has no sums)
+  auto sums = [](const GemmP &p) { return p.splits > 1 ? ((int64_t)p.M * (p.pitch / 4) + 255) / 256 : 0; };
+  const int64_t n = sums(x) + sums(w);
+  if (!n) return SNN_OK;
+  if (n * 256 >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "gated units backward: too large for one launch");
+  jobs.first = (int)sums(x);
+  hipLaunchKernelGGL(gemm_sum_kernel<T>, dim3((unsigned)n), dim3(256), 0, st, jobs);
+  return ops_launched("gated units backward, sums");
 }
 
 }  // namespace
@@ -940,7 +972,7 @@ int32_t snn_units_workspace_bytes(const snn_units_args *a, int32_t backward, siz
   const int planes = a->type == SNN_TYPE_FP32 ? 3 : 1;
   if (backward) {
     const UnitsPlan u = units_plan(*a);
-    *bytes = u.rows + u.cols + u.xt + u.wt + u.part;
+    *bytes = u.rows + u.cols + u.xt + u.wt + u.part_dx + u.part_dw;
     return SNN_OK;
   }
   int64_t row;
