@@ -208,6 +208,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const Jobs jobs) {
     const char *st = lds + buf * STAGE;
     prepare(buf ? buf - 1 : NS - 1);
     buf = buf + 1 < NS ? buf + 1 : 0;
+    __builtin_amdgcn_s_setprio(1);                           // (3 % of the forward product: the wavefront ahead stays ahead)
     static_for<QS * Q>([&](auto X) {
       constexpr int x = decltype(X)::value, g = x / Q, y = x % Q, s = (g + QS - 1) % QS, i = y / TN, j = y % TN;
       __builtin_amdgcn_sched_barrier(0);
@@ -216,6 +217,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const Jobs jobs) {
       if constexpr (2 * y + 1 < TM + TN) read(st, g, 2 * y + 1);
       if constexpr (x % EVERY == EVERY - 1 && x / EVERY < LOADS) load(x / EVERY);
     });
+    __builtin_amdgcn_s_setprio(0);
   }
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (no load outlives the workgroup's LDS)
@@ -343,7 +345,7 @@ template <typename T> __global__ __launch_bounds__(256) void units_sum_kernel(co
 // each of its wavefronts every WAVES-th piece of 128 bytes of the rows; their sums meet in LDS.  A wavefront brings its pieces into
 // LDS by itself, NB - 1 of them ahead (no barrier), and takes the operands of the matrix instructions from there: loaded straight
 // into operand registers, where neighbouring lanes have different rows, every 16 lanes touch 16 cache lines, and a compute unit
-// gets 16 bytes a cycle (64 rows, 2048 -> 4096, bf16: 14.4 us against FEWNOW).  fp32 stays fp32 here: the fp32 matrix instructions
+// gets 16 bytes a cycle (64 rows, 2048 -> 4096, bf16: 14.4 us against 9.3).  fp32 stays fp32 here: the fp32 matrix instructions
 // keep up, and the matrices need no pass before.
 constexpr int FEW = 64, FEW_UNITS = 16;
 
@@ -825,7 +827,8 @@ template <typename T> LayP lay_matrix(const snn_units_args &a, const void *w, ch
   return LayP{w, 0, a.D, Steps{1, 1 << 30, nullptr}, a.F, a.D, dst, stage, plane, a.D % 8 == 0 && aligned(w, 8 * sizeof(T))};
 }
 
-// Up to as many rows as the tiles, which lay fp32 matrices out first, are slower at.  FEWRULE
+// Up to 128 rows, of fp32 256, which the tiles would lay out first (us here and as tiles, 2048 -> 4096: bf16, 128 rows 16.8 and 19.4; fp32, 256
+// rows 90 and 114; 2048 -> 1024: 8.7 and 15.5, 23 and 44).
 bool few_rows(const snn_units_args &a) { return (int64_t)a.T * a.B <= (a.type == SNN_TYPE_FP32 ? 4 * FEW : 2 * FEW); }
 template <typename T, int MB, int WAVES, int NB> int launch_few(const FewP &p, bool wide, hipStream_t st) {
   const dim3 grid((p.F + FEW_UNITS - 1) / FEW_UNITS, (p.M + 16 * MB - 1) / (16 * MB));

@@ -644,7 +644,7 @@ struct NormCut {
   int nt, tpr_log2, K, R, loops, blocks;       // threads; threads a row (log2); column blocks; rows a thread; lots; workgroups a unit and group
   bool chunks;
 };
-NormCut norm_cut(const snn_norm_args &a, int vec) {
+NormCut norm_cut(const snn_norm_args &a, int vec, bool backward) {
   const size_t z = a.type == SNN_TYPE_FP32 ? 4 : 2;
   const int C = a.D / a.groups, slots = vec * z == 16 ? 8 : 16;
   const int64_t rows = a.per_step ? (int64_t)a.T * a.B : a.T, units = a.per_step ? 1 : a.B;
@@ -668,10 +668,20 @@ NormCut norm_cut(const snn_norm_args &a, int vec) {
     c.blocks = (int)((n + c.loops - 1) / c.loops);
     return c;
   }
-  const int64_t rp = c.nt >> c.tpr_log2;
   c.R = slots;
   c.blocks = 1;
-  if (c.K == 1 && blocks_of(rp * slots) == 1) return c;
+  // A sequence's group at once, where the registers of 256 threads hold it, or those of 512 and there are 64 groups at least; reverse with
+  // 16-byte vectors never, since x and dy with what is formed of them do not
+  // fit.  (us of a forward and a reverse call: 51 of 257 steps, 130 channels in 5 groups, fp32, 7.8 and 16.1, in chunks 12.6 and 18.6; 16 of
+  // 500 steps, 512 channels in 8, bf16, reverse at once 41.8, in chunks 22.2.)
+  if (c.K == 1 && !(backward && vec * z == 16)) {
+    if (blocks_of((256 >> c.tpr_log2) * slots) == 1) return c;
+    if (units * a.groups >= 64 && blocks_of((512 >> c.tpr_log2) * slots) == 1) {
+      c.nt = 512;
+      return c;
+    }
+  }
+  const int64_t rp = 256 >> c.tpr_log2;
   c.chunks = true;
   c.R = 64;                                    // rows a thread: as many as leave workgroups enough
   while (c.R > AHEAD && blocks_of(rp * c.R) * units * a.groups < 1024) c.R /= 2;
@@ -691,7 +701,7 @@ size_t part_bytes(const snn_norm_args &a, const NormCut &c) { return c.chunks ? 
 size_t norm_bytes(const snn_norm_args &a, bool backward) {
   size_t most = 0;
   for (int vec : {a.type == SNN_TYPE_FP32 ? 4 : 8, 2, 1}) {
-    const NormCut c = norm_cut(a, vec);
+    const NormCut c = norm_cut(a, vec, backward);
     most = std::max(most, part_bytes(a, c) + (backward ? rup256((size_t)(a.per_step ? 1 : a.B) * c.blocks * 2 * (size_t)a.D * 4) : 0));
   }
   return most;
@@ -718,7 +728,8 @@ int norm_grid(const snn_norm_args &a, const NormCut &c, dim3 &grid) {
 
 template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
   if (!per_step) {
-    if (!c.chunks) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, WHOLE, true>), grid, dim3(256), 0, st, p);
+    if (!c.chunks && c.nt == 512) hipLaunchKernelGGL((norm_forward_kernel<T, V, 512, WHOLE, true>), grid, dim3(512), 0, st, p);
+    else if (!c.chunks) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, WHOLE, true>), grid, dim3(256), 0, st, p);
     else {
       hipLaunchKernelGGL((norm_moments_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
       const int e = ops_launched("group norm, moments");
@@ -733,8 +744,12 @@ template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, co
 }
 template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
   if (!per_step) {
-    if (!c.chunks) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, WHOLE, true>), grid, dim3(256), 0, st, p);
-    else {
+    if (!c.chunks) {
+      if constexpr (sizeof(T) * V < 16) {
+        if (c.nt == 512) hipLaunchKernelGGL((norm_backward_kernel<T, V, 512, WHOLE, true>), grid, dim3(512), 0, st, p);
+        else hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, WHOLE, true>), grid, dim3(256), 0, st, p);
+      }
+    } else {
       hipLaunchKernelGGL((norm_slopes_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
       const int e = ops_launched("group norm backward, sums");
       if (e) return e;
@@ -779,7 +794,7 @@ int32_t snn_norm_forward(const snn_norm_args *a, void *saved, void *workspace, s
     return ops_fail(SNN_ERR_WORKSPACE, "group norm: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
   if (a->T == 0) return SNN_OK;
   const int vec = norm_vector(*a, nullptr);
-  const NormCut c = norm_cut(*a, vec);
+  const NormCut c = norm_cut(*a, vec, false);
   dim3 grid;
   if ((rc = norm_grid(*a, c, grid))) return rc;
   const NormP p = norm_args(*a, c, saved, workspace);
@@ -798,7 +813,7 @@ int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < need)
     return ops_fail(SNN_ERR_WORKSPACE, "group norm backward: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
   const int vec = norm_vector(*a, g);
-  const NormCut c = norm_cut(*a, vec);
+  const NormCut c = norm_cut(*a, vec, true);
   dim3 grid;
   if ((rc = norm_grid(*a, c, grid))) return rc;
   NormP p = norm_args(*a, c, const_cast<void *>(saved), workspace);
