@@ -475,6 +475,8 @@ def _rec_args(x, i, r, decay, sharpness, init, lengths, step=False):
     kind, dev = _start(x)
     shape, dtype, f32 = _sizes(x, step), x.dtype, torch.float32
     *_, B, D = shape
+    if not 0 < sharpness <= 3e38:
+        _refuse("sharpness has to be positive and finite")
     head = (1 if step else shape[0], B, D, kind, sharpness, *_first(x, shape), *_rows(i, dtype, dev, shape, "i"), *_rows(r, dtype, dev, shape, "r"))
     _need(decay is not None, "decay is needed")
     tail = (_dense(decay, dev, (D,), f32, "decay"), _dense(init, dev, (B, D), f32, "init"), _dense(lengths, dev, (B,), torch.int32, "lengths"))
@@ -529,8 +531,10 @@ def _norm_args(x, groups, weight, bias, silu, eps, per_step, lengths, step=False
     kind, dev = _start(x)
     shape, f32 = _sizes(x, step), torch.float32
     *_, B, D = shape
-    if groups < 1 or D % groups:
-        _refuse("groups has to divide D")
+    if not isinstance(groups, int) or groups < 1 or D % groups:
+        _refuse("groups has to be a whole number that divides D")
+    if not 0 <= eps <= 3e38:
+        _refuse("eps must not be negative and has to be finite")
     head = (1 if step else shape[0], B, D, groups, kind, 1 if silu else 0, 1 if per_step else 0, eps, *_first(x, shape))
     tail = (_dense(weight, dev, (D,), f32, "weight"), _dense(bias, dev, (D,), f32, "bias"), _dense(lengths, dev, (B,), torch.int32, "lengths"))
     return dev, lambda y: _NORM.pack(*head, y, B * D, D, *tail)
@@ -584,13 +588,13 @@ def _units_args(x, gate, up, act, lengths, step=False):
     kind, dev = _start(x)
     shape = _sizes(x, step)
     *_, B, D = shape
+    _need(gate is not None and up is not None, "gate and up are needed")
     if gate.dim() != 2 or gate.shape[1] != D or gate.shape[0] == 0:
         _refuse("gate has to be [F, D]", ERR_SHAPE)
     if act not in ACTS:
         _refuse(f"act is one of {', '.join(ACTS)}, not {act!r}")
     F = gate.shape[0]
     head = (1 if step else shape[0], B, D, F, kind, ACTS[act], *_first(x, shape))
-    _need(up is not None, "up is needed")
     tail = (_dense(gate, dev, (F, D), x.dtype, "gate"), _dense(up, dev, (F, D), x.dtype, "up"), _dense(lengths, dev, (B,), torch.int32, "lengths"))
     return dev, F, lambda y: _UNITS.pack(*head, y, B * F, F, *tail)
 

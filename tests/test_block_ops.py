@@ -578,7 +578,9 @@ def test_shapes_and_types_that_do_not_fit_are_refused():
     x, d = torch.zeros(4, 2, 8, device="cuda"), torch.zeros(8, device="cuda")
     w = torch.zeros(6, 8, device="cuda")
     bad = [lambda: snn.gated_recurrence(x, x[:3], x, d), lambda: snn.gated_recurrence(x, x, x.bfloat16(), d), lambda: snn.gated_recurrence(x, x, x, d[:7]),
-           lambda: snn.gated_recurrence(x, x, x, None), lambda: snn.gated_recurrence(x, x, x, d, sharpness=0.0), lambda: snn.gated_recurrence(x[0], x[0], x[0], d),
+           lambda: snn.gated_recurrence(x, x, x, None), lambda: snn.gated_recurrence(x, x, x, d, sharpness=0.0), lambda: snn.gated_recurrence(x, x, x, d, sharpness=1e39),
+           lambda: snn.gated_recurrence(x, x, x, d, sharpness=float("nan")), lambda: snn.group_norm(x, 2.0), lambda: snn.group_norm(x, 2, eps=1e40), lambda: snn.gated_units(x, None, w),
+           lambda: snn.gated_recurrence(x[0], x[0], x[0], d),
            lambda: snn.gated_recurrence(x, x, x, d, init=torch.zeros(2, 7, device="cuda")), lambda: snn.gated_recurrence(x, x, x, d.cpu()),
            lambda: snn.gated_recurrence_backward(x, None, x, x, x, d), lambda: snn.gated_recurrence_step(x[0], x[0], x[0], None, d),
            lambda: snn.gated_recurrence_step(x[0], x[0], x[0], torch.zeros(2, 8, device="cuda").bfloat16(), d),
@@ -593,3 +595,93 @@ def test_shapes_and_types_that_do_not_fit_are_refused():
         with pytest.raises(snn.SnnError):
             f()
             print("call", k, "was taken")
+
+
+# ------------------------------------------------------------------------------------------------ differences
+
+def check_differences(f, inputs, grads, dys, seed):
+    """<gradient, v> against (L(x + e v) - L(x - e v)) / 2e with L = sum of <dy, output>, in fp32 on the GPU, sums in 64 bits; v standard normal.
+
+    e = 2^-9.  Rounding: outputs are off by a few 2^-24 of themselves, at random, which e divides: 2^-22 2^8 |dy y| = 2^-14 |dy y|.  Truncation: e^2 / 6 of
+    the third derivative along v, which is some ten times the first for functions of a few steps of order one: 2^-16 |gradient|.  Both
+    are below 2^-11 of their norms with room for the factors that were not counted."""
+    gen = torch.Generator().manual_seed(seed)
+    e = 2.0 ** -9
+    for name, g in grads.items():
+        v = torch.randn(inputs[name].shape, generator=gen).cuda()
+        total, size = [], 0.0
+        for sign in (1, -1):
+            # (both ends as fp32 holds them: the difference is theirs)
+            outs = f(**(inputs | {name: inputs[name] + sign * e * v}))
+            total.append(sum((dy.double() * o.double()).sum() for dy, o in zip(dys, outs)).item())
+            size = sum(((dy.double() * o.double()) ** 2).sum() for dy, o in zip(dys, outs)).sqrt().item()
+        step = ((inputs[name] + e * v).double() - (inputs[name] - e * v).double()) / (2 * e)
+        want = (g.double() * step).sum().item()
+        got = (total[0] - total[1]) / (2 * e)
+        assert abs(got - want) <= 2.0 ** -11 * (torch.linalg.norm(g.double()).item() + size) * 2, (name, got, want)
+
+
+@pytest.mark.parametrize("T", (5, 40))
+def test_gradients_are_the_differences(T):
+    import paper_2402_18994_amd as snn
+    B, D, F, groups = 2, 24, 20, 3
+    gen = torch.Generator().manual_seed(T)
+    r = lambda *s: torch.randn(*s, generator=gen).cuda()
+    n = torch.tensor([T, T - 2], dtype=torch.int32, device="cuda")
+    i = {"x": r(T, B, D), "i": r(T, B, D), "r": r(T, B, D), "decay": r(D) - 2, "init": r(B, D)}
+    dys = (r(T, B, D), r(B, D))
+    o = snn.gated_recurrence(**i, lengths=n, save=True)
+    g = snn.gated_recurrence_backward(dys[0], o.saved, **i, lengths=n, d_state=dys[1])
+    check_differences(lambda **k: snn.gated_recurrence(**k, lengths=n)[:2], i, dict(zip(("x", "i", "r", "decay", "init"), g)), dys, 1)
+    for per_step in (False, True):
+        i = {"x": r(T, B, D), "weight": 1 + 0.1 * r(D), "bias": 0.1 * r(D)}
+        kw = dict(groups=groups, per_step=per_step, lengths=n)
+        o = snn.group_norm(**i, save=True, **kw)
+        g = snn.group_norm_backward(dys[0], o.saved, **i, **kw)
+        check_differences(lambda **k: snn.group_norm(**k, **kw)[:1], i, dict(zip(("x", "weight", "bias"), g)), dys[:1], 2)
+    for act in ("silu", "gelu"):
+        i = {"x": r(T, B, D), "gate": r(F, D) / 5, "up": r(F, D) / 5}
+        dy = r(T, B, F)
+        o = snn.gated_units(**i, act=act, lengths=n, save=True)
+        g = snn.gated_units_backward(dy, o.saved, **i, act=act, lengths=n)
+        check_differences(lambda **k: snn.gated_units(**k, act=act, lengths=n)[:1], i, dict(zip(("x", "gate", "up"), g)), (dy,), 3)
+
+
+# ------------------------------------------------------------------------------------------------ far apart
+
+def test_sequences_that_lie_more_than_2_31_elements_apart():
+    """Offsets are 64 bits wide: the sequences of a batch lie 2^31 + 64 elements apart."""
+    import paper_2402_18994_amd as snn
+    T, B, D, F = 70, 2, 64, 40
+    far = (1 << 31) + 64
+    store = torch.empty(far + T * D * 8, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator().manual_seed(9)
+    fresh = lambda *s: torch.randn(*s, generator=gen).bfloat16().cuda()
+    at = [0]
+
+    def apart(v):
+        w = store.as_strided(v.shape, (v.shape[-1], far, 1), at[0])
+        at[0] += T * v.shape[-1]
+        w.copy_(v)
+        return w
+
+    x, i, r, dy = (fresh(T, B, D) for _ in range(4))
+    dyf = fresh(T, B, F)
+    fx, fi, fr, fdy, fdyf = map(apart, (x, i, r, dy, dyf))
+    decay, gate, up = torch.randn(D, generator=gen).cuda() - 3, fresh(F, D) / 8, fresh(F, D) / 8
+    a, b = snn.gated_recurrence(x, i, r, decay, save=True), snn.gated_recurrence(fx, fi, fr, decay, save=True)
+    assert same(a, b)
+    assert same(snn.gated_recurrence_backward(dy, a.saved, x, i, r, decay), snn.gated_recurrence_backward(fdy, a.saved, fx, fi, fr, decay))
+    for per_step in (False, True):
+        a, b = (snn.group_norm(v, 4, per_step=per_step, save=True) for v in (x, fx))
+        assert same(a, b)
+        assert same(snn.group_norm_backward(dy, a.saved, x, 4, per_step=per_step), snn.group_norm_backward(fdy, a.saved, fx, 4, per_step=per_step))
+    a, b = (snn.gated_units(v, gate, up, save=True) for v in (x, fx))
+    close("y", b.y, a.y.double().cpu(), D, 2 * half_step(torch.bfloat16))
+    assert same(snn.gated_units_backward(dyf, a.saved, x, gate, up), snn.gated_units_backward(fdyf, a.saved, fx, gate, up))
+    for v in (x, fx):
+        steps = snn.group_norm_step(v[3], 4), snn.gated_units_step(v[3], gate, up), snn.gated_recurrence_step(v[3], v[4], v[5], torch.zeros(B, D, device="cuda"), decay)
+        if v is x:
+            want = steps
+    close("step of units", steps[1], want[1].double().cpu(), D, 2 * half_step(torch.bfloat16))
+    assert torch.equal(steps[0], want[0]) and torch.equal(steps[2], want[2])
