@@ -227,9 +227,6 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const Jobs jobs) {
     for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[1][j], xa[1][i], acc[i][j], 0, 0, 0);
 
   // A lane holds, of block (i, j), row m = lane % 32 and columns 8 g + 4 h + 0..3 in element 4 g + 0..3.
-  const bool rows_out = WHAT == UNITS || a.what == DX, in_parts = WHAT == GRADS && a.splits > 1;
-  const bool wide_out = rows_out ? ((uintptr_t)a.out.p | (uintptr_t)(a.out.st * (int64_t)sizeof(T)) | (uintptr_t)(a.out.sb * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0
-                                 : ((uintptr_t)a.w0 | (uintptr_t)a.w1 | (uintptr_t)((int64_t)a.N * sizeof(T))) % (4 * sizeof(T)) == 0;
   if (WHAT == UNITS && a.part)
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -246,27 +243,72 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const Jobs jobs) {
             *(Pack<float, 4> *)(at + (w * 4 + g) * 256) = {{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]}};
           }
       }
-  if (WHAT == UNITS && a.splits > 1) return;                 // (units_sum_kernel goes on)
+  if constexpr (WHAT == UNITS) {
+    if (a.splits > 1) return;                                // (units_sum_kernel goes on)
+    constexpr int U = BN / 2, PITCH = U * (int)sizeof(T) + 16;
+    if constexpr (sizeof(T) == 2) {
+      // Through LDS, so that a row's outputs leave together.  (From the accumulators, which have four units of 32 rows, 4096 rows, 2048 -> 8192
+      // took 258 us against 246.  fp32 rows leave in 16-byte pieces as it is, and wide tiles of them do not fit.)
+      static_assert(BM * PITCH <= NS * STAGE, "the tile's outputs fit");
+      __syncthreads();
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int m = m0 + (wm * TM + i) * 32 + (lane & 31);
-    if (m >= a.M) continue;
-    if (WHAT == UNITS) {
-      int t, b;
-      const bool live = a.steps.live(m, t, b);
-      T *row = (T *)a.out.p + t * a.out.st + b * a.out.sb;
+      for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN / 2; ++j)
+        for (int j = 0; j < TN / 2; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int n = n0 + (wn * TN / 2 + j) * 32 + 8 * g + 4 * h;
-          if (n >= a.N) continue;
-          float y[4];
+          for (int g = 0; g < 4; ++g) {
+            Pack<T, 4> y;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) y[k] = live ? act_of(a.act, acc[i][2 * j][4 * g + k]) * acc[i][2 * j + 1][4 * g + k] : 0.f;
-          give4<T>(row, n, a.N, wide_out, y);
+            for (int k = 0; k < 4; ++k) y.v[k] = narrow<T>(act_of(a.act, acc[i][2 * j][4 * g + k]) * acc[i][2 * j + 1][4 * g + k]);
+            *(Pack<T, 4> *)(lds + ((wm * TM + i) * 32 + (lane & 31)) * PITCH + ((wn * TN / 2 + j) * 32 + 8 * g + 4 * h) * (int)sizeof(T)) = y;
+          }
+      __syncthreads();
+      const uintptr_t all = (uintptr_t)a.out.p | (uintptr_t)(a.out.st * (int64_t)sizeof(T)) | (uintptr_t)(a.out.sb * (int64_t)sizeof(T)) | (uintptr_t)((int64_t)a.N * sizeof(T));
+      auto pieces = [&](auto piece) {                        // rows in pieces of this type
+        typedef decltype(piece) Piece;
+        constexpr int E = (int)(sizeof(Piece) / sizeof(T));
+        for (int q = threadIdx.x; q < BM * (U / E); q += NW * 64) {
+          const int r = q / (U / E), c = q % (U / E) * E, m = m0 + r;
+          if (m >= a.M || n0 + c >= a.N) continue;
+          int t, b;
+          const bool live = a.steps.live(m, t, b);
+          const Piece v = *(const Piece *)(lds + r * PITCH + c * (int)sizeof(T));
+          *(Piece *)((T *)a.out.p + t * a.out.st + b * a.out.sb + n0 + c) = live ? v : Piece{};
         }
+      };
+      if (all % 16 == 0) pieces(u32x4{});
+      else if (all % 8 == 0) pieces(u32x2{});
+      else pieces((unsigned short)0);
     } else {
+      const bool wide = ((uintptr_t)a.out.p | (uintptr_t)(a.out.st * (int64_t)sizeof(T)) | (uintptr_t)(a.out.sb * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int m = m0 + (wm * TM + i) * 32 + (lane & 31);
+        if (m >= a.M) continue;
+        int t, b;
+        const bool live = a.steps.live(m, t, b);
+        T *row = (T *)a.out.p + t * a.out.st + b * a.out.sb;
+#pragma unroll
+        for (int j = 0; j < TN / 2; ++j)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int n = n0 + (wn * TN / 2 + j) * 32 + 8 * g + 4 * h;
+            if (n >= a.N) continue;
+            float y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = live ? act_of(a.act, acc[i][2 * j][4 * g + k]) * acc[i][2 * j + 1][4 * g + k] : 0.f;
+            give4<T>(row, n, a.N, wide, y);
+          }
+      }
+    }
+  } else {
+    const bool rows_out = a.what == DX, in_parts = a.splits > 1;
+    const bool wide = rows_out ? ((uintptr_t)a.out.p | (uintptr_t)(a.out.st * (int64_t)sizeof(T)) | (uintptr_t)(a.out.sb * (int64_t)sizeof(T))) % (4 * sizeof(T)) == 0
+                               : ((uintptr_t)a.w0 | (uintptr_t)a.w1 | (uintptr_t)((int64_t)a.N * sizeof(T))) % (4 * sizeof(T)) == 0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m = m0 + (wm * TM + i) * 32 + (lane & 31);
+      if (m >= a.M) continue;
       int t = 0, b = 0;
       const bool live = in_parts || !rows_out || a.steps.live(m, t, b);
       T *row = in_parts ? nullptr : rows_out ? (T *)a.out.p + t * a.out.st + b * a.out.sb : m < a.M / 2 ? (T *)a.w0 + (int64_t)m * a.N : (T *)a.w1 + (int64_t)(m - a.M / 2) * a.N;
@@ -280,7 +322,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(const Jobs jobs) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[k] = live ? acc[i][j][4 * g + k] : 0.f;
           if (in_parts) *(Pack<float, 4> *)(a.part + ((int64_t)split * a.M + m) * a.pitch + n) = {{v[0], v[1], v[2], v[3]}};
-          else give4<T>(row, n, a.N, wide_out, v);
+          else give4<T>(row, n, a.N, wide, v);
         }
     }
   }
