@@ -8,7 +8,7 @@
 // chunk's (mean, sum of squares around it), a second one joins them and reads the rows again, which the last-level cache still has up to
 // some 200 MB.  (One workgroup of 1024 threads that holds 64 values a thread needs no second reading, but fills and empties a compute
 // unit in turn: 1024 steps of 8 x 2048 channels, 32 groups, bf16: forward 24.7 us against 24.0, reverse 226, out of registers, against 43.)
-// Sums over rows (dw, db) leave a row per chunk that a last launch adds up.
+// Sums over rows (dw, db) leave a row per chunk or workgroup, which a last launch adds up, or workgroups of the second one.
 #include "rows.hpp"
 
 #include <algorithm>
@@ -33,6 +33,8 @@ struct NormP {
   // reverse
   Rows<void> dy, dx;
   float *dpart;                             // [units * blocks][2][D]
+  float *dweight, *dbias;
+  unsigned main;                            // workgroups of a launch that are not there for dweight and dbias
 };
 
 // Sum over aligned sets of 2^w lanes, in all of them.
@@ -551,8 +553,23 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
   if (threadIdx.x == 0) a.part[unit * a.blocks + w.chunk] = {s1, s2};
 }
 
+// The gradients of weight and bias out of the chunks' sums; `block`: which 16 of their 2 D columns.
+__device__ __forceinline__ void sum_parameters(const float *part, int rows, int D, float *dweight, float *dbias, int64_t block, float *lds) {
+  const int64_t col = block * 16 + (threadIdx.x & 15);
+  const float s = sum_column(part, 2 * (int64_t)D, col, rows, lds);
+  if (threadIdx.x >= 16) return;
+  if (col < D) {
+    if (dweight) dweight[col] = s;
+  } else if (col < 2 * (int64_t)D && dbias) dbias[col - D] = s;
+}
+// The workgroups behind the first `a.main` add up the parameters' gradients, which wait for nothing but the launch before.
 template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_gradient_kernel(const NormP a) {
-  __shared__ float lds[2][NT / 64];
+  static_assert(NT == 256, "as sum_column takes it");
+  __shared__ float lds[NT];
+  if (blockIdx.x >= a.main) {
+    sum_parameters(a.dpart, a.units * a.blocks, a.D, a.dweight, a.dbias, blockIdx.x - a.main, lds);
+    return;
+  }
   const Run<T, VEC> w(a, NT);
   const int64_t unit = (int64_t)w.unit * a.G + w.g;
   const float2 st = a.saved[unit];
@@ -568,8 +585,8 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
     s2 += p.y;
   }
   const float n = 1.f / fmaxf((float)((int64_t)w.len * a.C), 1.f);
-  s1 = block_sum<NT>(s1, lds[0]) * n;
-  s2 = block_sum<NT>(s2, lds[1]) * n;
+  s1 = block_sum<NT>(s1, lds) * n;
+  s2 = block_sum<NT>(s2, lds + NT / 64) * n;
   for (int k = 0; k < a.K; ++k) {
     const int c = (k << a.tpr_log2) * VEC + w.col;
     if (c >= a.C) break;
@@ -607,12 +624,7 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
 
 __global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__ part, int rows, int D, float *dweight, float *dbias) {
   __shared__ float lds[256];
-  const int64_t col = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
-  const float s = sum_column(part, 2 * (int64_t)D, col, rows, lds);
-  if (threadIdx.x >= 16) return;
-  if (col < D) {
-    if (dweight) dweight[col] = s;
-  } else if (col < 2 * (int64_t)D && dbias) dbias[col - D] = s;
+  sum_parameters(part, rows, D, dweight, dbias, blockIdx.x, lds);
 }
 
 // ---------------------------------------------------------------- host
@@ -717,7 +729,7 @@ template <typename F> int with_vector(const snn_norm_args &a, int vec, F f) {
 NormP norm_args(const snn_norm_args &a, const NormCut &c, void *saved, void *workspace) {
   return NormP{a.T, a.B, a.D, a.groups, a.D / a.groups, a.silu, a.eps, a.per_step ? (int64_t)a.T * a.B : a.T, a.per_step ? 1 : a.B, c.blocks, c.loops,
                c.tpr_log2, c.K, c.R, Rows<void>(a.x, a.T), Rows<void>(a.y, a.T), a.weight, a.bias, a.lengths, (float2 *)saved, (float2 *)workspace,
-               Rows<void>(snn_rows{}), Rows<void>(snn_rows{}), nullptr};
+               Rows<void>(snn_rows{}), Rows<void>(snn_rows{}), nullptr, nullptr, nullptr, 0};
 }
 int norm_grid(const snn_norm_args &a, const NormCut &c, dim3 &grid) {
   const int64_t n = (int64_t)a.groups * (a.per_step ? 1 : a.B) * c.blocks;
@@ -742,6 +754,7 @@ template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, co
     hipLaunchKernelGGL((norm_forward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
   return ops_launched("group norm");
 }
+unsigned parameter_blocks(int D) { return (unsigned)((2 * (int64_t)D + 15) / 16); }
 template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
   if (!per_step) {
     if (!c.chunks) {
@@ -753,7 +766,7 @@ template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per
       hipLaunchKernelGGL((norm_slopes_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
       const int e = ops_launched("group norm backward, sums");
       if (e) return e;
-      hipLaunchKernelGGL((norm_gradient_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
+      hipLaunchKernelGGL((norm_gradient_kernel<T, V, 256>), dim3(grid.x + (p.dweight || p.dbias ? parameter_blocks(p.D) : 0)), dim3(256), 0, st, p);
     }
   } else if (c.K == 1) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, STEP, true>), grid, dim3(256), 0, st, p);
   else if (c.nt == 256) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, STEP, false>), grid, dim3(256), 0, st, p);
@@ -820,10 +833,13 @@ int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const
   p.dy = Rows<void>(g->dy, a->T);
   p.dx = Rows<void>(g->dx, a->T);
   p.dpart = (float *)((char *)workspace + part_bytes(*a, c));
+  p.dweight = g->dweight;
+  p.dbias = g->dbias;
+  p.main = grid.x;
   const hipStream_t st = (hipStream_t)stream;
   if (a->T > 0 && (rc = with_vector(*a, vec, [&](auto t, auto v) { return launch_norm_backward<decltype(t), v.value>(c, a->per_step, p, grid, st); }))) return rc;
-  if (!g->dweight && !g->dbias) return SNN_OK;
-  hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((2 * (int64_t)a->D + 15) / 16)), dim3(256), 0, st, p.dpart, a->T > 0 ? p.units * c.blocks : 0, a->D, g->dweight,
+  if ((!g->dweight && !g->dbias) || (a->T > 0 && c.chunks)) return SNN_OK;
+  hipLaunchKernelGGL(norm_sum_kernel, dim3(parameter_blocks(a->D)), dim3(256), 0, st, p.dpart, a->T > 0 ? p.units * c.blocks : 0, a->D, g->dweight,
                      g->dbias);
   return ops_launched("group norm backward, gradients of the parameters");
 }
