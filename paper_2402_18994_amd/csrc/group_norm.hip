@@ -139,11 +139,22 @@ template <typename P, int N> __device__ __forceinline__ void keep_packed(P (&v)[
   }
 }
 
+// A vector's weights and biases, as one load each (which need no more than an element's alignment).
 template <int VEC> __device__ __forceinline__ void params(const NormP &a, int d, float (&w)[VEC], float (&b)[VEC]) {
+  struct alignas(4) Values {
+    float v[VEC];
+  } x;
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) {
-    w[v] = a.weight ? a.weight[d + v] : 1.f;
-    b[v] = a.bias ? a.bias[d + v] : 0.f;
+  for (int v = 0; v < VEC; ++v) w[v] = 1.f, b[v] = 0.f;
+  if (a.weight) {
+    __builtin_memcpy(&x, a.weight + d, sizeof x);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) w[v] = x.v[v];
+  }
+  if (a.bias) {
+    __builtin_memcpy(&x, a.bias + d, sizeof x);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) b[v] = x.v[v];
   }
 }
 
@@ -160,7 +171,7 @@ __device__ __forceinline__ Where<T, VEC, K1> where(const NormP &a, bool step, in
   w.len = step ? 0 : __builtin_amdgcn_readfirstlane(length_of(a.lengths, w.unit, a.T));
   return w;
 }
-// For each of a thread's rows (K1), or for its one row: the sum over the row.  `lds` takes SLOTS * NT / 64 floats.
+// For each of a thread's rows (K1: of a wavefront's lanes at most), or for its one row: the sum over the row.  `lds` takes NT / 64 floats.
 template <int NT, int SLOTS, bool K1>
 __device__ __forceinline__ void row_sums(const NormP &a, float (&v)[SLOTS], float *lds) {
   if (!K1) {
@@ -171,20 +182,8 @@ __device__ __forceinline__ void row_sums(const NormP &a, float (&v)[SLOTS], floa
     for (int s = 1; s < SLOTS; ++s) v[s] = v[0];
     return;
   }
-  const int width = min(6, a.tpr_log2);
 #pragma unroll
-  for (int s = 0; s < SLOTS; ++s) v[s] = wave_sum(v[s], width);
-  if (a.tpr_log2 <= 6) return;
-  const int wave = threadIdx.x >> 6, each = 1 << (a.tpr_log2 - 6), first = wave & -each;
-  if ((threadIdx.x & 63) == 0)
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) lds[s * (NT / 64) + wave] = v[s];
-  __syncthreads();
-#pragma unroll
-  for (int s = 0; s < SLOTS; ++s) {
-    v[s] = 0.f;
-    for (int w = 0; w < each; ++w) v[s] += lds[s * (NT / 64) + first + w];
-  }
+  for (int s = 0; s < SLOTS; ++s) v[s] = wave_sum(v[s], a.tpr_log2);
 }
 
 __device__ __forceinline__ float output_of(float x, float mean, float rstd, float w, float b, int silu) {
@@ -208,7 +207,7 @@ template <int NT, int SLOTS, int MODE, bool K1> __device__ __forceinline__ void 
 template <typename T, int VEC, int NT, int MODE, bool K1>
 __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
   constexpr int SLOTS = Slots<T, VEC, MODE, K1>::N;
-  __shared__ float lds[2][SLOTS * (NT / 64)];
+  __shared__ float lds[2][NT / 64];
   auto w = where<T, VEC, K1>(a, MODE == STEP, NT);
   float wt[VEC], bs[VEC];
   if (K1) params<VEC>(a, w.channel(0) < a.C ? w.g * a.C + w.channel(0) : 0, wt, bs);
@@ -283,7 +282,7 @@ template <int VEC, int NT> __device__ __forceinline__ void column_sums(const Nor
 template <typename T, int VEC, int NT, int MODE, bool K1>
 __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
   constexpr int SLOTS = Slots<T, VEC, MODE, K1>::N;
-  __shared__ float lds[2][SLOTS * (NT / 64)];
+  __shared__ float lds[2][NT / 64];
   __shared__ float cols[K1 ? NT * VEC : 1];
   auto w = where<T, VEC, K1>(a, MODE == STEP, NT);
   const int chunk = (int)(blockIdx.x / ((unsigned)a.G * (unsigned)a.units));
@@ -360,6 +359,187 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
     for (int v = 0; v < VEC; ++v) {
       out[w.col * VEC + v] = dw[v];
       out[a.D + w.col * VEC + v] = db[v];
+    }
+}
+
+// The choice of `silu`, once for a kernel in place of once a value.
+template <typename F> __device__ __forceinline__ void with_silu(int silu, F f) {
+  if (silu) f(std::integral_constant<int, 1>());
+  else f(std::integral_constant<int, 0>());
+}
+
+// ---------------------------------------------------------------- long rows by themselves
+// Rows of more vectors than a wavefront has lanes: a wavefront each, KB vectors a lane, no barrier.  (A workgroup for a row waits at two
+// or three barriers for every row or two: 1024 x 8 rows of 2047 channels, bf16, 81 us forward and 450 reverse, against 34 and 101; rows of 4096, 73 and 366 against 19 and 62.)
+template <typename T, int VEC, int KB> struct LongRow {
+  int g, t, b;
+  int64_t m;
+  bool there, live;
+  __device__ __forceinline__ explicit LongRow(const NormP &a) {
+    const unsigned id = blockIdx.x * 4u + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = id / (unsigned)a.G;
+    g = (int)(id - row * a.G);
+    m = row;
+    there = m < a.rows;
+    t = (int)(row / (unsigned)a.B);
+    b = (int)(row - (unsigned)t * a.B);
+    live = there && t < length_of(a.lengths, b, a.T);
+  }
+  static __device__ __forceinline__ int channel(int s) { return (s * 64 + (int)(threadIdx.x & 63)) * VEC; }
+  // Every second or fourth vector: does the row end before it?
+  static __device__ __forceinline__ bool ends(const NormP &a, int s) { return s && s % (KB == 4 ? 2 : 4) == 0 && s * 64 * VEC >= a.C; }
+  template <typename R> __device__ __forceinline__ T *at(const NormP &a, const R &r) const { return (T *)r.p + b * r.sb + t * r.st + (int64_t)g * a.C; }
+  template <typename R> __device__ __forceinline__ void load(const NormP &a, const R &r, Pack<T, VEC> (&v)[KB]) const {
+    const T *row = at(a, r);
+#pragma unroll
+    for (int s = 0; s < KB; ++s) {
+      if (ends(a, s)) break;
+      v[s] = *(const Pack<T, VEC> *)(row + (channel(s) < a.C ? channel(s) : 0));   // (not used behind the row)
+    }
+  }
+  template <typename R> __device__ __forceinline__ void zeros(const NormP &a, const R &r) const {
+    const Pack<T, VEC> zero = {};
+    for (int s = 0; s < KB; ++s)
+      if (channel(s) < a.C) *(Pack<T, VEC> *)(at(a, r) + channel(s)) = zero;
+  }
+};
+template <typename T, int VEC, int KB> __global__ __launch_bounds__(256) void norm_rows_kernel(const NormP a) {
+  const LongRow<T, VEC, KB> w(a);
+  if (!w.there) return;
+  if (!w.live) {
+    w.zeros(a, a.y);
+    return;
+  }
+  Pack<T, VEC> x[KB];
+  w.load(a, a.x, x);
+  const float n = 1.f / (float)a.C;
+  float mean = 0.f, q = 0.f;
+#pragma unroll
+  for (int s = 0; s < KB; ++s) {
+    if (w.ends(a, s)) break;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) mean += w.channel(s) < a.C ? widen(x[s].v[v]) : 0.f;
+  }
+  mean = wave_sum(mean, 6) * n;
+#pragma unroll
+  for (int s = 0; s < KB; ++s) {
+    if (w.ends(a, s)) break;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const float e = w.channel(s) < a.C ? widen(x[s].v[v]) - mean : 0.f;
+      q = fmaf(e, e, q);
+    }
+  }
+  const float rstd = __builtin_amdgcn_rsqf(fmaf(wave_sum(q, 6), n, a.eps));
+  if (a.saved && (threadIdx.x & 63) == 0) a.saved[w.m * a.G + w.g] = {mean, rstd};
+  T *y = w.at(a, a.y);
+  with_silu(a.silu, [&](auto silu) {
+#pragma unroll
+    for (int s = 0; s < KB; ++s) {
+      if (w.ends(a, s)) break;
+      const int c = w.channel(s);
+      float wt[VEC], bs[VEC];
+      params<VEC>(a, w.g * a.C + (c < a.C ? c : 0), wt, bs);
+      Pack<T, VEC> out;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) out.v[v] = narrow<T>(output_of(widen(x[s].v[v]), mean, rstd, wt[v], bs[v], silu.value));
+      if (c < a.C) *(Pack<T, VEC> *)(y + c) = out;
+      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  });
+}
+template <typename T, int VEC, int KB> __global__ __launch_bounds__(256) void norm_rows_backward_kernel(const NormP a) {
+  const LongRow<T, VEC, KB> w(a);
+  if (!w.there) return;
+  if (!w.live) {
+    w.zeros(a, a.dx);
+    return;
+  }
+  Pack<T, VEC> x[KB], dy[KB];
+  w.load(a, a.x, x);
+  w.load(a, a.dy, dy);
+  const float2 st = a.saved[w.m * a.G + w.g];
+  const float n = 1.f / (float)a.C;
+  T *dx = w.at(a, a.dx);
+  with_silu(a.silu, [&](auto silu) {
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int s = 0; s < KB; ++s) {
+      if (w.ends(a, s)) break;
+      const int c = w.channel(s);
+      float wt[VEC], bs[VEC];
+      params<VEC>(a, w.g * a.C + (c < a.C ? c : 0), wt, bs);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float xh = (widen(x[s].v[v]) - st.x) * st.y;
+        float p;
+        gradient_of(widen(dy[s].v[v]), xh, wt[v], bs[v], silu.value, p);
+        p = c < a.C ? p : 0.f;                   // (behind the row x is its first value, and p xh a zero or one of the row's NaN)
+        s1 += p;
+        s2 = fmaf(p, xh, s2);
+      }
+      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+    s1 = wave_sum(s1, 6) * n;
+    s2 = wave_sum(s2, 6) * n;
+    keep_packed(x);
+    keep_packed(dy);
+    int first = w.g * a.C;                       // (the weights are loaded again: kept, they would be most of the registers)
+    asm volatile("" : "+s"(first));
+#pragma unroll
+    for (int s = 0; s < KB; ++s) {
+      if (w.ends(a, s)) break;
+      const int c = w.channel(s);
+      float wt[VEC], bs[VEC];
+      params<VEC>(a, first + (c < a.C ? c : 0), wt, bs);
+      Pack<T, VEC> d;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float xh = (widen(x[s].v[v]) - st.x) * st.y;
+        float p;
+        gradient_of(widen(dy[s].v[v]), xh, wt[v], bs[v], silu.value, p);
+        d.v[v] = narrow<T>(st.y * (p - s1 - xh * s2));
+      }
+      if (c < a.C) *(Pack<T, VEC> *)(dx + c) = d;
+      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  });
+}
+// Their dw and db: a lane has VEC columns, a wavefront every fourth row of the chunk blockIdx.y.
+template <typename T, int VEC> __global__ __launch_bounds__(256) void norm_columns_kernel(const NormP a) {
+  __shared__ float lds[4][2 * VEC][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (blockIdx.x * 64 + lane) * VEC;
+  const bool on = c < a.D;
+  const int cc = on ? c : 0, g = cc / a.C;
+  const int64_t first = (int64_t)blockIdx.y * a.R, end = min(a.rows, first + a.R);
+  float wt[VEC], bs[VEC], sums[2 * VEC];
+  params<VEC>(a, cc, wt, bs);
+#pragma unroll
+  for (int v = 0; v < 2 * VEC; ++v) sums[v] = 0.f;
+  with_silu(a.silu, [&](auto silu) {
+#pragma unroll 4
+    for (int64_t m = first + wave; m < end; m += 4) {
+      const int t = (int)((unsigned)m / (unsigned)a.B), b = (int)((unsigned)m - (unsigned)t * a.B);
+      if (t >= length_of(a.lengths, b, a.T)) continue;       // (for the whole wavefront)
+      const Pack<T, VEC> x = *(const Pack<T, VEC> *)((const T *)a.x.p + b * a.x.sb + t * a.x.st + cc), dy = *(const Pack<T, VEC> *)((const T *)a.dy.p + b * a.dy.sb + t * a.dy.st + cc);
+      const float2 st = a.saved[m * a.G + g];
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float xh = (widen(x.v[v]) - st.x) * st.y;
+        float p;
+        const float q = gradient_of(widen(dy.v[v]), xh, wt[v], bs[v], silu.value, p);
+        sums[v] = fmaf(q, xh, sums[v]);
+        sums[VEC + v] += q;
+      }
+    }
+  });
+#pragma unroll
+  for (int v = 0; v < 2 * VEC; ++v) lds[wave][v][lane] = sums[v];
+  __syncthreads();
+  if (wave == 0 && on)
+#pragma unroll
+    for (int v = 0; v < 2 * VEC; ++v) {
+      const float s = ((lds[0][v][lane] + lds[1][v][lane]) + lds[2][v][lane]) + lds[3][v][lane];
+      a.dpart[((int64_t)blockIdx.y * 2 + v / VEC) * a.D + c + v % VEC] = s;
     }
 }
 
@@ -655,6 +835,7 @@ int norm_check(const snn_norm_args *a, bool grads) {
 struct NormCut {
   int nt, tpr_log2, K, R, loops, blocks;       // threads; threads a row (log2); column blocks; rows a thread; lots; workgroups a unit and group
   bool chunks;
+  int long_row;                                // vectors a lane where a wavefront has a row, 0: otherwise
 };
 NormCut norm_cut(const snn_norm_args &a, int vec, bool backward) {
   const size_t z = a.type == SNN_TYPE_FP32 ? 4 : 2;
@@ -671,11 +852,24 @@ NormCut norm_cut(const snn_norm_args &a, int vec, bool backward) {
   fit(256);
   c.loops = 1;
   c.chunks = false;
+  c.long_row = 0;
+  if (a.per_step && C > 64 * vec) {
+    const int need = (C + 64 * vec - 1) / (64 * vec);
+    const int most = vec <= 2 ? 64 / vec : 16;
+    c.long_row = need <= 4 ? 4 : need <= 16 ? 16 : need <= most ? most : 0;
+    if (c.long_row) {                          // R: rows of a chunk of dw and db, in workgroups of 64 vectors of columns
+      const int64_t across = (a.D + 64 * vec - 1) / (64 * vec);
+      c.R = 256;
+      while (c.R > 16 && blocks_of(c.R) * across < 1024) c.R /= 2;
+      c.blocks = (int)blocks_of(c.R);
+      return c;
+    }
+    fit(1024);
+  }
   if (a.per_step) {
-    if (c.K > slots) fit(1024);                // (16384 channels one by one)
     const int64_t rp = c.nt >> c.tpr_log2;
     c.R = c.K == 1 && blocks_of(rp * 2) * a.groups >= 512 ? 2 : 1;
-    int64_t n = blocks_of(rp * c.R);
+    const int64_t n = blocks_of(rp * c.R);
     while (c.loops < 64 && blocks_of(rp * c.R * c.loops * 2) * a.groups >= 2048) c.loops *= 2;
     c.blocks = (int)((n + c.loops - 1) / c.loops);
     return c;
@@ -732,12 +926,24 @@ NormP norm_args(const snn_norm_args &a, const NormCut &c, void *saved, void *wor
                Rows<void>(snn_rows{}), Rows<void>(snn_rows{}), nullptr, nullptr, nullptr, 0};
 }
 int norm_grid(const snn_norm_args &a, const NormCut &c, dim3 &grid) {
+  if (c.long_row) {                            // a wavefront a row and group
+    const int64_t n = ((int64_t)a.T * a.B * a.groups + 3) / 4;
+    if (n * 256 >= (1ll << 32) || c.blocks > 65535) return ops_fail(SNN_ERR_ARG, "group norm: too large for one launch");
+    grid = dim3((unsigned)n);
+    return SNN_OK;
+  }
   const int64_t n = (int64_t)a.groups * (a.per_step ? 1 : a.B) * c.blocks;
   if (n * c.nt >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "group norm: too large for one launch");
   grid = dim3((unsigned)n);
   return SNN_OK;
 }
 
+template <typename T, int V, typename F> void with_long_row(int kb, F f) {
+  if constexpr (V <= 2)
+    if (kb == 64 / V) return f(std::integral_constant<int, 64 / V>());
+  if (kb == 16) f(std::integral_constant<int, 16>());
+  else f(std::integral_constant<int, 4>());
+}
 template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
   if (!per_step) {
     if (!c.chunks && c.nt == 512) hipLaunchKernelGGL((norm_forward_kernel<T, V, 512, WHOLE, true>), grid, dim3(512), 0, st, p);
@@ -748,10 +954,10 @@ template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, co
       if (e) return e;
       hipLaunchKernelGGL((norm_output_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
     }
-  } else if (c.K == 1) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, STEP, true>), grid, dim3(256), 0, st, p);
-  else if (c.nt == 256) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, STEP, false>), grid, dim3(256), 0, st, p);
-  else if constexpr (256 * V * Slots<T, V, STEP, false>::N < MOST_CHANNELS)
-    hipLaunchKernelGGL((norm_forward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
+  } else if (c.long_row)
+    with_long_row<T, V>(c.long_row, [&](auto kb) { hipLaunchKernelGGL((norm_rows_kernel<T, V, kb.value>), grid, dim3(256), 0, st, p); });
+  else if (c.K == 1) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, STEP, true>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((norm_forward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
   return ops_launched("group norm");
 }
 unsigned parameter_blocks(int D) { return (unsigned)((2 * (int64_t)D + 15) / 16); }
@@ -768,10 +974,14 @@ template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per
       if (e) return e;
       hipLaunchKernelGGL((norm_gradient_kernel<T, V, 256>), dim3(grid.x + (p.dweight || p.dbias ? parameter_blocks(p.D) : 0)), dim3(256), 0, st, p);
     }
+  } else if (c.long_row) {
+    with_long_row<T, V>(c.long_row, [&](auto kb) { hipLaunchKernelGGL((norm_rows_backward_kernel<T, V, kb.value>), grid, dim3(256), 0, st, p); });
+    if (!p.dweight && !p.dbias) return ops_launched("group norm backward");
+    const int e = ops_launched("group norm backward, rows");
+    if (e) return e;
+    hipLaunchKernelGGL((norm_columns_kernel<T, V>), dim3((p.D + 64 * V - 1) / (64 * V), c.blocks), dim3(256), 0, st, p);
   } else if (c.K == 1) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, STEP, true>), grid, dim3(256), 0, st, p);
-  else if (c.nt == 256) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, STEP, false>), grid, dim3(256), 0, st, p);
-  else if constexpr (256 * V * Slots<T, V, STEP, false>::N < MOST_CHANNELS)
-    hipLaunchKernelGGL((norm_backward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
+  else hipLaunchKernelGGL((norm_backward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
   return ops_launched("group norm backward");
 }
 

@@ -209,6 +209,17 @@ NORM = [  # T, B, D, groups, type, silu, per_step, lengths, weight, bias
     (300, 66, 128, 2, "bf16", True, False, "some", True, True),          # one chunk of a wide workgroup
     (700, 40, 32, 8, "bf16", True, True, "some", True, True),            # a workgroup takes several chunks
     (0, 2, 8, 2, "fp32", True, False, "none", True, True),
+    (30, 3, 4000, 2, "bf16", True, True, "some", True, True),            # rows that a wavefront takes, each count of vectors and alignment
+    (21, 3, 8192, 1, "bf16", False, True, "some", False, True),
+    (21, 3, 2050, 1, "bf16", True, True, "some", True, False),
+    (40, 2, 1030, 1, "bf16", True, True, "zero", True, True),
+    (21, 3, 4095, 1, "bf16", True, True, "some", True, True),
+    (33, 3, 516, 2, "fp32", True, True, "some", True, True),
+    (21, 3, 4096, 1, "fp32", False, True, "some", True, True),
+    (21, 3, 4094, 1, "fp32", True, True, "some", True, True),
+    (1, 5, 2047, 1, "fp32", True, True, "none", True, True),
+    (900, 9, 1040, 8, "fp32", True, True, "some", True, True),           # dw and db of several chunks of rows
+    (600, 9, 1044, 4, "bf16", True, True, "some", True, True),
 ]
 
 
