@@ -68,10 +68,10 @@ template <int NT> __device__ __forceinline__ float block_sum(float v, float *lds
   return s;
 }
 
-// Vectors that a thread holds at a time.  Rows that stand alone are taken two at a time (K1: a row is one vector a thread): more of them
-// cost registers and with them wavefronts.
-template <typename T, int VEC, int MODE, bool K1> struct Slots {
-  static constexpr int N = MODE == STEP && K1 ? 2 : sizeof(T) * VEC == 16 ? 8 : 16;
+// Vectors that a thread holds at a time, each of another row.  Rows that stand alone are taken two at a time: more of them cost registers
+// and with them wavefronts.
+template <typename T, int VEC, int MODE> struct Slots {
+  static constexpr int N = MODE == STEP ? 2 : sizeof(T) * VEC == 16 ? 8 : 16;
 };
 
 __device__ __forceinline__ float silu_slope(float v) {
@@ -89,15 +89,14 @@ __device__ __forceinline__ float gradient_of(float dy, float xh, float w, float 
 }
 
 // Where the vectors of a thread lie.
-template <typename T, int VEC, bool K1> struct Where {
+template <typename T, int VEC> struct Where {
   const NormP &a;
   int unit, g, len, rsub, col, rp;
   int64_t r0;
   bool step;
-  __device__ __forceinline__ int k(int s) const { return K1 ? 0 : s / a.R; }
-  __device__ __forceinline__ int channel(int s) const { return (k(s) << a.tpr_log2) * VEC + col * VEC; }      // within the group
-  __device__ __forceinline__ int64_t row(int s) const { return r0 + (int64_t)(K1 ? s : s % a.R) * rp + rsub; }
-  __device__ __forceinline__ bool there(int s) const { return row(s) < a.rows && channel(s) < a.C && (K1 ? s < a.R : s < a.K * a.R); }
+  __device__ __forceinline__ int channel() const { return col * VEC; }                                        // within the group
+  __device__ __forceinline__ int64_t row(int s) const { return r0 + (int64_t)s * rp + rsub; }
+  __device__ __forceinline__ bool there(int s) const { return row(s) < a.rows && channel() < a.C && s < a.R; }
   __device__ __forceinline__ void place(int64_t m, int &t, int &b) const {
     t = step ? (int)((uint32_t)m / (uint32_t)a.B) : (int)m;
     b = step ? (int)((uint32_t)m - (uint32_t)t * (uint32_t)a.B) : unit;
@@ -112,7 +111,7 @@ template <typename T, int VEC, bool K1> struct Where {
   template <typename R> __device__ __forceinline__ T *at(const R &r, int s) const {
     int t, b;
     place(row(s), t, b);
-    return (T *)r.p + b * r.sb + t * r.st + (int64_t)g * a.C + channel(s);
+    return (T *)r.p + b * r.sb + t * r.st + (int64_t)g * a.C + channel();
   }
 };
 
@@ -158,10 +157,10 @@ template <int VEC> __device__ __forceinline__ void params(const NormP &a, int d,
   }
 }
 
-template <typename T, int VEC, bool K1>
-__device__ __forceinline__ Where<T, VEC, K1> where(const NormP &a, bool step, int nt) {
+template <typename T, int VEC>
+__device__ __forceinline__ Where<T, VEC> where(const NormP &a, bool step, int nt) {
   const unsigned rest = blockIdx.x / (unsigned)a.G, turn = rest / (unsigned)a.units;
-  Where<T, VEC, K1> w{a, 0, 0, 0, 0, 0, 0, 0, step};
+  Where<T, VEC> w{a, 0, 0, 0, 0, 0, 0, 0, step};
   w.g = (int)(blockIdx.x - rest * a.G);
   w.unit = (int)(rest - turn * a.units);
   w.rsub = (int)threadIdx.x >> a.tpr_log2;
@@ -171,30 +170,16 @@ __device__ __forceinline__ Where<T, VEC, K1> where(const NormP &a, bool step, in
   w.len = step ? 0 : __builtin_amdgcn_readfirstlane(length_of(a.lengths, w.unit, a.T));
   return w;
 }
-// For each of a thread's rows (K1: of a wavefront's lanes at most), or for its one row: the sum over the row.  `lds` takes NT / 64 floats.
-template <int NT, int SLOTS, bool K1>
-__device__ __forceinline__ void row_sums(const NormP &a, float (&v)[SLOTS], float *lds) {
-  if (!K1) {
-#pragma unroll
-    for (int s = 1; s < SLOTS; ++s) v[0] += v[s];
-    v[0] = block_sum<NT>(v[0], lds);
-#pragma unroll
-    for (int s = 1; s < SLOTS; ++s) v[s] = v[0];
-    return;
-  }
-#pragma unroll
-  for (int s = 0; s < SLOTS; ++s) v[s] = wave_sum(v[s], a.tpr_log2);
-}
-
 __device__ __forceinline__ float output_of(float x, float mean, float rstd, float w, float b, int silu) {
   const float v = fmaf((x - mean) * rstd, w, b);
   return silu ? v * sigmoid_fast(v) : v;
 }
 
-// Sums over each row, or over all rows (in every slot).
-template <int NT, int SLOTS, int MODE, bool K1> __device__ __forceinline__ void sums_of(const NormP &a, float (&v)[SLOTS], float *lds) {
+// Sums over each row (of a wavefront's lanes at most), or over all rows (in every slot).  `lds` takes NT / 64 floats.
+template <int NT, int SLOTS, int MODE> __device__ __forceinline__ void sums_of(const NormP &a, float (&v)[SLOTS], float *lds) {
   if (MODE == STEP) {
-    row_sums<NT, SLOTS, K1>(a, v, lds);
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) v[s] = wave_sum(v[s], a.tpr_log2);
     return;
   }
 #pragma unroll
@@ -204,13 +189,13 @@ template <int NT, int SLOTS, int MODE, bool K1> __device__ __forceinline__ void 
   for (int s = 1; s < SLOTS; ++s) v[s] = v[0];
 }
 
-template <typename T, int VEC, int NT, int MODE, bool K1>
+template <typename T, int VEC, int NT, int MODE>
 __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
-  constexpr int SLOTS = Slots<T, VEC, MODE, K1>::N;
+  constexpr int SLOTS = Slots<T, VEC, MODE>::N;
   __shared__ float lds[2][NT / 64];
-  auto w = where<T, VEC, K1>(a, MODE == STEP, NT);
+  auto w = where<T, VEC>(a, MODE == STEP, NT);
   float wt[VEC], bs[VEC];
-  if (K1) params<VEC>(a, w.channel(0) < a.C ? w.g * a.C + w.channel(0) : 0, wt, bs);
+  params<VEC>(a, w.channel() < a.C ? w.g * a.C + w.channel() : 0, wt, bs);
   for (int loop = 0; loop < a.loops; ++loop, w.r0 += (int64_t)w.rp * a.R) {
     Pack<T, VEC> x[SLOTS];
     bool live[SLOTS];
@@ -221,14 +206,13 @@ __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
     }
     float mean[SLOTS], rstd[SLOTS];                          // (WHOLE: the same in all)
     const float n = MODE == STEP ? 1.f / (float)a.C : 1.f / fmaxf((float)((int64_t)w.len * a.C), 1.f);
-    if (MODE == STEP && loop) __syncthreads();               // (the sums of the loop before have been read)
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       mean[s] = 0.f;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) mean[s] += widen(x[s].v[v]);
     }
-    sums_of<NT, SLOTS, MODE, K1>(a, mean, lds[0]);
+    sums_of<NT, SLOTS, MODE>(a, mean, lds[0]);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       mean[s] *= n;
@@ -239,17 +223,16 @@ __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
         rstd[s] = fmaf(e, e, rstd[s]);
       }
     }
-    sums_of<NT, SLOTS, MODE, K1>(a, rstd, lds[1]);
+    sums_of<NT, SLOTS, MODE>(a, rstd, lds[1]);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       rstd[s] = __builtin_amdgcn_rsqf(fmaf(rstd[s], n, a.eps));
-      if (MODE == STEP && a.saved && w.col == 0 && (K1 || s == 0) && w.there(s)) a.saved[w.row(s) * a.G + w.g] = {mean[s], rstd[s]};
+      if (MODE == STEP && a.saved && w.col == 0 && w.there(s)) a.saved[w.row(s) * a.G + w.g] = {mean[s], rstd[s]};
     }
     if (MODE == WHOLE && a.saved && threadIdx.x == 0) a.saved[(int64_t)w.unit * a.G + w.g] = {mean[0], rstd[0]};
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       if (!w.there(s)) continue;
-      if (!K1) params<VEC>(a, w.g * a.C + w.channel(s), wt, bs);
       Pack<T, VEC> y;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) y.v[v] = narrow<T>(live[s] ? output_of(widen(x[s].v[v]), mean[s], rstd[s], wt[v], bs[v], a.silu) : 0.f);
@@ -279,15 +262,15 @@ template <int VEC, int NT> __device__ __forceinline__ void column_sums(const Nor
     }
 }
 
-template <typename T, int VEC, int NT, int MODE, bool K1>
+template <typename T, int VEC, int NT, int MODE>
 __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
-  constexpr int SLOTS = Slots<T, VEC, MODE, K1>::N;
+  constexpr int SLOTS = Slots<T, VEC, MODE>::N;
   __shared__ float lds[2][NT / 64];
-  __shared__ float cols[K1 ? NT * VEC : 1];
-  auto w = where<T, VEC, K1>(a, MODE == STEP, NT);
+  __shared__ float cols[NT * VEC];
+  auto w = where<T, VEC>(a, MODE == STEP, NT);
   const int chunk = (int)(blockIdx.x / ((unsigned)a.G * (unsigned)a.units));
   float wt[VEC], bs[VEC], dw[VEC], db[VEC];
-  if (K1) params<VEC>(a, w.channel(0) < a.C ? w.g * a.C + w.channel(0) : 0, wt, bs);
+  params<VEC>(a, w.channel() < a.C ? w.g * a.C + w.channel() : 0, wt, bs);
 #pragma unroll
   for (int v = 0; v < VEC; ++v) dw[v] = db[v] = 0.f;
   float *const out = a.dpart + ((int64_t)w.unit * a.blocks + chunk) * 2 * a.D + (int64_t)w.g * a.C;
@@ -305,11 +288,9 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
       mean[s] = m.x;
       rstd[s] = m.y;
     }
-    if (MODE == STEP && loop) __syncthreads();               // (the sums of the loop before have been read)
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       s1[s] = s2[s] = 0.f;
-      if (!K1) params<VEC>(a, w.there(s) ? w.g * a.C + w.channel(s) : 0, wt, bs);
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         const float xh = live[s] ? (widen(x[s].v[v]) - mean[s]) * rstd[s] : 0.f;
@@ -320,26 +301,14 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
         dw[v] = fmaf(q, xh, dw[v]);
         db[v] += q;
       }
-      if (!K1) {                                             // (a thread has these columns to itself)
-        if (w.channel(s) < a.C && s < a.K)
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) {
-            float *const o = out + w.channel(s) + v;
-            o[0] = loop ? o[0] + dw[v] : dw[v];
-            o[a.D] = loop ? o[a.D] + db[v] : db[v];
-          }
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) dw[v] = db[v] = 0.f;
-      }
     }
     keep_packed(x);
     keep_packed(dy);
-    sums_of<NT, SLOTS, MODE, K1>(a, s1, lds[0]);
-    sums_of<NT, SLOTS, MODE, K1>(a, s2, lds[1]);
+    sums_of<NT, SLOTS, MODE>(a, s1, lds[0]);
+    sums_of<NT, SLOTS, MODE>(a, s2, lds[1]);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       if (!w.there(s)) continue;
-      if (!K1) params<VEC>(a, w.g * a.C + w.channel(s), wt, bs);
       Pack<T, VEC> d;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
@@ -351,7 +320,6 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
       *(Pack<T, VEC> *)w.at(a.dx, s) = d;
     }
   }
-  if (!K1) return;
   column_sums<VEC, NT>(a, dw, cols);
   column_sums<VEC, NT>(a, db, cols);
   if ((int)threadIdx.x < (1 << a.tpr_log2) && w.col * VEC < a.C)
@@ -369,14 +337,17 @@ template <typename F> __device__ __forceinline__ void with_silu(int silu, F f) {
 }
 
 // ---------------------------------------------------------------- long rows by themselves
-// Rows of more vectors than a wavefront has lanes: a wavefront each, KB vectors a lane, no barrier.  (A workgroup for a row waits at two
-// or three barriers for every row or two: 1024 x 8 rows of 2047 channels, bf16, 81 us forward and 450 reverse, against 34 and 101; rows of 4096, 73 and 366 against 19 and 62.)
+constexpr int64_t ROWS_ACROSS = 1 << 20;        // workgroups of a launch's first dimension
+// Rows of more vectors than a wavefront has lanes: a wavefront each, no barrier.  It holds KB vectors a lane, or (AGAIN), where the row
+// is longer than they are, loads them in turn for each of its sums and for the outputs.  (A workgroup for a row waits at two or three
+// barriers for every row or two: 1024 x 8 rows of 2047 channels, bf16, 81 us forward and 450 reverse, against 34 and 86; 1024 x 4 of 4096,
+// 73 and 366 against 19 and 49.)
 template <typename T, int VEC, int KB> struct LongRow {
-  int g, t, b;
+  int g, t, b, base = 0;
   int64_t m;
   bool there, live;
   __device__ __forceinline__ explicit LongRow(const NormP &a) {
-    const unsigned id = blockIdx.x * 4u + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = id / (unsigned)a.G;
+    const unsigned id = (blockIdx.y * (unsigned)ROWS_ACROSS + blockIdx.x) * 4u + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = id / (unsigned)a.G;
     g = (int)(id - row * a.G);
     m = row;
     there = m < a.rows;
@@ -384,9 +355,9 @@ template <typename T, int VEC, int KB> struct LongRow {
     b = (int)(row - (unsigned)t * a.B);
     live = there && t < length_of(a.lengths, b, a.T);
   }
-  static __device__ __forceinline__ int channel(int s) { return (s * 64 + (int)(threadIdx.x & 63)) * VEC; }
+  __device__ __forceinline__ int channel(int s) const { return base + (s * 64 + (int)(threadIdx.x & 63)) * VEC; }
   // Every second or fourth vector: does the row end before it?
-  static __device__ __forceinline__ bool ends(const NormP &a, int s) { return s && s % (KB == 4 ? 2 : 4) == 0 && s * 64 * VEC >= a.C; }
+  __device__ __forceinline__ bool ends(const NormP &a, int s) const { return s && s % (KB == 4 ? 2 : 4) == 0 && base + s * 64 * VEC >= a.C; }
   template <typename R> __device__ __forceinline__ T *at(const NormP &a, const R &r) const { return (T *)r.p + b * r.sb + t * r.st + (int64_t)g * a.C; }
   template <typename R> __device__ __forceinline__ void load(const NormP &a, const R &r, Pack<T, VEC> (&v)[KB]) const {
     const T *row = at(a, r);
@@ -398,110 +369,136 @@ template <typename T, int VEC, int KB> struct LongRow {
   }
   template <typename R> __device__ __forceinline__ void zeros(const NormP &a, const R &r) const {
     const Pack<T, VEC> zero = {};
-    for (int s = 0; s < KB; ++s)
-      if (channel(s) < a.C) *(Pack<T, VEC> *)(at(a, r) + channel(s)) = zero;
+    for (int c = channel(0); c < a.C; c += 64 * VEC) *(Pack<T, VEC> *)(at(a, r) + c) = zero;
   }
 };
-template <typename T, int VEC, int KB> __global__ __launch_bounds__(256) void norm_rows_kernel(const NormP a) {
-  const LongRow<T, VEC, KB> w(a);
+template <typename T, int VEC, int KB, bool AGAIN> __global__ __launch_bounds__(256) void norm_rows_kernel(const NormP a) {
+  LongRow<T, VEC, KB> w(a);
   if (!w.there) return;
   if (!w.live) {
     w.zeros(a, a.y);
     return;
   }
   Pack<T, VEC> x[KB];
-  w.load(a, a.x, x);
+  if (!AGAIN) w.load(a, a.x, x);
+  auto over_row = [&](auto f) {
+    if (!AGAIN) return f();
+    for (w.base = 0; w.base < a.C; w.base += KB * 64 * VEC) {
+      w.load(a, a.x, x);
+      f();
+    }
+  };
   const float n = 1.f / (float)a.C;
   float mean = 0.f, q = 0.f;
+  over_row([&] {
 #pragma unroll
-  for (int s = 0; s < KB; ++s) {
-    if (w.ends(a, s)) break;
+    for (int s = 0; s < KB; ++s) {
+      if (w.ends(a, s)) break;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) mean += w.channel(s) < a.C ? widen(x[s].v[v]) : 0.f;
-  }
-  mean = wave_sum(mean, 6) * n;
-#pragma unroll
-  for (int s = 0; s < KB; ++s) {
-    if (w.ends(a, s)) break;
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      const float e = w.channel(s) < a.C ? widen(x[s].v[v]) - mean : 0.f;
-      q = fmaf(e, e, q);
+      for (int v = 0; v < VEC; ++v) mean += w.channel(s) < a.C ? widen(x[s].v[v]) : 0.f;
     }
-  }
+  });
+  mean = wave_sum(mean, 6) * n;
+  over_row([&] {
+#pragma unroll
+    for (int s = 0; s < KB; ++s) {
+      if (w.ends(a, s)) break;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float e = w.channel(s) < a.C ? widen(x[s].v[v]) - mean : 0.f;
+        q = fmaf(e, e, q);
+      }
+    }
+  });
   const float rstd = __builtin_amdgcn_rsqf(fmaf(wave_sum(q, 6), n, a.eps));
   if (a.saved && (threadIdx.x & 63) == 0) a.saved[w.m * a.G + w.g] = {mean, rstd};
   T *y = w.at(a, a.y);
   with_silu(a.silu, [&](auto silu) {
+    over_row([&] {
 #pragma unroll
-    for (int s = 0; s < KB; ++s) {
-      if (w.ends(a, s)) break;
-      const int c = w.channel(s);
-      float wt[VEC], bs[VEC];
-      params<VEC>(a, w.g * a.C + (c < a.C ? c : 0), wt, bs);
-      Pack<T, VEC> out;
+      for (int s = 0; s < KB; ++s) {
+        if (w.ends(a, s)) break;
+        const int c = w.channel(s);
+        float wt[VEC], bs[VEC];
+        params<VEC>(a, w.g * a.C + (c < a.C ? c : 0), wt, bs);
+        Pack<T, VEC> out;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) out.v[v] = narrow<T>(output_of(widen(x[s].v[v]), mean, rstd, wt[v], bs[v], silu.value));
-      if (c < a.C) *(Pack<T, VEC> *)(y + c) = out;
-      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-    }
+        for (int v = 0; v < VEC; ++v) out.v[v] = narrow<T>(output_of(widen(x[s].v[v]), mean, rstd, wt[v], bs[v], silu.value));
+        if (c < a.C) *(Pack<T, VEC> *)(y + c) = out;
+        if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+    });
   });
 }
-template <typename T, int VEC, int KB> __global__ __launch_bounds__(256) void norm_rows_backward_kernel(const NormP a) {
-  const LongRow<T, VEC, KB> w(a);
+template <typename T, int VEC, int KB, bool AGAIN> __global__ __launch_bounds__(256) void norm_rows_backward_kernel(const NormP a) {
+  LongRow<T, VEC, KB> w(a);
   if (!w.there) return;
   if (!w.live) {
     w.zeros(a, a.dx);
     return;
   }
   Pack<T, VEC> x[KB], dy[KB];
-  w.load(a, a.x, x);
-  w.load(a, a.dy, dy);
+  auto take = [&] {
+    w.load(a, a.x, x);
+    w.load(a, a.dy, dy);
+  };
+  if (!AGAIN) take();
+  auto over_row = [&](auto f) {
+    if (!AGAIN) return f();
+    for (w.base = 0; w.base < a.C; w.base += KB * 64 * VEC) {
+      take();
+      f();
+    }
+  };
   const float2 st = a.saved[w.m * a.G + w.g];
   const float n = 1.f / (float)a.C;
   T *dx = w.at(a, a.dx);
   with_silu(a.silu, [&](auto silu) {
     float s1 = 0.f, s2 = 0.f;
+    over_row([&] {
 #pragma unroll
-    for (int s = 0; s < KB; ++s) {
-      if (w.ends(a, s)) break;
-      const int c = w.channel(s);
-      float wt[VEC], bs[VEC];
-      params<VEC>(a, w.g * a.C + (c < a.C ? c : 0), wt, bs);
+      for (int s = 0; s < KB; ++s) {
+        if (w.ends(a, s)) break;
+        const int c = w.channel(s);
+        float wt[VEC], bs[VEC];
+        params<VEC>(a, w.g * a.C + (c < a.C ? c : 0), wt, bs);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        const float xh = (widen(x[s].v[v]) - st.x) * st.y;
-        float p;
-        gradient_of(widen(dy[s].v[v]), xh, wt[v], bs[v], silu.value, p);
-        p = c < a.C ? p : 0.f;                   // (behind the row x is its first value, and p xh a zero or one of the row's NaN)
-        s1 += p;
-        s2 = fmaf(p, xh, s2);
+        for (int v = 0; v < VEC; ++v) {
+          const float xh = (widen(x[s].v[v]) - st.x) * st.y;
+          float p;
+          gradient_of(widen(dy[s].v[v]), xh, wt[v], bs[v], silu.value, p);
+          p = c < a.C ? p : 0.f;                   // (behind the row x is its first value, and p xh a zero or one of the row's NaN)
+          s1 += p;
+          s2 = fmaf(p, xh, s2);
+        }
+        if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
-      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-    }
+    });
     s1 = wave_sum(s1, 6) * n;
     s2 = wave_sum(s2, 6) * n;
     keep_packed(x);
     keep_packed(dy);
     int first = w.g * a.C;                       // (the weights are loaded again: kept, they would be most of the registers)
     asm volatile("" : "+s"(first));
+    over_row([&] {
 #pragma unroll
-    for (int s = 0; s < KB; ++s) {
-      if (w.ends(a, s)) break;
-      const int c = w.channel(s);
-      float wt[VEC], bs[VEC];
-      params<VEC>(a, first + (c < a.C ? c : 0), wt, bs);
-      Pack<T, VEC> d;
+      for (int s = 0; s < KB; ++s) {
+        if (w.ends(a, s)) break;
+        const int c = w.channel(s);
+        float wt[VEC], bs[VEC];
+        params<VEC>(a, first + (c < a.C ? c : 0), wt, bs);
+        Pack<T, VEC> d;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        const float xh = (widen(x[s].v[v]) - st.x) * st.y;
-        float p;
-        gradient_of(widen(dy[s].v[v]), xh, wt[v], bs[v], silu.value, p);
-        d.v[v] = narrow<T>(st.y * (p - s1 - xh * s2));
+        for (int v = 0; v < VEC; ++v) {
+          const float xh = (widen(x[s].v[v]) - st.x) * st.y;
+          float p;
+          gradient_of(widen(dy[s].v[v]), xh, wt[v], bs[v], silu.value, p);
+          d.v[v] = narrow<T>(st.y * (p - s1 - xh * s2));
+        }
+        if (c < a.C) *(Pack<T, VEC> *)(dx + c) = d;
+        if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
-      if (c < a.C) *(Pack<T, VEC> *)(dx + c) = d;
-      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-    }
+    });
   });
 }
 // Their dw and db: a lane has VEC columns, a wavefront every fourth row of the chunk blockIdx.y.
@@ -835,40 +832,38 @@ int norm_check(const snn_norm_args *a, bool grads) {
 struct NormCut {
   int nt, tpr_log2, K, R, loops, blocks;       // threads; threads a row (log2); column blocks; rows a thread; lots; workgroups a unit and group
   bool chunks;
-  int long_row;                                // vectors a lane where a wavefront has a row, 0: otherwise
+  int long_row;                                // vectors a lane where a wavefront has a row (or AGAIN_ROW), 0: otherwise
 };
+constexpr int AGAIN_ROW = -1;
 NormCut norm_cut(const snn_norm_args &a, int vec, bool backward) {
   const size_t z = a.type == SNN_TYPE_FP32 ? 4 : 2;
   const int C = a.D / a.groups, slots = vec * z == 16 ? 8 : 16;
   const int64_t rows = a.per_step ? (int64_t)a.T * a.B : a.T, units = a.per_step ? 1 : a.B;
   NormCut c;
-  auto fit = [&](int nt) {
-    c.nt = nt;
-    c.tpr_log2 = 0;
-    while ((vec << c.tpr_log2) < C && (1 << c.tpr_log2) < nt) ++c.tpr_log2;
-    c.K = (C + (vec << c.tpr_log2) - 1) / (vec << c.tpr_log2);
-  };
   auto blocks_of = [&](int64_t each) { return std::max<int64_t>(1, (rows + each - 1) / each); };
-  fit(256);
+  c.nt = 256;
+  c.tpr_log2 = 0;
+  while ((vec << c.tpr_log2) < C && (1 << c.tpr_log2) < c.nt) ++c.tpr_log2;
+  c.K = (C + (vec << c.tpr_log2) - 1) / (vec << c.tpr_log2);
   c.loops = 1;
   c.chunks = false;
   c.long_row = 0;
   if (a.per_step && C > 64 * vec) {
     const int need = (C + 64 * vec - 1) / (64 * vec);
     const int most = vec <= 2 ? 64 / vec : 16;
-    c.long_row = need <= 4 ? 4 : need <= 16 ? 16 : need <= most ? most : 0;
-    if (c.long_row) {                          // R: rows of a chunk of dw and db, in workgroups of 64 vectors of columns
-      const int64_t across = (a.D + 64 * vec - 1) / (64 * vec);
-      c.R = 256;
-      while (c.R > 16 && blocks_of(c.R) * across < 1024) c.R /= 2;
-      c.blocks = (int)blocks_of(c.R);
-      return c;
-    }
-    fit(1024);
+    // Reverse no more than 4 vectors, as x and dy and what is formed of them fill the registers.  (us, held and loaded again: 8192 rows of
+    // 4096, fp32, forward 45 and 79, reverse 175 and 163; 4800 of 4095, 43 and 62, 216 and 122; 4096 of 4096, bf16, 18.7 and 18.9, 62 and 49.)
+    c.long_row = need <= 4 ? 4 : backward ? AGAIN_ROW : need <= 16 ? 16 : need <= most ? most : AGAIN_ROW;
+    const int64_t across = (a.D + 64 * vec - 1) / (64 * vec);
+    c.R = 256;                                 // rows of a chunk of dw and db, in workgroups of 64 vectors of columns
+    while (c.R > 16 && blocks_of(c.R) * across < 1024) c.R /= 2;
+    while (blocks_of(c.R) > 32768) c.R *= 2;
+    c.blocks = (int)blocks_of(c.R);
+    return c;
   }
   if (a.per_step) {
     const int64_t rp = c.nt >> c.tpr_log2;
-    c.R = c.K == 1 && blocks_of(rp * 2) * a.groups >= 512 ? 2 : 1;
+    c.R = blocks_of(rp * 2) * a.groups >= 512 ? 2 : 1;
     const int64_t n = blocks_of(rp * c.R);
     while (c.loops < 64 && blocks_of(rp * c.R * c.loops * 2) * a.groups >= 2048) c.loops *= 2;
     c.blocks = (int)((n + c.loops - 1) / c.loops);
@@ -928,8 +923,7 @@ NormP norm_args(const snn_norm_args &a, const NormCut &c, void *saved, void *wor
 int norm_grid(const snn_norm_args &a, const NormCut &c, dim3 &grid) {
   if (c.long_row) {                            // a wavefront a row and group
     const int64_t n = ((int64_t)a.T * a.B * a.groups + 3) / 4;
-    if (n * 256 >= (1ll << 32) || c.blocks > 65535) return ops_fail(SNN_ERR_ARG, "group norm: too large for one launch");
-    grid = dim3((unsigned)n);
+    grid = dim3((unsigned)std::min<int64_t>(n, ROWS_ACROSS), (unsigned)((n + ROWS_ACROSS - 1) / ROWS_ACROSS));
     return SNN_OK;
   }
   const int64_t n = (int64_t)a.groups * (a.per_step ? 1 : a.B) * c.blocks;
@@ -938,26 +932,29 @@ int norm_grid(const snn_norm_args &a, const NormCut &c, dim3 &grid) {
   return SNN_OK;
 }
 
-template <typename T, int V, typename F> void with_long_row(int kb, F f) {
-  if constexpr (V <= 2)
-    if (kb == 64 / V) return f(std::integral_constant<int, 64 / V>());
-  if (kb == 16) f(std::integral_constant<int, 16>());
-  else f(std::integral_constant<int, 4>());
+template <typename F> void held_or_again(int kb, F f) {
+  if (kb == AGAIN_ROW) f(std::integral_constant<int, 4>(), std::true_type());
+  else f(std::integral_constant<int, 4>(), std::false_type());
 }
 template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
   if (!per_step) {
-    if (!c.chunks && c.nt == 512) hipLaunchKernelGGL((norm_forward_kernel<T, V, 512, WHOLE, true>), grid, dim3(512), 0, st, p);
-    else if (!c.chunks) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, WHOLE, true>), grid, dim3(256), 0, st, p);
+    if (!c.chunks && c.nt == 512) hipLaunchKernelGGL((norm_forward_kernel<T, V, 512, WHOLE>), grid, dim3(512), 0, st, p);
+    else if (!c.chunks) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, WHOLE>), grid, dim3(256), 0, st, p);
     else {
       hipLaunchKernelGGL((norm_moments_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
       const int e = ops_launched("group norm, moments");
       if (e) return e;
       hipLaunchKernelGGL((norm_output_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
     }
-  } else if (c.long_row)
-    with_long_row<T, V>(c.long_row, [&](auto kb) { hipLaunchKernelGGL((norm_rows_kernel<T, V, kb.value>), grid, dim3(256), 0, st, p); });
-  else if (c.K == 1) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, STEP, true>), grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((norm_forward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
+  } else if (c.long_row) {
+    auto rows = [&](auto kb, auto again) { hipLaunchKernelGGL((norm_rows_kernel<T, V, kb.value, again.value>), grid, dim3(256), 0, st, p); };
+    bool done = false;
+    if constexpr (V <= 2)
+      if (c.long_row == 64 / V) rows(std::integral_constant<int, 64 / V>(), std::false_type()), done = true;
+    if (!done && c.long_row == 16) rows(std::integral_constant<int, 16>(), std::false_type()), done = true;
+    if (!done) held_or_again(c.long_row, rows);
+  }
+  else hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, STEP>), grid, dim3(256), 0, st, p);
   return ops_launched("group norm");
 }
 unsigned parameter_blocks(int D) { return (unsigned)((2 * (int64_t)D + 15) / 16); }
@@ -965,8 +962,8 @@ template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per
   if (!per_step) {
     if (!c.chunks) {
       if constexpr (sizeof(T) * V < 16) {
-        if (c.nt == 512) hipLaunchKernelGGL((norm_backward_kernel<T, V, 512, WHOLE, true>), grid, dim3(512), 0, st, p);
-        else hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, WHOLE, true>), grid, dim3(256), 0, st, p);
+        if (c.nt == 512) hipLaunchKernelGGL((norm_backward_kernel<T, V, 512, WHOLE>), grid, dim3(512), 0, st, p);
+        else hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, WHOLE>), grid, dim3(256), 0, st, p);
       }
     } else {
       hipLaunchKernelGGL((norm_slopes_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
@@ -975,13 +972,13 @@ template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per
       hipLaunchKernelGGL((norm_gradient_kernel<T, V, 256>), dim3(grid.x + (p.dweight || p.dbias ? parameter_blocks(p.D) : 0)), dim3(256), 0, st, p);
     }
   } else if (c.long_row) {
-    with_long_row<T, V>(c.long_row, [&](auto kb) { hipLaunchKernelGGL((norm_rows_backward_kernel<T, V, kb.value>), grid, dim3(256), 0, st, p); });
-    if (!p.dweight && !p.dbias) return ops_launched("group norm backward");
-    const int e = ops_launched("group norm backward, rows");
-    if (e) return e;
-    hipLaunchKernelGGL((norm_columns_kernel<T, V>), dim3((p.D + 64 * V - 1) / (64 * V), c.blocks), dim3(256), 0, st, p);
-  } else if (c.K == 1) hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, STEP, true>), grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((norm_backward_kernel<T, V, 1024, STEP, false>), grid, dim3(1024), 0, st, p);
+    if (p.dweight || p.dbias) {
+      hipLaunchKernelGGL((norm_columns_kernel<T, V>), dim3((p.D + 64 * V - 1) / (64 * V), c.blocks), dim3(256), 0, st, p);
+      const int e = ops_launched("group norm backward, parameters");
+      if (e) return e;
+    }
+    held_or_again(c.long_row, [&](auto kb, auto again) { hipLaunchKernelGGL((norm_rows_backward_kernel<T, V, kb.value, again.value>), grid, dim3(256), 0, st, p); });
+  } else hipLaunchKernelGGL((norm_backward_kernel<T, V, 256, STEP>), grid, dim3(256), 0, st, p);
   return ops_launched("group norm backward");
 }
 
