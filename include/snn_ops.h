@@ -199,8 +199,10 @@ int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const
 typedef enum { SNN_ACT_SILU = 0, SNN_ACT_GELU = 1 } snn_act;    /* GELU: v (1 + erf(v / sqrt(2))) / 2 */
 
 /* The matrices have a row for each unit (what a unit reads lies together) and are of the streamed type, as are their gradients; sums
- * are fp32, and fp32 operands of more than 256 rows enter the products as three bfloat16 pieces (all 24 bits, to multiples of 2^-133).  Rows of steps that do not
- * exist take no part, whatever they hold.  One step of every sequence is a call with T = 1.  Refused (SNN_ERR_ARG): D or F above 2^18, T * B above 2^28. */
+ * are fp32, and fp32 operands of more than 256 rows enter the products as three bfloat16 pieces (all 24 bits, to multiples of 2^-133).
+ * Rows of steps that do not exist take no part, whatever they hold.  An infinity or NaN in x stays in its row of y and dx; where the
+ * definition makes an infinity, that or NaN comes out (an infinity's pieces meet zeros).  One step of every sequence is a call with
+ * T = 1.  Refused (SNN_ERR_ARG): D or F above 2^18, T * B above 2^28. */
 typedef struct {
   int32_t T, B, D, F;
   int32_t type;

@@ -7,7 +7,7 @@
 // dy) are read once: mean, squares around it, outputs.  Otherwise a sequence's rows are cut into chunks: one launch leaves every
 // chunk's (mean, sum of squares around it), a second one joins them and reads the rows again, which the last-level cache still has up to
 // some 200 MB.  (One workgroup of 1024 threads that holds 64 values a thread needs no second reading, but fills and empties a compute
-// unit in turn: 1024 steps of 8 x 2048 channels, 32 groups, bf16: forward 24.7 us against 24.0, reverse 226, out of registers, against 43.)
+// unit in turn: 1024 steps of 8 x 2048 channels, 32 groups, bf16: forward 24.7 us against 22.7, reverse 226, out of registers, against 40.)
 // Sums over rows (dw, db) leave a row per chunk or workgroup, which a last launch adds up, or workgroups of the second one.
 #include "rows.hpp"
 
