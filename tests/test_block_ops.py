@@ -316,6 +316,23 @@ def test_group_norm_far_from_zero():
         assert (y - want).abs().max().item() < 3 * 2.0 ** -11
 
 
+def test_group_norm_of_more_rows_than_a_launch_is_wide():
+    """Rows stand alone, so the last ones of many are those of a call of their own; sums of whole numbers are exact."""
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    T, B, D = 70000, 64, 65                               # 4.48 million rows: more than 2^20 workgroups of four
+    x = torch.randn(T, B, D, device="cuda", generator=torch.Generator("cuda").manual_seed(5)).to(torch.bfloat16)
+    dy = torch.randint(-1, 2, (T, B, D), device="cuda", generator=torch.Generator("cuda").manual_seed(6), dtype=torch.int8).to(torch.bfloat16)
+    bias = torch.zeros(D, device="cuda")
+    kw = dict(silu=False, per_step=True)
+    o = group_norm(x, 1, None, bias, save=True, **kw)
+    g = group_norm_backward(dy, o.saved, x, 1, None, bias, **kw)
+    for part in (slice(0, 3), slice(35000, 35003), slice(T - 3, T)):
+        few = group_norm(x[part], 1, None, bias, save=True, **kw)
+        assert torch.equal(o.y[part], few.y)
+        assert torch.equal(g.dx[part], group_norm_backward(dy[part], few.saved, x[part], 1, None, bias, **kw).dx)
+    assert torch.equal(g.dbias.double(), dy.sum((0, 1), dtype=torch.float64))
+
+
 def test_group_norm_infinities_stay_in_their_group():
     from paper_2402_18994_amd import group_norm, group_norm_backward
     T, B, D, groups = 40, 3, 24, 3
