@@ -333,6 +333,22 @@ def test_group_norm_of_more_rows_than_a_launch_is_wide():
     assert torch.equal(g.dbias.double(), dy.sum((0, 1), dtype=torch.float64))
 
 
+@pytest.mark.parametrize("D", (64, 1040, 4096, 8448))
+@pytest.mark.parametrize("type", tuple(TYPES))
+def test_group_norm_parameters_anywhere(D, type):
+    """Weights and biases need no more than the alignment of a float32, however wide x is read."""
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    gen = torch.Generator().manual_seed(D)
+    x, dy = (on_gpu(rand(gen, 70, 3, D), TYPES[type]) for _ in range(2))
+    wide = on_gpu(rand(gen, 2, D + 1))
+    w, b = wide[0, 1:], wide[1, :D]
+    assert w.data_ptr() % 16 == 4
+    for per_step in (False, True):
+        a, c = (group_norm(x, 1, *p, per_step=per_step, save=True) for p in ((w, b), (w.clone(), b.clone())))
+        assert same(a, c)
+        assert same(*(group_norm_backward(dy, a.saved, x, 1, *p, per_step=per_step) for p in ((w, b), (w.clone(), b.clone()))))
+
+
 def test_group_norm_infinities_stay_in_their_group():
     from paper_2402_18994_amd import group_norm, group_norm_backward
     T, B, D, groups = 40, 3, 24, 3
