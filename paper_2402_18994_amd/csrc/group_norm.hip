@@ -586,10 +586,13 @@ template <typename P, int N> __device__ __forceinline__ void take(P (&v)[N], con
 struct Moments {
   float n, mean, m2;
 };
+// What the distance d of two means adds to the squares around the joint one.  The counts come first: with none on one side d is a mean itself,
+// whose square may be no fp32 number.
+__device__ __forceinline__ float apart(float d, float n, float share) { return d * (d * (n * share)); }
 // Both sets of values as one.
 __device__ __forceinline__ Moments joined(const Moments &p, const Moments &q) {
   const float n = p.n + q.n, share = q.n > 0.f ? q.n / n : 0.f, d = q.n > 0.f ? q.mean - p.mean : 0.f;
-  return {n, fmaf(d, share, p.mean), p.m2 + q.m2 + d * d * p.n * share};
+  return {n, fmaf(d, share, p.mean), p.m2 + q.m2 + apart(d, p.n, share)};
 }
 template <int NT> __device__ __forceinline__ Moments block_moments(Moments m, Moments *lds) {
 #pragma unroll
@@ -626,7 +629,7 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
         }
         const float count = m.n + VEC, share = VEC * rcp_fast(count), d = s - m.mean;
         const bool on = r + u < n;
-        m.m2 = on ? m.m2 + q + d * d * m.n * share : m.m2;
+        m.m2 = on ? m.m2 + q + apart(d, m.n, share) : m.m2;
         m.mean = on ? fmaf(d, share, m.mean) : m.mean;
         m.n = on ? count : m.n;
       }

@@ -1,0 +1,39 @@
+"""The gated block's operators at the ends of what they accept, on the GPU: magnitudes, counts, and the tails of an activation.
+
+Each tolerance is derived where it stands; 2^-24 is half a step of fp32."""
+import math
+
+import pytest
+import torch
+
+from tests import block_oracle as oracle
+from tests.test_seq_ops import TYPES, close, half_step, on_gpu, rand, rounded
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("T", (8, 900))
+def test_group_norm_of_values_whose_squares_overflow(T):
+    """fp32 values around 3e19 with a spread of a thousandth of that, whose squares around the mean are fp32 numbers and whose own
+    are not: in one workgroup, and in chunks.  A mean goes through less than 40 roundings (additions of a thread's rows, over lanes, wavefronts and chunks), each
+    2^-24 of itself, 1000 2^-24 of the spread; what else there is is 2^-24 of an output."""
+    from paper_2402_18994_amd import group_norm
+    gen = torch.Generator().manual_seed(T)
+    x = rounded(3e19 + 3e16 * rand(gen, T, 3, 64))
+    n = torch.tensor([T, T // 2 + 1, 0], dtype=torch.int32)
+    (want,) = oracle.norm(x, 2, silu=False, lengths=n)
+    y = group_norm(on_gpu(x), 2, silu=False, lengths=on_gpu(n, torch.int32)).y.double().cpu()
+    assert torch.isfinite(y).all() and (y - want).abs().max().item() < 40 * 1000 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("type", tuple(TYPES))
+@pytest.mark.parametrize("T", (8, 900))
+@pytest.mark.parametrize("value", (-2.0 ** 100, 3000.0))
+def test_group_norm_of_equal_values(value, T, type):
+    """Their deviations are zero, and the outputs the activation of the bias: in one workgroup, and in chunks."""
+    from paper_2402_18994_amd import group_norm
+    gen = torch.Generator().manual_seed(T)
+    bias, t = rounded(rand(gen, 64)), TYPES[type]
+    x = on_gpu(torch.full((T, 3, 64), value), t)
+    y = group_norm(x, 2, bias=on_gpu(bias)).y
+    close("y", y, (bias / (1 + torch.exp(-bias))).expand(T, 3, 64), 1, half_step(t))
