@@ -685,14 +685,13 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
   }
 }
 
-// Reverse: a chunk's sums of p and p xh, and of q xh and q over its rows.  xh = x rstd - mean rstd in one rounding: the rounding of
-// mean rstd moves xh by no more than the rounding of the mean does.
+// Reverse: a chunk's sums of p and p xh, and of q xh and q over its rows.  xh is formed of the difference, as forward: x rstd - mean rstd would
+// leave the rounding of mean rstd where x is the mean, and no number where that product is beyond fp32.
 template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_slopes_kernel(const NormP a) {
   __shared__ float lds[2][NT / 64], cols[NT * VEC];
   const Run<T, VEC> w(a, NT);
   const int64_t unit = (int64_t)w.unit * a.G + w.g;
   const float2 st = a.saved[unit];
-  const float shift = -st.x * st.y;
   float *const out = a.dpart + ((int64_t)w.unit * a.blocks + w.chunk) * 2 * a.D + (int64_t)w.g * a.C;
   float s1 = 0.f, s2 = 0.f;
   for (int k = 0; k < a.K; ++k) {
@@ -711,7 +710,7 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
         if (r + u < n)
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
-            const float xh = fmaf(widen(v[u].v[i]), st.y, shift);
+            const float xh = (widen(v[u].v[i]) - st.x) * st.y;
             float p;
             const float q = gradient_of(widen(d[u].v[i]), xh, wt[i], bs[i], a.silu, p);
             dw[i] = fmaf(q, xh, dw[i]);
@@ -759,7 +758,6 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
   const Run<T, VEC> w(a, NT);
   const int64_t unit = (int64_t)w.unit * a.G + w.g;
   const float2 st = a.saved[unit];
-  const float shift = -st.x * st.y;
   const int c0 = min(w.col, a.C - VEC);
   Pack<T, VEC> next[AHEAD_BWD], dnext[AHEAD_BWD];                    // (on their way while the chunks' sums are added)
   fetch_rows<T, VEC>(next, w.at(a, a.x, c0), a.x.p, w.rp * a.x.st, 0, w.live);
@@ -797,7 +795,7 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
         Pack<T, VEC> out;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          const float xh = fmaf(widen(v[u].v[i]), st.y, shift);
+          const float xh = (widen(v[u].v[i]) - st.x) * st.y;
           float p;
           gradient_of(widen(d[u].v[i]), xh, wt[i], bs[i], a.silu, p);
           out.v[i] = narrow<T>(r + u < w.live ? st.y * (p - s1 - xh * s2) : 0.f);

@@ -37,3 +37,23 @@ def test_group_norm_of_equal_values(value, T, type):
     x = on_gpu(torch.full((T, 3, 64), value), t)
     y = group_norm(x, 2, bias=on_gpu(bias)).y
     close("y", y, (bias / (1 + torch.exp(-bias))).expand(T, 3, 64), 1, half_step(t))
+
+
+@pytest.mark.parametrize("type", tuple(TYPES))
+@pytest.mark.parametrize("T", (4, 900))
+@pytest.mark.parametrize("value", (-2.0 ** 100, 3000.0, 2.0 ** 120))
+def test_group_norm_gradients_of_equal_values(value, T, type):
+    """Deviations of zero: dweight is zero, dbias = sum q with q = dy silu'(bias), dx = rstd (p - mean(p)) with p = q w, rstd = eps^(-1/2)."""
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    gen = torch.Generator().manual_seed(T)
+    w, bias, t = rounded(1 + 0.2 * rand(gen, 64)), rounded(rand(gen, 64)), TYPES[type]
+    dy, x = rounded(rand(gen, T, 3, 64), t), on_gpu(torch.full((T, 3, 64), value), t)
+    saved = group_norm(x, 2, on_gpu(w), on_gpu(bias), save=True).saved
+    g = group_norm_backward(on_gpu(dy, t), saved, x, 2, on_gpu(w), on_gpu(bias))
+    s = 1 / (1 + torch.exp(-bias))
+    q = dy * s * (1 + bias * (1 - s))
+    p = (q * w).view(T, 3, 2, 32)
+    dx = ((p - p.mean((0, 3), keepdim=True)) / math.sqrt(1e-5)).view(T, 3, 64)
+    assert (g.dweight == 0).all()
+    close("dbias", g.dbias, q.sum((0, 1)), 3 * T, 2.0 ** -24)
+    close("dx", g.dx, dx, 32 * T, half_step(t))
