@@ -34,8 +34,13 @@ struct NormP {
   Rows<void> dy, dx;
   float *dpart;                             // [units * blocks][2][D]
   float *dweight, *dbias;
-  unsigned main;                            // workgroups of a launch that are not there for dweight and dbias
+  unsigned main;                            // workgroups of a launch that have a part of x; behind them some are there for dweight and dbias
 };
+
+// A launch's dimension counts its threads in 32 bits: workgroups are numbered over two.
+constexpr unsigned ACROSS = 1 << 20;
+__device__ __forceinline__ unsigned workgroup() { return blockIdx.y * ACROSS + blockIdx.x; }
+dim3 grid_of(int64_t n) { return dim3((unsigned)std::min<int64_t>(n, ACROSS), (unsigned)((n + ACROSS - 1) / ACROSS)); }
 
 // Sum over aligned sets of 2^w lanes, in all of them.
 __device__ __forceinline__ float wave_sum(float v, int w) {
@@ -164,10 +169,10 @@ template <int VEC> __device__ __forceinline__ void params(const NormP &a, int d,
 }
 
 template <typename T, int VEC>
-__device__ __forceinline__ Where<T, VEC> where(const NormP &a, bool step, int nt) {
-  const unsigned rest = blockIdx.x / (unsigned)a.G, turn = rest / (unsigned)a.units;
+__device__ __forceinline__ Where<T, VEC> where(const NormP &a, unsigned id, bool step, int nt) {
+  const unsigned rest = id / (unsigned)a.G, turn = rest / (unsigned)a.units;
   Where<T, VEC> w{a, 0, 0, 0, 0, 0, 0, 0, step};
-  w.g = (int)(blockIdx.x - rest * a.G);
+  w.g = (int)(id - rest * a.G);
   w.unit = (int)(rest - turn * a.units);
   w.rsub = (int)threadIdx.x >> a.tpr_log2;
   w.col = (int)threadIdx.x & ((1 << a.tpr_log2) - 1);
@@ -199,7 +204,8 @@ template <typename T, int VEC, int NT, int MODE>
 __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
   constexpr int SLOTS = Slots<T, VEC, MODE>::N;
   __shared__ float lds[2][NT / 64];
-  auto w = where<T, VEC>(a, MODE == STEP, NT);
+  if (workgroup() >= a.main) return;
+  auto w = where<T, VEC>(a, workgroup(), MODE == STEP, NT);
   float wt[VEC], bs[VEC];
   params<VEC>(a, w.channel() < a.C ? w.g * a.C + w.channel() : 0, wt, bs);
   for (int loop = 0; loop < a.loops; ++loop, w.r0 += (int64_t)w.rp * a.R) {
@@ -276,8 +282,10 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
   constexpr int SLOTS = Slots<T, VEC, MODE>::N;
   __shared__ float lds[2][NT / 64];
   __shared__ float cols[NT * VEC];
-  auto w = where<T, VEC>(a, MODE == STEP, NT);
-  const int chunk = (int)(blockIdx.x / ((unsigned)a.G * (unsigned)a.units));
+  const unsigned id = workgroup();
+  if (id >= a.main) return;
+  auto w = where<T, VEC>(a, id, MODE == STEP, NT);
+  const int chunk = (int)(id / ((unsigned)a.G * (unsigned)a.units));
   const int silu = SILU < 0 ? a.silu : SILU;
   float wt[VEC], bs[VEC], dw[VEC], db[VEC];
   params<VEC>(a, w.channel() < a.C ? w.g * a.C + w.channel() : 0, wt, bs);
@@ -341,7 +349,6 @@ __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormP a) {
 }
 
 // ---------------------------------------------------------------- long rows by themselves
-constexpr int64_t ROWS_ACROSS = 1 << 20;        // workgroups of a launch's first dimension
 // Rows of more vectors than a wavefront has lanes: a wavefront each, no barrier.  It holds KB vectors a lane, or (AGAIN), where the row
 // is longer than they are, loads them in turn for each of its sums and for the outputs.  (A workgroup for a row waits at two or three
 // barriers for every row or two: 1024 x 8 rows of 2047 channels, bf16, 81 us forward and 450 reverse, against 34 and 86; 1024 x 4 of 4096,
@@ -351,7 +358,7 @@ template <typename T, int VEC, int KB> struct LongRow {
   int64_t m;
   bool there, live;
   __device__ __forceinline__ explicit LongRow(const NormP &a) {
-    const unsigned id = (blockIdx.y * (unsigned)ROWS_ACROSS + blockIdx.x) * 4u + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = id / (unsigned)a.G;
+    const unsigned id = workgroup() * 4u + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = id / (unsigned)a.G;
     g = (int)(id - row * a.G);
     m = row;
     there = m < a.rows;
@@ -551,9 +558,9 @@ constexpr int AHEAD = 4, AHEAD_BWD = 2;      // rows in flight a thread (reverse
 template <typename T, int VEC> struct Run {
   int unit, g, chunk, col, len, live, there, rp;
   int64_t first;
-  __device__ __forceinline__ Run(const NormP &a, int nt) {
-    const unsigned rest = blockIdx.x / (unsigned)a.G;
-    g = (int)(blockIdx.x - rest * a.G);
+  __device__ __forceinline__ Run(const NormP &a, unsigned id, int nt) {
+    const unsigned rest = id / (unsigned)a.G;
+    g = (int)(id - rest * a.G);
     chunk = (int)(rest / (unsigned)a.units);
     unit = (int)(rest - (unsigned)chunk * a.units);
     col = ((int)threadIdx.x & ((1 << a.tpr_log2) - 1)) * VEC;
@@ -608,7 +615,8 @@ template <int NT> __device__ __forceinline__ Moments block_moments(Moments m, Mo
 // Forward: a chunk's mean and sum of squares around it.  A thread goes from vector to vector, each with its own mean.
 template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_moments_kernel(const NormP a) {
   __shared__ Moments lds[NT / 64];
-  const Run<T, VEC> w(a, NT);
+  if (workgroup() >= a.main) return;
+  const Run<T, VEC> w(a, workgroup(), NT);
   Moments m = {0.f, 0.f, 0.f};
   for (int k = 0; k < a.K; ++k) {
     const int c = (k << a.tpr_log2) * VEC + w.col, n = c < a.C ? w.live : 0;
@@ -647,7 +655,8 @@ __device__ __forceinline__ float chunk_count(const NormP &a, int64_t rows, int c
 
 template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_output_kernel(const NormP a) {
   __shared__ Moments lds[NT / 64];
-  const Run<T, VEC> w(a, NT);
+  if (workgroup() >= a.main) return;
+  const Run<T, VEC> w(a, workgroup(), NT);
   const int64_t unit = (int64_t)w.unit * a.G + w.g;
   const int c0 = min(w.col, a.C - VEC);
   Pack<T, VEC> next[AHEAD];                                  // (on their way while the chunks are joined)
@@ -689,7 +698,8 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
 // leave the rounding of mean rstd where x is the mean, and no number where that product is beyond fp32.
 template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_slopes_kernel(const NormP a) {
   __shared__ float lds[2][NT / 64], cols[NT * VEC];
-  const Run<T, VEC> w(a, NT);
+  if (workgroup() >= a.main) return;
+  const Run<T, VEC> w(a, workgroup(), NT);
   const int64_t unit = (int64_t)w.unit * a.G + w.g;
   const float2 st = a.saved[unit];
   float *const out = a.dpart + ((int64_t)w.unit * a.blocks + w.chunk) * 2 * a.D + (int64_t)w.g * a.C;
@@ -751,11 +761,12 @@ __device__ __forceinline__ void sum_parameters(const float *part, int rows, int 
 template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void norm_gradient_kernel(const NormP a) {
   static_assert(NT == 256, "as sum_column takes it");
   __shared__ float lds[NT];
-  if (blockIdx.x >= a.main) {
-    sum_parameters(a.dpart, a.units * a.blocks, a.D, a.dweight, a.dbias, blockIdx.x - a.main, lds);
+  const unsigned id = workgroup();
+  if (id >= a.main) {
+    sum_parameters(a.dpart, a.units * a.blocks, a.D, a.dweight, a.dbias, id - a.main, lds);
     return;
   }
-  const Run<T, VEC> w(a, NT);
+  const Run<T, VEC> w(a, id, NT);
   const int64_t unit = (int64_t)w.unit * a.G + w.g;
   const float2 st = a.saved[unit];
   const int c0 = min(w.col, a.C - VEC);
@@ -922,28 +933,23 @@ template <typename F> int with_vector(const snn_norm_args &a, int vec, F f) {
   return vec == 8 ? f(__bf16(), integral_constant<int, 8>()) : vec == 2 ? f(__bf16(), integral_constant<int, 2>()) : f(__bf16(), integral_constant<int, 1>());
 }
 
+// Workgroups of the launches over x: fewer than 2^31, as T B groups is.
+int64_t norm_workgroups(const snn_norm_args &a, const NormCut &c) {
+  if (c.long_row) return ((int64_t)a.T * a.B * a.groups + 3) / 4;      // a wavefront a row and group
+  return (int64_t)a.groups * (a.per_step ? 1 : a.B) * c.blocks;
+}
+
 NormP norm_args(const snn_norm_args &a, const NormCut &c, void *saved, void *workspace) {
   return NormP{a.T, a.B, a.D, a.groups, a.D / a.groups, a.silu, a.eps, a.per_step ? (int64_t)a.T * a.B : a.T, a.per_step ? 1 : a.B, c.blocks, c.loops,
                c.tpr_log2, c.K, c.R, Rows<void>(a.x, a.T), Rows<void>(a.y, a.T), a.weight, a.bias, a.lengths, (float2 *)saved, (float2 *)workspace,
-               Rows<void>(snn_rows{}), Rows<void>(snn_rows{}), nullptr, nullptr, nullptr, 0};
+               Rows<void>(snn_rows{}), Rows<void>(snn_rows{}), nullptr, nullptr, nullptr, (unsigned)norm_workgroups(a, c)};
 }
-int norm_grid(const snn_norm_args &a, const NormCut &c, dim3 &grid) {
-  if (c.long_row) {                            // a wavefront a row and group
-    const int64_t n = ((int64_t)a.T * a.B * a.groups + 3) / 4;
-    grid = dim3((unsigned)std::min<int64_t>(n, ROWS_ACROSS), (unsigned)((n + ROWS_ACROSS - 1) / ROWS_ACROSS));
-    return SNN_OK;
-  }
-  const int64_t n = (int64_t)a.groups * (a.per_step ? 1 : a.B) * c.blocks;
-  if (n * c.nt >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "group norm: too large for one launch");
-  grid = dim3((unsigned)n);
-  return SNN_OK;
-}
-
 template <typename F> void held_or_again(int kb, F f) {
   if (kb == AGAIN_ROW) f(std::integral_constant<int, 4>(), std::true_type());
   else f(std::integral_constant<int, 4>(), std::false_type());
 }
-template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
+template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, const NormP &p, hipStream_t st) {
+  const dim3 grid = grid_of(p.main);
   if (!per_step) {
     if (!c.chunks && c.nt == 512) hipLaunchKernelGGL((norm_forward_kernel<T, V, 512, WHOLE>), grid, dim3(512), 0, st, p);
     else if (!c.chunks) hipLaunchKernelGGL((norm_forward_kernel<T, V, 256, WHOLE>), grid, dim3(256), 0, st, p);
@@ -965,7 +971,8 @@ template <typename T, int V> int launch_norm(const NormCut &c, bool per_step, co
   return ops_launched("group norm");
 }
 unsigned parameter_blocks(int D) { return (unsigned)((2 * (int64_t)D + 15) / 16); }
-template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per_step, const NormP &p, dim3 grid, hipStream_t st) {
+template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per_step, const NormP &p, hipStream_t st) {
+  const dim3 grid = grid_of(p.main);
   if (!per_step) {
     if (!c.chunks) {
       if constexpr (sizeof(T) * V < 16) {
@@ -976,7 +983,7 @@ template <typename T, int V> int launch_norm_backward(const NormCut &c, bool per
       hipLaunchKernelGGL((norm_slopes_kernel<T, V, 256>), grid, dim3(256), 0, st, p);
       const int e = ops_launched("group norm backward, sums");
       if (e) return e;
-      hipLaunchKernelGGL((norm_gradient_kernel<T, V, 256>), dim3(grid.x + (p.dweight || p.dbias ? parameter_blocks(p.D) : 0)), dim3(256), 0, st, p);
+      hipLaunchKernelGGL((norm_gradient_kernel<T, V, 256>), grid_of((int64_t)p.main + (p.dweight || p.dbias ? parameter_blocks(p.D) : 0)), dim3(256), 0, st, p);
     }
   } else if (c.long_row) {
     if (p.dweight || p.dbias) {
@@ -1023,10 +1030,8 @@ int32_t snn_norm_forward(const snn_norm_args *a, void *saved, void *workspace, s
   if (a->T == 0) return SNN_OK;
   const int vec = norm_vector(*a, nullptr);
   const NormCut c = norm_cut(*a, vec, false);
-  dim3 grid;
-  if ((rc = norm_grid(*a, c, grid))) return rc;
   const NormP p = norm_args(*a, c, saved, workspace);
-  return with_vector(*a, vec, [&](auto t, auto v) { return launch_norm<decltype(t), v.value>(c, a->per_step, p, grid, (hipStream_t)stream); });
+  return with_vector(*a, vec, [&](auto t, auto v) { return launch_norm<decltype(t), v.value>(c, a->per_step, p, (hipStream_t)stream); });
 }
 
 int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const void *saved, void *workspace, size_t workspace_bytes, void *stream) {
@@ -1042,17 +1047,14 @@ int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const
     return ops_fail(SNN_ERR_WORKSPACE, "group norm backward: %zu bytes of 16-byte aligned workspace are needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
   const int vec = norm_vector(*a, g);
   const NormCut c = norm_cut(*a, vec, true);
-  dim3 grid;
-  if ((rc = norm_grid(*a, c, grid))) return rc;
   NormP p = norm_args(*a, c, const_cast<void *>(saved), workspace);
   p.dy = Rows<void>(g->dy, a->T);
   p.dx = Rows<void>(g->dx, a->T);
   p.dpart = (float *)((char *)workspace + part_bytes(*a, c));
   p.dweight = g->dweight;
   p.dbias = g->dbias;
-  p.main = grid.x;
   const hipStream_t st = (hipStream_t)stream;
-  if (a->T > 0 && (rc = with_vector(*a, vec, [&](auto t, auto v) { return launch_norm_backward<decltype(t), v.value>(c, a->per_step, p, grid, st); }))) return rc;
+  if (a->T > 0 && (rc = with_vector(*a, vec, [&](auto t, auto v) { return launch_norm_backward<decltype(t), v.value>(c, a->per_step, p, st); }))) return rc;
   if ((!g->dweight && !g->dbias) || (a->T > 0 && c.chunks)) return SNN_OK;
   hipLaunchKernelGGL(norm_sum_kernel, dim3(parameter_blocks(a->D)), dim3(256), 0, st, p.dpart, a->T > 0 ? p.units * c.blocks : 0, a->D, g->dweight,
                      g->dbias);

@@ -57,3 +57,22 @@ def test_group_norm_gradients_of_equal_values(value, T, type):
     assert (g.dweight == 0).all()
     close("dbias", g.dbias, q.sum((0, 1)), 3 * T, 2.0 ** -24)
     close("dx", g.dx, dx, 32 * T, half_step(t))
+
+
+@pytest.mark.parametrize("T,C", ((4, 1), (2, 8)))
+def test_group_norm_of_many_sequences_and_groups(T, C):
+    """2^24 of them, more workgroups of 256 than a launch's first dimension counts threads: one channel a group, and eight (whose reverse pass
+    runs in chunks).  Sequences stand alone, so the last ones are those of a call of their own; sums of whole numbers are exact."""
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    B, G = 1 << 16, 256
+    gen = torch.Generator("cuda").manual_seed(T)
+    x = torch.randn(T, B, G * C, device="cuda", generator=gen).to(torch.bfloat16)
+    dy = torch.randint(-1, 2, (T, B, G * C), device="cuda", generator=gen, dtype=torch.int8).to(torch.bfloat16)
+    bias = torch.zeros(G * C, device="cuda")
+    o = group_norm(x, G, None, bias, silu=False, save=True)
+    g = group_norm_backward(dy, o.saved, x, G, None, bias, silu=False)
+    for at in (slice(0, 3), slice(B // 2 - 1, B // 2 + 2), slice(B - 3, B)):
+        few = group_norm(x[:, at], G, None, bias, silu=False, save=True)
+        assert torch.equal(o.y[:, at], few.y)
+        assert torch.equal(g.dx[:, at], group_norm_backward(dy[:, at], few.saved, x[:, at], G, None, bias, silu=False).dx)
+    assert torch.equal(g.dbias.double(), dy.sum((0, 1), dtype=torch.float64))
