@@ -76,3 +76,27 @@ def test_group_norm_of_many_sequences_and_groups(T, C):
         assert torch.equal(o.y[:, at], few.y)
         assert torch.equal(g.dx[:, at], group_norm_backward(dy[:, at], few.saved, x[:, at], G, None, bias, silu=False).dx)
     assert torch.equal(g.dbias.double(), dy.sum((0, 1), dtype=torch.float64))
+
+
+@pytest.mark.parametrize("rows", (1, 300))
+def test_gelu_far_from_zero(rows):
+    """GELU and its slope where they are small, every value by itself: units of one input, x = 1 and up = 1, give act(gate), and with dy = 1 dup is act(gate)
+    and dgate is act'(gate) in each of `rows` equal rows.
+
+    Off by: z = g / sqrt(2) is rounded twice, 2^-23 of itself, which moves erfc(z), whose logarithm's slope is -(2 z + 1 / z) at most, by (g^2 + 1)
+    2^-23 of itself; ten halves of a last place for erfc itself and the products.  In the slope exp(-g^2 / 2) has its argument rounded four times, 2 g^2
+    2^-24, and where g < -3 the terms, which differ in sign, are at most 1.3 times their sum.  Sums of equal rows: sqrt(rows) 2^-24 more, rows 2^-24 at most."""
+    from paper_2402_18994_amd import gated_units, gated_units_backward
+    for low, high in ((-9.0, -3.0), (0.25, 9.0)):
+        g = rounded(torch.linspace(low, high, 193, dtype=torch.float64))
+        x, gate, up = torch.ones(rows, 1, 1, device="cuda"), on_gpu(g)[:, None], torch.ones(193, 1, device="cuda")
+        o = gated_units(x, gate, up, act="gelu", save=True)
+        d = gated_units_backward(torch.ones_like(o.y), o.saved, x, gate, up, act="gelu")
+        act = 0.5 * g * torch.erfc(-g * 0.5 ** 0.5)
+        slope = 0.5 * torch.erfc(-g * 0.5 ** 0.5) + g * torch.exp(-0.5 * g * g) / math.sqrt(2 * math.pi)
+        off = (g * g + 1) * 2.0 ** -23 + 10 * 2.0 ** -24
+        sums = rows * 2.0 ** -24 if rows > 1 else 0.0
+        for name, got, want, tol in (("y", o.y[0, 0], act, off), ("last y", o.y[-1, 0], act, off), ("dup", d.dup[:, 0] / rows, act, off + sums),
+                                     ("dgate", d.dgate[:, 0] / rows, slope, 1.3 * (off + g * g * 2.0 ** -23 + 4 * 2.0 ** -24) + sums)):
+            worst = ((got.double().cpu() - want).abs() / want.abs() / tol).max().item()
+            assert worst <= 1, (name, low, worst)
