@@ -79,6 +79,13 @@ template <typename T, int VEC, int MODE> struct Slots {
   static constexpr int N = MODE == STEP ? 2 : sizeof(T) * VEC == 16 ? 8 : 16;
 };
 
+// 1 / sqrt(v).  The hardware's root takes what is below the least normal number, a variance without an eps may be, for zero.
+__device__ __forceinline__ float rstd_of(float v) {
+  const bool small = v < 0x1p-126f;
+  const float r = __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v);
+  return small ? r * 0x1p32f : r;
+}
+
 __device__ __forceinline__ float silu_slope(float v) {
   const float s = sigmoid_fast(v);
   return s * fmaf(v, 1.f - s, 1.f);
@@ -238,7 +245,7 @@ __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
     sums_of<NT, SLOTS, MODE>(a, rstd, lds[1]);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
-      rstd[s] = __builtin_amdgcn_rsqf(fmaf(rstd[s], n, a.eps));
+      rstd[s] = rstd_of(fmaf(rstd[s], n, a.eps));
       if (MODE == STEP && a.saved && w.col == 0 && w.there(s)) a.saved[w.row(s) * a.G + w.g] = {mean[s], rstd[s]};
     }
     if (MODE == WHOLE && a.saved && threadIdx.x == 0) a.saved[(int64_t)w.unit * a.G + w.g] = {mean[0], rstd[0]};
@@ -421,7 +428,7 @@ template <typename T, int VEC, int KB, bool AGAIN> __global__ __launch_bounds__(
       }
     }
   });
-  const float rstd = __builtin_amdgcn_rsqf(fmaf(wave_sum(q, 6), n, a.eps));
+  const float rstd = rstd_of(fmaf(wave_sum(q, 6), n, a.eps));
   if (a.saved && (threadIdx.x & 63) == 0) a.saved[w.m * a.G + w.g] = {mean, rstd};
   T *y = w.at(a, a.y);
   with_silu(a.silu, [&](auto silu) {
@@ -667,7 +674,7 @@ template <typename T, int VEC, int NT> __global__ __launch_bounds__(NT) void nor
     m = joined(m, Moments{chunk_count(a, (int64_t)w.rp * a.R, c, w.len), p.x, p.y});
   }
   m = block_moments<NT>(m, lds);
-  const float mean = m.mean, rstd = __builtin_amdgcn_rsqf(m.m2 / fmaxf(m.n, 1.f) + a.eps);
+  const float mean = m.mean, rstd = rstd_of(m.m2 / fmaxf(m.n, 1.f) + a.eps);
   if (a.saved && w.chunk == 0 && threadIdx.x == 0) a.saved[unit] = {mean, rstd};
   for (int k = 0; k < a.K; ++k) {
     const int c = (k << a.tpr_log2) * VEC + w.col;

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from tests import block_oracle as oracle
+from tests.seq_oracle import gradients
 from tests.test_seq_ops import TYPES, close, half_step, on_gpu, rand, rounded
 
 pytestmark = pytest.mark.gpu
@@ -100,3 +101,20 @@ def test_gelu_far_from_zero(rows):
                                      ("dgate", d.dgate[:, 0] / rows, slope, 1.3 * (off + g * g * 2.0 ** -23 + 4 * 2.0 ** -24) + sums)):
             worst = ((got.double().cpu() - want).abs() / want.abs() / tol).max().item()
             assert worst <= 1, (name, low, worst)
+
+
+@pytest.mark.parametrize("T,C,per_step", ((4, 32, False), (900, 32, False), (6, 32, True), (6, 1024, True), (6, 4096, True)))
+@pytest.mark.parametrize("type", tuple(TYPES))
+def test_group_norm_of_the_least_spread(T, C, per_step, type):
+    """Values of +-2^-65 and no eps: the variance, 2^-130, is below the least normal number, and the outputs are +-1 all the same."""
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    gen = torch.Generator().manual_seed(C)
+    t = TYPES[type]
+    sign = 1.0 - 2.0 * (torch.arange(2 * C) % 2).double().expand(T, 3, 2 * C)
+    x, dy = sign * 2.0 ** -65, rounded(rand(gen, T, 3, 2 * C), t)
+    kw = dict(silu=False, eps=0.0, per_step=per_step)
+    o = group_norm(on_gpu(x, t), 2, save=True, **kw)
+    assert torch.equal(o.y.double().cpu(), sign)
+    g = group_norm_backward(on_gpu(dy, t), o.saved, on_gpu(x, t), 2, **kw)
+    want = gradients(lambda **k: oracle.norm(k["x"], 2, **kw), {"x": x}, (dy,))
+    close("dx", g.dx, want["x"], C * (1 if per_step else T), half_step(t))
