@@ -943,8 +943,7 @@ template <typename T> int units_forward(const snn_units_args &a, void *saved, ch
 }
 
 template <typename T> __global__ __launch_bounds__(256) void clear_kernel(T *p, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) p[i] = narrow<T>(0.f);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = narrow<T>(0.f);
 }
 
 template <typename T> int units_backward(const snn_units_args &a, const snn_units_grads &g, const float *saved, char *ws, hipStream_t st) {
@@ -954,7 +953,7 @@ template <typename T> int units_backward(const snn_units_args &a, const snn_unit
   if (M == 0) {
     const int64_t n = (int64_t)a.F * a.D;
     for (void *w : {g.dgate, g.dup}) {
-      hipLaunchKernelGGL(clear_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (T *)w, n);
+      hipLaunchKernelGGL(clear_kernel<T>, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16)), dim3(256), 0, st, (T *)w, n);   // (up to 2^36 elements)
       if ((rc = ops_launched("gated units backward, no steps"))) return rc;
     }
     return SNN_OK;

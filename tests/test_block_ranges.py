@@ -118,3 +118,14 @@ def test_group_norm_of_the_least_spread(T, C, per_step, type):
     g = group_norm_backward(on_gpu(dy, t), o.saved, on_gpu(x, t), 2, **kw)
     want = gradients(lambda **k: oracle.norm(k["x"], 2, **kw), {"x": x}, (dy,))
     close("dx", g.dx, want["x"], C * (1 if per_step else T), half_step(t))
+
+
+def test_units_gradients_of_no_steps():
+    """Matrices of 2^32 elements, more than a launch's first dimension counts threads, get gradients of zero."""
+    from paper_2402_18994_amd import gated_units, gated_units_backward
+    F = D = 1 << 16
+    x, gate, up = (torch.empty(s, dtype=torch.bfloat16, device="cuda") for s in ((0, 1, D), (F, D), (F, D)))
+    o = gated_units(x, gate, up, save=True)
+    g = gated_units_backward(o.y, o.saved, x, gate, up)
+    for v in (g.dgate, g.dup):
+        assert not v.view(torch.int64).any()
