@@ -14,6 +14,7 @@
 // fp32 enters as three bfloat16 pieces, x = hi + mid + lo exactly (8 bits each).  Six of the nine products of pieces are summed, the
 // small ones first; those left out are 2^-25 of the product.  That costs 6 of the 16 times that bfloat16 is faster.
 #include "gemm_stream.hpp"
+#include "block_rules.hpp"
 #include "rows.hpp"
 
 #include <algorithm>
@@ -23,7 +24,6 @@ namespace snn {
 namespace {
 
 constexpr int WIDE_WM = 2, WIDE_WN = 4;      // wavefronts of a wide tile
-constexpr int KS = 64;                       // k of a stage: a row of it is 128 bytes
 
 // One side of a product: stage `kp` of plane `plane`, row r at p + r row + kp stage + plane plane (bytes).
 struct Side {
@@ -81,7 +81,6 @@ __device__ __forceinline__ float act_slope(int act, float g) {
 // G and U of 32 rows by 32 units as the accumulators hold them, which is how they are kept for the reverse pass: [G, U][g][lane][4],
 // row lane % 32, unit 8 g + 4 (lane / 32) + 0..3.  (Every store of a wavefront is one KiB; row by row it would be 32 pieces of 32
 // bytes, and the forward pass with them took 180 us longer where memory needs 50: 8192 rows, 4096 units.)
-constexpr int KEPT = 32 * 32 * 2;
 __host__ __device__ inline int64_t kept_block(int mb, int fb, int F) { return ((int64_t)mb * ((F + 31) / 32) + fb) * KEPT; }
 
 // Four neighbouring values of a row from column n on.
@@ -395,7 +394,7 @@ template <typename T> __global__ __launch_bounds__(256) void units_sum_kernel(co
 // into operand registers, where neighbouring lanes have different rows, every 16 lanes touch 16 cache lines, and a compute unit
 // gets 16 bytes a cycle (64 rows, 2048 -> 4096, bf16: 14.4 us against 9.3).  fp32 stays fp32 here: the fp32 matrix instructions
 // keep up, and the matrices need no pass before.
-constexpr int FEW = 64, FEW_UNITS = 16;
+constexpr int FEW_UNITS = 16;
 
 struct FewP {
   const void *gate, *up;
@@ -767,93 +766,14 @@ int units_check(const snn_units_args *a, bool grads) {
   return SNN_OK;
 }
 
-int panels_of(int64_t n) { return (int)((n + KS - 1) / KS); }
-int64_t panel_bytes(int64_t rows, int64_t k, int planes) { return rows * panels_of(k) * 128 * planes; }
-int pitch_of(int n) { return (n + 3) & ~3; }
-
-// x as it lies: one stride between rows, 16-byte pieces, whole stages, and tiles whose offsets fit 31 bits.
-bool x_direct(const snn_units_args &a, int64_t &row) {
-  const bool one = a.T <= 1 || a.B <= 1 || a.x.stride_t == a.x.stride_b * a.B;
-  row = (a.B > 1 ? a.x.stride_b : a.T > 1 ? a.x.stride_t : a.D) * 2;
-  return a.type == SNN_TYPE_BF16 && a.D % KS == 0 && one && aligned(a.x.p, 16) && row % 16 == 0 && row >= 0 && row < (1 << 22);
-}
-bool weights_direct(const snn_units_args &a) { return a.type == SNN_TYPE_BF16 && a.D % KS == 0 && aligned(a.gate, 16) && aligned(a.up, 16); }
-
-struct Tile {
-  int bm, bn;                                // of the product; wide: 256 x 256
-  bool wide;
-};
-Tile tile_of(int64_t m, int64_t n) {
-  const int64_t wide = ((m + 255) / 256) * ((n + 255) / 256);
-  return wide >= 192 ? Tile{256, 256, true} : Tile{128, 128, false};
-}
-struct Product {
-  Tile tile;
-  int mt, nt, splits;
-};
-size_t part_bytes(const Product &p, int64_t m, int n) { return p.splits > 1 ? rup256((size_t)p.splits * m * pitch_of(n) * 4) : 0; }
-
-int64_t kept_size(const snn_units_args &a) { return ((int64_t)a.T * a.B + 31) / 32 * ((a.F + 31) / 32) * KEPT; }
-// The forward product.  Its parts' sums cost 16 bytes a unit and part, and a launch: where tiles fill a third of
-// the chip at most, and have 32 stages (us without and with: 300 rows, 2048 -> 1024, bf16 20.4 and 15.9, fp32 95 and 44; 1000 rows,
-// 1000 -> 300, bf16, 16 stages 18.1 and 19.7; 2000 rows, 2048 -> 512, 128 tiles 21.6 and 22.5).
-Product units_product(const snn_units_args &a) {
-  const int64_t M = (int64_t)a.T * a.B, stages = (int64_t)panels_of(a.D) * (a.type == SNN_TYPE_FP32 ? 6 : 1);
-  Product p;
-  p.tile = tile_of(M, 2 * (int64_t)a.F);
-  p.mt = (int)((M + p.tile.bm - 1) / p.tile.bm);
-  p.nt = (a.F + p.tile.bn / 2 - 1) / (p.tile.bn / 2);
-  const int64_t tiles = std::max<int64_t>(1, (int64_t)p.mt * p.nt);
-  p.splits = stages >= 32 && tiles <= 85 ? (int)std::min<int64_t>({stages / 8, 16, 256 / tiles}) : 1;
-  return p;
-}
-
-struct UnitsPlan {                           // of the reverse pass
-  int64_t M;
-  int planes, segs;
-  Product dx, dw;
-  size_t rows, cols, xt, wt, part_dx, part_dw;   // bytes of each piece of the workspace
-};
-// Both products are one launch.  Small tiles, and parts of the contraction, where there are too few tiles for the chip: so many parts
-// that the workgroups (one a compute unit of wide tiles, two of small ones) have about the same number of stages, eight at least.
-UnitsPlan units_plan(const snn_units_args &a) {
-  UnitsPlan u;
-  u.M = (int64_t)a.T * a.B;
-  u.planes = a.type == SNN_TYPE_FP32 ? 3 : 1;
-  u.segs = u.planes == 3 ? 6 : 1;
-  const int64_t F2 = 2 * (int64_t)panels_of(a.F) * KS;
-  auto tiles = [](int64_t m, int64_t n, int b) { return (m + b - 1) / b * ((n + b - 1) / b); };
-  const bool wide = tiles(u.M, a.D, 256) + tiles(2 * (int64_t)a.F, a.D, 256) >= 192;
-  const int64_t stages_dx = (int64_t)2 * panels_of(a.F) * u.segs, stages_dw = (int64_t)panels_of(u.M) * u.segs;
-  const int b = wide ? 256 : 128;
-  const int64_t all = tiles(u.M, a.D, b) * stages_dx + tiles(2 * (int64_t)a.F, a.D, b) * stages_dw, each = std::max<int64_t>(8, all / (wide ? 256 : 512));
-  auto product = [&](int64_t m, int64_t stages) {
-    Product p;
-    p.tile = Tile{b, b, wide};
-    p.mt = (int)((m + b - 1) / b);
-    p.nt = (a.D + b - 1) / b;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, stages / each));
-    return p;
-  };
-  u.dx = product(u.M, stages_dx);
-  u.dw = product(2 * (int64_t)a.F, stages_dw);
-  u.rows = rup256(panel_bytes(u.M, F2, u.planes));
-  u.cols = rup256(panel_bytes(2 * (int64_t)a.F, u.M, u.planes));
-  u.xt = rup256(panel_bytes(a.D, u.M, u.planes));
-  u.wt = rup256(panel_bytes(a.D, F2, u.planes));
-  u.part_dx = part_bytes(u.dx, u.M, a.D);
-  u.part_dw = part_bytes(u.dw, 2 * (int64_t)a.F, a.D);
-  return u;
-}
-
 // Workgroups of a product.
 int64_t blocks_of(const GemmP &p) { return (int64_t)p.mt * p.nt * p.splits; }
 template <typename T, int WHAT> int launch_gemm(const Jobs &jobs, int64_t n, bool wide, hipStream_t st) {
   if (n * 512 >= (1ll << 32)) return ops_fail(SNN_ERR_ARG, "gated units: too large for one launch");
-  // (small tiles, up to one a compute unit: four stages in LDS, three of them on their way; more: two, and two workgroups a compute unit)
+  const int stages = gemm_stages(n, wide);
   auto k = wide ? gemm_kernel<T, WHAT, WIDE_WM, WIDE_WN, 8 / WIDE_WM, 8 / WIDE_WN, 64, 2>
-           : n <= 256 ? gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 4> : gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 2>;
-  const int bytes = wide ? 2 * (256 + 256) * 128 : (n <= 256 ? 4 : 2) * (128 + 128) * 128;
+           : stages == 4 ? gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 4> : gemm_kernel<T, WHAT, 2, 2, 2, 2, 64, 2>;
+  const int bytes = stages * (wide ? 256 + 256 : 128 + 128) * 128;
   const hipError_t e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != hipSuccess) return ops_fail(SNN_ERR_HIP, "gated units: %s", hipGetErrorString(e));
   hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(wide ? 64 * WIDE_WM * WIDE_WN : 256), bytes, st, jobs);
@@ -875,9 +795,6 @@ template <typename T> LayP lay_matrix(const snn_units_args &a, const void *w, ch
   return LayP{w, 0, a.D, Steps{1, 1 << 30, nullptr}, a.F, a.D, dst, stage, plane, a.D % 8 == 0 && aligned(w, 8 * sizeof(T))};
 }
 
-// Up to 128 rows, of fp32 256, which the tiles would lay out first (us here and as tiles, 2048 -> 4096: bf16, 128 rows 16.8 and 19.4; fp32, 256
-// rows 90 and 114; 2048 -> 1024: 8.7 and 15.5, 23 and 44).
-bool few_rows(const snn_units_args &a) { return (int64_t)a.T * a.B <= (a.type == SNN_TYPE_FP32 ? 4 * FEW : 2 * FEW); }
 template <typename T, int MB, int WAVES, int NB> int launch_few(const FewP &p, bool wide, hipStream_t st) {
   const dim3 grid((p.F + FEW_UNITS - 1) / FEW_UNITS, (p.M + 16 * MB - 1) / (16 * MB));
   if (!wide) hipLaunchKernelGGL((few_rows_any_kernel<T, MB>), grid, dim3(256), 0, st, p);
@@ -891,13 +808,11 @@ template <typename T, int MB, int WAVES, int NB> int launch_few(const FewP &p, b
   return ops_launched("gated units, few rows");
 }
 template <typename T> int units_few(const snn_units_args &a, void *saved, hipStream_t st) {
-  constexpr int E = 16 / sizeof(T);
   const FewP p{a.gate, a.up, Rows<void>(a.x, a.T), Rows<void>(a.y, a.T), Steps{a.T, a.B, a.lengths}, (float *)saved, a.T * a.B, a.D, a.F, a.act};
-  auto apart = [](int n, int64_t stride) { return n <= 1 ? 0 : stride < 0 || stride > (1 << 30) ? (int64_t)1 << 40 : (n - 1) * stride; };
-  const bool wide = a.D % E == 0 && aligned(a.gate, 16) && aligned(a.up, 16) && rows_take(a.x, a.T, a.B, E, sizeof(T)) &&
-                    (apart(a.T, a.x.stride_t) + apart(a.B, a.x.stride_b)) * (int64_t)sizeof(T) < (1 << 30);
+  const bool wide = few_in_pieces(a);
+  const int blocks = few_blocks(p.M);
   // (wavefronts by buffers: what 160 KiB of LDS hold)
-  return p.M <= 16 ? launch_few<T, 1, 8, 3>(p, wide, st) : p.M <= 32 ? launch_few<T, 2, 8, 2>(p, wide, st) : launch_few<T, 4, 4, 3>(p, wide, st);
+  return blocks == 1 ? launch_few<T, 1, 8, 3>(p, wide, st) : blocks == 2 ? launch_few<T, 2, 8, 2>(p, wide, st) : launch_few<T, 4, 4, 3>(p, wide, st);
 }
 
 template <typename T> int units_forward(const snn_units_args &a, void *saved, char *ws, hipStream_t st) {

@@ -9,6 +9,7 @@
 // some 200 MB.  (One workgroup of 1024 threads that holds 64 values a thread needs no second reading, but fills and empties a compute
 // unit in turn: 1024 steps of 8 x 2048 channels, 32 groups, bf16: forward 24.7 us against 22.7, reverse 226, out of registers, against 40.)
 // Sums over rows (dw, db) leave a row per chunk or workgroup, which a last launch adds up, or workgroups of the second one.
+#include "block_rules.hpp"
 #include "rows.hpp"
 
 #include <algorithm>
@@ -559,8 +560,6 @@ template <typename T, int VEC> __global__ __launch_bounds__(256) void norm_colum
 }
 
 // ---------------------------------------------------------------- chunks of a sequence
-constexpr int AHEAD = 4, AHEAD_BWD = 2;      // rows in flight a thread (reverse: of x and dy each)
-
 // A thread's column block k and its rows r0 + rsub + r rp, r < there, of which the first `live` exist in their sequence.
 template <typename T, int VEC> struct Run {
   int unit, g, chunk, col, len, live, there, rp;
@@ -853,75 +852,6 @@ int norm_check(const snn_norm_args *a, bool grads) {
   return SNN_OK;
 }
 
-// How a call is cut, for `vec` channels a vector.
-struct NormCut {
-  int nt, tpr_log2, K, R, loops, blocks;       // threads; threads a row (log2); column blocks; rows a thread; lots; workgroups a unit and group
-  bool chunks;
-  int long_row;                                // vectors a lane where a wavefront has a row (or AGAIN_ROW), 0: otherwise
-};
-constexpr int AGAIN_ROW = -1;
-NormCut norm_cut(const snn_norm_args &a, int vec, bool backward) {
-  const size_t z = a.type == SNN_TYPE_FP32 ? 4 : 2;
-  const int C = a.D / a.groups, slots = vec * z == 16 ? 8 : 16;
-  const int64_t rows = a.per_step ? (int64_t)a.T * a.B : a.T, units = a.per_step ? 1 : a.B;
-  NormCut c;
-  auto blocks_of = [&](int64_t each) { return std::max<int64_t>(1, (rows + each - 1) / each); };
-  c.nt = 256;
-  c.tpr_log2 = 0;
-  while ((vec << c.tpr_log2) < C && (1 << c.tpr_log2) < c.nt) ++c.tpr_log2;
-  c.K = (C + (vec << c.tpr_log2) - 1) / (vec << c.tpr_log2);
-  c.loops = 1;
-  c.chunks = false;
-  c.long_row = 0;
-  if (a.per_step && C > 64 * vec) {
-    const int need = (C + 64 * vec - 1) / (64 * vec);
-    const int most = vec <= 2 ? 64 / vec : 16;
-    // Reverse no more than 4 vectors, as x and dy and what is formed of them fill the registers.  (us, held and loaded again: 8192 rows of
-    // 4096, fp32, forward 45 and 79, reverse 175 and 163; 4800 of 4095, 43 and 62, 216 and 122; 4096 of 4096, bf16, 18.7 and 18.9, 62 and 49.)
-    c.long_row = need <= 4 ? 4 : backward ? AGAIN_ROW : need <= 16 ? 16 : need <= most ? most : AGAIN_ROW;
-    const int64_t across = (a.D + 64 * vec - 1) / (64 * vec);
-    c.R = 256;                                 // rows of a chunk of dw and db, in workgroups of 64 vectors of columns
-    while (c.R > 16 && blocks_of(c.R) * across < 1024) c.R /= 2;
-    while (blocks_of(c.R) > 32768) c.R *= 2;
-    c.blocks = (int)blocks_of(c.R);
-    return c;
-  }
-  if (a.per_step) {
-    const int64_t rp = c.nt >> c.tpr_log2;
-    c.R = blocks_of(rp * 2) * a.groups >= 512 ? 2 : 1;
-    const int64_t n = blocks_of(rp * c.R);
-    while (c.loops < 64 && blocks_of(rp * c.R * c.loops * 2) * a.groups >= 2048) c.loops *= 2;
-    c.blocks = (int)((n + c.loops - 1) / c.loops);
-    return c;
-  }
-  c.R = slots;
-  c.blocks = 1;
-  // A sequence's group at once, where the registers of 256 threads hold it, or those of 512 and there are 64 groups at least; reverse with
-  // 16-byte vectors never, since x and dy with what is formed of them do not
-  // fit.  (us of a forward and a reverse call: 51 of 257 steps, 130 channels in 5 groups, fp32, 7.8 and 16.1, in chunks 12.6 and 18.6; 16 of
-  // 500 steps, 512 channels in 8, bf16, reverse at once 41.8, in chunks 22.2.)
-  if (c.K == 1 && !(backward && vec * z == 16)) {
-    if (blocks_of((256 >> c.tpr_log2) * slots) == 1) return c;
-    if (units * a.groups >= 64 && blocks_of((512 >> c.tpr_log2) * slots) == 1) {
-      c.nt = 512;
-      return c;
-    }
-  }
-  const int64_t rp = 256 >> c.tpr_log2;
-  c.chunks = true;
-  c.R = 64;                                    // rows a thread: as many as leave 512 workgroups (1024: 2 to 25 % slower)
-  while (c.R > AHEAD && blocks_of(rp * c.R) * units * a.groups < 512) c.R /= 2;
-  c.blocks = (int)blocks_of(rp * c.R);
-  return c;
-}
-int norm_vector(const snn_norm_args &a, const snn_norm_grads *g) {
-  const size_t z = a.type == SNN_TYPE_FP32 ? 4 : 2;
-  for (int vec : {(int)(16 / z), 2}) {
-    auto take = [&](const snn_rows &r) { return rows_take(r, a.T, a.B, vec, z); };
-    if (a.D / a.groups % vec == 0 && take(a.x) && (g ? take(g->dy) && take(g->dx) : take(a.y))) return vec;
-  }
-  return 1;
-}
 // The workspace does not depend on the pointers, which decide how many channels a vector has.
 size_t part_bytes(const snn_norm_args &a, const NormCut &c) { return c.chunks ? rup256((size_t)a.B * a.groups * c.blocks * 8) : 0; }
 size_t norm_bytes(const snn_norm_args &a, bool backward) {

@@ -12,6 +12,7 @@
 // Measured, bfloat16, 1024 steps of 8 x 2048 channels: forward 33 us (134 MB, 4.1 TB/s; the same accesses without arithmetic take 23), reverse 55
 // (242 MB, 4.4 TB/s).  What bounds it are the vector units, 42 and 71 operations an element of which six are transcendental at half
 // rate, three quarters of the time; in the rest all wavefronts of a compute unit's one workgroup load, join or store.
+#include "block_rules.hpp"
 #include "rows.hpp"
 
 #include <algorithm>
@@ -20,8 +21,6 @@
 namespace snn {
 namespace {
 
-constexpr int STEPS = 8;                     // a run; the state before every run is what `saved` holds
-constexpr int CH = 64;                       // channels of a workgroup
 constexpr float LN2 = 0.6931471805599453f;
 
 struct RecP {
@@ -485,37 +484,8 @@ int recurrence_check(const snn_recurrence_args *a, bool step, bool grads) {
 }
 bool strides_fit(const snn_rows &r, int T, size_t z) { return T <= 1 || !r.p || (r.stride_t >= 0 && r.stride_t < (int64_t)((1 << 30) / (STEPS * z))); }
 
-size_t type_bytes(int32_t type) { return type == SNN_TYPE_FP32 ? 4 : 2; }
-
-// How time is cut: `waves` wavefronts a workgroup and segments of `tiles` tiles.  Segments cost a second reading, and are taken where
-// there are fewer (sequence, 64 channels) than workgroups that keep the chip busy: us of a forward (reverse) call in one piece and cut,
-// bf16 but for the second: 128 of 1024 steps 28.5 and 31.3 (55 and 45), 153 of 333 steps, fp32, 18.3 and 23.5 (30 and 35), 180 of
-// 200 steps 9.4 and 14.0 (21 and 25).  As many as make 1024 workgroups, reverse 512 (16 of 8192 steps: 36 and 39, reverse 51 and 45).
-struct RecCut {
-  int waves, tiles, nseg;
-};
-RecCut recurrence_cut(const snn_recurrence_args &a, int vec, bool backward) {
-  RecCut c;
-  const int64_t groups = (int64_t)(a.D + CH - 1) / CH * a.B;
-  const bool enough = groups >= (backward ? 144 : 128);
-  c.waves = !enough || a.T <= 64 ? 4 : backward ? 8 : 16;
-  const int tile = c.waves * vec * STEPS;                  // (Shape::TILE)
-  const int all = std::max(1, (int)(((int64_t)a.T + tile - 1) / tile));
-  const int64_t want = enough ? 1 : std::min<int64_t>(64, ((backward ? 512 : 1024) + groups - 1) / groups);
-  c.tiles = (int)((all + want - 1) / want);
-  c.nseg = (all + c.tiles - 1) / c.tiles;
-  return c;
-}
 // The workspace does not depend on the pointers, which decide between one channel a lane and two.
 int most_segments(const snn_recurrence_args &a, bool backward) { return std::max(recurrence_cut(a, 1, backward).nseg, recurrence_cut(a, 2, backward).nseg); }
-
-// Four bytes a lane: of bfloat16 two channels where rows allow it, of fp32 one (1024 steps of 8 x 2048 channels, two and one: 47.8 and 44.2 us,
-// reverse 102 and 96).
-bool two_channels(const snn_recurrence_args &a, const snn_recurrence_grads *g) {
-  const size_t z = type_bytes(a.type);
-  auto take = [&](const snn_rows &r) { return rows_take(r, a.T, a.B, 2, z); };
-  return a.type == SNN_TYPE_BF16 && a.D % 2 == 0 && take(a.x) && take(a.i) && take(a.r) && (g ? take(g->dy) && take(g->dx) && take(g->di) && take(g->dr) : take(a.y));
-}
 
 template <typename T, int VEC, int WAVES> int launch_forward(RecP p, hipStream_t st) {
   const int64_t each = (int64_t)p.groups * p.B;

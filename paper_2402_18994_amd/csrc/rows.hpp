@@ -34,9 +34,4 @@ __device__ __forceinline__ float add_32_apart(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Whether the rows of a tensor of T steps of B sequences can be taken `vec` elements of `size` bytes at a time.
-inline bool rows_take(const snn_rows &r, int T, int B, int vec, size_t size) {
-  return !r.p || (aligned(r.p, vec * size) && (T <= 1 || r.stride_t % vec == 0) && (B <= 1 || r.stride_b % vec == 0));
-}
-
 }  // namespace snn

@@ -5,7 +5,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
-#include "../../include/snn_ops.h"
+#include "ops_host.hpp"
 
 namespace snn {
 
@@ -16,9 +16,6 @@ inline int ops_launched(const char *what) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SNN_OK : ops_fail(SNN_ERR_HIP, "%s: launch failed: %s", what, hipGetErrorString(e));
 }
-
-inline bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-inline size_t rup256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // A tensor over time in a kernel's arguments.
 template <typename T> struct Rows {
