@@ -50,7 +50,7 @@ __device__ __forceinline__ float gate_of(float v, float &rest) {
 }
 // log2 of what a wholly open gate leaves; finite, so that a shut one (times zero) holds the state whatever `decay` is.
 __device__ __forceinline__ float rate_of(float sharpness, float decay) {
-  const float v = -sharpness * LOG2E * softplus(decay);
+  const float v = -sharpness * (LOG2E * softplus(decay));  // (sharpness LOG2E may be infinite, which times no decay is no number)
   return v < -0x1p127f ? -0x1p127f : v;
 }
 

@@ -129,3 +129,22 @@ def test_units_gradients_of_no_steps():
     g = gated_units_backward(o.y, o.saved, x, gate, up)
     for v in (g.dgate, g.dup):
         assert not v.view(torch.int64).any()
+
+
+@pytest.mark.parametrize("T", (1, 20, 200))
+def test_recurrence_of_the_largest_sharpness(T):
+    """3e38 is a finite number: channels with a decay of -inf keep their state for good, those with any other forget at once, y = sigmoid(i) x."""
+    from paper_2402_18994_amd import gated_recurrence, gated_recurrence_backward, gated_recurrence_step
+    B, D = 2, 70
+    gen = torch.Generator().manual_seed(T)
+    x, i, r, init = (rounded(rand(gen, *s)) for s in ((T, B, D), (T, B, D), (T, B, D), (B, D)))
+    decay = torch.where(torch.arange(D) % 2 == 0, float("-inf"), 0.0).float().cuda()
+    args = [on_gpu(v) for v in (x, i, r)]
+    want = torch.where(torch.arange(D) % 2 == 0, init, x / (1 + torch.exp(-i)))
+    o = gated_recurrence(*args, decay, sharpness=3e38, init=on_gpu(init), save=True)
+    close("y", o.y, want, 1, 2.0 ** -24)
+    g = gated_recurrence_backward(torch.ones_like(args[0]), o.saved, *args, decay, sharpness=3e38, init=on_gpu(init))
+    assert all(torch.isfinite(v).all() for v in g)
+    assert torch.equal(g.dinit.cpu(), torch.where(torch.arange(D) % 2 == 0, float(T), 0.0).expand(B, D))
+    state = on_gpu(init)
+    close("step", gated_recurrence_step(*(v[0] for v in args), state, decay, sharpness=3e38), want[0], 1, 2.0 ** -24)
