@@ -133,9 +133,11 @@ int32_t snn_scan_step(const snn_scan_args *a, void *hip_stream);
 
 /* ------------------------------------------------------------------ gated linear recurrence */
 /* One state a channel.  The state's variance stays that of the gated input: what the leak takes, sqrt(1 - a^2) gives.
- * D above 2^22, B times the number of 64-channel blocks from 2^22 on, and strides between steps that are negative or put eight steps
- * 1 GiB apart are refused (SNN_ERR_ARG).  decay = -inf keeps a state for good, and so does a step
- * with r = -inf (a gate below the least normal number is shut, whatever decay is); where a = 1 the gradient of r is its limit, zero. */
+ * D above 2^22, B times the number of 64-channel blocks from 2^22 on, T above 2^30, and strides between steps that are negative or put eight
+ * steps 1 GiB apart are refused (SNN_ERR_ARG).  decay = -inf keeps a state for good, and so does a step
+ * with r = -inf (a gate below the least normal number is shut, whatever decay is); where a = 1 the gradient of r is its limit, zero.
+ * Infinities and NaN in steps that exist stay in their sequence and channel and in the sum over them; where the definition makes an infinity,
+ * that or NaN comes out (runs of steps are joined by the product of their a, which may be zero where no a is). */
 typedef struct {
   int32_t T, B, D;
   int32_t type;
@@ -168,8 +170,10 @@ int32_t snn_recurrence_step(const snn_recurrence_args *a, void *hip_stream);
 /* ------------------------------------------------------------------ group norm */
 /* Channels d with the same d / (D / groups) form a group.  Statistics run over the group's channels and, unless per_step is
  * set, over the steps of the sequence that exist.  One step at a time (a stream) is a call with per_step, T = 1.  The variance is that
- * of the values themselves (divided by their number).  Refused (SNN_ERR_ARG): groups of more than 16384 channels, D above 2^22, T * B from
- * 2^31, T * B * groups from 2^31. */
+ * of the values themselves (divided by their number).  Statistics are fp32 numbers: a group whose values sum up beyond fp32 may give NaN, one
+ * whose squared deviations do the outputs of a deviation of zero, and with eps = 0 deviations below 2^-75 are none (a variance of zero without
+ * an eps gives NaN).  A NaN or an infinity makes its whole group NaN, no other.  Refused (SNN_ERR_ARG): groups of more than 16384 channels, D
+ * above 2^22, T * B from 2^31, T * B * groups and B * groups from 2^31. */
 typedef struct {
   int32_t T, B, D;
   int32_t groups;            /* divides D */
@@ -199,7 +203,10 @@ int32_t snn_norm_backward(const snn_norm_args *a, const snn_norm_grads *g, const
 typedef enum { SNN_ACT_SILU = 0, SNN_ACT_GELU = 1 } snn_act;    /* GELU: v (1 + erf(v / sqrt(2))) / 2 */
 
 /* The matrices have a row for each unit (what a unit reads lies together) and are of the streamed type, as are their gradients; sums
- * are fp32, and fp32 operands of more than 256 rows enter the products as three bfloat16 pieces (all 24 bits, to multiples of 2^-133).
+ * are fp32, and fp32 operands of more than 256 rows, in the reverse pass of any, enter the products as three bfloat16 pieces (all 24 bits, to
+ * multiples of 2^-133).  In the reverse pass the gradients of both products are rounded to the streamed type before they are multiplied again: in
+ * bfloat16 each term of dx, dgate and dup is off by up to 2^-8 of itself before the sum is rounded (together 2.3e-3 of their norm, of which
+ * rounding the sums alone is 1.7e-3).
  * Rows of steps that do not exist take no part, whatever they hold.  An infinity or NaN in x stays in its row of y and dx; where the
  * definition makes an infinity, that or NaN comes out (an infinity's pieces meet zeros).  One step of every sequence is a call with
  * T = 1.  Refused (SNN_ERR_ARG): D or F above 2^18, T * B above 2^28. */
@@ -220,7 +227,8 @@ typedef struct {
 } snn_units_grads;
 
 /* `saved` (may be NULL in a forward call): what both products came to, fp32; 16-byte aligned, as the workspaces are.  The workspace is
- * that of a call with these very arguments: strides and alignments decide what has to be laid out anew. */
+ * that of a call with these very arguments: strides and alignments decide what has to be laid out anew.  Bytes a value of y: `saved` 8; workspace of the
+ * reverse pass 8 in bfloat16 and 24 in fp32, and the layouts of x, gate and up beside them (8192 rows, 2048 -> 4096: 0.34 and 1.0 GB). */
 int32_t snn_units_workspace_bytes(const snn_units_args *a, int32_t backward, size_t *bytes);
 int32_t snn_units_saved_bytes(const snn_units_args *a, size_t *bytes);
 int32_t snn_units_forward(const snn_units_args *a, void *saved, void *workspace, size_t workspace_bytes, void *hip_stream);

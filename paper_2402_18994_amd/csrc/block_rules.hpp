@@ -87,9 +87,12 @@ constexpr int STEPS = 8;                     // a run; the state before every ru
 constexpr int CH = 64;                       // channels of a workgroup
 
 // How time is cut: `waves` wavefronts a workgroup and segments of `tiles` tiles.  Segments cost a second reading, and are taken where
-// there are fewer (sequence, 64 channels) than workgroups that keep the chip busy: us of a forward (reverse) call in one piece and cut,
-// bf16 but for the second: 128 of 1024 steps 28.5 and 31.3 (55 and 45), 153 of 333 steps, fp32, 18.3 and 23.5 (30 and 35), 180 of
-// 200 steps 9.4 and 14.0 (21 and 25).  As many as make 1024 workgroups, reverse 512 (16 of 8192 steps: 36 and 39, reverse 51 and 45).
+// there are fewer (sequence, 64 channels) than workgroups that keep the chip busy: us of a forward (reverse) call in one piece and cut, by
+// their number and steps, bf16: 64 of 1024 27 and 18 (52 and 28), of 4096 101 and 55 (185 and 71); 128 of 1024 29 and 32 (54 and 43), of 4096 103 and 95
+// (201 and 141); 140 of 8192 217 and 248 (396 and 356); 153 of 333 15.5 and 18.4 (27 and 29); 180 of 200 11.7 and 16.9 (22 and 29).  fp32: 128 of
+// 4096 150 and 212 (299 and 259), 153 of 333 15.2 and 20.1 (30 and 29), 180 of 200 13.3 and 18.7 (26 and 28).  The number of steps is not looked at:
+// few and short ones (64 of 128: 11.5 and 16.7, reverse 19 and 23) would be faster in one piece.  As many segments as make 1024 workgroups, reverse 512
+// (16 of 8192 steps, bf16, with 1024 and with 512: 36 and 37, reverse 51 and 42).
 struct RecCut {
   int waves, tiles, nseg;
 };

@@ -148,3 +148,16 @@ def test_recurrence_of_the_largest_sharpness(T):
     assert torch.equal(g.dinit.cpu(), torch.where(torch.arange(D) % 2 == 0, float(T), 0.0).expand(B, D))
     state = on_gpu(init)
     close("step", gated_recurrence_step(*(v[0] for v in args), state, decay, sharpness=3e38), want[0], 1, 2.0 ** -24)
+
+
+@pytest.mark.parametrize("T,C,per_step", ((8, 64, False), (900, 64, False), (8, 64, True), (8, 1024, True)))
+def test_group_norm_of_a_variance_beyond_fp32(T, C, per_step):
+    """Values of +-1e20, whose squares are no fp32 numbers, give the outputs of a deviation of zero, as the header says, and finite gradients."""
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    gen = torch.Generator().manual_seed(C)
+    bias = rounded(rand(gen, 2 * C))
+    x = on_gpu((1e20 - 2e20 * (torch.arange(2 * C) % 2)).expand(T, 3, 2 * C).contiguous())
+    o = group_norm(x, 2, bias=on_gpu(bias), per_step=per_step, save=True)
+    close("y", o.y, (bias / (1 + torch.exp(-bias))).expand(T, 3, 2 * C), 1, 2.0 ** -24)
+    g = group_norm_backward(torch.ones_like(x), o.saved, x, 2, bias=on_gpu(bias), per_step=per_step)
+    assert torch.isfinite(g.dx).all() and torch.isfinite(g.dbias).all()
