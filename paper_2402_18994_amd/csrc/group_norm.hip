@@ -80,6 +80,13 @@ template <typename T, int VEC, int MODE> struct Slots {
   static constexpr int N = MODE == STEP ? 2 : sizeof(T) * VEC == 16 ? 8 : 16;
 };
 
+// sum / n with `inverse` = 1 / n, brought to the nearest number by its remainder: the rounding of 1 / n alone would give equal values a mean
+// that is not their value, and deviations that without much of an eps are all there is.
+__device__ __forceinline__ float mean_of(float sum, float n, float inverse) {
+  const float m = sum * inverse;
+  return fmaf(fmaf(-m, n, sum), inverse, m);
+}
+
 // 1 / sqrt(v).  The hardware's root takes what is below the least normal number, a variance without an eps may be, for zero.
 __device__ __forceinline__ float rstd_of(float v) {
   const bool small = v < 0x1p-126f;
@@ -225,7 +232,7 @@ __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
       x[s] = fetch<T, VEC>(w, a.x, s, live[s]);
     }
     float mean[SLOTS], rstd[SLOTS];                          // (WHOLE: the same in all)
-    const float n = MODE == STEP ? 1.f / (float)a.C : 1.f / fmaxf((float)((int64_t)w.len * a.C), 1.f);
+    const float count = MODE == STEP ? (float)a.C : fmaxf((float)((int64_t)w.len * a.C), 1.f), n = 1.f / count;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
       mean[s] = 0.f;
@@ -235,7 +242,7 @@ __global__ __launch_bounds__(NT) void norm_forward_kernel(const NormP a) {
     sums_of<NT, SLOTS, MODE>(a, mean, lds[0]);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
-      mean[s] *= n;
+      mean[s] = mean_of(mean[s], count, n);
       rstd[s] = 0.f;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
@@ -417,7 +424,7 @@ template <typename T, int VEC, int KB, bool AGAIN> __global__ __launch_bounds__(
       for (int v = 0; v < VEC; ++v) mean += w.channel(s) < a.C ? widen(x[s].v[v]) : 0.f;
     }
   });
-  mean = wave_sum(mean, 6) * n;
+  mean = mean_of(wave_sum(mean, 6), (float)a.C, n);
   over_row([&] {
 #pragma unroll
     for (int s = 0; s < KB; ++s) {

@@ -161,3 +161,19 @@ def test_group_norm_of_a_variance_beyond_fp32(T, C, per_step):
     close("y", o.y, (bias / (1 + torch.exp(-bias))).expand(T, 3, 2 * C), 1, 2.0 ** -24)
     g = group_norm_backward(torch.ones_like(x), o.saved, x, 2, bias=on_gpu(bias), per_step=per_step)
     assert torch.isfinite(g.dx).all() and torch.isfinite(g.dbias).all()
+
+
+@pytest.mark.parametrize("T,C,per_step", ((7, 40, False), (300, 30, False), (7, 24, True), (5, 100, True), (5, 650, True), (5, 1000, True), (5, 5000, True)))
+@pytest.mark.parametrize("type", tuple(TYPES))
+def test_group_norm_of_equal_values_whatever_their_number(T, C, per_step, type):
+    """Numbers of values that are no powers of two: the mean of equal ones, whose sum is exact, is their value all the same, and the outputs are the activation of the
+    bias.  (Rows of more than 512 channels are a wavefront's, which holds them or loads them again; 40 sequences of 300 steps go through wide workgroups.)"""
+    from paper_2402_18994_amd import group_norm, group_norm_backward
+    gen = torch.Generator().manual_seed(C)
+    B, t = 40 if T == 300 else 3, TYPES[type]
+    bias = rounded(rand(gen, 2 * C))
+    x = on_gpu(torch.tensor([3000.0, -11.0]).repeat_interleave(C).expand(T, B, 2 * C).contiguous(), t)
+    o = group_norm(x, 2, bias=on_gpu(bias), per_step=per_step, save=True)
+    close("y", o.y, (bias / (1 + torch.exp(-bias))).expand(T, B, 2 * C), 1, half_step(t))
+    g = group_norm_backward(torch.ones_like(x), o.saved, x, 2, on_gpu(torch.ones(2 * C)), on_gpu(bias), per_step=per_step)
+    assert (g.dweight == 0).all()
